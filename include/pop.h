@@ -24,6 +24,7 @@
 #ifndef POP_H_
 #define POP_H_
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -300,6 +301,100 @@ int pop_decode_step(pop_partition_t* p, const void* x, int B, int k_candidate,
 int pop_prefill_scores_noalloc(const void* X, int L, int d,
                                const void* Wg, const void* Wu, const void* Wd, int N,
                                pop_dtype_t dtype, double* scores_out, void* cuda_stream);
+
+/*
+ * ---- A paged key / value cache held in 4 bits, and the attention that reads it -----------------------------------
+ * (The paper leaves attention as it is, Sec. 4.4; these entry points are for the library's users: once the FFN is
+ * pruned, the cache is the next thing a decoder streams for every token.)
+ *
+ * Format.  The cache of one layer is a device array pages[n_pages][n_kv_heads][page_size / 16] of tiles; a tile holds
+ * 16 consecutive tokens of one head.  For every group of 64 head dimensions (G = head_dim / 64 of them) a tile has 512
+ * bytes of key codes, then the value codes alike, then the parameters: POP_KV_TILE_BYTES(head_dim) bytes in all, which
+ * is 4.5 bits per element.
+ *   codes       32-bit words of 8 consecutive dimensions (e8 = dim % 64 / 8); the code of dimension j of the 8 sits at
+ *               bit 4 (j / 2) + 16 (j % 2).  Token t (0..15) of the tile has its key word e8 at word
+ *               16 (t % 8) + 4 (e8 / 2) + 2 (t / 8) + e8 % 2 of the group's 128 words, and its value word at
+ *               16 e8 + 4 (t % 8 / 2) + 2 (t / 8) + t % 2.
+ *   parameters  per token G pairs (scale, zero) of fp16 for the keys, then G for the values.
+ * A code c stands for scale * c + zero.  Of a group's 64 values x: zero = fp16(min), scale = fp16((max - min) * (1/15)),
+ * c = round((x - zero) * (1 / scale)) clamped to 0..15, each operation in fp32 (round to nearest, ties to even); a NaN
+ * counts as 0 and values beyond +-65504 as +-65504, so that what the cache holds is always finite.
+ * A slot is the place of one token: page * page_size + offset in the page.
+ *
+ * Restrictions: head_dim 64 or 128; page_size a multiple of 16 up to 1024; pages 16-byte aligned; at most
+ * POP_KV_MAX_REQUESTS requests in a call (POP_ERR_UNSUPPORTED otherwise).
+ */
+#define POP_KV_TILE              16
+#define POP_KV_GROUP             64
+#define POP_KV_MAX_REQUESTS    4096
+#define POP_KV_TILE_BYTES(head_dim) ((head_dim) / POP_KV_GROUP * (2 * 512 + POP_KV_TILE * 8))
+
+/* One layer's cache: caller-owned device memory of n_pages * pop_kv_page_bytes(); its contents need no initialisation. */
+typedef struct {
+    void* pages;
+    int n_pages, page_size, n_kv_heads, head_dim;
+} pop_kv_cache_t;
+
+/* Bytes of one page (host only). */
+int pop_kv_page_bytes(int page_size, int n_kv_heads, int head_dim, size_t* bytes);
+
+/*
+ * One step's block table and slot map from the lengths of its requests, entirely on the device.
+ *   ctx_lens [n_requests]   tokens request r has in the cache; new_lens [n_requests]: tokens it gets in this step (>= 0),
+ *                           or a negative number if it has finished.
+ *   block_table [n_requests][max_blocks]  page ids; the first ceil(ctx / page_size) of a row are valid.  In and out.
+ *   ring [n_pages], state {head, count}   the free pages: ring[(head + i) % n_pages], i < count.
+ * Row r gets pages for its blocks ceil(ctx / page_size) .. ceil((ctx + new) / page_size) - 1, taken from the ring's head in
+ * order of (request, block).  The pages of finished requests are put at the ring's tail in the same order (free from the
+ * next call on; their rows stay as they are).  state_out receives the new head and count and may be the same array as state_in.
+ * Outputs: q_indptr [n_requests + 1], the prefix sums of max(new, 0); kv_lens [n_requests] = ctx + new (0 if finished);
+ * for each of the n_tokens new tokens, in request order, its slot and its position in its request (both -1 past the last
+ * token; n_tokens is the capacity of the two arrays, tokens beyond it are not listed); info {new tokens, pages that
+ * were wanted and not given}.  A page is not given when the ring is empty or the row has max_blocks pages: its block table
+ * entry (if there is one) and its tokens' slots are -1, which the calls below leave out.
+ * All arrays device, int32 but for slots (int64); positions and info may be NULL.  The sums of ctx + new and of the pages
+ * stay below 2^31.
+ */
+int pop_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int n_requests, int page_size,
+                int32_t* ring, int n_pages, const int32_t* state_in, int32_t* state_out,
+                int32_t* block_table, int max_blocks, int n_tokens,
+                int32_t* q_indptr, int32_t* kv_lens, int64_t* slots, int32_t* positions, int32_t* info,
+                void* cuda_stream);
+
+/*
+ * Quantises n_tokens keys and values and writes them to their slots.  k, v: device arrays of `dtype`, token t's heads at
+ * k + t * k_stride, [n_kv_heads][head_dim] contiguous (strides in elements, so that k and v may be slices of a fused
+ * projection); 16-byte aligned, strides a multiple of 16 bytes.  slots: device int64; a slot outside the cache (-1) is
+ * skipped.  Two tokens of a call must not have the same slot.
+ */
+int pop_kv_append(const pop_kv_cache_t* cache, const void* k, long long k_stride, const void* v, long long v_stride,
+                  pop_dtype_t dtype, const int64_t* slots, int n_tokens, void* cuda_stream);
+
+/* The values that the given slots stand for: k, v [n_tokens][n_kv_heads][head_dim] of `dtype`, contiguous; zeros for a slot
+ * outside the cache.  For moving a cached prefix to a cache of another kind, or looking at what was kept of it. */
+int pop_kv_read(const pop_kv_cache_t* cache, const int64_t* slots, int n_tokens, pop_dtype_t dtype, void* k, void* v,
+                void* cuda_stream);
+
+/*
+ * Attention of each request's queries over its part of the cache (its new keys appended already).
+ *   q: device array of `dtype`, query token t's heads at q + t * q_stride, [n_heads][head_dim] contiguous; n_heads a multiple
+ *   of cache->n_kv_heads, query head h reads kv head h / (n_heads / n_kv_heads).  Request r's queries are the tokens
+ *   q_indptr[r] .. q_indptr[r + 1] - 1 (n of them; none, one, or many), and its keys the first kv_lens[r] tokens of block
+ *   table row r.  Query i of n stands at position p = kv_len - n + i and sees the keys j
+ *       j < kv_len,   and j <= p if causal,   and j > p - window if window > 0.
+ *   out [n_tokens][n_heads][head_dim] of `dtype`:  out = sum_j softmax_j(scale * q . k_j) v_j over the keys it sees; a query that
+ *   sees none gets zeros.  lse [n_tokens][n_heads] fp32 (or NULL): log of the sum of exp(scale * q . k_j), -inf if none.
+ * Tokens past q_indptr[n_requests] are not written.  Keys on a page that the table does not have (an id outside
+ * 0 .. n_pages - 1) are not seen.  kv_lens[r] <= max_blocks * page_size (more is cut to that).
+ * Products, softmax statistics and sums are kept in fp32.  Equal calls give equal results, bit for bit.
+ * workspace: device memory of pop_kv_attention_workspace() bytes, zeroed once before its first use; it serves one stream
+ * at a time.  Allocates nothing; may be captured into a CUDA graph.
+ */
+int pop_kv_attention_workspace(size_t* bytes);
+int pop_kv_attention(const pop_kv_cache_t* cache, const void* q, long long q_stride, pop_dtype_t dtype, int n_heads,
+                     int n_tokens, const int32_t* q_indptr, const int32_t* kv_lens, int n_requests,
+                     const int32_t* block_table, int max_blocks, float scale, int causal, int window,
+                     void* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 #ifdef __cplusplus
 }

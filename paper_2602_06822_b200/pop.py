@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import numpy as np
 
@@ -21,6 +21,7 @@ POP_ERR_TIMEOUT = -5
 POP_MAX_BATCH = 8
 POP_F32, POP_BF16 = 0, 1
 POP_NOALLOC_MAX_N = 32768
+POP_KV_TILE, POP_KV_GROUP, POP_KV_MAX_REQUESTS = 16, 64, 4096
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libpop.so")
 
@@ -32,6 +33,11 @@ class Ratios(C.Structure):
 class Config(C.Structure):
     _fields_ = [("decode_kernel", C.c_int), ("launch_mode", C.c_int), ("wait_budget_us", C.c_uint),
                 ("slab_cache_bytes", C.c_ulonglong)]
+
+
+class KVCacheDesc(C.Structure):
+    """pop_kv_cache_t"""
+    _fields_ = [("pages", C.c_void_p), ("n_pages", C.c_int), ("page_size", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int)]
 
 
 POP_DECODE_AUTO, POP_DECODE_FUSED, POP_DECODE_SIMPLE = 0, 1, 2
@@ -79,6 +85,13 @@ SIGNATURES = {
     "pop_partition_destroy": (C.c_int, [_P]),
     "pop_decode_step": (C.c_int, [_P, _P, C.c_int, C.c_int, _P, _P, _P, _P]),
     "pop_prefill_scores_noalloc": (C.c_int, [_P, C.c_int, C.c_int, _P, _P, _P, C.c_int, C.c_int, _P, _P]),
+    "pop_kv_page_bytes": (C.c_int, [C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
+    "pop_kv_plan": (C.c_int, [_P, _P, C.c_int, C.c_int, _P, C.c_int, _P, _P, _P, C.c_int, C.c_int, _P, _P, _P, _P, _P, _P]),
+    "pop_kv_append": (C.c_int, [C.POINTER(KVCacheDesc), _P, C.c_longlong, _P, C.c_longlong, C.c_int, _P, C.c_int, _P]),
+    "pop_kv_read": (C.c_int, [C.POINTER(KVCacheDesc), _P, C.c_int, C.c_int, _P, _P, _P]),
+    "pop_kv_attention_workspace": (C.c_int, [C.POINTER(C.c_size_t)]),
+    "pop_kv_attention": (C.c_int, [C.POINTER(KVCacheDesc), _P, C.c_longlong, C.c_int, C.c_int, C.c_int, _P, _P, C.c_int, _P, C.c_int,
+                                   C.c_float, C.c_int, C.c_int, _P, _P, _P, C.c_size_t, _P]),
 }
 
 
@@ -383,4 +396,178 @@ def prefill_scores_noalloc(X, Wg, Wu, Wd, out, stream=None):
     _check(lib().pop_prefill_scores_noalloc(X.data_ptr(), L, d, Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), N,
                                             _dtype_code(X), out.data_ptr(), _stream_ptr(stream)),
            "pop_prefill_scores_noalloc")
+    return out
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# The paged 4-bit key / value cache (pop_kv_*).  Tensors of one call are on one device, which is the current one.
+# ---------------------------------------------------------------------------------------------------------------------
+
+def kv_page_bytes(page_size: int, n_kv_heads: int, head_dim: int) -> int:
+    """Bytes of one page of one layer - host only."""
+    out = C.c_size_t()
+    _check(lib().pop_kv_page_bytes(page_size, n_kv_heads, head_dim, C.byref(out)), "pop_kv_page_bytes")
+    return out.value
+
+
+def kv_pages(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, device="cuda"):
+    """Uninitialised memory for one layer's cache: uint8 [n_pages, n_kv_heads, page_size / 16, tile bytes], the tensor that
+    the calls below take as ``pages``."""
+    per_tile = kv_page_bytes(POP_KV_TILE, 1, head_dim)
+    kv_page_bytes(page_size, n_kv_heads, head_dim)
+    return _torch().empty(n_pages, n_kv_heads, page_size // POP_KV_TILE, per_tile, dtype=_torch().uint8, device=device)
+
+
+def _kv_desc(pages) -> KVCacheDesc:
+    if pages.dim() != 4 or not pages.is_cuda or not pages.is_contiguous() or pages.element_size() != 1:
+        raise ValueError("pages must be a contiguous uint8 CUDA tensor as kv_pages() makes it")
+    n, h, tiles, nbytes = pages.shape
+    per_group = 2 * 512 + POP_KV_TILE * 8
+    if nbytes % per_group:
+        raise ValueError("pages must be a contiguous uint8 CUDA tensor as kv_pages() makes it")
+    return KVCacheDesc(pages.data_ptr(), n, tiles * POP_KV_TILE, h, nbytes // per_group * POP_KV_GROUP)
+
+
+def _same_device(dev, *tensors):
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError("all tensors of a call must be on one CUDA device")
+
+
+def _ints(t, dtype, what, dim=1):
+    if t.dtype != dtype or t.dim() != dim or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of {dim} dimension(s)")
+
+
+def _rows(t, heads: int, dim: int, what: str) -> int:
+    """Token stride (in elements) of [tokens, heads, dim] whose heads lie one after another."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"{what} must be [tokens, {heads}, {dim}]")
+    s = t.stride()
+    if t.shape[0] and (s[2] != 1 or (heads > 1 and s[1] != dim)):
+        raise ValueError(f"{what}: the heads of a token must be contiguous")
+    return s[0] if t.shape[0] > 1 else heads * dim
+
+
+def _used_on(stream, *tensors):
+    """Tells the caching allocator that tensors made here for the current stream are used on another one."""
+    if stream is not None and stream != _torch().cuda.current_stream():
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+class KVPlan(NamedTuple):
+    q_indptr: object      # int32 [requests + 1]
+    kv_lens: object       # int32 [requests]
+    slots: object         # int64 [tokens]
+    positions: object     # int32 [tokens]
+    state: object         # int32 [2]: head and count of the ring of free pages after this step
+    info: object          # int32 [2]: new tokens; pages wanted and not given
+
+
+def kv_plan(ctx_lens, new_lens, block_table, ring, state, page_size: int, n_tokens: int, state_out=None, stream=None) -> KVPlan:
+    """pop_kv_plan: block table (updated in place), slot map and lengths of one step.  ``state_out`` defaults to ``state``
+    (updated in place)."""
+    torch = _torch()
+    i32 = torch.int32
+    for t, w in ((ctx_lens, "ctx_lens"), (new_lens, "new_lens"), (ring, "ring"), (state, "state")):
+        _ints(t, i32, w)
+    _ints(block_table, i32, "block_table", 2)
+    if state_out is None:
+        state_out = state
+    else:
+        _ints(state_out, i32, "state_out")
+    R, dev = ctx_lens.shape[0], ctx_lens.device
+    if new_lens.shape[0] != R or block_table.shape[0] != R or state.shape[0] < 2 or state_out.shape[0] < 2:
+        raise ValueError("shape mismatch")
+    _same_device(dev, new_lens, block_table, ring, state, state_out)
+    ints = torch.empty(2 * R + 3 + n_tokens, dtype=i32, device=dev)      # one allocation for the int32 outputs
+    slots = torch.empty(n_tokens, dtype=torch.int64, device=dev)
+    at = ints.data_ptr()
+    _check(lib().pop_kv_plan(ctx_lens.data_ptr(), new_lens.data_ptr(), R, page_size, ring.data_ptr(), ring.shape[0], state.data_ptr(),
+                             state_out.data_ptr(), block_table.data_ptr(), block_table.shape[1], n_tokens, at, at + 4 * (R + 1),
+                             slots.data_ptr(), at + 4 * (2 * R + 3), at + 4 * (2 * R + 1), _stream_ptr(stream)), "pop_kv_plan")
+    _used_on(stream, ints, slots)
+    q_indptr, kv_lens, info, positions = ints.split((R + 1, R, 2, n_tokens))
+    return KVPlan(q_indptr, kv_lens, slots, positions, state_out, info)
+
+
+def kv_append(pages, k, v, slots, stream=None):
+    """pop_kv_append: k, v [T, n_kv_heads, head_dim] (token rows may be strided) quantised into the slots (int64 [T])."""
+    desc = _kv_desc(pages)
+    ks, vs = _rows(k, desc.n_kv_heads, desc.head_dim, "k"), _rows(v, desc.n_kv_heads, desc.head_dim, "v")
+    _ints(slots, _torch().int64, "slots")
+    if k.shape[0] != v.shape[0] or slots.shape[0] != k.shape[0]:
+        raise ValueError("k, v and slots must have one length")
+    if k.dtype != v.dtype:
+        raise TypeError("dtype mismatch")
+    _same_device(pages.device, k, v, slots)
+    _check(lib().pop_kv_append(C.byref(desc), k.data_ptr(), ks, v.data_ptr(), vs, _dtype_code(k), slots.data_ptr(), k.shape[0],
+                               _stream_ptr(stream)), "pop_kv_append")
+
+
+def kv_read(pages, slots, dtype, stream=None):
+    """pop_kv_read: (k, v) [T, n_kv_heads, head_dim] of ``dtype``, the values that the slots hold."""
+    torch = _torch()
+    desc = _kv_desc(pages)
+    _ints(slots, torch.int64, "slots")
+    _same_device(pages.device, slots)
+    k = torch.empty(slots.shape[0], desc.n_kv_heads, desc.head_dim, dtype=dtype, device=pages.device)
+    v = torch.empty_like(k)
+    _check(lib().pop_kv_read(C.byref(desc), slots.data_ptr(), slots.shape[0], _dtype_code(k), k.data_ptr(), v.data_ptr(),
+                             _stream_ptr(stream)), "pop_kv_read")
+    _used_on(stream, k, v)
+    return k, v
+
+
+_kv_workspaces = {}
+
+
+def _kv_workspace(device, stream_ptr: int):
+    """The attention's workspace of one (device, stream), made at its first call (outside any stream capture)."""
+    key = (device.index, stream_ptr)
+    ws = _kv_workspaces.get(key)
+    if ws is None:
+        torch = _torch()
+        n = C.c_size_t()
+        _check(lib().pop_kv_attention_workspace(C.byref(n)), "pop_kv_attention_workspace")
+        ws = torch.zeros(n.value, dtype=torch.uint8, device=device)
+        torch.cuda.current_stream(device).synchronize()                 # zeroed before any stream uses it
+        _kv_workspaces[key] = ws
+    return ws
+
+
+def kv_attention(pages, q, block_table, q_indptr, kv_lens, scale: Optional[float] = None, causal: bool = True, window: int = 0,
+                 out=None, lse_out=None, workspace=None, stream=None):
+    """pop_kv_attention: q [T, n_heads, head_dim] (token rows may be strided) over the cache -> out [T, n_heads, head_dim].
+    ``scale`` defaults to 1 / sqrt(head_dim); ``lse_out`` float32 [T, n_heads] receives the logarithms of the softmax sums.
+    ``workspace`` defaults to one kept for the stream."""
+    torch = _torch()
+    desc = _kv_desc(pages)
+    T, heads = q.shape[0], q.shape[1]
+    qs = _rows(q, heads, desc.head_dim, "q")
+    _ints(block_table, torch.int32, "block_table", 2)
+    _ints(q_indptr, torch.int32, "q_indptr")
+    _ints(kv_lens, torch.int32, "kv_lens")
+    R = kv_lens.shape[0]
+    if block_table.shape[0] != R or q_indptr.shape[0] != R + 1:
+        raise ValueError("block_table, q_indptr and kv_lens must be of one number of requests")
+    made = out is None
+    if made:
+        out = torch.empty(T, heads, desc.head_dim, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor of q's shape and dtype")
+    if lse_out is not None and (lse_out.dtype != torch.float32 or tuple(lse_out.shape) != (T, heads) or not lse_out.is_contiguous()):
+        raise ValueError("lse_out must be a contiguous float32 tensor [tokens, heads]")
+    st = _stream_ptr(stream)
+    if workspace is None:
+        workspace = _kv_workspace(q.device, st)
+    _same_device(pages.device, q, block_table, q_indptr, kv_lens, out, lse_out, workspace)
+    _check(lib().pop_kv_attention(C.byref(desc), q.data_ptr(), qs, _dtype_code(q), heads, T, q_indptr.data_ptr(), kv_lens.data_ptr(), R,
+                                  block_table.data_ptr(), block_table.shape[1], desc.head_dim ** -0.5 if scale is None else scale,
+                                  int(causal), int(window), out.data_ptr(), None if lse_out is None else lse_out.data_ptr(),
+                                  workspace.data_ptr(), workspace.numel() * workspace.element_size(), st), "pop_kv_attention")
+    if made:
+        _used_on(stream, out)
     return out

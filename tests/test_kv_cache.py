@@ -1,0 +1,572 @@
+"""The paged 4-bit key / value cache (pop_kv_plan, pop_kv_append, pop_kv_read, pop_kv_attention) against the numpy oracle.
+
+Tolerances, derived before the first run.  Plans and codes are exact.  Attention is compared with 64-bit attention over
+the values that the cache holds (so quantisation itself is no error):
+  fp32   a dot product is split into bf16 pieces whose products are exact and summed in fp32 on the tensor cores; a step of those
+         sums errs by at most 2^-21 + 2^-23 of its addends' magnitudes, D / 16 <= 8 steps, so a logit is off by at most
+         2^-18 * scale * |q|_1 * max|k| =: dS.  Probabilities then err by 2 dS relative, and everything after by as many fp32 steps
+         again on the values: |o - o_exact| <= (2 dS + 2^-17) max|v|.  In the 2-norm the signs average out: 1e-5.
+  bf16   keys and values may pass through fp16 (11 bits; the group's mid point is rounded once, the value once more): 2^-10 of
+         max|k| and max|v|, probabilities once to fp16 or a bf16 pair: 2^-11; the result is rounded to bf16: 2^-9 of itself.
+         |o - o_exact| <= (2 * 2^-10 * scale * |q|_1 * max|k| + 2^-9) max|v| + 2^-9 |o|;  in the 2-norm 2.5e-3 (the rounding to
+         bf16 alone has an rms of 1.7e-3).
+"""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import __graft_entry__ as ge
+from oracle import kv_oracle as ko
+from paper_2602_06822_b200 import pop
+
+F32, BF16 = torch.float32, torch.bfloat16
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    ge.build()
+    pop.lib()
+
+
+def i32(v):
+    return torch.tensor(np.asarray(v, dtype=np.int32), device=DEV)
+
+
+# ------------------------------------------------------------------------------------------------------------------ plan
+
+def plan_case(rng, R, page, max_ctx, max_new, finished, spare, max_blocks=None):
+    ctx = [int(x) for x in rng.integers(0, max_ctx + 1, R)]
+    new = [int(x) for x in rng.integers(0, max_new + 1, R)]
+    for r in range(R):
+        if finished and r % finished == 1:
+            new[r] = -1
+    blocks = [-(-c // page) for c in ctx]
+    need = sum(-(-(c + max(n, 0)) // page) - b for c, n, b in zip(ctx, new, blocks) if n >= 0)
+    n_pages = max(1, sum(blocks) + need + spare)
+    mb = max_blocks or max(1, max(-(-(c + max(n, 0)) // page) for c, n in zip(ctx, new)))
+    perm = rng.permutation(n_pages)
+    table = np.full((R, mb), -7, dtype=np.int32)
+    at = 0
+    for r, b in enumerate(blocks):
+        b = min(b, mb)
+        table[r, :b] = perm[at:at + b]
+        at += b
+    head = int(rng.integers(0, n_pages))
+    count = n_pages - at
+    ring = np.full(n_pages, -1, dtype=np.int32)
+    ring[(head + np.arange(count)) % n_pages] = perm[at:]
+    return ctx, new, table, ring, head, count
+
+
+def check_plan(ctx, new, table, ring, head, count, page, capacity, in_place):
+    want = ko.plan(ctx, new, table, ring, head, count, page, capacity)
+    tb, rg, state = i32(table), i32(ring), i32([head, count])
+    out = None if in_place else torch.full((2,), -1, dtype=torch.int32, device=DEV)
+    p = pop.kv_plan(i32(ctx), i32(new), tb, rg, state, page, capacity, state_out=out)
+    for name, got in (("table", tb), ("ring", rg), ("state", p.state), ("q_indptr", p.q_indptr), ("kv_lens", p.kv_lens),
+                      ("slots", p.slots), ("positions", p.positions), ("info", p.info)):
+        np.testing.assert_array_equal(got.cpu().numpy(), np.asarray(want[name]), err_msg=name)
+    if not in_place:
+        assert state.cpu().tolist() == [head, count]
+    return want
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("R,page,max_ctx,max_new,finished,spare", [
+    (1, 16, 0, 1, 0, 0), (1, 16, 100, 0, 0, 3), (1, 64, 0, 5000, 0, 1), (8, 16, 1200, 1, 0, 9), (37, 32, 300, 40, 5, 0),
+    (1023, 64, 500, 3, 7, 11), (1024, 128, 90, 1, 2, 0), (1025, 16, 33, 17, 3, 5), (4096, 64, 700, 30, 16, 1),
+])
+def test_plan_equals_the_oracle(R, page, max_ctx, max_new, finished, spare):
+    rng = np.random.default_rng(R + page)
+    case = plan_case(rng, R, page, max_ctx, max_new, finished, spare)
+    total = sum(max(n, 0) for n in case[1])
+    check_plan(*case, page, total, in_place=False)
+    check_plan(*case, page, total + 5, in_place=True)
+    if total > 2:
+        check_plan(*case, page, total - 2, in_place=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("R", [5, 3000])
+def test_plan_when_pages_run_out_or_the_row_is_full(R):
+    rng = np.random.default_rng(R)
+    ctx, new, table, ring, head, count = plan_case(rng, R, 16, 60, 40, 0, 0)
+    short = max(0, count // 2)                      # half of the pages are gone
+    want = check_plan(ctx, new, table, ring, head, short, 16, sum(new), in_place=False)
+    assert want["info"][1] > 0 and -1 in want["slots"]
+    ctx, new, table, ring, head, count = plan_case(rng, R, 16, 20, 60, 0, 50, max_blocks=3)
+    want = check_plan(ctx, new, table, ring, head, count, 16, sum(new), in_place=True)
+    assert -1 in want["slots"]
+
+
+@pytest.mark.gpu
+def test_plans_of_consecutive_steps_share_no_page():
+    """Forty steps of a small server: requests grow, finish and start again; at every step the live pages and the free ones
+    are a partition of all pages."""
+    rng = np.random.default_rng(5)
+    R, page, n_pages = 6, 16, 64
+    table, ring, state = i32(np.full((R, 16), -1)), i32(np.arange(n_pages)), i32([0, n_pages])
+    lens = np.zeros(R, dtype=np.int64)
+    for step in range(40):
+        new = rng.integers(0, 20, R)
+        for r in range(R):
+            if lens[r] + new[r] > 150 or (lens[r] > 0 and rng.random() < 0.1):
+                new[r] = -1
+        p = pop.kv_plan(i32(lens), i32(new), table, ring, state, page, int(np.maximum(new, 0).sum()))
+        lens = np.where(new < 0, 0, lens + new)
+        assert p.kv_lens.cpu().tolist() == lens.tolist() and p.info.cpu()[1] == 0
+        t, (head, count) = table.cpu().numpy(), state.cpu().tolist()
+        live = [int(x) for r in range(R) for x in t[r, :-(-int(lens[r]) // page)]]
+        free = ring.cpu().numpy()[(head + np.arange(count)) % n_pages].tolist()
+        assert sorted(live + free) == list(range(n_pages))
+
+
+# ------------------------------------------------------------------------------------------------------- append and read
+
+def filled(n_pages, page, heads, dim, value=255):
+    pages = pop.kv_pages(n_pages, page, heads, dim, DEV)
+    pages.fill_(value)
+    return pages
+
+
+def awkward_values(rng, T, H, D):
+    x = rng.standard_normal((T, H, D)).astype(np.float32)
+    x *= np.exp(rng.uniform(-6, 6, (T, H, 1))).astype(np.float32)
+    x += (rng.standard_normal((1, H, D)) * (rng.random((1, H, D)) < 0.1) * 20).astype(np.float32)
+    if T > 4:
+        x[1] = 3.0                                   # one value throughout: scale 0
+        x[2] = 0.0
+        x[3, 0, ::3] = np.inf
+        x[3, 0, 1::3] = np.nan
+        x[4, 0, 5] = -np.inf
+        x[4, -1] = np.linspace(0, 7.5, D)            # codes on ties
+    return x
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,H,D,page,fused", [(1, 1, 64, 16, False), (3, 2, 128, 16, True), (17, 3, 64, 32, True), (64, 8, 128, 64, False),
+                                              (150, 5, 128, 128, True), (333, 1, 64, 48, False)])
+def test_append_and_read(T, H, D, page, fused, dtype):
+    rng = np.random.default_rng(T + D)
+    n_pages = -(-T // page) + 2
+    slots = np.sort(rng.permutation(n_pages * page)[:T]) if T < 100 else rng.permutation(n_pages * page)[:T]
+    kx, vx = (torch.from_numpy(awkward_values(rng, T, H, D)).to(dtype) for _ in range(2))
+    if fused:
+        rows = torch.zeros(T, 4, H, D, dtype=dtype, device=DEV)
+        rows[:, 2], rows[:, 3] = kx.to(DEV), vx.to(DEV)
+        kd, vd = rows[:, 2], rows[:, 3]
+    else:
+        kd, vd = kx.to(DEV), vx.to(DEV)
+    pages = filled(n_pages, page, H, D)
+    pop.kv_append(pages, kd, vd, torch.from_numpy(slots).to(DEV))
+    raw = pages.cpu().numpy()
+    want = [ko.stored(x.float().numpy()) for x in (kx, vx)]
+    for i in rng.permutation(T)[:12]:                # byte for byte, by the format
+        for h in range(H):
+            got = ko.unpack_token(raw, int(slots[i]), h, D)
+            np.testing.assert_array_equal(got[0], want[0][i, h])
+            np.testing.assert_array_equal(got[1], want[1][i, h])
+    free = np.setdiff1d(np.arange(n_pages * page), slots)
+    G = D // 64
+    for s in free[:20]:                              # nobody else's place was touched
+        tile = raw[s // page, :, s % page // 16]
+        assert (tile[:, G * 1024:].reshape(H, 16, -1)[:, s % 16] == 255).all()
+    for out_dtype in (F32, BF16):
+        k, v = pop.kv_read(pages, torch.from_numpy(slots).to(DEV), out_dtype)
+        for got, w in ((k, want[0]), (v, want[1])):
+            ref = torch.from_numpy(w).float().to(out_dtype)     # one rounding of the exact value to fp32 (then bf16)
+            assert torch.equal(got.cpu(), ref)
+
+
+@pytest.mark.gpu
+def test_append_skips_slots_outside_the_cache_and_read_gives_zeros():
+    pages = filled(2, 16, 2, 64)
+    before = pages.clone()
+    k = torch.randn(3, 2, 64, device=DEV)
+    slots = torch.tensor([-1, 32, -5], device=DEV)
+    pop.kv_append(pages, k, k, slots)
+    assert torch.equal(pages, before)
+    a, b = pop.kv_read(pages, slots, F32)
+    assert float(a.abs().sum()) == 0.0 and float(b.abs().sum()) == 0.0
+    pop.kv_append(pages, k[:0], k[:0], slots[:0])
+    a, b = pop.kv_read(pages, slots[:0], BF16)
+    assert a.shape == (0, 2, 64) and b.dtype == BF16
+
+
+@pytest.mark.gpu
+def test_quantisation_error_is_half_a_step():
+    x = torch.randn(50, 4, 128, device=DEV)
+    pages = filled(4, 16, 4, 128)
+    slots = torch.arange(50, device=DEV)
+    pop.kv_append(pages, x, x, slots)
+    k, v = pop.kv_read(pages, slots, F32)
+    g = x.unflatten(-1, (2, 64))
+    step = (g.amax(-1) - g.amin(-1)) / 15
+    # half a step, plus what rounding the scale and the zero point to fp16 moves (2^-11 of each, 15 steps at most)
+    slack = step * (0.5 + 15 * 2.0 ** -11) + g.abs().amax(-1) * 2.0 ** -11
+    for y in (k, v):
+        assert ((y - x).unflatten(-1, (2, 64)).abs() <= slack[..., None] * (1 + 1e-5)).all()
+
+
+# --------------------------------------------------------------------------------------------------------------- attention
+
+class Setup:
+    """Requests with lengths ctx + new in a paged cache, with the exact stored values beside it."""
+
+    def __init__(self, seed, H, Hk, D, page, dtype, kv_lens, new, extra_pages=3, q_scale=1.5, pad_tokens=0, fused=False, first_page=0,
+                 k_scale=1.0):
+        rng = np.random.default_rng(seed)
+        self.H, self.Hk, self.D, self.page, self.dtype = H, Hk, D, page, dtype
+        self.kv_lens, self.new = [int(x) for x in kv_lens], [int(x) for x in new]
+        R = len(kv_lens)
+        blocks = [-(-n // page) for n in self.kv_lens]
+        mb = max(1, max(blocks))
+        n_pages = sum(blocks) + extra_pages
+        perm = rng.permutation(n_pages) + first_page
+        self.table = np.full((R, mb + 1), -1, dtype=np.int32)
+        at = 0
+        slots = []
+        for r, b in enumerate(blocks):
+            self.table[r, :b] = perm[at:at + b]
+            at += b
+            j = np.arange(self.kv_lens[r])
+            slots.append(self.table[r, j // page].astype(np.int64) * page + j % page)
+        slots = np.concatenate(slots)
+        total = len(slots)
+
+        def rnd(*shape):
+            return torch.from_numpy(rng.standard_normal(shape).astype(np.float32))
+
+        off = rnd(1, Hk, D) * 3 * torch.from_numpy((rng.random((1, Hk, D)) < 0.05).astype(np.float32))
+        k, v = ((rnd(total, Hk, D) + off) * k_scale).to(dtype), rnd(total, Hk, D).to(dtype)
+        self.k64, self.v64 = (ko.stored(x.float().numpy()) if total else np.zeros((0, Hk, D)) for x in (k, v))
+        T = sum(self.new)
+        q = (rnd(T + pad_tokens, H, D) * q_scale).to(dtype)
+        self.q64 = q.double().numpy()
+        if fused:
+            rows = torch.zeros(T + pad_tokens, H + 2 * Hk, D, dtype=dtype, device=DEV)
+            rows[:, :H] = q.to(DEV)
+            self.q = rows[:, :H]
+        else:
+            self.q = q.to(DEV)
+        self.pages = filled(n_pages + first_page, page, Hk, D)      # 0xff: NaN parameters wherever nothing is written
+        if total:
+            pop.kv_append(self.pages, k.to(DEV), v.to(DEV), torch.from_numpy(slots).to(DEV))
+        self.indptr = np.concatenate([[0], np.cumsum(self.new)])
+        self.T = T
+
+    def run(self, **kw):
+        return pop.kv_attention(self.pages, self.q, i32(self.table), i32(self.indptr), i32(self.kv_lens), **kw)
+
+    def check(self, causal=True, window=0, scale=None, want_lse=True, rows=None, absent=None, **kw):
+        lse = torch.full((self.q.shape[0], self.H), 7.0, device=DEV) if want_lse else None
+        out = torch.full(self.q.shape, 7.0, dtype=self.dtype, device=DEV)
+        self.run(causal=causal, window=window, scale=scale, out=out, lse_out=lse, **kw)
+        sc = self.D ** -0.5 if scale is None else scale
+        got, got_lse = out.double().cpu().numpy(), None if lse is None else lse.double().cpu().numpy()
+        assert (got[self.T:] == 7.0).all()                           # padding tokens are left alone
+        at, num, den = 0, 0.0, 0.0
+        for r, (L, n) in enumerate(zip(self.kv_lens, self.new)):
+            a, b = self.indptr[r], self.indptr[r + 1]
+            k, v = self.k64[at:at + L], self.v64[at:at + L]
+            at += L
+            if n == 0:
+                continue
+            ab = None if absent is None else absent.get(r)
+            o, l = ko.attention(self.q64[a:b], k, v, L - n, sc, causal, window, ab)
+            g = got[a:b]
+            empty = np.isneginf(l)
+            assert (g[empty] == 0.0).all()
+            if lse is not None:
+                assert (np.isneginf(got_lse[a:b]) == empty).all()
+            if L:
+                kmax, vmax = np.abs(k).max(), np.abs(v).max()
+                ds = abs(sc) * np.abs(self.q64[a:b]).sum(-1) * kmax          # [n, H]
+                if self.dtype == F32:
+                    tol = (2 * 2.0 ** -18 * ds + 2.0 ** -17) * vmax
+                    tl = 2.0 ** -18 * ds + 2.0 ** -18
+                else:
+                    tol = (2 * 2.0 ** -10 * ds + 2.0 ** -9) * vmax
+                    tl = 2.0 ** -10 * ds + 2.0 ** -18
+                err = np.abs(g - o) - (2.0 ** -9 * np.abs(o) if self.dtype == BF16 else 0.0)
+                assert (err <= tol[..., None]).all(), f"request {r} (kv {L}, new {n}): worst {np.max(err - tol[..., None]):.3e}"
+                if lse is not None:
+                    le = np.abs(got_lse[a:b] - l)[~empty]
+                    assert (le <= (tl + 2.0 ** -20 * np.abs(np.where(empty, 0.0, l)))[~empty]).all()
+            num += ((g - o) ** 2).sum()
+            den += (o ** 2).sum()
+        rel = np.sqrt(num / den) if den else 0.0
+        assert rel <= (1e-5 if self.dtype == F32 else 2.5e-3), f"2-norm error {rel:.3e}"
+        return out
+
+
+HEADS = [(1, 1), (4, 4), (8, 2), (6, 2), (5, 1), (8, 1), (12, 1), (20, 1), (28, 4)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("heads", HEADS)
+def test_single_tokens(heads, D, dtype):
+    kv = [1, 0, 15, 16, 17, 63, 64, 65, 200, 33, 1, 500]
+    new = [1, 1, 1, 1, 1, 1, 1, 1, 1, 0, 0, 1]
+    for page in (16, 64):
+        Setup(heads[0] + D, *heads, D, page, dtype, kv, new, fused=page == 64).check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 5), (True, 40), (False, 17), (True, 1)])
+def test_masks(causal, window, dtype):
+    # queries that stand before the first key (kv < new) see nothing; windows end inside tiles and pages
+    kv = [3, 0, 40, 130, 16, 97, 300]
+    new = [7, 2, 40, 3, 1, 50, 20]
+    for H, Hk, D in ((4, 2, 64), (3, 1, 128)):
+        Setup(window + 3, H, Hk, D, 32, dtype, kv, new).check(causal=causal, window=window)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("heads,D", [((4, 4), 128), ((8, 2), 128), ((6, 2), 64), ((5, 1), 128), ((2, 2), 64)])
+@pytest.mark.parametrize("kv,new", [([128], [128]), ([257], [257]), ([400, 70, 513], [129, 70, 300]), ([129, 1, 640, 0, 50], [1, 1, 383, 0, 33]),
+                                    ([100, 300], [200, 290])])
+def test_prompts(heads, D, kv, new, dtype):
+    s = Setup(sum(kv), *heads, D, 64, dtype, kv, new, pad_tokens=3, fused=True)
+    s.check()
+    s.check(window=77)
+    s.check(causal=False, want_lse=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_long_contexts_split_over_the_machine(dtype):
+    Setup(1, 8, 2, 128, 64, dtype, [20011], [1]).check()
+    Setup(2, 4, 4, 64, 128, dtype, [9000, 1, 333, 7777], [1, 1, 3, 2]).check()
+    Setup(3, 2, 1, 128, 16, dtype, [12345], [1]).check(window=5000)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_many_short_requests(dtype):
+    rng = np.random.default_rng(4)
+    kv = rng.integers(0, 70, 700)
+    Setup(4, 4, 2, 64, 16, dtype, kv, np.minimum(1, rng.integers(0, 5, 700))).check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_sharp_and_flat_softmax(dtype):
+    kv, new = [300, 150], [1, 150]
+    s = Setup(8, 4, 2, 128, 64, dtype, kv, new, q_scale=20.0)          # one key takes nearly all
+    s.check(scale=0.5 if dtype == F32 else None)
+    s.check(scale=0.0)                                                 # all keys alike
+    s.check(scale=-0.05)
+    Setup(9, 4, 2, 128, 64, dtype, kv, new, q_scale=1e-6).check()
+    Setup(10, 4, 2, 64, 64, dtype, kv, new, q_scale=3e4, k_scale=1e-4).check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new", [1, 60])
+def test_nan_and_infinite_queries_stay_in_their_rows(new):
+    for dtype in (BF16, F32):
+        s = Setup(11, 4, 2, 128, 64, dtype, [200, 90], [new, 3])
+        clean = s.run()
+        s.q[0, 1, 5] = float("nan")
+        s.q[new, 2, 7] = float("inf")
+        out = s.run()
+        assert torch.isnan(out[0, 1]).all()
+        keep = torch.ones(out.shape[:2], dtype=torch.bool, device=DEV)
+        keep[0, 1] = False
+        keep[new, 2] = False
+        assert torch.equal(out[keep], clean[keep]) and torch.isfinite(out[keep].float()).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_missing_pages_are_not_seen(dtype):
+    s = Setup(12, 4, 2, 64, 32, dtype, [200, 100, 64], [1, 100, 2])
+    s.table[0, 2] = -1
+    s.table[1, 0] = 10 ** 6
+    s.table[2, :] = -1
+    absent = {0: np.isin(np.arange(200) // 32, [2]), 1: np.arange(100) < 32, 2: np.ones(64, dtype=bool)}
+    s.check(absent=absent)
+
+
+@pytest.mark.gpu
+def test_lengths_beyond_the_table_are_cut():
+    s = Setup(13, 2, 2, 64, 16, BF16, [64, 40], [1, 1])
+    want = s.run(causal=False)
+    s.kv_lens = [10 ** 6, 40]
+    s.table = np.ascontiguousarray(s.table[:, :4])
+    assert torch.equal(s.run(causal=False), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_equal_calls_give_equal_bits_also_on_another_stream(dtype):
+    s = Setup(14, 8, 2, 128, 64, dtype, [5000, 300, 2000, 17], [1, 200, 3, 17])
+    a = s.run()
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        b = s.run(stream=st)
+    torch.cuda.current_stream().wait_stream(st)
+    assert torch.equal(a, b) and torch.equal(a, s.run())
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits():
+    page, Hk, D = 128, 8, 128
+    per_page = pop.kv_page_bytes(page, Hk, D)
+    first = (1 << 32) // per_page + 9                                  # every page lies past 4 GiB
+    for dtype, new in ((BF16, [1, 150]), (F32, [1, 20])):
+        s = Setup(15, 16, 8, D, page, dtype, [700, 150], new, first_page=first)
+        assert s.pages.numel() > 1 << 32
+        s.check()
+        slots = torch.tensor([int(s.table[0, 0]) * page + 5], device=DEV)
+        k, _ = pop.kv_read(s.pages, slots, F32)
+        assert torch.equal(k[0].cpu(), torch.from_numpy(s.k64[5]).float())
+        del s
+        torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+def test_a_step_in_a_cuda_graph():
+    """Plan, append and attention captured once and replayed: lengths live on the device, so the same graph serves every step."""
+    torch.manual_seed(0)
+    R, H, Hk, D, page, steps = 3, 8, 2, 128, 16, 20
+    q, k, v = (torch.randn(steps, R, h, D, device=DEV).bfloat16() for h in (H, Hk, Hk))
+    pages = filled(64, page, Hk, D)
+    table, ring, state = i32(np.full((R, 8), -1)), i32(np.random.default_rng(1).permutation(64)), i32([0, 64])
+    lens, ones = i32([0, 0, 0]), i32([1, 1, 1])
+    qs, ks, vs = q[0].clone(), k[0].clone(), v[0].clone()
+
+    def step():
+        p = pop.kv_plan(lens, ones, table, ring, state, page, R)
+        pop.kv_append(pages, ks, vs, p.slots)
+        o = pop.kv_attention(pages, qs, table, p.q_indptr, p.kv_lens)
+        lens.copy_(p.kv_lens)
+        return o
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()                                                          # the workspace of this stream comes into being
+        torch.cuda.synchronize()
+        lens.zero_()
+        table.fill_(-1)
+        state.copy_(i32([0, 64]))
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        out = step()
+    lens.zero_()
+    table.fill_(-1)
+    state.copy_(i32([0, 64]))
+    for s in range(steps):
+        qs.copy_(q[s]), ks.copy_(k[s]), vs.copy_(v[s])
+        g.replay()
+        torch.cuda.synchronize()
+        k64, v64 = (ko.stored(x[:s + 1].float().cpu().numpy().reshape(-1, Hk, D)).reshape(s + 1, R, Hk, D) for x in (k, v))
+        for r in range(R):
+            want, _ = ko.attention(q[s, r:r + 1].double().cpu().numpy(), k64[:, r], v64[:, r], s, D ** -0.5, True, 0)
+            got = out[r:r + 1].double().cpu().numpy()
+            assert np.linalg.norm(got - want) <= 4e-3 * np.linalg.norm(want)       # one row: up to 2^-8 of it
+
+
+# ---------------------------------------------------------------------------------------------------------------- refusals
+
+def test_page_bytes():
+    assert pop.kv_page_bytes(64, 8, 128) == 4 * 8 * 2304 and pop.kv_page_bytes(16, 1, 64) == 1152
+    for args in ((64, 8, 96), (24, 8, 128), (2048, 8, 128)):
+        with pytest.raises(pop.PopError) as e:
+            pop.kv_page_bytes(*args)
+        assert e.value.status == pop.POP_ERR_UNSUPPORTED
+    with pytest.raises(pop.PopError) as e:
+        pop.kv_page_bytes(0, 8, 128)
+    assert e.value.status == pop.POP_ERR_INVALID_ARG
+
+
+def _c_attention(**kw):
+    """pop_kv_attention with addresses that are never followed: every call here is refused on the host."""
+    a = dict(pages=1 << 20, n_pages=4, page_size=64, hk=2, dim=128, q=1 << 20, qs=512, dtype=pop.POP_BF16, heads=4, T=3, indptr=16, kv=16,
+             R=2, table=16, mb=2, scale=0.1, causal=1, window=0, out=1 << 20, lse=None, ws=1 << 20, wsb=1 << 40)
+    a.update(kw)
+    d = pop.KVCacheDesc(a["pages"], a["n_pages"], a["page_size"], a["hk"], a["dim"])
+    return pop.lib().pop_kv_attention(C.byref(d), a["q"], a["qs"], a["dtype"], a["heads"], a["T"], a["indptr"], a["kv"], a["R"], a["table"],
+                                      a["mb"], a["scale"], a["causal"], a["window"], a["out"], a["lse"], a["ws"], a["wsb"], None)
+
+
+@pytest.mark.parametrize("kw", [dict(pages=None), dict(pages=(1 << 20) + 8), dict(n_pages=0), dict(q=None), dict(q=(1 << 20) + 2), dict(qs=511),
+                                dict(qs=508), dict(heads=5), dict(heads=0), dict(T=-1), dict(R=0), dict(mb=0), dict(window=-1), dict(out=None),
+                                dict(ws=None), dict(wsb=1), dict(indptr=None), dict(kv=None), dict(table=None), dict(scale=float("nan")),
+                                dict(out=(1 << 20) + 4)])
+def test_attention_refuses_wrong_arguments(kw):
+    assert _c_attention(**kw) == pop.POP_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("kw", [dict(dim=96), dict(dim=256), dict(page_size=24), dict(page_size=2048), dict(dtype=7),
+                                dict(R=pop.POP_KV_MAX_REQUESTS + 1), dict(n_pages=1 << 30)])
+def test_attention_refuses_what_it_does_not_take(kw):
+    assert _c_attention(**kw) == pop.POP_ERR_UNSUPPORTED
+
+
+def test_no_tokens_is_no_work():
+    assert _c_attention(T=0, q=None, out=None) == pop.POP_OK
+
+
+def test_append_read_and_plan_refuse_wrong_arguments():
+    l = pop.lib()
+    P = 1 << 20
+
+    def desc(**kw):
+        a = dict(pages=P, n=4, page=64, hk=2, dim=128)
+        a.update(kw)
+        return C.byref(pop.KVCacheDesc(a["pages"], a["n"], a["page"], a["hk"], a["dim"]))
+
+    bad, no = pop.POP_ERR_INVALID_ARG, pop.POP_ERR_UNSUPPORTED
+    assert l.pop_kv_append(None, P, 256, P, 256, 1, P, 3, None) == bad
+    assert l.pop_kv_append(desc(), None, 256, P, 256, 1, P, 3, None) == bad
+    assert l.pop_kv_append(desc(), P, 255, P, 256, 1, P, 3, None) == bad
+    assert l.pop_kv_append(desc(), P, 256, P + 2, 256, 1, P, 3, None) == bad
+    assert l.pop_kv_append(desc(), P, 256, P, 256, 1, None, 3, None) == bad
+    assert l.pop_kv_append(desc(), P, 256, P, 256, 1, P, -1, None) == bad
+    assert l.pop_kv_append(desc(dim=80), P, 256, P, 256, 1, P, 3, None) == no
+    assert l.pop_kv_append(desc(), P, 256, P, 256, 5, P, 3, None) == no
+    assert l.pop_kv_append(desc(), None, 0, None, 0, 1, None, 0, None) == pop.POP_OK
+    assert l.pop_kv_read(desc(), P, 3, 1, None, P, None) == bad
+    assert l.pop_kv_read(desc(page=17), P, 3, 1, P, P, None) == no
+    assert l.pop_kv_attention_workspace(None) == bad and l.pop_kv_page_bytes(64, 8, 128, None) == bad
+    good = [P, P, 4, 16, P, 8, P, P, P, 2, 4, P, P, P, None, None, None]
+    for i in (0, 1, 4, 6, 7, 8, 11, 12, 13):
+        args = list(good)
+        args[i] = None
+        assert l.pop_kv_plan(*args) == bad
+    for i, v, rc in ((2, 0, bad), (2, 5000, no), (3, 20, no), (3, 0, bad), (5, 0, bad), (9, 0, bad), (10, -1, bad)):
+        args = list(good)
+        args[i] = v
+        assert l.pop_kv_plan(*args) == rc
+
+
+@pytest.mark.gpu
+def test_binding_refuses_wrong_tensors():
+    pages = filled(4, 16, 2, 64)
+    k = torch.randn(3, 2, 64, device=DEV)
+    slots = torch.arange(3, device=DEV)
+    for bad in (lambda: pop.kv_append(pages, k, k[:2], slots), lambda: pop.kv_append(pages, k[:, :1], k, slots),
+                lambda: pop.kv_append(pages, k, k, slots.int()), lambda: pop.kv_append(pages[:, :, :, ::2], k, k, slots),
+                lambda: pop.kv_append(pages, k.transpose(0, 1).contiguous().transpose(0, 1), k, slots),
+                lambda: pop.kv_append(pages, k, k, slots.cpu()), lambda: pop.kv_read(pages, slots.view(1, 3), F32),
+                lambda: pop.kv_attention(pages, k, i32([[0]]), i32([0, 3, 3]), i32([3])),
+                lambda: pop.kv_attention(pages, k, i32([[0]]), i32([0, 3]), i32([3]), out=k.bfloat16()),
+                lambda: pop.kv_attention(pages, k, i32([[0]]), i32([0, 3]), i32([3]), lse_out=k)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: pop.kv_append(pages, k.half(), k.half(), slots), lambda: pop.kv_append(pages, k, k.bfloat16(), slots),
+                lambda: pop.kv_read(pages, slots, torch.float16)):
+        with pytest.raises(TypeError):
+            bad()
