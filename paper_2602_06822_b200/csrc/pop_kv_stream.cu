@@ -9,39 +9,55 @@
 // finished by joining its parts (running maximum, sum, un-normalised output): inside the CTA through shared memory, between
 // CTAs through a workspace, by whichever CTA arrives last and in a fixed order.
 //
-// The arithmetic.  2 flops per code and query row would be nothing, but turning 4-bit codes into numbers one by one is not:
-// an SM has about three lane operations per code.  So codes become bf16 in pairs with one shift and one logical operation
-// (c << 3 under the bits 0x4180 is 16 + c), go through the tensor cores as they are, and their scales and zero points are applied
-// to what comes out, per token instead of per element:
-//   q.k_j = sum over groups of  s (q.(c + f) - q.f) + z sum(q)
-//   sum_j p_j v_j = sum_j (p_j s_j) (c_j + f_j)  +  sum_j p_j (z_j - s_j f_j)
-// with the offset f = 16 for the even member of a pair and -31 (sign bit, complemented code: the same one operation) for the odd
-// one.  With f = 16 for both, the sums over the tokens would grow with the context while the result does not, and the tensor cores'
-// truncation of their accumulator (toward zero, about 2^-24 of it at every step) would stay behind: 1 % of the result at 131k
-// tokens.  fp32 calls take one more operation per pair to get c - 8 itself, and start a new accumulator for every tile.
-// mma.m16n8k16 with the codes as the 16-row operand (rows = tokens for the keys, dimensions for the values) and the query rows as the
-// 8 columns: the memory format is made of its fragments, so that a lane's 16-byte load is its operand, and 8 query heads cost what
-// one does.  tcgen05 would need the codes unpacked through shared memory for a product whose 128-row operand is mostly padding.
-// p s enters as a sum of bf16 pieces (two for bf16 queries: 16 bits; three for fp32, whose q is split alike), so what the tensor cores
-// multiply is exact to fp32 level.  The maximum is only brought up to date when a logit passes it by 2^8 (the sums have room for
-// that in fp32), which takes the reduction over the warp out of most tiles.
+// The arithmetic.  2 flops per code and query row would be nothing, but turning 4-bit codes into numbers one by one is not: an SM
+// has about three lane operations per code, and only half of its lanes do logical ones.  So codes become fp16 in pairs by masking (c << 4 under the
+// bits 0x5400 is 64 + c, c under 0x6400 is 1024 + c) and go through the tensor cores as mma.m16n8k16 operands: the codes as the
+// 16-row side (rows = tokens for the keys, dimensions for the values), the query rows as the 8 columns.  The memory format is made of
+// those fragments, so that a lane's 16-byte load is its operand, and 8 query heads cost what one does.
+//   Keys: 64 + c as they are, in sums that start at -64 sum(q); scale and zero point are applied to the sums, per token instead of
+//   per element:  q.k_j = sum over groups of  s q.c + z sum(q).  (What the accumulator's truncation leaves of the 64 is 1e-5 of a logit.)
+//   The query is fp16 too, each row times a power of two that puts its largest element at 2^10, which loses nothing of bf16.
+//   Values: c - 8 exactly by one addition per pair, then s (c - 8) + (z + 8 s) in fp16 (11 bits: 2^-12 of rounding against the
+//   result's 2^-9).  Here an offset must not stay: summed over the tokens it would grow with the context, and the result does not.
+//   The weights p are fp16 in 2^-14 .. 2^15: the reference m stays at least 2^7 below the largest logit seen and is only brought up
+//   to date when one passes it by 2^15, which takes the reduction over the warp out of most tiles and leaves small weights, of
+//   which a long context has many, 2^32 of range.
+// tcgen05 would need the codes unpacked through shared memory for a product whose 128-row operand is mostly padding.
+//
+// fp32 calls take the same way with bf16 pieces: q and p s as sums of three (their products with c - 8 are exact), the values'
+// scales applied to p instead, sum_j p_j v_j = sum_j (p_j s_j) (c_j - 8) + sum_j p_j (z_j + 8 s_j), and a new accumulator for every
+// tile: the tensor cores truncate theirs toward zero at every step, which over a thousand tokens would be 1e-5.
+#include <type_traits>
+
 #include "pop_kv_attn.cuh"
 
 namespace {
 
 typedef unsigned long long ull;
 
+#ifndef KV_WARPS
+#define KV_WARPS 12
+#define KV_STAGES 5
+#endif
+
 template <typename T, int G, int NT> struct StreamCfg {
     static constexpr int D = 64 * G, ROWS = 8 * NT;
     static constexpr bool F32 = sizeof(T) == 4;
-    static constexpr int QS = F32 ? 3 : 1;                  // bf16 pieces of q
-    static constexpr int PS = F32 ? 3 : 2;                  // bf16 pieces of p s
-    static constexpr int WARPS = (NT == 1 && !F32) ? 16 : 8;
+    static constexpr int QS = F32 ? 3 : 1;                  // pieces of q
+    static constexpr int PS = 3;                            // bf16 pieces of p s (fp32)
+    static constexpr float RAISE = F32 ? 8.f : 15.f;        // the reference is raised when a logit is this far above it,
+    static constexpr float BELOW = F32 ? 0.f : 7.f;         // to this far below the logit
+    // Tiles that a warp works on at once: two independent chains of products, reductions and exponentials where registers allow
+    static constexpr int PAIR = (NT == 1 && !F32) ? 2 : 1;
+    static constexpr int WARPS = (NT == 1 && !F32) ? KV_WARPS : 8;
     static constexpr int TB = kv::tile_bytes(D);
     static constexpr int PIECE = ROWS * (D + 2) * 4;        // un-normalised output, maximum and sum of a part of a segment
-    static constexpr int STAGES = (PIECE + TB - 1) / TB > 3 ? (PIECE + TB - 1) / TB : (G == 1 ? 6 : 3);
+    static constexpr int MIN_STAGES = (PIECE + TB - 1) / TB;
+    static constexpr int STAGES = MIN_STAGES > (G == 1 ? 8 : KV_STAGES) ? MIN_STAGES : (G == 1 ? 8 : KV_STAGES);
     static constexpr int WARP_BYTES = STAGES * TB + PIECE;  // ring (its memory later holds the second piece) and first piece
 };
+
+template <int N> struct Const { static constexpr int value = N; };
 
 // Kept per piece: which segment it is a part of.
 struct PieceOf { ull begin, end; int r, hk, rb, valid; };
@@ -52,10 +68,14 @@ __device__ __forceinline__ void cp16(u32 dst, const void* src) {
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+template <bool F32>                                          // operands: bf16 pieces for fp32 calls, fp16 for bf16 ones
 __device__ __forceinline__ void mma16816(float (&c)[4], u32 a0, u32 a1, u32 a2, u32 a3, u32 b0, u32 b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    if constexpr (F32)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ u32 transpose8x8(u32 x) {
     u32 y;
@@ -66,16 +86,47 @@ __device__ __forceinline__ u32 pack_bf16(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const u32*>(&v);
 }
-// The i-th pair of codes of a word as bf16 numbers c + f.  EXACT: f = -8 for both; else 16 (low half) and -31 (high half).
-template <int I, bool EXACT> __device__ __forceinline__ u32 code_pair(u32 w) {
-    const u32 x = I == 0 ? w << 3 : w >> (I == 0 ? 0 : 4 * I - 3);
-    if constexpr (EXACT) {
-        const u32 y = (x & 0x00780078u) | 0x41804180u;
-        u32 r;
-        asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(y), "r"(0x41c041c0u));        // - 24
-        return r;
+__device__ __forceinline__ u32 pack_half(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const u32*>(&v);
+}
+__device__ __forceinline__ u32 hadd2(u32 a, u32 b) {
+    u32 r;
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ u32 hfma2(u32 a, u32 b, u32 c) {
+    u32 r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+__device__ __forceinline__ u32 mask_or(u32 x, u32 mask, u32 bits) {           // (x & mask) | bits in one operation
+    u32 r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(x), "r"(mask), "r"(bits));
+    return r;
+}
+// The four pairs of codes of a word as fp16 numbers 64 + c.
+__device__ __forceinline__ void code_pairs_64(u32 w, u32 (&x)[4]) {
+    x[0] = mask_or(w << 4, 0x00f000f0u, 0x54005400u);
+    x[1] = mask_or(w, 0x00f000f0u, 0x54005400u);
+    x[2] = mask_or(w >> 4, 0x00f000f0u, 0x54005400u);
+    x[3] = mask_or(w >> 8, 0x00f000f0u, 0x54005400u);
+}
+// The same as numbers c - 8, in fp16 or bf16.
+template <bool F32> __device__ __forceinline__ void code_pairs(u32 w, u32 (&x)[4]) {
+    if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const u32 y = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;                          // 128 + c
+            asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(x[i]) : "r"(y), "r"(0x43084308u));
+        }
+    } else {
+        const u32 v = w >> 8;
+        x[0] = hadd2(mask_or(w, 0x000f000fu, 0x64006400u), 0xe408e408u);                         // 1024 + c - 1032
+        x[1] = hadd2(mask_or(w, 0x00f000f0u, 0x54005400u), 0xd480d480u);                         // 64 + c - 72
+        x[2] = hadd2(mask_or(v, 0x000f000fu, 0x64006400u), 0xe408e408u);
+        x[3] = hadd2(mask_or(v, 0x00f000f0u, 0x54005400u), 0xd480d480u);
     }
-    return (x & 0x00780078u) ^ 0xc1f84180u;
 }
 
 __device__ __forceinline__ float2 half2_at(u32 w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
@@ -93,37 +144,66 @@ template <int ROWS> __device__ __forceinline__ Tiles request_tiles(const KvAttnA
     return t;
 }
 
-// The CTA (of C, over U units) that unit u belongs to: CTA c has units c U / C .. (c + 1) U / C - 1.
-__device__ __forceinline__ int cta_of(ull u, ull U, int C) { return (int)(((u + 1) * C - 1) / U); }
-
-// Joins n parts of one query row (part k at at(k); lane by lane over the dimensions) in the order of k; the result goes to the
-// part `to`, or, where that is NULL, to the output.
+// Joins n parts of one query row (part k at at(k)); the result goes to the part `to`, or, where that is NULL, to the output.  Maxima
+// and sums are read by a lane for each part, the outputs by a lane for every D / 32 dimensions, many parts on their way at once:
+// parts of other CTAs are a trip to L2 away.
 template <typename T, int D, int ROWS, bool GLOBAL, typename At>
 __device__ __forceinline__ void join_row(const KvAttnArgs& A, int r, int hk, int row, int n, At at, float* to) {
-    constexpr int PER = D / 32;
+    constexpr int PER = D / 32, BATCH = 8;
+    typedef typename std::conditional<PER == 4, float4, float2>::type Vec;
     const int lane = threadIdx.x & 31, col = row % ROWS;
-    auto ld = [](const float* p) { return GLOBAL ? __ldcg(p) : *p; };     // parts of other CTAs lie in L2
+    auto stats = [&](int k) {
+        const float2* p = reinterpret_cast<const float2*>(at(k) + ROWS * D + 2 * col);
+        return GLOBAL ? __ldcg(p) : *p;
+    };
     float m = -1e30f, l = 0.f, o[PER] = {};
-    for (int k = 0; k < n; ++k) m = fmaxf(m, ld(at(k) + ROWS * D + 2 * col));
-#pragma unroll 4
-    for (int k = 0; k < n; ++k) {
-        const float* p = at(k);
-        const float f = kv_exp2(ld(p + ROWS * D + 2 * col) - m);
-        l = fmaf(ld(p + ROWS * D + 2 * col + 1), f, l);
+    float2 mine = lane < n ? stats(lane) : make_float2(-1e30f, 0.f);
+    m = mine.x;
+    for (int k = lane + 32; k < n; k += 32) m = fmaxf(m, stats(k).x);
 #pragma unroll
-        for (int e = 0; e < PER; ++e) o[e] = fmaf(ld(p + col * D + lane + 32 * e), f, o[e]);
+    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+    for (int k0 = 0; k0 < n; k0 += 32) {
+        if (k0) mine = k0 + lane < n ? stats(k0 + lane) : make_float2(-1e30f, 0.f);
+        const float f = kv_exp2(mine.x - m);
+        l = fmaf(mine.y, f, l);
+        const int end = min(32, n - k0);
+        for (int k = 0; k < end; k += BATCH) {
+            Vec x[BATCH];
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                const Vec* p = reinterpret_cast<const Vec*>(at(k0 + min(k + b, end - 1)) + col * D) + lane;
+                x[b] = GLOBAL ? __ldcg(p) : *p;
+            }
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                const float w = __shfl_sync(~0u, f, min(k + b, 31));
+                if (k + b < end) {
+                    const float* y = reinterpret_cast<const float*>(&x[b]);
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) o[e] = fmaf(y[e], w, o[e]);
+                }
+            }
+        }
     }
-    if (to) {
 #pragma unroll
-        for (int e = 0; e < PER; ++e) to[col * D + lane + 32 * e] = o[e];
-        if (lane == 0) { to[ROWS * D + 2 * col] = m; to[ROWS * D + 2 * col + 1] = l; }
+    for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(~0u, l, d);
+    if (to) {
+        *(reinterpret_cast<Vec*>(to + col * D) + lane) = *reinterpret_cast<const Vec*>(o);
+        if (lane == 0) *reinterpret_cast<float2*>(to + ROWS * D + 2 * col) = make_float2(m, l);
         return;
     }
     const int i = row / A.ratio;
     const size_t out_at = (size_t)(A.indptr[r] + i) * A.H + hk * A.ratio + (row - i * A.ratio);
     const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* out = (T*)A.out + out_at * D + lane * PER;
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) ((T*)A.out)[out_at * D + lane + 32 * e] = Elem<T>::from_f32(o[e] * inv);
+        for (int e = 0; e < PER; ++e) o[e] *= inv;
+        *reinterpret_cast<Vec*>(out) = *reinterpret_cast<const Vec*>(o);
+    } else {
+#pragma unroll
+        for (int e = 0; e < PER; e += 2) reinterpret_cast<u32*>(out)[e / 2] = pack_bf16(o[e] * inv, o[e + 1] * inv);
+    }
     if (A.lse && lane == 0) A.lse[out_at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718f;
 }
 
@@ -133,18 +213,20 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
     constexpr int D = Cfg::D, ROWS = Cfg::ROWS, WARPS = Cfg::WARPS, TB = Cfg::TB, STAGES = Cfg::STAGES, QS = Cfg::QS, PS = Cfg::PS;
     extern __shared__ __align__(16) unsigned char kv_smem[];
     ull* prefix = reinterpret_cast<ull*>(kv_smem + (size_t)WARPS * Cfg::WARP_BYTES);        // [R + 1] units before request r
-    __shared__ ull scan_sum[WARPS];
-    __shared__ ull scan_carry;
+    __shared__ ull scan_sum[2][WARPS];
     __shared__ PieceOf piece_of[WARPS][2];
     __shared__ int last_of[2];
+    __shared__ unsigned char order[WARPS][32];                             // every warp's list of the CTA's pieces
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    asm volatile("griddepcontrol.wait;" ::: "memory");                     // launched while the kernel before it winds down
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---- units before every request
-    if (tid == 0) { scan_carry = 0; prefix[0] = 0; last_of[0] = last_of[1] = 0; }
-    if (tid < 2 * WARPS) piece_of[tid >> 1][tid & 1].valid = 0;
-    __syncthreads();
-    for (int r0 = 0; r0 < A.R; r0 += WARPS * 32) {
+    if (tid == 0) prefix[0] = 0;
+    if (lane < 2) piece_of[warp][lane].valid = 0;
+    ull U = 0;
+    for (int r0 = 0, turn = 0; r0 < A.R; r0 += WARPS * 32, turn ^= 1) {
         const int r = r0 + tid;
         ull v = 0;
         if (r < A.R) {
@@ -156,21 +238,26 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
             const ull u = __shfl_up_sync(~0u, v, d);
             if (lane >= d) v += u;
         }
-        if (lane == 31) scan_sum[warp] = v;
+        if (lane == 31) scan_sum[turn][warp] = v;
         __syncthreads();
-        v += scan_carry;
-        for (int w = 0; w < warp; ++w) v += scan_sum[w];
+        v += U;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            const ull x = scan_sum[turn][w];
+            if (w < warp) v += x;
+            U += x;
+        }
         if (r < A.R) prefix[r + 1] = v;
-        __syncthreads();
-        if (tid == WARPS * 32 - 1) scan_carry = v;
     }
     __syncthreads();
-    const ull U = prefix[A.R];
-    const int C = (int)min((ull)gridDim.x, U);
+    // units of a CTA (the last one may have fewer, further ones none)
+    const ull share = U >> 32 ? (U + gridDim.x - 1) / gridDim.x : (ull)(((u32)U + gridDim.x - 1) / gridDim.x);
     const int cta = blockIdx.x;
-    if (cta >= C) return;
-    const ull ca = (ull)cta * U / C, cb = (ull)(cta + 1) * U / C;
-    const ull wa = ca + (cb - ca) * warp / WARPS, wb = ca + (cb - ca) * (warp + 1) / WARPS;
+    const ull ca = cta * share;
+    if (ca >= U) return;
+    const ull cb = min(U, ca + share);
+    const u32 mine = (u32)(cb - ca);                                       // (2^32 units would be a day's work)
+    const ull wa = ca + (ull)mine * warp / WARPS, wb = ca + (ull)mine * (warp + 1) / WARPS;
 
     unsigned char* ring = kv_smem + (size_t)warp * Cfg::WARP_BYTES;
     const u32 ring_addr = (u32)__cvta_generic_to_shared(ring);
@@ -188,7 +275,8 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
         while (prefix[r + 1] <= u) ++r;
         const KvRequest rq = kv_request(A, r);
         const Tiles ti = request_tiles<ROWS>(A, rq);
-        const int seg = (int)((u - prefix[r]) / ti.count), hk = seg / ti.row_blocks, rb = seg - hk * ti.row_blocks;
+        const ull into = u - prefix[r];
+        const int seg = into >> 32 ? (int)(into / ti.count) : (int)((u32)into / (u32)ti.count), hk = seg / ti.row_blocks, rb = seg - hk * ti.row_blocks;
         const ull sb = prefix[r] + (ull)seg * ti.count, se = sb + ti.count;
         const ull pe = min(se, wb);
         const int rows = min(ROWS, rq.n * A.ratio - rb * ROWS), row0 = rb * ROWS;
@@ -198,9 +286,46 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
         const int t_lo = max(ti.first + (int)(u - sb), kv_first(A, p_lo) / kv::TILE);
         const int t_hi = min(ti.first + (int)(pe - sb), (kv_end(A, rq, p_hi) + kv::TILE - 1) / kv::TILE);
 
-        // query fragments: column g of n tile nt, dimensions 16 t .. 16 t + 15 of each group
+        // ---- the tiles, STAGES of them on their way; lane i keeps the id of page `block - in_ids + i`
+        const int32_t* row_table = A.table + (size_t)r * A.max_blocks;
+        const int tiles_per_page = A.page_size / kv::TILE;
+        int block = t_lo / tiles_per_page, in_page = t_lo - block * tiles_per_page, ids = 0, in_ids = 32;
+        const unsigned char* src = nullptr;                                // this lane's place in the next tile, NULL: its page is missing
+        auto open_page = [&]() {
+            if (in_ids == 32) {
+                ids = block + lane < A.max_blocks ? row_table[block + lane] : -1;
+                in_ids = 0;
+            }
+            const int page = __shfl_sync(~0u, ids, in_ids);
+            src = (u32)page < (u32)A.n_pages ? A.pages + (((size_t)page * A.Hk + hk) * tiles_per_page + in_page) * TB + lane * 16 : nullptr;
+        };
+        if (t_lo < t_hi) open_page();
+        u32 present = 0;                                                   // bit s: the tile in stage s is there
+        int next = t_lo, stage_in = 0;
+        auto issue = [&]() {
+            if (next < t_hi) {
+                if (in_page == tiles_per_page) { in_page = 0; ++block; ++in_ids; open_page(); }
+                present &= ~(1u << stage_in);
+                if (src) {
+                    present |= 1u << stage_in;
+                    const u32 dst = ring_addr + stage_in * TB + lane * 16;
+#pragma unroll
+                    for (int c = 0; c < TB / 16; c += 32)
+                        if (c + 32 <= TB / 16 || c + lane < TB / 16) cp16(dst + c * 16, src + c * 16);
+                    src += TB;
+                }
+                ++in_page;
+                ++next;
+                if (++stage_in == STAGES) stage_in = 0;
+            }
+            cp_commit();
+        };
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s) issue();
+
+        // ---- query fragments: column g of n tile nt, dimensions 16 t .. 16 t + 15 of each group
         u32 qf[NT][G][QS][8];
-        float qsum[NT][G][2], q0[NT][G][2];                                   // sum(q), and where the logits' sums start: -q.f
+        float q64[NT][G][2], sc[NT][2];                     // -64 sum(q) of a group, what takes a product to a logit
         int see_lo[NT][2], see_hi[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -208,43 +333,54 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
             const bool in = nt * 8 + g < rows;
             const int i = row / A.ratio;
             const T* qp = (const T*)A.q + (size_t)(rq.q0 + (in ? i : 0)) * A.q_stride + (size_t)(hk * A.ratio + (in ? row - i * A.ratio : 0)) * D + 16 * t;
+            float x[G][16], f = 1.f;
 #pragma unroll
-            for (int gr = 0; gr < G; ++gr) {
-                float x[16];
+            for (int gr = 0; gr < G; ++gr)
 #pragma unroll
                 for (int v = 0; v < 16 / Elem<T>::VEC; ++v) {
                     const uint4 raw = *reinterpret_cast<const uint4*>(qp + gr * 64 + v * Elem<T>::VEC);
                     float y[Elem<T>::VEC];
                     Elem<T>::unpack(raw, y);
 #pragma unroll
-                    for (int e = 0; e < Elem<T>::VEC; ++e) x[v * Elem<T>::VEC + e] = in ? y[e] : 0.f;
+                    for (int e = 0; e < Elem<T>::VEC; ++e) x[gr][v * Elem<T>::VEC + e] = in ? y[e] : 0.f;
                 }
-                float even = 0.f, odd = 0.f;
+            if constexpr (!Cfg::F32) {
+                float top = 0.f;
 #pragma unroll
-                for (int e = 0; e < 16; e += 2) { even += x[e]; odd += x[e + 1]; }
+                for (int gr = 0; gr < G; ++gr)
 #pragma unroll
-                for (int d = 1; d < 4; d <<= 1) { even += __shfl_xor_sync(~0u, even, d); odd += __shfl_xor_sync(~0u, odd, d); }
-                const float sum = even + odd, start = Cfg::F32 ? 0.f : 31.f * odd - 16.f * even;
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {                              // columns 2 t and 2 t + 1
-                    qsum[nt][gr][c] = __shfl_sync(~0u, sum, 8 * t + 4 * c);
-                    q0[nt][gr][c] = __shfl_sync(~0u, start, 8 * t + 4 * c);
-                }
-#pragma unroll
-                for (int s = 0; s < QS; ++s) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const u32 w = pack_bf16(x[2 * e], x[2 * e + 1]);
-                        qf[nt][gr][s][e] = w;
-                        if (s + 1 < QS) {
-                            x[2 * e] -= __uint_as_float(w << 16);
-                            x[2 * e + 1] -= __uint_as_float(w & 0xffff0000u);
-                        }
-                    }
-                }
+                    for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[gr][e]));
+                top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+                f = __uint_as_float((264u - max(__float_as_uint(top) >> 23, 30u)) << 23);        // 2^10 over the power of two in top
             }
 #pragma unroll
+            for (int gr = 0; gr < G; ++gr) {
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) { x[gr][e] *= f; sum += x[gr][e]; }
+                sum += __shfl_xor_sync(~0u, sum, 1);
+                sum += __shfl_xor_sync(~0u, sum, 2);
+#pragma unroll
+                for (int c = 0; c < 2; ++c) q64[nt][gr][c] = -64.f * __shfl_sync(~0u, sum, 8 * t + 4 * c);     // columns 2 t and 2 t + 1
+#pragma unroll
+                for (int s = 0; s < QS; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if constexpr (Cfg::F32) {
+                            const u32 w = pack_bf16(x[gr][2 * e], x[gr][2 * e + 1]);
+                            qf[nt][gr][s][e] = w;
+                            x[gr][2 * e] -= __uint_as_float(w << 16);
+                            x[gr][2 * e + 1] -= __uint_as_float(w & 0xffff0000u);
+                        } else {
+                            qf[nt][gr][s][e] = pack_half(x[gr][2 * e], x[gr][2 * e + 1]);
+                        }
+                    }
+            }
+            const float back = A.scale2 * __uint_as_float((254u << 23) - __float_as_uint(f));             // scale2 / f
+#pragma unroll
             for (int c = 0; c < 2; ++c) {
+                sc[nt][c] = __shfl_sync(~0u, back, 8 * t + 4 * c);
                 const int p = rq.pos0 + (row0 + nt * 8 + 2 * t + c) / A.ratio;
                 see_lo[nt][c] = kv_first(A, p);
                 see_hi[nt][c] = kv_end(A, rq, p);
@@ -252,7 +388,7 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
         }
 
         float acc[NT][G][4][4];
-        float m[NT][2], l[NT][2], corr[NT][G][2];
+        float m[NT][2], l[NT][2], corr[NT][G][2];                          // corr: sum of p (z + 8 s) (fp32 calls)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -266,124 +402,110 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                 }
             }
 
-        // ---- the tiles, STAGES - 1 of them on their way ahead of the one in hand; lane i keeps the id of page id_base + i
-        const int32_t* row_table = A.table + (size_t)r * A.max_blocks;
-        const int tiles_per_page = A.page_size / kv::TILE;
-        int id_base = 0, ids = 0;
-        bool have_ids = false;
-        u32 present = 0;                                                   // bit s: the tile in stage s is there
-        auto issue = [&](int tile, int stage) {
-            if (tile < t_hi) {
-                const int block = tile / tiles_per_page;
-                if (!have_ids || block >= id_base + 32) {
-                    id_base = block;
-                    const int b = block + lane;
-                    ids = b < A.max_blocks ? row_table[b] : -1;
-                    have_ids = true;
+        // ---- what is done with P tiles from `tile` on, at base[]; whole: every row sees every token of them
+        auto use_tiles = [&](int tile, unsigned char* const* base, auto count_, auto whole_) {
+            constexpr int P = decltype(count_)::value;
+            constexpr bool whole = decltype(whole_)::value;
+            auto params_of = [&](int p, int j, int from, u32 (&w)[G]) {    // token j of tile p: G words for the keys, the values' G further
+                const u32* params = reinterpret_cast<const u32*>(base[p]) + kv::param_words(G) + j * 2 * G + from;
+                if constexpr (G == 2) {
+                    const uint2 x = *reinterpret_cast<const uint2*>(params);
+                    w[0] = x.x; w[1] = x.y;
+                } else {
+                    w[0] = *params;
                 }
-                const int page = __shfl_sync(~0u, ids, block - id_base);
-                const bool there = (u32)page < (u32)A.n_pages;
-                present = (present & ~(1u << stage)) | ((there ? 1u : 0u) << stage);
-                if (there) {
-                    const unsigned char* src = A.pages + (((size_t)page * A.Hk + hk) * tiles_per_page + (tile - block * tiles_per_page)) * TB;
-                    const u32 dst = ring_addr + stage * TB;
+            };
+            if constexpr (!whole) {                      // places that no token was written to may hold anything, NaN too
 #pragma unroll
-                    for (int c = 0; c < TB / 16; c += 32)
-                        if (c + 32 <= TB / 16 || c + lane < TB / 16) cp16(dst + (c + lane) * 16, src + (c + lane) * 16);
-                }
+                for (int p = 0; p < P; ++p)
+                    for (int i = lane; i < kv::TILE * 2 * G; i += 32)
+                        if ((tile + p) * kv::TILE + i / (2 * G) >= rq.len) (reinterpret_cast<u32*>(base[p]) + kv::param_words(G))[i] = 0u;
+                __syncwarp();
             }
-            cp_commit();
-        };
-        int stage_in = 0, stage = 0;
-        __syncwarp();
+            // logits: element e of an accumulator is token (e < 2 ? g : g + 8) of the tile, column 2 t + e % 2
+            float s[P][NT][4];
 #pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s) { issue(t_lo + s, stage_in); ++stage_in; }
-        for (int tile = t_lo; tile < t_hi; ++tile) {
-            cp_wait<STAGES - 2>();
-            __syncwarp();
-            issue(tile + STAGES - 1, stage_in);
-            if (++stage_in == STAGES) stage_in = 0;
-            const unsigned char* base = ring + stage * TB;
-            const bool there = (present >> stage) & 1u;
-            if (++stage == STAGES) stage = 0;
-            if (!there) continue;
-
-            const int j0 = tile * kv::TILE + g, j1 = j0 + 8;
-            // parameters of tokens j0 and j1: keys' groups, then the values'
-            u32 pw[2][2 * G];
-            {
-                const u32* pp = reinterpret_cast<const u32*>(base) + kv::param_words(G);
+            for (int p = 0; p < P; ++p) {
+                u32 kp0[G], kp1[G];
+                params_of(p, g, 0, kp0);
+                params_of(p, g + 8, 0, kp1);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if constexpr (G == 2) {
-                        const uint4 x = *reinterpret_cast<const uint4*>(pp + (g + 8 * h) * 4);
-                        pw[h][0] = x.x; pw[h][1] = x.y; pw[h][2] = x.z; pw[h][3] = x.w;
-                    } else {
-                        const uint2 x = *reinterpret_cast<const uint2*>(pp + (g + 8 * h) * 2);
-                        pw[h][0] = x.x; pw[h][1] = x.y;
-                    }
-                }
-            }
-            const bool whole = tile * kv::TILE >= all_lo && (tile + 1) * kv::TILE <= all_hi;      // every row sees every token
-            if (!whole) {                               // places that no token was written to may hold anything, NaN too
-#pragma unroll
-                for (int x = 0; x < 2 * G; ++x) {
-                    if (j0 >= rq.len) pw[0][x] = 0u;
-                    if (j1 >= rq.len) pw[1][x] = 0u;
-                }
-            }
-            // ---- logits: element e of an accumulator is token (e < 2 ? j0 : j1), column 2 t + e % 2
-            float s[NT][4];
-#pragma unroll
-            for (int gr = 0; gr < G; ++gr) {
-                const uint4 kw = *reinterpret_cast<const uint4*>(base + gr * 512 + lane * 16);
-                float a[NT][4];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) { a[nt][0] = a[nt][2] = q0[nt][gr][0]; a[nt][1] = a[nt][3] = q0[nt][gr][1]; }
-                auto step = [&](int st, u32 a0, u32 a1, u32 a2, u32 a3) {
+                for (int gr = 0; gr < G; ++gr) {
+                    const uint4 kw = *reinterpret_cast<const uint4*>(base[p] + gr * 512 + lane * 16);
+                    float a[NT][4];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int x = QS - 1; x >= 0; --x) mma16816(a[nt], a0, a1, a2, a3, qf[nt][gr][x][2 * st], qf[nt][gr][x][2 * st + 1]);
-                };
-                step(0, code_pair<0, Cfg::F32>(kw.x), code_pair<0, Cfg::F32>(kw.z), code_pair<1, Cfg::F32>(kw.x), code_pair<1, Cfg::F32>(kw.z));
-                step(1, code_pair<2, Cfg::F32>(kw.x), code_pair<2, Cfg::F32>(kw.z), code_pair<3, Cfg::F32>(kw.x), code_pair<3, Cfg::F32>(kw.z));
-                step(2, code_pair<0, Cfg::F32>(kw.y), code_pair<0, Cfg::F32>(kw.w), code_pair<1, Cfg::F32>(kw.y), code_pair<1, Cfg::F32>(kw.w));
-                step(3, code_pair<2, Cfg::F32>(kw.y), code_pair<2, Cfg::F32>(kw.w), code_pair<3, Cfg::F32>(kw.y), code_pair<3, Cfg::F32>(kw.w));
-                const float2 p0 = half2_at(pw[0][gr]), p1 = half2_at(pw[1][gr]);
-                const float w0 = Cfg::F32 ? fmaf(8.f, p0.x, p0.y) : p0.y, w1 = Cfg::F32 ? fmaf(8.f, p1.x, p1.y) : p1.y;
+                        for (int e = 0; e < 4; ++e) a[nt][e] = Cfg::F32 ? 0.f : q64[nt][gr][e & 1];
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {                // words 0, 2 hold the dimensions of steps 0, 1, words 1, 3 of 2, 3
+                        u32 x[4], y[4];
+                        if constexpr (Cfg::F32) {
+                            code_pairs<true>(half ? kw.y : kw.x, x);
+                            code_pairs<true>(half ? kw.w : kw.z, y);
+                        } else {
+                            code_pairs_64(half ? kw.y : kw.x, x);
+                            code_pairs_64(half ? kw.w : kw.z, y);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int i = QS - 1; i >= 0; --i)
+                                    mma16816<Cfg::F32>(a[nt], x[2 * k], y[2 * k], x[2 * k + 1], y[2 * k + 1], qf[nt][gr][i][4 * half + 2 * k],
+                                                       qf[nt][gr][i][4 * half + 2 * k + 1]);
+                    }
+                    // scale and zero point; the sum of q is -1/64 of q64
+                    const float2 p0 = half2_at(kp0[gr]), p1 = half2_at(kp1[gr]);
+                    const float z0 = (Cfg::F32 ? fmaf(8.f, p0.x, p0.y) : p0.y) * -0.015625f, z1 = (Cfg::F32 ? fmaf(8.f, p1.x, p1.y) : p1.y) * -0.015625f;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float z = e < 2 ? z0 : z1, q1 = q64[nt][gr][e & 1];
+                            s[p][nt][e] = fmaf(e < 2 ? p0.x : p1.x, a[nt][e], gr == 0 ? z * q1 : fmaf(z, q1, s[p][nt][e]));
+                        }
+                }
+            }
+            // above the reference, in powers of two
+            float above[P][NT][4], top = -INFINITY;
+#pragma unroll
+            for (int p = 0; p < P; ++p)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float z = e < 2 ? w0 : w1, q1 = qsum[nt][gr][e & 1];
-                        s[nt][e] = fmaf(e < 2 ? p0.x : p1.x, a[nt][e], gr == 0 ? z * q1 : fmaf(z, q1, s[nt][e]));
+                        above[p][nt][e] = fmaf(s[p][nt][e], sc[nt][e & 1], -m[nt][e & 1]);
+                        if constexpr (!whole) {
+                            const int j = (tile + p) * kv::TILE + g + (e < 2 ? 0 : 8);
+                            if (j < see_lo[nt][e & 1] || j >= see_hi[nt][e & 1]) above[p][nt][e] = -INFINITY;
+                        }
+                        top = fmaxf(top, above[p][nt][e]);
                     }
-            }
-            bool raise = false;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[nt][e] *= A.scale2;
-                    if (!whole) {
-                        const int j = e < 2 ? j0 : j1;
-                        if (j < see_lo[nt][e & 1] || j >= see_hi[nt][e & 1]) s[nt][e] = -INFINITY;
-                    }
-                    raise |= s[nt][e] > m[nt][e & 1] + 8.f;
-                }
-            if (__any_sync(~0u, raise)) {
+            if (__any_sync(~0u, top > Cfg::RAISE)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        float x = fmaxf(s[nt][c], s[nt][2 + c]);
+                        float x = -INFINITY;
+#pragma unroll
+                        for (int p = 0; p < P; ++p)
+#pragma unroll
+                            for (int e = c; e < 4; e += 2)
+                                if (above[p][nt][e] != -INFINITY) x = fmaxf(x, s[p][nt][e] * sc[nt][c]);
                         x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
                         x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
                         x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
-                        if (!(x > m[nt][c] + 8.f)) x = m[nt][c];       // each query row by itself: rows do not influence each other
+                        // each query row by itself: rows do not influence each other
+                        if (x > m[nt][c] + Cfg::RAISE) x -= Cfg::BELOW; else x = m[nt][c];
                         const float f = kv_exp2(m[nt][c] - x);
                         m[nt][c] = x;
+#pragma unroll
+                        for (int p = 0; p < P; ++p)
+#pragma unroll
+                            for (int e = c; e < 4; e += 2)
+                                if (above[p][nt][e] != -INFINITY) above[p][nt][e] = fmaf(s[p][nt][e], sc[nt][c], -x);
                         l[nt][c] *= f;
 #pragma unroll
                         for (int gr = 0; gr < G; ++gr) {
@@ -394,61 +516,113 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                     }
             }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[nt][e] = kv_exp2(s[nt][e] - m[nt][e & 1]);
-                    l[nt][e & 1] += s[nt][e];
-                }
-            // ---- values
-#pragma unroll
-            for (int gr = 0; gr < G; ++gr) {
-                const float2 p0 = half2_at(pw[0][G + gr]), p1 = half2_at(pw[1][G + gr]);
-                const float f = Cfg::F32 ? 8.f : (g & 1) ? 31.f : -16.f;                  // tokens j0 and j1 are of g's parity
-                const float w0 = fmaf(f, p0.x, p0.y), w1 = fmaf(f, p1.x, p1.y);
-                u32 b[NT][PS][2];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float x[4];
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        corr[nt][gr][e & 1] = fmaf(s[nt][e], e < 2 ? w0 : w1, corr[nt][gr][e & 1]);
-                        x[e] = s[nt][e] * (e < 2 ? p0.x : p1.x);
+                        s[p][nt][e] = kv_exp2(above[p][nt][e]);
+                        l[nt][e & 1] += s[p][nt][e];
                     }
+            // values
 #pragma unroll
-                    for (int k = 0; k < PS; ++k) {
-                        const u32 h0 = pack_bf16(x[0], x[1]), h1 = pack_bf16(x[2], x[3]);
-                        b[nt][k][0] = transpose8x8(h0);
-                        b[nt][k][1] = transpose8x8(h1);
-                        if (k + 1 < PS) {
-                            x[0] -= __uint_as_float(h0 << 16); x[1] -= __uint_as_float(h0 & 0xffff0000u);
-                            x[2] -= __uint_as_float(h1 << 16); x[3] -= __uint_as_float(h1 & 0xffff0000u);
+            for (int p = 0; p < P; ++p) {
+                if constexpr (Cfg::F32) {
+                    u32 vp0[G], vp1[G];
+                    params_of(p, g, G, vp0);
+                    params_of(p, g + 8, G, vp1);
+#pragma unroll
+                    for (int gr = 0; gr < G; ++gr) {
+                        const float2 p0 = half2_at(vp0[gr]), p1 = half2_at(vp1[gr]);
+                        const float z0 = fmaf(8.f, p0.x, p0.y), z1 = fmaf(8.f, p1.x, p1.y);
+                        u32 b[NT][PS][2];
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            float x[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                corr[nt][gr][e & 1] = fmaf(s[p][nt][e], e < 2 ? z0 : z1, corr[nt][gr][e & 1]);
+                                x[e] = s[p][nt][e] * (e < 2 ? p0.x : p1.x);
+                            }
+#pragma unroll
+                            for (int k = 0; k < PS; ++k) {
+                                const u32 h0 = pack_bf16(x[0], x[1]), h1 = pack_bf16(x[2], x[3]);
+                                b[nt][k][0] = transpose8x8(h0);
+                                b[nt][k][1] = transpose8x8(h1);
+                                x[0] -= __uint_as_float(h0 << 16); x[1] -= __uint_as_float(h0 & 0xffff0000u);
+                                x[2] -= __uint_as_float(h1 << 16); x[3] -= __uint_as_float(h1 & 0xffff0000u);
+                            }
+                        }
+                        const uint4 vw = *reinterpret_cast<const uint4*>(base[p] + (G + gr) * 512 + lane * 16);
+                        u32 e0[4], e1[4], o0[4], o1[4];                    // even and odd dimensions of the lower and upper two tokens
+                        code_pairs<true>(__byte_perm(vw.x, vw.y, 0x5410), e0);
+                        code_pairs<true>(__byte_perm(vw.x, vw.y, 0x7632), o0);
+                        code_pairs<true>(__byte_perm(vw.z, vw.w, 0x5410), e1);
+                        code_pairs<true>(__byte_perm(vw.z, vw.w, 0x7632), o1);
+#pragma unroll
+                        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                                for (int k = PS - 1; k >= 0; --k) mma16816<true>(x, e0[mt], o0[mt], e1[mt], o1[mt], b[nt][k][0], b[nt][k][1]);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) acc[nt][gr][mt][e] += x[e];
+                            }
+                    }
+                } else {
+                    u32 b[NT][2], w[4][G];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        b[nt][0] = transpose8x8(pack_half(s[p][nt][0], s[p][nt][1]));
+                        b[nt][1] = transpose8x8(pack_half(s[p][nt][2], s[p][nt][3]));
+                    }
+                    params_of(p, 2 * t, G, w[0]);
+                    params_of(p, 2 * t + 1, G, w[1]);
+                    params_of(p, 2 * t + 8, G, w[2]);
+                    params_of(p, 2 * t + 9, G, w[3]);
+#pragma unroll
+                    for (int gr = 0; gr < G; ++gr) {
+                        const u32 s0 = __byte_perm(w[0][gr], w[1][gr], 0x5410), z0 = hfma2(s0, 0x48004800u, __byte_perm(w[0][gr], w[1][gr], 0x7632));
+                        const u32 s1 = __byte_perm(w[2][gr], w[3][gr], 0x5410), z1 = hfma2(s1, 0x48004800u, __byte_perm(w[2][gr], w[3][gr], 0x7632));
+                        const uint4 vw = *reinterpret_cast<const uint4*>(base[p] + (G + gr) * 512 + lane * 16);
+                        u32 e0[4], e1[4], o0[4], o1[4];
+                        code_pairs<false>(__byte_perm(vw.x, vw.y, 0x5410), e0);
+                        code_pairs<false>(__byte_perm(vw.x, vw.y, 0x7632), o0);
+                        code_pairs<false>(__byte_perm(vw.z, vw.w, 0x5410), e1);
+                        code_pairs<false>(__byte_perm(vw.z, vw.w, 0x7632), o1);
+#pragma unroll
+                        for (int mt = 0; mt < 4; ++mt) {
+                            const u32 a0 = hfma2(e0[mt], s0, z0), a1 = hfma2(o0[mt], s0, z0), a2 = hfma2(e1[mt], s1, z1), a3 = hfma2(o1[mt], s1, z1);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma16816<false>(acc[nt][gr][mt], a0, a1, a2, a3, b[nt][0], b[nt][1]);
                         }
                     }
                 }
-                const uint4 vw = *reinterpret_cast<const uint4*>(base + (G + gr) * 512 + lane * 16);
-                const u32 e0 = __byte_perm(vw.x, vw.y, 0x5410), o0 = __byte_perm(vw.x, vw.y, 0x7632);
-                const u32 e1 = __byte_perm(vw.z, vw.w, 0x5410), o1 = __byte_perm(vw.z, vw.w, 0x7632);
-                auto step = [&](int mt, u32 a0, u32 a1, u32 a2, u32 a3) {
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        if constexpr (Cfg::F32) {
-                            float x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                            for (int k = PS - 1; k >= 0; --k) mma16816(x, a0, a1, a2, a3, b[nt][k][0], b[nt][k][1]);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[nt][gr][mt][e] += x[e];
-                        } else {
-#pragma unroll
-                            for (int k = 0; k < PS; ++k) mma16816(acc[nt][gr][mt], a0, a1, a2, a3, b[nt][k][0], b[nt][k][1]);
-                        }
-                    }
-                };
-                step(0, code_pair<0, Cfg::F32>(e0), code_pair<0, Cfg::F32>(o0), code_pair<0, Cfg::F32>(e1), code_pair<0, Cfg::F32>(o1));
-                step(1, code_pair<1, Cfg::F32>(e0), code_pair<1, Cfg::F32>(o0), code_pair<1, Cfg::F32>(e1), code_pair<1, Cfg::F32>(o1));
-                step(2, code_pair<2, Cfg::F32>(e0), code_pair<2, Cfg::F32>(o0), code_pair<2, Cfg::F32>(e1), code_pair<2, Cfg::F32>(o1));
-                step(3, code_pair<3, Cfg::F32>(e0), code_pair<3, Cfg::F32>(o0), code_pair<3, Cfg::F32>(e1), code_pair<3, Cfg::F32>(o1));
             }
+        };
+
+        int stage = 0;
+        for (int tile = t_lo; tile < t_hi; tile += Cfg::PAIR) {
+            cp_wait<STAGES - Cfg::PAIR>();
+            __syncwarp();
+            unsigned char* base[Cfg::PAIR];
+            u32 there = 0;
+#pragma unroll
+            for (int p = 0; p < Cfg::PAIR; ++p) {
+                base[p] = ring + stage * TB;
+                there |= (tile + p < t_hi && ((present >> stage) & 1u)) ? 1u << p : 0u;
+                if (++stage == STAGES) stage = 0;
+            }
+            if (there == (1u << Cfg::PAIR) - 1u && tile * kv::TILE >= all_lo && (tile + Cfg::PAIR) * kv::TILE <= all_hi) {
+                use_tiles(tile, base, Const<Cfg::PAIR>(), Const<1>());
+            } else {
+                for (int p = 0; p < Cfg::PAIR; ++p)
+                    if (there >> p & 1u) use_tiles(tile + p, base + p, Const<1>(), Const<0>());
+            }
+            __syncwarp();
+#pragma unroll
+            for (int p = 0; p < Cfg::PAIR; ++p) issue();
         }
         cp_wait<0>();
         __syncwarp();
@@ -461,8 +635,10 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) {
                     l[nt][c] += __shfl_xor_sync(~0u, l[nt][c], d);
+                    if constexpr (Cfg::F32) {
 #pragma unroll
-                    for (int gr = 0; gr < G; ++gr) corr[nt][gr][c] += __shfl_xor_sync(~0u, corr[nt][gr][c], d);
+                        for (int gr = 0; gr < G; ++gr) corr[nt][gr][c] += __shfl_xor_sync(~0u, corr[nt][gr][c], d);
+                    }
                 }
         const bool complete = sb >= wa && se <= wb;
         const int slot = sb < wa ? 0 : 1;
@@ -481,8 +657,8 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                     float x[8];
 #pragma unroll
                     for (int mt = 0; mt < 4; ++mt) {
-                        x[2 * mt] = acc[nt][gr][mt][c] + corr[nt][gr][c];
-                        x[2 * mt + 1] = acc[nt][gr][mt][2 + c] + corr[nt][gr][c];
+                        x[2 * mt] = acc[nt][gr][mt][c] + (Cfg::F32 ? corr[nt][gr][c] : 0.f);
+                        x[2 * mt + 1] = acc[nt][gr][mt][2 + c] + (Cfg::F32 ? corr[nt][gr][c] : 0.f);
                     }
                     if (complete) {
 #pragma unroll
@@ -524,46 +700,47 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
         const KvRequest rq = kv_request(A, p.r);
         return min(ROWS, rq.n * A.ratio - p.rb * ROWS);
     };
+    // lane k has the segment of piece k: where it differs from the piece before, the parts of another segment begin
+    static_assert(2 * WARPS <= 32, "a lane per piece");
+    const bool held = lane < 2 * WARPS && piece_of[lane >> 1][lane & 1].valid;
+    const ull begin = held ? piece_of[lane >> 1][lane & 1].begin : 0;
+    const u32 pieces = __ballot_sync(~0u, held);
+    const u32 earlier = pieces & ((1u << lane) - 1u);
+    const ull begin_before = __shfl_sync(~0u, begin, earlier ? 31 - __clz(earlier) : lane);
+    u32 starts = __ballot_sync(~0u, held && (!earlier || begin_before != begin));
+    if (held) order[warp][__popc(earlier)] = (unsigned char)lane;
+    __syncwarp();
     PieceOf open[2];                                     // segments cut between CTAs: the one that began before, the one that goes on
     open[0].valid = open[1].valid = 0;
     int task = 0;
-    for (int k = 0; k < 2 * WARPS;) {
+    while (starts) {
+        const int k = __ffs(starts) - 1;
+        starts &= starts - 1u;
+        const int first = __popc(pieces & ((1u << k) - 1u));
+        const int n = __popc(starts ? pieces & ((starts & -starts) - 1u) : pieces) - first;
         const PieceOf p = piece_of[k >> 1][k & 1];
-        if (!p.valid) { ++k; continue; }
-        // the parts of this segment: slot k, then the first slots of the following warps
-        int list_n = 1, kk = k + 1;
-        int ks[WARPS + 1];
-        ks[0] = k;
-        for (; kk < 2 * WARPS; ++kk) {
-            const PieceOf& q = piece_of[kk >> 1][kk & 1];
-            if (!q.valid) continue;
-            if (q.begin != p.begin) break;
-            ks[list_n++] = kk;
-        }
         const bool inside = p.begin >= ca && p.end <= cb;
         const int slot = p.begin < ca ? 0 : 1;
         if (!inside) open[slot] = p;
         const int rows = rows_of(p);
         for (int c = 0; c < rows; ++c, ++task)
             if (task % WARPS == warp)
-                join_row<T, D, ROWS, false>(A, p.r, p.hk, p.rb * ROWS + c, list_n, [&](int i) { return smem_piece(ks[i]); },
-                                            inside ? nullptr : part(cta, slot));
-        k = kk;
+                join_row<T, D, ROWS, false>(A, p.r, p.hk, p.rb * ROWS + c, n,
+                                            [&](int i) { return smem_piece(order[warp][first + i]); }, inside ? nullptr : part(cta, slot));
     }
     if (!open[0].valid && !open[1].valid) return;        // the same for the whole CTA
     __syncthreads();
     if (tid < 2 && open[tid].valid) {
-        const int c0 = cta_of(open[tid].begin, U, C), c1 = cta_of(open[tid].end - 1, U, C);
-        __threadfence();
-        const u32 before = atomicAdd(counters + c0, 1u);
+        const int c0 = (int)(open[tid].begin / share), c1 = (int)((open[tid].end - 1) / share);
+        u32 before;                                       // releases this CTA's parts (ordered before it by the barrier), acquires the others'
+        asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(counters + c0) : "memory");
         last_of[tid] = before == (u32)(c1 - c0);
-        if (last_of[tid]) counters[c0] = 0u;             // ready for the next call
-        __threadfence();
+        if (last_of[tid]) counters[c0] = 0u;              // ready for the next call
     }
     __syncthreads();
     for (int s = 0; s < 2; ++s) {
         if (!open[s].valid || !last_of[s]) continue;
-        const int c0 = cta_of(open[s].begin, U, C), c1 = cta_of(open[s].end - 1, U, C);
+        const int c0 = (int)(open[s].begin / share), c1 = (int)((open[s].end - 1) / share);
         const int rows = rows_of(open[s]);
         for (int c = warp; c < rows; c += WARPS)
             join_row<T, D, ROWS, true>(A, open[s].r, open[s].hk, open[s].rb * ROWS + c, c1 - c0 + 1,
@@ -575,14 +752,27 @@ constexpr int MAX_CTAS = 256;
 constexpr int MAX_PIECE = 16 * (128 + 2) * 4;
 
 template <typename T, int G, int NT>
-int launch(const KvAttnArgs& A, void* workspace, int ctas, cudaStream_t st) {
+int launch(const KvAttnArgs& A, void* workspace, int device, int ctas, cudaStream_t st) {
     typedef StreamCfg<T, G, NT> Cfg;
+    constexpr int MAX_SMEM = Cfg::WARPS * Cfg::WARP_BYTES + (POP_KV_MAX_REQUESTS + 1) * 8;
     static_assert(Cfg::PIECE <= MAX_PIECE, "workspace");
-    const size_t smem = (size_t)Cfg::WARPS * Cfg::WARP_BYTES + (size_t)(A.R + 1) * 8;
-    static_assert((size_t)Cfg::WARPS * Cfg::WARP_BYTES + (POP_KV_MAX_REQUESTS + 1) * 8 <= 225 * 1024, "shared memory");
-    POP_CUDA(cudaFuncSetAttribute(kv_stream_kernel<T, G, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  (int)(Cfg::WARPS * Cfg::WARP_BYTES + (POP_KV_MAX_REQUESTS + 1) * 8)));
-    kv_stream_kernel<T, G, NT><<<ctas, Cfg::WARPS * 32, smem, st>>>(A, (u32*)workspace, (float*)((char*)workspace + MAX_CTAS * 4));
+    static_assert(MAX_SMEM <= 225 * 1024, "shared memory");
+    static bool ready[64];                                     // set once per device; setting it twice does no harm
+    if (device >= 64 || !ready[device]) {
+        POP_CUDA(cudaFuncSetAttribute(kv_stream_kernel<T, G, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM));
+        if (device < 64) ready[device] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(Cfg::WARPS * 32);
+    cfg.dynamicSmemBytes = (size_t)Cfg::WARPS * Cfg::WARP_BYTES + (size_t)(A.R + 1) * 8;
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    POP_CUDA(cudaLaunchKernelEx(&cfg, kv_stream_kernel<T, G, NT>, A, (u32*)workspace, (float*)((char*)workspace + MAX_CTAS * 4)));
     POP_LAUNCHED();
     return POP_OK;
 }
@@ -592,18 +782,23 @@ int launch(const KvAttnArgs& A, void* workspace, int ctas, cudaStream_t st) {
 size_t pop_kv_stream_workspace() { return MAX_CTAS * 4 + (size_t)MAX_CTAS * 2 * MAX_PIECE; }
 
 int pop_launch_kv_attention_stream(const KvAttnArgs& A, int head_dim, pop_dtype_t dtype, void* workspace, cudaStream_t st) {
-    int device = 0, sms = 0;
+    int device = 0;
     POP_CUDA(cudaGetDevice(&device));
-    POP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+    static int sms_of[64];                                     // asked for once per device
+    int sms = device < 64 ? sms_of[device] : 0;
+    if (!sms) {
+        POP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+        if (device < 64) sms_of[device] = sms;
+    }
     const int ctas = sms < MAX_CTAS ? sms : MAX_CTAS;
     // 8 query rows share one pass over the codes; a second set of 8 costs products only, so it pays as soon as the average request
     // has more than 8 rows
     const bool wide = (long long)((A.T + A.R - 1) / A.R) * A.ratio > 8;
     if (dtype == POP_BF16) {
         typedef __nv_bfloat16 T;
-        if (head_dim == 64) return wide ? launch<T, 1, 2>(A, workspace, ctas, st) : launch<T, 1, 1>(A, workspace, ctas, st);
-        return wide ? launch<T, 2, 2>(A, workspace, ctas, st) : launch<T, 2, 1>(A, workspace, ctas, st);
+        if (head_dim == 64) return wide ? launch<T, 1, 2>(A, workspace, device, ctas, st) : launch<T, 1, 1>(A, workspace, device, ctas, st);
+        return wide ? launch<T, 2, 2>(A, workspace, device, ctas, st) : launch<T, 2, 1>(A, workspace, device, ctas, st);
     }
-    if (head_dim == 64) return wide ? launch<float, 1, 2>(A, workspace, ctas, st) : launch<float, 1, 1>(A, workspace, ctas, st);
-    return wide ? launch<float, 2, 2>(A, workspace, ctas, st) : launch<float, 2, 1>(A, workspace, ctas, st);
+    if (head_dim == 64) return wide ? launch<float, 1, 2>(A, workspace, device, ctas, st) : launch<float, 1, 1>(A, workspace, device, ctas, st);
+    return wide ? launch<float, 2, 2>(A, workspace, device, ctas, st) : launch<float, 2, 1>(A, workspace, device, ctas, st);
 }
