@@ -59,8 +59,10 @@ template <typename T, int G, int NT> struct StreamCfg {
 
 template <int N> struct Const { static constexpr int value = N; };
 
-// Kept per piece: which segment it is a part of.
-struct PieceOf { ull begin, end; int r, hk, rb, valid; };
+// Kept per piece: the segment it is a part of (its units, its query rows and where they go).
+struct PieceOf { ull begin, end; int rows, row0, q0, hk, valid; };
+
+__device__ __forceinline__ ull div_units(ull a, ull b) { return (a | b) >> 32 ? a / b : (ull)((u32)a / (u32)b); }
 
 __device__ __forceinline__ void cp16(u32 dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -144,44 +146,41 @@ template <int ROWS> __device__ __forceinline__ Tiles request_tiles(const KvAttnA
     return t;
 }
 
-// Joins n parts of one query row (part k at at(k)); the result goes to the part `to`, or, where that is NULL, to the output.  Maxima
-// and sums are read by a lane for each part, the outputs by a lane for every D / 32 dimensions, many parts on their way at once:
-// parts of other CTAs are a trip to L2 away.
+// Joins n parts (part k at at(k)) of a segment's query row `col`; the result goes to the part `to`, or, where that is NULL, to the
+// output.  Parts of other CTAs are a trip to L2 away, so sixteen parts' maxima, sums and outputs are all on their way at once.
 template <typename T, int D, int ROWS, bool GLOBAL, typename At>
-__device__ __forceinline__ void join_row(const KvAttnArgs& A, int r, int hk, int row, int n, At at, float* to) {
-    constexpr int PER = D / 32, BATCH = 8;
+__device__ __forceinline__ void join_row(const KvAttnArgs& A, const PieceOf& seg, int col, int n, At at, float* to) {
+    constexpr int PER = D / 32, BATCH = 16;
     typedef typename std::conditional<PER == 4, float4, float2>::type Vec;
-    const int lane = threadIdx.x & 31, col = row % ROWS;
-    auto stats = [&](int k) {
-        const float2* p = reinterpret_cast<const float2*>(at(k) + ROWS * D + 2 * col);
-        return GLOBAL ? __ldcg(p) : *p;
-    };
+    const int lane = threadIdx.x & 31;
     float m = -1e30f, l = 0.f, o[PER] = {};
-    float2 mine = lane < n ? stats(lane) : make_float2(-1e30f, 0.f);
-    m = mine.x;
-    for (int k = lane + 32; k < n; k += 32) m = fmaxf(m, stats(k).x);
+    for (int k0 = 0; k0 < n; k0 += BATCH) {
+        const int end = min(BATCH, n - k0);
+        const float2* sp = reinterpret_cast<const float2*>(at(k0 + min(lane, end - 1)) + ROWS * D + 2 * col);
+        float2 st = GLOBAL ? __ldcg(sp) : *sp;                             // lane k: maximum and sum of part k0 + k
+        Vec x[BATCH];
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
-    for (int k0 = 0; k0 < n; k0 += 32) {
-        if (k0) mine = k0 + lane < n ? stats(k0 + lane) : make_float2(-1e30f, 0.f);
-        const float f = kv_exp2(mine.x - m);
-        l = fmaf(mine.y, f, l);
-        const int end = min(32, n - k0);
-        for (int k = 0; k < end; k += BATCH) {
-            Vec x[BATCH];
+        for (int b = 0; b < BATCH; ++b) {
+            const Vec* p = reinterpret_cast<const Vec*>(at(k0 + min(b, end - 1)) + col * D) + lane;
+            x[b] = GLOBAL ? __ldcg(p) : *p;
+        }
+        if (lane >= end) st = make_float2(-1e30f, 0.f);
+        float top = st.x;
 #pragma unroll
-            for (int b = 0; b < BATCH; ++b) {
-                const Vec* p = reinterpret_cast<const Vec*>(at(k0 + min(k + b, end - 1)) + col * D) + lane;
-                x[b] = GLOBAL ? __ldcg(p) : *p;
-            }
+        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+        top = fmaxf(top, m);
+        const float old = kv_exp2(m - top), f = lane < end ? kv_exp2(st.x - top) : 0.f;
+        m = top;
+        l = fmaf(l, old, st.y * f);                                         // each lane's own part of the sum
 #pragma unroll
-            for (int b = 0; b < BATCH; ++b) {
-                const float w = __shfl_sync(~0u, f, min(k + b, 31));
-                if (k + b < end) {
-                    const float* y = reinterpret_cast<const float*>(&x[b]);
+        for (int e = 0; e < PER; ++e) o[e] *= old;
 #pragma unroll
-                    for (int e = 0; e < PER; ++e) o[e] = fmaf(y[e], w, o[e]);
-                }
+        for (int b = 0; b < BATCH; ++b) {
+            const float w = __shfl_sync(~0u, f, b);
+            if (b < end) {
+                const float* y = reinterpret_cast<const float*>(&x[b]);
+#pragma unroll
+                for (int e = 0; e < PER; ++e) o[e] = fmaf(y[e], w, o[e]);
             }
         }
     }
@@ -192,8 +191,8 @@ __device__ __forceinline__ void join_row(const KvAttnArgs& A, int r, int hk, int
         if (lane == 0) *reinterpret_cast<float2*>(to + ROWS * D + 2 * col) = make_float2(m, l);
         return;
     }
-    const int i = row / A.ratio;
-    const size_t out_at = (size_t)(A.indptr[r] + i) * A.H + hk * A.ratio + (row - i * A.ratio);
+    const int row = seg.row0 + col, i = row / A.ratio;
+    const size_t out_at = (size_t)(seg.q0 + i) * A.H + seg.hk * A.ratio + (row - i * A.ratio);
     const float inv = l == 0.f ? 0.f : 1.f / l;
     T* out = (T*)A.out + out_at * D + lane * PER;
     if constexpr (sizeof(T) == 4) {
@@ -251,7 +250,7 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
     }
     __syncthreads();
     // units of a CTA (the last one may have fewer, further ones none)
-    const ull share = U >> 32 ? (U + gridDim.x - 1) / gridDim.x : (ull)(((u32)U + gridDim.x - 1) / gridDim.x);
+    const ull share = div_units(U + gridDim.x - 1, gridDim.x);
     const int cta = blockIdx.x;
     const ull ca = cta * share;
     if (ca >= U) return;
@@ -276,7 +275,7 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
         const KvRequest rq = kv_request(A, r);
         const Tiles ti = request_tiles<ROWS>(A, rq);
         const ull into = u - prefix[r];
-        const int seg = into >> 32 ? (int)(into / ti.count) : (int)((u32)into / (u32)ti.count), hk = seg / ti.row_blocks, rb = seg - hk * ti.row_blocks;
+        const int seg = (int)div_units(into, ti.count), hk = seg / ti.row_blocks, rb = seg - hk * ti.row_blocks;
         const ull sb = prefix[r] + (ull)seg * ti.count, se = sb + ti.count;
         const ull pe = min(se, wb);
         const int rows = min(ROWS, rq.n * A.ratio - rb * ROWS), row0 = rb * ROWS;
@@ -320,6 +319,19 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
             }
             cp_commit();
         };
+        // the query rows are asked for before the tiles, behind which they would have to queue
+        constexpr int VECS = 16 / Elem<T>::VEC;
+        uint4 q_raw[NT][G][VECS];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const bool in = nt * 8 + g < rows;
+            const int row = row0 + (in ? nt * 8 + g : 0), i = row / A.ratio;
+            const T* qp = (const T*)A.q + (size_t)(rq.q0 + i) * A.q_stride + (size_t)(hk * A.ratio + row - i * A.ratio) * D + 16 * t;
+#pragma unroll
+            for (int gr = 0; gr < G; ++gr)
+#pragma unroll
+                for (int v = 0; v < VECS; ++v) q_raw[nt][gr][v] = *reinterpret_cast<const uint4*>(qp + gr * 64 + v * Elem<T>::VEC);
+        }
 #pragma unroll
         for (int s = 0; s < STAGES; ++s) issue();
 
@@ -329,18 +341,14 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
         int see_lo[NT][2], see_hi[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int row = row0 + nt * 8 + g;
             const bool in = nt * 8 + g < rows;
-            const int i = row / A.ratio;
-            const T* qp = (const T*)A.q + (size_t)(rq.q0 + (in ? i : 0)) * A.q_stride + (size_t)(hk * A.ratio + (in ? row - i * A.ratio : 0)) * D + 16 * t;
             float x[G][16], f = 1.f;
 #pragma unroll
             for (int gr = 0; gr < G; ++gr)
 #pragma unroll
-                for (int v = 0; v < 16 / Elem<T>::VEC; ++v) {
-                    const uint4 raw = *reinterpret_cast<const uint4*>(qp + gr * 64 + v * Elem<T>::VEC);
+                for (int v = 0; v < VECS; ++v) {
                     float y[Elem<T>::VEC];
-                    Elem<T>::unpack(raw, y);
+                    Elem<T>::unpack(q_raw[nt][gr][v], y);
 #pragma unroll
                     for (int e = 0; e < Elem<T>::VEC; ++e) x[gr][v * Elem<T>::VEC + e] = in ? y[e] : 0.f;
                 }
@@ -685,7 +693,7 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                     }
                 }
             }
-        if (!complete && lane == 0) piece_of[warp][slot] = {sb, se, r, hk, rb, 1};
+        if (!complete && lane == 0) piece_of[warp][slot] = {sb, se, rows, row0, rq.q0, hk, 1};
         u = pe;
     }
     __syncthreads();
@@ -696,10 +704,6 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
         return (const float*)((k & 1) ? b : b + STAGES * TB);
     };
     auto part = [&](int c, int slot) { return parts + ((size_t)c * 2 + slot) * (ROWS * (D + 2)); };
-    auto rows_of = [&](const PieceOf& p) {
-        const KvRequest rq = kv_request(A, p.r);
-        return min(ROWS, rq.n * A.ratio - p.rb * ROWS);
-    };
     // lane k has the segment of piece k: where it differs from the piece before, the parts of another segment begin
     static_assert(2 * WARPS <= 32, "a lane per piece");
     const bool held = lane < 2 * WARPS && piece_of[lane >> 1][lane & 1].valid;
@@ -722,16 +726,15 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
         const bool inside = p.begin >= ca && p.end <= cb;
         const int slot = p.begin < ca ? 0 : 1;
         if (!inside) open[slot] = p;
-        const int rows = rows_of(p);
-        for (int c = 0; c < rows; ++c, ++task)
+        for (int c = 0; c < p.rows; ++c, ++task)
             if (task % WARPS == warp)
-                join_row<T, D, ROWS, false>(A, p.r, p.hk, p.rb * ROWS + c, n,
+                join_row<T, D, ROWS, false>(A, p, c, n,
                                             [&](int i) { return smem_piece(order[warp][first + i]); }, inside ? nullptr : part(cta, slot));
     }
     if (!open[0].valid && !open[1].valid) return;        // the same for the whole CTA
     __syncthreads();
     if (tid < 2 && open[tid].valid) {
-        const int c0 = (int)(open[tid].begin / share), c1 = (int)((open[tid].end - 1) / share);
+        const int c0 = (int)div_units(open[tid].begin, share), c1 = (int)div_units(open[tid].end - 1, share);
         u32 before;                                       // releases this CTA's parts (ordered before it by the barrier), acquires the others'
         asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(counters + c0) : "memory");
         last_of[tid] = before == (u32)(c1 - c0);
@@ -740,10 +743,9 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
     __syncthreads();
     for (int s = 0; s < 2; ++s) {
         if (!open[s].valid || !last_of[s]) continue;
-        const int c0 = (int)(open[s].begin / share), c1 = (int)((open[s].end - 1) / share);
-        const int rows = rows_of(open[s]);
-        for (int c = warp; c < rows; c += WARPS)
-            join_row<T, D, ROWS, true>(A, open[s].r, open[s].hk, open[s].rb * ROWS + c, c1 - c0 + 1,
+        const int c0 = (int)div_units(open[s].begin, share), c1 = (int)div_units(open[s].end - 1, share);
+        for (int c = warp; c < open[s].rows; c += WARPS)
+            join_row<T, D, ROWS, true>(A, open[s], c, c1 - c0 + 1,
                                        [&](int k) { return (const float*)part(c0 + k, k == 0 ? 1 : 0); }, nullptr);
     }
 }
