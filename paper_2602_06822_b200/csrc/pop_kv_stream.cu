@@ -14,8 +14,9 @@
 // bits 0x5400 is 64 + c, c under 0x6400 is 1024 + c) and go through the tensor cores as mma.m16n8k16 operands: the codes as the
 // 16-row side (rows = tokens for the keys, dimensions for the values), the query rows as the 8 columns.  The memory format is made of
 // those fragments, so that a lane's 16-byte load is its operand, and 8 query heads cost what one does.
-//   Keys: 64 + c as they are, in sums that start at -64 sum(q); scale and zero point are applied to the sums, per token instead of
-//   per element:  q.k_j = sum over groups of  s q.c + z sum(q).  (What the accumulator's truncation leaves of the 64 is 1e-5 of a logit.)
+//   Keys: c + f as they are, f = 1024 or 64, in sums that start at -q.f; scale and zero point are applied to the sums, per token
+//   instead of per element:  q.k_j = sum over groups of  s q.c + z sum(q).  (What the accumulator's truncation leaves of the 1024 is the
+//   same for all keys but for some 1e-5 of a logit.)
 //   The query is fp16 too, each row times a power of two that puts its largest element at 2^10, which loses nothing of bf16.
 //   Values: c - 8 exactly by one addition per pair, then s (c - 8) + (z + 8 s) in fp16 (11 bits: 2^-12 of rounding against the
 //   result's 2^-9).  Here an offset must not stay: summed over the tokens it would grow with the context, and the result does not.
@@ -37,7 +38,7 @@ typedef unsigned long long ull;
 
 #ifndef KV_WARPS
 #define KV_WARPS 12
-#define KV_STAGES 5
+#define KV_STAGES 3
 #endif
 
 template <typename T, int G, int NT> struct StreamCfg {
@@ -47,14 +48,16 @@ template <typename T, int G, int NT> struct StreamCfg {
     static constexpr int PS = 3;                            // bf16 pieces of p s (fp32)
     static constexpr float RAISE = F32 ? 8.f : 15.f;        // the reference is raised when a logit is this far above it,
     static constexpr float BELOW = F32 ? 0.f : 7.f;         // to this far below the logit
-    // Tiles that a warp works on at once: two independent chains of products, reductions and exponentials where registers allow
-    static constexpr int PAIR = (NT == 1 && !F32) ? 2 : 1;
+    // Tiles of a unit, which a warp works on at once: two independent chains of products, reductions and exponentials where
+    // registers allow
+    static constexpr int STEP = (NT == 1 && !F32) ? 2 : 1;
+    static constexpr int TOKENS = STEP * kv::TILE;
     static constexpr int WARPS = (NT == 1 && !F32) ? KV_WARPS : 8;
-    static constexpr int TB = kv::tile_bytes(D);
+    static constexpr int TB = kv::tile_bytes(D), UB = STEP * TB;
     static constexpr int PIECE = ROWS * (D + 2) * 4;        // un-normalised output, maximum and sum of a part of a segment
-    static constexpr int MIN_STAGES = (PIECE + TB - 1) / TB;
-    static constexpr int STAGES = MIN_STAGES > (G == 1 ? 8 : KV_STAGES) ? MIN_STAGES : (G == 1 ? 8 : KV_STAGES);
-    static constexpr int WARP_BYTES = STAGES * TB + PIECE;  // ring (its memory later holds the second piece) and first piece
+    static constexpr int MIN_STAGES = (PIECE + UB - 1) / UB, WANT = (G == 1 ? 2 : 1) * (STEP == 2 ? KV_STAGES : 5);
+    static constexpr int STAGES = MIN_STAGES > WANT ? MIN_STAGES : WANT;
+    static constexpr int WARP_BYTES = STAGES * UB + PIECE;  // ring (its memory later holds the second piece) and first piece
 };
 
 template <int N> struct Const { static constexpr int value = N; };
@@ -70,14 +73,21 @@ __device__ __forceinline__ void cp16(u32 dst, const void* src) {
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-template <bool F32>                                          // operands: bf16 pieces for fp32 calls, fp16 for bf16 ones
-__device__ __forceinline__ void mma16816(float (&c)[4], u32 a0, u32 a1, u32 a2, u32 a3, u32 b0, u32 b1) {
+// d = a b + c; operands: bf16 pieces for fp32 calls, fp16 for bf16 ones.
+template <bool F32>
+__device__ __forceinline__ void mma16816(float (&d)[4], u32 a0, u32 a1, u32 a2, u32 a3, u32 b0, u32 b1, float c0, float c1, float c2, float c3) {
     if constexpr (F32)
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
     else
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
+template <bool F32>
+__device__ __forceinline__ void mma16816(float (&d)[4], u32 a0, u32 a1, u32 a2, u32 a3, u32 b0, u32 b1) {
+    mma16816<F32>(d, a0, a1, a2, a3, b0, b1, d[0], d[1], d[2], d[3]);
 }
 __device__ __forceinline__ u32 transpose8x8(u32 x) {
     u32 y;
@@ -107,12 +117,13 @@ __device__ __forceinline__ u32 mask_or(u32 x, u32 mask, u32 bits) {           //
     asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(x), "r"(mask), "r"(bits));
     return r;
 }
-// The four pairs of codes of a word as fp16 numbers 64 + c.
-__device__ __forceinline__ void code_pairs_64(u32 w, u32 (&x)[4]) {
-    x[0] = mask_or(w << 4, 0x00f000f0u, 0x54005400u);
+// The four pairs of codes of a word as fp16 numbers 1024 + c (pairs 0 and 2) and 64 + c (1 and 3).
+__device__ __forceinline__ void code_pairs_raw(u32 w, u32 (&x)[4]) {
+    const u32 v = w >> 8;
+    x[0] = mask_or(w, 0x000f000fu, 0x64006400u);
     x[1] = mask_or(w, 0x00f000f0u, 0x54005400u);
-    x[2] = mask_or(w >> 4, 0x00f000f0u, 0x54005400u);
-    x[3] = mask_or(w >> 8, 0x00f000f0u, 0x54005400u);
+    x[2] = mask_or(v, 0x000f000fu, 0x64006400u);
+    x[3] = mask_or(v, 0x00f000f0u, 0x54005400u);
 }
 // The same as numbers c - 8, in fp16 or bf16.
 template <bool F32> __device__ __forceinline__ void code_pairs(u32 w, u32 (&x)[4]) {
@@ -123,28 +134,32 @@ template <bool F32> __device__ __forceinline__ void code_pairs(u32 w, u32 (&x)[4
             asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(x[i]) : "r"(y), "r"(0x43084308u));
         }
     } else {
-        const u32 v = w >> 8;
-        x[0] = hadd2(mask_or(w, 0x000f000fu, 0x64006400u), 0xe408e408u);                         // 1024 + c - 1032
-        x[1] = hadd2(mask_or(w, 0x00f000f0u, 0x54005400u), 0xd480d480u);                         // 64 + c - 72
-        x[2] = hadd2(mask_or(v, 0x000f000fu, 0x64006400u), 0xe408e408u);
-        x[3] = hadd2(mask_or(v, 0x00f000f0u, 0x54005400u), 0xd480d480u);
+        code_pairs_raw(w, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = hadd2(x[i], i & 1 ? 0xd480d480u : 0xe408e408u);       // - 72, - 1032
     }
 }
 
 __device__ __forceinline__ float2 half2_at(u32 w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 
-// Tiles that any query of a request sees: [first, first + count), count >= 1 as every segment has a unit that writes its result.
-struct Tiles { int first, count, row_blocks; };
-template <int ROWS> __device__ __forceinline__ Tiles request_tiles(const KvAttnArgs& A, const KvRequest& q) {
-    Tiles t = {0, 0, 0};
+// Units (of TOKENS keys) that any query of a request sees: [first, first + count), count >= 1 as every segment has a unit that
+// writes its result.
+struct Units { int first, count, row_blocks; };
+template <int ROWS, int TOKENS> __device__ __forceinline__ Units request_units(const KvAttnArgs& A, const KvRequest& q) {
+    Units t = {0, 0, 0};
     const long long rows = (long long)q.n * A.ratio;
     if (q.n <= 0 || rows >= A.prompt_rows) return t;
     t.row_blocks = (int)((rows + ROWS - 1) / ROWS);
     const int lo = min(kv_first(A, q.pos0), q.len), hi = kv_end(A, q, q.pos0 + q.n - 1);
-    t.first = lo / kv::TILE;
-    t.count = max(1, (hi + kv::TILE - 1) / kv::TILE - t.first);
+    t.first = lo / TOKENS;
+    t.count = max(1, (hi + TOKENS - 1) / TOKENS - t.first);
     return t;
 }
+
+// The sums over the requests are kept for every request, or for every fourth one where there are more than 1024.
+constexpr int MAX_SUMS = 1024;
+__host__ __device__ constexpr int sums_shift(int R) { return R <= MAX_SUMS ? 0 : 2; }
+static_assert((POP_KV_MAX_REQUESTS >> 2) <= MAX_SUMS, "sums");
 
 // Joins n parts (part k at at(k)) of a segment's query row `col`; the result goes to the part `to`, or, where that is NULL, to the
 // output.  Parts of other CTAs are a trip to L2 away, so sixteen parts' maxima, sums and outputs are all on their way at once.
@@ -211,7 +226,7 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
     typedef StreamCfg<T, G, NT> Cfg;
     constexpr int D = Cfg::D, ROWS = Cfg::ROWS, WARPS = Cfg::WARPS, TB = Cfg::TB, STAGES = Cfg::STAGES, QS = Cfg::QS, PS = Cfg::PS;
     extern __shared__ __align__(16) unsigned char kv_smem[];
-    ull* prefix = reinterpret_cast<ull*>(kv_smem + (size_t)WARPS * Cfg::WARP_BYTES);        // [R + 1] units before request r
+    ull* sums = reinterpret_cast<ull*>(kv_smem + (size_t)WARPS * Cfg::WARP_BYTES);          // units before request r << sums_shift(R)
     __shared__ ull scan_sum[2][WARPS];
     __shared__ PieceOf piece_of[WARPS][2];
     __shared__ int last_of[2];
@@ -222,16 +237,17 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---- units before every request
-    if (tid == 0) prefix[0] = 0;
+    const int shift = sums_shift(A.R);
     if (lane < 2) piece_of[warp][lane].valid = 0;
     ull U = 0;
     for (int r0 = 0, turn = 0; r0 < A.R; r0 += WARPS * 32, turn ^= 1) {
         const int r = r0 + tid;
         ull v = 0;
         if (r < A.R) {
-            const Tiles ti = request_tiles<ROWS>(A, kv_request(A, r));
-            v = (ull)ti.count * ti.row_blocks * A.Hk;
+            const Units un = request_units<ROWS, Cfg::TOKENS>(A, kv_request(A, r));
+            v = (ull)un.count * un.row_blocks * A.Hk;
         }
+        const ull own = v;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const ull u = __shfl_up_sync(~0u, v, d);
@@ -239,14 +255,14 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
         }
         if (lane == 31) scan_sum[turn][warp] = v;
         __syncthreads();
-        v += U;
+        v += U - own;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
             const ull x = scan_sum[turn][w];
             if (w < warp) v += x;
             U += x;
         }
-        if (r < A.R) prefix[r + 1] = v;
+        if (r < A.R && (r & ((1 << shift) - 1)) == 0) sums[r >> shift] = v;
     }
     __syncthreads();
     // units of a CTA (the last one may have fewer, further ones none)
@@ -263,32 +279,37 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
 
     // ---- this warp's units, segment by segment
     int r = 0;
+    ull before = 0;                                                        // units before request r
     if (wa < wb) {
-        int hi = A.R;
+        int hi = ((A.R - 1) >> shift) + 1;
         while (hi - r > 1) {
             const int mid = (r + hi) >> 1;
-            if (prefix[mid] <= wa) r = mid; else hi = mid;
+            if (sums[mid] <= wa) r = mid; else hi = mid;
         }
+        before = sums[r];
+        r <<= shift;
     }
     for (ull u = wa; u < wb;) {
-        while (prefix[r + 1] <= u) ++r;
         const KvRequest rq = kv_request(A, r);
-        const Tiles ti = request_tiles<ROWS>(A, rq);
-        const ull into = u - prefix[r];
-        const int seg = (int)div_units(into, ti.count), hk = seg / ti.row_blocks, rb = seg - hk * ti.row_blocks;
-        const ull sb = prefix[r] + (ull)seg * ti.count, se = sb + ti.count;
+        const Units un = request_units<ROWS, Cfg::TOKENS>(A, rq);
+        const ull all = (ull)un.count * un.row_blocks * A.Hk;
+        if (before + all <= u) { before += all; ++r; continue; }
+        const int seg = (int)div_units(u - before, un.count), hk = seg / un.row_blocks, rb = seg - hk * un.row_blocks;
+        const ull sb = before + (ull)seg * un.count, se = sb + un.count;
         const ull pe = min(se, wb);
         const int rows = min(ROWS, rq.n * A.ratio - rb * ROWS), row0 = rb * ROWS;
-        // tiles of this part, less those that no row of the block sees
+        // units of this part, less those that no row of the block sees
         const int p_lo = rq.pos0 + row0 / A.ratio, p_hi = rq.pos0 + (row0 + rows - 1) / A.ratio;
         const int all_lo = kv_first(A, p_hi), all_hi = kv_end(A, rq, p_lo);          // keys that every row sees
-        const int t_lo = max(ti.first + (int)(u - sb), kv_first(A, p_lo) / kv::TILE);
-        const int t_hi = min(ti.first + (int)(pe - sb), (kv_end(A, rq, p_hi) + kv::TILE - 1) / kv::TILE);
+        const int some_lo = kv_first(A, p_lo), some_hi = kv_end(A, rq, p_hi);        // keys that any row sees
+        const int u_lo = max(un.first + (int)(u - sb), some_lo / Cfg::TOKENS);
+        const int u_hi = min(un.first + (int)(pe - sb), (some_hi + Cfg::TOKENS - 1) / Cfg::TOKENS);
 
-        // ---- the tiles, STAGES of them on their way; lane i keeps the id of page `block - in_ids + i`
+        // ---- the units, STAGES of them on their way.  Lane i keeps the id of page ids_from + i.
         const int32_t* row_table = A.table + (size_t)r * A.max_blocks;
         const int tiles_per_page = A.page_size / kv::TILE;
-        int block = t_lo / tiles_per_page, in_page = t_lo - block * tiles_per_page, ids = 0, in_ids = 32;
+        int tile_in = u_lo * Cfg::STEP, block = tile_in / tiles_per_page, in_page = tile_in - block * tiles_per_page, ids = 0, in_ids = 32;
+        const int tile_end = (some_hi + kv::TILE - 1) / kv::TILE;
         const unsigned char* src = nullptr;                                // this lane's place in the next tile, NULL: its page is missing
         auto open_page = [&]() {
             if (in_ids == 32) {
@@ -298,27 +319,41 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
             const int page = __shfl_sync(~0u, ids, in_ids);
             src = (u32)page < (u32)A.n_pages ? A.pages + (((size_t)page * A.Hk + hk) * tiles_per_page + in_page) * TB + lane * 16 : nullptr;
         };
-        if (t_lo < t_hi) open_page();
-        u32 present = 0;                                                   // bit s: the tile in stage s is there
-        int next = t_lo, stage_in = 0;
+        if (u_lo < u_hi) open_page();
+        u32 present = 0;                                                   // bits STEP * s ..: the tiles in stage s are there
+        int next = u_lo, stage_in = 0;
+        const bool even_pages = tiles_per_page % Cfg::STEP == 0;           // no unit lies on two pages
         auto issue = [&]() {
-            if (next < t_hi) {
-                if (in_page == tiles_per_page) { in_page = 0; ++block; ++in_ids; open_page(); }
-                present &= ~(1u << stage_in);
-                if (src) {
-                    present |= 1u << stage_in;
-                    const u32 dst = ring_addr + stage_in * TB + lane * 16;
+            if (next < u_hi) {
+                const u32 dst = ring_addr + stage_in * Cfg::UB + lane * 16;
+                present &= ~(((1u << Cfg::STEP) - 1u) << (Cfg::STEP * stage_in));
+                if (Cfg::STEP == 1 || even_pages) {
+                    if (in_page == tiles_per_page) { in_page = 0; ++block; ++in_ids; open_page(); }
+                    if (src) {
+                        present |= ((1u << Cfg::STEP) - 1u) << (Cfg::STEP * stage_in);
 #pragma unroll
-                    for (int c = 0; c < TB / 16; c += 32)
-                        if (c + 32 <= TB / 16 || c + lane < TB / 16) cp16(dst + c * 16, src + c * 16);
-                    src += TB;
+                        for (int c = 0; c < Cfg::UB / 16; c += 32)
+                            if (c + 32 <= Cfg::UB / 16 || c + lane < Cfg::UB / 16) cp16(dst + c * 16, src + c * 16);
+                        src += Cfg::UB;
+                    }
+                    in_page += Cfg::STEP;
+                } else {
+                    for (int p = 0; p < Cfg::STEP; ++p) {
+                        if (in_page == tiles_per_page) { in_page = 0; ++block; ++in_ids; open_page(); }
+                        if (src && next * Cfg::STEP + p < tile_end) {
+                            present |= 1u << (Cfg::STEP * stage_in + p);
+                            for (int c = lane; c < TB / 16; c += 32) cp16(dst + p * TB + (c - lane) * 16, src + (c - lane) * 16);
+                            src += TB;
+                        }
+                        ++in_page;
+                    }
                 }
-                ++in_page;
                 ++next;
                 if (++stage_in == STAGES) stage_in = 0;
             }
             cp_commit();
         };
+
         // the query rows are asked for before the tiles, behind which they would have to queue
         constexpr int VECS = 16 / Elem<T>::VEC;
         uint4 q_raw[NT][G][VECS];
@@ -337,7 +372,7 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
 
         // ---- query fragments: column g of n tile nt, dimensions 16 t .. 16 t + 15 of each group
         u32 qf[NT][G][QS][8];
-        float q64[NT][G][2], sc[NT][2];                     // -64 sum(q) of a group, what takes a product to a logit
+        float qsum[NT][G][2], q0[NT][G][2], sc[NT][2];      // sum(q) of a group, -q.f, what takes a product to a logit
         int see_lo[NT][2], see_hi[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -364,13 +399,17 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
             }
 #pragma unroll
             for (int gr = 0; gr < G; ++gr) {
-                float sum = 0.f;
+                float far = 0.f, near = 0.f;                              // dimensions whose codes read as 1024 + c and as 64 + c
 #pragma unroll
-                for (int e = 0; e < 16; ++e) { x[gr][e] *= f; sum += x[gr][e]; }
-                sum += __shfl_xor_sync(~0u, sum, 1);
-                sum += __shfl_xor_sync(~0u, sum, 2);
+                for (int e = 0; e < 16; ++e) { x[gr][e] *= f; (e & 2 ? near : far) += x[gr][e]; }
 #pragma unroll
-                for (int c = 0; c < 2; ++c) q64[nt][gr][c] = -64.f * __shfl_sync(~0u, sum, 8 * t + 4 * c);     // columns 2 t and 2 t + 1
+                for (int d = 1; d < 4; d <<= 1) { far += __shfl_xor_sync(~0u, far, d); near += __shfl_xor_sync(~0u, near, d); }
+                const float start = -(1024.f * far + 64.f * near);
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {                              // columns 2 t and 2 t + 1
+                    qsum[nt][gr][c] = __shfl_sync(~0u, far + near, 8 * t + 4 * c);
+                    q0[nt][gr][c] = __shfl_sync(~0u, start, 8 * t + 4 * c);
+                }
 #pragma unroll
                 for (int s = 0; s < QS; ++s)
 #pragma unroll
@@ -410,12 +449,12 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                 }
             }
 
-        // ---- what is done with P tiles from `tile` on, at base[]; whole: every row sees every token of them
-        auto use_tiles = [&](int tile, unsigned char* const* base, auto count_, auto whole_) {
+        // ---- what is done with P tiles from `tile` on, at base; whole: every row sees every token of them
+        auto use_tiles = [&](int tile, unsigned char* base, auto count_, auto whole_) {
             constexpr int P = decltype(count_)::value;
             constexpr bool whole = decltype(whole_)::value;
             auto params_of = [&](int p, int j, int from, u32 (&w)[G]) {    // token j of tile p: G words for the keys, the values' G further
-                const u32* params = reinterpret_cast<const u32*>(base[p]) + kv::param_words(G) + j * 2 * G + from;
+                const u32* params = reinterpret_cast<const u32*>((base + p * TB)) + kv::param_words(G) + j * 2 * G + from;
                 if constexpr (G == 2) {
                     const uint2 x = *reinterpret_cast<const uint2*>(params);
                     w[0] = x.x; w[1] = x.y;
@@ -427,7 +466,7 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
 #pragma unroll
                 for (int p = 0; p < P; ++p)
                     for (int i = lane; i < kv::TILE * 2 * G; i += 32)
-                        if ((tile + p) * kv::TILE + i / (2 * G) >= rq.len) (reinterpret_cast<u32*>(base[p]) + kv::param_words(G))[i] = 0u;
+                        if ((tile + p) * kv::TILE + i / (2 * G) >= rq.len) (reinterpret_cast<u32*>((base + p * TB)) + kv::param_words(G))[i] = 0u;
                 __syncwarp();
             }
             // logits: element e of an accumulator is token (e < 2 ? g : g + 8) of the tile, column 2 t + e % 2
@@ -439,12 +478,8 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                 params_of(p, g + 8, 0, kp1);
 #pragma unroll
                 for (int gr = 0; gr < G; ++gr) {
-                    const uint4 kw = *reinterpret_cast<const uint4*>(base[p] + gr * 512 + lane * 16);
+                    const uint4 kw = *reinterpret_cast<const uint4*>((base + p * TB) + gr * 512 + lane * 16);
                     float a[NT][4];
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) a[nt][e] = Cfg::F32 ? 0.f : q64[nt][gr][e & 1];
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {                // words 0, 2 hold the dimensions of steps 0, 1, words 1, 3 of 2, 3
                         u32 x[4], y[4];
@@ -452,26 +487,31 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                             code_pairs<true>(half ? kw.y : kw.x, x);
                             code_pairs<true>(half ? kw.w : kw.z, y);
                         } else {
-                            code_pairs_64(half ? kw.y : kw.x, x);
-                            code_pairs_64(half ? kw.w : kw.z, y);
+                            code_pairs_raw(half ? kw.y : kw.x, x);
+                            code_pairs_raw(half ? kw.w : kw.z, y);
                         }
 #pragma unroll
                         for (int k = 0; k < 2; ++k)
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                                for (int i = QS - 1; i >= 0; --i)
-                                    mma16816<Cfg::F32>(a[nt], x[2 * k], y[2 * k], x[2 * k + 1], y[2 * k + 1], qf[nt][gr][i][4 * half + 2 * k],
-                                                       qf[nt][gr][i][4 * half + 2 * k + 1]);
+                                for (int i = QS - 1; i >= 0; --i) {
+                                    const u32 b0 = qf[nt][gr][i][4 * half + 2 * k], b1 = qf[nt][gr][i][4 * half + 2 * k + 1];
+                                    if (half == 0 && k == 0 && i == QS - 1) {
+                                        const float c0 = Cfg::F32 ? 0.f : q0[nt][gr][0], c1 = Cfg::F32 ? 0.f : q0[nt][gr][1];
+                                        mma16816<Cfg::F32>(a[nt], x[0], y[0], x[1], y[1], b0, b1, c0, c1, c0, c1);
+                                    } else {
+                                        mma16816<Cfg::F32>(a[nt], x[2 * k], y[2 * k], x[2 * k + 1], y[2 * k + 1], b0, b1);
+                                    }
+                                }
                     }
-                    // scale and zero point; the sum of q is -1/64 of q64
                     const float2 p0 = half2_at(kp0[gr]), p1 = half2_at(kp1[gr]);
-                    const float z0 = (Cfg::F32 ? fmaf(8.f, p0.x, p0.y) : p0.y) * -0.015625f, z1 = (Cfg::F32 ? fmaf(8.f, p1.x, p1.y) : p1.y) * -0.015625f;
+                    const float z0 = Cfg::F32 ? fmaf(8.f, p0.x, p0.y) : p0.y, z1 = Cfg::F32 ? fmaf(8.f, p1.x, p1.y) : p1.y;
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const float z = e < 2 ? z0 : z1, q1 = q64[nt][gr][e & 1];
+                            const float z = e < 2 ? z0 : z1, q1 = qsum[nt][gr][e & 1];
                             s[p][nt][e] = fmaf(e < 2 ? p0.x : p1.x, a[nt][e], gr == 0 ? z * q1 : fmaf(z, q1, s[p][nt][e]));
                         }
                 }
@@ -561,7 +601,7 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                                 x[2] -= __uint_as_float(h1 << 16); x[3] -= __uint_as_float(h1 & 0xffff0000u);
                             }
                         }
-                        const uint4 vw = *reinterpret_cast<const uint4*>(base[p] + (G + gr) * 512 + lane * 16);
+                        const uint4 vw = *reinterpret_cast<const uint4*>((base + p * TB) + (G + gr) * 512 + lane * 16);
                         u32 e0[4], e1[4], o0[4], o1[4];                    // even and odd dimensions of the lower and upper two tokens
                         code_pairs<true>(__byte_perm(vw.x, vw.y, 0x5410), e0);
                         code_pairs<true>(__byte_perm(vw.x, vw.y, 0x7632), o0);
@@ -593,7 +633,7 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                     for (int gr = 0; gr < G; ++gr) {
                         const u32 s0 = __byte_perm(w[0][gr], w[1][gr], 0x5410), z0 = hfma2(s0, 0x48004800u, __byte_perm(w[0][gr], w[1][gr], 0x7632));
                         const u32 s1 = __byte_perm(w[2][gr], w[3][gr], 0x5410), z1 = hfma2(s1, 0x48004800u, __byte_perm(w[2][gr], w[3][gr], 0x7632));
-                        const uint4 vw = *reinterpret_cast<const uint4*>(base[p] + (G + gr) * 512 + lane * 16);
+                        const uint4 vw = *reinterpret_cast<const uint4*>((base + p * TB) + (G + gr) * 512 + lane * 16);
                         u32 e0[4], e1[4], o0[4], o1[4];
                         code_pairs<false>(__byte_perm(vw.x, vw.y, 0x5410), e0);
                         code_pairs<false>(__byte_perm(vw.x, vw.y, 0x7632), o0);
@@ -611,26 +651,20 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
         };
 
         int stage = 0;
-        for (int tile = t_lo; tile < t_hi; tile += Cfg::PAIR) {
-            cp_wait<STAGES - Cfg::PAIR>();
+        for (int unit = u_lo; unit < u_hi; ++unit) {
+            cp_wait<STAGES - 1>();
             __syncwarp();
-            unsigned char* base[Cfg::PAIR];
-            u32 there = 0;
-#pragma unroll
-            for (int p = 0; p < Cfg::PAIR; ++p) {
-                base[p] = ring + stage * TB;
-                there |= (tile + p < t_hi && ((present >> stage) & 1u)) ? 1u << p : 0u;
-                if (++stage == STAGES) stage = 0;
-            }
-            if (there == (1u << Cfg::PAIR) - 1u && tile * kv::TILE >= all_lo && (tile + Cfg::PAIR) * kv::TILE <= all_hi) {
-                use_tiles(tile, base, Const<Cfg::PAIR>(), Const<1>());
+            unsigned char* base = ring + stage * Cfg::UB;
+            const u32 there = present >> (Cfg::STEP * stage) & ((1u << Cfg::STEP) - 1u);
+            if (++stage == STAGES) stage = 0;
+            if (there == (1u << Cfg::STEP) - 1u && unit * Cfg::TOKENS >= all_lo && (unit + 1) * Cfg::TOKENS <= all_hi) {
+                use_tiles(unit * Cfg::STEP, base, Const<Cfg::STEP>(), Const<1>());
             } else {
-                for (int p = 0; p < Cfg::PAIR; ++p)
-                    if (there >> p & 1u) use_tiles(tile + p, base + p, Const<1>(), Const<0>());
+                for (int p = 0; p < Cfg::STEP; ++p)
+                    if (there >> p & 1u) use_tiles(unit * Cfg::STEP + p, base + p * TB, Const<1>(), Const<0>());
             }
             __syncwarp();
-#pragma unroll
-            for (int p = 0; p < Cfg::PAIR; ++p) issue();
+            issue();
         }
         cp_wait<0>();
         __syncwarp();
@@ -650,7 +684,7 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                 }
         const bool complete = sb >= wa && se <= wb;
         const int slot = sb < wa ? 0 : 1;
-        float* piece = reinterpret_cast<float*>(slot == 0 ? ring + STAGES * TB : ring);
+        float* piece = reinterpret_cast<float*>(slot == 0 ? ring + STAGES * Cfg::UB : ring);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -701,7 +735,7 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
     // ---- segments cut between warps: each row is joined by one warp
     auto smem_piece = [&](int k) {                                                   // k = 2 * warp + slot
         unsigned char* b = kv_smem + (size_t)(k >> 1) * Cfg::WARP_BYTES;
-        return (const float*)((k & 1) ? b : b + STAGES * TB);
+        return (const float*)((k & 1) ? b : b + STAGES * Cfg::UB);
     };
     auto part = [&](int c, int slot) { return parts + ((size_t)c * 2 + slot) * (ROWS * (D + 2)); };
     // lane k has the segment of piece k: where it differs from the piece before, the parts of another segment begin
@@ -756,7 +790,7 @@ constexpr int MAX_PIECE = 16 * (128 + 2) * 4;
 template <typename T, int G, int NT>
 int launch(const KvAttnArgs& A, void* workspace, int device, int ctas, cudaStream_t st) {
     typedef StreamCfg<T, G, NT> Cfg;
-    constexpr int MAX_SMEM = Cfg::WARPS * Cfg::WARP_BYTES + (POP_KV_MAX_REQUESTS + 1) * 8;
+    constexpr int MAX_SMEM = Cfg::WARPS * Cfg::WARP_BYTES + MAX_SUMS * 8;
     static_assert(Cfg::PIECE <= MAX_PIECE, "workspace");
     static_assert(MAX_SMEM <= 225 * 1024, "shared memory");
     static bool ready[64];                                     // set once per device; setting it twice does no harm
@@ -767,7 +801,7 @@ int launch(const KvAttnArgs& A, void* workspace, int device, int ctas, cudaStrea
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas);
     cfg.blockDim = dim3(Cfg::WARPS * 32);
-    cfg.dynamicSmemBytes = (size_t)Cfg::WARPS * Cfg::WARP_BYTES + (size_t)(A.R + 1) * 8;
+    cfg.dynamicSmemBytes = (size_t)Cfg::WARPS * Cfg::WARP_BYTES + (size_t)(((A.R - 1) >> sums_shift(A.R)) + 1) * 8;
     cfg.stream = st;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
