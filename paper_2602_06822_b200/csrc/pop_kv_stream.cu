@@ -39,6 +39,7 @@ typedef unsigned long long ull;
 #ifndef KV_WARPS
 #define KV_WARPS 12
 #define KV_STAGES 3
+#define KV_STEP 2
 #endif
 
 template <typename T, int G, int NT> struct StreamCfg {
@@ -50,12 +51,12 @@ template <typename T, int G, int NT> struct StreamCfg {
     static constexpr float BELOW = F32 ? 0.f : 7.f;         // to this far below the logit
     // Tiles of a unit, which a warp works on at once: two independent chains of products, reductions and exponentials where
     // registers allow
-    static constexpr int STEP = (NT == 1 && !F32) ? 2 : 1;
+    static constexpr int STEP = (NT == 1 && !F32) ? KV_STEP : 1;
     static constexpr int TOKENS = STEP * kv::TILE;
     static constexpr int WARPS = (NT == 1 && !F32) ? KV_WARPS : 8;
     static constexpr int TB = kv::tile_bytes(D), UB = STEP * TB;
-    static constexpr int PIECE = ROWS * (D + 2) * 4;        // un-normalised output, maximum and sum of a part of a segment
-    static constexpr int MIN_STAGES = (PIECE + UB - 1) / UB, WANT = (G == 1 ? 2 : 1) * (STEP == 2 ? KV_STAGES : 5);
+    static constexpr int PIECE = ROWS * (D + 4) * 4;        // un-normalised output, then (maximum, sum, -, -) of a part of a segment
+    static constexpr int MIN_STAGES = (PIECE + UB - 1) / UB, WANT = (G == 1 ? 2 : 1) * (NT == 1 && !F32 ? KV_STAGES : 5);
     static constexpr int STAGES = MIN_STAGES > WANT ? MIN_STAGES : WANT;
     static constexpr int WARP_BYTES = STAGES * UB + PIECE;  // ring (its memory later holds the second piece) and first piece
 };
@@ -156,54 +157,46 @@ template <int ROWS, int TOKENS> __device__ __forceinline__ Units request_units(c
     return t;
 }
 
+constexpr int SNAP = 40;                                       // units, see the kernel
+
 // The sums over the requests are kept for every request, or for every fourth one where there are more than 1024.
 constexpr int MAX_SUMS = 1024;
 __host__ __device__ constexpr int sums_shift(int R) { return R <= MAX_SUMS ? 0 : 2; }
 static_assert((POP_KV_MAX_REQUESTS >> 2) <= MAX_SUMS, "sums");
 
-// Joins n parts (part k at at(k)) of a segment's query row `col`; the result goes to the part `to`, or, where that is NULL, to the
-// output.  Parts of other CTAs are a trip to L2 away, so sixteen parts' maxima, sums and outputs are all on their way at once.
-template <typename T, int D, int ROWS, bool GLOBAL, typename At>
-__device__ __forceinline__ void join_row(const KvAttnArgs& A, const PieceOf& seg, int col, int n, At at, float* to) {
-    constexpr int PER = D / 32, BATCH = 16;
+// Joins n parts of a segment's query row `col` that lie in shared memory: part k's output at places[k] (a byte offset), its maximum
+// and sum `stats` bytes further.  The result goes to the part `to` or, where that is NULL, to the output.  One small function for all
+// uses: this code runs once or twice a call, mostly from beyond the instruction cache.
+template <typename T, int D, int ROWS>
+__device__ __noinline__ void join_row(const KvAttnArgs& A, const PieceOf& seg, int col, const unsigned char* smem, const u32* places, int n,
+                                      u32 stats, float* to, float2* carry) {
+    constexpr int PER = D / 32;
     typedef typename std::conditional<PER == 4, float4, float2>::type Vec;
     const int lane = threadIdx.x & 31;
-    float m = -1e30f, l = 0.f, o[PER] = {};
-    for (int k0 = 0; k0 < n; k0 += BATCH) {
-        const int end = min(BATCH, n - k0);
-        const float2* sp = reinterpret_cast<const float2*>(at(k0 + min(lane, end - 1)) + ROWS * D + 2 * col);
-        float2 st = GLOBAL ? __ldcg(sp) : *sp;                             // lane k: maximum and sum of part k0 + k
-        Vec x[BATCH];
+    const float2 st = lane < n ? *reinterpret_cast<const float2*>(smem + places[lane] + stats) : make_float2(-1e30f, 0.f);
+    float m = st.x;
 #pragma unroll
-        for (int b = 0; b < BATCH; ++b) {
-            const Vec* p = reinterpret_cast<const Vec*>(at(k0 + min(b, end - 1)) + col * D) + lane;
-            x[b] = GLOBAL ? __ldcg(p) : *p;
-        }
-        if (lane >= end) st = make_float2(-1e30f, 0.f);
-        float top = st.x;
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-        top = fmaxf(top, m);
-        const float old = kv_exp2(m - top), f = lane < end ? kv_exp2(st.x - top) : 0.f;
-        m = top;
-        l = fmaf(l, old, st.y * f);                                         // each lane's own part of the sum
-#pragma unroll
-        for (int e = 0; e < PER; ++e) o[e] *= old;
-#pragma unroll
-        for (int b = 0; b < BATCH; ++b) {
-            const float w = __shfl_sync(~0u, f, b);
-            if (b < end) {
-                const float* y = reinterpret_cast<const float*>(&x[b]);
-#pragma unroll
-                for (int e = 0; e < PER; ++e) o[e] = fmaf(y[e], w, o[e]);
-            }
-        }
-    }
+    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+    const float f = kv_exp2(st.x - m);
+    float l = st.y * f, o[PER] = {};
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(~0u, l, d);
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) {
+        const float w = __shfl_sync(~0u, f, k);
+        const Vec x = *(reinterpret_cast<const Vec*>(smem + places[k]) + lane);
+        const float* y = reinterpret_cast<const float*>(&x);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) o[e] = fmaf(y[e], w, o[e]);
+    }
     if (to) {
         *(reinterpret_cast<Vec*>(to + col * D) + lane) = *reinterpret_cast<const Vec*>(o);
-        if (lane == 0) *reinterpret_cast<float2*>(to + ROWS * D + 2 * col) = make_float2(m, l);
+        if (lane == 0) *reinterpret_cast<float2*>(to + ROWS * D + 4 * col) = make_float2(m, l);
+        return;
+    }
+    if (carry) {                                                           // more parts to come: kept as a part
+        *(reinterpret_cast<Vec*>(carry) + lane) = *reinterpret_cast<const Vec*>(o);
+        if (lane == 0) *reinterpret_cast<float2*>(reinterpret_cast<unsigned char*>(carry) + stats) = make_float2(m, l);
         return;
     }
     const int row = seg.row0 + col, i = row / A.ratio;
@@ -229,8 +222,8 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
     ull* sums = reinterpret_cast<ull*>(kv_smem + (size_t)WARPS * Cfg::WARP_BYTES);          // units before request r << sums_shift(R)
     __shared__ ull scan_sum[2][WARPS];
     __shared__ PieceOf piece_of[WARPS][2];
-    __shared__ int last_of[2];
-    __shared__ unsigned char order[WARPS][32];                             // every warp's list of the CTA's pieces
+    __shared__ int last_of[2], cut_ctas[2][2];
+    __shared__ u32 places[WARPS][32];                                      // every warp's list of parts
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     asm volatile("griddepcontrol.wait;" ::: "memory");                     // launched while the kernel before it winds down
@@ -268,9 +261,31 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
     // units of a CTA (the last one may have fewer, further ones none)
     const ull share = div_units(U + gridDim.x - 1, gridDim.x);
     const int cta = blockIdx.x;
-    const ull ca = cta * share;
-    if (ca >= U) return;
-    const ull cb = min(U, ca + share);
+    ull ca = min(U, cta * share), cb = min(U, ca + share);
+    // Joining CTAs' parts takes some 5 us, in which a CTA goes through SNAP units.  So where there is no more than that to do for each, the
+    // cuts between CTAs are moved to the nearer end of a segment that is no longer than that either.
+    if (share < SNAP) {
+        ull at = (lane & 1) ? cb : ca;
+        if (at < U && at > 0) {
+            int lo = 0, hi = ((A.R - 1) >> shift) + 1;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (sums[mid] <= at) lo = mid; else hi = mid;
+            }
+            ull base = sums[lo];
+            for (int q = lo << shift;; ++q) {
+                const Units un = request_units<ROWS, Cfg::TOKENS>(A, kv_request(A, q));
+                const ull all = (ull)un.count * un.row_blocks * A.Hk;
+                if (base + all <= at) { base += all; continue; }
+                const ull begin = base + div_units(at - base, un.count) * un.count;
+                if (un.count <= SNAP) at = 2 * (at - begin) < (ull)un.count ? begin : begin + un.count;
+                break;
+            }
+        }
+        ca = __shfl_sync(~0u, at, 0);
+        cb = __shfl_sync(~0u, at, 1);
+    }
+    if (ca >= cb) return;
     const u32 mine = (u32)(cb - ca);                                       // (2^32 units would be a day's work)
     const ull wa = ca + (ull)mine * warp / WARPS, wb = ca + (ull)mine * (warp + 1) / WARPS;
 
@@ -722,8 +737,7 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                     if (complete) {
                         if (A.lse) A.lse[at] = l[nt][c] == 0.f ? -INFINITY : (m[nt][c] + log2f(l[nt][c])) * 0.69314718f;
                     } else {
-                        piece[ROWS * D + 2 * col] = m[nt][c];
-                        piece[ROWS * D + 2 * col + 1] = l[nt][c];
+                        *reinterpret_cast<float2*>(piece + ROWS * D + 4 * col) = make_float2(m[nt][c], l[nt][c]);
                     }
                 }
             }
@@ -733,12 +747,8 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
     __syncthreads();
 
     // ---- segments cut between warps: each row is joined by one warp
-    auto smem_piece = [&](int k) {                                                   // k = 2 * warp + slot
-        unsigned char* b = kv_smem + (size_t)(k >> 1) * Cfg::WARP_BYTES;
-        return (const float*)((k & 1) ? b : b + STAGES * Cfg::UB);
-    };
-    auto part = [&](int c, int slot) { return parts + ((size_t)c * 2 + slot) * (ROWS * (D + 2)); };
-    // lane k has the segment of piece k: where it differs from the piece before, the parts of another segment begin
+    auto part = [&](int c, int slot) { return parts + ((size_t)c * 2 + slot) * (ROWS * (D + 4)); };
+    // lane k has piece k = 2 * warp + slot: where its segment differs from the piece before, the parts of another segment begin
     static_assert(2 * WARPS <= 32, "a lane per piece");
     const bool held = lane < 2 * WARPS && piece_of[lane >> 1][lane & 1].valid;
     const ull begin = held ? piece_of[lane >> 1][lane & 1].begin : 0;
@@ -746,46 +756,75 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
     const u32 earlier = pieces & ((1u << lane) - 1u);
     const ull begin_before = __shfl_sync(~0u, begin, earlier ? 31 - __clz(earlier) : lane);
     u32 starts = __ballot_sync(~0u, held && (!earlier || begin_before != begin));
-    if (held) order[warp][__popc(earlier)] = (unsigned char)lane;
-    __syncwarp();
-    PieceOf open[2];                                     // segments cut between CTAs: the one that began before, the one that goes on
-    open[0].valid = open[1].valid = 0;
+    const u32 where = (lane >> 1) * Cfg::WARP_BYTES + ((lane & 1) ? 0 : STAGES * Cfg::UB);
+    int cut[2] = {-1, -1};                               // pieces of the segments cut between CTAs: the one begun before, the one that goes on
     int task = 0;
     while (starts) {
         const int k = __ffs(starts) - 1;
         starts &= starts - 1u;
-        const int first = __popc(pieces & ((1u << k) - 1u));
-        const int n = __popc(starts ? pieces & ((starts & -starts) - 1u) : pieces) - first;
-        const PieceOf p = piece_of[k >> 1][k & 1];
+        const u32 of_segment = pieces & ~((1u << k) - 1u) & (starts ? (starts & -starts) - 1u : ~0u);
+        const PieceOf& p = piece_of[k >> 1][k & 1];
         const bool inside = p.begin >= ca && p.end <= cb;
         const int slot = p.begin < ca ? 0 : 1;
-        if (!inside) open[slot] = p;
+        if (!inside) cut[slot] = k;
         for (int c = 0; c < p.rows; ++c, ++task)
-            if (task % WARPS == warp)
-                join_row<T, D, ROWS, false>(A, p, c, n,
-                                            [&](int i) { return smem_piece(order[warp][first + i]); }, inside ? nullptr : part(cta, slot));
+            if (task % WARPS == warp) {
+                __syncwarp();
+                if (of_segment >> lane & 1u) places[warp][__popc(of_segment & ((1u << lane) - 1u))] = where + c * D * 4;
+                __syncwarp();
+                join_row<T, D, ROWS>(A, p, c, kv_smem, places[warp], __popc(of_segment), (ROWS - c) * D * 4 + c * 16,
+                                     inside ? nullptr : part(cta, slot), nullptr);
+            }
     }
-    if (!open[0].valid && !open[1].valid) return;        // the same for the whole CTA
+    if (cut[0] < 0 && cut[1] < 0) return;                // the same for the whole CTA
     __syncthreads();
-    if (tid < 2 && open[tid].valid) {
-        const int c0 = (int)div_units(open[tid].begin, share), c1 = (int)div_units(open[tid].end - 1, share);
-        u32 before;                                       // releases this CTA's parts (ordered before it by the barrier), acquires the others'
-        asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(counters + c0) : "memory");
-        last_of[tid] = before == (u32)(c1 - c0);
-        if (last_of[tid]) counters[c0] = 0u;              // ready for the next call
+    if (tid < 2) {
+        const int k = tid ? cut[1] : cut[0];
+        int last = 0;
+        if (k >= 0) {
+            const PieceOf& p = piece_of[k >> 1][k & 1];
+            const int c0 = (int)div_units(p.begin, share), c1 = (int)div_units(p.end - 1, share);
+            u32 arrived;                                  // releases this CTA's parts (ordered before it by the barrier), acquires the others'
+            asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(arrived) : "l"(counters + c0) : "memory");
+            last = arrived == (u32)(c1 - c0);
+            if (last) counters[c0] = 0u;                  // ready for the next call
+            cut_ctas[tid][0] = c0;
+            cut_ctas[tid][1] = c1;
+        }
+        last_of[tid] = last;
     }
     __syncthreads();
     for (int s = 0; s < 2; ++s) {
-        if (!open[s].valid || !last_of[s]) continue;
-        const int c0 = (int)div_units(open[s].begin, share), c1 = (int)div_units(open[s].end - 1, share);
-        for (int c = warp; c < open[s].rows; c += WARPS)
-            join_row<T, D, ROWS, true>(A, open[s], c, c1 - c0 + 1,
-                                       [&](int k) { return (const float*)part(c0 + k, k == 0 ? 1 : 0); }, nullptr);
+        if (!last_of[s]) continue;
+        const int k = s ? cut[1] : cut[0], c0 = cut_ctas[s][0], n = cut_ctas[s][1] - c0 + 1;
+        const PieceOf& p = piece_of[k >> 1][k & 1];
+        for (int c = warp; c < p.rows; c += WARPS) {
+            // the parts come through the ring (nothing else is in it any more), as many as it holds on their way at once; what they make
+            // stays there as a part of the next ones
+            constexpr int ROOM = D * 4 + 16, MOST = Cfg::WARP_BYTES / ROOM < 32 ? Cfg::WARP_BYTES / ROOM : 32;
+            __syncwarp();
+            places[warp][lane] = warp * Cfg::WARP_BYTES + lane * ROOM;
+            for (int from = 0; from < n;) {
+                const int kept = from ? 1 : 0, more = min(MOST - kept, n - from);
+                for (int i = 0; i < more; ++i) {
+                    const float* src = part(c0 + from + i, from + i == 0 ? 1 : 0);
+                    const u32 dst = ring_addr + (kept + i) * ROOM;
+                    if (lane < D / 4) cp16(dst + lane * 16, src + c * D + lane * 4);
+                    if (lane == 0) cp16(dst + D * 4, src + ROWS * D + c * 4);
+                }
+                cp_commit();
+                cp_wait<0>();
+                __syncwarp();
+                from += more;
+                join_row<T, D, ROWS>(A, p, c, kv_smem, places[warp], kept + more, D * 4, nullptr, from < n ? reinterpret_cast<float2*>(ring) : nullptr);
+                __syncwarp();
+            }
+        }
     }
 }
 
 constexpr int MAX_CTAS = 256;
-constexpr int MAX_PIECE = 16 * (128 + 2) * 4;
+constexpr int MAX_PIECE = 16 * (128 + 4) * 4;
 
 template <typename T, int G, int NT>
 int launch(const KvAttnArgs& A, void* workspace, int device, int ctas, cudaStream_t st) {
