@@ -389,8 +389,11 @@ int pop_kv_read(const pop_kv_cache_t* cache, const int64_t* slots, int n_tokens,
  * Products, softmax statistics and sums are kept in fp32.  Equal calls give equal results, bit for bit.
  * workspace: device memory of pop_kv_attention_workspace() bytes, zeroed once before its first use; it serves one stream
  * at a time.  Allocates nothing; may be captured into a CUDA graph.
+ * pop_kv_attention_check synchronises the stream and reports whether a bounded wait of a call on this workspace ran out since
+ * the last check (POP_ERR_TIMEOUT: that call's result is undefined; the workspace stays usable).
  */
 int pop_kv_attention_workspace(size_t* bytes);
+int pop_kv_attention_check(void* workspace, void* cuda_stream);
 int pop_kv_attention(const pop_kv_cache_t* cache, const void* q, long long q_stride, pop_dtype_t dtype, int n_heads,
                      int n_tokens, const int32_t* q_indptr, const int32_t* kv_lens, int n_requests,
                      const int32_t* block_table, int max_blocks, float scale, int causal, int window,

@@ -48,5 +48,7 @@ __device__ __forceinline__ float kv_exp2(float x) {
     return y;
 }
 
-int pop_launch_kv_attention_stream(const KvAttnArgs& A, int head_dim, pop_dtype_t dtype, void* workspace, cudaStream_t st);
+int pop_launch_kv_attention_stream(const KvAttnArgs& A, int head_dim, pop_dtype_t dtype, void* workspace, int device, int ctas, cudaStream_t st);
 size_t pop_kv_stream_workspace();
+int pop_kv_stream_max_ctas();
+int pop_launch_kv_attention_prompt(const KvAttnArgs& A, int head_dim, u32* status, int device, int ctas, cudaStream_t st);

@@ -1,0 +1,652 @@
+// Attention over the paged 4-bit cache for many query rows per request (prompts and their chunks), bf16, on the 5th-generation
+// tensor cores.  Same mathematics as the streaming kernel; here the 4 D flops of every visible (query, key) pair are what counts.
+//
+// Unit of work ("item"): 256 query rows of one (request, kv head) - rows are (token, head of the kv head's group), so grouped heads
+// share the unpacked keys - as two M = 128 tiles, against the keys in blocks of 128:
+//   S_i = Q_i K^T   (tcgen05.mma, both operands in shared memory)            tensor memory columns 128 i .. 128 i + 127
+//   P_i = 2^(S_i scale - m)  in fp16, over the first half of S_i             read back by the softmax warps, written in place
+//   O_i += P_i V    (A operand from tensor memory, V from shared memory)     columns 256 + D i ..
+// A block costs the tensor cores 2048 cycles at D = 128, the exponentials (16 per cycle and SM) 2048, and shared memory (Q, K
+// and V read by the MMAs, K and V written by the unpacking warps) 2048, so everything has to run beside everything else:
+//   warps 0-3, 4-7   softmax of tile 0 and 1: one thread owns one row.  One pass over S: the reference m is only raised when a logit
+//                    passes it by 2^15 (fp16's room; it is set 2^7 below the row's largest logit so far), which rescales O and the
+//                    part of P written so far; after a row's first block that is rare.
+//   warps 8-11       unpack keys and values: each 16-token tile of the cache straight from global memory (the next block's words are
+//                    on their way while this one's are unpacked) into fp16 in the MMAs' 128-byte swizzle: c - 8 exactly, then
+//                    s (c - 8) + (z + 8 s) with one rounding each to 11 bits
+//   warp 12          issues the MMAs: tile 0's products run while tile 1's softmax does, and the other way round
+// The items of a request are dealt out from its last rows (most keys under a causal mask) to its first.
+// Every wait is bounded; one that runs out sets the status word and the CTA winds down.
+#include "pop_kv_attn.cuh"
+
+namespace {
+
+constexpr int BN = 128;                        // keys of a block
+constexpr int THREADS = 16 * 32;             // four warpgroups; the last one has the MMA warp alone
+// registers of a thread after the split (the block is launched with 128): 2 * 184 + 104 + 40 = 4 * 128
+#define KV_REGS_SOFTMAX "184"
+#define KV_REGS_UNPACK "104"
+#define KV_REGS_MMA "40"
+constexpr int SOFTMAX_WARPS = 8, UNPACK_WARPS = 4, MMA_WARP = 12;
+constexpr int STAGES = 2;                      // of unpacked key and value blocks
+constexpr float RAISE = 15.f, BELOW = 7.f;
+constexpr unsigned long long WAIT_NS = 200ull * 1000ull * 1000ull;
+
+template <int D> struct PromptCfg {
+    static constexpr int G = D / 64, TILE = 128 * D * 2;                    // bytes of a 128-row operand tile
+    static constexpr int Q = 0, K = 2 * TILE, V = K + STAGES * TILE, BARS = V + STAGES * TILE;
+    static constexpr int BYTES = BARS + 256;                                // then the items before every request
+};
+
+__device__ __forceinline__ u32 smem_u32(const void* p) { return (u32)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(u32 bar, u32 count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(u32 bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ u32 mbar_try_wait(u32 bar, u32 parity) {
+    u32 ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
+    return ok;
+}
+// Waits for the phase of the given parity; gives up (false) after WAIT_NS or when another role has.
+__device__ __forceinline__ bool mbar_wait(u32 bar, u32 parity, volatile int* abort_flag, u32* status) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const unsigned long long t0 = pop_global_ns();
+    for (u32 it = 1;; ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((it & 31u) == 0u) {
+            if (*abort_flag) return false;
+            if (pop_global_ns() - t0 > WAIT_NS) {
+                *abort_flag = 1;
+                atomicExch(status, 1u);
+                return false;
+            }
+        }
+    }
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void to_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ void umma_ss(u32 d, u64 a, u64 b, u32 idesc, u32 accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma_ts(u32 d, u32 a, u64 b, u32 idesc, u32 accumulate) {       // A from tensor memory
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma_commit(u32 bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// 32 consecutive columns of this thread's lane; the registers are valid after tmem_wait_ld().
+__device__ __forceinline__ void tmem_ld32(u32 addr, u32 (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld(u32 (&r)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));             // no use of them moves up over the wait
+}
+__device__ __forceinline__ void tmem_st32(u32 addr, const u32 (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(u32 addr, u32 (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) asm volatile("" : "+r"(r[i]));
+}
+__device__ __forceinline__ void tmem_st16(u32 addr, const u32 (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Shared-memory descriptors, 128-byte swizzle (layout type 2, version 1).  K-major (Q, K): rows of 64 elements, groups of 8 rows 1024
+// bytes apart.  MN-major (V as [key][64 dimensions]): 8 keys 1024 bytes apart (stride offset), the next 64 dimensions one half
+// tile further (leading offset).
+__device__ __forceinline__ u64 desc_k_major(u32 addr) {
+    return (u64)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ u64 desc_mn_major(u32 addr) {
+    return (u64)((addr & 0x3ffffu) >> 4) | ((u64)(128 * 128 / 16) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+// Instruction descriptors: fp32 accumulator, fp16 operands, N / 8 at bit 17, M / 16 at bit 24; bit 16: B is MN-major.
+constexpr u32 IDESC_S = (1u << 4) | ((u32)(BN >> 3) << 17) | (8u << 24);
+template <int D> constexpr u32 IDESC_O = (1u << 4) | (1u << 16) | ((u32)(D >> 3) << 17) | (8u << 24);
+
+__device__ __forceinline__ u32 half2_bits(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const u32*>(&v);
+}
+__device__ __forceinline__ u32 mask_or(u32 x, u32 mask, u32 bits) {
+    u32 r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(x), "r"(mask), "r"(bits));
+    return r;
+}
+__device__ __forceinline__ u32 hadd2(u32 a, u32 b) {
+    u32 r;
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ u32 hfma2(u32 a, u32 b, u32 c) {
+    u32 r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+// The eight values of a word under the parameters p = (scale, zero).
+__device__ __forceinline__ uint4 unpack_word(u32 w, u32 p) {
+    const u32 s = __byte_perm(p, p, 0x1010), z = hfma2(s, 0x48004800u, __byte_perm(p, p, 0x3232)), v = w >> 8;     // z + 8 s
+    uint4 r;
+    r.x = hfma2(hadd2(mask_or(w, 0x000f000fu, 0x64006400u), 0xe408e408u), s, z);                // (1024 + c) - 1032 = c - 8
+    r.y = hfma2(hadd2(mask_or(w, 0x00f000f0u, 0x54005400u), 0xd480d480u), s, z);                // (64 + c) - 72
+    r.z = hfma2(hadd2(mask_or(v, 0x000f000fu, 0x64006400u), 0xe408e408u), s, z);
+    r.w = hfma2(hadd2(mask_or(v, 0x00f000f0u, 0x54005400u), 0xd480d480u), s, z);
+    return r;
+}
+__device__ __forceinline__ void st_shared(u32 addr, const uint4& v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+// Byte offset of 16-byte chunk c (of 8) of row r in a tile of 128-byte rows under the 128-byte swizzle.
+__device__ __forceinline__ u32 swizzled(int r, int c) { return (u32)(r * 128 + ((c ^ (r & 7)) << 4)); }
+
+struct Item {
+    int r, hk, row0, rows;               // query rows row0 .. row0 + rows - 1 (<= 256) of (request r, kv head hk)
+    KvRequest rq;
+    int first;                           // first block
+    int n0, n1;                          // blocks of either tile of 128 rows, from `first` on
+};
+
+__device__ __forceinline__ int request_items(const KvAttnArgs& A, int r) {
+    const KvRequest q = kv_request(A, r);
+    const long long rows = (long long)q.n * A.ratio;
+    return q.n > 0 && rows >= A.prompt_rows ? (int)((rows + 255) / 256) * A.Hk : 0;
+}
+
+__device__ __forceinline__ Item find_item(const KvAttnArgs& A, const int* before, int item) {
+    int lo = 0, hi = A.R;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (before[mid] <= item) lo = mid; else hi = mid;
+    }
+    Item it;
+    it.r = lo;
+    it.rq = kv_request(A, lo);
+    const int rows = it.rq.n * A.ratio, tiles = (rows + 255) / 256, i = item - before[lo];
+    it.hk = i % A.Hk;
+    it.row0 = (tiles - 1 - i / A.Hk) * 256;
+    it.rows = min(256, rows - it.row0);
+    it.first = min(kv_first(A, it.rq.pos0 + it.row0 / A.ratio), it.rq.len) / BN;
+    auto blocks = [&](int rows) { return max(0, (kv_end(A, it.rq, it.rq.pos0 + (it.row0 + rows - 1) / A.ratio) + BN - 1) / BN - it.first); };
+    it.n0 = blocks(min(it.rows, 128));
+    it.n1 = it.rows > 128 ? blocks(it.rows) : 0;
+    return it;
+}
+
+// One 16-token tile's words (lane L = 4 g + t: see the cache's format).
+template <int G> struct TileWords {
+    uint4 k[G], v[G];
+    u32 kp[2][G], vp[4][G];              // parameters: keys of tokens g, g + 8; values of tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+    u32 absent;                          // it has keys, and its page is missing
+};
+
+template <int D>
+__global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs A, u32* status) {
+    typedef PromptCfg<D> Cfg;
+    constexpr int G = Cfg::G, TB = kv::tile_bytes(D);
+    extern __shared__ unsigned char raw_smem[];
+    __shared__ u32 tmem_slot;
+    __shared__ int abort_flag;
+    __shared__ int warp_sum[2][THREADS / 32];
+    __shared__ unsigned char absent_tiles[4][8];           // by block: a stage is refilled before the last softmax warp has looked
+    const u32 base = (smem_u32(raw_smem) + 1023u) & ~1023u;
+    unsigned char* smem = raw_smem + (base - smem_u32(raw_smem));
+    int* before = reinterpret_cast<int*>(smem + Cfg::BYTES);               // [R + 1] items before request r
+    const u32 bars = base + Cfg::BARS;
+    const u32 q_full = bars, s_full = bars + 16, p_full = bars + 32, o_done = bars + 48;                 // + 8 * tile
+    const u32 k_full = bars + 64, v_full = bars + 80, k_empty = bars + 96, v_empty = bars + 112, drain = bars + 128;   // + 8 * stage
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    volatile int* abortp = &abort_flag;
+
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // ---- items before every request
+    if (tid == 0) { abort_flag = 0; before[0] = 0; }
+    int total = 0;
+    for (int r0 = 0, turn = 0; r0 < A.R; r0 += THREADS, turn ^= 1) {
+        const int r = r0 + tid;
+        int v = r < A.R ? request_items(A, r) : 0;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int u = __shfl_up_sync(~0u, v, d);
+            if (lane >= d) v += u;
+        }
+        if (lane == 31) warp_sum[turn][warp] = v;
+        __syncthreads();
+        v += total;
+        for (int w = 0; w < THREADS / 32; ++w) {
+            if (w < warp) v += warp_sum[turn][w];
+            total += warp_sum[turn][w];
+        }
+        if (r < A.R) before[r + 1] = v;
+    }
+    if ((int)blockIdx.x >= total) return;                                  // the same for the whole CTA
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(q_full + 8 * i, 128);
+            mbar_init(s_full + 8 * i, 1);
+            mbar_init(p_full + 8 * i, 128);
+            mbar_init(o_done + 8 * i, 1);
+            mbar_init(k_full + 8 * i, UNPACK_WARPS);
+            mbar_init(v_full + 8 * i, UNPACK_WARPS);
+            mbar_init(k_empty + 8 * i, 1);
+            mbar_init(v_empty + 8 * i, 1);
+        }
+        mbar_init(drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == MMA_WARP) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const u32 tmem = tmem_slot;
+
+    if (warp < SOFTMAX_WARPS) {
+        // ------------------------------------------------------------------ softmax: this thread's row of tile `half`
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 " KV_REGS_SOFTMAX ";");
+        const int half = warp >> 2, row_in = tid & 127;
+        const u32 lane_base = tmem + ((u32)((warp & 3) * 32) << 16);
+        const u32 t_s = lane_base + 128u * half, t_o = lane_base + 256u + (u32)(D * half);
+        const u32 q_tile = base + Cfg::Q + half * Cfg::TILE;
+        u32 s_phase = 0, o_phase = 0, block = 0;                           // block: of all items, for the stage of absent_tiles
+        bool ok = true;
+        for (int item = blockIdx.x; item < total && ok; item += gridDim.x) {
+            const Item it = find_item(A, before, item);
+            const int n = half ? it.n1 : it.n0, n_both = max(it.n0, it.n1);
+            const bool in = 128 * half + row_in < it.rows;
+            const int row = it.row0 + 128 * half + (in ? row_in : 0), i = row / A.ratio;
+            const size_t out_at = (size_t)(it.rq.q0 + i) * A.H + it.hk * A.ratio + (row - i * A.ratio);
+            const int pos = it.rq.pos0 + i, see_lo = kv_first(A, pos), see_hi = in ? kv_end(A, it.rq, pos) : 0;
+            float m = -1e30f, l = 0.f, sc = 0.f;
+            if (n > 0) {
+                // the row as fp16, times a power of two that puts its largest element at 2^10
+                const __nv_bfloat16* qp = (const __nv_bfloat16*)A.q + (size_t)(it.rq.q0 + i) * A.q_stride +
+                                          (size_t)(it.hk * A.ratio + (row - i * A.ratio)) * D;
+                uint4 raw[D / 8];
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) raw[c] = in ? *reinterpret_cast<const uint4*>(qp + 8 * c) : make_uint4(0u, 0u, 0u, 0u);
+                u32 top = 0u;                                              // largest magnitude, as bf16 bits
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    const u32 w[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7fffu, w[e] >> 16 & 0x7fffu));
+                }
+                const float f = __uint_as_float((264u - max(top >> 7, 30u)) << 23);
+                sc = A.scale2 * __uint_as_float((254u << 23) - __float_as_uint(f));
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    float x[8];
+                    Elem<__nv_bfloat16>::unpack(raw[c], x);
+                    const uint4 h = make_uint4(half2_bits(x[0] * f, x[1] * f), half2_bits(x[2] * f, x[3] * f),
+                                               half2_bits(x[4] * f, x[5] * f), half2_bits(x[6] * f, x[7] * f));
+                    st_shared(q_tile + (c / 8) * (128 * 128) + swizzled(row_in, c % 8), h);
+                }
+                to_async_proxy();
+                mbar_arrive(q_full + 8 * half);
+            }
+            // blocks [it.first + whole_lo, it.first + whole_hi) are seen by every row of the tile
+            const int r_first = it.row0 + 128 * half, r_last = it.row0 + min(it.rows, 128 * half + 128) - 1;
+            const int key_lo = kv_first(A, it.rq.pos0 + r_last / A.ratio), key_hi = kv_end(A, it.rq, it.rq.pos0 + r_first / A.ratio);
+            for (int j = 0; j < n && ok; ++j) {
+                ok = __all_sync(~0u, mbar_wait(s_full + 8 * half, s_phase, abortp, status));
+                if (!ok) break;
+                s_phase ^= 1u;
+                tc_after();
+                const int k0 = (it.first + j) * BN;
+                const uint2 absent = *reinterpret_cast<const uint2*>(absent_tiles[(block + j) & 3]);      // a byte for each 16 keys
+                const bool whole = k0 >= key_lo && k0 + BN <= key_hi && (absent.x | absent.y) == 0u;
+                const int from = see_lo - k0, to_key = see_hi - k0;
+                auto seen = [&](int key) {                                  // key of the block
+                    return key >= from && key < to_key && (((key < 64 ? absent.x : absent.y) >> ((key >> 4 & 3) * 8)) & 1u) == 0u;
+                };
+                if (j == 0) {                                               // the reference, from the first block's logits
+                    float top = -INFINITY;
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        u32 v[32];
+                        tmem_ld32(t_s + 32u * c, v);
+                        tmem_wait_ld(v);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const float x = __uint_as_float(v[e]) * sc;
+                            if (whole || seen(32 * c + e)) top = fmaxf(top, x);
+                        }
+                    }
+                    if (top > -1e30f) m = top - BELOW;
+                }
+                u32 v[2][32];
+                tmem_ld32(t_s, v[0]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    u32 (&w)[32] = v[c & 1];
+                    tmem_wait_ld(w);
+                    if (c < 3) tmem_ld32(t_s + 32u * (c + 1), v[(c + 1) & 1]);
+                    float x[32], top = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {                       // packed: two per instruction
+                        const float2 y = __ffma2_rn(make_float2(__uint_as_float(w[e]), __uint_as_float(w[e + 1])), make_float2(sc, sc), make_float2(-m, -m));
+                        x[e] = y.x;
+                        x[e + 1] = y.y;
+                    }
+                    if (!whole) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!seen(32 * c + e)) x[e] = -INFINITY;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) top = fmaxf(top, x[e]);
+                    if (__any_sync(~0u, top > RAISE)) {
+                        // raised: what was summed under the old reference is scaled, in l, O and this block's part of P
+                        float best = -INFINITY;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (x[e] != -INFINITY) best = fmaxf(best, __uint_as_float(w[e]) * sc);
+                        const float to = top > RAISE ? best - BELOW : m, f = kv_exp2(m - to);
+                        if (top > RAISE) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (x[e] != -INFINITY) x[e] = fmaf(__uint_as_float(w[e]), sc, -to);
+                        }
+                        m = to;
+                        l *= f;
+                        if (c < 3) tmem_wait_ld(v[(c + 1) & 1]);
+                        const u32 f2 = half2_bits(f, f);
+#pragma unroll 1
+                        for (int b = 0; b < c; ++b) {
+                            u32 y[16];
+                            tmem_wait_st();
+                            tmem_ld16(t_s + 16u * b, y);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) y[e] = hfma2(y[e], f2, 0u);
+                            tmem_st16(t_s + 16u * b, y);
+                        }
+                        if (j > 0) {
+                            ok = __all_sync(~0u, mbar_wait(o_done + 8 * half, o_phase ^ 1u, abortp, status));      // the products of block j - 1 are in O
+                            tc_after();
+#pragma unroll 1
+                            for (int b = 0; ok && b < D / 32; ++b) {
+                                u32 y[32];
+                                tmem_ld32(t_o + 32u * b, y);
+                                tmem_wait_ld(y);
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
+                                tmem_st32(t_o + 32u * b, y);
+                            }
+                        }
+                    }
+                    u32 p[16];
+                    float2 l2[2] = {make_float2(l, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        const float a = kv_exp2(x[e]), b = kv_exp2(x[e + 1]);
+                        l2[e / 2 & 1] = __fadd2_rn(l2[e / 2 & 1], make_float2(a, b));
+                        p[e / 2] = half2_bits(a, b);
+                    }
+                    l = (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
+                    tmem_st16(t_s + 16u * c, p);
+                }
+                tmem_wait_st();
+                tc_before();
+                mbar_arrive(p_full + 8 * half);
+                o_phase ^= 1u;                                              // now the parity that block j's products complete, flipped
+            }
+            block += n_both;
+            if (!ok) break;
+            if (n > 0) {
+                ok = __all_sync(~0u, mbar_wait(o_done + 8 * half, o_phase ^ 1u, abortp, status));
+                if (!ok) break;
+                tc_after();
+            }
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            __nv_bfloat16* out = (__nv_bfloat16*)A.out + out_at * D;
+#pragma unroll 1
+            for (int b = 0; b < D / 32; ++b) {
+                u32 y[32];
+                if (n > 0) {
+                    tmem_ld32(t_o + 32u * b, y);
+                    tmem_wait_ld(y);
+                }
+#pragma unroll
+                for (int e = 0; e < 32; e += 8) {
+                    u32 z[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float a = n > 0 ? __uint_as_float(y[e + 2 * k]) * inv : 0.f, c = n > 0 ? __uint_as_float(y[e + 2 * k + 1]) * inv : 0.f;
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(a, c);
+                        z[k] = *reinterpret_cast<const u32*>(&h);
+                    }
+                    if (in) *reinterpret_cast<uint4*>(out + 32 * b + e) = l == 0.f ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(z[0], z[1], z[2], z[3]);
+                }
+                __syncwarp();
+            }
+            if (in && A.lse) A.lse[out_at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718f;
+            tc_before();
+        }
+    } else if (warp < SOFTMAX_WARPS + UNPACK_WARPS) {
+        // ------------------------------------------------------------------ unpacking: 16-token tiles 2 w and 2 w + 1 of every block
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 " KV_REGS_UNPACK ";");
+        const int w = warp - SOFTMAX_WARPS, g = lane >> 2, t = lane & 3;
+        const int tiles_per_page = A.page_size / kv::TILE;
+        auto fetch = [&](const Item& it, int j, int i, TileWords<G>& b) {
+            const int tile = (it.first + j) * (BN / kv::TILE) + 2 * w + i, key0 = tile * kv::TILE;
+            const int at = tile / tiles_per_page;
+            int page = -1;
+            b.absent = 0u;
+            if (key0 < it.rq.len) {
+                page = A.table[(size_t)it.r * A.max_blocks + at];
+                if ((u32)page >= (u32)A.n_pages) { page = -1; b.absent = 1u; }
+            }
+            const unsigned char* src = A.pages + (((size_t)max(page, 0) * A.Hk + it.hk) * tiles_per_page + (tile - at * tiles_per_page)) * TB;
+#pragma unroll
+            for (int gr = 0; gr < G; ++gr) {
+                b.k[gr] = page >= 0 ? __ldg(reinterpret_cast<const uint4*>(src + gr * 512) + lane) : make_uint4(0u, 0u, 0u, 0u);
+                b.v[gr] = page >= 0 ? __ldg(reinterpret_cast<const uint4*>(src + (G + gr) * 512) + lane) : make_uint4(0u, 0u, 0u, 0u);
+            }
+            const u32* params = reinterpret_cast<const u32*>(src) + kv::param_words(G);
+            auto params_of = [&](int token, int from, u32 (&p)[G]) {         // zeros for tokens that are not there: a value of 0
+#pragma unroll
+                for (int gr = 0; gr < G; ++gr) p[gr] = page >= 0 && key0 + token < it.rq.len ? __ldg(params + token * 2 * G + from + gr) : 0u;
+            };
+            params_of(g, 0, b.kp[0]);
+            params_of(g + 8, 0, b.kp[1]);
+            params_of(2 * t, G, b.vp[0]);
+            params_of(2 * t + 1, G, b.vp[1]);
+            params_of(2 * t + 8, G, b.vp[2]);
+            params_of(2 * t + 9, G, b.vp[3]);
+        };
+        u32 stage = 0, phase = 0, block = 0;
+        bool ok = true;
+        for (int item = blockIdx.x; item < total && ok; item += gridDim.x) {
+            const Item it = find_item(A, before, item);
+            const int n = max(it.n0, it.n1);
+            TileWords<G> now, next;
+            if (n > 0) fetch(it, 0, 0, now);
+            for (int j = 0; j < n && ok; ++j) {
+                const u32 kt = base + Cfg::K + stage * Cfg::TILE, vt = base + Cfg::V + stage * Cfg::TILE;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (i == 0) fetch(it, j, 1, next);
+                    else if (j + 1 < n) fetch(it, j + 1, 0, next);
+                    if (i == 0) {
+                        ok = __all_sync(~0u, mbar_wait(k_empty + 8 * stage, phase ^ 1u, abortp, status));
+                        if (!ok) break;
+                    }
+#pragma unroll
+                    for (int gr = 0; gr < G; ++gr) {
+                        const int row = (2 * w + i) * kv::TILE + g;
+                        const u32 half = kt + gr * (128 * 128);
+                        st_shared(half + swizzled(row, 2 * t), unpack_word(now.k[gr].x, now.kp[0][gr]));
+                        st_shared(half + swizzled(row, 2 * t + 1), unpack_word(now.k[gr].y, now.kp[0][gr]));
+                        st_shared(half + swizzled(row + 8, 2 * t), unpack_word(now.k[gr].z, now.kp[1][gr]));
+                        st_shared(half + swizzled(row + 8, 2 * t + 1), unpack_word(now.k[gr].w, now.kp[1][gr]));
+                    }
+                    if (lane == 0) absent_tiles[block & 3][2 * w + i] = (unsigned char)now.absent;
+                    if (i == 1) {
+                        to_async_proxy();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(k_full + 8 * stage);
+                    } else {
+                        ok = __all_sync(~0u, mbar_wait(v_empty + 8 * stage, phase ^ 1u, abortp, status));
+                        if (!ok) break;
+                    }
+#pragma unroll
+                    for (int gr = 0; gr < G; ++gr) {
+                        const int row = (2 * w + i) * kv::TILE + 2 * t;
+                        const u32 half = vt + gr * (128 * 128);
+                        st_shared(half + swizzled(row, g), unpack_word(now.v[gr].x, now.vp[0][gr]));
+                        st_shared(half + swizzled(row + 1, g), unpack_word(now.v[gr].y, now.vp[1][gr]));
+                        st_shared(half + swizzled(row + 8, g), unpack_word(now.v[gr].z, now.vp[2][gr]));
+                        st_shared(half + swizzled(row + 9, g), unpack_word(now.v[gr].w, now.vp[3][gr]));
+                    }
+                    if (i == 1) {
+                        to_async_proxy();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(v_full + 8 * stage);
+                    }
+                    now = next;
+                }
+                ++block;
+                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 " KV_REGS_MMA ";");
+    }
+    if (warp == MMA_WARP && lane == 0) {
+        // ------------------------------------------------------------------ MMA issue
+        u32 block = 0, q_phase[2] = {0u, 0u}, p_phase[2] = {0u, 0u};
+        bool ok = true;
+        for (int item = blockIdx.x; item < total && ok; item += gridDim.x) {
+            const Item it = find_item(A, before, item);
+            const int n = max(it.n0, it.n1);
+            auto stage_of = [&](int j) { return (block + j) & 1u; };
+            auto phase_of = [&](int j) { return ((block + j) >> 1) & 1u; };
+            auto scores = [&](int half, int j) {
+                const u32 q = base + Cfg::Q + half * Cfg::TILE, k = base + Cfg::K + stage_of(j) * Cfg::TILE;
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s) {                          // 16 dimensions: 32 bytes along the swizzled row
+                    const u32 at = (s / 4) * (128 * 128) + (s % 4) * 32;
+                    umma_ss(tmem + 128u * half, desc_k_major(q + at), desc_k_major(k + at), IDESC_S, s > 0);
+                }
+                umma_commit(s_full + 8 * half);
+            };
+            auto outputs = [&](int half, int j) {
+                const u32 v = base + Cfg::V + stage_of(j) * Cfg::TILE;
+#pragma unroll
+                for (int s = 0; s < BN / 16; ++s)                           // 16 keys: 8 columns of P, 16 rows of V
+                    umma_ts(tmem + 256u + (u32)(D * half), tmem + 128u * half + 8u * s, desc_mn_major(v + s * 16 * 128), IDESC_O<D>, j > 0 || s > 0);
+                umma_commit(o_done + 8 * half);
+            };
+            if (n > 0) {
+                ok = mbar_wait(k_full + 8 * stage_of(0), phase_of(0), abortp, status);
+                for (int half = 0; half < 2 && ok; ++half)
+                    if ((half ? it.n1 : it.n0) > 0) {
+                        ok = mbar_wait(q_full + 8 * half, q_phase[half], abortp, status);
+                        if (!ok) break;
+                        q_phase[half] ^= 1u;
+                        tc_after();
+                        scores(half, 0);
+                    }
+                if (!ok) break;
+                umma_commit(k_empty + 8 * stage_of(0));
+            }
+            for (int j = 0; j < n && ok; ++j) {
+                if (j + 1 < n) ok = mbar_wait(k_full + 8 * stage_of(j + 1), phase_of(j + 1), abortp, status);
+                if (ok) ok = mbar_wait(v_full + 8 * stage_of(j), phase_of(j), abortp, status);
+                for (int half = 0; half < 2 && ok; ++half) {
+                    const int n_half = half ? it.n1 : it.n0;
+                    if (j < n_half) {
+                        ok = mbar_wait(p_full + 8 * half, p_phase[half], abortp, status);
+                        if (!ok) break;
+                        p_phase[half] ^= 1u;
+                        tc_after();
+                        outputs(half, j);
+                    }
+                    if (j + 1 < n_half) scores(half, j + 1);             // behind the products that read P out of the same columns
+                }
+                if (!ok) break;
+                umma_commit(v_empty + 8 * stage_of(j));
+                if (j + 1 < n) umma_commit(k_empty + 8 * stage_of(j + 1));
+            }
+            block += n;
+        }
+        // nothing of this CTA may still be executing on the tensor cores when tensor memory is given back
+        umma_commit(drain);
+        const unsigned long long t0 = pop_global_ns();
+        while (!mbar_try_wait(drain, 0u) && pop_global_ns() - t0 < WAIT_NS) {}
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+template <int D> int launch(const KvAttnArgs& A, u32* status, int device, int ctas, cudaStream_t st) {
+    typedef PromptCfg<D> Cfg;
+    constexpr int MAX_SMEM = Cfg::BYTES + 1024 + (POP_KV_MAX_REQUESTS + 1) * 4;
+    static_assert(MAX_SMEM <= 225 * 1024, "shared memory");
+    static bool ready[64];                                     // set once per device; setting it twice does no harm
+    if (device >= 64 || !ready[device]) {
+        POP_CUDA(cudaFuncSetAttribute(kv_prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM));
+        if (device < 64) ready[device] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = Cfg::BYTES + 1024 + (size_t)(A.R + 1) * 4;
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    POP_CUDA(cudaLaunchKernelEx(&cfg, kv_prompt_kernel<D>, A, status));
+    POP_LAUNCHED();
+    return POP_OK;
+}
+
+}  // namespace
+
+int pop_launch_kv_attention_prompt(const KvAttnArgs& A, int head_dim, u32* status, int device, int ctas, cudaStream_t st) {
+    return head_dim == 64 ? launch<64>(A, status, device, ctas, st) : launch<128>(A, status, device, ctas, st);
+}

@@ -855,17 +855,9 @@ int launch(const KvAttnArgs& A, void* workspace, int device, int ctas, cudaStrea
 }  // namespace
 
 size_t pop_kv_stream_workspace() { return MAX_CTAS * 4 + (size_t)MAX_CTAS * 2 * MAX_PIECE; }
+int pop_kv_stream_max_ctas() { return MAX_CTAS; }
 
-int pop_launch_kv_attention_stream(const KvAttnArgs& A, int head_dim, pop_dtype_t dtype, void* workspace, cudaStream_t st) {
-    int device = 0;
-    POP_CUDA(cudaGetDevice(&device));
-    static int sms_of[64];                                     // asked for once per device
-    int sms = device < 64 ? sms_of[device] : 0;
-    if (!sms) {
-        POP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
-        if (device < 64) sms_of[device] = sms;
-    }
-    const int ctas = sms < MAX_CTAS ? sms : MAX_CTAS;
+int pop_launch_kv_attention_stream(const KvAttnArgs& A, int head_dim, pop_dtype_t dtype, void* workspace, int device, int ctas, cudaStream_t st) {
     // 8 query rows share one pass over the codes; a second set of 8 costs products only, so it pays as soon as the average request
     // has more than 8 rows
     const bool wide = (long long)((A.T + A.R - 1) / A.R) * A.ratio > 8;

@@ -90,6 +90,7 @@ SIGNATURES = {
     "pop_kv_append": (C.c_int, [C.POINTER(KVCacheDesc), _P, C.c_longlong, _P, C.c_longlong, C.c_int, _P, C.c_int, _P]),
     "pop_kv_read": (C.c_int, [C.POINTER(KVCacheDesc), _P, C.c_int, C.c_int, _P, _P, _P]),
     "pop_kv_attention_workspace": (C.c_int, [C.POINTER(C.c_size_t)]),
+    "pop_kv_attention_check": (C.c_int, [_P, _P]),
     "pop_kv_attention": (C.c_int, [C.POINTER(KVCacheDesc), _P, C.c_longlong, C.c_int, C.c_int, C.c_int, _P, _P, C.c_int, _P, C.c_int,
                                    C.c_float, C.c_int, C.c_int, _P, _P, _P, C.c_size_t, _P]),
 }
@@ -571,3 +572,11 @@ def kv_attention(pages, q, block_table, q_indptr, kv_lens, scale: Optional[float
     if made:
         _used_on(stream, out)
     return out
+
+
+def kv_attention_check(device="cuda", workspace=None, stream=None):
+    """pop_kv_attention_check for the stream's own workspace (or the one given): synchronises, raises PopError if a wait ran out."""
+    st = _stream_ptr(stream)
+    if workspace is None:
+        workspace = _kv_workspace(_torch().empty(0, device=device).device, st)
+    _check(lib().pop_kv_attention_check(workspace.data_ptr(), st), "pop_kv_attention_check")
