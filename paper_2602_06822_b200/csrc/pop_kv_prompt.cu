@@ -11,10 +11,9 @@
 //   warps 0-3, 4-7   softmax of tile 0 and 1: one thread owns one row.  One pass over S: the reference m is only raised when a logit
 //                    passes it by 2^15 (fp16's room; it is set 2^7 below the row's largest logit so far), which rescales O and the
 //                    part of P written so far; after a row's first block that is rare.
-//   warps 8-11       unpack keys and values: each 16-token tile of the cache straight from global memory (the next block's words are
-//                    on their way while this one's are unpacked) into fp16 in the MMAs' 128-byte swizzle: c - 8 exactly, then
-//                    s (c - 8) + (z + 8 s) with one rounding each to 11 bits
-//   warp 12          issues the MMAs: tile 0's products run while tile 1's softmax does, and the other way round
+//   warps 8-13       unpack keys and values: 16-token tiles of the cache, brought to shared memory one tile ahead (cp.async), into fp16
+//                    in the MMAs' 128-byte swizzle: c - 8 exactly, then s (c - 8) + (z + 8 s) with one rounding each to 11 bits
+//   warp 14          issues the MMAs: tile 0's products run while tile 1's softmax does, and the other way round
 // The items of a request are dealt out from its last rows (most keys under a causal mask) to its first.
 // Every wait is bounded; one that runs out sets the status word and the CTA winds down.
 #include "pop_kv_attn.cuh"
@@ -22,20 +21,21 @@
 namespace {
 
 constexpr int BN = 128;                        // keys of a block
-constexpr int THREADS = 16 * 32;             // four warpgroups; the last one has the MMA warp alone
-// registers of a thread after the split (the block is launched with 128): 2 * 184 + 104 + 40 = 4 * 128
+constexpr int THREADS = 16 * 32;             // four warpgroups (warp 15 has nothing to do)
+constexpr int SOFTMAX_WARPS = 8, UNPACK_WARPS = 6, MMA_WARP = 14;
+// registers of a thread after the split (the block is launched with 128): 2 * 184 + 2 * 72 = 4 * 128
 #define KV_REGS_SOFTMAX "184"
-#define KV_REGS_UNPACK "104"
-#define KV_REGS_MMA "40"
-constexpr int SOFTMAX_WARPS = 8, UNPACK_WARPS = 4, MMA_WARP = 12;
+#define KV_REGS_OTHERS "72"
 constexpr int STAGES = 2;                      // of unpacked key and value blocks
 constexpr float RAISE = 15.f, BELOW = 7.f;
 constexpr unsigned long long WAIT_NS = 200ull * 1000ull * 1000ull;
 
 template <int D> struct PromptCfg {
     static constexpr int G = D / 64, TILE = 128 * D * 2;                    // bytes of a 128-row operand tile
-    static constexpr int Q = 0, K = 2 * TILE, V = K + STAGES * TILE, BARS = V + STAGES * TILE;
-    static constexpr int BYTES = BARS + 256;                                // then the items before every request
+    static constexpr int TB = kv::tile_bytes(D);
+    static constexpr int Q = 0, K = 2 * TILE, V = K + STAGES * TILE, RAW = V + STAGES * TILE;
+    static constexpr int BARS = RAW + UNPACK_WARPS * 2 * TB;                // RAW: two tiles of the cache for each unpacking warp
+    static constexpr int BYTES = BARS + 256;                                // then the items before every (fourth) request
 };
 
 __device__ __forceinline__ u32 smem_u32(const void* p) { return (u32)__cvta_generic_to_shared(p); }
@@ -189,16 +189,20 @@ __device__ __forceinline__ int request_items(const KvAttnArgs& A, int r) {
     return q.n > 0 && rows >= A.prompt_rows ? (int)((rows + 255) / 256) * A.Hk : 0;
 }
 
-__device__ __forceinline__ Item find_item(const KvAttnArgs& A, const int* before, int item) {
-    int lo = 0, hi = A.R;
+// before[i]: items before request i << shift (every request, or every fourth one where there are more than 1024)
+__device__ __forceinline__ Item find_item(const KvAttnArgs& A, const int* before, int shift, int item) {
+    int lo = 0, hi = ((A.R - 1) >> shift) + 1;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (before[mid] <= item) lo = mid; else hi = mid;
     }
     Item it;
-    it.r = lo;
-    it.rq = kv_request(A, lo);
-    const int rows = it.rq.n * A.ratio, tiles = (rows + 255) / 256, i = item - before[lo];
+    int i = item - before[lo];
+    it.r = lo << shift;
+    if (shift)
+        for (int n; i >= (n = request_items(A, it.r)); ++it.r) i -= n;
+    it.rq = kv_request(A, it.r);
+    const int rows = it.rq.n * A.ratio, tiles = (rows + 255) / 256;
     it.hk = i % A.Hk;
     it.row0 = (tiles - 1 - i / A.Hk) * 256;
     it.rows = min(256, rows - it.row0);
@@ -209,17 +213,10 @@ __device__ __forceinline__ Item find_item(const KvAttnArgs& A, const int* before
     return it;
 }
 
-// One 16-token tile's words (lane L = 4 g + t: see the cache's format).
-template <int G> struct TileWords {
-    uint4 k[G], v[G];
-    u32 kp[2][G], vp[4][G];              // parameters: keys of tokens g, g + 8; values of tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
-    u32 absent;                          // it has keys, and its page is missing
-};
-
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs A, u32* status) {
     typedef PromptCfg<D> Cfg;
-    constexpr int G = Cfg::G, TB = kv::tile_bytes(D);
+    constexpr int G = Cfg::G, TB = Cfg::TB;
     extern __shared__ unsigned char raw_smem[];
     __shared__ u32 tmem_slot;
     __shared__ int abort_flag;
@@ -227,7 +224,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
     __shared__ unsigned char absent_tiles[4][8];           // by block: a stage is refilled before the last softmax warp has looked
     const u32 base = (smem_u32(raw_smem) + 1023u) & ~1023u;
     unsigned char* smem = raw_smem + (base - smem_u32(raw_smem));
-    int* before = reinterpret_cast<int*>(smem + Cfg::BYTES);               // [R + 1] items before request r
+    int* before = reinterpret_cast<int*>(smem + Cfg::BYTES);               // items before request i << shift
+    const int shift = A.R <= 1024 ? 0 : 2;
     const u32 bars = base + Cfg::BARS;
     const u32 q_full = bars, s_full = bars + 16, p_full = bars + 32, o_done = bars + 48;                 // + 8 * tile
     const u32 k_full = bars + 64, v_full = bars + 80, k_empty = bars + 96, v_empty = bars + 112, drain = bars + 128;   // + 8 * stage
@@ -237,11 +235,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     // ---- items before every request
-    if (tid == 0) { abort_flag = 0; before[0] = 0; }
+    if (tid == 0) abort_flag = 0;
     int total = 0;
     for (int r0 = 0, turn = 0; r0 < A.R; r0 += THREADS, turn ^= 1) {
         const int r = r0 + tid;
-        int v = r < A.R ? request_items(A, r) : 0;
+        const int own = r < A.R ? request_items(A, r) : 0;
+        int v = own;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const int u = __shfl_up_sync(~0u, v, d);
@@ -249,12 +248,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
         }
         if (lane == 31) warp_sum[turn][warp] = v;
         __syncthreads();
-        v += total;
+        v += total - own;
         for (int w = 0; w < THREADS / 32; ++w) {
             if (w < warp) v += warp_sum[turn][w];
             total += warp_sum[turn][w];
         }
-        if (r < A.R) before[r + 1] = v;
+        if (r < A.R && (r & ((1 << shift) - 1)) == 0) before[r >> shift] = v;
     }
     if ((int)blockIdx.x >= total) return;                                  // the same for the whole CTA
     if (tid == 0) {
@@ -263,8 +262,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
             mbar_init(s_full + 8 * i, 1);
             mbar_init(p_full + 8 * i, 128);
             mbar_init(o_done + 8 * i, 1);
-            mbar_init(k_full + 8 * i, UNPACK_WARPS);
-            mbar_init(v_full + 8 * i, UNPACK_WARPS);
+            mbar_init(k_full + 8 * i, BN / kv::TILE);
+            mbar_init(v_full + 8 * i, BN / kv::TILE);
             mbar_init(k_empty + 8 * i, 1);
             mbar_init(v_empty + 8 * i, 1);
         }
@@ -279,6 +278,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
     __syncthreads();
     tc_after();
     const u32 tmem = tmem_slot;
+    // the CTA's items: forwards and backwards in turn through the CTAs, which evens out lists that run from long to short
+    const int ctas = min((int)gridDim.x, total);
+    auto item_at = [&](int turn) { return turn * ctas + ((turn & 1) ? ctas - 1 - (int)blockIdx.x : (int)blockIdx.x); };
 
     if (warp < SOFTMAX_WARPS) {
         // ------------------------------------------------------------------ softmax: this thread's row of tile `half`
@@ -289,14 +291,15 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
         const u32 q_tile = base + Cfg::Q + half * Cfg::TILE;
         u32 s_phase = 0, o_phase = 0, block = 0;                           // block: of all items, for the stage of absent_tiles
         bool ok = true;
-        for (int item = blockIdx.x; item < total && ok; item += gridDim.x) {
-            const Item it = find_item(A, before, item);
+        for (int item = item_at(0), turn = 0; item < total && ok; item = item_at(++turn)) {
+            const Item it = find_item(A, before, shift, item);
             const int n = half ? it.n1 : it.n0, n_both = max(it.n0, it.n1);
             const bool in = 128 * half + row_in < it.rows;
             const int row = it.row0 + 128 * half + (in ? row_in : 0), i = row / A.ratio;
             const size_t out_at = (size_t)(it.rq.q0 + i) * A.H + it.hk * A.ratio + (row - i * A.ratio);
             const int pos = it.rq.pos0 + i, see_lo = kv_first(A, pos), see_hi = in ? kv_end(A, it.rq, pos) : 0;
-            float m = -1e30f, l = 0.f, sc = 0.f;
+            float m = -1e30f, sc = 0.f;
+            float2 l = make_float2(0.f, 0.f);                                // the sum, even and odd keys
             if (n > 0) {
                 // the row as fp16, times a power of two that puts its largest element at 2^10
                 const __nv_bfloat16* qp = (const __nv_bfloat16*)A.q + (size_t)(it.rq.q0 + i) * A.q_stride +
@@ -354,42 +357,49 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
                     }
                     if (top > -1e30f) m = top - BELOW;
                 }
-                u32 v[2][32];
-                tmem_ld32(t_s, v[0]);
-#pragma unroll
+                u32 v[32];
+                tmem_ld32(t_s, v);
+#pragma unroll 1
                 for (int c = 0; c < 4; ++c) {
-                    u32 (&w)[32] = v[c & 1];
-                    tmem_wait_ld(w);
-                    if (c < 3) tmem_ld32(t_s + 32u * (c + 1), v[(c + 1) & 1]);
-                    float x[32], top = -INFINITY;
+                    tmem_wait_ld(v);
+                    float2 x[16];                                           // packed: two per instruction
 #pragma unroll
-                    for (int e = 0; e < 32; e += 2) {                       // packed: two per instruction
-                        const float2 y = __ffma2_rn(make_float2(__uint_as_float(w[e]), __uint_as_float(w[e + 1])), make_float2(sc, sc), make_float2(-m, -m));
-                        x[e] = y.x;
-                        x[e + 1] = y.y;
-                    }
+                    for (int e = 0; e < 16; ++e)
+                        x[e] = __ffma2_rn(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), make_float2(sc, sc), make_float2(-m, -m));
+                    if (c < 3) tmem_ld32(t_s + 32u * (c + 1), v);
                     if (!whole) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (!seen(32 * c + e)) x[e] = -INFINITY;
+                        for (int e = 0; e < 16; ++e) {
+                            if (!seen(32 * c + 2 * e)) x[e].x = -INFINITY;
+                            if (!seen(32 * c + 2 * e + 1)) x[e].y = -INFINITY;
+                        }
                     }
+                    float top = -INFINITY;
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) top = fmaxf(top, x[e]);
+                    for (int e = 0; e < 16; ++e) top = fmaxf(top, fmaxf(x[e].x, x[e].y));
                     if (__any_sync(~0u, top > RAISE)) {
                         // raised: what was summed under the old reference is scaled, in l, O and this block's part of P
+                        u32 w[32];
+                        if (c < 3) tmem_wait_ld(v);
+                        tmem_ld32(t_s + 32u * c, w);
+                        tmem_wait_ld(w);
                         float best = -INFINITY;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (x[e] != -INFINITY) best = fmaxf(best, __uint_as_float(w[e]) * sc);
+                        for (int e = 0; e < 16; ++e) {
+                            if (x[e].x != -INFINITY) best = fmaxf(best, __uint_as_float(w[2 * e]) * sc);
+                            if (x[e].y != -INFINITY) best = fmaxf(best, __uint_as_float(w[2 * e + 1]) * sc);
+                        }
                         const float to = top > RAISE ? best - BELOW : m, f = kv_exp2(m - to);
                         if (top > RAISE) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (x[e] != -INFINITY) x[e] = fmaf(__uint_as_float(w[e]), sc, -to);
+                            for (int e = 0; e < 16; ++e) {
+                                if (x[e].x != -INFINITY) x[e].x = fmaf(__uint_as_float(w[2 * e]), sc, -to);
+                                if (x[e].y != -INFINITY) x[e].y = fmaf(__uint_as_float(w[2 * e + 1]), sc, -to);
+                            }
                         }
                         m = to;
-                        l *= f;
-                        if (c < 3) tmem_wait_ld(v[(c + 1) & 1]);
+                        l.x *= f;
+                        l.y *= f;
                         const u32 f2 = half2_bits(f, f);
 #pragma unroll 1
                         for (int b = 0; b < c; ++b) {
@@ -405,24 +415,21 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
                             tc_after();
 #pragma unroll 1
                             for (int b = 0; ok && b < D / 32; ++b) {
-                                u32 y[32];
-                                tmem_ld32(t_o + 32u * b, y);
-                                tmem_wait_ld(y);
+                                tmem_ld32(t_o + 32u * b, w);
+                                tmem_wait_ld(w);
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
-                                tmem_st32(t_o + 32u * b, y);
+                                for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * f);
+                                tmem_st32(t_o + 32u * b, w);
                             }
                         }
                     }
                     u32 p[16];
-                    float2 l2[2] = {make_float2(l, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        const float a = kv_exp2(x[e]), b = kv_exp2(x[e + 1]);
-                        l2[e / 2 & 1] = __fadd2_rn(l2[e / 2 & 1], make_float2(a, b));
-                        p[e / 2] = half2_bits(a, b);
+                    for (int e = 0; e < 16; ++e) {
+                        const float2 y = make_float2(kv_exp2(x[e].x), kv_exp2(x[e].y));
+                        l = __fadd2_rn(l, y);
+                        p[e] = half2_bits(y.x, y.y);
                     }
-                    l = (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
                     tmem_st16(t_s + 16u * c, p);
                 }
                 tmem_wait_st();
@@ -437,7 +444,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
                 if (!ok) break;
                 tc_after();
             }
-            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const float sum = l.x + l.y, inv = sum == 0.f ? 0.f : 1.f / sum;
             __nv_bfloat16* out = (__nv_bfloat16*)A.out + out_at * D;
 #pragma unroll 1
             for (int b = 0; b < D / 32; ++b) {
@@ -455,109 +462,113 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
                         const __nv_bfloat162 h = __floats2bfloat162_rn(a, c);
                         z[k] = *reinterpret_cast<const u32*>(&h);
                     }
-                    if (in) *reinterpret_cast<uint4*>(out + 32 * b + e) = l == 0.f ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(z[0], z[1], z[2], z[3]);
+                    if (in) *reinterpret_cast<uint4*>(out + 32 * b + e) = sum == 0.f ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(z[0], z[1], z[2], z[3]);
                 }
                 __syncwarp();
             }
-            if (in && A.lse) A.lse[out_at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718f;
+            if (in && A.lse) A.lse[out_at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.69314718f;
             tc_before();
         }
     } else if (warp < SOFTMAX_WARPS + UNPACK_WARPS) {
-        // ------------------------------------------------------------------ unpacking: 16-token tiles 2 w and 2 w + 1 of every block
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 " KV_REGS_UNPACK ";");
+        // ------------------------------------------------------------------ unpacking: every sixth 16-token tile of an item's blocks
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 " KV_REGS_OTHERS ";");
+        constexpr int PER_BLOCK = BN / kv::TILE;
         const int w = warp - SOFTMAX_WARPS, g = lane >> 2, t = lane & 3;
         const int tiles_per_page = A.page_size / kv::TILE;
-        auto fetch = [&](const Item& it, int j, int i, TileWords<G>& b) {
-            const int tile = (it.first + j) * (BN / kv::TILE) + 2 * w + i, key0 = tile * kv::TILE;
-            const int at = tile / tiles_per_page;
-            int page = -1;
-            b.absent = 0u;
-            if (key0 < it.rq.len) {
-                page = A.table[(size_t)it.r * A.max_blocks + at];
-                if ((u32)page >= (u32)A.n_pages) { page = -1; b.absent = 1u; }
-            }
-            const unsigned char* src = A.pages + (((size_t)max(page, 0) * A.Hk + it.hk) * tiles_per_page + (tile - at * tiles_per_page)) * TB;
-#pragma unroll
-            for (int gr = 0; gr < G; ++gr) {
-                b.k[gr] = page >= 0 ? __ldg(reinterpret_cast<const uint4*>(src + gr * 512) + lane) : make_uint4(0u, 0u, 0u, 0u);
-                b.v[gr] = page >= 0 ? __ldg(reinterpret_cast<const uint4*>(src + (G + gr) * 512) + lane) : make_uint4(0u, 0u, 0u, 0u);
-            }
-            const u32* params = reinterpret_cast<const u32*>(src) + kv::param_words(G);
-            auto params_of = [&](int token, int from, u32 (&p)[G]) {         // zeros for tokens that are not there: a value of 0
-#pragma unroll
-                for (int gr = 0; gr < G; ++gr) p[gr] = page >= 0 && key0 + token < it.rq.len ? __ldg(params + token * 2 * G + from + gr) : 0u;
-            };
-            params_of(g, 0, b.kp[0]);
-            params_of(g + 8, 0, b.kp[1]);
-            params_of(2 * t, G, b.vp[0]);
-            params_of(2 * t + 1, G, b.vp[1]);
-            params_of(2 * t + 8, G, b.vp[2]);
-            params_of(2 * t + 9, G, b.vp[3]);
-        };
-        u32 stage = 0, phase = 0, block = 0;
+        unsigned char* raw = smem + Cfg::RAW + w * 2 * TB;
+        const u32 raw_addr = base + Cfg::RAW + w * 2 * TB;
+        u32 block = 0;                                                     // blocks of the items before
         bool ok = true;
-        for (int item = blockIdx.x; item < total && ok; item += gridDim.x) {
-            const Item it = find_item(A, before, item);
-            const int n = max(it.n0, it.n1);
-            TileWords<G> now, next;
-            if (n > 0) fetch(it, 0, 0, now);
-            for (int j = 0; j < n && ok; ++j) {
-                const u32 kt = base + Cfg::K + stage * Cfg::TILE, vt = base + Cfg::V + stage * Cfg::TILE;
+        for (int item = item_at(0), turn = 0; item < total && ok; item = item_at(++turn)) {
+            const Item it = find_item(A, before, shift, item);
+            const int n = max(it.n0, it.n1), steps = n * PER_BLOCK, tile0 = it.first * PER_BLOCK;
+            const int32_t* row_table = A.table + (size_t)it.r * A.max_blocks;
+            int ids = 0, in_ids = 32;
+            u32 there = 0;                                                 // bit b: the tile in buffer b came
+            auto fetch = [&](int step, int buffer) {                        // tile `step` of the item into a buffer
+                if (step < steps) {
+                    if (in_ids == 32) {                                     // lane i: the page of the i-th tile from here on, -1: missing, -2: no keys
+                        const int tile = tile0 + step + UNPACK_WARPS * lane;
+                        ids = tile * kv::TILE < it.rq.len ? row_table[tile / tiles_per_page] : -2;
+                        if (ids != -2 && (u32)ids >= (u32)A.n_pages) ids = -1;
+                        in_ids = 0;
+                    }
+                    const int page = __shfl_sync(~0u, ids, in_ids), tile = tile0 + step;
+                    ++in_ids;
+                    there &= ~(0x101u << buffer);
+                    there |= (page >= 0 ? 1u : page == -1 ? 0x100u : 0u) << buffer;                       // bits 8, 9: missing
+                    if (page >= 0) {
+                        const unsigned char* src = A.pages + (((size_t)page * A.Hk + it.hk) * tiles_per_page + tile % tiles_per_page) * TB + lane * 16;
+                        const u32 dst = raw_addr + buffer * TB + lane * 16;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if (i == 0) fetch(it, j, 1, next);
-                    else if (j + 1 < n) fetch(it, j + 1, 0, next);
-                    if (i == 0) {
-                        ok = __all_sync(~0u, mbar_wait(k_empty + 8 * stage, phase ^ 1u, abortp, status));
-                        if (!ok) break;
+                        for (int c = 0; c < TB / 16; c += 32)
+                            if (c + 32 <= TB / 16 || c + lane < TB / 16)
+                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + c * 16), "l"(src + c * 16) : "memory");
                     }
-#pragma unroll
-                    for (int gr = 0; gr < G; ++gr) {
-                        const int row = (2 * w + i) * kv::TILE + g;
-                        const u32 half = kt + gr * (128 * 128);
-                        st_shared(half + swizzled(row, 2 * t), unpack_word(now.k[gr].x, now.kp[0][gr]));
-                        st_shared(half + swizzled(row, 2 * t + 1), unpack_word(now.k[gr].y, now.kp[0][gr]));
-                        st_shared(half + swizzled(row + 8, 2 * t), unpack_word(now.k[gr].z, now.kp[1][gr]));
-                        st_shared(half + swizzled(row + 8, 2 * t + 1), unpack_word(now.k[gr].w, now.kp[1][gr]));
-                    }
-                    if (lane == 0) absent_tiles[block & 3][2 * w + i] = (unsigned char)now.absent;
-                    if (i == 1) {
-                        to_async_proxy();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(k_full + 8 * stage);
-                    } else {
-                        ok = __all_sync(~0u, mbar_wait(v_empty + 8 * stage, phase ^ 1u, abortp, status));
-                        if (!ok) break;
-                    }
-#pragma unroll
-                    for (int gr = 0; gr < G; ++gr) {
-                        const int row = (2 * w + i) * kv::TILE + 2 * t;
-                        const u32 half = vt + gr * (128 * 128);
-                        st_shared(half + swizzled(row, g), unpack_word(now.v[gr].x, now.vp[0][gr]));
-                        st_shared(half + swizzled(row + 1, g), unpack_word(now.v[gr].y, now.vp[1][gr]));
-                        st_shared(half + swizzled(row + 8, g), unpack_word(now.v[gr].z, now.vp[2][gr]));
-                        st_shared(half + swizzled(row + 9, g), unpack_word(now.v[gr].w, now.vp[3][gr]));
-                    }
-                    if (i == 1) {
-                        to_async_proxy();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(v_full + 8 * stage);
-                    }
-                    now = next;
                 }
-                ++block;
-                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            };
+            fetch(w, 0);
+            int buffer = 0;
+            for (int step = w; step < steps; step += UNPACK_WARPS, buffer ^= 1) {
+                fetch(step + UNPACK_WARPS, buffer ^ 1);
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+                __syncwarp();
+                const int j = step / PER_BLOCK, in_block = step % PER_BLOCK, key0 = (tile0 + step) * kv::TILE;
+                const u32 b = block + j, stage = b & 1u, parity = (b >> 1 & 1u) ^ 1u;
+                const bool came = there >> buffer & 1u;
+                const unsigned char* src = raw + buffer * TB;
+                const u32* params = reinterpret_cast<const u32*>(src) + kv::param_words(G);
+                auto words = [&](int at) { return came ? *reinterpret_cast<const uint4*>(src + at * 512 + lane * 16) : make_uint4(0u, 0u, 0u, 0u); };
+                auto param = [&](int token, int at) {                       // zero for a token that is not there: its values are 0
+                    return came && key0 + token < it.rq.len ? params[token * 2 * G + at] : 0u;
+                };
+                const u32 kt = base + Cfg::K + stage * Cfg::TILE, vt = base + Cfg::V + stage * Cfg::TILE;
+                ok = __all_sync(~0u, mbar_wait(k_empty + 8 * stage, parity, abortp, status));
+                if (!ok) break;
+#pragma unroll
+                for (int gr = 0; gr < G; ++gr) {
+                    const uint4 x = words(gr);
+                    const int row = in_block * kv::TILE + g;
+                    const u32 half = kt + gr * (128 * 128), p0 = param(g, gr), p1 = param(g + 8, gr);
+                    st_shared(half + swizzled(row, 2 * t), unpack_word(x.x, p0));
+                    st_shared(half + swizzled(row, 2 * t + 1), unpack_word(x.y, p0));
+                    st_shared(half + swizzled(row + 8, 2 * t), unpack_word(x.z, p1));
+                    st_shared(half + swizzled(row + 8, 2 * t + 1), unpack_word(x.w, p1));
+                }
+                if (lane == 0) absent_tiles[b & 3][in_block] = (unsigned char)(there >> (8 + buffer) & 1u);
+                to_async_proxy();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(k_full + 8 * stage);
+                ok = __all_sync(~0u, mbar_wait(v_empty + 8 * stage, parity, abortp, status));
+                if (!ok) break;
+#pragma unroll
+                for (int gr = 0; gr < G; ++gr) {
+                    const uint4 x = words(G + gr);
+                    const int row = in_block * kv::TILE + 2 * t;
+                    const u32 half = vt + gr * (128 * 128);
+                    st_shared(half + swizzled(row, g), unpack_word(x.x, param(2 * t, G + gr)));
+                    st_shared(half + swizzled(row + 1, g), unpack_word(x.y, param(2 * t + 1, G + gr)));
+                    st_shared(half + swizzled(row + 8, g), unpack_word(x.z, param(2 * t + 8, G + gr)));
+                    st_shared(half + swizzled(row + 9, g), unpack_word(x.w, param(2 * t + 9, G + gr)));
+                }
+                to_async_proxy();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(v_full + 8 * stage);
             }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();
+            block += n;
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 " KV_REGS_MMA ";");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 " KV_REGS_OTHERS ";");
     }
     if (warp == MMA_WARP && lane == 0) {
         // ------------------------------------------------------------------ MMA issue
         u32 block = 0, q_phase[2] = {0u, 0u}, p_phase[2] = {0u, 0u};
         bool ok = true;
-        for (int item = blockIdx.x; item < total && ok; item += gridDim.x) {
-            const Item it = find_item(A, before, item);
+        for (int item = item_at(0), turn = 0; item < total && ok; item = item_at(++turn)) {
+            const Item it = find_item(A, before, shift, item);
             const int n = max(it.n0, it.n1);
             auto stage_of = [&](int j) { return (block + j) & 1u; };
             auto phase_of = [&](int j) { return ((block + j) >> 1) & 1u; };
@@ -623,8 +634,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
 
 template <int D> int launch(const KvAttnArgs& A, u32* status, int device, int ctas, cudaStream_t st) {
     typedef PromptCfg<D> Cfg;
-    constexpr int MAX_SMEM = Cfg::BYTES + 1024 + (POP_KV_MAX_REQUESTS + 1) * 4;
-    static_assert(MAX_SMEM <= 225 * 1024, "shared memory");
+    constexpr int MAX_SMEM = Cfg::BYTES + 1024 + 1024 * 4;
+    static_assert((POP_KV_MAX_REQUESTS >> 2) <= 1024, "sums");
+    static_assert(MAX_SMEM <= 226 * 1024, "shared memory");
     static bool ready[64];                                     // set once per device; setting it twice does no harm
     if (device >= 64 || !ready[device]) {
         POP_CUDA(cudaFuncSetAttribute(kv_prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM));
@@ -633,7 +645,7 @@ template <int D> int launch(const KvAttnArgs& A, u32* status, int device, int ct
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas);
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = Cfg::BYTES + 1024 + (size_t)(A.R + 1) * 4;
+    cfg.dynamicSmemBytes = Cfg::BYTES + 1024 + (size_t)(((A.R - 1) >> (A.R <= 1024 ? 0 : 2)) + 1) * 4;
     cfg.stream = st;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
