@@ -8,10 +8,10 @@
 //   O_i += P_i V    (A operand from tensor memory, V from shared memory)     columns 256 + D i ..
 // A block costs the tensor cores 2048 cycles at D = 128, the exponentials (16 per cycle and SM) 2048, and shared memory (Q, K
 // and V read by the MMAs, K and V written by the unpacking warps) 2048, so everything has to run beside everything else:
-//   warps 0-3, 4-7   softmax of tile 0 and 1: one thread owns one row.  One pass over S: the reference m is only raised when a logit
-//                    passes it by 2^15 (fp16's room; it is set 2^7 below the row's largest logit so far), which rescales O and the
-//                    part of P written so far; after a row's first block that is rare.
-//   warps 8-13       unpack keys and values: 16-token tiles of the cache, brought to shared memory one tile ahead (cp.async), into fp16
+//   warps 0-3, 4-7   softmax of tile 0 and 1: one thread owns one row and holds its 128 products.  The reference m is only raised when a
+//                    logit passes it by 2^15 (fp16's room; it is set 2^7 below the row's largest logit so far), which rescales O; after a
+//                    row's first block that is rare.
+//   warps 8-13       unpack keys and values: 16-token tiles of the cache, brought to shared memory two steps ahead (cp.async), into fp16
 //                    in the MMAs' 128-byte swizzle: c - 8 exactly, then s (c - 8) + (z + 8 s) with one rounding each to 11 bits
 //   warp 14          issues the MMAs: tile 0's products run while tile 1's softmax does, and the other way round
 // The items of a request are dealt out from its last rows (most keys under a causal mask) to its first.
@@ -27,6 +27,7 @@ constexpr int SOFTMAX_WARPS = 8, UNPACK_WARPS = 6, MMA_WARP = 14;
 #define KV_REGS_SOFTMAX "184"
 #define KV_REGS_OTHERS "72"
 constexpr int STAGES = 2;                      // of unpacked key and value blocks
+constexpr int BUFFERS = 3;                     // of an unpacking warp: tiles on their way
 constexpr float RAISE = 15.f, BELOW = 7.f;
 constexpr unsigned long long WAIT_NS = 200ull * 1000ull * 1000ull;
 
@@ -34,7 +35,8 @@ template <int D> struct PromptCfg {
     static constexpr int G = D / 64, TILE = 128 * D * 2;                    // bytes of a 128-row operand tile
     static constexpr int TB = kv::tile_bytes(D);
     static constexpr int Q = 0, K = 2 * TILE, V = K + STAGES * TILE, RAW = V + STAGES * TILE;
-    static constexpr int BARS = RAW + UNPACK_WARPS * 2 * TB;                // RAW: two tiles of the cache for each unpacking warp
+    static constexpr int HALF = G * 512 + kv::TILE * G * 8;                 // a tile's keys or values with all its parameters
+    static constexpr int BARS = RAW + UNPACK_WARPS * BUFFERS * HALF;
     static constexpr int BYTES = BARS + 256;                                // then the items before every (fourth) request
 };
 
@@ -72,16 +74,23 @@ __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::befor
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void to_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-__device__ __forceinline__ void umma_ss(u32 d, u64 a, u64 b, u32 idesc, u32 accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+// The MMA warp stays together (so that descriptors live in uniform registers) and one lane of it issues.
+__device__ __forceinline__ u32 elect_lane() {
+    u32 mine;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(mine));
+    return mine;
 }
-__device__ __forceinline__ void umma_ts(u32 d, u32 a, u64 b, u32 idesc, u32 accumulate) {       // A from tensor memory
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+__device__ __forceinline__ void umma_ss(u32 mine, u32 d, u64 a, u64 b, u32 idesc, u32 accumulate) {
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(mine) : "memory");
 }
-__device__ __forceinline__ void umma_commit(u32 bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void umma_ts(u32 mine, u32 d, u32 a, u64 b, u32 idesc, u32 accumulate) {       // A from tensor memory
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(mine) : "memory");
+}
+__device__ __forceinline__ void umma_commit(u32 mine, u32 bar) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+                 ::"r"(bar), "r"(mine) : "memory");
 }
 // 32 consecutive columns of this thread's lane; the registers are valid after tmem_wait_ld().
 __device__ __forceinline__ void tmem_ld32(u32 addr, u32 (&r)[32]) {
@@ -99,16 +108,6 @@ __device__ __forceinline__ void tmem_wait_ld(u32 (&r)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
     for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));             // no use of them moves up over the wait
-}
-__device__ __forceinline__ void tmem_st32(u32 addr, const u32 (&r)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
-        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr) : "memory");
 }
 __device__ __forceinline__ void tmem_ld16(u32 addr, u32 (&r)[16]) {
     asm volatile(
@@ -299,7 +298,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
             const size_t out_at = (size_t)(it.rq.q0 + i) * A.H + it.hk * A.ratio + (row - i * A.ratio);
             const int pos = it.rq.pos0 + i, see_lo = kv_first(A, pos), see_hi = in ? kv_end(A, it.rq, pos) : 0;
             float m = -1e30f, sc = 0.f;
-            float2 l = make_float2(0.f, 0.f);                                // the sum, even and odd keys
+            float2 l[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};    // the sum, in four parts
             if (n > 0) {
                 // the row as fp16, times a power of two that puts its largest element at 2^10
                 const __nv_bfloat16* qp = (const __nv_bfloat16*)A.q + (size_t)(it.rq.q0 + i) * A.q_stride +
@@ -314,8 +313,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
 #pragma unroll
                     for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7fffu, w[e] >> 16 & 0x7fffu));
                 }
-                const float f = __uint_as_float((264u - max(top >> 7, 30u)) << 23);
-                sc = A.scale2 * __uint_as_float((254u << 23) - __float_as_uint(f));
+                float f = __uint_as_float((264u - max(top >> 7, 30u)) << 23);
+                // the scale's sign goes with the row, so that the largest product is the largest logit (and is never quite 0: a hidden key's
+                // -inf has to stay one)
+                sc = fmaxf(fabsf(A.scale2) * __uint_as_float((254u << 23) - __float_as_uint(f)), 1e-37f);
+                if (A.scale2 < 0.f) f = -f;
 #pragma unroll
                 for (int c = 0; c < D / 8; ++c) {
                     float x[8];
@@ -342,92 +344,53 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
                 auto seen = [&](int key) {                                  // key of the block
                     return key >= from && key < to_key && (((key < 64 ? absent.x : absent.y) >> ((key >> 4 & 3) * 8)) & 1u) == 0u;
                 };
-                if (j == 0) {                                               // the reference, from the first block's logits
-                    float top = -INFINITY;
-#pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        u32 v[32];
-                        tmem_ld32(t_s + 32u * c, v);
-                        tmem_wait_ld(v);
+                u32 v[4][32];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const float x = __uint_as_float(v[e]) * sc;
-                            if (whole || seen(32 * c + e)) top = fmaxf(top, x);
-                        }
-                    }
-                    if (top > -1e30f) m = top - BELOW;
+                for (int c = 0; c < 4; ++c) tmem_ld32(t_s + 32u * c, v[c]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_wait_ld(v[c]);
+                if (!whole) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!seen(32 * c + e)) v[c][e] = 0xff800000u;   // -inf
                 }
-                u32 v[32];
-                tmem_ld32(t_s, v);
-#pragma unroll 1
+                float tops[4];
+#pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    tmem_wait_ld(v);
-                    float2 x[16];                                           // packed: two per instruction
+                    tops[c] = -INFINITY;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        x[e] = __ffma2_rn(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), make_float2(sc, sc), make_float2(-m, -m));
-                    if (c < 3) tmem_ld32(t_s + 32u * (c + 1), v);
-                    if (!whole) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            if (!seen(32 * c + 2 * e)) x[e].x = -INFINITY;
-                            if (!seen(32 * c + 2 * e + 1)) x[e].y = -INFINITY;
-                        }
-                    }
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) top = fmaxf(top, fmaxf(x[e].x, x[e].y));
-                    if (__any_sync(~0u, top > RAISE)) {
-                        // raised: what was summed under the old reference is scaled, in l, O and this block's part of P
-                        u32 w[32];
-                        if (c < 3) tmem_wait_ld(v);
-                        tmem_ld32(t_s + 32u * c, w);
-                        tmem_wait_ld(w);
-                        float best = -INFINITY;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            if (x[e].x != -INFINITY) best = fmaxf(best, __uint_as_float(w[2 * e]) * sc);
-                            if (x[e].y != -INFINITY) best = fmaxf(best, __uint_as_float(w[2 * e + 1]) * sc);
-                        }
-                        const float to = top > RAISE ? best - BELOW : m, f = kv_exp2(m - to);
-                        if (top > RAISE) {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                if (x[e].x != -INFINITY) x[e].x = fmaf(__uint_as_float(w[2 * e]), sc, -to);
-                                if (x[e].y != -INFINITY) x[e].y = fmaf(__uint_as_float(w[2 * e + 1]), sc, -to);
-                            }
-                        }
-                        m = to;
-                        l.x *= f;
-                        l.y *= f;
-                        const u32 f2 = half2_bits(f, f);
+                    for (int e = 0; e < 32; e += 2) tops[c] = fmaxf(tops[c], fmaxf(__uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1])));
+                }
+                const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * sc;
+                if (__any_sync(~0u, top - m > RAISE)) {                     // (m starts far below anything)
+                    const float to = top - m > RAISE ? top - BELOW : m, f = kv_exp2(m - to);
+                    m = to;
+                    l[0] = __fmul2_rn(l[0], make_float2(f, f));
+                    l[1] = __fmul2_rn(l[1], make_float2(f, f));
+                    if (j > 0) {
+                        ok = __all_sync(~0u, mbar_wait(o_done + 8 * half, o_phase ^ 1u, abortp, status));      // the products of block j - 1 are in O
+                        tc_after();
 #pragma unroll 1
-                        for (int b = 0; b < c; ++b) {
+                        for (int b = 0; ok && b < D / 16; ++b) {
                             u32 y[16];
-                            tmem_wait_st();
-                            tmem_ld16(t_s + 16u * b, y);
+                            tmem_ld16(t_o + 16u * b, y);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) y[e] = hfma2(y[e], f2, 0u);
-                            tmem_st16(t_s + 16u * b, y);
-                        }
-                        if (j > 0) {
-                            ok = __all_sync(~0u, mbar_wait(o_done + 8 * half, o_phase ^ 1u, abortp, status));      // the products of block j - 1 are in O
-                            tc_after();
-#pragma unroll 1
-                            for (int b = 0; ok && b < D / 32; ++b) {
-                                tmem_ld32(t_o + 32u * b, w);
-                                tmem_wait_ld(w);
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * f);
-                                tmem_st32(t_o + 32u * b, w);
-                            }
+                            for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
+                            tmem_st16(t_o + 16u * b, y);
                         }
                     }
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
                     u32 p[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const float2 y = make_float2(kv_exp2(x[e].x), kv_exp2(x[e].y));
-                        l = __fadd2_rn(l, y);
+                    for (int e = 0; e < 16; ++e) {                          // packed: two per instruction
+                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[c][2 * e]), __uint_as_float(v[c][2 * e + 1])), make_float2(sc, sc),
+                                                    make_float2(-m, -m));
+                        const float2 y = make_float2(kv_exp2(x.x), kv_exp2(x.y));
+                        l[e & 1] = __fadd2_rn(l[e & 1], y);
                         p[e] = half2_bits(y.x, y.y);
                     }
                     tmem_st16(t_s + 16u * c, p);
@@ -444,7 +407,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
                 if (!ok) break;
                 tc_after();
             }
-            const float sum = l.x + l.y, inv = sum == 0.f ? 0.f : 1.f / sum;
+            const float sum = (l[0].x + l[0].y) + (l[1].x + l[1].y), inv = sum == 0.f ? 0.f : 1.f / sum;
             __nv_bfloat16* out = (__nv_bfloat16*)A.out + out_at * D;
 #pragma unroll 1
             for (int b = 0; b < D / 32; ++b) {
@@ -470,91 +433,112 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
             tc_before();
         }
     } else if (warp < SOFTMAX_WARPS + UNPACK_WARPS) {
-        // ------------------------------------------------------------------ unpacking: every sixth 16-token tile of an item's blocks
+        // ------------------------------------------------------------------ unpacking: every sixth step of an item
         asm volatile("setmaxnreg.dec.sync.aligned.u32 " KV_REGS_OTHERS ";");
         constexpr int PER_BLOCK = BN / kv::TILE;
         const int w = warp - SOFTMAX_WARPS, g = lane >> 2, t = lane & 3;
         const int tiles_per_page = A.page_size / kv::TILE;
-        unsigned char* raw = smem + Cfg::RAW + w * 2 * TB;
-        const u32 raw_addr = base + Cfg::RAW + w * 2 * TB;
+        unsigned char* raw = smem + Cfg::RAW + w * BUFFERS * Cfg::HALF;
+        const u32 raw_addr = base + Cfg::RAW + w * BUFFERS * Cfg::HALF;
         u32 block = 0;                                                     // blocks of the items before
         bool ok = true;
         for (int item = item_at(0), turn = 0; item < total && ok; item = item_at(++turn)) {
             const Item it = find_item(A, before, shift, item);
-            const int n = max(it.n0, it.n1), steps = n * PER_BLOCK, tile0 = it.first * PER_BLOCK;
+            const int n = max(it.n0, it.n1), steps = 2 * n * PER_BLOCK, tile0 = it.first * PER_BLOCK;
             const int32_t* row_table = A.table + (size_t)it.r * A.max_blocks;
+            // A step is the keys or the values of one tile, in the order in which they are needed: the keys of block 0, then those of block
+            // b + 1 and the values of block b in turn, at the end the last block's values.
+            auto step_at = [&](int step, int& j, int& in_block) {          // returns whether it is values
+                const int after = step - PER_BLOCK, round = after >> 4, i = after & 15;
+                const bool values = step >= PER_BLOCK && (i >= PER_BLOCK || round == n - 1);
+                j = step < PER_BLOCK ? 0 : values ? round : round + 1;
+                in_block = step & 7;
+                return values;
+            };
+            static_assert(PER_BLOCK == 8, "step_at");
             int ids = 0, in_ids = 32;
-            u32 there = 0;                                                 // bit b: the tile in buffer b came
-            auto fetch = [&](int step, int buffer) {                        // tile `step` of the item into a buffer
+            u32 there = 0;                                                 // bit b: the tile in buffer b came; bit 8 + b: its page is missing
+            auto fetch = [&](int step, int buffer) {
                 if (step < steps) {
-                    if (in_ids == 32) {                                     // lane i: the page of the i-th tile from here on, -1: missing, -2: no keys
-                        const int tile = tile0 + step + UNPACK_WARPS * lane;
+                    int j, in_block;
+                    if (in_ids == 32) {                                     // lane i: the page of the i-th step from here on, -1: missing, -2: no keys
+                        step_at(step + UNPACK_WARPS * lane, j, in_block);
+                        const int tile = tile0 + j * PER_BLOCK + in_block;
                         ids = tile * kv::TILE < it.rq.len ? row_table[tile / tiles_per_page] : -2;
                         if (ids != -2 && (u32)ids >= (u32)A.n_pages) ids = -1;
                         in_ids = 0;
                     }
-                    const int page = __shfl_sync(~0u, ids, in_ids), tile = tile0 + step;
+                    const bool values = step_at(step, j, in_block);
+                    const int page = __shfl_sync(~0u, ids, in_ids), tile = tile0 + j * PER_BLOCK + in_block;
                     ++in_ids;
                     there &= ~(0x101u << buffer);
-                    there |= (page >= 0 ? 1u : page == -1 ? 0x100u : 0u) << buffer;                       // bits 8, 9: missing
-                    if (page >= 0) {
-                        const unsigned char* src = A.pages + (((size_t)page * A.Hk + it.hk) * tiles_per_page + tile % tiles_per_page) * TB + lane * 16;
-                        const u32 dst = raw_addr + buffer * TB + lane * 16;
+                    there |= (page >= 0 ? 1u : page == -1 ? 0x100u : 0u) << buffer;
+                    if (page >= 0) {                                        // the codes of the keys or the values, and the parameters of both
+                        const unsigned char* src = A.pages + (((size_t)page * A.Hk + it.hk) * tiles_per_page + tile % tiles_per_page) * TB;
+                        const unsigned char* codes = src + (values ? G * 512 : 0);
+                        const u32 dst = raw_addr + buffer * Cfg::HALF;
 #pragma unroll
-                        for (int c = 0; c < TB / 16; c += 32)
-                            if (c + 32 <= TB / 16 || c + lane < TB / 16)
-                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + c * 16), "l"(src + c * 16) : "memory");
+                        for (int c = 0; c < G; ++c)
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (c * 32 + lane) * 16), "l"(codes + (c * 32 + lane) * 16) : "memory");
+                        if (lane < G * 8)
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (G * 32 + lane) * 16), "l"(src + (G * 64 + lane) * 16) : "memory");
                     }
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
             };
-            fetch(w, 0);
-            int buffer = 0;
-            for (int step = w; step < steps; step += UNPACK_WARPS, buffer ^= 1) {
-                fetch(step + UNPACK_WARPS, buffer ^ 1);
-                asm volatile("cp.async.wait_group 1;" ::: "memory");
+            int buffer_in = 0, buffer = 0;
+#pragma unroll
+            for (int s = 0; s < BUFFERS - 1; ++s) { fetch(w + s * UNPACK_WARPS, buffer_in); ++buffer_in; }
+            for (int step = w; step < steps; step += UNPACK_WARPS) {
+                fetch(step + (BUFFERS - 1) * UNPACK_WARPS, buffer_in);
+                if (++buffer_in == BUFFERS) buffer_in = 0;
+                asm volatile("cp.async.wait_group %0;" ::"n"(BUFFERS - 1) : "memory");
                 __syncwarp();
-                const int j = step / PER_BLOCK, in_block = step % PER_BLOCK, key0 = (tile0 + step) * kv::TILE;
+                int j, in_block;
+                const bool values = step_at(step, j, in_block);
+                const int key0 = (tile0 + j * PER_BLOCK + in_block) * kv::TILE;
                 const u32 b = block + j, stage = b & 1u, parity = (b >> 1 & 1u) ^ 1u;
                 const bool came = there >> buffer & 1u;
-                const unsigned char* src = raw + buffer * TB;
-                const u32* params = reinterpret_cast<const u32*>(src) + kv::param_words(G);
-                auto words = [&](int at) { return came ? *reinterpret_cast<const uint4*>(src + at * 512 + lane * 16) : make_uint4(0u, 0u, 0u, 0u); };
+                const unsigned char* src = raw + buffer * Cfg::HALF;
+                const u32* params = reinterpret_cast<const u32*>(src) + G * kv::GROUP_WORDS;
+                auto words = [&](int gr) { return came ? *reinterpret_cast<const uint4*>(src + gr * 512 + lane * 16) : make_uint4(0u, 0u, 0u, 0u); };
                 auto param = [&](int token, int at) {                       // zero for a token that is not there: its values are 0
                     return came && key0 + token < it.rq.len ? params[token * 2 * G + at] : 0u;
                 };
-                const u32 kt = base + Cfg::K + stage * Cfg::TILE, vt = base + Cfg::V + stage * Cfg::TILE;
-                ok = __all_sync(~0u, mbar_wait(k_empty + 8 * stage, parity, abortp, status));
-                if (!ok) break;
+                if (!values) {
+                    const u32 kt = base + Cfg::K + stage * Cfg::TILE;
+                    ok = __all_sync(~0u, mbar_wait(k_empty + 8 * stage, parity, abortp, status));
+                    if (!ok) break;
 #pragma unroll
-                for (int gr = 0; gr < G; ++gr) {
-                    const uint4 x = words(gr);
-                    const int row = in_block * kv::TILE + g;
-                    const u32 half = kt + gr * (128 * 128), p0 = param(g, gr), p1 = param(g + 8, gr);
-                    st_shared(half + swizzled(row, 2 * t), unpack_word(x.x, p0));
-                    st_shared(half + swizzled(row, 2 * t + 1), unpack_word(x.y, p0));
-                    st_shared(half + swizzled(row + 8, 2 * t), unpack_word(x.z, p1));
-                    st_shared(half + swizzled(row + 8, 2 * t + 1), unpack_word(x.w, p1));
+                    for (int gr = 0; gr < G; ++gr) {
+                        const uint4 x = words(gr);
+                        const int row = in_block * kv::TILE + g;
+                        const u32 half = kt + gr * (128 * 128), p0 = param(g, gr), p1 = param(g + 8, gr);
+                        st_shared(half + swizzled(row, 2 * t), unpack_word(x.x, p0));
+                        st_shared(half + swizzled(row, 2 * t + 1), unpack_word(x.y, p0));
+                        st_shared(half + swizzled(row + 8, 2 * t), unpack_word(x.z, p1));
+                        st_shared(half + swizzled(row + 8, 2 * t + 1), unpack_word(x.w, p1));
+                    }
+                    if (lane == 0) absent_tiles[b & 3][in_block] = (unsigned char)(there >> (8 + buffer) & 1u);
+                } else {
+                    const u32 vt = base + Cfg::V + stage * Cfg::TILE;
+                    ok = __all_sync(~0u, mbar_wait(v_empty + 8 * stage, parity, abortp, status));
+                    if (!ok) break;
+#pragma unroll
+                    for (int gr = 0; gr < G; ++gr) {
+                        const uint4 x = words(gr);
+                        const int row = in_block * kv::TILE + 2 * t;
+                        const u32 half = vt + gr * (128 * 128);
+                        st_shared(half + swizzled(row, g), unpack_word(x.x, param(2 * t, G + gr)));
+                        st_shared(half + swizzled(row + 1, g), unpack_word(x.y, param(2 * t + 1, G + gr)));
+                        st_shared(half + swizzled(row + 8, g), unpack_word(x.z, param(2 * t + 8, G + gr)));
+                        st_shared(half + swizzled(row + 9, g), unpack_word(x.w, param(2 * t + 9, G + gr)));
+                    }
                 }
-                if (lane == 0) absent_tiles[b & 3][in_block] = (unsigned char)(there >> (8 + buffer) & 1u);
                 to_async_proxy();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(k_full + 8 * stage);
-                ok = __all_sync(~0u, mbar_wait(v_empty + 8 * stage, parity, abortp, status));
-                if (!ok) break;
-#pragma unroll
-                for (int gr = 0; gr < G; ++gr) {
-                    const uint4 x = words(G + gr);
-                    const int row = in_block * kv::TILE + 2 * t;
-                    const u32 half = vt + gr * (128 * 128);
-                    st_shared(half + swizzled(row, g), unpack_word(x.x, param(2 * t, G + gr)));
-                    st_shared(half + swizzled(row + 1, g), unpack_word(x.y, param(2 * t + 1, G + gr)));
-                    st_shared(half + swizzled(row + 8, g), unpack_word(x.z, param(2 * t + 8, G + gr)));
-                    st_shared(half + swizzled(row + 9, g), unpack_word(x.w, param(2 * t + 9, G + gr)));
-                }
-                to_async_proxy();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(v_full + 8 * stage);
+                if (lane == 0) mbar_arrive((values ? v_full : k_full) + 8 * stage);
+                if (++buffer == BUFFERS) buffer = 0;
             }
             asm volatile("cp.async.wait_group 0;" ::: "memory");
             __syncwarp();
@@ -563,68 +547,77 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 " KV_REGS_OTHERS ";");
     }
-    if (warp == MMA_WARP && lane == 0) {
+    if (warp == MMA_WARP) {
         // ------------------------------------------------------------------ MMA issue
-        u32 block = 0, q_phase[2] = {0u, 0u}, p_phase[2] = {0u, 0u};
+        const u32 mine = elect_lane(), tm = __shfl_sync(~0u, tmem, 0);
+        const u64 dq = desc_k_major(base + Cfg::Q), dk = desc_k_major(base + Cfg::K), dv = desc_mn_major(base + Cfg::V);
+        u32 block = 0, q_phase = 0u, p_phase0 = 0u, p_phase1 = 0u;         // q_phase: a bit for each tile
         bool ok = true;
+        auto wait = [&](u32 bar, u32 parity) {
+            ok = __all_sync(~0u, mbar_wait(bar, parity, abortp, status));
+            return ok;
+        };
         for (int item = item_at(0), turn = 0; item < total && ok; item = item_at(++turn)) {
             const Item it = find_item(A, before, shift, item);
             const int n = max(it.n0, it.n1);
             auto stage_of = [&](int j) { return (block + j) & 1u; };
             auto phase_of = [&](int j) { return ((block + j) >> 1) & 1u; };
             auto scores = [&](int half, int j) {
-                const u32 q = base + Cfg::Q + half * Cfg::TILE, k = base + Cfg::K + stage_of(j) * Cfg::TILE;
+                const u64 q = dq + (u64)(half * (Cfg::TILE / 16)), k = dk + (u64)(stage_of(j) * (Cfg::TILE / 16));
 #pragma unroll
                 for (int s = 0; s < D / 16; ++s) {                          // 16 dimensions: 32 bytes along the swizzled row
-                    const u32 at = (s / 4) * (128 * 128) + (s % 4) * 32;
-                    umma_ss(tmem + 128u * half, desc_k_major(q + at), desc_k_major(k + at), IDESC_S, s > 0);
+                    const u64 at = (s / 4) * (128 * 128 / 16) + (s % 4) * 2;
+                    umma_ss(mine, tm + 128u * half, q + at, k + at, IDESC_S, s > 0);
                 }
-                umma_commit(s_full + 8 * half);
+                umma_commit(mine, s_full + 8 * half);
             };
             auto outputs = [&](int half, int j) {
-                const u32 v = base + Cfg::V + stage_of(j) * Cfg::TILE;
+                const u64 v = dv + (u64)(stage_of(j) * (Cfg::TILE / 16));
 #pragma unroll
                 for (int s = 0; s < BN / 16; ++s)                           // 16 keys: 8 columns of P, 16 rows of V
-                    umma_ts(tmem + 256u + (u32)(D * half), tmem + 128u * half + 8u * s, desc_mn_major(v + s * 16 * 128), IDESC_O<D>, j > 0 || s > 0);
-                umma_commit(o_done + 8 * half);
+                    umma_ts(mine, tm + 256u + (u32)(D * half), tm + 128u * half + 8u * s, v + (u64)(s * 16 * 128 / 16), IDESC_O<D>, j > 0 || s > 0);
+                umma_commit(mine, o_done + 8 * half);
             };
             if (n > 0) {
-                ok = mbar_wait(k_full + 8 * stage_of(0), phase_of(0), abortp, status);
-                for (int half = 0; half < 2 && ok; ++half)
-                    if ((half ? it.n1 : it.n0) > 0) {
-                        ok = mbar_wait(q_full + 8 * half, q_phase[half], abortp, status);
-                        if (!ok) break;
-                        q_phase[half] ^= 1u;
+                if (!wait(k_full + 8 * stage_of(0), phase_of(0))) break;
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                    if ((half ? it.n1 : it.n0) > 0 && ok) {
+                        if (!wait(q_full + 8 * half, q_phase >> half & 1u)) break;
+                        q_phase ^= 1u << half;
                         tc_after();
                         scores(half, 0);
                     }
                 if (!ok) break;
-                umma_commit(k_empty + 8 * stage_of(0));
+                umma_commit(mine, k_empty + 8 * stage_of(0));
             }
-            for (int j = 0; j < n && ok; ++j) {
-                if (j + 1 < n) ok = mbar_wait(k_full + 8 * stage_of(j + 1), phase_of(j + 1), abortp, status);
-                if (ok) ok = mbar_wait(v_full + 8 * stage_of(j), phase_of(j), abortp, status);
-                for (int half = 0; half < 2 && ok; ++half) {
-                    const int n_half = half ? it.n1 : it.n0;
-                    if (j < n_half) {
-                        ok = mbar_wait(p_full + 8 * half, p_phase[half], abortp, status);
-                        if (!ok) break;
-                        p_phase[half] ^= 1u;
-                        tc_after();
-                        outputs(half, j);
-                    }
-                    if (j + 1 < n_half) scores(half, j + 1);             // behind the products that read P out of the same columns
+            for (int j = 0; j < n; ++j) {
+                if (j + 1 < n && !wait(k_full + 8 * stage_of(j + 1), phase_of(j + 1))) break;
+                if (!wait(v_full + 8 * stage_of(j), phase_of(j))) break;
+                if (j < it.n0) {
+                    if (!wait(p_full, p_phase0)) break;
+                    p_phase0 ^= 1u;
+                    tc_after();
+                    outputs(0, j);
+                    if (j + 1 < it.n0) scores(0, j + 1);                    // behind the products that read P out of the same columns
                 }
-                if (!ok) break;
-                umma_commit(v_empty + 8 * stage_of(j));
-                if (j + 1 < n) umma_commit(k_empty + 8 * stage_of(j + 1));
+                if (j < it.n1) {
+                    if (!wait(p_full + 8, p_phase1)) break;
+                    p_phase1 ^= 1u;
+                    tc_after();
+                    outputs(1, j);
+                    if (j + 1 < it.n1) scores(1, j + 1);
+                }
+                umma_commit(mine, v_empty + 8 * stage_of(j));
+                if (j + 1 < n) umma_commit(mine, k_empty + 8 * stage_of(j + 1));
             }
             block += n;
         }
         // nothing of this CTA may still be executing on the tensor cores when tensor memory is given back
-        umma_commit(drain);
+        umma_commit(mine, drain);
         const unsigned long long t0 = pop_global_ns();
         while (!mbar_try_wait(drain, 0u) && pop_global_ns() - t0 < WAIT_NS) {}
+        __syncwarp();
     }
     tc_before();
     __syncthreads();
