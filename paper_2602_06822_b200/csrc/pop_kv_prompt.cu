@@ -11,9 +11,9 @@
 //   warps 0-3, 4-7   softmax of tile 0 and 1: one thread owns one row and holds its 128 products.  The reference m is only raised when a
 //                    logit passes it by 2^15 (fp16's room; it is set 2^7 below the row's largest logit so far), which rescales O; after a
 //                    row's first block that is rare.
-//   warps 8-13       unpack keys and values: 16-token tiles of the cache, brought to shared memory two steps ahead (cp.async), into fp16
+//   warps 8-14       unpack keys and values: 16-token tiles of the cache, brought to shared memory two steps ahead (cp.async), into fp16
 //                    in the MMAs' 128-byte swizzle: c - 8 exactly, then s (c - 8) + (z + 8 s) with one rounding each to 11 bits
-//   warp 14          issues the MMAs: tile 0's products run while tile 1's softmax does, and the other way round
+//   warp 15          issues the MMAs: tile 0's products run while tile 1's softmax does, and the other way round
 // The items of a request are dealt out from its last rows (most keys under a causal mask) to its first.
 // Every wait is bounded; one that runs out sets the status word and the CTA winds down.
 #include "pop_kv_attn.cuh"
@@ -21,8 +21,8 @@
 namespace {
 
 constexpr int BN = 128;                        // keys of a block
-constexpr int THREADS = 16 * 32;             // four warpgroups (warp 15 has nothing to do)
-constexpr int SOFTMAX_WARPS = 8, UNPACK_WARPS = 6, MMA_WARP = 14;
+constexpr int THREADS = 16 * 32;             // four warpgroups
+constexpr int SOFTMAX_WARPS = 8, UNPACK_WARPS = 7, MMA_WARP = 15;
 // registers of a thread after the split (the block is launched with 128): 2 * 184 + 2 * 72 = 4 * 128
 #define KV_REGS_SOFTMAX "184"
 #define KV_REGS_OTHERS "72"
@@ -159,14 +159,20 @@ __device__ __forceinline__ u32 hfma2(u32 a, u32 b, u32 c) {
     asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
     return r;
 }
-// The eight values of a word under the parameters p = (scale, zero).
-__device__ __forceinline__ uint4 unpack_word(u32 w, u32 p) {
-    const u32 s = __byte_perm(p, p, 0x1010), z = hfma2(s, 0x48004800u, __byte_perm(p, p, 0x3232)), v = w >> 8;     // z + 8 s
+// Scale and z + 8 s of a parameter word, each twice.
+struct ScaleZero { u32 s, z; };
+__device__ __forceinline__ ScaleZero scale_zero(u32 p) {
+    const u32 s = __byte_perm(p, p, 0x1010);
+    return {s, hfma2(s, 0x48004800u, __byte_perm(p, p, 0x3232))};
+}
+// The eight values of a word.
+__device__ __forceinline__ uint4 unpack_word(u32 w, const ScaleZero& p) {
+    const u32 v = w >> 8;
     uint4 r;
-    r.x = hfma2(hadd2(mask_or(w, 0x000f000fu, 0x64006400u), 0xe408e408u), s, z);                // (1024 + c) - 1032 = c - 8
-    r.y = hfma2(hadd2(mask_or(w, 0x00f000f0u, 0x54005400u), 0xd480d480u), s, z);                // (64 + c) - 72
-    r.z = hfma2(hadd2(mask_or(v, 0x000f000fu, 0x64006400u), 0xe408e408u), s, z);
-    r.w = hfma2(hadd2(mask_or(v, 0x00f000f0u, 0x54005400u), 0xd480d480u), s, z);
+    r.x = hfma2(hadd2(mask_or(w, 0x000f000fu, 0x64006400u), 0xe408e408u), p.s, p.z);            // (1024 + c) - 1032 = c - 8
+    r.y = hfma2(hadd2(mask_or(w, 0x00f000f0u, 0x54005400u), 0xd480d480u), p.s, p.z);            // (64 + c) - 72
+    r.z = hfma2(hadd2(mask_or(v, 0x000f000fu, 0x64006400u), 0xe408e408u), p.s, p.z);
+    r.w = hfma2(hadd2(mask_or(v, 0x00f000f0u, 0x54005400u), 0xd480d480u), p.s, p.z);
     return r;
 }
 __device__ __forceinline__ void st_shared(u32 addr, const uint4& v) {
@@ -433,13 +439,15 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
             tc_before();
         }
     } else if (warp < SOFTMAX_WARPS + UNPACK_WARPS) {
-        // ------------------------------------------------------------------ unpacking: every sixth step of an item
+        // ------------------------------------------------------------------ unpacking: every seventh step of an item
         asm volatile("setmaxnreg.dec.sync.aligned.u32 " KV_REGS_OTHERS ";");
         constexpr int PER_BLOCK = BN / kv::TILE;
         const int w = warp - SOFTMAX_WARPS, g = lane >> 2, t = lane & 3;
         const int tiles_per_page = A.page_size / kv::TILE;
         unsigned char* raw = smem + Cfg::RAW + w * BUFFERS * Cfg::HALF;
         const u32 raw_addr = base + Cfg::RAW + w * BUFFERS * Cfg::HALF;
+        // this lane's places in a tile's 16 rows of 128 bytes (8 rows further the swizzle is the same)
+        const u32 k_at[2] = {swizzled(g, 2 * t), swizzled(g, 2 * t + 1)}, v_at[2] = {swizzled(2 * t, g), swizzled(2 * t + 1, g)};
         u32 block = 0;                                                     // blocks of the items before
         bool ok = true;
         for (int item = item_at(0), turn = 0; item < total && ok; item = item_at(++turn)) {
@@ -456,32 +464,36 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
                 return values;
             };
             static_assert(PER_BLOCK == 8, "step_at");
-            int ids = 0, in_ids = 32;
-            u32 there = 0;                                                 // bit b: the tile in buffer b came; bit 8 + b: its page is missing
+            // Lane i keeps the source of the i-th step from here on: its address, or 0 (its page is missing) or 1 (it has no keys).
+            unsigned long long source = 0;
+            int in_sources = 32;
+            u32 state = 0;                                                 // two bits for each buffer: what came is 0 a tile, 1 part of one, 2 missing, 3 no keys
             auto fetch = [&](int step, int buffer) {
                 if (step < steps) {
-                    int j, in_block;
-                    if (in_ids == 32) {                                     // lane i: the page of the i-th step from here on, -1: missing, -2: no keys
-                        step_at(step + UNPACK_WARPS * lane, j, in_block);
+                    if (in_sources == 32) {
+                        int j, in_block;
+                        const bool values = step_at(step + UNPACK_WARPS * lane, j, in_block);
                         const int tile = tile0 + j * PER_BLOCK + in_block;
-                        ids = tile * kv::TILE < it.rq.len ? row_table[tile / tiles_per_page] : -2;
-                        if (ids != -2 && (u32)ids >= (u32)A.n_pages) ids = -1;
-                        in_ids = 0;
+                        source = 1;
+                        if (tile * kv::TILE < it.rq.len) {
+                            const int at = tile / tiles_per_page, page = row_table[at];
+                            const unsigned char* src = A.pages + (((size_t)(u32)page * A.Hk + it.hk) * tiles_per_page + (tile - at * tiles_per_page)) * TB;
+                            source = (u32)page >= (u32)A.n_pages ? 0ull : (unsigned long long)src | (values ? 8ull : 0ull) | ((tile + 1) * kv::TILE > it.rq.len ? 4ull : 0ull);
+                        }
+                        in_sources = 0;
                     }
-                    const bool values = step_at(step, j, in_block);
-                    const int page = __shfl_sync(~0u, ids, in_ids), tile = tile0 + j * PER_BLOCK + in_block;
-                    ++in_ids;
-                    there &= ~(0x101u << buffer);
-                    there |= (page >= 0 ? 1u : page == -1 ? 0x100u : 0u) << buffer;
-                    if (page >= 0) {                                        // the codes of the keys or the values, and the parameters of both
-                        const unsigned char* src = A.pages + (((size_t)page * A.Hk + it.hk) * tiles_per_page + tile % tiles_per_page) * TB;
-                        const unsigned char* codes = src + (values ? G * 512 : 0);
-                        const u32 dst = raw_addr + buffer * Cfg::HALF;
+                    const unsigned long long from = __shfl_sync(~0u, source, in_sources);
+                    ++in_sources;
+                    const u32 what = from >> 4 ? (u32)(from >> 2 & 1ull) : from ? 3u : 2u;
+                    state = (state & ~(3u << (2 * buffer))) | what << (2 * buffer);
+                    if (what < 2u) {                                        // the codes of the keys or the values, and the parameters of both
+                        const unsigned char* src = reinterpret_cast<const unsigned char*>(from & ~15ull) + lane * 16;
+                        const unsigned char* codes = src + ((from & 8ull) ? G * 512 : 0);
+                        const u32 dst = raw_addr + buffer * Cfg::HALF + lane * 16;
 #pragma unroll
                         for (int c = 0; c < G; ++c)
-                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (c * 32 + lane) * 16), "l"(codes + (c * 32 + lane) * 16) : "memory");
-                        if (lane < G * 8)
-                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (G * 32 + lane) * 16), "l"(src + (G * 64 + lane) * 16) : "memory");
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + c * 512), "l"(codes + c * 512) : "memory");
+                        if (lane < G * 8) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + G * 512), "l"(src + G * 1024) : "memory");
                     }
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
@@ -496,48 +508,56 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
                 __syncwarp();
                 int j, in_block;
                 const bool values = step_at(step, j, in_block);
-                const int key0 = (tile0 + j * PER_BLOCK + in_block) * kv::TILE;
-                const u32 b = block + j, stage = b & 1u, parity = (b >> 1 & 1u) ^ 1u;
-                const bool came = there >> buffer & 1u;
-                const unsigned char* src = raw + buffer * Cfg::HALF;
-                const u32* params = reinterpret_cast<const u32*>(src) + G * kv::GROUP_WORDS;
-                auto words = [&](int gr) { return came ? *reinterpret_cast<const uint4*>(src + gr * 512 + lane * 16) : make_uint4(0u, 0u, 0u, 0u); };
-                auto param = [&](int token, int at) {                       // zero for a token that is not there: its values are 0
-                    return came && key0 + token < it.rq.len ? params[token * 2 * G + at] : 0u;
-                };
+                const u32 b = block + j, stage = b & 1u, what = state >> (2 * buffer) & 3u;
+                unsigned char* src = raw + buffer * Cfg::HALF;
+                u32* params = reinterpret_cast<u32*>(src) + G * kv::GROUP_WORDS;
+                if (what != 0u) {                                           // tokens that are not there get values of 0
+                    const int key0 = (tile0 + j * PER_BLOCK + in_block) * kv::TILE;
+                    for (int i = lane; i < kv::TILE * 2 * G; i += 32)
+                        if (what > 1u || key0 + i / (2 * G) >= it.rq.len) params[i] = 0u;
+                    __syncwarp();
+                }
+                const u32 full = (values ? v_full : k_full) + 8 * stage;
+                ok = __all_sync(~0u, mbar_wait((values ? v_empty : k_empty) + 8 * stage, (b >> 1 & 1u) ^ 1u, abortp, status));
+                if (!ok) break;
+                const u32 to = base + (values ? Cfg::V : Cfg::K) + stage * Cfg::TILE + in_block * (kv::TILE * 128);
+                uint4 x[G];
+#pragma unroll
+                for (int gr = 0; gr < G; ++gr) x[gr] = *reinterpret_cast<const uint4*>(src + gr * 512 + lane * 16);
                 if (!values) {
-                    const u32 kt = base + Cfg::K + stage * Cfg::TILE;
-                    ok = __all_sync(~0u, mbar_wait(k_empty + 8 * stage, parity, abortp, status));
-                    if (!ok) break;
+                    // words 0, 1: token g, dimensions 16 t ..; words 2, 3: token g + 8
+                    u32 p[2][G];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int gr = 0; gr < G; ++gr) p[i][gr] = params[(g + 8 * i) * 2 * G + gr];
 #pragma unroll
                     for (int gr = 0; gr < G; ++gr) {
-                        const uint4 x = words(gr);
-                        const int row = in_block * kv::TILE + g;
-                        const u32 half = kt + gr * (128 * 128), p0 = param(g, gr), p1 = param(g + 8, gr);
-                        st_shared(half + swizzled(row, 2 * t), unpack_word(x.x, p0));
-                        st_shared(half + swizzled(row, 2 * t + 1), unpack_word(x.y, p0));
-                        st_shared(half + swizzled(row + 8, 2 * t), unpack_word(x.z, p1));
-                        st_shared(half + swizzled(row + 8, 2 * t + 1), unpack_word(x.w, p1));
+                        const ScaleZero p0 = scale_zero(p[0][gr]), p1 = scale_zero(p[1][gr]);
+                        st_shared(to + gr * (128 * 128) + k_at[0], unpack_word(x[gr].x, p0));
+                        st_shared(to + gr * (128 * 128) + k_at[1], unpack_word(x[gr].y, p0));
+                        st_shared(to + gr * (128 * 128) + 1024 + k_at[0], unpack_word(x[gr].z, p1));
+                        st_shared(to + gr * (128 * 128) + 1024 + k_at[1], unpack_word(x[gr].w, p1));
                     }
-                    if (lane == 0) absent_tiles[b & 3][in_block] = (unsigned char)(there >> (8 + buffer) & 1u);
+                    if (lane == 0) absent_tiles[b & 3][in_block] = what == 2u;
                 } else {
-                    const u32 vt = base + Cfg::V + stage * Cfg::TILE;
-                    ok = __all_sync(~0u, mbar_wait(v_empty + 8 * stage, parity, abortp, status));
-                    if (!ok) break;
+                    // words 0..3: tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9, dimensions 8 g ..
+                    u32 p[4][G];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int gr = 0; gr < G; ++gr) p[i][gr] = params[(2 * t + (i & 1) + 8 * (i >> 1)) * 2 * G + G + gr];
 #pragma unroll
                     for (int gr = 0; gr < G; ++gr) {
-                        const uint4 x = words(gr);
-                        const int row = in_block * kv::TILE + 2 * t;
-                        const u32 half = vt + gr * (128 * 128);
-                        st_shared(half + swizzled(row, g), unpack_word(x.x, param(2 * t, G + gr)));
-                        st_shared(half + swizzled(row + 1, g), unpack_word(x.y, param(2 * t + 1, G + gr)));
-                        st_shared(half + swizzled(row + 8, g), unpack_word(x.z, param(2 * t + 8, G + gr)));
-                        st_shared(half + swizzled(row + 9, g), unpack_word(x.w, param(2 * t + 9, G + gr)));
+                        st_shared(to + gr * (128 * 128) + v_at[0], unpack_word(x[gr].x, scale_zero(p[0][gr])));
+                        st_shared(to + gr * (128 * 128) + v_at[1], unpack_word(x[gr].y, scale_zero(p[1][gr])));
+                        st_shared(to + gr * (128 * 128) + 1024 + v_at[0], unpack_word(x[gr].z, scale_zero(p[2][gr])));
+                        st_shared(to + gr * (128 * 128) + 1024 + v_at[1], unpack_word(x[gr].w, scale_zero(p[3][gr])));
                     }
                 }
                 to_async_proxy();
                 __syncwarp();
-                if (lane == 0) mbar_arrive((values ? v_full : k_full) + 8 * stage);
+                if (lane == 0) mbar_arrive(full);
                 if (++buffer == BUFFERS) buffer = 0;
             }
             asm volatile("cp.async.wait_group 0;" ::: "memory");
