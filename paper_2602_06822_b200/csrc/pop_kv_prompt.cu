@@ -23,9 +23,9 @@ namespace {
 constexpr int BN = 128;                        // keys of a block
 constexpr int THREADS = 16 * 32;             // four warpgroups
 constexpr int SOFTMAX_WARPS = 8, UNPACK_WARPS = 7, MMA_WARP = 15;
-// registers of a thread after the split (the block is launched with 128): 2 * 184 + 2 * 72 = 4 * 128
-#define KV_REGS_SOFTMAX "184"
-#define KV_REGS_OTHERS "72"
+// registers of a thread after the split (the block is launched with 128): 2 * 200 + 2 * 56 = 4 * 128
+#define KV_REGS_SOFTMAX "200"
+#define KV_REGS_OTHERS "56"
 constexpr int STAGES = 2;                      // of unpacked key and value blocks
 constexpr int BUFFERS = 3;                     // of an unpacking warp: tiles on their way
 constexpr float RAISE = 15.f, BELOW = 7.f;
@@ -49,9 +49,9 @@ __device__ __forceinline__ u32 mbar_try_wait(u32 bar, u32 parity) {
     u32 ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok;
 }
 // Waits for the phase of the given parity; gives up (false) after WAIT_NS or when another role has.
