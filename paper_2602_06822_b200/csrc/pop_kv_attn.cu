@@ -53,11 +53,11 @@ extern "C" int pop_kv_attention(const pop_kv_cache_t* c, const void* q, long lon
     const bool prompts = dtype == POP_BF16 && (long long)n_tokens * ratio >= PROMPT_ROWS;     // there may be requests of that many rows
     const KvAttnArgs A = {(const unsigned char*)c->pages, c->n_pages, c->page_size, c->n_kv_heads, q, q_stride, n_heads, n_tokens, ratio,
                           q_indptr, kv_lens, n_requests, block_table, max_blocks, scale * 1.44269504f, causal, window, out, lse,
-                          prompts ? PROMPT_ROWS : INT_MAX};
+                          prompts ? (n_requests == 1 ? 1 : PROMPT_ROWS) : INT_MAX};
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (prompts) {
         rc = pop_launch_kv_attention_prompt(A, c->head_dim, (u32*)workspace, device, sms, st);
-        if (rc != POP_OK) return rc;
+        if (rc != POP_OK || n_requests == 1) return rc;         // (a single request is taken by one kernel, whatever its length)
     }
     const int ctas = sms < pop_kv_stream_max_ctas() ? sms : pop_kv_stream_max_ctas();
     return pop_launch_kv_attention_stream(A, c->head_dim, dtype, (char*)workspace + STATUS_BYTES, device, ctas, st);

@@ -346,10 +346,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
                 const int k0 = (it.first + j) * BN;
                 const uint2 absent = *reinterpret_cast<const uint2*>(absent_tiles[(block + j) & 3]);      // a byte for each 16 keys
                 const bool whole = k0 >= key_lo && k0 + BN <= key_hi && (absent.x | absent.y) == 0u;
-                const int from = see_lo - k0, to_key = see_hi - k0;
-                auto seen = [&](int key) {                                  // key of the block
-                    return key >= from && key < to_key && (((key < 64 ? absent.x : absent.y) >> ((key >> 4 & 3) * 8)) & 1u) == 0u;
-                };
                 u32 v[4][32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(t_s + 32u * c, v[c]);
@@ -357,10 +353,16 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
                 for (int c = 0; c < 4; ++c) tmem_wait_ld(v[c]);
                 if (!whole) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                    for (int c = 0; c < 4; ++c) {                           // a bit for each key that is seen
+                        const int from = min(max(see_lo - k0 - 32 * c, 0), 32), to_key = min(max(see_hi - k0 - 32 * c, 0), 32);
+                        const u32 gone = (c < 2 ? absent.x : absent.y) >> (16 * (c & 1));
+                        u32 seen = (to_key == 32 ? ~0u : (1u << to_key) - 1u) & (from == 32 ? 0u : ~0u << from);
+                        if (gone & 0x01u) seen &= 0xffff0000u;
+                        if (gone & 0x100u) seen &= 0x0000ffffu;
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
-                            if (!seen(32 * c + e)) v[c][e] = 0xff800000u;   // -inf
+                            if (!(seen >> e & 1u)) v[c][e] = 0xff800000u;     // -inf
+                    }
                 }
                 float tops[4];
 #pragma unroll

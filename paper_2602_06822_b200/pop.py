@@ -157,11 +157,17 @@ def region_sizes(N: int, ratios) -> Tuple[int, int, int, int]:
     return tuple(o.value for o in out)
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    if not torch.cuda.is_available():
-        raise RuntimeError("paper_2602_06822_b200 needs a CUDA device (there is no CPU path)")
-    return torch
+    global _torch_module
+    if _torch_module is None:                  # asked once: the question costs more than some of the calls
+        import torch
+        if not torch.cuda.is_available():
+            raise RuntimeError("paper_2602_06822_b200 needs a CUDA device (there is no CPU path)")
+        _torch_module = torch
+    return _torch_module
 
 
 def _dtype_code(t) -> int:
@@ -174,9 +180,10 @@ def _dtype_code(t) -> int:
 
 
 def _stream_ptr(stream=None) -> int:
-    torch = _torch()
-    s = torch.cuda.current_stream() if stream is None else stream
-    return int(s.cuda_stream)
+    if stream is None:
+        torch = _torch()
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return int(stream.cuda_stream)
 
 
 class _DevView:
