@@ -36,12 +36,6 @@ namespace {
 
 typedef unsigned long long ull;
 
-#ifndef KV_WARPS
-#define KV_WARPS 12
-#define KV_STAGES 3
-#define KV_STEP 2
-#endif
-
 template <typename T, int G, int NT> struct StreamCfg {
     static constexpr int D = 64 * G, ROWS = 8 * NT;
     static constexpr bool F32 = sizeof(T) == 4;
@@ -51,12 +45,12 @@ template <typename T, int G, int NT> struct StreamCfg {
     static constexpr float BELOW = F32 ? 0.f : 7.f;         // to this far below the logit
     // Tiles of a unit, which a warp works on at once: two independent chains of products, reductions and exponentials where
     // registers allow
-    static constexpr int STEP = (NT == 1 && !F32) ? KV_STEP : 1;
+    static constexpr int STEP = (NT == 1 && !F32) ? 2 : 1;
     static constexpr int TOKENS = STEP * kv::TILE;
-    static constexpr int WARPS = (NT == 1 && !F32) ? KV_WARPS : 8;
+    static constexpr int WARPS = (NT == 1 && !F32) ? 12 : 8;
     static constexpr int TB = kv::tile_bytes(D), UB = STEP * TB;
     static constexpr int PIECE = ROWS * (D + 4) * 4;        // un-normalised output, then (maximum, sum, -, -) of a part of a segment
-    static constexpr int MIN_STAGES = (PIECE + UB - 1) / UB, WANT = (G == 1 ? 2 : 1) * (NT == 1 && !F32 ? KV_STAGES : 5);
+    static constexpr int MIN_STAGES = (PIECE + UB - 1) / UB, WANT = (G == 1 ? 2 : 1) * (STEP == 2 ? 3 : 5);
     static constexpr int STAGES = MIN_STAGES > WANT ? MIN_STAGES : WANT;
     static constexpr int WARP_BYTES = STAGES * UB + PIECE;  // ring (its memory later holds the second piece) and first piece
 };
