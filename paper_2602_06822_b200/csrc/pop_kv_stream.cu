@@ -52,6 +52,9 @@ template <typename T, int G, int NT> struct StreamCfg {
     static constexpr int PIECE = ROWS * (D + 4) * 4;        // un-normalised output, then (maximum, sum, -, -) of a part of a segment
     static constexpr int MIN_STAGES = (PIECE + UB - 1) / UB, WANT = (G == 1 ? 2 : 1) * (STEP == 2 ? 3 : 5);
     static constexpr int STAGES = MIN_STAGES > WANT ? MIN_STAGES : WANT;
+    // Segments up to this many units are not cut between CTAs where the whole call is that small (see there; 8 kv heads of 300 tokens 10.3 -> 9.2
+    // us, of 1000 tokens it would be 10.7 -> 12.4)
+    static constexpr int SNAP = F32 ? 0 : WARPS;
     static constexpr int WARP_BYTES = STAGES * UB + PIECE;  // ring (its memory later holds the second piece) and first piece
 };
 
@@ -137,8 +140,9 @@ template <bool F32> __device__ __forceinline__ void code_pairs(u32 w, u32 (&x)[4
 
 __device__ __forceinline__ float2 half2_at(u32 w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 
-// Units (of TOKENS keys) that any query of a request sees: [first, first + count), count >= 1 as every segment has a unit that
-// writes its result.
+// Units (of TOKENS keys) of each row block's segment of a request: count >= 1, as every segment has a unit that writes its result.  Under a
+// causal window each row block has its own band of keys, `first` on; else all blocks are given the keys that any query of the request
+// sees.
 struct Units { int first, count, row_blocks; };
 template <int ROWS, int TOKENS> __device__ __forceinline__ Units request_units(const KvAttnArgs& A, const KvRequest& q) {
     Units t = {0, 0, 0};
@@ -148,10 +152,12 @@ template <int ROWS, int TOKENS> __device__ __forceinline__ Units request_units(c
     const int lo = min(kv_first(A, q.pos0), q.len), hi = kv_end(A, q, q.pos0 + q.n - 1);
     t.first = lo / TOKENS;
     t.count = max(1, (hi + TOKENS - 1) / TOKENS - t.first);
+    if (A.causal && A.window > 0 && t.row_blocks > 1) {
+        const int band = (A.window + (ROWS - 1) / A.ratio + TOKENS - 1) / TOKENS + 1;       // the rows of a block are of (ROWS - 1) / ratio + 2 tokens
+        if (band < t.count) { t.count = band; t.first = -1; }
+    }
     return t;
 }
-
-constexpr int SNAP = 40;                                       // units, see the kernel
 
 // The sums over the requests are kept for every request, or for every fourth one where there are more than 1024.
 constexpr int MAX_SUMS = 1024;
@@ -159,10 +165,10 @@ __host__ __device__ constexpr int sums_shift(int R) { return R <= MAX_SUMS ? 0 :
 static_assert((POP_KV_MAX_REQUESTS >> 2) <= MAX_SUMS, "sums");
 
 // Joins n parts of a segment's query row `col` that lie in shared memory: part k's output at places[k] (a byte offset), its maximum
-// and sum `stats` bytes further.  The result goes to the part `to` or, where that is NULL, to the output.  One small function for all
-// uses: this code runs once or twice a call, mostly from beyond the instruction cache.
+// and sum `stats` bytes further.  The result goes to the part `to` or, where that is NULL, to the output.  Small code, as it runs once
+// or twice a call, mostly from beyond the instruction cache.
 template <typename T, int D, int ROWS>
-__device__ __noinline__ void join_row(const KvAttnArgs& A, const PieceOf& seg, int col, const unsigned char* smem, const u32* places, int n,
+__device__ __forceinline__ void join_row(const KvAttnArgs& A, const PieceOf& seg, int col, const unsigned char* smem, const u32* places, int n,
                                       u32 stats, float* to, float2* carry) {
     constexpr int PER = D / 32;
     typedef typename std::conditional<PER == 4, float4, float2>::type Vec;
@@ -256,9 +262,9 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
     const ull share = div_units(U + gridDim.x - 1, gridDim.x);
     const int cta = blockIdx.x;
     ull ca = min(U, cta * share), cb = min(U, ca + share);
-    // Joining CTAs' parts takes some 5 us, in which a CTA goes through SNAP units.  So where there is no more than that to do for each, the
-    // cuts between CTAs are moved to the nearer end of a segment that is no longer than that either.
-    if (share < SNAP) {
+    // Where a CTA has no more than SNAP units to do, which costs it no more than joining would, the cuts between CTAs are moved to the
+    // nearer end of a segment that is no longer than that either.
+    if (Cfg::SNAP > 0 && share < (ull)Cfg::SNAP) {
         ull at = (lane & 1) ? cb : ca;
         if (at < U && at > 0) {
             int lo = 0, hi = ((A.R - 1) >> shift) + 1;
@@ -272,7 +278,7 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                 const ull all = (ull)un.count * un.row_blocks * A.Hk;
                 if (base + all <= at) { base += all; continue; }
                 const ull begin = base + div_units(at - base, un.count) * un.count;
-                if (un.count <= SNAP) at = 2 * (at - begin) < (ull)un.count ? begin : begin + un.count;
+                if (un.count <= Cfg::SNAP) at = 2 * (at - begin) < (ull)un.count ? begin : begin + un.count;
                 break;
             }
         }
@@ -311,8 +317,9 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
         const int p_lo = rq.pos0 + row0 / A.ratio, p_hi = rq.pos0 + (row0 + rows - 1) / A.ratio;
         const int all_lo = kv_first(A, p_hi), all_hi = kv_end(A, rq, p_lo);          // keys that every row sees
         const int some_lo = kv_first(A, p_lo), some_hi = kv_end(A, rq, p_hi);        // keys that any row sees
-        const int u_lo = max(un.first + (int)(u - sb), some_lo / Cfg::TOKENS);
-        const int u_hi = min(un.first + (int)(pe - sb), (some_hi + Cfg::TOKENS - 1) / Cfg::TOKENS);
+        const int first = un.first < 0 ? min(some_lo, rq.len) / Cfg::TOKENS : un.first;
+        const int u_lo = max(first + (int)(u - sb), some_lo / Cfg::TOKENS);
+        const int u_hi = min(first + (int)(pe - sb), (some_hi + Cfg::TOKENS - 1) / Cfg::TOKENS);
 
         // ---- the units, STAGES of them on their way.  Lane i keeps the id of page ids_from + i.
         const int32_t* row_table = A.table + (size_t)r * A.max_blocks;

@@ -7,6 +7,9 @@ and the residual stream are plain torch ops in bf16; every FFN goes through the 
 (`pop_prefill_partition_with_output` for the prompt, `pop_decode_step` per generated token), or,
 for the dense baseline of the latency table, through torch linear layers.
 
+With ``kv_cache="int4"`` keys and values go to the library's paged 4-bit cache instead and attention reads them there
+(`pop_kv_plan` once a step, `pop_kv_append` and `pop_kv_attention` in every layer).
+
 Weights are synthetic (seeded, ~ N(0, 0.02^2)); token ids are a seeded sequence that is fed
 teacher-forced, so that no sampling and no LM head are needed.
 """
@@ -40,9 +43,13 @@ def ratios_for(r: float, gamma: float = 0.1):
 
 
 class Decoder:
-    """ffn = "pop" (every FFN through the library, ratios given) or "dense" (torch linear layers)."""
+    """ffn = "pop" (every FFN through the library, ratios given) or "dense" (torch linear layers); kv_cache = "bf16" (torch) or
+    "int4" (the library's paged 4-bit cache, for up to kv_tokens tokens)."""
 
-    def __init__(self, cfg: DecoderConfig, device="cuda:0", ffn: str = "pop", ratios=None, k: Optional[int] = None):
+    def __init__(self, cfg: DecoderConfig, device="cuda:0", ffn: str = "pop", ratios=None, k: Optional[int] = None, kv_cache: str = "bf16",
+                 kv_tokens: int = 2048):
+        if kv_cache not in ("bf16", "int4"):
+            raise ValueError("kv_cache must be \"bf16\" or \"int4\"")
         self.cfg, self.dev, self.ffn = cfg, torch.device(device), ffn
         g = torch.Generator(device=self.dev)
         g.manual_seed(cfg.seed)
@@ -63,6 +70,8 @@ class Decoder:
         self.weights = [pop.Weights(l["Wg"], l["Wu"], l["Wd"]) for l in self.layers] if ffn == "pop" else None
         self.parts: List[Optional[pop.Partition]] = [None] * cfg.n_layers
         self.kv: List[Optional[tuple]] = [None] * cfg.n_layers
+        self.cache4 = pop.KVCache(cfg.n_layers, 1, kv_tokens, cfg.n_heads, self.hd, device=self.dev) if kv_cache == "int4" else None
+        self.one = torch.ones(1, device=self.dev, dtype=torch.int32)
         self.pos = 0
         self.trace = None          # when a dict: (layer, step) -> recorded FFN inputs / outputs, for layer-local parity
         self.timers = None         # when a dict: "attention" / "mlp" -> list of (start, end) CUDA events
@@ -87,6 +96,12 @@ class Decoder:
         q = self.rope(F.linear(a, L["Wq"]).view(T, cfg.n_heads, self.hd), pos0)
         kx = self.rope(F.linear(a, L["Wk"]).view(T, cfg.n_heads, self.hd), pos0)
         vx = F.linear(a, L["Wv"]).view(T, cfg.n_heads, self.hd)
+        if self.cache4 is not None:
+            self.cache4.append(li, kx, vx)
+            o = self.cache4.attend(li, q)
+            if self.trace is not None:
+                self.trace[("attention", li, pos0)] = (q, kx, vx, o)
+            return F.linear(o.view(T, cfg.d), L["Wo"])
         if self.kv[li] is None:
             K, V = kx, vx
         else:
@@ -116,6 +131,8 @@ class Decoder:
     def prefill(self, ids: torch.Tensor):
         """ids [T] prompt token ids -> hidden states [T, d] after the last layer.  Builds every layer's partition."""
         assert self.pos == 0
+        if self.cache4 is not None:
+            self.cache4.plan(torch.tensor([ids.shape[0]], device=self.dev, dtype=torch.int32), ids.shape[0])
         h = self.embed[ids]
         for li in range(self.cfg.n_layers):
             with self._timed("attention"):
@@ -137,6 +154,8 @@ class Decoder:
 
     def decode(self, tok: torch.Tensor, step: int = 0):
         """One teacher-forced token id [1] -> hidden state [1, d]."""
+        if self.cache4 is not None:
+            self.cache4.plan(self.one, 1)
         h = self.embed[tok]
         for li in range(self.cfg.n_layers):
             with self._timed("attention"):
@@ -169,7 +188,7 @@ class Decoder:
         self.ids_dev = ids_all.to(self.dev)
         self.pos_t = torch.tensor([self.pos], device=self.dev, dtype=torch.int64)
         self.kv_static = []
-        for li in range(cfg.n_layers):
+        for li in range(cfg.n_layers if self.cache4 is None else 0):      # (the 4-bit cache is static as it is)
             K = torch.zeros(max_len, cfg.n_heads, self.hd, device=self.dev, dtype=torch.bfloat16)
             V = torch.zeros_like(K)
             if self.kv[li] is not None:
@@ -182,6 +201,8 @@ class Decoder:
     def step_static(self, attention: bool = True, mlp: bool = True):
         """One teacher-forced token at the device-side position; no host-side value enters the launches."""
         cfg = self.cfg
+        if attention and self.cache4 is not None:
+            self.cache4.plan(self.one, 1)
         h = self.embed.index_select(0, self.ids_dev.index_select(0, self.pos_t))
         ang = self.pos_t.float()[:, None] * self.inv_freq[None, :]
         cos, sin = torch.cos(ang)[:, None, :], torch.sin(ang)[:, None, :]
@@ -199,11 +220,16 @@ class Decoder:
                 q = rope1(F.linear(a, L["Wq"]).view(1, cfg.n_heads, self.hd))
                 kx = rope1(F.linear(a, L["Wk"]).view(1, cfg.n_heads, self.hd))
                 vx = F.linear(a, L["Wv"]).view(1, cfg.n_heads, self.hd)
-                K, V = self.kv_static[li]
-                K.index_copy_(0, self.pos_t, kx)
-                V.index_copy_(0, self.pos_t, vx)
-                o = F.scaled_dot_product_attention(q.transpose(0, 1), K.transpose(0, 1), V.transpose(0, 1), attn_mask=mask)
-                h = h + F.linear(o.transpose(0, 1).reshape(1, cfg.d), L["Wo"])
+                if self.cache4 is not None:
+                    self.cache4.append(li, kx, vx)
+                    o = self.cache4.attend(li, q).view(1, cfg.d)
+                else:
+                    K, V = self.kv_static[li]
+                    K.index_copy_(0, self.pos_t, kx)
+                    V.index_copy_(0, self.pos_t, vx)
+                    o = F.scaled_dot_product_attention(q.transpose(0, 1), K.transpose(0, 1), V.transpose(0, 1), attn_mask=mask)
+                    o = o.transpose(0, 1).reshape(1, cfg.d)
+                h = h + F.linear(o, L["Wo"])
             if mlp:
                 f = self.rmsnorm(h)
                 if self.ffn == "pop":
@@ -216,11 +242,25 @@ class Decoder:
         self.pos_t += 1
         return h
 
+    def rewind(self, pos: int):
+        """Static decoding: back to `pos` tokens (the prompt's), so that a captured step can be replayed from there."""
+        self.pos_t.fill_(pos)
+        if self.cache4 is not None:
+            c = self.cache4
+            keep = -(-pos // c.page_size)                     # pages behind the prompt's are free again
+            c.lens.fill_(pos)
+            c.state.copy_(torch.tensor([keep, c.n_pages - keep], dtype=torch.int32))
+
     def reset(self):
         self.kv = [None] * self.cfg.n_layers
+        if self.cache4 is not None:
+            self.cache4.reset()
         self.pos = 0
 
     def close(self):
+        if self.cache4 is not None:
+            pop.kv_attention_check(self.dev)
+            self.cache4 = None
         for p in self.parts:
             if p is not None:
                 p.destroy()
@@ -237,8 +277,8 @@ def seeded_ids(cfg: DecoderConfig, n: int, seed: int, device) -> torch.Tensor:
     return torch.randint(0, cfg.vocab, (n,), generator=g).to(device)
 
 
-def _replay_ms(graph, n, pos_t, pos0):
-    pos_t.fill_(pos0)
+def _replay_ms(graph, n, m, pos0):
+    m.rewind(pos0)
     e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     torch.cuda.synchronize()
     e0.record()
@@ -249,7 +289,8 @@ def _replay_ms(graph, n, pos_t, pos0):
     return e0.elapsed_time(e1)
 
 
-def latency_table(cfg: Optional[DecoderConfig] = None, n_in: int = 128, n_out: int = 128, device="cuda:0", reps: int = 3):
+def latency_table(cfg: Optional[DecoderConfig] = None, n_in: int = 128, n_out: int = 128, device="cuda:0", reps: int = 3,
+                  kv_cache: str = "bf16"):
     """Attention / MLP / end-to-end latency of `n_in` prompt tokens + `n_out` generated tokens, dense and with POP
     at the paper's two MLP channel ratios for Llama-2-7B (29.9 % and 59.8 %: App. A.1), gamma 0.1: the shape of the
     paper's Table 4 (which was measured on an RTX A6000 with trained weights, module times by CUDA events).
@@ -260,7 +301,8 @@ def latency_table(cfg: Optional[DecoderConfig] = None, n_in: int = 128, n_out: i
     cfg = cfg or DecoderConfig()
     rows = []
     for label, ffn, r in (("dense", "dense", None), ("POP, MLP ratio 29.9 %", "pop", 0.299), ("POP, MLP ratio 59.8 %", "pop", 0.598)):
-        m = Decoder(cfg, device, ffn=ffn, ratios=ratios_for(r) if r is not None else None)
+        # every replay of a captured step appends a token: room for all of them in the 4-bit cache
+        m = Decoder(cfg, device, ffn=ffn, ratios=ratios_for(r) if r is not None else None, kv_cache=kv_cache, kv_tokens=n_in + n_out + 8)
         ids = seeded_ids(cfg, n_in + n_out + 1, 17, m.dev)
         prefill_ms = []
         for rep in range(2):
@@ -276,18 +318,18 @@ def latency_table(cfg: Optional[DecoderConfig] = None, n_in: int = 128, n_out: i
         graphs = {}
         side = torch.cuda.Stream()
         for name, att, mlp in (("e2e", True, True), ("attention", True, False), ("mlp", False, True)):
-            m.pos_t.fill_(n_in)
+            m.rewind(n_in)
             side.wait_stream(torch.cuda.current_stream())
             with torch.cuda.stream(side):
                 m.step_static(att, mlp)                   # warm-up outside capture (lazy initialisations)
             torch.cuda.synchronize()
-            m.pos_t.fill_(n_in)
+            m.rewind(n_in)
             gph = torch.cuda.CUDAGraph()
             with torch.cuda.graph(gph, stream=side):
                 m.step_static(att, mlp)
             graphs[name] = gph
         torch.cuda.synchronize()
-        t = {name: min(_replay_ms(gph, n_out, m.pos_t, n_in) for _ in range(reps)) for name, gph in graphs.items()}
+        t = {name: min(_replay_ms(gph, n_out, m, n_in) for _ in range(reps)) for name, gph in graphs.items()}
         if ffn == "pop":
             for p in m.parts:
                 p.check()
@@ -317,7 +359,8 @@ if __name__ == "__main__":
     ap.add_argument("--layers", type=int, default=32)
     ap.add_argument("--n-in", type=int, default=128)
     ap.add_argument("--n-out", type=int, default=128)
+    ap.add_argument("--kv-cache", choices=("bf16", "int4"), default="bf16")
     a = ap.parse_args()
     ge.build()
-    for rw in latency_table(DecoderConfig(n_layers=a.layers), a.n_in, a.n_out):
+    for rw in latency_table(DecoderConfig(n_layers=a.layers), a.n_in, a.n_out, kv_cache=a.kv_cache):
         print(json.dumps(rw))

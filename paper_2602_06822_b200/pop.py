@@ -497,7 +497,7 @@ def kv_plan(ctx_lens, new_lens, block_table, ring, state, page_size: int, n_toke
                              state_out.data_ptr(), block_table.data_ptr(), block_table.shape[1], n_tokens, at, at + 4 * (R + 1),
                              slots.data_ptr(), at + 4 * (2 * R + 3), at + 4 * (2 * R + 1), _stream_ptr(stream)), "pop_kv_plan")
     _used_on(stream, ints, slots)
-    q_indptr, kv_lens, info, positions = ints.split((R + 1, R, 2, n_tokens))
+    q_indptr, kv_lens, info, positions = ints.split_with_sizes((R + 1, R, 2, n_tokens))
     return KVPlan(q_indptr, kv_lens, slots, positions, state_out, info)
 
 
@@ -587,3 +587,46 @@ def kv_attention_check(device="cuda", workspace=None, stream=None):
     if workspace is None:
         workspace = _kv_workspace(_torch().empty(0, device=device).device, st)
     _check(lib().pop_kv_attention_check(workspace.data_ptr(), st), "pop_kv_attention_check")
+
+
+class KVCache:
+    """A decoder's paged 4-bit cache: the pages of its layers, the block table of its requests and the ring of free pages.
+    One step of all requests is ``plan()`` once, then ``append()`` and ``attend()`` in every layer; everything stays on the device
+    and keeps its addresses, so a step can be captured into a CUDA graph (``plan`` with a fixed number of tokens)."""
+
+    def __init__(self, n_layers: int, n_requests: int, max_tokens: int, n_kv_heads: int, head_dim: int, page_size: int = 64,
+                 n_pages: Optional[int] = None, device="cuda"):
+        torch = _torch()
+        self.page_size = page_size
+        max_blocks = -(-max_tokens // page_size)
+        self.n_pages = n_requests * max_blocks if n_pages is None else n_pages
+        self.pages = [kv_pages(self.n_pages, page_size, n_kv_heads, head_dim, device) for _ in range(n_layers)]
+        i32 = dict(dtype=torch.int32, device=device)
+        self.block_table = torch.empty(n_requests, max_blocks, **i32)
+        self.ring = torch.empty(self.n_pages, **i32)
+        self.state = torch.empty(2, **i32)
+        self.lens = torch.empty(n_requests, **i32)
+        self.step: Optional[KVPlan] = None
+        self.reset()
+
+    def reset(self):
+        """All requests empty, all pages free."""
+        torch = _torch()
+        self.block_table.fill_(-1)
+        torch.arange(self.n_pages, out=self.ring)
+        self.state.copy_(torch.tensor([0, self.n_pages], dtype=torch.int32))
+        self.lens.zero_()
+        self.step = None
+
+    def plan(self, new_lens, n_tokens: int) -> KVPlan:
+        """The step's plan (kv_plan): new_lens int32 [requests] tokens each request gets (negative: it has finished), n_tokens in all.
+        ``step.info[1]`` counts pages that were wanted and not there."""
+        self.step = kv_plan(self.lens, new_lens, self.block_table, self.ring, self.state, self.page_size, n_tokens)
+        self.lens.copy_(self.step.kv_lens)
+        return self.step
+
+    def append(self, layer: int, k, v):
+        kv_append(self.pages[layer], k, v, self.step.slots)
+
+    def attend(self, layer: int, q, **kw):
+        return kv_attention(self.pages[layer], q, self.block_table, self.step.q_indptr, self.step.kv_lens, **kw)

@@ -1,0 +1,104 @@
+"""The decoder with the paged 4-bit cache (plan, append and attention of the library on the path): every layer's attention, from the
+queries, keys and values that it actually had, against 64-bit attention over what the cache holds of them, and the captured step
+against the eager one.  Tolerance as for bf16 attention in test_kv_cache.py (2.5e-3 in the 2-norm; a single row up to 4e-3)."""
+import numpy as np
+import pytest
+import torch
+
+import __graft_entry__ as ge
+from oracle import kv_oracle as ko
+from paper_2602_06822_b200 import decoder as dec, pop
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    ge.build()
+    pop.lib()
+
+
+def host64(t):
+    return t.detach().double().cpu().numpy()
+
+
+@pytest.mark.parametrize("ffn", ["pop", "dense"])
+def test_every_layers_attention(ffn):
+    cfg = dec.DecoderConfig(n_layers=3, d=2048, n_heads=16, N=2816, vocab=512, seed=5)
+    n_in, n_out = 130, 6
+    m = dec.Decoder(cfg, ffn=ffn, ratios=dec.ratios_for(0.2) if ffn == "pop" else None, kv_cache="int4", kv_tokens=160)
+    ids = dec.seeded_ids(cfg, n_in + n_out, 9, m.dev)
+    m.trace = {}
+    m.prefill(ids[:n_in])
+    for s in range(n_out):
+        m.decode(ids[n_in + s: n_in + s + 1], s)
+    torch.cuda.synchronize()
+    assert m.cache4.lens.tolist() == [n_in + n_out]
+    for li in range(cfg.n_layers):
+        steps = [m.trace[("attention", li, p)] for p in [0] + list(range(n_in, n_in + n_out))]
+        k, v = (ko.stored(torch.cat([s[i] for s in steps]).float().cpu().numpy()) for i in (1, 2))
+        at = 0
+        for q, kx, _, o in steps:
+            n = q.shape[0]
+            want, _ = ko.attention(host64(q), k[:at + n], v[:at + n], at, m.hd ** -0.5, True, 0)
+            err = np.linalg.norm(host64(o) - want) / np.linalg.norm(want)
+            assert err <= (2.5e-3 if n > 1 else 4e-3), f"layer {li} at {at}: {err:.2e}"
+            at += n
+    m.close()
+
+
+def test_captured_steps_equal_eager_ones():
+    cfg = dec.DecoderConfig(n_layers=2, d=2048, n_heads=16, N=2816, vocab=512, seed=6)
+    n_in, n_out = 70, 5
+    m = dec.Decoder(cfg, ffn="dense", kv_cache="int4", kv_tokens=96)
+    ids = dec.seeded_ids(cfg, n_in + n_out, 3, m.dev)
+    m.prefill(ids[:n_in])
+    m.begin_static(ids, n_in + n_out)
+    eager = [m.step_static().clone() for _ in range(n_out)]
+    m.rewind(n_in)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        m.step_static()                                    # warm-up outside the capture
+    torch.cuda.synchronize()
+    m.rewind(n_in)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        h = m.step_static()
+    m.rewind(n_in)
+    for s in range(n_out):
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(h, eager[s]), f"step {s}"
+    assert m.cache4.lens.tolist() == [n_in + n_out]
+    m.close()
+
+
+def test_cache_keeps_its_pages_to_itself_over_requests_that_come_and_go():
+    cache = pop.KVCache(2, 3, 64, 2, 64, page_size=16, n_pages=9, device="cuda:0")
+    rng = np.random.default_rng(2)
+    held = [np.zeros((0, 2, 2, 64), dtype=np.float32) for _ in range(3)]
+    for new in ([20, 5, 0], [1, 1, 30], [-1, 20, 1], [16, -1, 1], [1, 40, 1]):
+        n = sum(max(x, 0) for x in new)
+        k = rng.standard_normal((n, 2, 2, 64)).astype(np.float32)
+        step = cache.plan(torch.tensor(new, dtype=torch.int32, device="cuda:0"), n)
+        assert step.info.tolist() == [n, 0]
+        t = torch.from_numpy(k).cuda()
+        for layer in range(2):
+            cache.append(layer, t[:, 0].contiguous() + layer, t[:, 1].contiguous() + layer)
+        at = 0
+        for r, x in enumerate(new):
+            if x < 0:
+                held[r] = held[r][:0]
+            else:
+                held[r] = np.concatenate([held[r], k[at:at + x]])
+                at += x
+        table = cache.block_table.cpu().numpy()
+        for r in range(3):
+            j = np.arange(len(held[r]))
+            slots = torch.from_numpy(table[r, j // 16].astype(np.int64) * 16 + j % 16).cuda()
+            for layer in range(2):
+                got = pop.kv_read(cache.pages[layer], slots, torch.float32)
+                for i in range(2):
+                    want = ko.stored(held[r][:, i] + np.float32(layer)) if len(j) else held[r][:, i]
+                    np.testing.assert_array_equal(got[i].cpu().numpy(), want.astype(np.float32))
