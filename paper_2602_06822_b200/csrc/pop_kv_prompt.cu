@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
     __shared__ u32 tmem_slot;
     __shared__ int abort_flag;
     __shared__ int warp_sum[2][THREADS / 32];
-    __shared__ unsigned char absent_tiles[4][8];           // by block: a stage is refilled before the last softmax warp has looked
+    __shared__ __align__(8) unsigned char absent_tiles[4][8];           // by block: a stage is refilled before the last softmax warp has looked
     const u32 base = (smem_u32(raw_smem) + 1023u) & ~1023u;
     unsigned char* smem = raw_smem + (base - smem_u32(raw_smem));
     int* before = reinterpret_cast<int*>(smem + Cfg::BYTES);               // items before request i << shift
@@ -287,9 +287,14 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
     const int ctas = min((int)gridDim.x, total);
     auto item_at = [&](int turn) { return turn * ctas + ((turn & 1) ? ctas - 1 - (int)blockIdx.x : (int)blockIdx.x); };
 
+    auto all_done = [&]() {                                                // the CTA's last meeting, at the end of every role
+        tc_before();
+        asm volatile("bar.sync 0;" ::: "memory");
+        tc_after();
+    };
     if (warp < SOFTMAX_WARPS) {
-        // ------------------------------------------------------------------ softmax: this thread's row of tile `half`
         asm volatile("setmaxnreg.inc.sync.aligned.u32 " KV_REGS_SOFTMAX ";");
+        // ------------------------------------------------------------------ softmax: this thread's row of tile `half`
         const int half = warp >> 2, row_in = tid & 127;
         const u32 lane_base = tmem + ((u32)((warp & 3) * 32) << 16);
         const u32 t_s = lane_base + 128u * half, t_o = lane_base + 256u + (u32)(D * half);
@@ -440,211 +445,212 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
             if (in && A.lse) A.lse[out_at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.69314718f;
             tc_before();
         }
-    } else if (warp < SOFTMAX_WARPS + UNPACK_WARPS) {
-        // ------------------------------------------------------------------ unpacking: every seventh step of an item
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 " KV_REGS_OTHERS ";");
-        constexpr int PER_BLOCK = BN / kv::TILE;
-        const int w = warp - SOFTMAX_WARPS, g = lane >> 2, t = lane & 3;
-        const int tiles_per_page = A.page_size / kv::TILE;
-        unsigned char* raw = smem + Cfg::RAW + w * BUFFERS * Cfg::HALF;
-        const u32 raw_addr = base + Cfg::RAW + w * BUFFERS * Cfg::HALF;
-        // this lane's places in a tile's 16 rows of 128 bytes (8 rows further the swizzle is the same)
-        const u32 k_at[2] = {swizzled(g, 2 * t), swizzled(g, 2 * t + 1)}, v_at[2] = {swizzled(2 * t, g), swizzled(2 * t + 1, g)};
-        u32 block = 0;                                                     // blocks of the items before
-        bool ok = true;
-        for (int item = item_at(0), turn = 0; item < total && ok; item = item_at(++turn)) {
-            const Item it = find_item(A, before, shift, item);
-            const int n = max(it.n0, it.n1), steps = 2 * n * PER_BLOCK, tile0 = it.first * PER_BLOCK;
-            const int32_t* row_table = A.table + (size_t)it.r * A.max_blocks;
-            // A step is the keys or the values of one tile, in the order in which they are needed: the keys of block 0, then those of block
-            // b + 1 and the values of block b in turn, at the end the last block's values.
-            auto step_at = [&](int step, int& j, int& in_block) {          // returns whether it is values
-                const int after = step - PER_BLOCK, round = after >> 4, i = after & 15;
-                const bool values = step >= PER_BLOCK && (i >= PER_BLOCK || round == n - 1);
-                j = step < PER_BLOCK ? 0 : values ? round : round + 1;
-                in_block = step & 7;
-                return values;
-            };
-            static_assert(PER_BLOCK == 8, "step_at");
-            // Lane i keeps the source of the i-th step from here on: its address, or 0 (its page is missing) or 1 (it has no keys).
-            unsigned long long source = 0;
-            int in_sources = 32;
-            u32 state = 0;                                                 // two bits for each buffer: what came is 0 a tile, 1 part of one, 2 missing, 3 no keys
-            auto fetch = [&](int step, int buffer) {
-                if (step < steps) {
-                    if (in_sources == 32) {
-                        int j, in_block;
-                        const bool values = step_at(step + UNPACK_WARPS * lane, j, in_block);
-                        const int tile = tile0 + j * PER_BLOCK + in_block;
-                        source = 1;
-                        if (tile * kv::TILE < it.rq.len) {
-                            const int at = tile / tiles_per_page, page = row_table[at];
-                            const unsigned char* src = A.pages + (((size_t)(u32)page * A.Hk + it.hk) * tiles_per_page + (tile - at * tiles_per_page)) * TB;
-                            source = (u32)page >= (u32)A.n_pages ? 0ull : (unsigned long long)src | (values ? 8ull : 0ull) | ((tile + 1) * kv::TILE > it.rq.len ? 4ull : 0ull);
-                        }
-                        in_sources = 0;
-                    }
-                    const unsigned long long from = __shfl_sync(~0u, source, in_sources);
-                    ++in_sources;
-                    const u32 what = from >> 4 ? (u32)(from >> 2 & 1ull) : from ? 3u : 2u;
-                    state = (state & ~(3u << (2 * buffer))) | what << (2 * buffer);
-                    if (what < 2u) {                                        // the codes of the keys or the values, and the parameters of both
-                        const unsigned char* src = reinterpret_cast<const unsigned char*>(from & ~15ull) + lane * 16;
-                        const unsigned char* codes = src + ((from & 8ull) ? G * 512 : 0);
-                        const u32 dst = raw_addr + buffer * Cfg::HALF + lane * 16;
-#pragma unroll
-                        for (int c = 0; c < G; ++c)
-                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + c * 512), "l"(codes + c * 512) : "memory");
-                        if (lane < G * 8) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + G * 512), "l"(src + G * 1024) : "memory");
-                    }
-                }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-            };
-            int buffer_in = 0, buffer = 0;
-#pragma unroll
-            for (int s = 0; s < BUFFERS - 1; ++s) { fetch(w + s * UNPACK_WARPS, buffer_in); ++buffer_in; }
-            for (int step = w; step < steps; step += UNPACK_WARPS) {
-                fetch(step + (BUFFERS - 1) * UNPACK_WARPS, buffer_in);
-                if (++buffer_in == BUFFERS) buffer_in = 0;
-                asm volatile("cp.async.wait_group %0;" ::"n"(BUFFERS - 1) : "memory");
-                __syncwarp();
-                int j, in_block;
-                const bool values = step_at(step, j, in_block);
-                const u32 b = block + j, stage = b & 1u, what = state >> (2 * buffer) & 3u;
-                unsigned char* src = raw + buffer * Cfg::HALF;
-                u32* params = reinterpret_cast<u32*>(src) + G * kv::GROUP_WORDS;
-                if (what != 0u) {                                           // tokens that are not there get values of 0
-                    const int key0 = (tile0 + j * PER_BLOCK + in_block) * kv::TILE;
-                    for (int i = lane; i < kv::TILE * 2 * G; i += 32)
-                        if (what > 1u || key0 + i / (2 * G) >= it.rq.len) params[i] = 0u;
-                    __syncwarp();
-                }
-                const u32 full = (values ? v_full : k_full) + 8 * stage;
-                ok = __all_sync(~0u, mbar_wait((values ? v_empty : k_empty) + 8 * stage, (b >> 1 & 1u) ^ 1u, abortp, status));
-                if (!ok) break;
-                const u32 to = base + (values ? Cfg::V : Cfg::K) + stage * Cfg::TILE + in_block * (kv::TILE * 128);
-                uint4 x[G];
-#pragma unroll
-                for (int gr = 0; gr < G; ++gr) x[gr] = *reinterpret_cast<const uint4*>(src + gr * 512 + lane * 16);
-                if (!values) {
-                    // words 0, 1: token g, dimensions 16 t ..; words 2, 3: token g + 8
-                    u32 p[2][G];
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int gr = 0; gr < G; ++gr) p[i][gr] = params[(g + 8 * i) * 2 * G + gr];
-#pragma unroll
-                    for (int gr = 0; gr < G; ++gr) {
-                        const ScaleZero p0 = scale_zero(p[0][gr]), p1 = scale_zero(p[1][gr]);
-                        st_shared(to + gr * (128 * 128) + k_at[0], unpack_word(x[gr].x, p0));
-                        st_shared(to + gr * (128 * 128) + k_at[1], unpack_word(x[gr].y, p0));
-                        st_shared(to + gr * (128 * 128) + 1024 + k_at[0], unpack_word(x[gr].z, p1));
-                        st_shared(to + gr * (128 * 128) + 1024 + k_at[1], unpack_word(x[gr].w, p1));
-                    }
-                    if (lane == 0) absent_tiles[b & 3][in_block] = what == 2u;
-                } else {
-                    // words 0..3: tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9, dimensions 8 g ..
-                    u32 p[4][G];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int gr = 0; gr < G; ++gr) p[i][gr] = params[(2 * t + (i & 1) + 8 * (i >> 1)) * 2 * G + G + gr];
-#pragma unroll
-                    for (int gr = 0; gr < G; ++gr) {
-                        st_shared(to + gr * (128 * 128) + v_at[0], unpack_word(x[gr].x, scale_zero(p[0][gr])));
-                        st_shared(to + gr * (128 * 128) + v_at[1], unpack_word(x[gr].y, scale_zero(p[1][gr])));
-                        st_shared(to + gr * (128 * 128) + 1024 + v_at[0], unpack_word(x[gr].z, scale_zero(p[2][gr])));
-                        st_shared(to + gr * (128 * 128) + 1024 + v_at[1], unpack_word(x[gr].w, scale_zero(p[3][gr])));
-                    }
-                }
-                to_async_proxy();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(full);
-                if (++buffer == BUFFERS) buffer = 0;
-            }
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-            __syncwarp();
-            block += n;
-        }
+        all_done();
     } else {
+        // One instruction for the warpgroup that both of the following roles have warps of (its warps have to execute the same one), ahead of
+        // all their code.  No code is shared again behind the roles: it might be given registers that these warps no longer have.
         asm volatile("setmaxnreg.dec.sync.aligned.u32 " KV_REGS_OTHERS ";");
-    }
-    if (warp == MMA_WARP) {
-        // ------------------------------------------------------------------ MMA issue
-        const u32 mine = elect_lane(), tm = __shfl_sync(~0u, tmem, 0);
-        const u64 dq = desc_k_major(base + Cfg::Q), dk = desc_k_major(base + Cfg::K), dv = desc_mn_major(base + Cfg::V);
-        u32 block = 0, q_phase = 0u, p_phase0 = 0u, p_phase1 = 0u;         // q_phase: a bit for each tile
-        bool ok = true;
-        auto wait = [&](u32 bar, u32 parity) {
-            ok = __all_sync(~0u, mbar_wait(bar, parity, abortp, status));
-            return ok;
-        };
-        for (int item = item_at(0), turn = 0; item < total && ok; item = item_at(++turn)) {
-            const Item it = find_item(A, before, shift, item);
-            const int n = max(it.n0, it.n1);
-            auto stage_of = [&](int j) { return (block + j) & 1u; };
-            auto phase_of = [&](int j) { return ((block + j) >> 1) & 1u; };
-            auto scores = [&](int half, int j) {
-                const u64 q = dq + (u64)(half * (Cfg::TILE / 16)), k = dk + (u64)(stage_of(j) * (Cfg::TILE / 16));
+        if (warp != MMA_WARP) {
+            // ------------------------------------------------------------------ unpacking: every seventh step of an item
+            constexpr int PER_BLOCK = BN / kv::TILE;
+            const int w = warp - SOFTMAX_WARPS, g = lane >> 2, t = lane & 3;
+            const int tiles_per_page = A.page_size / kv::TILE;
+            unsigned char* raw = smem + Cfg::RAW + w * BUFFERS * Cfg::HALF;
+            const u32 raw_addr = base + Cfg::RAW + w * BUFFERS * Cfg::HALF;
+            // this lane's places in a tile's 16 rows of 128 bytes (8 rows further the swizzle is the same)
+            const u32 k_at[2] = {swizzled(g, 2 * t), swizzled(g, 2 * t + 1)}, v_at[2] = {swizzled(2 * t, g), swizzled(2 * t + 1, g)};
+            u32 block = 0;                                                     // blocks of the items before
+            bool ok = true;
+            for (int item = item_at(0), turn = 0; item < total && ok; item = item_at(++turn)) {
+                const Item it = find_item(A, before, shift, item);
+                const int n = max(it.n0, it.n1), steps = 2 * n * PER_BLOCK, tile0 = it.first * PER_BLOCK;
+                const int32_t* row_table = A.table + (size_t)it.r * A.max_blocks;
+                // A step is the keys or the values of one tile, in the order in which they are needed: the keys of block 0, then those of block
+                // b + 1 and the values of block b in turn, at the end the last block's values.
+                auto step_at = [&](int step, int& j, int& in_block) {          // returns whether it is values
+                    const int after = step - PER_BLOCK, round = after >> 4, i = after & 15;
+                    const bool values = step >= PER_BLOCK && (i >= PER_BLOCK || round == n - 1);
+                    j = step < PER_BLOCK ? 0 : values ? round : round + 1;
+                    in_block = step & 7;
+                    return values;
+                };
+                static_assert(PER_BLOCK == 8, "step_at");
+                // Lane i keeps the source of the i-th step from here on: its address, or 0 (its page is missing) or 1 (it has no keys).
+                unsigned long long source = 0;
+                int in_sources = 32;
+                u32 state = 0;                                                 // two bits for each buffer: what came is 0 a tile, 1 part of one, 2 missing, 3 no keys
+                auto fetch = [&](int step, int buffer) {
+                    if (step < steps) {
+                        if (in_sources == 32) {
+                            int j, in_block;
+                            const bool values = step_at(step + UNPACK_WARPS * lane, j, in_block);
+                            const int tile = tile0 + j * PER_BLOCK + in_block;
+                            source = 1;
+                            if (tile * kv::TILE < it.rq.len) {
+                                const int at = tile / tiles_per_page, page = row_table[at];
+                                const unsigned char* src = A.pages + (((size_t)(u32)page * A.Hk + it.hk) * tiles_per_page + (tile - at * tiles_per_page)) * TB;
+                                source = (u32)page >= (u32)A.n_pages ? 0ull : (unsigned long long)src | (values ? 8ull : 0ull) | ((tile + 1) * kv::TILE > it.rq.len ? 4ull : 0ull);
+                            }
+                            in_sources = 0;
+                        }
+                        const unsigned long long from = __shfl_sync(~0u, source, in_sources);
+                        ++in_sources;
+                        const u32 what = from >> 4 ? (u32)(from >> 2 & 1ull) : from ? 3u : 2u;
+                        state = (state & ~(3u << (2 * buffer))) | what << (2 * buffer);
+                        if (what < 2u) {                                        // the codes of the keys or the values, and the parameters of both
+                            const unsigned char* src = reinterpret_cast<const unsigned char*>(from & ~15ull) + lane * 16;
+                            const unsigned char* codes = src + ((from & 8ull) ? G * 512 : 0);
+                            const u32 dst = raw_addr + buffer * Cfg::HALF + lane * 16;
 #pragma unroll
-                for (int s = 0; s < D / 16; ++s) {                          // 16 dimensions: 32 bytes along the swizzled row
-                    const u64 at = (s / 4) * (128 * 128 / 16) + (s % 4) * 2;
-                    umma_ss(mine, tm + 128u * half, q + at, k + at, IDESC_S, s > 0);
-                }
-                umma_commit(mine, s_full + 8 * half);
-            };
-            auto outputs = [&](int half, int j) {
-                const u64 v = dv + (u64)(stage_of(j) * (Cfg::TILE / 16));
-#pragma unroll
-                for (int s = 0; s < BN / 16; ++s)                           // 16 keys: 8 columns of P, 16 rows of V
-                    umma_ts(mine, tm + 256u + (u32)(D * half), tm + 128u * half + 8u * s, v + (u64)(s * 16 * 128 / 16), IDESC_O<D>, j > 0 || s > 0);
-                umma_commit(mine, o_done + 8 * half);
-            };
-            if (n > 0) {
-                if (!wait(k_full + 8 * stage_of(0), phase_of(0))) break;
-#pragma unroll
-                for (int half = 0; half < 2; ++half)
-                    if ((half ? it.n1 : it.n0) > 0 && ok) {
-                        if (!wait(q_full + 8 * half, q_phase >> half & 1u)) break;
-                        q_phase ^= 1u << half;
-                        tc_after();
-                        scores(half, 0);
+                            for (int c = 0; c < G; ++c)
+                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + c * 512), "l"(codes + c * 512) : "memory");
+                            if (lane < G * 8) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + G * 512), "l"(src + G * 1024) : "memory");
+                        }
                     }
-                if (!ok) break;
-                umma_commit(mine, k_empty + 8 * stage_of(0));
-            }
-            for (int j = 0; j < n; ++j) {
-                if (j + 1 < n && !wait(k_full + 8 * stage_of(j + 1), phase_of(j + 1))) break;
-                if (!wait(v_full + 8 * stage_of(j), phase_of(j))) break;
-                if (j < it.n0) {
-                    if (!wait(p_full, p_phase0)) break;
-                    p_phase0 ^= 1u;
-                    tc_after();
-                    outputs(0, j);
-                    if (j + 1 < it.n0) scores(0, j + 1);                    // behind the products that read P out of the same columns
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                };
+                int buffer_in = 0, buffer = 0;
+#pragma unroll
+                for (int s = 0; s < BUFFERS - 1; ++s) { fetch(w + s * UNPACK_WARPS, buffer_in); ++buffer_in; }
+                for (int step = w; step < steps; step += UNPACK_WARPS) {
+                    fetch(step + (BUFFERS - 1) * UNPACK_WARPS, buffer_in);
+                    if (++buffer_in == BUFFERS) buffer_in = 0;
+                    asm volatile("cp.async.wait_group %0;" ::"n"(BUFFERS - 1) : "memory");
+                    __syncwarp();
+                    int j, in_block;
+                    const bool values = step_at(step, j, in_block);
+                    const u32 b = block + j, stage = b & 1u, what = state >> (2 * buffer) & 3u;
+                    unsigned char* src = raw + buffer * Cfg::HALF;
+                    u32* params = reinterpret_cast<u32*>(src) + G * kv::GROUP_WORDS;
+                    if (what != 0u) {                                           // tokens that are not there get values of 0
+                        const int key0 = (tile0 + j * PER_BLOCK + in_block) * kv::TILE;
+                        for (int i = lane; i < kv::TILE * 2 * G; i += 32)
+                            if (what > 1u || key0 + i / (2 * G) >= it.rq.len) params[i] = 0u;
+                        __syncwarp();
+                    }
+                    const u32 full = (values ? v_full : k_full) + 8 * stage;
+                    ok = __all_sync(~0u, mbar_wait((values ? v_empty : k_empty) + 8 * stage, (b >> 1 & 1u) ^ 1u, abortp, status));
+                    if (!ok) break;
+                    const u32 to = base + (values ? Cfg::V : Cfg::K) + stage * Cfg::TILE + in_block * (kv::TILE * 128);
+                    uint4 x[G];
+#pragma unroll
+                    for (int gr = 0; gr < G; ++gr) x[gr] = *reinterpret_cast<const uint4*>(src + gr * 512 + lane * 16);
+                    if (!values) {
+                        // words 0, 1: token g, dimensions 16 t ..; words 2, 3: token g + 8
+                        u32 p[2][G];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int gr = 0; gr < G; ++gr) p[i][gr] = params[(g + 8 * i) * 2 * G + gr];
+#pragma unroll
+                        for (int gr = 0; gr < G; ++gr) {
+                            const ScaleZero p0 = scale_zero(p[0][gr]), p1 = scale_zero(p[1][gr]);
+                            st_shared(to + gr * (128 * 128) + k_at[0], unpack_word(x[gr].x, p0));
+                            st_shared(to + gr * (128 * 128) + k_at[1], unpack_word(x[gr].y, p0));
+                            st_shared(to + gr * (128 * 128) + 1024 + k_at[0], unpack_word(x[gr].z, p1));
+                            st_shared(to + gr * (128 * 128) + 1024 + k_at[1], unpack_word(x[gr].w, p1));
+                        }
+                        if (lane == 0) absent_tiles[b & 3][in_block] = what == 2u;
+                    } else {
+                        // words 0..3: tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9, dimensions 8 g ..
+                        u32 p[4][G];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int gr = 0; gr < G; ++gr) p[i][gr] = params[(2 * t + (i & 1) + 8 * (i >> 1)) * 2 * G + G + gr];
+#pragma unroll
+                        for (int gr = 0; gr < G; ++gr) {
+                            st_shared(to + gr * (128 * 128) + v_at[0], unpack_word(x[gr].x, scale_zero(p[0][gr])));
+                            st_shared(to + gr * (128 * 128) + v_at[1], unpack_word(x[gr].y, scale_zero(p[1][gr])));
+                            st_shared(to + gr * (128 * 128) + 1024 + v_at[0], unpack_word(x[gr].z, scale_zero(p[2][gr])));
+                            st_shared(to + gr * (128 * 128) + 1024 + v_at[1], unpack_word(x[gr].w, scale_zero(p[3][gr])));
+                        }
+                    }
+                    to_async_proxy();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(full);
+                    if (++buffer == BUFFERS) buffer = 0;
                 }
-                if (j < it.n1) {
-                    if (!wait(p_full + 8, p_phase1)) break;
-                    p_phase1 ^= 1u;
-                    tc_after();
-                    outputs(1, j);
-                    if (j + 1 < it.n1) scores(1, j + 1);
-                }
-                umma_commit(mine, v_empty + 8 * stage_of(j));
-                if (j + 1 < n) umma_commit(mine, k_empty + 8 * stage_of(j + 1));
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                __syncwarp();
+                block += n;
             }
-            block += n;
-        }
-        // nothing of this CTA may still be executing on the tensor cores when tensor memory is given back
-        umma_commit(mine, drain);
-        const unsigned long long t0 = pop_global_ns();
-        while (!mbar_try_wait(drain, 0u) && pop_global_ns() - t0 < WAIT_NS) {}
-        __syncwarp();
+            all_done();
+        } else {
+            // ------------------------------------------------------------------ MMA issue
+            const u32 mine = elect_lane(), tm = __shfl_sync(~0u, tmem, 0);
+            const u64 dq = desc_k_major(base + Cfg::Q), dk = desc_k_major(base + Cfg::K), dv = desc_mn_major(base + Cfg::V);
+            u32 block = 0, q_phase = 0u, p_phase0 = 0u, p_phase1 = 0u;         // q_phase: a bit for each tile
+            bool ok = true;
+            auto wait = [&](u32 bar, u32 parity) {
+                ok = __all_sync(~0u, mbar_wait(bar, parity, abortp, status));
+                return ok;
+            };
+            for (int item = item_at(0), turn = 0; item < total && ok; item = item_at(++turn)) {
+                const Item it = find_item(A, before, shift, item);
+                const int n = max(it.n0, it.n1);
+                auto stage_of = [&](int j) { return (block + j) & 1u; };
+                auto phase_of = [&](int j) { return ((block + j) >> 1) & 1u; };
+                auto scores = [&](int half, int j) {
+                    const u64 q = dq + (u64)(half * (Cfg::TILE / 16)), k = dk + (u64)(stage_of(j) * (Cfg::TILE / 16));
+#pragma unroll
+                    for (int s = 0; s < D / 16; ++s) {                          // 16 dimensions: 32 bytes along the swizzled row
+                        const u64 at = (s / 4) * (128 * 128 / 16) + (s % 4) * 2;
+                        umma_ss(mine, tm + 128u * half, q + at, k + at, IDESC_S, s > 0);
+                    }
+                    umma_commit(mine, s_full + 8 * half);
+                };
+                auto outputs = [&](int half, int j) {
+                    const u64 v = dv + (u64)(stage_of(j) * (Cfg::TILE / 16));
+#pragma unroll
+                    for (int s = 0; s < BN / 16; ++s)                           // 16 keys: 8 columns of P, 16 rows of V
+                        umma_ts(mine, tm + 256u + (u32)(D * half), tm + 128u * half + 8u * s, v + (u64)(s * 16 * 128 / 16), IDESC_O<D>, j > 0 || s > 0);
+                    umma_commit(mine, o_done + 8 * half);
+                };
+                if (n > 0) {
+                    if (!wait(k_full + 8 * stage_of(0), phase_of(0))) break;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+                        if ((half ? it.n1 : it.n0) > 0 && ok) {
+                            if (!wait(q_full + 8 * half, q_phase >> half & 1u)) break;
+                            q_phase ^= 1u << half;
+                            tc_after();
+                            scores(half, 0);
+                        }
+                    if (!ok) break;
+                    umma_commit(mine, k_empty + 8 * stage_of(0));
+                }
+                for (int j = 0; j < n; ++j) {
+                    if (j + 1 < n && !wait(k_full + 8 * stage_of(j + 1), phase_of(j + 1))) break;
+                    if (!wait(v_full + 8 * stage_of(j), phase_of(j))) break;
+                    if (j < it.n0) {
+                        if (!wait(p_full, p_phase0)) break;
+                        p_phase0 ^= 1u;
+                        tc_after();
+                        outputs(0, j);
+                        if (j + 1 < it.n0) scores(0, j + 1);                    // behind the products that read P out of the same columns
+                    }
+                    if (j < it.n1) {
+                        if (!wait(p_full + 8, p_phase1)) break;
+                        p_phase1 ^= 1u;
+                        tc_after();
+                        outputs(1, j);
+                        if (j + 1 < it.n1) scores(1, j + 1);
+                    }
+                    umma_commit(mine, v_empty + 8 * stage_of(j));
+                    if (j + 1 < n) umma_commit(mine, k_empty + 8 * stage_of(j + 1));
+                }
+                block += n;
+            }
+            // nothing of this CTA may still be executing on the tensor cores when tensor memory is given back
+            umma_commit(mine, drain);
+            const unsigned long long t0 = pop_global_ns();
+            while (!mbar_try_wait(drain, 0u) && pop_global_ns() - t0 < WAIT_NS) {}
+            __syncwarp();
+            all_done();
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
     }
-    tc_before();
-    __syncthreads();
-    tc_after();
-    if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
 }
 
 template <int D> int launch(const KvAttnArgs& A, u32* status, int device, int ctas, cudaStream_t st) {
