@@ -553,6 +553,53 @@ def test_append_read_and_plan_refuse_wrong_arguments():
 
 
 @pytest.mark.gpu
+def test_check_reports_a_wait_that_ran_out_and_clears_it():
+    """The status word as a kernel that gives up would leave it (set from the host: no kernel is made to give up)."""
+    s = Setup(21, 4, 2, 64, 16, BF16, [150, 20], [150, 1])
+    n = C.c_size_t()
+    assert pop.lib().pop_kv_attention_workspace(C.byref(n)) == pop.POP_OK
+    ws = torch.zeros(n.value, dtype=torch.uint8, device=DEV)
+    want = s.run(workspace=ws)
+    pop.kv_attention_check(DEV, workspace=ws)
+    ws[0] = 1
+    with pytest.raises(pop.PopError) as e:
+        pop.kv_attention_check(DEV, workspace=ws)
+    assert e.value.status == pop.POP_ERR_TIMEOUT
+    pop.kv_attention_check(DEV, workspace=ws)
+    assert torch.equal(s.run(workspace=ws), want)                      # usable afterwards
+    pop.kv_attention_check(DEV)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,H,requests", [(40, 3, 1), (1200, 8, 3), (2100, 8, 700)])
+def test_append_of_runs_that_begin_anywhere(T, H, requests):
+    """Whole tiles, parts of tiles and single tokens in one call, and skipped tokens among them; few and many tokens."""
+    rng = np.random.default_rng(T)
+    page, D = 32, 128
+    cut = np.sort(rng.choice(np.arange(1, T), requests - 1, replace=False)) if requests > 1 else []
+    new = np.diff(np.concatenate([[0], cut, [T]])).astype(int)
+    ctx = rng.integers(0, 70, requests)
+    blocks = [-(-int(c + n) // page) for c, n in zip(ctx, new)]
+    perm, at, slots = rng.permutation(sum(blocks)), 0, []
+    for c, n, b in zip(ctx, new, blocks):
+        j = np.arange(c, c + n)
+        slots.append(perm[at:at + b][j // page] * page + j % page)
+        at += b
+    slots = np.concatenate(slots)
+    skip = rng.random(T) < 0.02
+    pages = filled(sum(blocks), page, H, D)
+    for dtype in (BF16, F32):
+        k, v = (torch.from_numpy(rng.standard_normal((T, H, D)).astype(np.float32)).to(dtype) for _ in range(2))
+        given = torch.from_numpy(np.where(skip, -1, slots)).to(DEV)
+        pop.kv_append(pages, k.to(DEV), v.to(DEV), given)
+        a, b = pop.kv_read(pages, given, F32)
+        for x, y in ((k, a), (v, b)):
+            want = ko.stored(x.float().numpy()).astype(np.float32)
+            want[skip] = 0
+            np.testing.assert_array_equal(y.cpu().numpy(), want)
+
+
+@pytest.mark.gpu
 def test_binding_refuses_wrong_tensors():
     pages = filled(4, 16, 2, 64)
     k = torch.randn(3, 2, 64, device=DEV)
