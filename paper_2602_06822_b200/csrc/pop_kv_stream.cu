@@ -174,9 +174,8 @@ __device__ __forceinline__ void join_row(const KvAttnArgs& A, const PieceOf& seg
     typedef typename std::conditional<PER == 4, float4, float2>::type Vec;
     const int lane = threadIdx.x & 31;
     const float2 st = lane < n ? *reinterpret_cast<const float2*>(smem + places[lane] + stats) : make_float2(-1e30f, 0.f);
-    float m = st.x;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+    float m;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(st.x));
     const float f = kv_exp2(st.x - m);
     float l = st.y * f, o[PER] = {};
 #pragma unroll
@@ -321,6 +320,20 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
         const int u_lo = max(first + (int)(u - sb), some_lo / Cfg::TOKENS);
         const int u_hi = min(first + (int)(pe - sb), (some_hi + Cfg::TOKENS - 1) / Cfg::TOKENS);
 
+        // ---- the query rows, asked for before the page ids and the tiles, behind which they would have to queue
+        constexpr int VECS = 16 / Elem<T>::VEC;
+        uint4 q_raw[NT][G][VECS];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const bool in = nt * 8 + g < rows;
+            const int row = row0 + (in ? nt * 8 + g : 0), i = row / A.ratio;
+            const T* qp = (const T*)A.q + (size_t)(rq.q0 + i) * A.q_stride + (size_t)(hk * A.ratio + row - i * A.ratio) * D + 16 * t;
+#pragma unroll
+            for (int gr = 0; gr < G; ++gr)
+#pragma unroll
+                for (int v = 0; v < VECS; ++v) q_raw[nt][gr][v] = *reinterpret_cast<const uint4*>(qp + gr * 64 + v * Elem<T>::VEC);
+        }
+
         // ---- the units, STAGES of them on their way.  Lane i keeps the id of page ids_from + i.
         const int32_t* row_table = A.table + (size_t)r * A.max_blocks;
         const int tiles_per_page = A.page_size / kv::TILE;
@@ -370,19 +383,6 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
             cp_commit();
         };
 
-        // the query rows are asked for before the tiles, behind which they would have to queue
-        constexpr int VECS = 16 / Elem<T>::VEC;
-        uint4 q_raw[NT][G][VECS];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const bool in = nt * 8 + g < rows;
-            const int row = row0 + (in ? nt * 8 + g : 0), i = row / A.ratio;
-            const T* qp = (const T*)A.q + (size_t)(rq.q0 + i) * A.q_stride + (size_t)(hk * A.ratio + row - i * A.ratio) * D + 16 * t;
-#pragma unroll
-            for (int gr = 0; gr < G; ++gr)
-#pragma unroll
-                for (int v = 0; v < VECS; ++v) q_raw[nt][gr][v] = *reinterpret_cast<const uint4*>(qp + gr * 64 + v * Elem<T>::VEC);
-        }
 #pragma unroll
         for (int s = 0; s < STAGES; ++s) issue();
 
@@ -751,31 +751,31 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
     auto part = [&](int c, int slot) { return parts + ((size_t)c * 2 + slot) * (ROWS * (D + 4)); };
     // lane k has piece k = 2 * warp + slot: where its segment differs from the piece before, the parts of another segment begin
     static_assert(2 * WARPS <= 32, "a lane per piece");
-    const bool held = lane < 2 * WARPS && piece_of[lane >> 1][lane & 1].valid;
-    const ull begin = held ? piece_of[lane >> 1][lane & 1].begin : 0;
-    const u32 pieces = __ballot_sync(~0u, held);
-    const u32 earlier = pieces & ((1u << lane) - 1u);
+    const PieceOf& own = piece_of[lane < 2 * WARPS ? lane >> 1 : 0][lane & 1];
+    const bool held = lane < 2 * WARPS && own.valid;
+    const ull begin = held ? own.begin : 0, end = held ? own.end : 0;
+    const u32 pieces = __ballot_sync(~0u, held), before_me = (1u << lane) - 1u;
+    const u32 earlier = pieces & before_me;
     const ull begin_before = __shfl_sync(~0u, begin, earlier ? 31 - __clz(earlier) : lane);
-    u32 starts = __ballot_sync(~0u, held && (!earlier || begin_before != begin));
+    const bool starts_here = held && (!earlier || begin_before != begin);
+    const u32 starts = __ballot_sync(~0u, starts_here);
+    const int segment = __popc(starts & before_me), most_rows = (int)__reduce_max_sync(~0u, held ? (u32)own.rows : 0u);
+    // the first pieces of the segments cut between CTAs: the one begun before, the one that goes on
+    const int cut[2] = {__ffs(__ballot_sync(~0u, starts_here && begin < ca)) - 1,
+                        __ffs(__ballot_sync(~0u, starts_here && begin >= ca && end > cb)) - 1};
     const u32 where = (lane >> 1) * Cfg::WARP_BYTES + ((lane & 1) ? 0 : STAGES * Cfg::UB);
-    int cut[2] = {-1, -1};                               // pieces of the segments cut between CTAs: the one begun before, the one that goes on
-    int task = 0;
-    while (starts) {
-        const int k = __ffs(starts) - 1;
-        starts &= starts - 1u;
-        const u32 of_segment = pieces & ~((1u << k) - 1u) & (starts ? (starts & -starts) - 1u : ~0u);
+    for (int task = warp; task < __popc(starts) * most_rows; task += WARPS) {
+        const int of = task / most_rows, c = task - of * most_rows;
+        const int k = __ffs(__ballot_sync(~0u, starts_here && segment == of)) - 1;
         const PieceOf& p = piece_of[k >> 1][k & 1];
-        const bool inside = p.begin >= ca && p.end <= cb;
-        const int slot = p.begin < ca ? 0 : 1;
-        if (!inside) cut[slot] = k;
-        for (int c = 0; c < p.rows; ++c, ++task)
-            if (task % WARPS == warp) {
-                __syncwarp();
-                if (of_segment >> lane & 1u) places[warp][__popc(of_segment & ((1u << lane) - 1u))] = where + c * D * 4;
-                __syncwarp();
-                join_row<T, D, ROWS>(A, p, c, kv_smem, places[warp], __popc(of_segment), (ROWS - c) * D * 4 + c * 16,
-                                     inside ? nullptr : part(cta, slot), nullptr);
-            }
+        if (c >= p.rows) continue;
+        const u32 later = starts & ~((2u << k) - 1u);
+        const u32 of_segment = pieces & ~((1u << k) - 1u) & (later ? (later & -later) - 1u : ~0u);
+        __syncwarp();
+        if (of_segment >> lane & 1u) places[warp][__popc(of_segment & before_me)] = where + c * D * 4;
+        __syncwarp();
+        join_row<T, D, ROWS>(A, p, c, kv_smem, places[warp], __popc(of_segment), (ROWS - c) * D * 4 + c * 16,
+                             k == cut[0] ? part(cta, 0) : k == cut[1] ? part(cta, 1) : nullptr, nullptr);
     }
     if (cut[0] < 0 && cut[1] < 0) return;                // the same for the whole CTA
     __syncthreads();
@@ -795,31 +795,30 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
         last_of[tid] = last;
     }
     __syncthreads();
-    for (int s = 0; s < 2; ++s) {
-        if (!last_of[s]) continue;
-        const int k = s ? cut[1] : cut[0], c0 = cut_ctas[s][0], n = cut_ctas[s][1] - c0 + 1;
+    const int rows_of[2] = {last_of[0] ? piece_of[cut[0] >> 1][cut[0] & 1].rows : 0, last_of[1] ? piece_of[cut[1] >> 1][cut[1] & 1].rows : 0};
+    for (int task = warp; task < rows_of[0] + rows_of[1]; task += WARPS) {
+        const int s = task < rows_of[0] ? 0 : 1, c = s ? task - rows_of[0] : task;
+        const int k = cut[s], c0 = cut_ctas[s][0], n = cut_ctas[s][1] - c0 + 1;
         const PieceOf& p = piece_of[k >> 1][k & 1];
-        for (int c = warp; c < p.rows; c += WARPS) {
-            // the parts come through the ring (nothing else is in it any more), as many as it holds on their way at once; what they make
-            // stays there as a part of the next ones
-            constexpr int ROOM = D * 4 + 16, MOST = Cfg::WARP_BYTES / ROOM < 32 ? Cfg::WARP_BYTES / ROOM : 32;
-            __syncwarp();
-            places[warp][lane] = warp * Cfg::WARP_BYTES + lane * ROOM;
-            for (int from = 0; from < n;) {
-                const int kept = from ? 1 : 0, more = min(MOST - kept, n - from);
-                for (int i = 0; i < more; ++i) {
-                    const float* src = part(c0 + from + i, from + i == 0 ? 1 : 0);
-                    const u32 dst = ring_addr + (kept + i) * ROOM;
-                    if (lane < D / 4) cp16(dst + lane * 16, src + c * D + lane * 4);
-                    if (lane == 0) cp16(dst + D * 4, src + ROWS * D + c * 4);
-                }
-                cp_commit();
-                cp_wait<0>();
-                __syncwarp();
-                from += more;
-                join_row<T, D, ROWS>(A, p, c, kv_smem, places[warp], kept + more, D * 4, nullptr, from < n ? reinterpret_cast<float2*>(ring) : nullptr);
-                __syncwarp();
+        // the parts come through the ring (nothing else is in it any more), as many as it holds on their way at once; what they make
+        // stays there as a part of the next ones
+        constexpr int ROOM = D * 4 + 16, MOST = Cfg::WARP_BYTES / ROOM < 32 ? Cfg::WARP_BYTES / ROOM : 32;
+        __syncwarp();
+        places[warp][lane] = warp * Cfg::WARP_BYTES + lane * ROOM;
+        for (int from = 0; from < n;) {
+            const int kept = from ? 1 : 0, more = min(MOST - kept, n - from);
+            for (int i = 0; i < more; ++i) {
+                const float* src = part(c0 + from + i, from + i == 0 ? 1 : 0);
+                const u32 dst = ring_addr + (kept + i) * ROOM;
+                if (lane < D / 4) cp16(dst + lane * 16, src + c * D + lane * 4);
+                if (lane == 0) cp16(dst + D * 4, src + ROWS * D + c * 4);
             }
+            cp_commit();
+            cp_wait<0>();
+            __syncwarp();
+            from += more;
+            join_row<T, D, ROWS>(A, p, c, kv_smem, places[warp], kept + more, D * 4, nullptr, from < n ? reinterpret_cast<float2*>(ring) : nullptr);
+            __syncwarp();
         }
     }
 }
