@@ -15,6 +15,10 @@
 //                    in the MMAs' 128-byte swizzle: c - 8 exactly, then s (c - 8) + (z + 8 s) with one rounding each to 11 bits
 //   warp 15          issues the MMAs: tile 0's products run while tile 1's softmax does, and the other way round
 // The items of a request are dealt out from its last rows (most keys under a causal mask) to its first.
+// Measured (head_dim 128, causal, bf16): 32 heads of 16384 tokens 2.33 ms = 945 TFLOP/s; six chunks of 65 .. 2049 tokens behind 100 .. 4100
+// cached ones (32 heads on 8) 262 us = 680 TFLOP/s; 32 heads of 1024 tokens 30 us = 290 TFLOP/s, of which the longest item's 8 blocks take
+// 20.  A block takes 4400 cycles instead of 2048: a softmax warp needs 2050 for its row's part (read 180, maximum 410, exponentials
+// and packing 1460) and waits 1460 for the next product, which waits for the unpacked keys and for the other tile's product.
 // Every wait is bounded; one that runs out sets the status word and the CTA winds down.
 #include "pop_kv_attn.cuh"
 
@@ -649,7 +653,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const KvAttnArgs 
             __syncwarp();
             all_done();
             asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
-    }
+        }
     }
 }
 
