@@ -62,6 +62,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_plan_kernel(const PlanArgs P)
     int* give = take + P.R + 1;                  // [R + 1] pages to give back before r
     __shared__ Sum3 warp_sum[PLAN_THREADS / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    kv::follow();
     const int head = P.state_in[0], count = P.state_in[1];
 
     // PER consecutive requests to a thread
@@ -202,12 +203,12 @@ extern "C" int pop_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int
     cfg.blockDim = dim3(PLAN_THREADS);
     cfg.dynamicSmemBytes = 3 * (size_t)(n_requests + 1) * sizeof(int);
     cfg.stream = (cudaStream_t)cuda_stream;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = ctas;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = in_place && ctas > 1 ? 1 : 0;
+    cudaLaunchAttribute attr[2] = {kv::following()};
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = in_place && ctas > 1 ? 2 : 1;
     if (cfg.dynamicSmemBytes > 48 * 1024)
         POP_CUDA(cudaFuncSetAttribute(kv_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * (POP_KV_MAX_REQUESTS + 1) * (int)sizeof(int)));
     POP_CUDA(cudaLaunchKernelEx(&cfg, kv_plan_kernel, P));
@@ -224,7 +225,9 @@ extern "C" int pop_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int
 // shared memory and moved as the consecutive bytes that they are; only what is not part of such a run goes word by word.
 // That costs a chain of three trips to memory, which a call of few tokens does not earn back: there every thread has 8 dimensions of
 // one token to itself.  (16384 tokens of 8 heads of 128, bf16: append 26.9 us against 34.1 thread by thread, read 17.5 against 28.2; the
-// bytes alone take 13.3 each at the measured copy rate.  512 tokens: 3.7 against 2.8 and 3.1 against 2.5.)
+// bytes alone take 13.3 each at the measured copy rate.  512 tokens: 3.7 against 2.4 and 3.1 against 2.5.)
+// The kernel for few tokens is launched while the one before it winds down (256 tokens 2.4 -> 2.0 us).  The other one is not: its CTAs
+// would gather on the SMs that the kernel before leaves first (append and read of 1024 tokens of 32 heads 13.8 -> 16.2 us).
 // Quantising is the other bound: 13 instructions a value were 12 us of the 16384 tokens' time.  Extremes two at a time in bf16, packed
 // fp32 arithmetic, no clamping where a group's extremes stay inside, and 16 values of a group to a lane make it about 8.
 namespace {
@@ -428,6 +431,7 @@ template <int G> __device__ __forceinline__ int param_at(int tt, int value, int 
 template <typename T, int G>
 __global__ void __launch_bounds__(256) kv_append_few_kernel(const T* k, long long ks, const T* v, long long vs, const SlotArgs S) {
     constexpr int WORDS = kv::tile_bytes(64 * G) / 4;
+    kv::follow();
     const u32 per_token = (u32)S.H * G * 8, i = blockIdx.x * 256 + threadIdx.x, t = i / per_token, rest = i - t * per_token;
     const int value = blockIdx.y, h = (int)(rest / (G * 8)), g = (int)(rest / 8) % G, e8 = (int)rest & 7;
     const bool in = t < (u32)S.T;
@@ -521,6 +525,7 @@ __device__ __forceinline__ void put8(__nv_bfloat16* p, const float (&x)[8]) {
 template <typename T, int G>
 __global__ void __launch_bounds__(256) kv_read_few_kernel(T* k, T* v, const SlotArgs S) {
     constexpr int WORDS = kv::tile_bytes(64 * G) / 4;
+    kv::follow();
     const u32 per_token = (u32)S.H * G * 8, i = blockIdx.x * 256 + threadIdx.x, t = i / per_token, rest = i - t * per_token;
     const int value = blockIdx.y, h = (int)(rest / (G * 8)), g = (int)(rest / 8) % G, e8 = (int)rest & 7;
     if (t >= (u32)S.T) return;
@@ -595,13 +600,15 @@ int plan_launch(const pop_kv_cache_t* c, const int64_t* slots, int n_tokens, Lau
 }
 
 template <typename T, int G>
-void append(const Launch& l, const void* k, long long ks, const void* v, long long vs, cudaStream_t st) {
-    if (l.few) kv_append_few_kernel<T, G><<<l.grid, 256, 0, st>>>((const T*)k, ks, (const T*)v, vs, l.S);
-    else kv_append_kernel<T, G><<<l.grid, WARPS * 32, 0, st>>>((const T*)k, ks, (const T*)v, vs, l.S);
+cudaError_t append(const Launch& l, const void* k, long long ks, const void* v, long long vs, cudaStream_t st) {
+    if (l.few) return kv::launch(kv_append_few_kernel<T, G>, l.grid, 256, st, (const T*)k, ks, (const T*)v, vs, l.S);
+    kv_append_kernel<T, G><<<l.grid, WARPS * 32, 0, st>>>((const T*)k, ks, (const T*)v, vs, l.S);
+    return cudaGetLastError();
 }
-template <typename T, int G> void read(const Launch& l, void* k, void* v, cudaStream_t st) {
-    if (l.few) kv_read_few_kernel<T, G><<<l.grid, 256, 0, st>>>((T*)k, (T*)v, l.S);
-    else kv_read_kernel<T, G><<<l.grid, WARPS * 32, 0, st>>>((T*)k, (T*)v, l.S);
+template <typename T, int G> cudaError_t read(const Launch& l, void* k, void* v, cudaStream_t st) {
+    if (l.few) return kv::launch(kv_read_few_kernel<T, G>, l.grid, 256, st, (T*)k, (T*)v, l.S);
+    kv_read_kernel<T, G><<<l.grid, WARPS * 32, 0, st>>>((T*)k, (T*)v, l.S);
+    return cudaGetLastError();
 }
 
 }  // namespace
@@ -616,13 +623,10 @@ extern "C" int pop_kv_append(const pop_kv_cache_t* c, const void* k, long long k
     if (rc == POP_OK) rc = kv::check_rows(v, v_stride, c->n_kv_heads, c->head_dim, dtype);
     if (rc != POP_OK) return rc;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (dtype == POP_BF16) {
-        if (c->head_dim == 64) append<__nv_bfloat16, 1>(l, k, k_stride, v, v_stride, st);
-        else append<__nv_bfloat16, 2>(l, k, k_stride, v, v_stride, st);
-    } else {
-        if (c->head_dim == 64) append<float, 1>(l, k, k_stride, v, v_stride, st);
-        else append<float, 2>(l, k, k_stride, v, v_stride, st);
-    }
+    if (dtype == POP_BF16)
+        POP_CUDA((c->head_dim == 64 ? append<__nv_bfloat16, 1>(l, k, k_stride, v, v_stride, st) : append<__nv_bfloat16, 2>(l, k, k_stride, v, v_stride, st)));
+    else
+        POP_CUDA((c->head_dim == 64 ? append<float, 1>(l, k, k_stride, v, v_stride, st) : append<float, 2>(l, k, k_stride, v, v_stride, st)));
     POP_LAUNCHED();
     return POP_OK;
 }
@@ -638,13 +642,10 @@ extern "C" int pop_kv_read(const pop_kv_cache_t* c, const int64_t* slots, int n_
     if (rc == POP_OK) rc = kv::check_rows(v, row, c->n_kv_heads, c->head_dim, dtype);
     if (rc != POP_OK) return rc;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (dtype == POP_BF16) {
-        if (c->head_dim == 64) read<__nv_bfloat16, 1>(l, k, v, st);
-        else read<__nv_bfloat16, 2>(l, k, v, st);
-    } else {
-        if (c->head_dim == 64) read<float, 1>(l, k, v, st);
-        else read<float, 2>(l, k, v, st);
-    }
+    if (dtype == POP_BF16)
+        POP_CUDA((c->head_dim == 64 ? read<__nv_bfloat16, 1>(l, k, v, st) : read<__nv_bfloat16, 2>(l, k, v, st)));
+    else
+        POP_CUDA((c->head_dim == 64 ? read<float, 1>(l, k, v, st) : read<float, 2>(l, k, v, st)));
     POP_LAUNCHED();
     return POP_OK;
 }

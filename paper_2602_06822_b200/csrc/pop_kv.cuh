@@ -27,6 +27,29 @@ __host__ __device__ constexpr int param_words(int G) { return 2 * G * GROUP_WORD
 __host__ __device__ constexpr int key_word(int t, int e8) { return 16 * (t & 7) + 4 * (e8 >> 1) + 2 * (t >> 3) + (e8 & 1); }
 __host__ __device__ constexpr int value_word(int t, int e8) { return 16 * e8 + 4 * ((t & 7) >> 1) + 2 * (t >> 3) + (t & 1); }
 
+// A kernel that may be launched while the one before it in its stream winds down.  It says `follow()` before anything else: from there on the
+// one before has finished, and the next one may be launched.
+__device__ __forceinline__ void follow() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+inline cudaLaunchAttribute following() {
+    cudaLaunchAttribute a;
+    a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a.val.programmaticStreamSerializationAllowed = 1;
+    return a;
+}
+template <typename... P, typename... A> cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t st, A... args) {
+    cudaLaunchAttribute attr = following();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
 inline int check_cache(const pop_kv_cache_t* c) {
     if (!c || !c->pages || c->n_pages <= 0 || c->page_size <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0) return POP_ERR_INVALID_ARG;
     if (((uintptr_t)c->pages & 15u) != 0) return POP_ERR_INVALID_ARG;
