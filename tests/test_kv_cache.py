@@ -553,6 +553,15 @@ def test_append_read_and_plan_refuse_wrong_arguments():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(4, 4), (8, 2)])
+@pytest.mark.parametrize("kv,new", [([0] * 70 + [300] + [9] * 89, [0] * 70 + [150] + [0] * 89),     # a prompt among requests without tokens
+                                    ([200, 90, 33], [64, 1, 1]), ([200, 90, 33], [65, 1, 1]), ([200, 90, 33], [17, 0, 1]),
+                                    ([200, 90, 0], [18, 0, 0]), ([64], [16]), ([65], [17])])
+def test_lengths_at_which_kernels_change(kv, new, heads):
+    Setup(len(kv) + sum(new), *heads, 64, 16, BF16, kv, new).check()
+
+
+@pytest.mark.gpu
 def test_check_reports_a_wait_that_ran_out_and_clears_it():
     """The status word as a kernel that gives up would leave it (set from the host: no kernel is made to give up)."""
     s = Setup(21, 4, 2, 64, 16, BF16, [150, 20], [150, 1])
