@@ -30,7 +30,7 @@
 // tile: the tensor cores truncate theirs toward zero at every step, which over a thousand tokens would be 1e-5.
 //
 // Measured (head_dim 128, 4 query heads to each of 8 kv heads, bf16, one call after the other on new inputs): one token against 131070
-// 41.4 us = 3.65 TB/s, 64 tokens against 500 .. 8000 each 53.2 us = 3.78 TB/s, one against 1152 with 32 heads alone 9.9 us.  In the long
+// 41.4 us = 3.65 TB/s, 64 tokens against 500 .. 8000 each 53.2 us = 3.78 TB/s, one against 1152 with 32 heads alone 9.5 us.  In the long
 // one 5 us pass before the first tile is there (lengths, page ids, tiles: three trips to memory one after the other, and code that is
 // not in the instruction cache), 30 in the loop (5.0 TB/s; four of five issue slots taken, so it is instructions that are left to save) and
 // 6 in joining.  Fetching a unit by one bulk copy instead of nine 512-byte ones: 42.4 and 55.2 us.  14 or 16 warps with fewer registers:
@@ -59,8 +59,8 @@ template <typename T, int G, int NT> struct StreamCfg {
     static constexpr int PIECE = ROWS * (D + 4) * 4;        // un-normalised output, then (maximum, sum, -, -) of a part of a segment
     static constexpr int MIN_STAGES = (PIECE + UB - 1) / UB, WANT = (G == 1 ? 2 : 1) * (STEP == 2 ? 3 : 5);
     static constexpr int STAGES = MIN_STAGES > WANT ? MIN_STAGES : WANT;
-    // Segments up to this many units are not cut between CTAs where the whole call is that small (see there; 8 kv heads of 300 tokens 10.3 -> 9.2
-    // us, of 1000 tokens it would be 10.7 -> 12.4; both before joining got cheaper)
+    // Where no segment has more units than this, and no CTA would, none is cut between CTAs (see there; one request of 8 kv heads and 300 keys
+    // 9.3 -> 8.2 us, of 400, with longer segments allowed, 9.4 -> 9.6)
     static constexpr int SNAP = F32 ? 0 : WARPS;
     static constexpr int WARP_BYTES = STAGES * UB + PIECE;  // ring (its memory later holds the second piece) and first piece
 };
@@ -239,12 +239,14 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
     const int shift = sums_shift(A.R);
     if (lane < 2) piece_of[warp][lane].valid = 0;
     ull U = 0;
+    bool short_ones = true;                                                // no segment has more than SNAP units
     for (int r0 = 0, turn = 0; r0 < A.R; r0 += WARPS * 32, turn ^= 1) {
         const int r = r0 + tid;
         ull v = 0;
         if (r < A.R) {
             const Units un = request_units<ROWS, Cfg::TOKENS>(A, kv_request(A, r));
             v = (ull)un.count * un.row_blocks * A.Hk;
+            short_ones &= un.count <= Cfg::SNAP;
         }
         const ull own = v;
 #pragma unroll
@@ -263,14 +265,15 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
         }
         if (r < A.R && (r & ((1 << shift) - 1)) == 0) sums[r >> shift] = v;
     }
-    __syncthreads();
+    short_ones = __syncthreads_and(short_ones);
     // units of a CTA (the last one may have fewer, further ones none)
     const ull share = div_units(U + gridDim.x - 1, gridDim.x);
     const int cta = blockIdx.x;
     ull ca = min(U, cta * share), cb = min(U, ca + share);
     // Where a CTA has no more than SNAP units to do, which costs it no more than joining would, the cuts between CTAs are moved to the
-    // nearer end of a segment that is no longer than that either.
-    if (Cfg::SNAP > 0 && share < (ull)Cfg::SNAP) {
+    // nearer end of a segment, if all are that short.  (Looking takes half a microsecond, so not for those among others: 32 requests of 50 .. 450
+    // keys 11.0 us without, 12.7 with it.)
+    if (Cfg::SNAP > 0 && short_ones && share < (ull)Cfg::SNAP) {
         ull at = (lane & 1) ? cb : ca;
         if (at < U && at > 0) {
             int lo = 0, hi = ((A.R - 1) >> shift) + 1;
@@ -284,7 +287,7 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                 const ull all = (ull)un.count * un.row_blocks * A.Hk;
                 if (base + all <= at) { base += all; continue; }
                 const ull begin = base + div_units(at - base, un.count) * un.count;
-                if (un.count <= Cfg::SNAP) at = 2 * (at - begin) < (ull)un.count ? begin : begin + un.count;
+                at = 2 * (at - begin) < (ull)un.count ? begin : begin + un.count;
                 break;
             }
         }
