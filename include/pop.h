@@ -381,7 +381,7 @@ int pop_kv_read(const pop_kv_cache_t* cache, const int64_t* slots, int n_tokens,
  *   of cache->n_kv_heads, query head h reads kv head h / (n_heads / n_kv_heads).  Request r's queries are the tokens
  *   q_indptr[r] .. q_indptr[r + 1] - 1 (n of them; none, one, or many), and its keys the first kv_lens[r] tokens of block
  *   table row r.  Query i of n stands at position p = kv_len - n + i and sees the keys j
- *       j < kv_len,   and j <= p if causal,   and j > p - window if window > 0.
+ *       j < kv_len,   and j <= p if causal,   and j > p - window if window > 0   (any window up to 2^31 - 1).
  *   out [n_tokens][n_heads][head_dim] of `dtype`:  out = sum_j softmax_j(scale * q . k_j) v_j over the keys it sees; a query that
  *   sees none gets zeros.  lse [n_tokens][n_heads] fp32 (or NULL): log of the sum of exp(scale * q . k_j), -inf if none.
  * Tokens past q_indptr[n_requests] are not written.  Keys on a page that the table does not have (an id outside

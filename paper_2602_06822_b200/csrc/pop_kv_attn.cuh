@@ -38,9 +38,30 @@ __device__ __forceinline__ KvRequest kv_request(const KvAttnArgs& A, int r) {
     return q;
 }
 
-// Keys [lo, hi) that the query at position p sees.
-__device__ __forceinline__ int kv_first(const KvAttnArgs& A, int p) { return A.window > 0 ? max(0, p - A.window + 1) : 0; }
-__device__ __forceinline__ int kv_end(const KvAttnArgs& A, const KvRequest& q, int p) { return A.causal ? min(q.len, max(0, p + 1)) : q.len; }
+// Keys [lo, hi) that the query at position p sees.  (p - window is formed only where it cannot leave 32 bits: any window may be asked for, up
+// to 2^31 - 1, and p may be negative.)
+__host__ __device__ __forceinline__ int kv_first(const KvAttnArgs& A, int p) { return A.window > 0 && p >= A.window ? p - A.window + 1 : 0; }
+__host__ __device__ __forceinline__ int kv_end(const KvAttnArgs& A, const KvRequest& q, int p) { return A.causal ? min(q.len, max(0, p + 1)) : q.len; }
+
+// The streaming kernel's units (of TOKENS keys) of each row block's segment of a request: count >= 1, as every segment has a unit that
+// writes its result.  Under a causal window each row block has its own band of keys, `first` on; else all blocks are given the keys that any
+// query of the request sees.
+struct Units { int first, count, row_blocks; };
+template <int ROWS, int TOKENS> __host__ __device__ __forceinline__ Units request_units(const KvAttnArgs& A, const KvRequest& q) {
+    Units t = {0, 0, 0};
+    const long long rows = (long long)q.n * A.ratio;
+    if (q.n <= 0 || rows >= A.prompt_rows) return t;
+    t.row_blocks = (int)((rows + ROWS - 1) / ROWS);
+    const int lo = min(kv_first(A, q.pos0), q.len), hi = kv_end(A, q, q.pos0 + q.n - 1);
+    t.first = lo / TOKENS;
+    t.count = max(1, (hi + TOKENS - 1) / TOKENS - t.first);
+    if (A.causal && A.window > 0 && t.row_blocks > 1) {
+        // the rows of a block are of (ROWS - 1) / ratio + 2 tokens (a window near 2^31 would leave 32 bits here)
+        const u32 band = ((u32)A.window + (u32)((ROWS - 1) / A.ratio + TOKENS - 1)) / TOKENS + 1;
+        if (band < (u32)t.count) { t.count = (int)band; t.first = -1; }
+    }
+    return t;
+}
 
 __device__ __forceinline__ float kv_exp2(float x) {
     float y;

@@ -147,25 +147,6 @@ template <bool F32> __device__ __forceinline__ void code_pairs(u32 w, u32 (&x)[4
 
 __device__ __forceinline__ float2 half2_at(u32 w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 
-// Units (of TOKENS keys) of each row block's segment of a request: count >= 1, as every segment has a unit that writes its result.  Under a
-// causal window each row block has its own band of keys, `first` on; else all blocks are given the keys that any query of the request
-// sees.
-struct Units { int first, count, row_blocks; };
-template <int ROWS, int TOKENS> __device__ __forceinline__ Units request_units(const KvAttnArgs& A, const KvRequest& q) {
-    Units t = {0, 0, 0};
-    const long long rows = (long long)q.n * A.ratio;
-    if (q.n <= 0 || rows >= A.prompt_rows) return t;
-    t.row_blocks = (int)((rows + ROWS - 1) / ROWS);
-    const int lo = min(kv_first(A, q.pos0), q.len), hi = kv_end(A, q, q.pos0 + q.n - 1);
-    t.first = lo / TOKENS;
-    t.count = max(1, (hi + TOKENS - 1) / TOKENS - t.first);
-    if (A.causal && A.window > 0 && t.row_blocks > 1) {
-        const int band = (A.window + (ROWS - 1) / A.ratio + TOKENS - 1) / TOKENS + 1;       // the rows of a block are of (ROWS - 1) / ratio + 2 tokens
-        if (band < t.count) { t.count = band; t.first = -1; }
-    }
-    return t;
-}
-
 // The sums over the requests are kept for every request, or for every fourth one where there are more than 1024.
 constexpr int MAX_SUMS = 1024;
 __host__ __device__ constexpr int sums_shift(int R) { return R <= MAX_SUMS ? 0 : 2; }

@@ -568,13 +568,14 @@ def kv_attention(pages, q, block_table, q_indptr, kv_lens, scale: Optional[float
         raise ValueError("out must be a contiguous tensor of q's shape and dtype")
     if lse_out is not None and (lse_out.dtype != torch.float32 or tuple(lse_out.shape) != (T, heads) or not lse_out.is_contiguous()):
         raise ValueError("lse_out must be a contiguous float32 tensor [tokens, heads]")
+    window = max(-1, min(int(window), 2**31 - 1))            # (what a C int holds: -1 is refused, 2^31 - 1 hides nothing)
     st = _stream_ptr(stream)
     if workspace is None:
         workspace = _kv_workspace(q.device, st)
     _same_device(pages.device, q, block_table, q_indptr, kv_lens, out, lse_out, workspace)
     _check(lib().pop_kv_attention(C.byref(desc), q.data_ptr(), qs, _dtype_code(q), heads, T, q_indptr.data_ptr(), kv_lens.data_ptr(), R,
                                   block_table.data_ptr(), block_table.shape[1], desc.head_dim ** -0.5 if scale is None else scale,
-                                  int(causal), int(window), out.data_ptr(), None if lse_out is None else lse_out.data_ptr(),
+                                  int(causal), window, out.data_ptr(), None if lse_out is None else lse_out.data_ptr(),
                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), st), "pop_kv_attention")
     if made:
         _used_on(stream, out)

@@ -626,3 +626,23 @@ def test_binding_refuses_wrong_tensors():
                 lambda: pop.kv_read(pages, slots, torch.float16)):
         with pytest.raises(TypeError):
             bad()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 8, 2 ** 30, 2 ** 33])
+def test_a_window_beyond_every_length_hides_nothing(window, dtype):
+    """Row blocks of the streaming kernel (fp32, and bf16 requests of 17 to 64 rows), prompts, queries before the first key."""
+    s = Setup(22, 4, 2, 64, 16, dtype, [300, 90, 40, 5, 700], [150, 9, 30, 32, 1])
+    for causal in (True, False):
+        assert torch.equal(s.run(causal=causal, window=window), s.run(causal=causal, window=0))
+    s.check(window=window)
+
+
+@pytest.mark.gpu
+def test_negative_windows_are_refused():
+    s = Setup(23, 2, 2, 64, 16, BF16, [20], [1])
+    for window in (-1, -2 ** 31, -2 ** 32 - 5):
+        with pytest.raises(pop.PopError) as e:
+            s.run(window=window)
+        assert e.value.status == pop.POP_ERR_INVALID_ARG
