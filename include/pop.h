@@ -350,7 +350,7 @@ int pop_kv_page_bytes(int page_size, int n_kv_heads, int head_dim, size_t* bytes
  * Outputs: q_indptr [n_requests + 1], the prefix sums of max(new, 0); kv_lens [n_requests] = ctx + new (0 if finished);
  * for each of the n_tokens new tokens, in request order, its slot and its position in its request (both -1 past the last
  * token; n_tokens is the capacity of the two arrays, tokens beyond it are not listed); info {new tokens, pages that
- * were wanted and not given}.  A page is not given when the ring is empty or the row has max_blocks pages: its block table
+ * were wanted and not given}.  A page is not given when the ring is empty or the row has no place for it (max_blocks): its block table
  * entry (if there is one) and its tokens' slots are -1, which the calls below leave out.
  * All arrays device, int32 but for slots (int64); positions and info may be NULL.  The sums of ctx + new and of the pages
  * stay below 2^31.

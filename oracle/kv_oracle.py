@@ -16,13 +16,12 @@ def plan(ctx, new, table, ring, head, count, page, capacity):
             indptr.append(indptr[-1])
             continue
         for b in range(had, -(-(c + n) // page)):
-            p = -1
-            if want < count:
-                p = int(ring[(head + want) % n_pages])
-                got += 1
             want += 1
-            if b < max_blocks:
-                table[r, b] = p
+            if b < max_blocks:                       # the row has a place for it
+                table[r, b] = -1
+                if got < count:
+                    table[r, b] = ring[(head + got) % n_pages]
+                    got += 1
         for i in range(n):
             b = (c + i) // page
             p = int(table[r, b]) if b < max_blocks else -1

@@ -61,6 +61,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_plan_kernel(const PlanArgs P)
     int* take = tok + P.R + 1;                   // [R + 1] pages to take before r
     int* give = take + P.R + 1;                  // [R + 1] pages to give back before r
     __shared__ Sum3 warp_sum[PLAN_THREADS / 32];
+    __shared__ int beyond;                       // pages wanted for blocks that the rows have no place for
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     kv::follow();
     const int head = P.state_in[0], count = P.state_in[1];
@@ -77,6 +78,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_plan_kernel(const PlanArgs P)
         new_of[k] = in ? P.fresh[r] : 0;
     }
     Sum3 mine[PER], sum = {0, 0, 0};
+    int over = 0;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int r = tid * per + k, ctx = ctx_of[k], n = new_of[k];
@@ -84,7 +86,12 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_plan_kernel(const PlanArgs P)
         if (k < per && r < P.R) {
             const int had = (ctx + P.page_size - 1) / P.page_size;
             if (n < 0) mine[k].c = min(had, P.max_blocks);
-            else { mine[k].a = n; mine[k].b = (ctx + n + P.page_size - 1) / P.page_size - had; }
+            else {                               // a page for every new block that the row has a place for
+                const int want = (ctx + n + P.page_size - 1) / P.page_size;
+                mine[k].a = n;
+                mine[k].b = max(0, min(want, P.max_blocks) - had);
+                over += want - had - mine[k].b;
+            }
             if (blockIdx.x == 0) P.kv_lens[r] = n < 0 ? 0 : ctx + n;
         }
         sum = sum + mine[k];
@@ -96,7 +103,9 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_plan_kernel(const PlanArgs P)
         if (lane >= d) upto = upto + u;
     }
     if (lane == 31) warp_sum[warp] = upto;
+    if (tid == 0) beyond = 0;
     __syncthreads();
+    if (over) atomicAdd(&beyond, over);
     Sum3 before = warp_sum[lane];                                           // every warp sums up the warps for itself
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -162,8 +171,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_plan_kernel(const PlanArgs P)
     for (int i = first; i < n_take; i += stride) {
         const int r = find_request(take, P.R, i, 0);
         const int ctx = max(P.ctx[r], 0);
-        const int block = (ctx + P.page_size - 1) / P.page_size + (i - take[r]);
-        if (block < P.max_blocks) P.table[(size_t)r * P.max_blocks + block] = taken_page(i);
+        P.table[(size_t)r * P.max_blocks + (ctx + P.page_size - 1) / P.page_size + (i - take[r])] = taken_page(i);
     }
     if (P.state_in == P.state_out && gridDim.x > 1) cg::this_cluster().sync();      // every CTA has read the state
     else __syncthreads();
@@ -171,7 +179,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_plan_kernel(const PlanArgs P)
         const int got = min(n_take, count);
         P.state_out[0] = (int)(((long long)head + got) % P.n_pages);
         P.state_out[1] = min(P.n_pages, count - got + n_give);
-        if (P.info) { P.info[0] = n_tok; P.info[1] = n_take - got; }
+        if (P.info) { P.info[0] = n_tok; P.info[1] = n_take - got + beyond; }
     }
 }
 

@@ -646,3 +646,51 @@ def test_negative_windows_are_refused():
         with pytest.raises(pop.PopError) as e:
             s.run(window=window)
         assert e.value.status == pop.POP_ERR_INVALID_ARG
+
+
+FULL_ROWS = [     # ctx, new, max_blocks, free pages -> state, info, what each row has then (pages of 16 tokens, free ones 100, 101, ..)
+    ([0], [80], 3, 10, [3, 7], [80, 2], [[100, 101, 102]]),
+    ([32], [64], 2, 6, [0, 6], [64, 4], [[0, 1]]),
+    ([60, 5], [40, 30], 2, 4, [1, 3], [70, 4], [[0, 1], [2, 100]]),
+    ([0, 20, 0], [70, 40, 20], 3, 5, [5, 0], [130, 4], [[100, 101, 102], [0, 1, 103], [104, -1, -7]]),
+]
+
+
+def full_row_case(ctx, new, max_blocks, free):
+    table, at = np.full((len(ctx), max_blocks), -7, dtype=np.int32), 0
+    for r, c in enumerate(ctx):
+        n = min(-(-c // 16), max_blocks)
+        table[r, :n] = range(at, at + n)
+        at += n
+    ring = np.full(110, -1, dtype=np.int32)
+    ring[:free] = range(100, 100 + free)
+    return table, ring
+
+
+@pytest.mark.parametrize("ctx,new,max_blocks,free,state,info,rows", FULL_ROWS)
+def test_oracle_gives_a_full_row_no_pages(ctx, new, max_blocks, free, state, info, rows):
+    table, ring = full_row_case(ctx, new, max_blocks, free)
+    w = ko.plan(ctx, new, table, ring, 0, free, 16, sum(new))
+    assert w["state"] == state and w["info"] == info and w["table"].tolist() == rows
+    lost = sum(max(0, c + n - max(c, max_blocks * 16)) for c, n in zip(ctx, new))
+    assert w["slots"].count(-1) >= lost
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("ctx,new,max_blocks,free,state,info,rows", FULL_ROWS)
+def test_a_full_row_takes_no_pages_from_the_ring(ctx, new, max_blocks, free, state, info, rows, in_place):
+    table, ring = full_row_case(ctx, new, max_blocks, free)
+    w = check_plan(ctx, new, table, ring, 0, free, 16, sum(new), in_place)
+    assert w["state"] == state and w["info"] == info
+
+
+@pytest.mark.gpu
+def test_many_full_rows_among_others():
+    rng = np.random.default_rng(31)
+    for R in (900, 4096):
+        ctx, new, table, ring, head, count = plan_case(rng, R, 16, 20, 60, 7, 50, max_blocks=3)
+        for in_place in (True, False):
+            w = check_plan(ctx, new, table, ring, head, count, 16, sum(max(n, 0) for n in new), in_place)
+            over = sum(-(-(c + n) // 16) - max(3, -(-c // 16)) for c, n in zip(ctx, new) if n >= 0 and c + n > 48)
+            assert w["info"][1] == over > 0
