@@ -346,7 +346,7 @@ int pop_kv_page_bytes(int page_size, int n_kv_heads, int head_dim, size_t* bytes
  *   ring [n_pages], state {head, count}   the free pages: ring[(head + i) % n_pages], i < count.
  * Row r gets pages for its blocks ceil(ctx / page_size) .. ceil((ctx + new) / page_size) - 1, taken from the ring's head in
  * order of (request, block).  The pages of finished requests are put at the ring's tail in the same order (free from the
- * next call on; their rows stay as they are).  state_out receives the new head and count and may be the same array as state_in.
+ * next call on; their rows stay as they are, and entries that are no page, as -1, are passed over).  state_out receives the new head and count and may be the same array as state_in.
  * Outputs: q_indptr [n_requests + 1], the prefix sums of max(new, 0); kv_lens [n_requests] = ctx + new (0 if finished);
  * for each of the n_tokens new tokens, in request order, its slot and its position in its request (both -1 past the last
  * token; n_tokens is the capacity of the two arrays, tokens beyond it are not listed); info {new tokens, pages that

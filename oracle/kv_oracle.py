@@ -11,7 +11,7 @@ def plan(ctx, new, table, ring, head, count, page, capacity):
     for r, (c, n) in enumerate(zip(ctx, new)):
         had = -(-c // page)
         if n < 0:
-            given_back += [int(p) for p in table[r, :min(had, max_blocks)]]
+            given_back += [int(p) for p in table[r, :min(had, max_blocks)] if 0 <= p < n_pages]
             kv_lens.append(0)
             indptr.append(indptr[-1])
             continue
@@ -25,7 +25,7 @@ def plan(ctx, new, table, ring, head, count, page, capacity):
         for i in range(n):
             b = (c + i) // page
             p = int(table[r, b]) if b < max_blocks else -1
-            slots.append(p * page + (c + i) % page if p >= 0 else -1)
+            slots.append(p * page + (c + i) % page if 0 <= p < n_pages else -1)
             positions.append(c + i)
         kv_lens.append(c + n)
         indptr.append(indptr[-1] + n)

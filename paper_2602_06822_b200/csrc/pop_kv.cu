@@ -7,8 +7,8 @@ namespace cg = cooperative_groups;
 
 // ---------------------------------------------------------------------------------------------------------------- plan
 //
-// Three exclusive sums over the requests (new tokens, pages to take, pages to give back), then three flat loops over the
-// tokens and the pages, each of which finds its request in its sum.  The sums are so short (at most 4096 requests, four to a
+// Three exclusive sums over the requests (new tokens, pages to take, table entries to give back), then three flat loops over the
+// tokens, the pages and the entries, each of which finds its request in its sum.  The sums are so short (at most 4096 requests, four to a
 // thread) that every CTA computes all of them for itself in shared memory, which leaves one thing to order: where the ring's new
 // state goes to the place of the old one, it must not be written before every CTA has read that.  Then the grid is one
 // thread-block cluster, whose barrier does that in hardware, with no flag in memory to clear and no second launch; where it goes
@@ -61,6 +61,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_plan_kernel(const PlanArgs P)
     int* take = tok + P.R + 1;                   // [R + 1] pages to take before r
     int* give = take + P.R + 1;                  // [R + 1] pages to give back before r
     __shared__ Sum3 warp_sum[PLAN_THREADS / 32];
+    __shared__ int warp_pages[2][PLAN_THREADS / 32];
     __shared__ int beyond;                       // pages wanted for blocks that the rows have no place for
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     kv::follow();
@@ -162,10 +163,42 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_plan_kernel(const PlanArgs P)
         P.slots[i] = slot;
         if (P.positions) P.positions[i] = pos;
     }
-    for (int i = first; i < n_give; i += stride) {
-        const int r = find_request(give, P.R, i, 0);
-        const int page = P.table[(size_t)r * P.max_blocks + (i - give[r])];
-        if (count + i < P.n_pages) P.ring[(int)(((long long)head + count + i) % P.n_pages)] = page;
+    // The pages of finished requests: where an entry of their rows is no page (it was refused when it was wanted), those behind it move up, so one
+    // CTA goes through them all, four entries to a thread at a time.
+    int given = 0;
+    if (blockIdx.x == gridDim.x - 1) {
+        constexpr int FOUR = 4;
+        for (int i0 = 0, turn = 0; i0 < n_give; i0 += FOUR * PLAN_THREADS, turn ^= 1) {
+            int page[FOUR], r = 0, n = 0;
+#pragma unroll
+            for (int k = 0; k < FOUR; ++k) {
+                const int i = i0 + FOUR * tid + k;
+                page[k] = -1;
+                if (i < n_give) {
+                    r = find_request(give, P.R, i, r);
+                    page[k] = P.table[(size_t)r * P.max_blocks + (i - give[r])];
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < FOUR; ++k) n += (u32)page[k] < (u32)P.n_pages;
+            int at = n;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int u = __shfl_up_sync(~0u, at, d);
+                if (lane >= d) at += u;
+            }
+            if (lane == 31) warp_pages[turn][warp] = at;
+            __syncthreads();
+            const int of_warp = warp_pages[turn][lane];
+            at += count + given - n + (int)__reduce_add_sync(~0u, lane < warp ? of_warp : 0);
+            given += (int)__reduce_add_sync(~0u, of_warp);
+#pragma unroll
+            for (int k = 0; k < FOUR; ++k)
+                if ((u32)page[k] < (u32)P.n_pages) {
+                    if (at < P.n_pages) P.ring[(int)(((long long)head + at) % P.n_pages)] = page[k];
+                    ++at;
+                }
+        }
     }
     // (the ring's cells written above are free ones, those read by taken_page are not: the two never meet)
     for (int i = first; i < n_take; i += stride) {
@@ -175,10 +208,10 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_plan_kernel(const PlanArgs P)
     }
     if (P.state_in == P.state_out && gridDim.x > 1) cg::this_cluster().sync();      // every CTA has read the state
     else __syncthreads();
-    if (blockIdx.x == 0 && tid == 0) {
+    if (blockIdx.x == gridDim.x - 1 && tid == 0) {
         const int got = min(n_take, count);
         P.state_out[0] = (int)(((long long)head + got) % P.n_pages);
-        P.state_out[1] = min(P.n_pages, count - got + n_give);
+        P.state_out[1] = min(P.n_pages, count - got + given);
         if (P.info) { P.info[0] = n_tok; P.info[1] = n_take - got + beyond; }
     }
 }

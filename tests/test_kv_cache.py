@@ -694,3 +694,52 @@ def test_many_full_rows_among_others():
             w = check_plan(ctx, new, table, ring, head, count, 16, sum(max(n, 0) for n in new), in_place)
             over = sum(-(-(c + n) // 16) - max(3, -(-c // 16)) for c, n in zip(ctx, new) if n >= 0 and c + n > 48)
             assert w["info"][1] == over > 0
+
+
+def short_of_pages(plan, steps, seed):
+    """A server with fewer pages than its requests want and rows that they outgrow: some are refused pages, finish, and start again.  After
+    every step the pages in the live rows and the free ones are all pages, each once."""
+    rng = np.random.default_rng(seed)
+    R, page, mb, n_pages = 7, 16, 6, 20
+    table, ring, head, count = np.full((R, mb), -1, dtype=np.int32), rng.permutation(n_pages).astype(np.int32), 3, n_pages
+    lens, refused, holes = np.zeros(R, dtype=np.int64), 0, 0
+    for _ in range(steps):
+        new = rng.integers(0, 50, R)
+        new[(lens > 0) & (rng.random(R) < 0.25)] = -1
+        for r in np.flatnonzero(new < 0):
+            holes += int((table[r, :min(mb, -(-lens[r] // page))] < 0).sum())
+        w = plan(lens.tolist(), new.tolist(), table, ring, head, count, page)
+        table, ring, (head, count) = np.asarray(w["table"]), np.asarray(w["ring"]), w["state"]
+        lens = np.asarray(w["kv_lens"])
+        refused += w["info"][1]
+        rows = np.concatenate([table[r, :min(mb, -(-int(n) // page))] for r, n in enumerate(lens)])
+        free = ring[(head + np.arange(count)) % n_pages]
+        assert sorted(rows[rows >= 0].tolist() + free.tolist()) == list(range(n_pages))
+        assert w["slots"].count(-1) == 0 or refused
+    assert refused > 0 and holes > 0
+
+
+@pytest.mark.parametrize("seed", [0, 1])
+def test_oracle_recovers_from_running_out_of_pages(seed):
+    short_of_pages(lambda c, n, t, r, h, k, page: ko.plan(c, n, t, r, h, k, page, sum(max(x, 0) for x in n)), 60, seed)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("in_place", [True, False])
+def test_pages_run_out_and_come_back(in_place):
+    short_of_pages(lambda c, n, t, r, h, k, page: check_plan(c, n, t, r, h, k, page, sum(max(x, 0) for x in n), in_place), 60, 2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("R,max_ctx", [(40, 900), (4000, 500)])
+def test_finished_rows_with_entries_that_are_no_page(R, max_ctx, in_place):
+    """Also more entries than are given back at a time (4096)."""
+    rng = np.random.default_rng(R)
+    ctx, new, table, ring, head, count = plan_case(rng, R, 16, max_ctx, 20, 2, 5)
+    hole = rng.random(table.shape) < 0.2
+    table[hole] = np.where(rng.random(int(hole.sum())) < 0.5, -1, 10 ** 6)
+    gone = [int(p) for r in range(R) if new[r] < 0 for p in table[r, :-(-ctx[r] // 16)]]
+    assert len(gone) > (4096 if R > 1000 else 100)
+    w = check_plan(ctx, new, table, ring, head, count, 16, sum(max(n, 0) for n in new), in_place)
+    assert w["state"][1] == count + sum(0 <= p < len(ring) for p in gone) - (w["state"][0] - head) % len(ring)
