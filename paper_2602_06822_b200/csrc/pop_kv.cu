@@ -39,6 +39,12 @@ __device__ __forceinline__ Sum3 shfl_up3(Sum3 v, int d) {
     return {__shfl_up_sync(~0u, v.a, d), __shfl_up_sync(~0u, v.b, d), __shfl_up_sync(~0u, v.c, d)};
 }
 
+struct PlanShared {                              // beside the sums, which are as long as there are requests
+    Sum3 warp_sum[PLAN_THREADS / 32];
+    int warp_pages[2][PLAN_THREADS / 32];
+    int beyond;                                  // pages wanted for blocks that the rows have no place for
+};
+
 // The last r with sum[r] <= i (sum[0] = 0, sum[R] > i), at or behind `from`: a few steps forward, then bisection.
 __device__ __forceinline__ int find_request(const int* sum, int R, int i, int from) {
     int lo = from;
@@ -60,9 +66,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_plan_kernel(const PlanArgs P)
     int* tok = plan_smem;                        // [R + 1] new tokens before request r
     int* take = tok + P.R + 1;                   // [R + 1] pages to take before r
     int* give = take + P.R + 1;                  // [R + 1] pages to give back before r
-    __shared__ Sum3 warp_sum[PLAN_THREADS / 32];
-    __shared__ int warp_pages[2][PLAN_THREADS / 32];
-    __shared__ int beyond;                       // pages wanted for blocks that the rows have no place for
+    __shared__ PlanShared shared;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     kv::follow();
     const int head = P.state_in[0], count = P.state_in[1];
@@ -103,11 +107,11 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_plan_kernel(const PlanArgs P)
         const Sum3 u = shfl_up3(upto, d);
         if (lane >= d) upto = upto + u;
     }
-    if (lane == 31) warp_sum[warp] = upto;
-    if (tid == 0) beyond = 0;
+    if (lane == 31) shared.warp_sum[warp] = upto;
+    if (tid == 0) shared.beyond = 0;
     __syncthreads();
-    if (over) atomicAdd(&beyond, over);
-    Sum3 before = warp_sum[lane];                                           // every warp sums up the warps for itself
+    if (over) atomicAdd(&shared.beyond, over);
+    Sum3 before = shared.warp_sum[lane];                                    // every warp sums up the warps for itself
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         const Sum3 u = shfl_up3(before, d);
@@ -187,9 +191,9 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_plan_kernel(const PlanArgs P)
                 const int u = __shfl_up_sync(~0u, at, d);
                 if (lane >= d) at += u;
             }
-            if (lane == 31) warp_pages[turn][warp] = at;
+            if (lane == 31) shared.warp_pages[turn][warp] = at;
             __syncthreads();
-            const int of_warp = warp_pages[turn][lane];
+            const int of_warp = shared.warp_pages[turn][lane];
             at += count + given - n + (int)__reduce_add_sync(~0u, lane < warp ? of_warp : 0);
             given += (int)__reduce_add_sync(~0u, of_warp);
 #pragma unroll
@@ -212,7 +216,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_plan_kernel(const PlanArgs P)
         const int got = min(n_take, count);
         P.state_out[0] = (int)(((long long)head + got) % P.n_pages);
         P.state_out[1] = min(P.n_pages, count - got + given);
-        if (P.info) { P.info[0] = n_tok; P.info[1] = n_take - got + beyond; }
+        if (P.info) { P.info[0] = n_tok; P.info[1] = n_take - got + shared.beyond; }
     }
 }
 
@@ -250,7 +254,7 @@ extern "C" int pop_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = in_place && ctas > 1 ? 2 : 1;
-    if (cfg.dynamicSmemBytes > 48 * 1024)
+    if (cfg.dynamicSmemBytes + sizeof(PlanShared) > 48 * 1024)       // (the limit is one for both)
         POP_CUDA(cudaFuncSetAttribute(kv_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * (POP_KV_MAX_REQUESTS + 1) * (int)sizeof(int)));
     POP_CUDA(cudaLaunchKernelEx(&cfg, kv_plan_kernel, P));
     POP_LAUNCHED();

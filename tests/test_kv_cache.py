@@ -12,6 +12,8 @@ the values that the cache holds (so quantisation itself is no error):
          bf16 alone has an rms of 1.7e-3).
 """
 import ctypes as C
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -743,3 +745,19 @@ def test_finished_rows_with_entries_that_are_no_page(R, max_ctx, in_place):
     assert len(gone) > (4096 if R > 1000 else 100)
     w = check_plan(ctx, new, table, ring, head, count, 16, sum(max(n, 0) for n in new), in_place)
     assert w["state"][1] == count + sum(0 <= p < len(ring) for p in gone) - (w["state"][0] - head) % len(ring)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("R", [4000, 4063, 4064, 4095])
+def test_plans_of_nearly_the_most_requests_as_a_process_first_call(R):
+    """(A larger call before would have asked for the shared memory that these need, so each has a process of its own.)"""
+    code = f"""
+import torch
+from paper_2602_06822_b200 import pop
+R, kw = {R}, dict(dtype=torch.int32, device="cuda")
+table = torch.full((R, 2), -1, **kw)
+p = pop.kv_plan(torch.zeros(R, **kw), torch.ones(R, **kw), table, torch.arange(R + 3, **kw), torch.tensor([0, R + 3], **kw), 16, R)
+assert p.q_indptr.tolist() == list(range(R + 1)) and p.slots.tolist() == list(range(0, 16 * R, 16))
+assert table[:, 0].tolist() == list(range(R)) and p.state.tolist() == [R, 3] and p.info.tolist() == [R, 0]
+"""
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=ge.ROOT, timeout=300)
