@@ -69,6 +69,19 @@ __device__ __forceinline__ float kv_exp2(float x) {
     return y;
 }
 
+// The elements of a group are 65504 at most (an infinite one is stored as that), but s and z are rounded, so that what its top code stands for,
+// 15 s + z, can come to 65520 and more, up to 65536, which is fp16's infinity.  Numbers in fp16 are limited to 65504 (2^-11 of them).
+__device__ __forceinline__ u32 kv_limited(u32 pair) {
+    u32 r;
+    asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(pair), "r"(0x7bff7bffu));
+    return r;
+}
+// A parameter word (s in the lower half, z in the upper) of such a group.
+__device__ __forceinline__ bool kv_past_half(u32 word) {
+    const __half2 p = *reinterpret_cast<const __half2*>(&word);
+    return __hisinf(__hfma(__low2half(p), __float2half_rn(15.f), __high2half(p))) != 0;
+}
+
 int pop_launch_kv_attention_stream(const KvAttnArgs& A, int head_dim, pop_dtype_t dtype, void* workspace, int device, int ctas, cudaStream_t st);
 size_t pop_kv_stream_workspace();
 int pop_kv_stream_max_ctas();

@@ -12,7 +12,7 @@
 //                    logit passes it by 2^15 (fp16's room; it is set 2^7 below the row's largest logit so far), which rescales O; after a
 //                    row's first block that is rare.
 //   warps 8-14       unpack keys and values: 16-token tiles of the cache, brought to shared memory two steps ahead (cp.async), into fp16
-//                    in the MMAs' 128-byte swizzle: c - 8 exactly, then s (c - 8) + (z + 8 s) with one rounding each to 11 bits
+//                    in the MMAs' 128-byte swizzle: c exactly, then s c + z, which rounds once to 11 bits
 //   warp 15          issues the MMAs: tile 0's products run while tile 1's softmax does, and the other way round
 // The items of a request are dealt out from its last rows (most keys under a causal mask) to its first.
 // Measured (head_dim 128, causal, bf16): 32 heads of 16384 tokens 2.33 ms = 945 TFLOP/s; six chunks of 65 .. 2049 tokens behind 100 .. 4100
@@ -163,20 +163,18 @@ __device__ __forceinline__ u32 hfma2(u32 a, u32 b, u32 c) {
     asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
     return r;
 }
-// Scale and z + 8 s of a parameter word, each twice.
+// Scale and zero point of a parameter word, each twice.
 struct ScaleZero { u32 s, z; };
-__device__ __forceinline__ ScaleZero scale_zero(u32 p) {
-    const u32 s = __byte_perm(p, p, 0x1010);
-    return {s, hfma2(s, 0x48004800u, __byte_perm(p, p, 0x3232))};
-}
-// The eight values of a word.
+__device__ __forceinline__ ScaleZero scale_zero(u32 p) { return {__byte_perm(p, p, 0x1010), __byte_perm(p, p, 0x3232)}; }
+// The eight values of a word: c exactly, then s c + z, which rounds once, kept in fp16's range.  (Finding out first which tiles need that, as the
+// streaming kernel does, took longer: a 1024-token prompt 30.3 us, with a branch for each step 30.8.)
 __device__ __forceinline__ uint4 unpack_word(u32 w, const ScaleZero& p) {
     const u32 v = w >> 8;
     uint4 r;
-    r.x = hfma2(hadd2(mask_or(w, 0x000f000fu, 0x64006400u), 0xe408e408u), p.s, p.z);            // (1024 + c) - 1032 = c - 8
-    r.y = hfma2(hadd2(mask_or(w, 0x00f000f0u, 0x54005400u), 0xd480d480u), p.s, p.z);            // (64 + c) - 72
-    r.z = hfma2(hadd2(mask_or(v, 0x000f000fu, 0x64006400u), 0xe408e408u), p.s, p.z);
-    r.w = hfma2(hadd2(mask_or(v, 0x00f000f0u, 0x54005400u), 0xd480d480u), p.s, p.z);
+    r.x = kv_limited(hfma2(hadd2(mask_or(w, 0x000f000fu, 0x64006400u), 0xe400e400u), p.s, p.z));            // (1024 + c) - 1024
+    r.y = kv_limited(hfma2(hadd2(mask_or(w, 0x00f000f0u, 0x54005400u), 0xd400d400u), p.s, p.z));            // (64 + c) - 64
+    r.z = kv_limited(hfma2(hadd2(mask_or(v, 0x000f000fu, 0x64006400u), 0xe400e400u), p.s, p.z));
+    r.w = kv_limited(hfma2(hadd2(mask_or(v, 0x00f000f0u, 0x54005400u), 0xd400d400u), p.s, p.z));
     return r;
 }
 __device__ __forceinline__ void st_shared(u32 addr, const uint4& v) {

@@ -18,8 +18,10 @@
 //   instead of per element:  q.k_j = sum over groups of  s q.c + z sum(q).  (What the accumulator's truncation leaves of the 1024 is the
 //   same for all keys but for some 1e-5 of a logit.)
 //   The query is fp16 too, each row times a power of two that puts its largest element at 2^10, which loses nothing of bf16.
-//   Values: c - 8 exactly by one addition per pair, then s (c - 8) + (z + 8 s) in fp16 (11 bits: 2^-12 of rounding against the
+//   Values: c exactly by one addition per pair, then s c + z in fp16 by one multiply-add, which rounds once (11 bits: 2^-12 against the
 //   result's 2^-9).  Here an offset must not stay: summed over the tokens it would grow with the context, and the result does not.
+//   Tiles with numbers past the range of fp16 (see kv_past_half) go the way of those that not every row sees, where they are limited.  (Looking
+//   for them: 64 requests 52.9 -> 53.9 us.)
 //   The weights p are fp16 in 2^-14 .. 2^15: the reference m stays at least 2^7 below the largest logit seen and is only brought up
 //   to date when one passes it by 2^15, which takes the reduction over the warp out of most tiles and leaves small weights, of
 //   which a long context has many, 2^32 of range.
@@ -130,7 +132,7 @@ __device__ __forceinline__ void code_pairs_raw(u32 w, u32 (&x)[4]) {
     x[2] = mask_or(v, 0x000f000fu, 0x64006400u);
     x[3] = mask_or(v, 0x00f000f0u, 0x54005400u);
 }
-// The same as numbers c - 8, in fp16 or bf16.
+// The same as numbers: c in fp16, c - 8 in bf16.
 template <bool F32> __device__ __forceinline__ void code_pairs(u32 w, u32 (&x)[4]) {
     if constexpr (F32) {
 #pragma unroll
@@ -141,7 +143,7 @@ template <bool F32> __device__ __forceinline__ void code_pairs(u32 w, u32 (&x)[4
     } else {
         code_pairs_raw(w, x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = hadd2(x[i], i & 1 ? 0xd480d480u : 0xe408e408u);       // - 72, - 1032
+        for (int i = 0; i < 4; ++i) x[i] = hadd2(x[i], i & 1 ? 0xd400d400u : 0xe400e400u);       // - 64, - 1024
     }
 }
 
@@ -456,8 +458,9 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                 }
             }
 
-        // ---- what is done with P tiles from `tile` on, at base; whole: every row sees every token of them
-        auto use_tiles = [&](int tile, unsigned char* base, auto count_, auto whole_) {
+        // ---- what is done with P tiles from `tile` on, at base; whole: every row sees every token of them, and their values are in fp16's range
+        // (found out here: if they are not, nothing has been done and false is returned)
+        auto use_tiles = [&](int tile, unsigned char* base, auto count_, auto whole_) -> bool {
             constexpr int P = decltype(count_)::value;
             constexpr bool whole = decltype(whole_)::value;
             auto params_of = [&](int p, int j, int from, u32 (&w)[G]) {    // token j of tile p: G words for the keys, the values' G further
@@ -538,7 +541,16 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                         }
                         top = fmaxf(top, above[p][nt][e]);
                     }
-            if (__any_sync(~0u, top > Cfg::RAISE)) {
+            bool past = false;
+            if constexpr (whole && !Cfg::F32) {          // the values' parameters, a word or none of each tile to a lane
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const u32* words = reinterpret_cast<const u32*>(base + p * TB) + kv::param_words(G) + G;
+                    if (G == 2 || lane < kv::TILE) past |= kv_past_half(words[lane / G * 2 * G + lane % G]);
+                }
+            }
+            if (__any_sync(~0u, top > Cfg::RAISE || past)) {
+                if (whole && !Cfg::F32 && __any_sync(~0u, past)) return false;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -638,8 +650,8 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                     params_of(p, 2 * t + 9, G, w[3]);
 #pragma unroll
                     for (int gr = 0; gr < G; ++gr) {
-                        const u32 s0 = __byte_perm(w[0][gr], w[1][gr], 0x5410), z0 = hfma2(s0, 0x48004800u, __byte_perm(w[0][gr], w[1][gr], 0x7632));
-                        const u32 s1 = __byte_perm(w[2][gr], w[3][gr], 0x5410), z1 = hfma2(s1, 0x48004800u, __byte_perm(w[2][gr], w[3][gr], 0x7632));
+                        const u32 s0 = __byte_perm(w[0][gr], w[1][gr], 0x5410), z0 = __byte_perm(w[0][gr], w[1][gr], 0x7632);
+                        const u32 s1 = __byte_perm(w[2][gr], w[3][gr], 0x5410), z1 = __byte_perm(w[2][gr], w[3][gr], 0x7632);
                         const uint4 vw = *reinterpret_cast<const uint4*>((base + p * TB) + (G + gr) * 512 + lane * 16);
                         u32 e0[4], e1[4], o0[4], o1[4];
                         code_pairs<false>(__byte_perm(vw.x, vw.y, 0x5410), e0);
@@ -648,13 +660,15 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
                         code_pairs<false>(__byte_perm(vw.z, vw.w, 0x7632), o1);
 #pragma unroll
                         for (int mt = 0; mt < 4; ++mt) {
-                            const u32 a0 = hfma2(e0[mt], s0, z0), a1 = hfma2(o0[mt], s0, z0), a2 = hfma2(e1[mt], s1, z1), a3 = hfma2(o1[mt], s1, z1);
+                            u32 a0 = hfma2(e0[mt], s0, z0), a1 = hfma2(o0[mt], s0, z0), a2 = hfma2(e1[mt], s1, z1), a3 = hfma2(o1[mt], s1, z1);
+                            if constexpr (!whole) { a0 = kv_limited(a0); a1 = kv_limited(a1); a2 = kv_limited(a2); a3 = kv_limited(a3); }
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) mma16816<false>(acc[nt][gr][mt], a0, a1, a2, a3, b[nt][0], b[nt][1]);
                         }
                     }
                 }
             }
+            return true;
         };
 
         int stage = 0;
@@ -664,9 +678,8 @@ __global__ void __launch_bounds__(StreamCfg<T, G, NT>::WARPS * 32, 1) kv_stream_
             unsigned char* base = ring + stage * Cfg::UB;
             const u32 there = present >> (Cfg::STEP * stage) & ((1u << Cfg::STEP) - 1u);
             if (++stage == STAGES) stage = 0;
-            if (there == (1u << Cfg::STEP) - 1u && unit * Cfg::TOKENS >= all_lo && (unit + 1) * Cfg::TOKENS <= all_hi) {
-                use_tiles(unit * Cfg::STEP, base, Const<Cfg::STEP>(), Const<1>());
-            } else {
+            const bool whole = there == (1u << Cfg::STEP) - 1u && unit * Cfg::TOKENS >= all_lo && (unit + 1) * Cfg::TOKENS <= all_hi;
+            if (!whole || !use_tiles(unit * Cfg::STEP, base, Const<Cfg::STEP>(), Const<1>())) {
                 for (int p = 0; p < Cfg::STEP; ++p)
                     if (there >> p & 1u) use_tiles(unit * Cfg::STEP + p, base + p * TB, Const<1>(), Const<0>());
             }

@@ -761,3 +761,117 @@ assert p.q_indptr.tolist() == list(range(R + 1)) and p.slots.tolist() == list(ra
 assert table[:, 0].tolist() == list(range(R)) and p.state.tolist() == [R, 3] and p.info.tolist() == [R, 0]
 """
     subprocess.run([sys.executable, "-c", code], check=True, cwd=ge.ROOT, timeout=300)
+
+
+# Values that the cache holds are finite (infinities count as +-65504), but with the rounding of scale and zero point a group's top code can
+# stand for up to 65536, which fp16 has no finite number for.  Each row: what is put at dimensions 5 and 70 of a row of ordinary values, or
+# the whole row.
+def saturated_rows(rng, Hk, D):
+    rows = []
+    for a, b in ((np.inf, 1.0), (np.inf, -np.inf), (-np.inf, np.inf), (65504.0, 65504.0), (-65504.0, 7e4), (65280.0, 0.0), (3e38, 3.0)):
+        x = rng.standard_normal((Hk, D)).astype(np.float32)
+        x[:, 5], x[:, D - 58] = a, b                              # (D = 64: dimensions 5 and 6 of one group)
+        rows.append(x)
+    both = rng.standard_normal((Hk, D)).astype(np.float32)
+    both[:, ::9], both[:, 1::9] = np.inf, -np.inf
+    rows += [both, np.full((Hk, D), np.inf, dtype=np.float32), np.full((Hk, D), -np.inf, dtype=np.float32)]
+    for lo, hi in ((-65504.0, -65414.0), (65400.0, 65504.0), (0.0, 65504.0), (1.0, 65504.0), (-34814.0, 65504.0), (3e4, 65504.0)):
+        rows.append(np.linspace(lo, hi, D, dtype=np.float32)[None].repeat(Hk, 0))
+    return rows
+
+
+def put(s, r, j, k, v):
+    """Key and value [Hk, D] (fp32, of s's type) as token j of request r, in the cache and in the exact values beside it."""
+    k, v = (torch.from_numpy(x)[None].to(s.dtype) for x in (k, v))
+    slot = int(s.table[r, j // s.page]) * s.page + j % s.page
+    pop.kv_append(s.pages, k.to(DEV), v.to(DEV), torch.tensor([slot], device=DEV))
+    at = sum(s.kv_lens[:r]) + j
+    s.k64[at], s.v64[at] = (ko.stored(x.float().numpy())[0] for x in (k, v))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_reads_saturated_values_as_finite(D, dtype):
+    """One key, so that the output is its value.  bf16: one of the two numbers next to it (it is rounded to fp16, or limited to 65504,
+    and then to bf16).  fp32: three bf16 pieces and the sums of its group's codes."""
+    rng = np.random.default_rng(41)
+    rows = saturated_rows(rng, 2, D)
+    one = Setup(41, 4, 2, D, 16, dtype, [1] * len(rows), [1] * len(rows))
+    many = [Setup(42 + i, 4, 2, D, 16, dtype, [1], [70]) for i in range(len(rows))]
+    for i, x in enumerate(rows):
+        put(one, i, 0, one.k64[i].astype(np.float32), x)
+        put(many[i], 0, 0, many[i].k64[0].astype(np.float32), x)
+    got = [one.run(causal=False).double().cpu().numpy()[:, None]]
+    got += [np.stack([m.run(causal=False).double().cpu().numpy() for m in many])]
+    want = one.v64.repeat(2, 1)                                    # [request, heads, D]
+    group = np.abs(want).reshape(len(rows), 4, -1, 64).max(-1, keepdims=True).repeat(64, -1).reshape(want.shape)
+    size = np.abs(want).astype(np.float32).view(np.uint32)
+    below, above = (((size >> 16) + i << 16).astype(np.uint32).view(np.float32).astype(np.float64) for i in (0, 1))
+    for g in got:
+        assert np.isfinite(g).all()
+        if dtype == BF16:
+            assert (((np.abs(g) == below[:, None]) | (np.abs(g) == above[:, None])) & (g * want[:, None] >= 0)).all()
+        else:
+            assert (np.abs(g - want[:, None]) <= (2.0 ** -18 * (np.abs(want) + group))[:, None]).all()
+
+
+def near_in_every_element(s, **mask):
+    """bf16 attention, element by element (a 2-norm would be that of the few elements that are large).  Keys may be rounded to fp16: a logit is
+    off by 2^-11 of ds = scale |q|_1 max|k|, a weight by twice that and its own 2^-11; a value by 2^-11, or 2^-11 where it is limited;
+    the result by 2^-8, half a unit of bf16."""
+    got = s.run(**mask).double().cpu().numpy()
+    at = 0
+    for r, (L, n) in enumerate(zip(s.kv_lens, s.new)):
+        a, b = s.indptr[r], s.indptr[r + 1]
+        q, k, v = s.q64[a:b], s.k64[at:at + L], s.v64[at:at + L]
+        o, size = (ko.attention(q, k, x, L - n, s.D ** -0.5, mask.get("causal", True), mask.get("window", 0))[0] for x in (v, np.abs(v)))
+        ds = s.D ** -0.5 * np.abs(q).sum(-1, keepdims=True) * np.abs(k).max()
+        off = (2 * 2.0 ** -11 * ds + 3 * 2.0 ** -11) * size
+        assert (np.abs(got[a:b] - o) <= off + 2.0 ** -8 * (np.abs(o) + off)).all()
+        at += L
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kv,new", [([150], [9]), ([150], [70]), ([400, 150], [1, 100]), ([90, 150], [1, 12])])
+def test_saturated_tokens_that_are_hidden_change_nothing(kv, new, D, dtype):
+    """The last request's token 141: queries that do not see it (causal, window) have the bits that they have with an ordinary one there,
+    those that do are near the exact result."""
+    rng = np.random.default_rng(43)
+    r, j = len(kv) - 1, 141
+    first = sum(new[:r])
+    masks = [dict(causal=True), dict(causal=True, window=3), dict(causal=False, window=4)]
+    s = Setup(43, 4, 2, D, 32, dtype, kv, new)
+    clean = [s.run(**m) for m in masks]
+    k0, v0 = (x[sum(kv[:r]) + j].astype(np.float32) for x in (s.k64, s.v64))
+    pos = torch.arange(new[r], device=DEV) + kv[r] - new[r]
+    hidden = [pos < j, (pos < j) | (pos - j >= 3), pos - j >= 4]
+    for x in saturated_rows(rng, 2, D):
+        for key, value in ((k0, x), (x, v0), (x, x)):
+            put(s, r, j, key, value)
+            for m, c, h in zip(masks, clean, hidden):
+                out = s.run(**m)
+                assert torch.isfinite(out.float()).all()
+                assert torch.equal(out[:first], c[:first]) and torch.equal(out[first:][h], c[first:][h])
+        put(s, r, j, k0, x)
+        for m in masks:
+            if dtype == F32:
+                s.check(want_lse=False, **m)
+            else:
+                near_in_every_element(s, **m)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kv,new", [([600], [1]), ([600, 40], [5, 1]), ([600], [90])])
+def test_saturated_tokens_all_over_the_context(kv, new, D):
+    rng = np.random.default_rng(44)
+    s = Setup(44, 8, 2, D, 64, BF16, kv, new)
+    rows = saturated_rows(rng, 2, D)
+    for i, j in enumerate([*range(0, 590, 37), 64, 65, 100, 101]):
+        put(s, 0, j, s.k64[j].astype(np.float32), rows[i % len(rows)])
+    near_in_every_element(s)
+    near_in_every_element(s, window=50)
+    near_in_every_element(s, causal=False)
