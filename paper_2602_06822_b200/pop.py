@@ -408,7 +408,7 @@ def prefill_scores_noalloc(X, Wg, Wu, Wd, out, stream=None):
 
 
 # ---------------------------------------------------------------------------------------------------------------------
-# The paged 4-bit key / value cache (pop_kv_*).  Tensors of one call are on one device, which is the current one.
+# The paged 4-bit key / value cache (pop_kv_*).  The tensors of a call have to be on the current device.
 # ---------------------------------------------------------------------------------------------------------------------
 
 def kv_page_bytes(page_size: int, n_kv_heads: int, head_dim: int) -> int:
@@ -436,10 +436,15 @@ def _kv_desc(pages) -> KVCacheDesc:
     return KVCacheDesc(pages.data_ptr(), n, tiles * POP_KV_TILE, h, nbytes // per_group * POP_KV_GROUP)
 
 
-def _same_device(dev, *tensors):
+def _on_current_device(stream, *tensors):
+    """The kernels run on the current device and follow the addresses they are given there: a tensor (or a stream) of another device, or of the
+    host, must not reach them."""
+    here = _torch()._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and t.device != dev:
-            raise ValueError("all tensors of a call must be on one CUDA device")
+        if t is not None and (not t.is_cuda or t.get_device() != here):
+            raise ValueError(f"all tensors of a call must be on the current CUDA device ({here}), one is on {t.device}")
+    if stream is not None and getattr(stream, "device_index", here) != here:
+        raise ValueError(f"the stream is not one of the current CUDA device ({here})")
 
 
 def _ints(t, dtype, what, dim=1):
@@ -489,7 +494,7 @@ def kv_plan(ctx_lens, new_lens, block_table, ring, state, page_size: int, n_toke
     R, dev = ctx_lens.shape[0], ctx_lens.device
     if new_lens.shape[0] != R or block_table.shape[0] != R or state.shape[0] < 2 or state_out.shape[0] < 2:
         raise ValueError("shape mismatch")
-    _same_device(dev, new_lens, block_table, ring, state, state_out)
+    _on_current_device(stream, ctx_lens, new_lens, block_table, ring, state, state_out)
     ints = torch.empty(2 * R + 3 + n_tokens, dtype=i32, device=dev)      # one allocation for the int32 outputs
     slots = torch.empty(n_tokens, dtype=torch.int64, device=dev)
     at = ints.data_ptr()
@@ -510,7 +515,7 @@ def kv_append(pages, k, v, slots, stream=None):
         raise ValueError("k, v and slots must have one length")
     if k.dtype != v.dtype:
         raise TypeError("dtype mismatch")
-    _same_device(pages.device, k, v, slots)
+    _on_current_device(stream, pages, k, v, slots)
     _check(lib().pop_kv_append(C.byref(desc), k.data_ptr(), ks, v.data_ptr(), vs, _dtype_code(k), slots.data_ptr(), k.shape[0],
                                _stream_ptr(stream)), "pop_kv_append")
 
@@ -520,7 +525,7 @@ def kv_read(pages, slots, dtype, stream=None):
     torch = _torch()
     desc = _kv_desc(pages)
     _ints(slots, torch.int64, "slots")
-    _same_device(pages.device, slots)
+    _on_current_device(stream, pages, slots)
     k = torch.empty(slots.shape[0], desc.n_kv_heads, desc.head_dim, dtype=dtype, device=pages.device)
     v = torch.empty_like(k)
     _check(lib().pop_kv_read(C.byref(desc), slots.data_ptr(), slots.shape[0], _dtype_code(k), k.data_ptr(), v.data_ptr(),
@@ -561,6 +566,7 @@ def kv_attention(pages, q, block_table, q_indptr, kv_lens, scale: Optional[float
     R = kv_lens.shape[0]
     if block_table.shape[0] != R or q_indptr.shape[0] != R + 1:
         raise ValueError("block_table, q_indptr and kv_lens must be of one number of requests")
+    _on_current_device(stream, pages, q, block_table, q_indptr, kv_lens, out, lse_out, workspace)
     made = out is None
     if made:
         out = torch.empty(T, heads, desc.head_dim, dtype=q.dtype, device=q.device)
@@ -572,7 +578,6 @@ def kv_attention(pages, q, block_table, q_indptr, kv_lens, scale: Optional[float
     st = _stream_ptr(stream)
     if workspace is None:
         workspace = _kv_workspace(q.device, st)
-    _same_device(pages.device, q, block_table, q_indptr, kv_lens, out, lse_out, workspace)
     _check(lib().pop_kv_attention(C.byref(desc), q.data_ptr(), qs, _dtype_code(q), heads, T, q_indptr.data_ptr(), kv_lens.data_ptr(), R,
                                   block_table.data_ptr(), block_table.shape[1], desc.head_dim ** -0.5 if scale is None else scale,
                                   int(causal), window, out.data_ptr(), None if lse_out is None else lse_out.data_ptr(),
@@ -587,6 +592,7 @@ def kv_attention_check(device="cuda", workspace=None, stream=None):
     st = _stream_ptr(stream)
     if workspace is None:
         workspace = _kv_workspace(_torch().empty(0, device=device).device, st)
+    _on_current_device(stream, workspace)
     _check(lib().pop_kv_attention_check(workspace.data_ptr(), st), "pop_kv_attention_check")
 
 

@@ -875,3 +875,59 @@ def test_saturated_tokens_all_over_the_context(kv, new, D):
     near_in_every_element(s)
     near_in_every_element(s, window=50)
     near_in_every_element(s, causal=False)
+
+
+def calls_of_every_kind(pages, k, slots, ctx, table, ring, state, indptr, stream=None):
+    """(which argument, call without it): the calls of the binding with one tensor given from outside."""
+    plan = dict(ctx_lens=ctx, new_lens=ctx, block_table=table, ring=ring, state=state, state_out=state.clone())
+    attend = dict(pages=pages, q=k, block_table=table, q_indptr=indptr, kv_lens=ctx, out=k.clone(),
+                  lse_out=torch.zeros(k.shape[:2], device=DEV), workspace=torch.zeros(16 << 20, dtype=torch.uint8, device=DEV))
+    for name, t in plan.items():
+        yield name, t, lambda x, name=name: pop.kv_plan(**{**plan, name: x}, page_size=16, n_tokens=1, stream=stream)
+    for name, t in (("pages", pages), ("k", k), ("v", k), ("slots", slots)):
+        yield name, t, lambda x, name=name: pop.kv_append(**{**dict(pages=pages, k=k, v=k, slots=slots), name: x}, stream=stream)
+    for name, t in (("pages", pages), ("slots", slots)):
+        yield name, t, lambda x, name=name: pop.kv_read(**{**dict(pages=pages, slots=slots), name: x}, dtype=F32, stream=stream)
+    for name, t in attend.items():
+        yield name, t, lambda x, name=name: pop.kv_attention(**{**attend, name: x}, stream=stream)
+
+
+def small_arguments():
+    ctx = i32([1, 1])
+    return (filled(4, 16, 2, 64), torch.randn(2, 2, 64, device=DEV), torch.arange(2, device=DEV), ctx, i32([[0], [1]]), i32([2, 3, 0, 0]),
+            i32([0, 2]), i32([0, 1, 2]))
+
+
+@pytest.mark.gpu
+def test_host_tensors_are_refused():
+    """One of them on the host, and all of a plan's (which would then be on one device, but not on this one)."""
+    for name, t, call in calls_of_every_kind(*small_arguments()):
+        with pytest.raises(ValueError):
+            call(t.cpu())
+    ctx, table, ring, state = (x.cpu() for x in (i32([1, 1]), i32([[0], [1]]), i32([2, 3, 0, 0]), i32([0, 2])))
+    with pytest.raises(ValueError):
+        pop.kv_plan(ctx, ctx, table, ring, state, 16, 2)
+
+
+@pytest.mark.gpu
+def test_tensors_of_another_device_than_the_current_one_are_refused(monkeypatch):
+    args = small_arguments()
+    calls = list(calls_of_every_kind(*args))
+    cache = pop.KVCache(1, 1, 32, 2, 64)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)                 # as if another one were current: nothing may be launched
+    before = pop.kernel_launch_count()
+    for name, t, call in calls:
+        with pytest.raises(ValueError):
+            call(t)
+    with pytest.raises(ValueError):
+        cache.plan(i32([1]), 1)
+    assert pop.kernel_launch_count() == before
+
+
+@pytest.mark.gpu
+def test_a_stream_of_another_device_is_refused():
+    class Elsewhere:
+        device_index, cuda_stream = 1, 0
+    for name, t, call in calls_of_every_kind(*small_arguments(), stream=Elsewhere()):
+        with pytest.raises(ValueError):
+            call(t)
