@@ -470,6 +470,12 @@ def _used_on(stream, *tensors):
                 t.record_stream(stream)
 
 
+def _no_gradient(*tensors):
+    """The cache has no backward pass (its values are rounded to 4 bits): a gradient must not end here unnoticed."""
+    if _torch().is_grad_enabled() and any(t.requires_grad for t in tensors):
+        raise ValueError("the 4-bit cache has no backward pass: detach() what requires a gradient, or call under torch.no_grad()")
+
+
 class KVPlan(NamedTuple):
     q_indptr: object      # int32 [requests + 1]
     kv_lens: object       # int32 [requests]
@@ -516,6 +522,7 @@ def kv_append(pages, k, v, slots, stream=None):
     if k.dtype != v.dtype:
         raise TypeError("dtype mismatch")
     _on_current_device(stream, pages, k, v, slots)
+    _no_gradient(k, v)
     _check(lib().pop_kv_append(C.byref(desc), k.data_ptr(), ks, v.data_ptr(), vs, _dtype_code(k), slots.data_ptr(), k.shape[0],
                                _stream_ptr(stream)), "pop_kv_append")
 
@@ -567,6 +574,7 @@ def kv_attention(pages, q, block_table, q_indptr, kv_lens, scale: Optional[float
     if block_table.shape[0] != R or q_indptr.shape[0] != R + 1:
         raise ValueError("block_table, q_indptr and kv_lens must be of one number of requests")
     _on_current_device(stream, pages, q, block_table, q_indptr, kv_lens, out, lse_out, workspace)
+    _no_gradient(q)
     made = out is None
     if made:
         out = torch.empty(T, heads, desc.head_dim, dtype=q.dtype, device=q.device)

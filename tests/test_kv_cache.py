@@ -931,3 +931,17 @@ def test_a_stream_of_another_device_is_refused():
     for name, t, call in calls_of_every_kind(*small_arguments(), stream=Elsewhere()):
         with pytest.raises(ValueError):
             call(t)
+
+
+@pytest.mark.gpu
+def test_tensors_that_require_a_gradient_are_refused():
+    pages, k, slots, ctx, table, _, _, indptr = small_arguments()
+    x = k.clone().requires_grad_()
+    for call in (lambda: pop.kv_append(pages, x, k, slots), lambda: pop.kv_append(pages, k, x * 2, slots),
+                 lambda: pop.kv_attention(pages, x, table, indptr, ctx)):
+        with pytest.raises(ValueError, match="backward"):
+            call()
+    with torch.no_grad():
+        pop.kv_append(pages, x, x, slots * 16)                       # (each request's first token)
+        want = pop.kv_attention(pages, x, table, indptr, ctx)
+    assert torch.equal(pop.kv_attention(pages, x.detach(), table, indptr, ctx), want)
