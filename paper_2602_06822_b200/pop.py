@@ -147,6 +147,7 @@ def set_config(**fields) -> Config:
 
 
 def release_cached_memory():
+    _kv_workspaces.clear()              # (their memory goes back to torch, in the order of the streams that they were made on)
     _check(lib().pop_release_cached_memory(), "pop_release_cached_memory")
 
 
@@ -541,20 +542,32 @@ def kv_read(pages, slots, dtype, stream=None):
     return k, v
 
 
+def kv_workspace(device="cuda"):
+    """A workspace for kv_attention, zeroed on the current stream.  Calls that share one must not run at the same time: it is for one stream, one
+    cache or one captured graph."""
+    n = C.c_size_t()
+    _check(lib().pop_kv_attention_workspace(C.byref(n)), "pop_kv_attention_workspace")
+    return _torch().zeros(n.value, dtype=_torch().uint8, device=device)
+
+
 _kv_workspaces = {}
 
 
-def _kv_workspace(device, stream_ptr: int):
-    """The attention's workspace of one (device, stream), made at its first call (outside any stream capture)."""
-    key = (device.index, stream_ptr)
+def _kv_workspace(device, stream):
+    """The workspace of a call that was given none: the one kept for its (device, stream).  A call that is being captured gets one of its own, as the
+    graph may be replayed on any stream, beside other work of this one."""
+    torch = _torch()
+    if stream is not None:                                              # made on the stream that uses it
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(stream.cuda_stream)
+        with torch.cuda.stream(stream):
+            return _kv_workspace(device, None)
+    if torch.cuda.is_current_stream_capturing():
+        return kv_workspace(device)
+    key = (device.index, _stream_ptr())
     ws = _kv_workspaces.get(key)
     if ws is None:
-        torch = _torch()
-        n = C.c_size_t()
-        _check(lib().pop_kv_attention_workspace(C.byref(n)), "pop_kv_attention_workspace")
-        ws = torch.zeros(n.value, dtype=torch.uint8, device=device)
-        torch.cuda.current_stream(device).synchronize()                 # zeroed before any stream uses it
-        _kv_workspaces[key] = ws
+        ws = _kv_workspaces[key] = kv_workspace(device)
     return ws
 
 
@@ -562,7 +575,8 @@ def kv_attention(pages, q, block_table, q_indptr, kv_lens, scale: Optional[float
                  out=None, lse_out=None, workspace=None, stream=None):
     """pop_kv_attention: q [T, n_heads, head_dim] (token rows may be strided) over the cache -> out [T, n_heads, head_dim].
     ``scale`` defaults to 1 / sqrt(head_dim); ``lse_out`` float32 [T, n_heads] receives the logarithms of the softmax sums.
-    ``workspace`` defaults to one kept for the stream."""
+    ``workspace`` (kv_workspace()) defaults to one kept for the stream, or, in a call that is being captured into a graph, to one that the graph
+    zeroes for every such call: a captured step should bring its own."""
     torch = _torch()
     desc = _kv_desc(pages)
     T, heads = q.shape[0], q.shape[1]
@@ -585,7 +599,7 @@ def kv_attention(pages, q, block_table, q_indptr, kv_lens, scale: Optional[float
     window = max(-1, min(int(window), 2**31 - 1))            # (what a C int holds: -1 is refused, 2^31 - 1 hides nothing)
     st = _stream_ptr(stream)
     if workspace is None:
-        workspace = _kv_workspace(q.device, st)
+        workspace = _kv_workspace(q.device, stream)
     _check(lib().pop_kv_attention(C.byref(desc), q.data_ptr(), qs, _dtype_code(q), heads, T, q_indptr.data_ptr(), kv_lens.data_ptr(), R,
                                   block_table.data_ptr(), block_table.shape[1], desc.head_dim ** -0.5 if scale is None else scale,
                                   int(causal), window, out.data_ptr(), None if lse_out is None else lse_out.data_ptr(),
@@ -599,15 +613,16 @@ def kv_attention_check(device="cuda", workspace=None, stream=None):
     """pop_kv_attention_check for the stream's own workspace (or the one given): synchronises, raises PopError if a wait ran out."""
     st = _stream_ptr(stream)
     if workspace is None:
-        workspace = _kv_workspace(_torch().empty(0, device=device).device, st)
+        workspace = _kv_workspace(_torch().empty(0, device=device).device, stream)
     _on_current_device(stream, workspace)
     _check(lib().pop_kv_attention_check(workspace.data_ptr(), st), "pop_kv_attention_check")
 
 
 class KVCache:
-    """A decoder's paged 4-bit cache: the pages of its layers, the block table of its requests and the ring of free pages.
-    One step of all requests is ``plan()`` once, then ``append()`` and ``attend()`` in every layer; everything stays on the device
-    and keeps its addresses, so a step can be captured into a CUDA graph (``plan`` with a fixed number of tokens)."""
+    """A decoder's paged 4-bit cache: the pages of its layers, the block table of its requests, the ring of free pages and the attention's
+    workspace.  One step of all requests is ``plan()`` once, then ``append()`` and ``attend()`` in every layer; everything stays on the device
+    and keeps its addresses, so a step can be captured into a CUDA graph (``plan`` with a fixed number of tokens).  A cache is for one stream at a
+    time; several caches, and graphs of them, may run side by side."""
 
     def __init__(self, n_layers: int, n_requests: int, max_tokens: int, n_kv_heads: int, head_dim: int, page_size: int = 64,
                  n_pages: Optional[int] = None, device="cuda"):
@@ -621,6 +636,7 @@ class KVCache:
         self.ring = torch.empty(self.n_pages, **i32)
         self.state = torch.empty(2, **i32)
         self.lens = torch.empty(n_requests, **i32)
+        self.workspace = kv_workspace(device)
         self.step: Optional[KVPlan] = None
         self.reset()
 
@@ -644,4 +660,5 @@ class KVCache:
         kv_append(self.pages[layer], k, v, self.step.slots)
 
     def attend(self, layer: int, q, **kw):
+        kw.setdefault("workspace", self.workspace)
         return kv_attention(self.pages[layer], q, self.block_table, self.step.q_indptr, self.step.kv_lens, **kw)

@@ -102,3 +102,98 @@ def test_cache_keeps_its_pages_to_itself_over_requests_that_come_and_go():
                 for i in range(2):
                     want = ko.stored(held[r][:, i] + np.float32(layer)) if len(j) else held[r][:, i]
                     np.testing.assert_array_equal(got[i].cpu().numpy(), want.astype(np.float32))
+
+
+def decode_steps(seed, tokens):
+    """A cache with a context long enough to be split over the machine, and a decode step of it: (run one step, its static inputs)."""
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(seed)
+    cache = pop.KVCache(2, 2, tokens + 64, 8, 64, page_size=64, device="cuda:0")
+    n = [tokens, tokens // 3]
+    cache.plan(torch.tensor(n, dtype=torch.int32, device="cuda:0"), sum(n))
+    for layer in range(2):
+        k, v = (torch.randn(sum(n), 8, 64, generator=g, device="cuda:0").bfloat16() for _ in range(2))
+        cache.append(layer, k, v)
+    one = torch.ones(2, dtype=torch.int32, device="cuda:0")
+    q, k, v = (torch.randn(2, 8, 64, generator=g, device="cuda:0").bfloat16() for _ in range(3))
+
+    def step():
+        cache.plan(one, 2)
+        out = []
+        for layer in range(2):
+            cache.append(layer, k, v)
+            out.append(cache.attend(layer, q))
+        return torch.stack(out)
+
+    def back():
+        cache.lens.copy_(torch.tensor(n))
+        cache.state.copy_(torch.tensor([sum(-(-x // 64) for x in n), cache.n_pages - sum(-(-x // 64) for x in n)]))
+    return cache, step, back
+
+
+def test_graphs_of_two_caches_run_side_by_side():
+    """Warmed up on a side stream, captured on the stream that torch.cuda.graph shares by default, replayed on two streams at once."""
+    caches = [decode_steps(seed, 9000) for seed in (1, 2)]
+    side = torch.cuda.Stream()
+    want, graphs, outs = [], [], []
+    for _, step, back in caches:
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            want.append(step().clone())
+        torch.cuda.synchronize()
+        back()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(step())
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in caches]
+    for _ in range(20):
+        for _, _, back in caches:
+            back()
+        torch.cuda.synchronize()
+        for st, g in zip(streams, graphs):
+            with torch.cuda.stream(st):
+                g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert torch.equal(a, b)
+
+
+def test_attention_without_a_workspace_captured_as_its_first_call():
+    """Two graphs of plain kv_attention calls: neither has the workspace of the capture stream or of the other."""
+    cases = []
+    for seed in (3, 4):
+        cache, step, _ = decode_steps(seed, 9000)
+        step()
+        q = torch.randn(2, 8, 64, device="cuda:0").bfloat16()
+        args = (cache.pages[0], q, cache.block_table, cache.step.q_indptr, cache.step.kv_lens)
+        cases.append((args, pop.kv_attention(*args, workspace=pop.kv_workspace())))
+    pop.release_cached_memory()
+    graphs, outs = [], []
+    for args, _ in cases:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            a = pop.kv_attention(*args)
+            b = pop.kv_attention(*args)
+        graphs.append(g)
+        outs.append((a, b))
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(20):
+        for st, g in zip(streams, graphs):
+            with torch.cuda.stream(st):
+                g.replay()
+        torch.cuda.synchronize()
+        for (a, b), (_, want) in zip(outs, cases):
+            assert torch.equal(a, want) and torch.equal(b, want)
+
+
+def test_workspaces_kept_for_streams_are_released():
+    cache, step, _ = decode_steps(5, 200)
+    step()
+    q = torch.randn(2, 8, 64, device="cuda:0").bfloat16()
+    args = (cache.pages[0], q, cache.block_table, cache.step.q_indptr, cache.step.kv_lens)
+    want = pop.kv_attention(*args)
+    held = torch.cuda.memory_allocated()
+    pop.release_cached_memory()
+    assert torch.cuda.memory_allocated() < held
+    assert torch.equal(pop.kv_attention(*args), want)
