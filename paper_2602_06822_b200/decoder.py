@@ -259,7 +259,7 @@ class Decoder:
 
     def close(self):
         if self.cache4 is not None:
-            pop.kv_attention_check(self.dev)
+            self.cache4.check()
             self.cache4 = None
         for p in self.parts:
             if p is not None:
@@ -330,6 +330,8 @@ def latency_table(cfg: Optional[DecoderConfig] = None, n_in: int = 128, n_out: i
             graphs[name] = gph
         torch.cuda.synchronize()
         t = {name: min(_replay_ms(gph, n_out, m, n_in) for _ in range(reps)) for name, gph in graphs.items()}
+        if m.cache4 is not None:
+            m.cache4.check()
         if ffn == "pop":
             for p in m.parts:
                 p.check()

@@ -610,7 +610,8 @@ def kv_attention(pages, q, block_table, q_indptr, kv_lens, scale: Optional[float
 
 
 def kv_attention_check(device="cuda", workspace=None, stream=None):
-    """pop_kv_attention_check for the stream's own workspace (or the one given): synchronises, raises PopError if a wait ran out."""
+    """pop_kv_attention_check for the workspace given, or the one kept for the stream: synchronises, raises PopError if a wait ran out.  (KVCache
+    has a check() of its own.  A captured call that was given no workspace cannot be checked.)"""
     st = _stream_ptr(stream)
     if workspace is None:
         workspace = _kv_workspace(_torch().empty(0, device=device).device, stream)
@@ -662,3 +663,8 @@ class KVCache:
     def attend(self, layer: int, q, **kw):
         kw.setdefault("workspace", self.workspace)
         return kv_attention(self.pages[layer], q, self.block_table, self.step.q_indptr, self.step.kv_lens, **kw)
+
+    def check(self):
+        """Synchronises the current stream; raises PopError if a wait of one of the cache's attention calls up to here ran out since the last check,
+        whichever stream or graph it ran in."""
+        kv_attention_check(workspace=self.workspace)

@@ -197,3 +197,28 @@ def test_workspaces_kept_for_streams_are_released():
     pop.release_cached_memory()
     assert torch.cuda.memory_allocated() < held
     assert torch.equal(pop.kv_attention(*args), want)
+
+
+def test_a_wait_that_ran_out_on_another_stream_is_reported():
+    """The status word as a kernel that gives up would leave it, set from the host: it is the cache's, whatever stream or graph the call ran in."""
+    cache, step, back = decode_steps(6, 300)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    cache.check()
+    cache.workspace[0] = 1
+    with pytest.raises(pop.PopError) as e:
+        cache.check()
+    assert e.value.status == pop.POP_ERR_TIMEOUT
+    cache.check()
+
+    cfg = dec.DecoderConfig(n_layers=1, d=1024, n_heads=8, N=1408, vocab=64, seed=7)
+    m = dec.Decoder(cfg, ffn="dense", kv_cache="int4", kv_tokens=80)
+    ids = dec.seeded_ids(cfg, 40, 3, m.dev)
+    m.prefill(ids[:30])
+    m.cache4.workspace[0] = 1
+    with pytest.raises(pop.PopError):
+        m.close()
+    m.close()
