@@ -127,10 +127,16 @@ class Decoder:
         L = self.layers[li]
         return F.linear(F.silu(F.linear(f, L["Wg"])) * F.linear(f, L["Wu"]), L["Wd"])
 
+    def _check_room(self, tokens: int):
+        """The 4-bit cache has no slots past its last page, and attention leaves out what has none: the decoder does not go there."""
+        if self.cache4 is not None and tokens > self.cache4.max_tokens:
+            raise ValueError(f"{tokens} tokens are more than the 4-bit cache has room for ({self.cache4.max_tokens}, from kv_tokens)")
+
     # ------------------------------------------------------------------ the two stages
     def prefill(self, ids: torch.Tensor):
         """ids [T] prompt token ids -> hidden states [T, d] after the last layer.  Builds every layer's partition."""
         assert self.pos == 0
+        self._check_room(ids.shape[0])
         if self.cache4 is not None:
             self.cache4.plan(torch.tensor([ids.shape[0]], device=self.dev, dtype=torch.int32), ids.shape[0])
         h = self.embed[ids]
@@ -154,6 +160,7 @@ class Decoder:
 
     def decode(self, tok: torch.Tensor, step: int = 0):
         """One teacher-forced token id [1] -> hidden state [1, d]."""
+        self._check_room(self.pos + 1)
         if self.cache4 is not None:
             self.cache4.plan(self.one, 1)
         h = self.embed[tok]
@@ -184,6 +191,7 @@ class Decoder:
         """After prefill: moves the KV cache into preallocated [max_len] buffers and keeps the position and the
         teacher-forced token ids on the device, so that one decode step is a fixed sequence of launches."""
         cfg = self.cfg
+        self._check_room(max_len)
         self.max_len = max_len
         self.ids_dev = ids_all.to(self.dev)
         self.pos_t = torch.tensor([self.pos], device=self.dev, dtype=torch.int64)

@@ -630,6 +630,7 @@ class KVCache:
         torch = _torch()
         self.page_size = page_size
         max_blocks = -(-max_tokens // page_size)
+        self.max_tokens = max_blocks * page_size                  # of a request: what its row of the block table has place for
         self.n_pages = n_requests * max_blocks if n_pages is None else n_pages
         self.pages = [kv_pages(self.n_pages, page_size, n_kv_heads, head_dim, device) for _ in range(n_layers)]
         i32 = dict(dtype=torch.int32, device=device)

@@ -222,3 +222,25 @@ def test_a_wait_that_ran_out_on_another_stream_is_reported():
     with pytest.raises(pop.PopError):
         m.close()
     m.close()
+
+
+def test_more_tokens_than_the_cache_has_room_for_are_refused():
+    cfg = dec.DecoderConfig(n_layers=1, d=1024, n_heads=8, N=1408, vocab=64, seed=8)
+    m = dec.Decoder(cfg, ffn="dense", kv_cache="int4", kv_tokens=60)               # one page: 64 tokens
+    ids = dec.seeded_ids(cfg, 80, 3, m.dev)
+    with pytest.raises(ValueError, match="kv_tokens"):
+        m.prefill(ids[:65])
+    m.prefill(ids[:62])
+    with pytest.raises(ValueError, match="kv_tokens"):
+        m.begin_static(ids, 65)
+    m.begin_static(ids, 64)
+    for i in (62, 63):
+        m.decode(ids[i: i + 1])
+    with pytest.raises(ValueError, match="kv_tokens"):
+        m.decode(ids[64:65])
+    assert m.cache4.lens.tolist() == [64] and m.cache4.step.info.tolist() == [1, 0]
+    m.close()
+    m = dec.Decoder(cfg, ffn="dense", kv_cache="bf16", kv_tokens=60)               # torch's cache grows
+    m.prefill(ids[:70])
+    m.decode(ids[70:71])
+    m.close()
