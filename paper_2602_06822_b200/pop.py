@@ -442,7 +442,7 @@ def _on_current_device(stream, *tensors):
     host, must not reach them."""
     here = _torch()._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != here):
+        if t is not None and t.get_device() != here:                    # (-1 on the host)
             raise ValueError(f"all tensors of a call must be on the current CUDA device ({here}), one is on {t.device}")
     if stream is not None and getattr(stream, "device_index", here) != here:
         raise ValueError(f"the stream is not one of the current CUDA device ({here})")
@@ -473,8 +473,9 @@ def _used_on(stream, *tensors):
 
 def _no_gradient(*tensors):
     """The cache has no backward pass (its values are rounded to 4 bits): a gradient must not end here unnoticed."""
-    if _torch().is_grad_enabled() and any(t.requires_grad for t in tensors):
-        raise ValueError("the 4-bit cache has no backward pass: detach() what requires a gradient, or call under torch.no_grad()")
+    for t in tensors:
+        if t.requires_grad and _torch().is_grad_enabled():
+            raise ValueError("the 4-bit cache has no backward pass: detach() what requires a gradient, or call under torch.no_grad()")
 
 
 class KVPlan(NamedTuple):
@@ -553,7 +554,7 @@ def kv_workspace(device="cuda"):
 _kv_workspaces = {}
 
 
-def _kv_workspace(device, stream):
+def _kv_workspace(device: int, stream):
     """The workspace of a call that was given none: the one kept for its (device, stream).  A call that is being captured gets one of its own, as the
     graph may be replayed on any stream, beside other work of this one."""
     torch = _torch()
@@ -562,9 +563,9 @@ def _kv_workspace(device, stream):
             stream = torch.cuda.ExternalStream(stream.cuda_stream)
         with torch.cuda.stream(stream):
             return _kv_workspace(device, None)
-    if torch.cuda.is_current_stream_capturing():
+    if torch._C._cuda_isCurrentStreamCapturing():
         return kv_workspace(device)
-    key = (device.index, _stream_ptr())
+    key = (device, torch._C._cuda_getCurrentRawStream(device))
     ws = _kv_workspaces.get(key)
     if ws is None:
         ws = _kv_workspaces[key] = kv_workspace(device)
@@ -596,10 +597,12 @@ def kv_attention(pages, q, block_table, q_indptr, kv_lens, scale: Optional[float
         raise ValueError("out must be a contiguous tensor of q's shape and dtype")
     if lse_out is not None and (lse_out.dtype != torch.float32 or tuple(lse_out.shape) != (T, heads) or not lse_out.is_contiguous()):
         raise ValueError("lse_out must be a contiguous float32 tensor [tokens, heads]")
-    window = max(-1, min(int(window), 2**31 - 1))            # (what a C int holds: -1 is refused, 2^31 - 1 hides nothing)
+    window = int(window)
+    if not 0 <= window < 2**31:                              # (what a C int holds: -1 is refused, 2^31 - 1 hides nothing)
+        window = -1 if window < 0 else 2**31 - 1
     st = _stream_ptr(stream)
     if workspace is None:
-        workspace = _kv_workspace(q.device, stream)
+        workspace = _kv_workspace(q.get_device(), stream)
     _check(lib().pop_kv_attention(C.byref(desc), q.data_ptr(), qs, _dtype_code(q), heads, T, q_indptr.data_ptr(), kv_lens.data_ptr(), R,
                                   block_table.data_ptr(), block_table.shape[1], desc.head_dim ** -0.5 if scale is None else scale,
                                   int(causal), window, out.data_ptr(), None if lse_out is None else lse_out.data_ptr(),
@@ -614,7 +617,7 @@ def kv_attention_check(device="cuda", workspace=None, stream=None):
     has a check() of its own.  A captured call that was given no workspace cannot be checked.)"""
     st = _stream_ptr(stream)
     if workspace is None:
-        workspace = _kv_workspace(_torch().empty(0, device=device).device, stream)
+        workspace = _kv_workspace(_torch().empty(0, device=device).get_device(), stream)
     _on_current_device(stream, workspace)
     _check(lib().pop_kv_attention_check(workspace.data_ptr(), st), "pop_kv_attention_check")
 
