@@ -346,7 +346,8 @@ int pop_kv_page_bytes(int page_size, int n_kv_heads, int head_dim, size_t* bytes
  *   ring [n_pages], state {head, count}   the free pages: ring[(head + i) % n_pages], i < count.
  * Row r gets pages for its blocks ceil(ctx / page_size) .. ceil((ctx + new) / page_size) - 1, taken from the ring's head in
  * order of (request, block).  The pages of finished requests are put at the ring's tail in the same order (free from the
- * next call on; their rows stay as they are, and entries that are no page, as -1, are passed over).  state_out receives the new head and count and may be the same array as state_in.
+ * next call on; their rows stay as they are, and entries that are no page, as -1, are passed over).  state_out receives the new
+ * head and count and may be the same array as state_in.
  * Outputs: q_indptr [n_requests + 1], the prefix sums of max(new, 0); kv_lens [n_requests] = ctx + new (0 if finished);
  * for each of the n_tokens new tokens, in request order, its slot and its position in its request (both -1 past the last
  * token; n_tokens is the capacity of the two arrays, tokens beyond it are not listed); info {new tokens, pages that
@@ -386,9 +387,11 @@ int pop_kv_read(const pop_kv_cache_t* cache, const int64_t* slots, int n_tokens,
  *   sees none gets zeros.  lse [n_tokens][n_heads] fp32 (or NULL): log of the sum of exp(scale * q . k_j), -inf if none.
  * Tokens past q_indptr[n_requests] are not written.  Keys on a page that the table does not have (an id outside
  * 0 .. n_pages - 1) are not seen.  kv_lens[r] <= max_blocks * page_size (more is cut to that).
- * Products, softmax statistics and sums are kept in fp32.  Equal calls give equal results, bit for bit.
- * workspace: device memory of pop_kv_attention_workspace() bytes, zeroed once before its first use; it serves one stream
- * at a time.  Allocates nothing; may be captured into a CUDA graph.
+ * Sums (of products, of weights, of weighted values) and the softmax's maxima are kept in fp32.  fp32 calls multiply bf16 pieces that make up
+ * fp32 numbers; bf16 calls multiply fp16 numbers (11 bits): q exactly but for a power of two, values, weights and, of requests with many rows, keys
+ * rounded once, numbers beyond 65504 as 65504.  Equal calls give equal results, bit for bit.
+ * workspace: device memory of pop_kv_attention_workspace() bytes, 16-byte aligned, zeroed once before its first use.  Calls that share one must
+ * not run at the same time: not on two streams, and not in two graphs that are replayed side by side.  Allocates nothing; may be captured into a CUDA graph.
  * pop_kv_attention_check synchronises the stream and reports whether a bounded wait of a call on this workspace ran out since
  * the last check (POP_ERR_TIMEOUT: that call's result is undefined; the workspace stays usable).
  */

@@ -13,7 +13,7 @@ namespace cg = cooperative_groups;
 // state goes to the place of the old one, it must not be written before every CTA has read that.  Then the grid is one
 // thread-block cluster, whose barrier does that in hardware, with no flag in memory to clear and no second launch; where it goes
 // elsewhere the grid is as large as the tokens ask for.
-// All latency: 4.9 us for 8 requests, 9.8 us for 2048 requests with 99040 new tokens (1.25 MB, 0.2 us of copying).
+// All latency: 4.9 us for 8 requests; for 2048 requests with 99040 new tokens (1.25 MB, 0.2 us of copying) 19.7 us with the state in place, 8.8 elsewhere.
 namespace {
 
 constexpr int PLAN_THREADS = 1024;
@@ -269,12 +269,13 @@ extern "C" int pop_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int
 // at the slots first, and 16 tokens that are a whole tile of the cache, wherever in the window they begin, are put together in
 // shared memory and moved as the consecutive bytes that they are; only what is not part of such a run goes word by word.
 // That costs a chain of three trips to memory, which a call of few tokens does not earn back: there every thread has 8 dimensions of
-// one token to itself.  (16384 tokens of 8 heads of 128, bf16: append 26.9 us against 34.1 thread by thread, read 17.5 against 28.2; the
+// one token to itself.  (16384 tokens of 8 heads of 128, bf16: append 27 us against 34 thread by thread, read 18 against 28; the
 // bytes alone take 13.3 each at the measured copy rate.  512 tokens: 3.7 against 2.4 and 3.1 against 2.5.)
 // The kernel for few tokens is launched while the one before it winds down (256 tokens 2.4 -> 2.0 us).  The other one is not: its CTAs
 // would gather on the SMs that the kernel before leaves first (append and read of 1024 tokens of 32 heads 13.8 -> 16.2 us).
-// Quantising is the other bound: 13 instructions a value were 12 us of the 16384 tokens' time.  Extremes two at a time in bf16, packed
-// fp32 arithmetic, no clamping where a group's extremes stay inside, and 16 values of a group to a lane make it about 8.
+// Quantising is the other bound: 17 instructions a value in all are 15 us of the 16384 tokens' issue slots, with extremes two at a time in bf16, packed
+// fp32 arithmetic, no clamping where a group's extremes stay inside, and 16 values of a group to a lane; the rest of the time a warp waits for its
+// first loads.
 namespace {
 
 constexpr int WARPS = 8;                         // of a CTA, each on its own

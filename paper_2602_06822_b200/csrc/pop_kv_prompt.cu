@@ -15,9 +15,9 @@
 //                    in the MMAs' 128-byte swizzle: c exactly, then s c + z, which rounds once to 11 bits
 //   warp 15          issues the MMAs: tile 0's products run while tile 1's softmax does, and the other way round
 // The items of a request are dealt out from its last rows (most keys under a causal mask) to its first.
-// Measured (head_dim 128, causal, bf16): 32 heads of 16384 tokens 2.33 ms = 945 TFLOP/s; six chunks of 65 .. 2049 tokens behind 100 .. 4100
-// cached ones (32 heads on 8) 262 us = 680 TFLOP/s; 32 heads of 1024 tokens 30 us = 290 TFLOP/s, of which the longest item's 8 blocks take
-// 20.  A block takes 4400 cycles instead of 2048: a softmax warp needs 2050 for its row's part (read 180, maximum 410, exponentials
+// Measured (head_dim 128, causal, bf16): 32 heads of 16384 tokens 2.3 ms = 950 TFLOP/s; six chunks of 65 .. 2049 tokens behind 100 .. 4100
+// cached ones (32 heads on 8) 267 to 295 us by the box, 605 TFLOP/s or more; 32 heads of 1024 tokens 30 us = 285 TFLOP/s, of which the longest item's
+// 8 blocks take 20.  A block takes 4400 cycles instead of 2048: a softmax warp needs 2050 for its row's part (read 180, maximum 410, exponentials
 // and packing 1460) and waits 1460 for the next product, which waits for the unpacked keys and for the other tile's product.
 // Every wait is bounded; one that runs out sets the status word and the CTA winds down.
 #include "pop_kv_attn.cuh"

@@ -32,10 +32,10 @@
 // tile: the tensor cores truncate theirs toward zero at every step, which over a thousand tokens would be 1e-5.
 //
 // Measured (head_dim 128, 4 query heads to each of 8 kv heads, bf16, one call after the other on new inputs): one token against 131070
-// 41.4 us = 3.65 TB/s, 64 tokens against 500 .. 8000 each 53.2 us = 3.78 TB/s, one against 1152 with 32 heads alone 9.5 us.  In the long
+// 41.9 us = 3.6 TB/s, 64 tokens against 500 .. 8000 each 54.0 us = 3.7 TB/s, one against 1152 with 32 heads alone 9.4 us.  In the long
 // one 5 us pass before the first tile is there (lengths, page ids, tiles: three trips to memory one after the other, and code that is
-// not in the instruction cache), 30 in the loop (5.0 TB/s; four of five issue slots taken, so it is instructions that are left to save) and
-// 6 in joining.  Fetching a unit by one bulk copy instead of nine 512-byte ones: 42.4 and 55.2 us.  14 or 16 warps with fewer registers:
+// not in the instruction cache), 31 in the loop (4.9 TB/s; four of five issue slots taken, so it is instructions that are left to save) and
+// 6 in joining.  Fetching a unit by one bulk copy instead of nine 512-byte ones cost 1 and 2 us.  14 or 16 warps with fewer registers:
 // slower.
 #include <type_traits>
 

@@ -44,7 +44,7 @@ def ratios_for(r: float, gamma: float = 0.1):
 
 class Decoder:
     """ffn = "pop" (every FFN through the library, ratios given) or "dense" (torch linear layers); kv_cache = "bf16" (torch) or
-    "int4" (the library's paged 4-bit cache, for up to kv_tokens tokens)."""
+    "int4" (the library's paged 4-bit cache, for up to kv_tokens tokens, in whole pages; more are refused)."""
 
     def __init__(self, cfg: DecoderConfig, device="cuda:0", ffn: str = "pop", ratios=None, k: Optional[int] = None, kv_cache: str = "bf16",
                  kv_tokens: int = 2048):
