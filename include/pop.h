@@ -402,6 +402,110 @@ int pop_kv_attention(const pop_kv_cache_t* cache, const void* q, long long q_str
                      const int32_t* block_table, int max_blocks, float scale, int causal, int window,
                      void* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/*
+ * ---- What a decoder layer does around its attention: norms, an 8-bit product, rotary positions ---------------------
+ * (Not in the paper either: with the FFN pruned and the cache in 4 bits, these and the projections' weights are what is left
+ * of a decode step.)  Inference only.  All arrays are device memory; rows of [d] elements lie `stride` elements apart, so that
+ * they may be slices of a wider projection.  Calls allocate nothing and may be captured into a CUDA graph.
+ */
+
+/*
+ * Norms before and after a block, with the block's gate and the residual addition between them.  For each token, with
+ * rms(x) = x / sqrt(mean(x^2) + eps) over its d elements:
+ *     b  = u                               the block's output; with post_norm  rms(u) * post_gain
+ *     h' = h_scale * h + u_scale * gate * b
+ *     f  = rms(h') * gain                  what the next block is given
+ *   h, u, h_out [n_tokens][d] of `dtype`; u NULL: there is no block (h' = h_scale * h; gate, post_norm and post_gain must be absent).
+ *   post_gain, gain [d] of `dtype`, NULL = all ones.  gate: rows of [d], one for each token, or one for all of them
+ *   (gate_stride 0), NULL = ones.
+ *   h_out NULL: not written.  It may be h (same stride) or u; f may be u or h where these are contiguous: nothing else may overlap.
+ *   f [n_tokens][d] contiguous of `dtype`, or NULL.  f_codes [n_tokens][d] with f_scales [ceil(d / 128)][n_tokens]: the same f as
+ *   pop_fp8_quantize would give it for f in 32 bits, or NULL (both, one, or neither of f and f_codes may be asked for; d a multiple of 16, all
+ *   pointers and rows 16-byte aligned for the codes).
+ * Any d up to POP_NORM_MAX_D.  Arithmetic and sums are 32-bit, f comes from h' before h' is rounded to `dtype`.
+ */
+#define POP_NORM_MAX_D  32768
+typedef struct {
+    const void *h, *u, *post_gain, *gate, *gain;
+    long long h_stride, u_stride, gate_stride;
+    void *h_out, *f, *f_codes;
+    float* f_scales;
+    long long h_out_stride;
+    float h_scale, u_scale, eps;
+    int post_norm;
+} pop_block_norm_t;
+int pop_block_norm(const pop_block_norm_t* args, int n_tokens, int d, pop_dtype_t dtype, void* cuda_stream);
+
+/*
+ * 8-bit floating point with a scale for every block of POP_FP8_BLOCK elements.
+ *   x [rows][K] of `dtype`, K a multiple of 16.  block_rows 1 (activations): every 128 consecutive elements of a row share a scale,
+ *   scales [ceil(K / 128)][rows]; block_rows 128 (weights): 128 rows x 128 elements do, scales [ceil(rows / 128)][ceil(K / 128)].
+ *   codes [rows][K]: e4m3 (sign, 4 bits of exponent, 3 of mantissa, no infinities, 0x7f NaN).  A code c stands for scale * c:
+ *     scale = max(a * (1 / 448), 2^-126) with a the largest magnitude among the block's finite elements,
+ *     c = x * (1 / scale) rounded to nearest even, at most 448; each operation in fp32.
+ *   An element that is not finite becomes NaN, and so does whatever is computed from it.
+ *
+ * pop_fp8_linear: y = x W^T from codes,  y[m][n] = sum_kb xs[kb][m] ws[n / 128][kb] sum_{k in kb} x[m][k] w[n][k], rounded once to `dtype`;
+ *   y rows [N] of `dtype`, y_stride elements apart.  The sum inside a block runs on the tensor cores (32-bit accumulators), the sum over
+ *   blocks in fp32.  Any M >= 0 and N >= 1; K a multiple of 16; codes 16-byte aligned.
+ * pop_fp8_linear_rows: the same for x [M][K] of x_dtype, quantised on the way (block_rows 1).  workspace: device memory of
+ *   pop_fp8_linear_workspace() bytes, 16-byte aligned, need not be initialised, for one call at a time.
+ * Equal calls give equal results, bit for bit, and so does a token among others (whatever M, up to the order of the fp32 sums, which
+ * goes by M, N and K).
+ * pop_fp8_check synchronises the stream and reports whether a bounded device-side wait of one of these calls ran out on the current device
+ * since the last check (POP_ERR_TIMEOUT: that call's y is undefined).
+ */
+#define POP_FP8_BLOCK  128
+int pop_fp8_quantize(const void* x, long long x_stride, int rows, int K, pop_dtype_t dtype, int block_rows, void* codes, float* scales,
+                     void* cuda_stream);
+int pop_fp8_linear(const void* x_codes, const float* x_scales, int M, const void* w_codes, const float* w_scales, int N, int K,
+                   void* y, long long y_stride, pop_dtype_t y_dtype, void* cuda_stream);
+int pop_fp8_linear_workspace(int M, int K, size_t* bytes);
+int pop_fp8_linear_rows(const void* x, long long x_stride, pop_dtype_t x_dtype, int M, const void* w_codes, const float* w_scales, int N, int K,
+                        void* y, long long y_stride, pop_dtype_t y_dtype, void* workspace, size_t workspace_bytes, void* cuda_stream);
+int pop_fp8_check(void* cuda_stream);
+
+/*
+ * Rotary positions.  The first rot_dim elements of a head are rot_dim / 2 pairs, (i, i + rot_dim / 2) or, interleaved, (2 i, 2 i + 1);
+ * pair i of a token at position p is turned by the angle p * w_i and multiplied by `magnitude`:
+ *     a' = a cos - b sin,  b' = b cos + a sin.
+ * pop_rope_frequencies (host only) gives w_i / 2 pi as 64-bit fractions of a turn, so that the angle of any position is exact to 2^-33 turns:
+ *   w_i = base^(-2 i / rot_dim), changed by `scaling` for contexts `factor` times original_positions (positions the model was trained on):
+ *     POP_ROPE_NONE     as it is
+ *     POP_ROPE_LINEAR   w / factor
+ *     POP_ROPE_NTK      base becomes base * factor^(rot_dim / (rot_dim - 2))
+ *     POP_ROPE_YARN     w / factor for pairs that turn less than beta_slow times within original_positions, w for those that turn more than
+ *                       beta_fast times, a ramp over the pair's index in between (its ends rounded outwards); magnitude 0.1 ln(factor) + 1
+ *     POP_ROPE_BANDS    by the turns t within original_positions: w / factor below beta_slow, w above beta_fast, linear in t in between
+ *   beta_fast, beta_slow: 0 = 32 and 1 (YARN), 4 and 1 (BANDS).  *magnitude receives that factor, 1 for the others.
+ * pop_rope: q [n_tokens][q_heads][head_dim] -> q_out, and k with k_heads alike (k NULL: q alone).  Rows may be strided, heads of a token are contiguous;
+ *   the outputs may be the inputs (then with the same strides).  freq: device array of rot_dim / 2.  inverse: turned by -p * w (the transposed map).
+ *   A token whose position is negative is left out: its rows are not written.  head_dim and rot_dim even, rot_dim <= head_dim <= POP_ROPE_MAX_DIM.
+ *   cos and sin are computed in 64 bits and rounded to fp32; every product and sum of the rotation is an fp32 operation.
+ * pop_kv_append_rope: q -> q_out as above, and k, rotated in fp32, and v into their slots of the 4-bit cache as pop_kv_append does it (a token whose
+ *   slot is outside the cache or whose position is negative is not stored).  Heads, alignment and strides as in pop_kv_append.
+ */
+#define POP_ROPE_MAX_DIM  512
+typedef enum { POP_ROPE_NONE = 0, POP_ROPE_LINEAR = 1, POP_ROPE_NTK = 2, POP_ROPE_YARN = 3, POP_ROPE_BANDS = 4 } pop_rope_scaling_t;
+typedef struct {
+    int rot_dim;
+    double base;
+    pop_rope_scaling_t scaling;
+    double factor, original_positions, beta_fast, beta_slow;
+} pop_rope_params_t;
+typedef struct {
+    const uint64_t* freq;         /* device [rot_dim / 2] */
+    int rot_dim, interleaved;
+    double magnitude;
+} pop_rope_t;
+int pop_rope_frequencies(const pop_rope_params_t* params, uint64_t* h_freq, double* magnitude);
+int pop_rope(const pop_rope_t* rope, int inverse, const int32_t* positions, int n_tokens, int head_dim, pop_dtype_t dtype,
+             const void* q, long long q_stride, int q_heads, void* q_out, long long q_out_stride,
+             const void* k, long long k_stride, int k_heads, void* k_out, long long k_out_stride, void* cuda_stream);
+int pop_kv_append_rope(const pop_kv_cache_t* cache, const pop_rope_t* rope, const int32_t* positions, const void* q, long long q_stride, int n_heads,
+                       void* q_out, long long q_out_stride, const void* k, long long k_stride, const void* v, long long v_stride,
+                       pop_dtype_t dtype, const int64_t* slots, int n_tokens, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,269 @@
+// 8-bit floating point: the quantisers, the product for few tokens, argument checks and the choice of kernels.
+#include "pop_fp8.cuh"
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------------------- quantisers
+//
+// Bound by memory: an element is read once and its code written.  A block of a row is 16 lanes' (bf16) or 32 lanes' (fp32) one load
+// of 16 bytes each, its maximum a few shuffles.
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+    static constexpr int E = 4;
+    __device__ static void open(const uint4& r, float (&x)[4]) { Elem<float>::unpack(r, x); }
+};
+template <> struct Vec<__nv_bfloat16> {
+    static constexpr int E = 8;
+    __device__ static void open(const uint4& r, float (&x)[8]) { Elem<__nv_bfloat16>::unpack(r, x); }
+};
+template <int E> __device__ __forceinline__ void put_codes(unsigned char* to, const u32 (&c)[E / 4]) {
+    if constexpr (E == 4) *reinterpret_cast<u32*>(to) = c[0];
+    else *reinterpret_cast<uint2*>(to) = make_uint2(c[0], c[1]);
+}
+
+template <typename T> __global__ void __launch_bounds__(256) quantise_rows_kernel(const T* x, long long stride, int rows, int K, int KB, unsigned char* codes, float* scales) {
+    constexpr int E = Vec<T>::E, LANES = fp8::BLOCK / E;
+    kv::follow();
+    const long long task = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;      // a block of a row
+    const int row = (int)(task / KB), kb = (int)(task - (long long)row * KB), at = kb * fp8::BLOCK + (threadIdx.x % LANES) * E;
+    const bool in = row < rows && at < K;
+    float v[E] = {};
+    if (in) Vec<T>::open(__ldcs(reinterpret_cast<const uint4*>(x + (long long)row * stride + at)), v);
+    u32 c[E / 4];
+    const float scale = fp8::quantise_row(v, c);
+    if (!in) return;
+    put_codes<E>(codes + (size_t)row * K + at, c);
+    if (threadIdx.x % LANES == 0) scales[(size_t)kb * rows + row] = scale;
+}
+
+// Weights: a CTA has a block of 128 x 128.
+template <typename T> __global__ void __launch_bounds__(256) quantise_blocks_kernel(const T* x, long long stride, int rows, int K, int KB, unsigned char* codes, float* scales) {
+    constexpr int E = Vec<T>::E, LANES = fp8::BLOCK / E, STEP = 256 / LANES, N = fp8::BLOCK / STEP;
+    __shared__ float part[8];
+    const int nb = blockIdx.x / KB, kb = blockIdx.x - nb * KB, at = kb * fp8::BLOCK + (threadIdx.x % LANES) * E;
+    const int first = nb * fp8::BLOCK + threadIdx.x / LANES;
+    uint4 raw[N];
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int row = first + i * STEP;
+        raw[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (row < rows && at < K) raw[i] = __ldcs(reinterpret_cast<const uint4*>(x + (long long)row * stride + at));
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float v[E];
+        Vec<T>::open(raw[i], v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) top = fmaxf(top, fp8::magnitude(v[e]));
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, part[i]);
+    const float scale = fp8::scale_of(top), factor = fp8::factor_of(scale);
+    if (threadIdx.x == 0) scales[(size_t)nb * KB + kb] = scale;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int row = first + i * STEP;
+        if (row >= rows || at >= K) continue;
+        float v[E];
+        Vec<T>::open(raw[i], v);
+        u32 c[E / 4];
+#pragma unroll
+        for (int j = 0; j < E / 4; ++j) c[j] = fp8::codes4(v + 4 * j, factor);
+        put_codes<E>(codes + (size_t)row * K + at, c);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------- product, few tokens
+//
+// Bound by the weights' bytes, N K of them, each used for at most 16 tokens.  A CTA has 16 rows of W, its eight warps every eighth block of
+// 128 along K.  mma.m16n8k32 takes the rows of W as its 16 rows and the tokens as its 8 columns; in which order the 128 elements of a block
+// go through its four steps does not matter as long as both operands have the same, so a lane loads 16 bytes of a row at a
+// time and uses them as they are: no shared memory, and four lanes have 64 consecutive bytes.
+// A block's sum starts from zero and is scaled into the running sums in fp32.
+constexpr int STREAM_WARPS = 8, STREAM_ROWS = 16, STREAM_DEPTH = 4;
+
+__device__ __forceinline__ void mma_e4m3(float (&c)[4], u32 a0, u32 a1, u32 a2, u32 a3, u32 b0, u32 b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Two of the four steps from 16 bytes of rows g and g + 8 of W and of token g.
+__device__ __forceinline__ void two_steps(float (&c)[4], const uint4& a, const uint4& b, const uint4& x) {
+    mma_e4m3(c, a.x, b.x, a.y, b.y, x.x, x.y);
+    mma_e4m3(c, a.z, b.z, a.w, b.w, x.z, x.w);
+}
+
+template <typename T> __device__ __forceinline__ void put(T* y, float v) { *y = Elem<T>::from_f32(v); }
+
+template <typename T, int NT> __global__ void __launch_bounds__(STREAM_WARPS * 32, 2) fp8_stream_kernel(const fp8::LinearArgs A) {
+    __shared__ float sums[STREAM_WARPS][NT * 8][STREAM_ROWS + 1];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int n0 = blockIdx.x * STREAM_ROWS;
+    kv::follow();
+    float acc[NT][4] = {};
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+    for (int first = warp; first < A.KB; first += STREAM_WARPS * STREAM_DEPTH) {
+        uint4 w[STREAM_DEPTH][4], x[STREAM_DEPTH][NT][2];
+#pragma unroll
+        for (int i = 0; i < STREAM_DEPTH; ++i) {
+            const int kb = first + i * STREAM_WARPS;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {                    // rows g, g + 8; halves of the block
+                const int row = n0 + g + 8 * (j & 1), at = kb * fp8::BLOCK + 64 * (j >> 1) + 16 * t;
+                w[i][j] = none;
+                if (row < A.N && at < A.K) w[i][j] = __ldcs(reinterpret_cast<const uint4*>(A.w + (size_t)row * A.K + at));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < STREAM_DEPTH; ++i) {
+            const int kb = first + i * STREAM_WARPS;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int at = kb * fp8::BLOCK + 64 * j + 16 * t;
+                    x[i][nt][j] = none;
+                    if (8 * nt + g < A.M && at < A.K) x[i][nt][j] = *reinterpret_cast<const uint4*>(A.x + (size_t)(8 * nt + g) * A.K + at);
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < STREAM_DEPTH; ++i) {
+            const int kb = first + i * STREAM_WARPS;
+            if (kb >= A.KB) break;
+            const float ws = A.ws[(size_t)(n0 / fp8::BLOCK) * A.KB + kb];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float c[4] = {};
+                two_steps(c, w[i][0], w[i][1], x[i][nt][0]);
+                two_steps(c, w[i][2], w[i][3], x[i][nt][1]);
+                const int m = 8 * nt + 2 * t;
+                const float s0 = m < A.M ? ws * A.xs[(size_t)kb * A.M + m] : 0.f, s1 = m + 1 < A.M ? ws * A.xs[(size_t)kb * A.M + m + 1] : 0.f;
+                acc[nt][0] = fmaf(c[0], s0, acc[nt][0]);
+                acc[nt][1] = fmaf(c[1], s1, acc[nt][1]);
+                acc[nt][2] = fmaf(c[2], s0, acc[nt][2]);
+                acc[nt][3] = fmaf(c[3], s1, acc[nt][3]);
+            }
+        }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sums[warp][8 * nt + 2 * t + (j & 1)][g + 8 * (j >> 1)] = acc[nt][j];
+    __syncthreads();
+    for (int i = threadIdx.x; i < NT * 8 * STREAM_ROWS; i += STREAM_WARPS * 32) {
+        const int m = i / STREAM_ROWS, n = i % STREAM_ROWS;
+        if (m >= A.M || n0 + n >= A.N) continue;
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < STREAM_WARPS; ++w) s += sums[w][m][n];
+        put((T*)A.y + (long long)m * A.y_stride + n0 + n, s);
+    }
+}
+
+template <typename T> cudaError_t stream(const fp8::LinearArgs& A, cudaStream_t st) {
+    const dim3 grid((A.N + STREAM_ROWS - 1) / STREAM_ROWS);
+    return A.M <= 8 ? kv::launch(fp8_stream_kernel<T, 1>, grid, STREAM_WARPS * 32, st, A) : kv::launch(fp8_stream_kernel<T, 2>, grid, STREAM_WARPS * 32, st, A);
+}
+
+constexpr int STREAM_TOKENS = 16;
+
+int sms_of(int* sms) {
+    int device = 0;
+    POP_CUDA(cudaGetDevice(&device));
+    static int known[64];                                     // asked for once per device
+    *sms = device < 64 ? known[device] : 0;
+    if (!*sms) {
+        POP_CUDA(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, device));
+        if (device < 64) known[device] = *sms;
+    }
+    return POP_OK;
+}
+
+int check_shape(int rows, int K) {
+    if (rows < 0 || K <= 0) return POP_ERR_INVALID_ARG;
+    return K % 16 == 0 ? POP_OK : POP_ERR_UNSUPPORTED;
+}
+int check_x(const void* x, long long stride, int K, pop_dtype_t dtype) {
+    if (dtype != POP_F32 && dtype != POP_BF16) return POP_ERR_UNSUPPORTED;
+    const int es = dtype == POP_F32 ? 4 : 2;
+    return !x || ((uintptr_t)x & 15u) != 0 || stride < K || (stride * es) % 16 != 0 ? POP_ERR_INVALID_ARG : POP_OK;
+}
+
+}  // namespace
+
+extern "C" int pop_fp8_quantize(const void* x, long long x_stride, int rows, int K, pop_dtype_t dtype, int block_rows, void* codes, float* scales,
+                                void* cuda_stream) {
+    int rc = check_shape(rows, K);
+    if (rc != POP_OK) return rc;
+    if (block_rows != 1 && block_rows != fp8::BLOCK) return POP_ERR_INVALID_ARG;
+    if (rows == 0) return POP_OK;
+    rc = check_x(x, x_stride, K, dtype);
+    if (rc != POP_OK) return rc;
+    if (!codes || !scales || ((uintptr_t)codes & 15u) != 0 || ((uintptr_t)scales & 3u) != 0) return POP_ERR_INVALID_ARG;
+    const int KB = fp8::blocks(K), lanes = fp8::BLOCK / (dtype == POP_F32 ? 4 : 8);
+    const long long ctas = block_rows == 1 ? ((long long)rows * KB + 256 / lanes - 1) / (256 / lanes) : (long long)fp8::blocks(rows) * KB;
+    if (ctas > 0x7fffffffll) return POP_ERR_UNSUPPORTED;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    const dim3 grid((u32)ctas);
+    unsigned char* to = (unsigned char*)codes;
+    if (block_rows == 1) {
+        if (dtype == POP_BF16) POP_CUDA(kv::launch(quantise_rows_kernel<__nv_bfloat16>, grid, 256, st, (const __nv_bfloat16*)x, x_stride, rows, K, KB, to, scales));
+        else POP_CUDA(kv::launch(quantise_rows_kernel<float>, grid, 256, st, (const float*)x, x_stride, rows, K, KB, to, scales));
+    } else if (dtype == POP_BF16) {
+        quantise_blocks_kernel<<<grid, 256, 0, st>>>((const __nv_bfloat16*)x, x_stride, rows, K, KB, to, scales);
+    } else {
+        quantise_blocks_kernel<<<grid, 256, 0, st>>>((const float*)x, x_stride, rows, K, KB, to, scales);
+    }
+    POP_LAUNCHED();
+    return POP_OK;
+}
+
+extern "C" int pop_fp8_linear(const void* x_codes, const float* x_scales, int M, const void* w_codes, const float* w_scales, int N, int K,
+                              void* y, long long y_stride, pop_dtype_t y_dtype, void* cuda_stream) {
+    int rc = check_shape(M, K);
+    if (rc != POP_OK) return rc;
+    if (N <= 0) return POP_ERR_INVALID_ARG;
+    if (y_dtype != POP_F32 && y_dtype != POP_BF16) return POP_ERR_UNSUPPORTED;
+    if (M == 0) return POP_OK;
+    if (!x_codes || !x_scales || !w_codes || !w_scales || !y || y_stride < N) return POP_ERR_INVALID_ARG;
+    if ((((uintptr_t)x_codes | (uintptr_t)w_codes) & 15u) != 0 || (((uintptr_t)x_scales | (uintptr_t)w_scales) & 3u) != 0) return POP_ERR_INVALID_ARG;
+    if ((uintptr_t)y & (y_dtype == POP_F32 ? 3u : 1u)) return POP_ERR_INVALID_ARG;
+    const fp8::LinearArgs A = {(const unsigned char*)x_codes, (const unsigned char*)w_codes, x_scales, w_scales, M, N, K, fp8::blocks(K), y, y_stride};
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (M <= STREAM_TOKENS) {
+        POP_CUDA((y_dtype == POP_BF16 ? stream<__nv_bfloat16>(A, st) : stream<float>(A, st)));
+        POP_LAUNCHED();
+        return POP_OK;
+    }
+    int sms = 0;
+    rc = sms_of(&sms);
+    return rc != POP_OK ? rc : pop_launch_fp8_gemm(A, y_dtype, sms, st);
+}
+
+extern "C" int pop_fp8_linear_workspace(int M, int K, size_t* bytes) {
+    if (!bytes) return POP_ERR_INVALID_ARG;
+    const int rc = check_shape(M, K);
+    if (rc != POP_OK) return rc;
+    *bytes = (size_t)fp8::blocks(K) * M * sizeof(float) + 16 + (size_t)M * K;      // scales, then codes at the next 16 bytes
+    return POP_OK;
+}
+
+extern "C" int pop_fp8_linear_rows(const void* x, long long x_stride, pop_dtype_t x_dtype, int M, const void* w_codes, const float* w_scales, int N, int K,
+                                   void* y, long long y_stride, pop_dtype_t y_dtype, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    size_t need = 0;
+    int rc = pop_fp8_linear_workspace(M, K, &need);
+    if (rc != POP_OK) return rc;
+    if (N <= 0) return POP_ERR_INVALID_ARG;
+    if (y_dtype != POP_F32 && y_dtype != POP_BF16) return POP_ERR_UNSUPPORTED;
+    if (M == 0) return POP_OK;
+    if (!w_codes || !w_scales || !y || y_stride < N || !workspace || workspace_bytes < need || ((uintptr_t)workspace & 15u) != 0) return POP_ERR_INVALID_ARG;
+    float* scales = (float*)workspace;
+    unsigned char* codes = (unsigned char*)workspace + (((size_t)fp8::blocks(K) * M * sizeof(float) + 15) & ~(size_t)15);
+    rc = pop_fp8_quantize(x, x_stride, M, K, x_dtype, 1, codes, scales, cuda_stream);
+    return rc != POP_OK ? rc : pop_fp8_linear(codes, scales, M, w_codes, w_scales, N, K, y, y_stride, y_dtype, cuda_stream);
+}

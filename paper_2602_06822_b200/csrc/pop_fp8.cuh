@@ -1,0 +1,53 @@
+// 8-bit floating point with a scale for every block of 128 (the public description is in include/pop.h).
+#pragma once
+
+#include "pop_kv.cuh"
+
+namespace fp8 {
+
+constexpr int BLOCK = POP_FP8_BLOCK;
+
+// The scale of a block whose largest finite magnitude is `top`, and the factor that its elements are multiplied with.
+__device__ __forceinline__ float scale_of(float top) { return fmaxf(__fmul_rn(top, 1.f / 448.f), 1.17549435e-38f); }
+__device__ __forceinline__ float factor_of(float scale) { return __frcp_rn(scale); }
+// |x|, 0 where x is not finite
+__device__ __forceinline__ float magnitude(float x) { const float m = fabsf(x); return m < INFINITY ? m : 0.f; }
+
+// Four values as codes.  (The conversion turns NaN into 0x7f, but an infinity into 448.)
+__device__ __forceinline__ u32 codes4(const float* x, float factor) {
+    float y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = fabsf(x[j]) < INFINITY ? __fmul_rn(x[j], factor) : __int_as_float(0x7fffffff);
+    unsigned short lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(y[1]), "f"(y[0]));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(y[3]), "f"(y[2]));
+    return (u32)lo | (u32)hi << 16;
+}
+
+// E values of a block that 128 / E consecutive lanes have (zeros where a lane is past the row's end): codes and the block's scale.
+template <int E> __device__ __forceinline__ float quantise_row(const float (&x)[E], u32 (&codes)[E / 4]) {
+    float top = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) top = fmaxf(top, magnitude(x[e]));
+#pragma unroll
+    for (int o = BLOCK / E / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    const float scale = scale_of(top), factor = factor_of(scale);
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i) codes[i] = codes4(x + 4 * i, factor);
+    return scale;
+}
+
+struct LinearArgs {
+    const unsigned char *x, *w;
+    const float *xs, *ws;
+    int M, N, K, KB;              // KB = ceil(K / 128)
+    void* y;
+    long long y_stride;
+};
+
+__host__ __device__ constexpr int blocks(int n) { return (n + BLOCK - 1) / BLOCK; }
+
+}  // namespace fp8
+
+// pop_fp8_gemm.cu: many tokens, on the tensor cores
+int pop_launch_fp8_gemm(const fp8::LinearArgs& A, pop_dtype_t y_dtype, int sms, cudaStream_t st);

@@ -1,0 +1,401 @@
+// The product of 8-bit operands with a scale for every block of 128, for many tokens:
+//
+//   y[m][n] = sum over blocks kb of  xs[kb][m] ws[n / 128][kb]  sum_{k in kb} x[m][k] w[n][k]
+//
+// on the tensor cores (tcgen05, kind f8f6f4).  The scales differ from block to block, so a block's sum cannot run on into the next one's:
+// every block of 128 (four MMAs of K = 32) starts a fresh accumulator in tensor memory, and the epilogue's warps add it, times its
+// scale, to running sums in their registers while the tensor cores work on the next block in the other accumulator.  Tokens are the MMA's
+// 128 rows (tensor-memory lanes): a thread has one token, and its scale for a block is one number for all of its columns.
+//
+// Warp roles (320 threads, one CTA per SM, persistent over tiles of 128 tokens x BN outputs):
+//   warp 0      TMA producer (one lane): x tile and W tile of a block per stage
+//   warp 1      allocates tensor memory; one lane issues the MMAs and the commits
+//   warps 2..9  epilogue: warp w has lanes 32 (w % 4) .. + 31, columns of half (w - 2) / 4
+// Where there are too few tiles for the machine, a cluster of S CTAs shares a tile, each with a range of the blocks; the partial sums
+// are joined through distributed shared memory in the order of the ranks, so results do not depend on timing.
+// Every wait is bounded; one that runs out sets the device's status word (pop_fp8_check) and the CTA winds down.
+#include <cuda.h>          // CUtensorMap and its enums (the encoder itself is looked up through the runtime)
+
+#include "pop_fp8.cuh"
+
+namespace {
+
+constexpr int BM = 128;                          // tokens of a tile
+constexpr int X_BYTES = BM * fp8::BLOCK;         // 16 KB: 128 rows of one 128-byte swizzle span
+constexpr int THREADS = 320, EPI_WARPS = 8;
+constexpr int SMEM_LIMIT = 227 * 1024;
+constexpr u64 WAIT_BUDGET_NS = 200ull * 1000ull * 1000ull;      // per wait
+
+template <int BN> struct Tile {
+    static constexpr int STAGE_BYTES = X_BYTES + BN * fp8::BLOCK;
+    static constexpr int STAGES_FIT = (SMEM_LIMIT - 2048) / STAGE_BYTES, STAGES = STAGES_FIT < 6 ? STAGES_FIT : 6;
+    static constexpr int SMEM = STAGES * STAGE_BYTES + 1024;
+    static constexpr u32 COLS = 2 * BN;          // two accumulators; a power of two, 32 at least
+    // fp32 accumulator (bits 4-5 = 1), A and B e4m3 (bits 7-9, 10-12 = 0), both K-major, N / 8 at bit 17, M / 16 at bit 24
+    static constexpr u32 IDESC = (1u << 4) | ((u32)(BN >> 3) << 17) | ((u32)(BM >> 4) << 24);
+    static_assert(STAGES * STAGE_BYTES >= BM * BN * 4, "partial sums of a tile go where the stages were");
+};
+
+__device__ u32 fp8_status;                       // 0, or which role gave up a wait
+enum { GAVE_UP_PRODUCER = 1, GAVE_UP_MMA = 2, GAVE_UP_EPILOGUE = 3 };
+
+__device__ __forceinline__ u32 smem_u32(const void* p) { return (u32)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(u32 bar, u32 count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void mbar_expect_tx(u32 bar, u32 bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(u32 bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ u32 mbar_try_wait(u32 bar, u32 parity) {
+    u32 ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
+    return ok;
+}
+// False when the wait has lasted too long, or another role of the CTA has given up (the caller leaves its loop).
+__device__ __forceinline__ bool mbar_wait(u32 bar, u32 parity, volatile int* gave_up, u32 code) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const u64 t0 = pop_global_ns();
+    for (u32 it = 1;; ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((it & 31u) == 0u) {
+            if (*gave_up) return false;
+            if (pop_global_ns() - t0 > WAIT_BUDGET_NS) {
+                *gave_up = 1;
+                atomicCAS(&fp8_status, 0u, code);
+                return false;
+            }
+        }
+    }
+}
+__device__ __forceinline__ void tma_load(u32 dst, const CUtensorMap* map, int x, int y, u32 bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(reinterpret_cast<u64>(map)), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void umma_f8(u32 d, u64 a, u64 b, u32 idesc, u32 accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma_commit(u32 bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// 32 consecutive columns of this thread's tensor-memory lane.
+__device__ __forceinline__ void tmem_ld32(u32 addr, float (&v)[32]) {
+    u32 r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+}
+// K-major tile of 128-byte rows in the 128-byte swizzle: groups of 8 rows are 1024 bytes apart, descriptor version 1, layout type 2.
+__device__ __forceinline__ u64 smem_desc(u32 addr) { return (u64)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61); }
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float remote(u32 addr, u32 rank) {            // a float at the same place in another CTA's shared memory
+    u32 there;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ void put8(float* y, const float (&v)[8]) {
+    reinterpret_cast<float4*>(y)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(y)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void put8(__nv_bfloat16* y, const float (&v)[8]) {
+    __nv_bfloat162 r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    *reinterpret_cast<uint4*>(y) = *reinterpret_cast<const uint4*>(r);
+}
+
+struct GemmArgs {
+    fp8::LinearArgs A;
+    int m_tiles, n_tiles, wide;                  // wide: rows of y may be written 8 elements at a time
+};
+
+// Eight columns of token m's row, from column n on.
+template <typename T> __device__ __forceinline__ void write8(const GemmArgs& G, int m, int n, const float (&v)[8]) {
+    if (m >= G.A.M || n >= G.A.N) return;
+    T* y = (T*)G.A.y + (long long)m * G.A.y_stride + n;
+    if (G.wide && n + 8 <= G.A.N) {
+        put8(y, v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (n + j < G.A.N) y[j] = Elem<T>::from_f32(v[j]);
+    }
+}
+
+template <typename T, int BN>
+__global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                                                              const GemmArgs G, const int S) {
+    typedef Tile<BN> L;
+    extern __shared__ unsigned char raw_smem[];
+    __shared__ u32 tmem_slot;
+    __shared__ int gave_up_flag;
+    __shared__ u64 bars[2 * L::STAGES + 5];
+    volatile int* gave_up = &gave_up_flag;
+    const u32 tiles = (smem_u32(raw_smem) + 1023u) & ~1023u;
+    const u32 full = smem_u32(bars), empty = full + 8 * L::STAGES, acc_full = full + 16 * L::STAGES, acc_empty = acc_full + 16, drain = acc_full + 32;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        gave_up_flag = 0;
+        for (int s = 0; s < L::STAGES; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(acc_full + 8 * b, 1); mbar_init(acc_empty + 8 * b, EPI_WARPS); }
+        mbar_init(drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(L::COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const u32 tmem = tmem_slot;
+    kv::follow();
+
+    // this CTA's tiles (one, if it shares it with others) and its range of their blocks
+    const int units = G.m_tiles * G.n_tiles, rank = blockIdx.x % S, kb0 = (int)((long long)G.A.KB * rank / S), kb1 = (int)((long long)G.A.KB * (rank + 1) / S);
+    const int first = blockIdx.x / S, step = gridDim.x / S;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0, issued = 0;
+            u32 ph = 0;
+            bool ok = true;
+            for (int unit = first; unit < units && ok; unit += step) {
+                const int mt = unit % G.m_tiles, nt = unit / G.m_tiles;
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    ok = mbar_wait(empty + 8 * s, ph ^ 1u, gave_up, GAVE_UP_PRODUCER);
+                    if (!ok) break;
+                    const u32 dst = tiles + (u32)s * L::STAGE_BYTES, bar = full + 8 * s;
+                    mbar_expect_tx(bar, L::STAGE_BYTES);
+                    tma_load(dst, &map_x, kb * fp8::BLOCK, mt * BM, bar);
+                    tma_load(dst + X_BYTES, &map_w, kb * fp8::BLOCK, nt * BN, bar);
+                    ++issued;
+                    if (++s == L::STAGES) { s = 0; ph ^= 1u; }
+                }
+            }
+            if (!ok) {                           // copies in flight still land in this CTA's shared memory: wait for them (bounded)
+                for (int j = 1; j <= min(issued, L::STAGES); ++j) {
+                    const int sj = s - j < 0 ? s - j + L::STAGES : s - j;
+                    const u32 pj = s - j < 0 ? ph ^ 1u : ph;
+                    const u64 t0 = pop_global_ns();
+                    while (!mbar_try_wait(full + 8 * sj, pj) && pop_global_ns() - t0 < WAIT_BUDGET_NS) {}
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            int s = 0, buf = 0;
+            u32 ph = 0, acc_ph = 0;              // bit b: phase of accumulator b
+            bool ok = true;
+            for (int unit = first; unit < units && ok; unit += step) {
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    ok = mbar_wait(acc_empty + 8 * buf, ((acc_ph >> buf) & 1u) ^ 1u, gave_up, GAVE_UP_MMA) && mbar_wait(full + 8 * s, ph, gave_up, GAVE_UP_MMA);
+                    if (!ok) break;
+                    tc_after();
+                    const u64 x = smem_desc(tiles + (u32)s * L::STAGE_BYTES), w = smem_desc(tiles + (u32)s * L::STAGE_BYTES + X_BYTES);
+#pragma unroll
+                    for (int k = 0; k < fp8::BLOCK / 32; ++k)              // K = 32 is 32 bytes along the swizzled row
+                        umma_f8(tmem + (u32)(buf * BN), x + 2ull * k, w + 2ull * k, L::IDESC, k > 0);
+                    umma_commit(empty + 8 * s);
+                    umma_commit(acc_full + 8 * buf);
+                    acc_ph ^= 1u << buf;
+                    buf ^= 1;
+                    if (++s == L::STAGES) { s = 0; ph ^= 1u; }
+                }
+            }
+            // nothing of this CTA may still run on the tensor cores when tensor memory is given back
+            umma_commit(drain);
+            const u64 t0 = pop_global_ns();
+            while (!mbar_try_wait(drain, 0u) && pop_global_ns() - t0 < WAIT_BUDGET_NS) {}
+        }
+    } else {
+        constexpr int HALF = BN / 2;
+        const int quarter = warp & 3, half = (warp - 2) >> 2, row = quarter * 32 + lane;
+        const u32 at = tmem + ((u32)(quarter * 32) << 16) + (u32)(half * HALF);
+        int buf = 0;
+        u32 acc_ph = 0;
+        bool ok = true;
+        for (int unit = first; unit < units && ok; unit += step) {
+            const int mt = unit % G.m_tiles, nt = unit / G.m_tiles, m = mt * BM + row, n0 = nt * BN + half * HALF;
+            const float* xs = G.A.xs + min(m, G.A.M - 1);
+            const float* ws = G.A.ws + (size_t)min(n0 / fp8::BLOCK, (G.A.N - 1) / fp8::BLOCK) * G.A.KB;
+            float2 acc[HALF / 2];
+#pragma unroll
+            for (int j = 0; j < HALF / 2; ++j) acc[j] = make_float2(0.f, 0.f);
+            // scales two blocks ahead: a trip to L2 is about a block's time
+            auto scale_at = [&](int kb) { return kb < kb1 ? __ldg(xs + (size_t)kb * G.A.M) * __ldg(ws + kb) : 0.f; };
+            float s0 = scale_at(kb0), s1 = scale_at(kb0 + 1);
+            for (int kb = kb0; kb < kb1; ++kb) {
+                const float s2 = scale_at(kb + 2);
+                ok = mbar_wait(acc_full + 8 * buf, (acc_ph >> buf) & 1u, gave_up, GAVE_UP_EPILOGUE);
+                ok = __all_sync(~0u, ok);
+                if (!ok) break;
+                tc_after();
+#pragma unroll
+                for (int p = 0; p < HALF / 32; ++p) {
+                    float v[32];
+                    tmem_ld32(at + (u32)(buf * BN + 32 * p), v);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) acc[16 * p + j] = __ffma2_rn(make_float2(v[2 * j], v[2 * j + 1]), make_float2(s0, s0), acc[16 * p + j]);
+                }
+                tc_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
+                acc_ph ^= 1u << buf;
+                buf ^= 1;
+                s0 = s1;
+                s1 = s2;
+            }
+            if (!ok) break;
+            if (S == 1) {
+#pragma unroll
+                for (int j = 0; j < HALF; j += 8) {
+                    float v[8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { v[2 * i] = acc[j / 2 + i].x; v[2 * i + 1] = acc[j / 2 + i].y; }
+                    write8<T>(G, m, n0 + j, v);
+                }
+            } else {                             // partial sums, by columns, where the stages were (all of them have been used)
+                float* part = reinterpret_cast<float*>(raw_smem + (tiles - smem_u32(raw_smem)));
+#pragma unroll
+                for (int j = 0; j < HALF / 2; ++j) {
+                    part[(half * HALF + 2 * j) * BM + row] = acc[j].x;
+                    part[(half * HALF + 2 * j + 1) * BM + row] = acc[j].y;
+                }
+            }
+        }
+    }
+    __syncwarp();
+    if (S > 1) {                                 // one tile a cluster; rank r finishes columns [r, r + 1) BN / S
+        cluster_sync();
+        if (warp >= 2) {
+            const int row = (warp & 3) * 32 + lane, half = (warp - 2) >> 2, cols = BN / S / 2;      // BN / S is a multiple of 16
+            const int c0 = rank * (BN / S) + half * cols, mt = first % G.m_tiles, nt = first / G.m_tiles;
+            for (int c = c0; c < c0 + cols; c += 8) {
+                float v[8] = {};
+                for (int r = 0; r < S; ++r)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] += remote(tiles + (u32)(((c + j) * BM + row) * 4), (u32)r);
+                write8<T>(G, mt * BM + row, nt * BN + c, v);
+            }
+        }
+        cluster_sync();                          // the others' shared memory stays until all have read it
+    }
+    tc_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::COLS) : "memory");
+    }
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encoder() {
+    static EncodeTiledFn fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) f = nullptr;
+        (void)cudaGetLastError();
+        return (EncodeTiledFn)f;
+    }();
+    return fn;
+}
+// codes [rows][K]; box = 128 bytes (the swizzle span) x `box_rows` rows; what is outside reads as zero
+int make_map(CUtensorMap* map, const void* codes, int rows, int K, int box_rows) {
+    EncodeTiledFn enc = encoder();
+    if (!enc) { pop_set_cuda_error(cudaErrorNotSupported, "cuTensorMapEncodeTiled is not available from this driver"); return POP_ERR_CUDA; }
+    const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)K};
+    const cuuint32_t box[2] = {(cuuint32_t)fp8::BLOCK, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+    if (enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(codes), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
+        pop_set_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled rejected the codes");
+        return POP_ERR_CUDA;
+    }
+    return POP_OK;
+}
+
+template <typename T, int BN> int launch(const fp8::LinearArgs& A, int S, int sms, cudaStream_t st) {
+    typedef Tile<BN> L;
+    CUtensorMap mx, mw;
+    int rc = make_map(&mx, A.x, A.M, A.K, BM);
+    if (rc == POP_OK) rc = make_map(&mw, A.w, A.N, A.K, BN);
+    if (rc != POP_OK) return rc;
+    static thread_local int ready = -1;
+    int device = 0;
+    POP_CUDA(cudaGetDevice(&device));
+    if (ready != device) {
+        POP_CUDA(cudaFuncSetAttribute(fp8_gemm_kernel<T, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM));
+        ready = device;
+    }
+    GemmArgs G = {A, (A.M + BM - 1) / BM, (A.N + BN - 1) / BN, 0};
+    G.wide = ((uintptr_t)A.y & 15u) == 0 && (A.y_stride * (long long)sizeof(T)) % 16 == 0;
+    if ((long long)G.m_tiles * G.n_tiles > 0x3fffffffll) return POP_ERR_UNSUPPORTED;
+    const int units = G.m_tiles * G.n_tiles;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(S > 1 ? units * S : (units < sms ? units : sms));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = L::SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2] = {kv::following()};
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = S;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = S > 1 ? 2 : 1;
+    POP_CUDA(cudaLaunchKernelEx(&cfg, fp8_gemm_kernel<T, BN>, mx, mw, G, S));
+    POP_LAUNCHED();
+    return POP_OK;
+}
+
+template <typename T> int choose(const fp8::LinearArgs& A, int sms, cudaStream_t st) {
+    const long long m_tiles = (A.M + BM - 1) / BM;
+    auto tiles = [&](int bn) { return m_tiles * ((A.N + bn - 1) / bn); };
+    if (tiles(256) >= sms) return launch<T, 256>(A, 1, sms, st);
+    int S = 1;                                   // CTAs to a tile: as many as fill the machine, each with two blocks at least
+    while (S < 8 && tiles(128) * (2 * S) <= sms && A.KB >= 4 * S) S *= 2;
+    return launch<T, 128>(A, S, sms, st);
+}
+
+}  // namespace
+
+int pop_launch_fp8_gemm(const fp8::LinearArgs& A, pop_dtype_t y_dtype, int sms, cudaStream_t st) {
+    return y_dtype == POP_BF16 ? choose<__nv_bfloat16>(A, sms, st) : choose<float>(A, sms, st);
+}
+
+extern "C" int pop_fp8_check(void* cuda_stream) {
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    u32 status = 0;
+    POP_CUDA(cudaMemcpyFromSymbolAsync(&status, fp8_status, sizeof(status), 0, cudaMemcpyDeviceToHost, st));
+    POP_CUDA(cudaStreamSynchronize(st));
+    if (status == 0) return POP_OK;
+    status = 0;
+    POP_CUDA(cudaMemcpyToSymbolAsync(fp8_status, &status, sizeof(status), 0, cudaMemcpyHostToDevice, st));
+    POP_CUDA(cudaStreamSynchronize(st));
+    return POP_ERR_TIMEOUT;
+}

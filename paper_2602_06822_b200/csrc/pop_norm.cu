@@ -1,0 +1,197 @@
+// Norms before and after a block, with its gate and the residual addition between them, in one pass:
+//
+//   b = u  or  rms(u) post_gain;   h' = h_scale h + u_scale gate b;   f = rms(h') gain;   rms(x) = x / sqrt(mean(x^2) + eps)
+//
+// Bound by memory: h and u are read, h' and f written, once each.  So a row is kept in registers from its first load to its
+// last store: one CTA a row, a thread has up to V vectors of 16 bytes of it, and the row's one or two sums go through
+// shared memory.  h is asked for together with u, so that the first sum's barrier costs no second trip to memory.
+#include "pop_fp8.cuh"
+
+namespace {
+
+struct NormArgs {
+    pop_block_norm_t a;
+    int T, d;
+};
+
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+    return x;
+}
+// The sum over the CTA's threads, the same in all of them; `part` is used by one sum only.
+__device__ __forceinline__ float cta_sum(float x, float* part) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    x = warp_sum(x);
+    if (lane == 0) part[warp] = x;
+    __syncthreads();
+    return warp_sum(lane < warps ? part[lane] : 0.f);
+}
+
+// E consecutive elements: a vector of 16 bytes, or (E = 1) one element.
+template <typename T, int E> struct Piece;
+template <> struct Piece<float, 4> {
+    typedef float4 raw;
+    __device__ static void open(const raw& r, float (&x)[4]) { x[0] = r.x; x[1] = r.y; x[2] = r.z; x[3] = r.w; }
+    __device__ static raw close(const float (&x)[4]) { return make_float4(x[0], x[1], x[2], x[3]); }
+};
+template <> struct Piece<__nv_bfloat16, 8> {
+    typedef uint4 raw;
+    __device__ static void open(const raw& r, float (&x)[8]) { Elem<__nv_bfloat16>::unpack(r, x); }
+    __device__ static raw close(const float (&x)[8]) {
+        __nv_bfloat162 r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        return *reinterpret_cast<const uint4*>(r);
+    }
+};
+template <typename T> struct Piece<T, 1> {
+    typedef T raw;
+    __device__ static void open(const raw& r, float (&x)[1]) { x[0] = Elem<T>::to_f32(r); }
+    __device__ static raw close(const float (&x)[1]) { return Elem<T>::from_f32(x[0]); }
+};
+
+template <typename T, int E, int V>
+__global__ void __launch_bounds__(1024) block_norm_kernel(const NormArgs N) {
+    typedef Piece<T, E> P;
+    typedef typename P::raw Raw;
+    __shared__ float part[2][32];
+    const pop_block_norm_t& a = N.a;
+    kv::follow();
+    const int row = blockIdx.x, pieces = N.d / E, step = blockDim.x;
+    const Raw* h = reinterpret_cast<const Raw*>((const T*)a.h + (long long)row * a.h_stride);
+    const Raw* u = reinterpret_cast<const Raw*>((const T*)a.u + (long long)row * a.u_stride);
+    const Raw* gate = reinterpret_cast<const Raw*>((const T*)a.gate + (long long)row * a.gate_stride);
+    Raw hr[V], ur[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int i = threadIdx.x + v * step;
+        if (i < pieces) {
+            hr[v] = h[i];
+            if (a.u) ur[v] = u[i];
+        }
+    }
+    float r = 1.f;
+    if (a.post_norm) {
+        float sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if ((int)threadIdx.x + v * step < pieces) {
+                float x[E];
+                P::open(ur[v], x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum = fmaf(x[e], x[e], sum);
+            }
+        r = rsqrtf(cta_sum(sum, part[0]) / (float)N.d + a.eps);
+    }
+    float x[V][E], sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int i = threadIdx.x + v * step;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[v][e] = 0.f;
+        if (i < pieces) {
+            P::open(hr[v], x[v]);
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[v][e] *= a.h_scale;
+            if (a.u) {
+                float b[E], m[E];
+                P::open(ur[v], b);
+                if (a.post_norm) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) b[e] *= r;
+                    if (a.post_gain) {
+                        P::open(reinterpret_cast<const Raw*>(a.post_gain)[i], m);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) b[e] *= m[e];
+                    }
+                }
+                if (a.gate) {
+                    P::open(gate[i], m);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) b[e] *= m[e];
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[v][e] = fmaf(a.u_scale, b[e], x[v][e]);
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum = fmaf(x[v][e], x[v][e], sum);
+        }
+    }
+    if (a.h_out) {
+        Raw* to = reinterpret_cast<Raw*>((T*)a.h_out + (long long)row * a.h_out_stride);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if ((int)threadIdx.x + v * step < pieces) to[threadIdx.x + v * step] = P::close(x[v]);
+    }
+    if (!a.f && !a.f_codes) return;
+    r = rsqrtf(cta_sum(sum, part[1]) / (float)N.d + a.eps);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int i = threadIdx.x + v * step;
+        const bool in = i < pieces;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[v][e] *= r;
+        if (in && a.gain) {
+            float m[E];
+            P::open(reinterpret_cast<const Raw*>(a.gain)[i], m);
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[v][e] *= m[e];
+        }
+        if (in && a.f) reinterpret_cast<Raw*>(a.f)[(size_t)row * pieces + i] = P::close(x[v]);
+        if constexpr (E >= 4) {
+            if (a.f_codes) {
+                u32 codes[E / 4];
+                const float scale = fp8::quantise_row(x[v], codes);        // (lanes past the row's end have zeros)
+                if (in) {
+                    u32* to = reinterpret_cast<u32*>((unsigned char*)a.f_codes + (size_t)row * N.d + (size_t)i * E);
+#pragma unroll
+                    for (int c = 0; c < E / 4; ++c) to[c] = codes[c];
+                    if (i % (128 / E) == 0) a.f_scales[(size_t)(i / (128 / E)) * N.T + row] = scale;
+                }
+            }
+        }
+    }
+}
+
+template <typename T, int E> cudaError_t launch_norm(const NormArgs& N, cudaStream_t st) {
+    const int pieces = N.d / E;
+    // one vector a thread while a CTA holds the row that way: the row's latency counts, and enough rows fill the machine anyhow
+    auto threads = [&](int v) { const int t = (pieces + v - 1) / v; return (t + 31) / 32 * 32; };
+    constexpr int MOST = E == 1 ? 32 : POP_NORM_MAX_D / 1024 / E;
+    if (threads(1) <= 1024) return kv::launch(block_norm_kernel<T, E, 1>, dim3(N.T), threads(1), st, N);
+    if (threads(2) <= 1024) return kv::launch(block_norm_kernel<T, E, 2>, dim3(N.T), threads(2), st, N);
+    if (threads(4) <= 1024) return kv::launch(block_norm_kernel<T, E, 4>, dim3(N.T), threads(4), st, N);
+    return kv::launch(block_norm_kernel<T, E, MOST>, dim3(N.T), threads(MOST), st, N);
+}
+
+}  // namespace
+
+extern "C" int pop_block_norm(const pop_block_norm_t* a, int n_tokens, int d, pop_dtype_t dtype, void* cuda_stream) {
+    if (!a || n_tokens < 0 || d <= 0) return POP_ERR_INVALID_ARG;
+    if (dtype != POP_F32 && dtype != POP_BF16) return POP_ERR_UNSUPPORTED;
+    if (d > POP_NORM_MAX_D) return POP_ERR_UNSUPPORTED;
+    if (!(a->eps >= 0.f) || !(a->h_scale == a->h_scale) || !(a->u_scale == a->u_scale)) return POP_ERR_INVALID_ARG;
+    if (n_tokens == 0) return POP_OK;                     // (and no pointers)
+    if (!a->u && (a->gate || a->post_norm || a->post_gain)) return POP_ERR_INVALID_ARG;
+    if (a->post_gain && !a->post_norm) return POP_ERR_INVALID_ARG;
+    if ((a->f_codes == nullptr) != (a->f_scales == nullptr)) return POP_ERR_INVALID_ARG;
+    if (!a->h_out && !a->f && !a->f_codes) return POP_ERR_INVALID_ARG;
+    const size_t es = dtype == POP_F32 ? 4 : 2;
+    if (!a->h || a->h_stride < d || (a->u && a->u_stride < d) || (a->h_out && a->h_out_stride < d)) return POP_ERR_INVALID_ARG;
+    if (a->gate && a->gate_stride != 0 && a->gate_stride < d) return POP_ERR_INVALID_ARG;
+    const uintptr_t any = (uintptr_t)a->h | (uintptr_t)a->u | (uintptr_t)a->post_gain | (uintptr_t)a->gate | (uintptr_t)a->gain | (uintptr_t)a->h_out |
+                          (uintptr_t)a->f;
+    if (any & (es - 1)) return POP_ERR_INVALID_ARG;
+    const long long strides = (long long)d | a->h_stride | (a->u ? a->u_stride : 0) | (a->h_out ? a->h_out_stride : 0) | (a->gate ? a->gate_stride : 0);
+    const bool vectors = (any & 15u) == 0 && (strides * (long long)es) % 16 == 0;
+    if (a->f_codes && (!vectors || d % 16 != 0 || ((uintptr_t)a->f_codes & 15u) != 0 || ((uintptr_t)a->f_scales & 3u) != 0)) return POP_ERR_UNSUPPORTED;
+    const NormArgs N = {*a, n_tokens, d};
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (dtype == POP_BF16)
+        POP_CUDA((vectors ? launch_norm<__nv_bfloat16, 8>(N, st) : launch_norm<__nv_bfloat16, 1>(N, st)));
+    else
+        POP_CUDA((vectors ? launch_norm<float, 4>(N, st) : launch_norm<float, 1>(N, st)));
+    POP_LAUNCHED();
+    return POP_OK;
+}

@@ -1,0 +1,292 @@
+// Rotary positions, alone and on the way into the paged 4-bit cache:
+//
+//   a' = a cos(p w_i) - b sin(p w_i),   b' = b cos(p w_i) + a sin(p w_i)      for pair i of a head, at position p
+//
+// Angles.  w_i / 2 pi is a 64-bit fraction of a turn, so p w_i modulo a turn is one integer product whose overflow drops the whole
+// turns: exact for any position, where a product in fp32 is off by 0.004 of a radian at position 65536.  Its cosine and sine are taken in 64 bits and
+// rounded to fp32, and every product and sum of the rotation is rounded by itself: what the 4-bit quantiser sees is then the same
+// whichever kernel, batch or machine rotated it, down to which code a value at a border gets.
+//
+// Bound by memory (rows are read and written once); the 64-bit cosines are shared by all heads of a token through shared memory.
+#include <math.h>
+
+#include "pop_kv_slots.cuh"
+
+namespace {
+
+constexpr int TABLE = 256;                       // (token, pair) angles of a CTA
+
+struct Angles {
+    const u64* freq;
+    const int32_t* positions;
+    int T, pairs;                                // pairs = rot_dim / 2
+    double magnitude;
+    int inverse;
+};
+
+// (cos, sin) of pair i at position p
+__device__ __forceinline__ float2 turn(const Angles& A, int p, int i) {
+    const u64 part = (u64)p * A.freq[i];                                     // of a turn, in 2^-64
+    double s, c;
+    sincospi((double)(long long)part * 0x1p-63, &s, &c);
+    return make_float2((float)(c * A.magnitude), (float)((A.inverse ? -s : s) * A.magnitude));
+}
+__device__ __forceinline__ void rotate(float& a, float& b, float2 cs) {
+    const float x = __fsub_rn(__fmul_rn(a, cs.x), __fmul_rn(b, cs.y)), y = __fadd_rn(__fmul_rn(b, cs.x), __fmul_rn(a, cs.y));
+    a = x;
+    b = y;
+}
+
+// ------------------------------------------------------------------------------------------------------------- alone
+//
+// An item is E pairs of a head: two vectors of E elements, which hold the pairs' first and second elements (halves of the rotated part) or,
+// interleaved, E / 2 whole pairs each; or one vector of the part that is not rotated, where it has to be copied.
+// E = 1 serves any size, stride and alignment.
+struct Rows {
+    const void* in;
+    void* out;
+    long long in_stride, out_stride;
+    int heads, copy;                             // copy: vectors of a head that are not rotated and go to another place
+};
+struct RopeArgs {
+    Angles A;
+    int D, tokens, interleaved;                  // tokens of a CTA
+    Rows x[2];                                   // q, k
+};
+
+template <typename T, int E> struct Vec { uint4 v; };
+template <typename T> struct Vec<T, 1> { T v; };
+template <typename T, int E> __device__ __forceinline__ void open(const Vec<T, E>& r, float (&x)[E]) {
+    if constexpr (E == 1) x[0] = Elem<T>::to_f32(r.v);
+    else Elem<T>::unpack(r.v, x);
+}
+__device__ __forceinline__ Vec<float, 4> close(const float (&x)[4]) {
+    return {make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]))};
+}
+__device__ __forceinline__ Vec<__nv_bfloat16, 8> close(const float (&x)[8]) {
+    __nv_bfloat162 r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    return {*reinterpret_cast<const uint4*>(r)};
+}
+template <typename T> __device__ __forceinline__ Vec<T, 1> close1(const float (&x)[1]) { return {Elem<T>::from_f32(x[0])}; }
+template <typename T, int E> __device__ __forceinline__ Vec<T, E> closed(const float (&x)[E]) {
+    if constexpr (E == 1) return close1<T>(x);
+    else return close(x);
+}
+
+template <typename T, int E> __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs R) {
+    typedef Vec<T, E> V;
+    __shared__ float2 table[TABLE];
+    kv::follow();
+    const Rows X = blockIdx.y % 2u ? R.x[1] : R.x[0];
+    const int t0 = blockIdx.x * R.tokens, n = min(R.tokens, R.A.T - t0), pairs = R.A.pairs, parts = gridDim.y / 2u, part = blockIdx.y / 2u;
+    if (X.heads == 0) return;
+    for (int i = threadIdx.x; i < n * pairs; i += 256) {
+        const int p = R.A.positions[t0 + i / pairs];
+        if (p >= 0) table[i] = turn(R.A, p, i % pairs);
+    }
+    __syncthreads();
+    const int turned = pairs / E, per_head = turned + X.copy, per_token = X.heads * per_head;
+    for (int i = part * 256 + threadIdx.x; i < n * per_token; i += 256 * parts) {
+        const int token = i / per_token, rest = i - token * per_token, head = rest / per_head, c = rest - head * per_head;
+        if (R.A.positions[t0 + token] < 0) continue;
+        const T* from = (const T*)X.in + (long long)(t0 + token) * X.in_stride + (long long)head * R.D;
+        T* to = (T*)X.out + (long long)(t0 + token) * X.out_stride + (long long)head * R.D;
+        if (c >= turned) {
+            const int at = 2 * pairs + (c - turned) * E;
+            *reinterpret_cast<V*>(to + at) = *reinterpret_cast<const V*>(from + at);
+            continue;
+        }
+        const int a0 = R.interleaved ? 2 * c * E : c * E, b0 = R.interleaved ? a0 + E : pairs + c * E;
+        float a[E], b[E];
+        open(*reinterpret_cast<const V*>(from + a0), a);
+        open(*reinterpret_cast<const V*>(from + b0), b);
+        const float2* cs = table + token * pairs + c * E;
+        if (E > 1 && R.interleaved) {
+#pragma unroll
+            for (int e = 0; e + 1 < E; e += 2) { rotate(a[e], a[e + 1], cs[e / 2]); rotate(b[e], b[e + 1], cs[E / 2 + e / 2]); }
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) rotate(a[e], b[e], cs[e]);
+        }
+        *reinterpret_cast<V*>(to + a0) = closed<T, E>(a);
+        *reinterpret_cast<V*>(to + b0) = closed<T, E>(b);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------- into the cache
+//
+// A thread has 8 dimensions of one token's query head, key or value; a group's 8 lanes quantise together.  The other elements of its pairs
+// are read once more from the row (which is in the cache by then).
+struct AppendArgs {
+    Angles A;
+    int interleaved, Hq;
+    const void *q, *k, *v;
+    void* q_out;
+    long long qs, qos, ks, vs;
+    kv::SlotArgs S;
+};
+
+template <typename T, int G> __global__ void __launch_bounds__(256) rope_append_few_kernel(const AppendArgs P) {
+    constexpr int D = 64 * G, WORDS = kv::tile_bytes(D) / 4, PIECES = 8 * G;
+    __shared__ float2 table[D / 2];
+    kv::follow();
+    const int t = blockIdx.x, pairs = P.A.pairs, p = P.A.positions[t];
+    if (p < 0) return;
+    for (int i = threadIdx.x; i < pairs; i += 256) table[i] = turn(P.A, p, i);
+    __syncthreads();
+    const int Hk = P.S.H, per_token = (P.Hq + 2 * Hk) * PIECES;
+    const long long slot = P.S.slots[t];
+    const bool kept = slot >= 0 && slot < P.S.n_slots;
+    for (int i0 = blockIdx.y * 256; i0 < per_token; i0 += gridDim.y * 256) {
+        const int i = i0 + threadIdx.x;
+        const bool in = i < per_token;
+        const int head = in ? i / PIECES : 0, c = i % PIECES;
+        const int kind = head < P.Hq ? 0 : head < P.Hq + Hk ? 1 : 2, h = kind == 0 ? head : kind == 1 ? head - P.Hq : head - P.Hq - Hk;
+        const T* row = (kind == 0 ? (const T*)P.q + (long long)t * P.qs : kind == 1 ? (const T*)P.k + (long long)t * P.ks : (const T*)P.v + (long long)t * P.vs) + (size_t)h * D;
+        kv::Raw8<float> x[1] = {kv::no_raw<float>()};
+        float v[8] = {};
+        if (in) kv::values_of(kv::load_raw(row + 8 * c), v);
+        if (in && kind < 2 && 8 * c < 2 * pairs) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int j = 8 * c + e;
+                if (j >= 2 * pairs) continue;
+                const bool second = P.interleaved ? j & 1 : j >= pairs;
+                const int pair = P.interleaved ? j >> 1 : second ? j - pairs : j, mate = P.interleaved ? j ^ 1 : second ? j - pairs : j + pairs;
+                const float o = Elem<T>::to_f32(row[mate]);
+                float a = second ? o : v[e], b = second ? v[e] : o;
+                rotate(a, b, table[pair]);
+                v[e] = second ? b : a;
+            }
+        }
+        if (in && kind == 0) kv::put8((T*)P.q_out + (long long)t * P.qos + (size_t)h * D + 8 * c, v);
+        x[0].v[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        x[0].v[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+        u32 params, word[1];
+        kv::quantise(x, word, params);
+        if (!in || kind == 0 || !kept) continue;
+        u32* to = P.S.pages + kv::tile_base(P.S, slot, h, WORDS);
+        const int g = c / 8, e8 = c % 8, value = kind - 1;
+        to[kv::word_at<G>((int)slot & 15, value, g, e8)] = word[0];
+        if (e8 == 0) to[kv::param_at<G>((int)slot & 15, value, g)] = params;
+    }
+}
+
+int check_rope(const pop_rope_t* r, int head_dim) {
+    if (!r || !r->freq || r->rot_dim <= 0 || r->rot_dim % 2 != 0 || head_dim <= 0 || head_dim % 2 != 0 || r->rot_dim > head_dim) return POP_ERR_INVALID_ARG;
+    if (((uintptr_t)r->freq & 7u) != 0 || !(r->magnitude == r->magnitude)) return POP_ERR_INVALID_ARG;
+    return head_dim <= POP_ROPE_MAX_DIM ? POP_OK : POP_ERR_UNSUPPORTED;
+}
+
+template <typename T> cudaError_t rope(RopeArgs R, bool vectors, cudaStream_t st) {
+    const int E = vectors ? 16 / (int)sizeof(T) : 1;
+    long long items = 0;
+    for (int i = 0; i < 2; ++i) {
+        R.x[i].copy = R.x[i].in == R.x[i].out ? 0 : (R.D - 2 * R.A.pairs) / E;
+        const long long n = (long long)R.x[i].heads * (R.A.pairs / E + R.x[i].copy);
+        items = n > items ? n : items;
+    }
+    R.tokens = TABLE / R.A.pairs;
+    if (R.tokens > 1 && (R.A.T + R.tokens - 1) / R.tokens < 1024) R.tokens = 1;      // few tokens: a CTA for each
+    const long long parts = (items * R.tokens + 1023) / 1024;                         // some four items a thread
+    const dim3 grid((R.A.T + R.tokens - 1) / R.tokens, 2 * (u32)(parts < 1 ? 1 : parts > 16 ? 16 : parts));
+    return vectors ? kv::launch(rope_kernel<T, 16 / (int)sizeof(T)>, grid, 256, st, R) : kv::launch(rope_kernel<T, 1>, grid, 256, st, R);
+}
+
+template <typename T, int G> cudaError_t append(const AppendArgs& P, cudaStream_t st) {
+    const int items = (P.Hq + 2 * P.S.H) * 8 * G, parts = P.A.T >= 512 ? 1 : (items + 255) / 256;
+    return kv::launch(rope_append_few_kernel<T, G>, dim3(P.A.T, parts < 65535 ? parts : 65535), 256, st, P);
+}
+
+}  // namespace
+
+extern "C" int pop_rope_frequencies(const pop_rope_params_t* p, uint64_t* h_freq, double* magnitude) {
+    if (!p || !h_freq || !magnitude || p->rot_dim <= 0 || p->rot_dim % 2 != 0 || !(p->base > 1.0) || !(p->base < 1e30)) return POP_ERR_INVALID_ARG;
+    if (p->scaling < POP_ROPE_NONE || p->scaling > POP_ROPE_BANDS) return POP_ERR_INVALID_ARG;
+    const bool scaled = p->scaling != POP_ROPE_NONE, parts = p->scaling == POP_ROPE_YARN || p->scaling == POP_ROPE_BANDS;
+    if (scaled && !(p->factor >= 1.0 && p->factor < 1e9)) return POP_ERR_INVALID_ARG;
+    const long double fast = p->beta_fast != 0.0 ? p->beta_fast : p->scaling == POP_ROPE_YARN ? 32.0 : 4.0, slow = p->beta_slow != 0.0 ? p->beta_slow : 1.0;
+    if (parts && !(p->original_positions >= 1.0 && p->original_positions < 1e12 && slow > 0.0L && fast > slow)) return POP_ERR_INVALID_ARG;
+    if (p->scaling == POP_ROPE_NTK && p->rot_dim <= 2) return POP_ERR_INVALID_ARG;
+    const int r = p->rot_dim;
+    const long double tau = 6.283185307179586476925286766559L, factor = scaled ? p->factor : 1.0;
+    const long double base = p->scaling == POP_ROPE_NTK ? p->base * powl(factor, (long double)r / (r - 2)) : p->base;
+    // YARN: the (fractional) index of the pair that turns `t` times within the original positions
+    auto index_of = [&](long double t) { return r * logl(p->original_positions / (t * tau)) / (2 * logl(base)); };
+    const long double lo = parts ? fmaxl(floorl(index_of(fast)), 0) : 0, hi = parts ? fminl(ceill(index_of(slow)), r - 1) : 0;
+    for (int i = 0; i < r / 2; ++i) {
+        long double w = powl(base, -2.0L * i / r), keep = 1;
+        if (p->scaling == POP_ROPE_LINEAR) keep = 0;
+        if (p->scaling == POP_ROPE_YARN) keep = 1 - fminl(fmaxl((i - lo) / fmaxl(hi - lo, 1e-3L), 0), 1);
+        if (p->scaling == POP_ROPE_BANDS) keep = fminl(fmaxl((p->original_positions * w / tau - slow) / (fast - slow), 0), 1);
+        w = w * keep + w / factor * (1 - keep);
+        h_freq[i] = (uint64_t)rintl(w / tau * 18446744073709551616.0L);          // (w <= 1: less than a sixth of a turn)
+    }
+    *magnitude = p->scaling == POP_ROPE_YARN ? (double)(0.1L * logl(factor) + 1) : 1.0;
+    return POP_OK;
+}
+
+extern "C" int pop_rope(const pop_rope_t* rope_, int inverse, const int32_t* positions, int n_tokens, int head_dim, pop_dtype_t dtype,
+                        const void* q, long long q_stride, int q_heads, void* q_out, long long q_out_stride,
+                        const void* k, long long k_stride, int k_heads, void* k_out, long long k_out_stride, void* cuda_stream) {
+    int rc = check_rope(rope_, head_dim);
+    if (rc != POP_OK) return rc;
+    if (dtype != POP_F32 && dtype != POP_BF16) return POP_ERR_UNSUPPORTED;
+    if (n_tokens < 0 || q_heads <= 0 || (k && k_heads <= 0)) return POP_ERR_INVALID_ARG;
+    if (n_tokens == 0) return POP_OK;
+    if (!positions || !q || !q_out || (k && !k_out)) return POP_ERR_INVALID_ARG;
+    if ((long long)q_heads * head_dim > (1 << 24) || (k && (long long)k_heads * head_dim > (1 << 24))) return POP_ERR_UNSUPPORTED;
+    const int es = dtype == POP_F32 ? 4 : 2, E = 16 / es;
+    const long long row_q = (long long)q_heads * head_dim, row_k = (long long)k_heads * head_dim;
+    if (q_stride < row_q || q_out_stride < row_q || (k && (k_stride < row_k || k_out_stride < row_k))) return POP_ERR_INVALID_ARG;
+    if ((q == q_out && q_stride != q_out_stride) || (k && k == k_out && k_stride != k_out_stride)) return POP_ERR_INVALID_ARG;
+    uintptr_t at = (uintptr_t)q | (uintptr_t)q_out;
+    long long sizes = head_dim | q_stride | q_out_stride;
+    if (k) { at |= (uintptr_t)k | (uintptr_t)k_out; sizes |= k_stride | k_out_stride; }
+    if (at & (es - 1)) return POP_ERR_INVALID_ARG;
+    const bool vectors = (at & 15u) == 0 && sizes % E == 0 && rope_->rot_dim % (2 * E) == 0;
+    RopeArgs R = {};
+    R.A = {(const u64*)rope_->freq, positions, n_tokens, rope_->rot_dim / 2, rope_->magnitude, inverse != 0};
+    R.D = head_dim;
+    R.interleaved = rope_->interleaved != 0;
+    R.x[0] = {q, q_out, q_stride, q_out_stride, q_heads, 0};
+    if (k) R.x[1] = {k, k_out, k_stride, k_out_stride, k_heads, 0};
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    POP_CUDA((dtype == POP_BF16 ? rope<__nv_bfloat16>(R, vectors, st) : rope<float>(R, vectors, st)));
+    POP_LAUNCHED();
+    return POP_OK;
+}
+
+extern "C" int pop_kv_append_rope(const pop_kv_cache_t* c, const pop_rope_t* rope_, const int32_t* positions, const void* q, long long q_stride, int n_heads,
+                                  void* q_out, long long q_out_stride, const void* k, long long k_stride, const void* v, long long v_stride,
+                                  pop_dtype_t dtype, const int64_t* slots, int n_tokens, void* cuda_stream) {
+    int rc = kv::check_cache(c);
+    if (rc == POP_OK) rc = check_rope(rope_, c->head_dim);
+    if (rc != POP_OK) return rc;
+    if (n_tokens < 0 || n_heads <= 0) return POP_ERR_INVALID_ARG;
+    if (n_tokens == 0) return POP_OK;
+    if (!positions || !slots) return POP_ERR_INVALID_ARG;
+    if ((long long)(n_heads + 2ll * c->n_kv_heads) * c->head_dim > (1 << 24)) return POP_ERR_UNSUPPORTED;
+    rc = kv::check_rows(q, q_stride, n_heads, c->head_dim, dtype);
+    if (rc == POP_OK) rc = kv::check_rows(q_out, q_out_stride, n_heads, c->head_dim, dtype);
+    if (rc == POP_OK) rc = kv::check_rows(k, k_stride, c->n_kv_heads, c->head_dim, dtype);
+    if (rc == POP_OK) rc = kv::check_rows(v, v_stride, c->n_kv_heads, c->head_dim, dtype);
+    if (rc != POP_OK) return rc;
+    if (q == q_out) return POP_ERR_INVALID_ARG;            // (a thread reads its pairs' other elements from the row)
+    AppendArgs P = {};
+    P.A = {(const u64*)rope_->freq, positions, n_tokens, rope_->rot_dim / 2, rope_->magnitude, 0};
+    P.interleaved = rope_->interleaved != 0;
+    P.Hq = n_heads;
+    P.q = q; P.k = k; P.v = v; P.q_out = q_out;
+    P.qs = q_stride; P.qos = q_out_stride; P.ks = k_stride; P.vs = v_stride;
+    P.S = {(u32*)c->pages, c->page_size, c->n_kv_heads, n_tokens, (long long)c->n_pages * c->page_size, slots};
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (dtype == POP_BF16)
+        POP_CUDA((c->head_dim == 64 ? append<__nv_bfloat16, 1>(P, st) : append<__nv_bfloat16, 2>(P, st)));
+    else
+        POP_CUDA((c->head_dim == 64 ? append<float, 1>(P, st) : append<float, 2>(P, st)));
+    POP_LAUNCHED();
+    return POP_OK;
+}

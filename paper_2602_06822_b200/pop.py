@@ -22,6 +22,8 @@ POP_MAX_BATCH = 8
 POP_F32, POP_BF16 = 0, 1
 POP_NOALLOC_MAX_N = 32768
 POP_KV_TILE, POP_KV_GROUP, POP_KV_MAX_REQUESTS = 16, 64, 4096
+POP_NORM_MAX_D, POP_FP8_BLOCK, POP_ROPE_MAX_DIM = 32768, 128, 512
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libpop.so")
 
@@ -38,6 +40,24 @@ class Config(C.Structure):
 class KVCacheDesc(C.Structure):
     """pop_kv_cache_t"""
     _fields_ = [("pages", C.c_void_p), ("n_pages", C.c_int), ("page_size", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int)]
+
+
+class BlockNormArgs(C.Structure):
+    """pop_block_norm_t"""
+    _fields_ = ([(n, C.c_void_p) for n in ("h", "u", "post_gain", "gate", "gain")] + [(n, C.c_longlong) for n in ("h_stride", "u_stride", "gate_stride")]
+                + [(n, C.c_void_p) for n in ("h_out", "f", "f_codes", "f_scales")] + [("h_out_stride", C.c_longlong)]
+                + [(n, C.c_float) for n in ("h_scale", "u_scale", "eps")] + [("post_norm", C.c_int)])
+
+
+class RopeParams(C.Structure):
+    """pop_rope_params_t"""
+    _fields_ = [("rot_dim", C.c_int), ("base", C.c_double), ("scaling", C.c_int)] + [(n, C.c_double) for n in
+                ("factor", "original_positions", "beta_fast", "beta_slow")]
+
+
+class RopeDesc(C.Structure):
+    """pop_rope_t"""
+    _fields_ = [("freq", C.c_void_p), ("rot_dim", C.c_int), ("interleaved", C.c_int), ("magnitude", C.c_double)]
 
 
 POP_DECODE_AUTO, POP_DECODE_FUSED, POP_DECODE_SIMPLE = 0, 1, 2
@@ -93,6 +113,16 @@ SIGNATURES = {
     "pop_kv_attention_check": (C.c_int, [_P, _P]),
     "pop_kv_attention": (C.c_int, [C.POINTER(KVCacheDesc), _P, C.c_longlong, C.c_int, C.c_int, C.c_int, _P, _P, C.c_int, _P, C.c_int,
                                    C.c_float, C.c_int, C.c_int, _P, _P, _P, C.c_size_t, _P]),
+    "pop_block_norm": (C.c_int, [C.POINTER(BlockNormArgs), C.c_int, C.c_int, C.c_int, _P]),
+    "pop_fp8_quantize": (C.c_int, [_P, C.c_longlong, C.c_int, C.c_int, C.c_int, C.c_int, _P, _P, _P]),
+    "pop_fp8_linear": (C.c_int, [_P, _P, C.c_int, _P, _P, C.c_int, C.c_int, _P, C.c_longlong, C.c_int, _P]),
+    "pop_fp8_linear_workspace": (C.c_int, [C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
+    "pop_fp8_linear_rows": (C.c_int, [_P, C.c_longlong, C.c_int, C.c_int, _P, _P, C.c_int, C.c_int, _P, C.c_longlong, C.c_int, _P, C.c_size_t, _P]),
+    "pop_fp8_check": (C.c_int, [_P]),
+    "pop_rope_frequencies": (C.c_int, [C.POINTER(RopeParams), _P, C.POINTER(C.c_double)]),
+    "pop_rope": (C.c_int, [C.POINTER(RopeDesc), C.c_int, _P, C.c_int, C.c_int, C.c_int] + [_P, C.c_longlong, C.c_int, _P, C.c_longlong] * 2 + [_P]),
+    "pop_kv_append_rope": (C.c_int, [C.POINTER(KVCacheDesc), C.POINTER(RopeDesc), _P, _P, C.c_longlong, C.c_int, _P, C.c_longlong, _P, C.c_longlong,
+                                     _P, C.c_longlong, C.c_int, _P, C.c_int, _P]),
 }
 
 
@@ -664,6 +694,10 @@ class KVCache:
     def append(self, layer: int, k, v):
         kv_append(self.pages[layer], k, v, self.step.slots)
 
+    def append_rope(self, layer: int, rope: "Rope", q, k, v, q_out=None):
+        """Rotates q and k to the step's positions; k and v go to the cache, the rotated q comes back (kv_append_rope)."""
+        return kv_append_rope(self.pages[layer], rope, self.step.positions, q, k, v, self.step.slots, q_out)
+
     def attend(self, layer: int, q, **kw):
         kw.setdefault("workspace", self.workspace)
         return kv_attention(self.pages[layer], q, self.block_table, self.step.q_indptr, self.step.kv_lens, **kw)
@@ -672,3 +706,261 @@ class KVCache:
         """Synchronises the current stream; raises PopError if a wait of one of the cache's attention calls up to here ran out since the last check,
         whichever stream or graph it ran in."""
         kv_attention_check(workspace=self.workspace)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# What a decoder layer does around its attention: norms, the 8-bit product, rotary positions.  The tensors of a call have to be on the
+# current device.
+# ---------------------------------------------------------------------------------------------------------------------
+
+def _inference_only(what, *tensors):
+    """These calls have no backward pass: a gradient must not end here unnoticed."""
+    for t in tensors:
+        if t is not None and t.requires_grad and _torch().is_grad_enabled():
+            raise ValueError(f"{what} has no backward pass: detach() what requires a gradient, or call under torch.no_grad()")
+
+
+def _matrix(t, what: str, d: Optional[int] = None) -> int:
+    """Row stride (in elements) of [rows, d] whose rows are contiguous."""
+    if t.dim() != 2 or t.shape[1] == 0 or (d is not None and t.shape[1] != d):
+        raise ValueError(f"{what} must be [rows, {'d' if d is None else d}]")
+    if t.shape[0] and t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: the elements of a row must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _same_type(dtype, *tensors):
+    for t in tensors:
+        if t is not None and t.dtype != dtype:
+            raise TypeError("dtype mismatch")
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+class Fp8Rows(NamedTuple):
+    """Activations in 8 bits: a scale for every 128 elements of a row."""
+    codes: object         # float8_e4m3fn [rows, K]
+    scales: object        # float32 [ceil(K / 128), rows]
+
+
+class Fp8Weights(NamedTuple):
+    """A weight matrix in 8 bits: a scale for every 128 x 128 elements."""
+    codes: object         # float8_e4m3fn [N, K]
+    scales: object        # float32 [ceil(N / 128), ceil(K / 128)]
+
+
+def _fp8_blocks(n: int) -> int:
+    return -(-n // POP_FP8_BLOCK)
+
+
+def _check_fp8(codes, scales, shape, what: str):
+    torch = _torch()
+    if codes.dtype != torch.float8_e4m3fn or codes.dim() != 2 or not codes.is_contiguous():
+        raise ValueError(f"{what}: codes must be a contiguous float8_e4m3fn matrix")
+    if scales.dtype != torch.float32 or tuple(scales.shape) != shape or not scales.is_contiguous():
+        raise ValueError(f"{what}: scales must be a contiguous float32 tensor {list(shape)}")
+
+
+def _fp8_quantize(x, block_rows: int, shape, stream):
+    torch = _torch()
+    stride = _matrix(x, "x")
+    _on_current_device(stream, x)
+    _inference_only("fp8_quantize", x)
+    rows, K = x.shape
+    codes = torch.empty(rows, K, dtype=torch.float8_e4m3fn, device=x.device)
+    scales = torch.empty(shape, dtype=torch.float32, device=x.device)
+    _check(lib().pop_fp8_quantize(x.data_ptr(), stride, rows, K, _dtype_code(x), block_rows, codes.data_ptr(), scales.data_ptr(), _stream_ptr(stream)),
+           "pop_fp8_quantize")
+    _used_on(stream, codes, scales)
+    return codes, scales
+
+
+def fp8_quantize(x, stream=None) -> Fp8Rows:
+    """pop_fp8_quantize of activations x [rows, K] (rows may be strided; K a multiple of 16)."""
+    return Fp8Rows(*_fp8_quantize(x, 1, (_fp8_blocks(x.shape[-1]), x.shape[0]), stream))
+
+
+def fp8_weights(w, stream=None) -> Fp8Weights:
+    """pop_fp8_quantize of a weight matrix w [N, K], once: the codes are a copy, w is not needed any more."""
+    return Fp8Weights(*_fp8_quantize(w, POP_FP8_BLOCK, (_fp8_blocks(w.shape[0]), _fp8_blocks(w.shape[-1])), stream))
+
+
+def fp8_linear(x, w: Fp8Weights, out=None, dtype=None, stream=None):
+    """pop_fp8_linear: x [M, K] (bf16 or fp32, quantised on the way, or Fp8Rows) times w^T -> [M, N] of ``dtype`` (x's own by default, bfloat16
+    for Fp8Rows).  ``out``: rows may be strided."""
+    torch = _torch()
+    wc, ws = w
+    _check_fp8(wc, ws, (_fp8_blocks(wc.shape[0]), _fp8_blocks(wc.shape[-1])), "w")
+    N, K = wc.shape
+    rows = isinstance(x, Fp8Rows)
+    xc = x.codes if rows else x
+    if rows:
+        _check_fp8(xc, x.scales, (_fp8_blocks(K), xc.shape[0]), "x")
+    stride = _matrix(xc, "x", K)
+    M = xc.shape[0]
+    made = out is None
+    if made:
+        out = torch.empty(M, N, dtype=dtype if dtype is not None else torch.bfloat16 if rows else x.dtype, device=xc.device)
+    elif tuple(out.shape) != (M, N) or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"out must be [{M}, {N}] of the dtype asked for")
+    y_stride = _matrix(out, "out", N)
+    _on_current_device(stream, xc, wc, ws, out, x.scales if rows else None)
+    _inference_only("fp8_linear", xc, out)
+    l, st = lib(), _stream_ptr(stream)
+    if rows:
+        _check(l.pop_fp8_linear(xc.data_ptr(), x.scales.data_ptr(), M, wc.data_ptr(), ws.data_ptr(), N, K, out.data_ptr(), y_stride, _dtype_code(out), st),
+               "pop_fp8_linear")
+        if made:
+            _used_on(stream, out)
+        return out
+    need = C.c_size_t()
+    _check(l.pop_fp8_linear_workspace(M, K, C.byref(need)), "pop_fp8_linear_workspace")
+    workspace = torch.empty(need.value, dtype=torch.uint8, device=xc.device)
+    _check(l.pop_fp8_linear_rows(x.data_ptr(), stride, _dtype_code(x), M, wc.data_ptr(), ws.data_ptr(), N, K, out.data_ptr(), y_stride, _dtype_code(out),
+                                 workspace.data_ptr(), need.value, st), "pop_fp8_linear_rows")
+    _used_on(stream, workspace, out if made else None)
+    return out
+
+
+def fp8_check(stream=None):
+    """pop_fp8_check: synchronises, raises PopError if a wait of an fp8_linear call on the current device ran out since the last check."""
+    _check(lib().pop_fp8_check(_stream_ptr(stream)), "pop_fp8_check")
+
+
+def block_norm(h, u=None, *, post_norm: bool = False, post_gain=None, gate=None, h_scale: float = 1.0, u_scale: float = 1.0, gain=None,
+               eps: float = 1e-5, fp8: bool = False, h_out=None, stream=None):
+    """pop_block_norm: (h', f) with h' = h_scale h + u_scale gate b, b = u or rms(u) post_gain, f = rms(h') gain.
+    h, u [T, d] (rows may be strided); post_gain, gain [d]; gate [T, d], [1, d] or [d].  ``fp8``: f as Fp8Rows.  ``h_out`` receives h' (h itself, or
+    another tensor; a new one by default).  Without u (and h_scale 1) h' is h, and nothing is written."""
+    torch = _torch()
+    a = BlockNormArgs()
+    a.h_stride = _matrix(h, "h")
+    T, d = h.shape
+    if u is not None:
+        if u.shape != h.shape:
+            raise ValueError("u must have h's shape")
+        a.u_stride = _matrix(u, "u")
+    if gate is not None:
+        if gate.dim() == 1:
+            gate = gate.unsqueeze(0)
+        if gate.dim() != 2 or gate.shape[1] != d or gate.shape[0] not in (1, T):
+            raise ValueError("gate must be [T, d], [1, d] or [d]")
+        a.gate_stride = _matrix(gate, "gate") if gate.shape[0] == T and T > 1 else 0
+        if a.gate_stride == 0 and gate.stride(1) != 1 and d > 1:
+            raise ValueError("gate: the elements of a row must be contiguous")
+    for t in (post_gain, gain):
+        if t is not None and (tuple(t.shape) != (d,) or (d > 1 and t.stride(0) != 1)):
+            raise ValueError("gains must be contiguous tensors [d]")
+    _same_type(h.dtype, u, post_gain, gate, gain, h_out)
+    dt = _dtype_code(h)
+    made = h_out is None
+    if made:
+        h_out = h if u is None and h_scale == 1.0 else torch.empty(T, d, dtype=h.dtype, device=h.device)
+    elif h_out.shape != h.shape:
+        raise ValueError("h_out must have h's shape")
+    if h_out is not h or u is not None or h_scale != 1.0:
+        a.h_out_stride = _matrix(h_out, "h_out")
+        a.h_out = h_out.data_ptr()
+    if fp8:
+        f = Fp8Rows(torch.empty(T, d, dtype=torch.float8_e4m3fn, device=h.device), torch.empty(_fp8_blocks(d), T, dtype=torch.float32, device=h.device))
+        a.f_codes, a.f_scales = f.codes.data_ptr(), f.scales.data_ptr()
+    else:
+        f = torch.empty(T, d, dtype=h.dtype, device=h.device)
+        a.f = f.data_ptr()
+    _on_current_device(stream, h, u, post_gain, gate, gain, h_out)
+    _inference_only("block_norm", h, u, post_gain, gate, gain, h_out)
+    a.h, a.u, a.post_gain, a.gate, a.gain = _ptr(h), _ptr(u), _ptr(post_gain), _ptr(gate), _ptr(gain)
+    a.h_scale, a.u_scale, a.eps, a.post_norm = h_scale, u_scale, eps, bool(post_norm)
+    _check(lib().pop_block_norm(C.byref(a), T, d, dt, _stream_ptr(stream)), "pop_block_norm")
+    _used_on(stream, *(f if fp8 else (f,)), h_out if made and h_out is not h else None)
+    return h_out, f
+
+
+class Rope:
+    """Rotary positions of the first ``rot_dim`` dimensions of a head: pairs (i, i + rot_dim / 2), or neighbours if ``interleaved``.  ``scaling``:
+    "none", "linear", "ntk", "yarn" or "bands" (see pop_rope_frequencies), for contexts ``factor`` times ``original_positions``.  Keeps the table of
+    frequencies on ``device``."""
+
+    def __init__(self, rot_dim: int, base: float = 10000.0, interleaved: bool = False, scaling: str = "none", factor: float = 1.0,
+                 original_positions: float = 4096, beta_fast: float = 0.0, beta_slow: float = 0.0, device="cuda"):
+        if scaling not in ROPE_SCALINGS:
+            raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}")
+        freq, magnitude = rope_frequencies(rot_dim, base, scaling, factor, original_positions, beta_fast, beta_slow)
+        self.rot_dim, self.interleaved, self.magnitude = rot_dim, bool(interleaved), magnitude
+        self.freq = _torch().from_numpy(freq.view(np.int64)).to(device)
+        self.desc = RopeDesc(self.freq.data_ptr(), rot_dim, int(self.interleaved), magnitude)
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_positions: float = 4096,
+                     beta_fast: float = 0.0, beta_slow: float = 0.0) -> Tuple[np.ndarray, float]:
+    """pop_rope_frequencies: (uint64 [rot_dim / 2], turns per position in units of 2^-64; magnitude) - host only."""
+    freq, magnitude = np.zeros(max(1, rot_dim // 2), dtype=np.uint64), C.c_double()
+    params = RopeParams(rot_dim, base, ROPE_SCALINGS[scaling], factor, original_positions, beta_fast, beta_slow)
+    _check(lib().pop_rope_frequencies(C.byref(params), freq.ctypes.data, C.byref(magnitude)), "pop_rope_frequencies")
+    return freq, magnitude.value
+
+
+def _rope_rows(t, dim: int, what: str):
+    if t.dim() != 3 or t.shape[1] == 0:
+        raise ValueError(f"{what} must be [tokens, heads, {dim}]")
+    return _rows(t, t.shape[1], dim, what)
+
+
+def rope(rope: Rope, positions, q, k=None, inverse: bool = False, q_out=None, k_out=None, stream=None):
+    """pop_rope: q (and k) [T, heads, head_dim] turned to their positions (int32 [T]; rows of negative ones are left out): new tensors, or ``q_out`` /
+    ``k_out``, which may be q and k themselves.  Returns q_out, or (q_out, k_out)."""
+    torch = _torch()
+    dim = q.shape[-1]
+    qs = _rope_rows(q, dim, "q")
+    T = q.shape[0]
+    _ints(positions, torch.int32, "positions")
+    if positions.shape[0] != T or (k is not None and k.shape[0] != T):
+        raise ValueError("q, k and positions must have one length")
+    made = (q_out is None, k is not None and k_out is None)
+    if made[0]:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if made[1]:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    if q_out.shape != q.shape or (k is not None and k_out.shape != k.shape) or (k is None and k_out is not None):
+        raise ValueError("outputs must have the shapes of q and k")
+    qos = _rope_rows(q_out, dim, "q_out")
+    ks = kos = 0
+    if k is not None:
+        ks, kos = _rope_rows(k, dim, "k"), _rope_rows(k_out, dim, "k_out")
+    _same_type(q.dtype, k, q_out, k_out)
+    _on_current_device(stream, rope.freq, positions, q, k, q_out, k_out)
+    _inference_only("rope", q, k, q_out, k_out)
+    _check(lib().pop_rope(C.byref(rope.desc), int(inverse), positions.data_ptr(), T, dim, _dtype_code(q), q.data_ptr(), qs, q.shape[1], q_out.data_ptr(), qos,
+                          _ptr(k), ks, 0 if k is None else k.shape[1], _ptr(k_out), kos, _stream_ptr(stream)), "pop_rope")
+    _used_on(stream, q_out if made[0] else None, k_out if made[1] else None)
+    return q_out if k is None else (q_out, k_out)
+
+
+def kv_append_rope(pages, rope: Rope, positions, q, k, v, slots, q_out=None, stream=None):
+    """pop_kv_append_rope: q [T, heads, head_dim] and k [T, n_kv_heads, head_dim] turned to their positions; k and v quantised into the slots (int64 [T])
+    of the 4-bit cache, the turned q returned.  Token rows may be strided."""
+    torch = _torch()
+    desc = _kv_desc(pages)
+    H, D = desc.n_kv_heads, desc.head_dim
+    qs, ks, vs = _rope_rows(q, D, "q"), _rows(k, H, D, "k"), _rows(v, H, D, "v")
+    T = q.shape[0]
+    _ints(slots, torch.int64, "slots")
+    _ints(positions, torch.int32, "positions")
+    if k.shape[0] != T or v.shape[0] != T or slots.shape[0] != T or positions.shape[0] != T:
+        raise ValueError("q, k, v, positions and slots must have one length")
+    made = q_out is None
+    if made:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif q_out.shape != q.shape:
+        raise ValueError("q_out must have q's shape")
+    qos = _rope_rows(q_out, D, "q_out")
+    _same_type(q.dtype, k, v, q_out)
+    _on_current_device(stream, pages, rope.freq, positions, q, k, v, slots, q_out)
+    _inference_only("kv_append_rope", q, k, v, q_out)
+    _check(lib().pop_kv_append_rope(C.byref(desc), C.byref(rope.desc), positions.data_ptr(), q.data_ptr(), qs, q.shape[1], q_out.data_ptr(), qos,
+                                    k.data_ptr(), ks, v.data_ptr(), vs, _dtype_code(q), slots.data_ptr(), T, _stream_ptr(stream)), "pop_kv_append_rope")
+    if made:
+        _used_on(stream, q_out)
+    return q_out

@@ -1,0 +1,568 @@
+"""Norms around a block, the 8-bit product and rotary positions (pop_block_norm, pop_fp8_quantize, pop_fp8_linear, pop_rope,
+pop_kv_append_rope) against the numpy oracle.
+
+Tolerances, derived before the first run (u = 2^-24, half a step of fp32; H = half a step of the result's type, 2^-8 of it for bf16, 2^-24 for fp32).
+  norm   a sum of d squares is taken in chains of at most 64 additions and 10 levels of tree: 80 u of it, half of that in the root; with the division, the
+         root (2 steps) and up to four products a term of h' errs by 50 u of its magnitude:  e' = 50 u (|h_scale h| + |u_scale gate b|), and h' by e' + H |h'|.
+         f adds the same again for its own root and product, and what e' does to its mean:  ef = |f| (60 u + |e'|_2 / |h'|_2) + e' |f / h'| + H |f|.
+  codes  scales and codes of pop_fp8_quantize are exact.  Those that a norm writes belong to an f that is off by ef: the value is off by ef and
+         half a step of e4m3, 2^-4 of it or 2^-10 scales.
+  linear products of codes are exact, a step of 32 of them errs by at most (2^-21 + 2^-23) of the addends' magnitudes (rule of the tensor core's accumulator: aligned, cut
+         and truncated), four steps a block; the sums over blocks and up to three joins by u each.  With A the sum of all magnitudes:
+         |y - exact| <= (4 (2^-21 + 2^-23) + (blocks + 12) u) A + H |y|.
+  rope   rotations are exact in the arithmetic that the header states (cosines rounded to fp32, every product and sum): equal to the oracle's in fp32, and after
+         one rounding in bf16.  A cosine in 64 bits may round to the other fp32 neighbour only within 2^-29 of a step of the border: not in these inputs.
+"""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import __graft_entry__ as ge
+from oracle import kv_oracle as ko
+from oracle import layer_oracle as lo
+from paper_2602_06822_b200 import pop
+
+F32, BF16 = torch.float32, torch.bfloat16
+DEV = "cuda:0"
+U = 2.0 ** -24
+HALF = {F32: 2.0 ** -24, BF16: 2.0 ** -8}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    ge.build()
+    pop.lib()
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def rnd(rng, shape, dtype, scale=1.0):
+    return torch.from_numpy((rng.standard_normal(shape) * scale).astype(np.float32)).to(dtype).to(DEV)
+
+
+def within(got, want, bound, what):
+    got, want = host(got), np.asarray(want)
+    assert got.shape == want.shape
+    over = np.abs(got - want) - bound
+    assert np.all(np.isfinite(got)) and np.all(over <= 0), f"{what}: {np.max(over)} over the bound, worst relative {np.max(np.abs(got - want) / (bound + 1e-300))}"
+
+
+# ------------------------------------------------------------------------------------------------------------------ norm
+
+def norm_bounds(dtype, h, b, f, h_scale):
+    """Errors of h' and of f, before and after their rounding."""
+    new = np.abs(host(h) * h_scale + b)
+    e = 50 * U * (np.abs(host(h) * h_scale) + np.abs(b))
+    rel = np.linalg.norm(e, axis=1, keepdims=True) / np.maximum(np.linalg.norm(new, axis=1, keepdims=True), 1e-30)
+    ratio = np.abs(f) / np.maximum(new, 1e-30)
+    ef = np.abs(f) * (60 * U + rel) + e * np.where(new > 0, ratio, 1e6)
+    return e + HALF[dtype] * (new + e), ef, HALF[dtype] * (np.abs(f) + ef) + ef
+
+
+def check_norm(h, u, dtype, post=False, post_gain=None, gate=None, h_scale=1.0, u_scale=1.0, gain=None, **kw):
+    want_h, want_f, b = lo.block_norm(host(h), None if u is None else host(u), post, None if post_gain is None else host(post_gain),
+                                      None if gate is None else host(gate), np.float32(h_scale), np.float32(u_scale), None if gain is None else host(gain))
+    eh, ef, efr = norm_bounds(dtype, h, b, want_f, h_scale)
+    got_h, got_f = pop.block_norm(h, u, post_norm=post, post_gain=post_gain, gate=gate, h_scale=h_scale, u_scale=u_scale, gain=gain, **kw)
+    within(got_h, want_h, eh, "h'")
+    if kw.get("fp8"):
+        s = np.repeat(host(got_f.scales).T, 128, 1)[:, :h.shape[1]]
+        vals = lo.values(got_f.codes.view(torch.uint8).cpu().numpy(), got_f.scales.cpu().numpy(), 1)
+        over = np.abs(vals - want_f) - (2.0 ** -4 * (np.abs(want_f) + ef) + 2.0 ** -10 * s + ef)
+        assert np.all(over <= 0), over.max()
+        top = np.abs(np.pad(want_f, ((0, 0), (0, -h.shape[1] % 128)))).reshape(h.shape[0], -1, 128).max(2).T / 448
+        assert np.all(np.abs(host(got_f.scales) - top) <= top * (200 * U) + 2.0 ** -126)
+    else:
+        within(got_f, want_f, efr, "f")
+    return got_h, got_f
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,d", [(1, 1), (1, 4096), (3, 7), (5, 128), (33, 1001), (2, 8192), (2, 8200), (3, 12289), (1, 32768), (700, 64)])
+def test_norm_sizes(T, d, dtype):
+    rng = np.random.default_rng(T * 100003 + d)
+    h, u, g1, g2 = (rnd(rng, s, dtype) for s in ((T, d), (T, d), (d,), (d,)))
+    gate = rnd(rng, (T, d), dtype)
+    check_norm(h, u, dtype, post=True, post_gain=g1, gate=gate, h_scale=0.75, u_scale=-1.5, gain=g2)
+    check_norm(h, u, dtype)
+    check_norm(h, None, dtype, gain=g2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d", [256, 1001])
+def test_norm_options_and_strides(d, dtype):
+    rng = np.random.default_rng(d)
+    T = 9
+    wide = rnd(rng, (T, 3 * d + 24), dtype)
+    h, u = wide[:, :d], wide[:, d + 8:2 * d + 8]
+    row = rnd(rng, (1, d), dtype)
+    for kw in (dict(post=True), dict(gate=row), dict(gate=row[0], u_scale=0.0), dict(gate=wide[:, 2 * d + 16:3 * d + 16], h_scale=0.0), dict(post=True, gate=row, gain=row[0])):
+        check_norm(h, u, dtype, **kw)
+    # in place, in a strided stream; equal to the call that is not, bit for bit
+    want_h, want_f = pop.block_norm(h, u, post_norm=True)
+    other = wide.clone()
+    got_h, got_f = pop.block_norm(other[:, :d], other[:, d + 8:2 * d + 8], post_norm=True, h_out=other[:, :d])
+    assert torch.equal(other[:, :d], want_h) and torch.equal(got_f, want_f)
+    assert torch.equal(other[:, d:], wide[:, d:])
+    # no block: the stream is what it was
+    same, f = pop.block_norm(h)
+    assert same is h
+    half, _ = pop.block_norm(h, h_scale=0.5)
+    within(half, host(h) * 0.5, HALF[dtype] * np.abs(host(h)), "h_scale")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,d", [(1, 16), (3, 144), (5, 4096), (2, 11008), (2, 32768)])
+def test_norm_to_fp8(T, d, dtype):
+    rng = np.random.default_rng(d + T)
+    h, u, g = rnd(rng, (T, d), dtype), rnd(rng, (T, d), dtype), rnd(rng, (d,), dtype)
+    plain_h, _ = check_norm(h, u, dtype, gain=g)
+    fp8_h, _ = check_norm(h, u, dtype, gain=g, fp8=True)
+    assert torch.equal(plain_h, fp8_h)
+
+
+@pytest.mark.gpu
+def test_norm_of_rows_without_values():
+    """Zeros stay zeros (eps keeps the root away from zero); a row with NaN or an infinity is NaN, its neighbours are not."""
+    for dtype in (F32, BF16):
+        h = torch.ones(4, 256, dtype=dtype, device=DEV)
+        h[0] = 0
+        h[1, 3] = float("nan")
+        h[2, 200] = float("inf")
+        _, f = pop.block_norm(h)
+        assert torch.all(f[0] == 0) and torch.isnan(f[1]).all() and torch.isnan(f[2, 200]) and torch.all(f[2, :200] == 0)
+        assert torch.isfinite(f[3]).all()
+        _, q = pop.block_norm(h, fp8=True)
+        c = q.codes.view(torch.uint8)
+        assert torch.all(c[0] & 127 == 0) and torch.all(c[1] & 127 == 127) and int(c[2, 200]) & 127 == 127 and torch.all(c[3] == 126)
+    h0, f0 = pop.block_norm(torch.ones(0, 64, device=DEV), torch.ones(0, 64, device=DEV))
+    assert h0.shape == f0.shape == (0, 64)
+
+
+# ------------------------------------------------------------------------------------------------------------------- fp8
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,K", [(1, 16), (1, 4096), (7, 144), (128, 128), (129, 272), (300, 1360), (1000, 64)])
+def test_quantise_equals_the_oracle(rows, K, dtype):
+    rng = np.random.default_rng(rows + K)
+    x = rnd(rng, (rows, K + 16), dtype) * torch.exp(torch.from_numpy(rng.standard_normal((rows, 1)) * 3).to(DEV)).to(dtype)
+    x[0, 0], x[rows // 2, K // 2], x[-1, K - 1] = float("nan"), float("inf"), float("-inf")
+    if rows > 5:
+        x[3], x[4] = 0, 1e-39
+    x = x[:, :K]
+    for block_rows, fn in ((1, pop.fp8_quantize), (128, pop.fp8_weights)):
+        codes, scales = fn(x)
+        want_c, want_s = lo.quantise(host(x), block_rows)
+        np.testing.assert_array_equal(scales.cpu().numpy(), want_s)
+        got = codes.view(torch.uint8).cpu().numpy()
+        nan = want_c & 127 == 127
+        np.testing.assert_array_equal(np.where(nan, got & 127, got), np.where(nan, 127, want_c))
+        assert np.array_equal(np.isnan(lo.CODES[got]), ~np.isfinite(host(x)))
+
+
+def test_the_oracle_codes_are_e4m3():
+    """Pinned by torch's conversion (on the CPU): every code's value, and rounding to it."""
+    c = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()
+    np.testing.assert_array_equal(c, lo.CODES)
+    x = np.concatenate([np.random.default_rng(1).standard_normal(20000) * 60, np.linspace(-448, 448, 28673), lo.CODES[:127], [0.0, 2.0 ** -10, 3 * 2.0 ** -10]])
+    want = torch.from_numpy(x).float().to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    np.testing.assert_array_equal(lo.code_of(x.astype(np.float32).astype(np.float64)), want)
+
+
+def check_linear(M, N, K, x_dtype, rng, x=None, **kw):
+    w = pop.fp8_weights(rnd(rng, (N, K), BF16, 0.05))
+    x = rnd(rng, (M, K), x_dtype) if x is None else x
+    q = pop.fp8_quantize(x)
+    y = pop.fp8_linear(x, w, **kw)
+    xv = lo.values(q.codes.view(torch.uint8).cpu().numpy(), q.scales.cpu().numpy(), 1)
+    wv = lo.values(w.codes.view(torch.uint8).cpu().numpy(), w.scales.cpu().numpy(), 128)
+    want = torch.from_numpy(xv).to(DEV) @ torch.from_numpy(wv).to(DEV).T
+    size = (torch.from_numpy(np.abs(xv)).to(DEV) @ torch.from_numpy(np.abs(wv)).to(DEV).T).cpu().numpy()
+    want = want.cpu().numpy()
+    bound = (4 * (2.0 ** -21 + 2.0 ** -23) + (-(-K // 128) + 12) * U) * size
+    within(y, want, bound + HALF[y.dtype] * (np.abs(want) + bound), "y")
+    again = pop.fp8_linear(q, w, dtype=y.dtype)
+    assert torch.equal(again, y if y.is_contiguous() else y.contiguous())
+    pop.fp8_check()
+    return y
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,N,K", [
+    (1, 1, 16), (1, 4096, 4096), (2, 17, 128), (8, 129, 1360), (9, 300, 256), (16, 1000, 4112), (17, 64, 144), (17, 1000, 4096), (31, 129, 11008),
+    (64, 4096, 512), (100, 250, 2000), (127, 128, 128), (128, 256, 1024), (129, 257, 1040), (333, 1000, 1360), (1000, 4100, 528), (600, 12000, 272),
+])
+def test_linear_sizes(M, N, K, dtype):
+    check_linear(M, N, K, dtype, np.random.default_rng(M * 31 + N * 7 + K))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 5, 13, 40, 200, 1300])
+def test_linear_types_strides_and_repeats(M):
+    rng = np.random.default_rng(M)
+    N, K = 516, 640
+    x = rnd(rng, (M, 2 * K), BF16)[:, K:]
+    for dtype in (BF16, F32):
+        wide = torch.full((M, N + 12), 7.0, dtype=dtype, device=DEV)
+        y = check_linear(M, N, K, BF16, np.random.default_rng(5), x=x, out=wide[:, 4:4 + N])
+        assert torch.all(wide[:, :4] == 7) and torch.all(wide[:, 4 + N:] == 7)
+        z = check_linear(M, N, K, BF16, np.random.default_rng(5), x=x, dtype=dtype)
+        assert torch.equal(y, z)
+    odd = torch.full((M, 517), 7.0, dtype=BF16, device=DEV)                  # rows that are no multiple of 16 bytes
+    check_linear(M, 516, K, BF16, np.random.default_rng(5), x=x, out=odd[:, 1:])
+    assert torch.all(odd[:, 0] == 7)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [3, 50, 400])
+def test_linear_carries_nan_and_nothing_else(M):
+    """A token with an element that is not finite is NaN everywhere, the others are what they are without it; zero rows give zeros."""
+    rng = np.random.default_rng(M)
+    x = rnd(rng, (M, 384), BF16)
+    w = pop.fp8_weights(rnd(rng, (200, 384), BF16, 0.05))
+    want = pop.fp8_linear(x, w)
+    y = x.clone()
+    y[1, 130] = float("inf")
+    y[2] = 0
+    got = pop.fp8_linear(y, w)
+    assert torch.isnan(got[1]).all() and torch.all(got[2] == 0)
+    keep = [i for i in range(M) if i not in (1, 2)]
+    assert torch.equal(got[keep], want[keep])
+    assert pop.fp8_linear(x[:0], w).shape == (0, 200)
+
+
+@pytest.mark.gpu
+def test_linear_magnitudes():
+    """Blocks of very different size side by side: every block has its own scale, so each counts by what it is."""
+    rng = np.random.default_rng(3)
+    x = rnd(rng, (40, 1024), F32)
+    x = x * torch.tensor([2.0 ** (8 * (i % 5) - 16) for i in range(8)], device=DEV).repeat_interleave(128)
+    check_linear(40, 300, 1024, F32, rng, x=x)
+    check_linear(4, 300, 1024, F32, rng, x=x[:4] * 1e30)
+    check_linear(4, 300, 1024, F32, rng, x=x[:4] * 1e-30)
+
+
+# ------------------------------------------------------------------------------------------------------------------ rope
+
+SCALINGS = [("none", {}), ("linear", dict(factor=4.0)), ("ntk", dict(factor=8.0)), ("yarn", dict(factor=16.0)),
+            ("yarn", dict(factor=2.0, original_positions=300, beta_fast=20, beta_slow=2)), ("bands", dict(factor=8.0, original_positions=8192)),
+            ("bands", dict(factor=1.0))]
+
+
+@pytest.mark.parametrize("scaling,kw", SCALINGS)
+@pytest.mark.parametrize("rot,base", [(2, 10000.0), (4, 10000.0), (96, 1e6), (128, 10000.0), (512, 5e5)])
+def test_frequencies(scaling, kw, rot, base):
+    if scaling == "ntk" and rot == 2:
+        return
+    got, m = pop.rope_frequencies(rot, base, scaling, **kw)
+    want, wm = lo.rope_frequencies(rot, base, scaling, kw.get("factor", 1.0), kw.get("original_positions", 4096.0), kw.get("beta_fast"), kw.get("beta_slow", 1.0))
+    turns = got.astype(np.longdouble) / np.longdouble(2.0) ** 64
+    # the oracle's powers and logarithms are in 64 bits: some twenty roundings of 2^-53, exponents up to ln(base) = 14; and a frequency is a whole
+    # number of 2^-64 turns, off by half of one, 2^-65 (for the slowest pairs, 2e-7 turns a position, that is 1.3e-13 of it)
+    assert np.all(np.abs(turns * 2 * np.pi - want) < 300 * 2.0 ** -53 * want + 2.0 ** -65 * 2 * np.pi) and abs(m - wm) < 1e-15
+
+
+def rope_case(rng, T, H, Hk, D, dtype, far=0):
+    rows = rnd(rng, (T, H + 2 * Hk, D), dtype)
+    pos = rng.integers(0, 2000, T) + far
+    return rows[:, :H], rows[:, H:H + Hk], rows[:, H + Hk:], pos
+
+
+def to_dev(v, dtype=torch.int32):
+    return torch.from_numpy(np.asarray(v)).to(DEV, dtype)
+
+
+def check_equal(got, want32, dtype):
+    want = torch.from_numpy(want32).to(dtype)
+    assert torch.equal(got.cpu(), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("T,H,Hk,D,rot", [(1, 32, 32, 128, 128), (13, 8, 2, 64, 64), (5, 3, 1, 80, 20), (300, 6, 2, 96, 24), (2, 1, 1, 2, 2), (7, 5, 3, 130, 66),
+                                          (3, 2, 1, 512, 512), (1500, 4, 1, 128, 64)])
+def test_rope_equals_the_oracle(T, H, Hk, D, rot, interleaved, dtype):
+    rng = np.random.default_rng(T + D + rot)
+    q, k, _, pos = rope_case(rng, T, H, Hk, D, dtype, far=100000 if T < 20 else 0)
+    r = pop.Rope(rot, interleaved=interleaved, scaling="yarn" if T == 13 else "none", factor=4.0, device=DEV)
+    cos, sin = lo.cos_sin(pop.rope_frequencies(rot, scaling="yarn" if T == 13 else "none", factor=4.0)[0], r.magnitude, pos)
+    p = to_dev(pos)
+    for inverse in (False, True):
+        gq, gk = pop.rope(r, p, q, k, inverse=inverse)
+        check_equal(gq, lo.rotate(host(q), cos, sin, interleaved, inverse), dtype)
+        check_equal(gk, lo.rotate(host(k), cos, sin, interleaved, inverse), dtype)
+    # alone, dense, and in place among other columns
+    assert torch.equal(pop.rope(r, p, q.contiguous(), inverse=True), gq)
+    rows = torch.cat([q, k], 1)
+    pop.rope(r, p, rows[:, :H], rows[:, H:], inverse=True, q_out=rows[:, :H], k_out=rows[:, H:])
+    assert torch.equal(rows, torch.cat([gq, gk], 1))
+
+
+@pytest.mark.gpu
+def test_rope_far_positions_and_rows_left_out():
+    rng = np.random.default_rng(0)
+    q = rnd(rng, (6, 2, 64), F32)
+    pos = np.array([0, -1, 2**31 - 1, 131071, -7, 1 << 24])
+    r = pop.Rope(64, device=DEV)
+    cos, sin = lo.cos_sin(pop.rope_frequencies(64)[0], r.magnitude, np.maximum(pos, 0))
+    out = torch.full_like(q, 5.0)
+    pop.rope(r, to_dev(pos), q, q_out=out)
+    want = lo.rotate(host(q), cos, sin, False)
+    want[[1, 4]] = 5.0
+    check_equal(out, want, F32)
+    # against the definition in 64 bits: the angle of position 2^31 - 1 is right to 2^-33 turns
+    angle = np.outer(np.maximum(pos, 0).astype(np.float64), lo.rope_frequencies(64)[0])
+    for t in (2, 3, 5):
+        for i in (20, 31):                                                   # slow pairs: 64 bits hold these angles
+            assert abs(cos[t, i] - np.cos(angle[t, i])) < 1e-6
+    back = pop.rope(r, to_dev(np.maximum(pos, 0)), pop.rope(r, to_dev(np.maximum(pos, 0)), q), inverse=True)
+    assert torch.max(torch.abs(back - q)) < 16 * U * 5                       # two turns: six roundings of values below 5 in each
+    assert pop.rope(r, to_dev(np.zeros(0)), q[:0]).shape == (0, 2, 64)
+
+
+def cached(pages, slots, dtype=F32):
+    return pop.kv_read(pages, slots, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D,rot,interleaved", [(64, 64, False), (128, 128, False), (128, 64, False), (128, 128, True), (64, 16, True), (64, 20, False), (128, 48, False)])
+@pytest.mark.parametrize("T,H,Hk,page", [(1, 4, 4, 16), (13, 8, 2, 64), (700, 6, 3, 32), (3000, 4, 2, 64)])
+def test_append_rope_is_rope_then_append(T, H, Hk, page, D, rot, interleaved, dtype):
+    """q as pop_rope gives it, and the pages, byte for byte, as pop_kv_append leaves them for keys that pop_rope turned in fp32."""
+    rng = np.random.default_rng(T + D + rot)
+    q, k, v, pos = rope_case(rng, T, H, Hk, D, dtype)
+    r = pop.Rope(rot, interleaved=interleaved, scaling="bands", factor=2.0, device=DEV)
+    n_pages = -(-T // page) + 2
+    slots = rng.permutation(n_pages)[:, None] * page + np.arange(page)
+    slots = slots.reshape(-1)[5:5 + T]                                       # begins and ends inside a tile
+    slots[rng.integers(0, T, T // 50)] = -1
+    if T > 1:
+        slots[-1] = n_pages * page                                           # outside the cache
+        pos[T // 3] = -1
+    s, p = to_dev(slots, torch.int64), to_dev(pos)
+    fused, apart = (torch.full_like(pop.kv_pages(n_pages, page, Hk, D, DEV), 90) for _ in range(2))
+    out = torch.full(q.shape, 3.0, dtype=dtype, device=DEV)
+    got = pop.kv_append_rope(fused, r, p, q, k, v, s, q_out=out)
+    want = torch.full_like(out, 3.0)
+    pop.rope(r, p, q, q_out=want)
+    assert torch.equal(got, want)
+    kf = pop.rope(r, p, k.float().contiguous())
+    left_out = torch.where(p < 0, torch.full_like(s, -1), s)
+    pop.kv_append(apart, kf, v.float().contiguous(), left_out)
+    assert torch.equal(fused, apart)
+    # and the keys are what the format says of the oracle's rotation
+    if T <= 13:
+        cos, sin = lo.cos_sin(pop.rope_frequencies(rot, scaling="bands", factor=2.0)[0], r.magnitude, np.maximum(pos, 0))
+        here = [i for i in range(T) if 0 <= slots[i] < n_pages * page and pos[i] >= 0]
+        got_k, _ = cached(fused, s)
+        np.testing.assert_array_equal(got_k.cpu().numpy()[here], ko.stored(lo.rotate(host(k), cos, sin, interleaved))[here].astype(np.float32))
+
+
+# ------------------------------------------------------------------------------------------- used together, graphs, streams
+
+class Layer:
+    """The attention block of a decoder layer as a user strings the calls together: norm -> projections -> rotation into the cache -> attention ->
+    projection -> residual and the next norm."""
+
+    def __init__(self, d, H, Hk, D, tokens, requests):
+        rng = np.random.default_rng(11)
+        self.H, self.Hk, self.D = H, Hk, D
+        self.wqkv = pop.fp8_weights(rnd(rng, ((H + 2 * Hk) * D, d), BF16, d ** -0.5))
+        self.wo = pop.fp8_weights(rnd(rng, (d, H * D), BF16, (H * D) ** -0.5))
+        self.g1, self.g2 = rnd(rng, (d,), BF16, 0.1) + 1, rnd(rng, (d,), BF16, 0.1) + 1
+        self.cache = pop.KVCache(1, requests, tokens, Hk, D, device=DEV)
+        self.rope = pop.Rope(D, device=DEV)
+
+    def __call__(self, h, new, n):
+        T = h.shape[0]
+        self.cache.plan(new, n)
+        _, f = pop.block_norm(h, gain=self.g1, fp8=True)
+        qkv = pop.fp8_linear(f, self.wqkv).view(T, self.H + 2 * self.Hk, self.D)
+        q = self.cache.append_rope(0, self.rope, qkv[:, :self.H], qkv[:, self.H:self.H + self.Hk], qkv[:, self.H + self.Hk:])
+        o = self.cache.attend(0, q)
+        return pop.block_norm(h, pop.fp8_linear(o.view(T, -1), self.wo), gain=self.g2)
+
+
+@pytest.mark.gpu
+def test_layer_against_64_bits():
+    """Two steps (prompts, then single tokens) of two requests against the same layer in 64 bits on the unquantised weights' codes: the roundings to 8 and 4 bits
+    on the way are the operators' own, so only the layer's result is compared, in the 2-norm: e4m3 steps of the norm's and of the attention's output (rms 2^-5.3 of each
+    element, independent), the 4-bit keys and values (step 1 / 15 of a range of some 5 deviations: rms 0.1 of a value), all of them inside the block's output, which
+    is a third of the stream here: 0.1 / 3 of it; 5 % is asked for."""
+    d, H, Hk, D = 256, 4, 2, 64
+    L = Layer(d, H, Hk, D, 256, 2)
+    rng = np.random.default_rng(2)
+    held = [np.zeros((0, 2, Hk, D)) for _ in range(2)]
+    wqkv, wo = (lo.values(w.codes.view(torch.uint8).cpu().numpy(), w.scales.cpu().numpy(), 128) for w in (L.wqkv, L.wo))
+    freq = pop.rope_frequencies(D)[0]
+    for new in ((70, 9), (1, 1)):
+        n = sum(new)
+        h = rnd(rng, (n, d), BF16)
+        got_h, got_f = L(h, to_dev(new), n)
+        _, f, _ = lo.block_norm(host(h), gain=host(L.g1))
+        qkv = (f @ wqkv.T).reshape(n, H + 2 * Hk, D)
+        out, at = np.zeros((n, H, D)), 0
+        for r, m in enumerate(new):
+            pos = np.arange(len(held[r]), len(held[r]) + m)
+            cos, sin = lo.cos_sin(freq, 1.0, pos)
+            q, k = (lo.rotate(x[at:at + m], cos, sin, False).astype(np.float64) for x in (qkv[:, :H], qkv[:, H:H + Hk]))
+            held[r] = np.concatenate([held[r], np.stack([k, qkv[at:at + m, H + Hk:]], 1)])
+            out[at:at + m], _ = ko.attention(q, held[r][:, 0], held[r][:, 1], pos[0], D ** -0.5, True, 0)
+            at += m
+        want_h, want_f, _ = lo.block_norm(host(h), (out.reshape(n, -1) @ wo.T), gain=host(L.g2))
+        for got, want in ((got_h, want_h), (got_f, want_f)):
+            assert np.linalg.norm(host(got) - want) / np.linalg.norm(want) < 0.05
+    L.cache.check()
+    pop.fp8_check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [1, 40])
+def test_layer_captured_and_replayed(tokens):
+    """A captured step gives what the eager one gives, on another stream, twice, and two graphs side by side."""
+    d, H, Hk, D = 512, 4, 2, 128
+    rng = np.random.default_rng(4)
+    h = rnd(rng, (tokens, d), BF16)
+    new = to_dev([tokens])
+    eager = Layer(d, H, Hk, D, 512, 1)
+    want = [tuple(t.clone() for t in eager(h, new, tokens)) for _ in range(3)]
+    layers = [Layer(d, H, Hk, D, 512, 1) for _ in range(2)]
+    graphs, outs, streams = [], [], [torch.cuda.Stream() for _ in range(2)]
+    for L, s in zip(layers, streams):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            L(h, new, tokens)                                                # loads what is loaded lazily
+        torch.cuda.synchronize()
+        L.cache.reset()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            outs.append(L(h, new, tokens))
+        graphs.append(g)
+        torch.cuda.synchronize()
+    for i in range(3):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for o in outs:
+            assert torch.equal(o[0], want[i][0]) and torch.equal(o[1], want[i][1])
+
+
+@pytest.mark.gpu
+def test_calls_on_another_stream():
+    rng = np.random.default_rng(8)
+    x, big = rnd(rng, (300, 512), BF16), rnd(rng, (4096, 4096), F32)
+    w = pop.fp8_weights(rnd(rng, (512, 512), BF16, 0.05))
+    r, pos = pop.Rope(64, device=DEV), to_dev(np.arange(300))
+    want = (pop.block_norm(x, x), pop.fp8_linear(x, w), pop.rope(r, pos, x.view(300, 8, 64)), pop.fp8_quantize(x))
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(4):
+            big = big @ big * 1e-4                                           # the stream is busy when the calls are made
+        y = x * 1
+    got = (pop.block_norm(y, y, stream=s), pop.fp8_linear(y, w, stream=s), pop.rope(r, pos, y.view(300, 8, 64), stream=s), pop.fp8_quantize(y, stream=s))
+    s.synchronize()
+    for a, b in zip(want, got):
+        for p, q in zip(a if isinstance(a, tuple) else (a,), b if isinstance(b, tuple) else (b,)):
+            assert torch.equal(p.view(torch.uint8), q.view(torch.uint8))
+
+
+# -------------------------------------------------------------------------------------------------------------- refusals
+
+BAD, NO = pop.POP_ERR_INVALID_ARG, pop.POP_ERR_UNSUPPORTED
+A = 1 << 20                                     # an address that no call gets as far as using
+
+
+def norm_status(T=4, d=64, dtype=0, **kw):
+    a = pop.BlockNormArgs()
+    for k, v in dict(dict(h=A, u=A, h_stride=64, u_stride=64, h_out=A, h_out_stride=64, f=A, h_scale=1.0, u_scale=1.0, eps=1e-5), **kw).items():
+        setattr(a, k, v)
+    return pop.lib().pop_block_norm(C.byref(a), T, d, dtype, None)
+
+
+@pytest.mark.parametrize("status,kw", [
+    (BAD, dict(T=-1)), (BAD, dict(d=0)), (NO, dict(dtype=7)), (NO, dict(d=pop.POP_NORM_MAX_D + 1)), (BAD, dict(h=None)), (BAD, dict(h_stride=63)),
+    (BAD, dict(u_stride=3)), (BAD, dict(h_out_stride=8)), (BAD, dict(gate=A, gate_stride=32)), (BAD, dict(u=None, gate=A)), (BAD, dict(u=None, post_norm=1)),
+    (BAD, dict(post_gain=A)), (BAD, dict(f=None, h_out=None)), (BAD, dict(f_codes=A)), (BAD, dict(f_scales=A)), (BAD, dict(eps=-1.0)), (BAD, dict(eps=float("nan"))),
+    (BAD, dict(h_scale=float("nan"))), (BAD, dict(h=A + 2)), (NO, dict(f_codes=A, f_scales=A, d=40, h_stride=64)), (NO, dict(f_codes=A + 4, f_scales=A)),
+    (NO, dict(f_codes=A, f_scales=A, h=A + 8)), (0, dict(T=0)),
+])
+def test_norm_refusals(status, kw):
+    assert norm_status(**kw) == status
+    assert pop.lib().pop_block_norm(None, 1, 8, 0, None) == BAD
+
+
+def test_fp8_refusals():
+    l = pop.lib()
+    quant = lambda x=A, stride=64, rows=4, K=64, dtype=1, block=1, codes=A, scales=A: l.pop_fp8_quantize(x, stride, rows, K, dtype, block, codes, scales, None)      # noqa: E731
+    for status, kw in ((BAD, dict(x=None)), (BAD, dict(x=A + 8)), (BAD, dict(stride=32)), (BAD, dict(stride=65)), (BAD, dict(rows=-1)), (BAD, dict(K=0)), (NO, dict(K=72)),
+                       (NO, dict(dtype=5)), (BAD, dict(block=64)), (BAD, dict(codes=None)), (BAD, dict(codes=A + 8)), (BAD, dict(scales=None)), (0, dict(rows=0))):
+        assert quant(**kw) == status, kw
+    lin = lambda x=A, xs=A, M=4, w=A, ws=A, N=64, K=64, y=A, ys=64, dt=1: l.pop_fp8_linear(x, xs, M, w, ws, N, K, y, ys, dt, None)                                   # noqa: E731
+    for status, kw in ((BAD, dict(x=None)), (BAD, dict(xs=None)), (BAD, dict(w=None)), (BAD, dict(ws=None)), (BAD, dict(y=None)), (BAD, dict(M=-2)), (BAD, dict(N=0)),
+                       (BAD, dict(K=0)), (NO, dict(K=100)), (BAD, dict(ys=63)), (NO, dict(dt=3)), (BAD, dict(x=A + 4)), (BAD, dict(w=A + 8)), (BAD, dict(y=A + 1)), (0, dict(M=0))):
+        assert lin(**kw) == status, kw
+    need = C.c_size_t()
+    assert l.pop_fp8_linear_workspace(3, 64, None) == BAD and l.pop_fp8_linear_workspace(3, 63, C.byref(need)) == NO
+    assert l.pop_fp8_linear_workspace(3, 64, C.byref(need)) == 0 and need.value >= 3 * 64 + 12
+    rows = lambda ws=A, n=1 << 20, x=A: l.pop_fp8_linear_rows(x, 64, 1, 4, A, A, 64, 64, A, 64, 1, ws, n, None)                                                      # noqa: E731
+    assert rows(ws=None) == BAD and rows(n=8) == BAD and rows(ws=A + 8) == BAD and rows(x=None) == BAD
+
+
+def test_rope_refusals():
+    l = pop.lib()
+    for kw in (dict(rot_dim=0), dict(rot_dim=7), dict(base=1.0), dict(base=float("nan")), dict(scaling="linear", factor=0.5), dict(scaling="ntk", rot_dim=2, factor=2.0),
+               dict(scaling="yarn", factor=2.0, beta_fast=1.0, beta_slow=2.0), dict(scaling="bands", factor=2.0, original_positions=0.0)):
+        with pytest.raises(pop.PopError) as e:
+            pop.rope_frequencies(**dict(dict(rot_dim=64), **kw))
+        assert e.value.status == BAD
+    desc = lambda freq=A, rot=64, inter=0, m=1.0: C.byref(pop.RopeDesc(freq, rot, inter, m))                                                                        # noqa: E731
+    rope = lambda d=None, pos=A, T=4, D=64, dt=0, q=A, qs=128, H=2, o=A, os=128, k=None, ks=0, Hk=0, ko_=None, kos=0: l.pop_rope(                                   # noqa: E731
+        d or desc(), 0, pos, T, D, dt, q, qs, H, o, os, k, ks, Hk, ko_, kos, None)
+    for status, kw in ((BAD, dict(d=desc(freq=None))), (BAD, dict(d=desc(rot=66))), (BAD, dict(d=desc(rot=3))), (BAD, dict(d=desc(m=float("nan")))), (BAD, dict(pos=None)),
+                       (BAD, dict(T=-1)), (BAD, dict(D=63)), (NO, dict(D=514, qs=2000, os=2000)), (NO, dict(dt=9)), (BAD, dict(q=None)), (BAD, dict(o=None)), (BAD, dict(qs=127)),
+                       (BAD, dict(os=100)), (BAD, dict(H=0)), (BAD, dict(k=A, Hk=1, ks=64)), (BAD, dict(k=A, Hk=0, ks=64, ko_=A, kos=64)), (BAD, dict(q=A + 2)),
+                       (BAD, dict(qs=130)), (0, dict(T=0))):
+        assert rope(**kw) == status, kw
+    cache = pop.KVCacheDesc(A, 4, 16, 2, 64)
+    app = lambda c=cache, d=None, pos=A, q=A, qs=256, H=4, o=A + 4096, os=256, k=A, ks=128, v=A, vs=128, dt=1, s=A, T=4: l.pop_kv_append_rope(                        # noqa: E731
+        C.byref(c), d or desc(), pos, q, qs, H, o, os, k, ks, v, vs, dt, s, T, None)
+    for status, kw in ((NO, dict(c=pop.KVCacheDesc(A, 4, 16, 2, 96))), (BAD, dict(d=desc(rot=128))), (BAD, dict(pos=None)), (BAD, dict(s=None)), (BAD, dict(H=0)), (BAD, dict(T=-1)),
+                       (BAD, dict(o=A)), (BAD, dict(qs=255)), (BAD, dict(ks=64)), (BAD, dict(v=None)), (BAD, dict(k=A + 8)), (NO, dict(dt=4)), (0, dict(T=0))):
+        assert app(**kw) == status, kw
+
+
+@pytest.mark.gpu
+def test_binding_refusals():
+    x, w = torch.ones(4, 64, device=DEV), pop.fp8_weights(torch.ones(128, 64, device=DEV))
+    r, pos = pop.Rope(64, device=DEV), to_dev([0, 1, 2, 3])
+    q = x.view(4, 1, 64)
+    grad = x.clone().requires_grad_()
+    for fn in (lambda: pop.block_norm(grad), lambda: pop.fp8_linear(grad, w), lambda: pop.fp8_quantize(grad), lambda: pop.rope(r, pos, grad.view(4, 1, 64)),
+               lambda: pop.block_norm(x.cpu()), lambda: pop.fp8_linear(x, pop.Fp8Weights(w.codes.cpu(), w.scales)), lambda: pop.rope(r, pos.cpu(), q),
+               lambda: pop.block_norm(x.t()), lambda: pop.block_norm(x, x[:3]), lambda: pop.block_norm(x, x, gate=x[:2]), lambda: pop.block_norm(x, gain=x[0, :32]),
+               lambda: pop.fp8_linear(x[:, :32], w), lambda: pop.fp8_linear(x, w, out=x), lambda: pop.fp8_linear(x, pop.Fp8Weights(w.codes, w.scales[:0])),
+               lambda: pop.rope(r, pos[:3], q), lambda: pop.rope(r, pos.long(), q), lambda: pop.rope(r, pos, q, q_out=q[:, :, :32])):
+        with pytest.raises(ValueError):
+            fn()
+    for fn in (lambda: pop.block_norm(x.half()), lambda: pop.block_norm(x, x.bfloat16()), lambda: pop.rope(r, pos, q, q.bfloat16())):
+        with pytest.raises(TypeError):
+            fn()
+    for fn in (lambda: pop.block_norm(x, gate=x), lambda: pop.block_norm(x, x, post_gain=x[0]), lambda: pop.fp8_quantize(x[:, :24]),
+               lambda: pop.rope(pop.Rope(128, device=DEV), pos, q)):
+        with pytest.raises(pop.PopError):
+            fn()
+    with torch.no_grad():
+        pop.block_norm(grad)
