@@ -7,10 +7,12 @@
 // scale, to running sums in their registers while the tensor cores work on the next block in the other accumulator.  Tokens are the MMA's
 // 128 rows (tensor-memory lanes): a thread has one token, and its scale for a block is one number for all of its columns.
 //
-// Warp roles (320 threads, one CTA per SM, persistent over tiles of 128 tokens x BN outputs):
-//   warp 0      TMA producer (one lane): x tile and W tile of a block per stage
-//   warp 1      allocates tensor memory; one lane issues the MMAs and the commits
-//   warps 2..9  epilogue: warp w has lanes 32 (w % 4) .. + 31, columns of half (w - 2) / 4
+// Warp roles (384 threads, one CTA per SM, persistent over tiles of 128 tokens x BN outputs):
+//   warp 0       TMA producer (one lane): x tile and W tile of a block per stage
+//   warp 1       allocates tensor memory; one lane issues the MMAs and the commits
+//   warp 2       brings the scales (x's times W's) of coming blocks to shared memory, where a trip to L2 stops nobody
+//   warp 3       completes the warpgroup, whose registers go to the others
+//   warps 4..11  epilogue: warp w has lanes 32 (w % 4) .. + 31, columns of half (w - 4) / 4
 // Where there are too few tiles for the machine, a cluster of S CTAs shares a tile, each with a range of the blocks; the partial sums
 // are joined through distributed shared memory in the order of the ranks, so results do not depend on timing.
 // Every wait is bounded; one that runs out sets the device's status word (pop_fp8_check) and the CTA winds down.
@@ -22,7 +24,11 @@ namespace {
 
 constexpr int BM = 128;                          // tokens of a tile
 constexpr int X_BYTES = BM * fp8::BLOCK;         // 16 KB: 128 rows of one 128-byte swizzle span
-constexpr int THREADS = 320, EPI_WARPS = 8;
+constexpr int THREADS = 384, EPI_WARPS = 8;
+// registers of a thread: 128 * 72 + 256 * 216 <= 384 * 168, what the block is launched with
+#define FP8_REGS_OTHERS "72"
+#define FP8_REGS_EPILOGUE "216"
+constexpr int SLOTS = 8, AHEAD = 4;              // blocks whose scales are held, and asked for at a time
 constexpr int SMEM_LIMIT = 227 * 1024;
 constexpr u64 WAIT_BUDGET_NS = 200ull * 1000ull * 1000ull;      // per wait
 
@@ -37,7 +43,7 @@ template <int BN> struct Tile {
 };
 
 __device__ u32 fp8_status;                       // 0, or which role gave up a wait
-enum { GAVE_UP_PRODUCER = 1, GAVE_UP_MMA = 2, GAVE_UP_EPILOGUE = 3 };
+enum { GAVE_UP_PRODUCER = 1, GAVE_UP_MMA = 2, GAVE_UP_EPILOGUE = 3, GAVE_UP_SCALES = 4 };
 
 __device__ __forceinline__ u32 smem_u32(const void* p) { return (u32)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void mbar_init(u32 bar, u32 count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
@@ -153,15 +159,18 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
     extern __shared__ unsigned char raw_smem[];
     __shared__ u32 tmem_slot;
     __shared__ int gave_up_flag;
-    __shared__ u64 bars[2 * L::STAGES + 5];
+    __shared__ u64 bars[2 * L::STAGES + 5 + 2 * SLOTS];
+    __shared__ float scales[SLOTS][2][BM];       // a block's, for the halves of the columns
     volatile int* gave_up = &gave_up_flag;
     const u32 tiles = (smem_u32(raw_smem) + 1023u) & ~1023u;
     const u32 full = smem_u32(bars), empty = full + 8 * L::STAGES, acc_full = full + 16 * L::STAGES, acc_empty = acc_full + 16, drain = acc_full + 32;
+    const u32 sc_full = drain + 8, sc_empty = sc_full + 8 * SLOTS;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         gave_up_flag = 0;
         for (int s = 0; s < L::STAGES; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(acc_full + 8 * b, 1); mbar_init(acc_empty + 8 * b, EPI_WARPS); }
+        for (int i = 0; i < SLOTS; ++i) { mbar_init(sc_full + 8 * i, 1); mbar_init(sc_empty + 8 * i, EPI_WARPS); }
         mbar_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -179,7 +188,16 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
     const int units = G.m_tiles * G.n_tiles, rank = blockIdx.x % S, kb0 = (int)((long long)G.A.KB * rank / S), kb1 = (int)((long long)G.A.KB * (rank + 1) / S);
     const int first = blockIdx.x / S, step = gridDim.x / S;
 
-    if (warp == 0) {
+    auto all_done = [&]() {                      // the CTA's last meeting, at the end of every role
+        tc_before();
+        asm volatile("bar.sync 0;" ::: "memory");
+        tc_after();
+    };
+    if (warp < 4) {
+      // One instruction for the warpgroup, ahead of all its roles' code.  No code is shared again behind the roles: it might be given registers
+      // that these warps no longer have.
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 " FP8_REGS_OTHERS ";");
+      if (warp == 0) {
         if (lane == 0) {
             int s = 0, issued = 0;
             u32 ph = 0;
@@ -206,7 +224,7 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
                 }
             }
         }
-    } else if (warp == 1) {
+      } else if (warp == 1) {
         if (lane == 0) {
             int s = 0, buf = 0;
             u32 ph = 0, acc_ph = 0;              // bit b: phase of accumulator b
@@ -232,43 +250,84 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
             const u64 t0 = pop_global_ns();
             while (!mbar_try_wait(drain, 0u) && pop_global_ns() - t0 < WAIT_BUDGET_NS) {}
         }
+      }
+      else if (warp == 2) {
+        int slot = 0;
+        u32 ph = 0;
+        bool ok = true;
+        for (int unit = first; unit < units && ok; unit += step) {
+            const int m0 = unit % G.m_tiles * BM, n0 = unit / G.m_tiles * BN;
+            const float* ws[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) ws[h] = G.A.ws + (size_t)min((n0 + h * (BN / 2)) / fp8::BLOCK, (G.A.N - 1) / fp8::BLOCK) * G.A.KB;
+            for (int group = kb0; group < kb1 && ok; group += AHEAD) {
+                float x[AHEAD][BM / 32], w[AHEAD][2];
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const int kb = min(group + i, kb1 - 1);
+#pragma unroll
+                    for (int j = 0; j < BM / 32; ++j) x[i][j] = __ldg(G.A.xs + (size_t)kb * G.A.M + min(m0 + 32 * j + lane, G.A.M - 1));
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) w[i][h] = __ldg(ws[h] + kb);
+                }
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    if (group + i >= kb1) break;
+                    ok = __all_sync(~0u, mbar_wait(sc_empty + 8 * slot, ph ^ 1u, gave_up, GAVE_UP_SCALES));
+                    if (!ok) break;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int j = 0; j < BM / 32; ++j) scales[slot][h][32 * j + lane] = x[i][j] * w[i][h];
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(sc_full + 8 * slot);
+                    if (++slot == SLOTS) { slot = 0; ph ^= 1u; }
+                }
+            }
+        }
+      }
+      __syncwarp();
+      if (S > 1) {
+          cluster_sync();                        // the partial sums are there
+          cluster_sync();                        // and have been read
+      }
+      all_done();
+      if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::COLS) : "memory");
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 " FP8_REGS_EPILOGUE ";");
         constexpr int HALF = BN / 2;
-        const int quarter = warp & 3, half = (warp - 2) >> 2, row = quarter * 32 + lane;
+        const int quarter = warp & 3, half = (warp - 4) >> 2, row = quarter * 32 + lane;
         const u32 at = tmem + ((u32)(quarter * 32) << 16) + (u32)(half * HALF);
-        int buf = 0;
-        u32 acc_ph = 0;
+        int buf = 0, slot = 0;
+        u32 acc_ph = 0, slot_ph = 0;
         bool ok = true;
         for (int unit = first; unit < units && ok; unit += step) {
             const int mt = unit % G.m_tiles, nt = unit / G.m_tiles, m = mt * BM + row, n0 = nt * BN + half * HALF;
-            const float* xs = G.A.xs + min(m, G.A.M - 1);
-            const float* ws = G.A.ws + (size_t)min(n0 / fp8::BLOCK, (G.A.N - 1) / fp8::BLOCK) * G.A.KB;
             float2 acc[HALF / 2];
 #pragma unroll
             for (int j = 0; j < HALF / 2; ++j) acc[j] = make_float2(0.f, 0.f);
-            // scales two blocks ahead: a trip to L2 is about a block's time
-            auto scale_at = [&](int kb) { return kb < kb1 ? __ldg(xs + (size_t)kb * G.A.M) * __ldg(ws + kb) : 0.f; };
-            float s0 = scale_at(kb0), s1 = scale_at(kb0 + 1);
             for (int kb = kb0; kb < kb1; ++kb) {
-                const float s2 = scale_at(kb + 2);
-                ok = mbar_wait(acc_full + 8 * buf, (acc_ph >> buf) & 1u, gave_up, GAVE_UP_EPILOGUE);
+                ok = mbar_wait(sc_full + 8 * slot, slot_ph, gave_up, GAVE_UP_EPILOGUE) && mbar_wait(acc_full + 8 * buf, (acc_ph >> buf) & 1u, gave_up, GAVE_UP_EPILOGUE);
                 ok = __all_sync(~0u, ok);
                 if (!ok) break;
+                const float2 scale = make_float2(scales[slot][half][row], scales[slot][half][row]);
                 tc_after();
 #pragma unroll
                 for (int p = 0; p < HALF / 32; ++p) {
                     float v[32];
                     tmem_ld32(at + (u32)(buf * BN + 32 * p), v);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[16 * p + j] = __ffma2_rn(make_float2(v[2 * j], v[2 * j + 1]), make_float2(s0, s0), acc[16 * p + j]);
+                    for (int j = 0; j < 16; ++j) acc[16 * p + j] = __ffma2_rn(make_float2(v[2 * j], v[2 * j + 1]), scale, acc[16 * p + j]);
                 }
                 tc_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
+                if (lane == 0) {
+                    mbar_arrive(acc_empty + 8 * buf);
+                    mbar_arrive(sc_empty + 8 * slot);
+                }
                 acc_ph ^= 1u << buf;
                 buf ^= 1;
-                s0 = s1;
-                s1 = s2;
+                if (++slot == SLOTS) { slot = 0; slot_ph ^= 1u; }
             }
             if (!ok) break;
             if (S == 1) {
@@ -288,13 +347,10 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
                 }
             }
         }
-    }
-    __syncwarp();
-    if (S > 1) {                                 // one tile a cluster; rank r finishes columns [r, r + 1) BN / S
-        cluster_sync();
-        if (warp >= 2) {
-            const int row = (warp & 3) * 32 + lane, half = (warp - 2) >> 2, cols = BN / S / 2;      // BN / S is a multiple of 16
-            const int c0 = rank * (BN / S) + half * cols, mt = first % G.m_tiles, nt = first / G.m_tiles;
+        __syncwarp();
+        if (S > 1) {                             // one tile a cluster; rank r finishes columns [r, r + 1) BN / S, a multiple of 16 of them
+            cluster_sync();
+            const int cols = BN / S / 2, c0 = rank * (BN / S) + half * cols, mt = first % G.m_tiles, nt = first / G.m_tiles;
             for (int c = c0; c < c0 + cols; c += 8) {
                 float v[8] = {};
                 for (int r = 0; r < S; ++r)
@@ -302,14 +358,9 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
                     for (int j = 0; j < 8; ++j) v[j] += remote(tiles + (u32)(((c + j) * BM + row) * 4), (u32)r);
                 write8<T>(G, mt * BM + row, nt * BN + c, v);
             }
+            cluster_sync();                      // the others' shared memory stays until all have read it
         }
-        cluster_sync();                          // the others' shared memory stays until all have read it
-    }
-    tc_before();
-    __syncthreads();
-    if (warp == 1) {
-        tc_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::COLS) : "memory");
+        all_done();
     }
 }
 
