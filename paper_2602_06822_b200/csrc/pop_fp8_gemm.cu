@@ -7,9 +7,13 @@
 // scale, to running sums in their registers while the tensor cores work on the next block in the other accumulator.  Tokens are the MMA's
 // 128 rows (tensor-memory lanes): a thread has one token, and its scale for a block is one number for all of its columns.
 //
-// Warp roles (384 threads, one CTA per SM, persistent over tiles of 128 tokens x BN outputs):
-//   warp 0       TMA producer (one lane): x tile and W tile of a block per stage
-//   warp 1       allocates tensor memory; one lane issues the MMAs and the commits
+// What feeds the tensor cores is shared memory: a block of a tile of 128 x 256 is 48 KB, written once and read once, which alone takes 770
+// cycles at 128 bytes a cycle where the MMAs take 512.  So with many tokens two CTAs on neighbouring SMs share a tile of 256 x 256 (cta_group::2): each has
+// its own 128 tokens, but only half of the rows of W, 32 KB a block.
+//
+// Warp roles (384 threads, one CTA per SM, persistent over tiles of CG x 128 tokens x BN outputs):
+//   warp 0       TMA producer (one lane): this CTA's part of the x and W tiles of a block per stage
+//   warp 1       allocates tensor memory; one lane (of a pair, the first CTA's) issues the MMAs and the commits
 //   warp 2       brings the scales (x's times W's) of coming blocks to shared memory, where a trip to L2 stops nobody
 //   warp 3       completes the warpgroup, whose registers go to the others
 //   warps 4..11  epilogue: warp w has lanes 32 (w % 4) .. + 31, columns of half (w - 4) / 4
@@ -29,17 +33,18 @@ constexpr int THREADS = 384, EPI_WARPS = 8;
 #define FP8_REGS_OTHERS "72"
 #define FP8_REGS_EPILOGUE "216"
 constexpr int SLOTS = 8, AHEAD = 4;              // blocks whose scales are held, and asked for at a time
+constexpr int OUT_ROW = 128 + 16, OUT_WARP = 32 * OUT_ROW;      // 128 bytes of each of a warp's rows on their way to memory, without bank conflicts
 constexpr int SMEM_LIMIT = 227 * 1024;
 constexpr u64 WAIT_BUDGET_NS = 200ull * 1000ull * 1000ull;      // per wait
 
-template <int BN> struct Tile {
-    static constexpr int STAGE_BYTES = X_BYTES + BN * fp8::BLOCK;
-    static constexpr int STAGES_FIT = (SMEM_LIMIT - 2048) / STAGE_BYTES, STAGES = STAGES_FIT < 6 ? STAGES_FIT : 6;
-    static constexpr int SMEM = STAGES * STAGE_BYTES + 1024;
+// A tile of CG CTAs: each has 128 tokens and BN / CG rows of W in its shared memory, 128 tokens x BN sums in its tensor memory.
+template <int BN, int CG> struct Tile {
+    static constexpr int W_ROWS = BN / CG, STAGE_BYTES = X_BYTES + W_ROWS * fp8::BLOCK, STAGES = 5;
+    static constexpr int OUT = STAGES * STAGE_BYTES, SMEM = OUT + EPI_WARPS * OUT_WARP + 1024;
     static constexpr u32 COLS = 2 * BN;          // two accumulators; a power of two, 32 at least
     // fp32 accumulator (bits 4-5 = 1), A and B e4m3 (bits 7-9, 10-12 = 0), both K-major, N / 8 at bit 17, M / 16 at bit 24
-    static constexpr u32 IDESC = (1u << 4) | ((u32)(BN >> 3) << 17) | ((u32)(BM >> 4) << 24);
-    static_assert(STAGES * STAGE_BYTES >= BM * BN * 4, "partial sums of a tile go where the stages were");
+    static constexpr u32 IDESC = (1u << 4) | ((u32)(BN >> 3) << 17) | ((u32)(CG * BM >> 4) << 24);
+    static_assert(SMEM <= SMEM_LIMIT - 9 * 1024 && (CG == 2 || STAGES * STAGE_BYTES >= BM * BN * 4), "partial sums of a tile go where the stages were");
 };
 
 __device__ u32 fp8_status;                       // 0, or which role gave up a wait
@@ -47,17 +52,14 @@ enum { GAVE_UP_PRODUCER = 1, GAVE_UP_MMA = 2, GAVE_UP_EPILOGUE = 3, GAVE_UP_SCAL
 
 __device__ __forceinline__ u32 smem_u32(const void* p) { return (u32)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void mbar_init(u32 bar, u32 count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
-__device__ __forceinline__ void mbar_expect_tx(u32 bar, u32 bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ void mbar_arrive(u32 bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ u32 mbar_try_wait(u32 bar, u32 parity) {
     u32 ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok;
 }
 // False when the wait has lasted too long, or another role of the CTA has given up (the caller leaves its loop).
@@ -76,21 +78,61 @@ __device__ __forceinline__ bool mbar_wait(u32 bar, u32 parity, volatile int* gav
         }
     }
 }
-__device__ __forceinline__ void tma_load(u32 dst, const CUtensorMap* map, int x, int y, u32 bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(dst), "l"(reinterpret_cast<u64>(map)), "r"(x), "r"(y), "r"(bar) : "memory");
+// The producer's and the MMAs' warp stay together, so that addresses and descriptors live in uniform registers, and one lane (`mine`) issues.
+// (With one lane in a branch of its own the four MMAs of a block took 290 cycles to issue.)
+__device__ __forceinline__ u32 elect_lane() {
+    u32 mine;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(mine));
+    return mine;
+}
+__device__ __forceinline__ void mbar_expect_tx(u32 mine, u32 bar, u32 bytes) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes), "r"(mine) : "memory");
+}
+// (of a pair: the barrier may be the other CTA's)
+template <int CG> __device__ __forceinline__ void tma_load(u32 mine, u32 dst, const CUtensorMap* map, int x, int y, u32 bar) {
+    if constexpr (CG == 1)
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t@q cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+                     ::"r"(dst), "l"(reinterpret_cast<u64>(map)), "r"(x), "r"(y), "r"(bar), "r"(mine) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t@q cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+                     ::"r"(dst), "l"(reinterpret_cast<u64>(map)), "r"(x), "r"(y), "r"(bar), "r"(mine) : "memory");
 }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void umma_f8(u32 d, u64 a, u64 b, u32 idesc, u32 accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+template <int CG> __device__ __forceinline__ void umma_f8(u32 mine, u32 d, u64 a, u64 b, u32 idesc, u32 accumulate) {
+    if constexpr (CG == 1)
+        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(mine) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(mine) : "memory");
 }
-__device__ __forceinline__ void umma_commit(u32 bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+// An arrival when every MMA issued so far has completed: at this place in the shared memory of all CTAs of the tile, or (here) of this one.
+template <int CG> __device__ __forceinline__ void umma_commit_here(u32 mine, u32 bar) {
+    if constexpr (CG == 1)
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(mine) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(mine) : "memory");
+}
+template <int CG> __device__ __forceinline__ void umma_commit(u32 mine, u32 bar) {
+    if constexpr (CG == 1)
+        umma_commit_here<1>(mine, bar);
+    else
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}"
+                     ::"r"(bar), "h"((unsigned short)3), "r"(mine) : "memory");
+}
+template <int CG> __device__ __forceinline__ void tmem_alloc(u32 slot, u32 cols) {
+    if constexpr (CG == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+}
+template <int CG> __device__ __forceinline__ void tmem_free(u32 tmem, u32 cols) {
+    if constexpr (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
 }
 // 32 consecutive columns of this thread's tensor-memory lane.
 __device__ __forceinline__ void tmem_ld32(u32 addr, float (&v)[32]) {
@@ -115,13 +157,19 @@ __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ float remote(u32 addr, u32 rank) {            // a float at the same place in another CTA's shared memory
+__device__ __forceinline__ u32 at_rank(u32 addr, u32 rank) {             // the same place in another CTA's shared memory
     u32 there;
-    float v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
+    return there;
+}
+__device__ __forceinline__ float remote(u32 addr, u32 rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at_rank(addr, rank)) : "memory");
     return v;
 }
+// An arrival at another CTA's barrier.  Nothing in memory is handed over with it (accumulators are, which tcgen05's own fences order), so it needs no
+// cluster-wide release, which would wait for the thread's stores at every block (1800 cycles of epilogue a block instead of 500).
+__device__ __forceinline__ void mbar_arrive_at(u32 bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
 __device__ __forceinline__ void put8(float* y, const float (&v)[8]) {
     reinterpret_cast<float4*>(y)[0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -136,8 +184,16 @@ __device__ __forceinline__ void put8(__nv_bfloat16* y, const float (&v)[8]) {
 
 struct GemmArgs {
     fp8::LinearArgs A;
-    int m_tiles, n_tiles, wide;                  // wide: rows of y may be written 8 elements at a time
+    int m_tiles, n_tiles, wide;                  // wide: rows of y may be written 16 bytes at a time
 };
+
+// Tiles in bands of BAND along the tokens, so that those worked on at one time share rows of x as much as rows of W.
+constexpr int BAND = 8;
+__device__ __forceinline__ void place(const GemmArgs& G, int unit, int& mt, int& nt) {
+    const int band = unit / (BAND * G.n_tiles), rest = unit - band * BAND * G.n_tiles, rows = min(BAND, G.m_tiles - band * BAND);
+    nt = rest / rows;
+    mt = band * BAND + rest - nt * rows;
+}
 
 // Eight columns of token m's row, from column n on.
 template <typename T> __device__ __forceinline__ void write8(const GemmArgs& G, int m, int n, const float (&v)[8]) {
@@ -151,11 +207,38 @@ template <typename T> __device__ __forceinline__ void write8(const GemmArgs& G, 
             if (n + j < G.A.N) y[j] = Elem<T>::from_f32(v[j]);
     }
 }
+// A warp's 32 rows (from m0 on) of 128 bytes each (from column n on), which its lanes have by rows, go to memory by lines: a row's 128 bytes are
+// written by eight lanes.  (Written straight from the registers, 16 bytes of 32 rows at a time, a tile took 10000 cycles.)
+template <typename T> __device__ __forceinline__ void write_rows(const GemmArgs& G, unsigned char* stage, int m0, int n, const float2 (&v)[64 / (int)sizeof(T)]) {
+    constexpr int N = 128 / (int)sizeof(T);
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int j = 0; j < N; j += 8) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { x[2 * i] = v[j / 2 + i].x; x[2 * i + 1] = v[j / 2 + i].y; }
+        put8(reinterpret_cast<T*>(stage + lane * OUT_ROW) + j, x);
+    }
+    __syncwarp();
+    if (G.wide && n + N <= G.A.N) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + (lane >> 3);
+            const uint4 x = *reinterpret_cast<const uint4*>(stage + r * OUT_ROW + (lane & 7) * 16);
+            if (m0 + r < G.A.M) *reinterpret_cast<uint4*>((unsigned char*)((T*)G.A.y + (long long)(m0 + r) * G.A.y_stride + n) + (lane & 7) * 16) = x;
+        }
+    } else {
+        for (int r = 0; r < 32 && m0 + r < G.A.M; ++r)
+            for (int j = lane; j < N && n + j < G.A.N; j += 32)
+                ((T*)G.A.y + (long long)(m0 + r) * G.A.y_stride + n)[j] = reinterpret_cast<const T*>(stage + r * OUT_ROW)[j];
+    }
+    __syncwarp();
+}
 
-template <typename T, int BN>
+template <typename T, int BN, int CG>
 __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                                                               const GemmArgs G, const int S) {
-    typedef Tile<BN> L;
+    typedef Tile<BN, CG> L;
     extern __shared__ unsigned char raw_smem[];
     __shared__ u32 tmem_slot;
     __shared__ int gave_up_flag;
@@ -169,28 +252,30 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
     if (threadIdx.x == 0) {
         gave_up_flag = 0;
         for (int s = 0; s < L::STAGES; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(acc_full + 8 * b, 1); mbar_init(acc_empty + 8 * b, EPI_WARPS); }
+        for (int b = 0; b < 2; ++b) { mbar_init(acc_full + 8 * b, 1); mbar_init(acc_empty + 8 * b, CG * EPI_WARPS); }
         for (int i = 0; i < SLOTS; ++i) { mbar_init(sc_full + 8 * i, 1); mbar_init(sc_empty + 8 * i, EPI_WARPS); }
         mbar_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(L::COLS) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
+    if (warp == 1) tmem_alloc<CG>(smem_u32(&tmem_slot), L::COLS);
+    __syncwarp();
     tc_before();
-    __syncthreads();
+    if (CG == 2) cluster_sync();                 // the other's barriers and tensor memory are used, too
+    else __syncthreads();
     tc_after();
     const u32 tmem = tmem_slot;
     kv::follow();
 
-    // this CTA's tiles (one, if it shares it with others) and its range of their blocks
-    const int units = G.m_tiles * G.n_tiles, rank = blockIdx.x % S, kb0 = (int)((long long)G.A.KB * rank / S), kb1 = (int)((long long)G.A.KB * (rank + 1) / S);
-    const int first = blockIdx.x / S, step = gridDim.x / S;
+    // This CTA's tiles: one, if a cluster of S shares it by blocks; of a pair, its half of them (tokens and rows of W).  The first CTA of a pair has the
+    // barriers that its MMA thread waits for.
+    const int units = G.m_tiles * G.n_tiles, group = S * CG, rank = blockIdx.x % group, first = blockIdx.x / group, step = gridDim.x / group;
+    const int kb0 = CG == 2 ? 0 : (int)((long long)G.A.KB * rank / S), kb1 = CG == 2 ? G.A.KB : (int)((long long)G.A.KB * (rank + 1) / S);
+    const int half_m = CG == 2 ? rank * BM : 0, half_w = CG == 2 ? rank * L::W_ROWS : 0;
 
-    auto all_done = [&]() {                      // the CTA's last meeting, at the end of every role
+    auto all_done = [&]() {                      // the last meeting of the tile's CTAs, at the end of every role
         tc_before();
-        asm volatile("bar.sync 0;" ::: "memory");
+        if (CG == 2) cluster_sync();
+        else asm volatile("bar.sync 0;" ::: "memory");
         tc_after();
     };
     if (warp < 4) {
@@ -198,55 +283,59 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
       // that these warps no longer have.
       asm volatile("setmaxnreg.dec.sync.aligned.u32 " FP8_REGS_OTHERS ";");
       if (warp == 0) {
-        if (lane == 0) {
-            int s = 0, issued = 0;
-            u32 ph = 0;
-            bool ok = true;
-            for (int unit = first; unit < units && ok; unit += step) {
-                const int mt = unit % G.m_tiles, nt = unit / G.m_tiles;
-                for (int kb = kb0; kb < kb1; ++kb) {
-                    ok = mbar_wait(empty + 8 * s, ph ^ 1u, gave_up, GAVE_UP_PRODUCER);
-                    if (!ok) break;
-                    const u32 dst = tiles + (u32)s * L::STAGE_BYTES, bar = full + 8 * s;
-                    mbar_expect_tx(bar, L::STAGE_BYTES);
-                    tma_load(dst, &map_x, kb * fp8::BLOCK, mt * BM, bar);
-                    tma_load(dst + X_BYTES, &map_w, kb * fp8::BLOCK, nt * BN, bar);
-                    ++issued;
-                    if (++s == L::STAGES) { s = 0; ph ^= 1u; }
-                }
+        const u32 mine = elect_lane();
+        int s = 0, issued = 0;
+        u32 ph = 0;
+        bool ok = true;
+        for (int unit = first; unit < units && ok; unit += step) {
+            int mt, nt;
+            place(G, unit, mt, nt);
+            for (int kb = kb0; kb < kb1; ++kb) {
+                ok = __all_sync(~0u, mbar_wait(empty + 8 * s, ph ^ 1u, gave_up, GAVE_UP_PRODUCER));
+                if (!ok) break;
+                const u32 dst = tiles + (u32)s * L::STAGE_BYTES, bar = CG == 2 ? at_rank(full + 8 * s, 0) : full + 8 * s;
+                if (CG == 1 || rank == 0) mbar_expect_tx(mine, full + 8 * s, CG * L::STAGE_BYTES);         // what both bring
+                tma_load<CG>(mine, dst, &map_x, kb * fp8::BLOCK, mt * CG * BM + half_m, bar);
+                tma_load<CG>(mine, dst + X_BYTES, &map_w, kb * fp8::BLOCK, nt * BN + half_w, bar);
+                ++issued;
+                if (++s == L::STAGES) { s = 0; ph ^= 1u; }
             }
-            if (!ok) {                           // copies in flight still land in this CTA's shared memory: wait for them (bounded)
-                for (int j = 1; j <= min(issued, L::STAGES); ++j) {
-                    const int sj = s - j < 0 ? s - j + L::STAGES : s - j;
-                    const u32 pj = s - j < 0 ? ph ^ 1u : ph;
-                    const u64 t0 = pop_global_ns();
-                    while (!mbar_try_wait(full + 8 * sj, pj) && pop_global_ns() - t0 < WAIT_BUDGET_NS) {}
-                }
+        }
+        // copies in flight still land in shared memory: wait for them (bounded; the first of a pair for both, as the other leaves after it)
+        if (!ok && (CG == 1 || rank == 0)) {
+            for (int j = 1; j <= min(issued, L::STAGES); ++j) {
+                const int sj = s - j < 0 ? s - j + L::STAGES : s - j;
+                const u32 pj = s - j < 0 ? ph ^ 1u : ph;
+                const u64 t0 = pop_global_ns();
+                while (!mbar_try_wait(full + 8 * sj, pj) && pop_global_ns() - t0 < WAIT_BUDGET_NS) {}
             }
         }
       } else if (warp == 1) {
-        if (lane == 0) {
+        if (CG == 1 || rank == 0) {
+            const u32 mine = elect_lane(), tm = __shfl_sync(~0u, tmem, 0);
+            const u64 dx = smem_desc(tiles), dw = smem_desc(tiles + X_BYTES);
             int s = 0, buf = 0;
             u32 ph = 0, acc_ph = 0;              // bit b: phase of accumulator b
             bool ok = true;
             for (int unit = first; unit < units && ok; unit += step) {
                 for (int kb = kb0; kb < kb1; ++kb) {
-                    ok = mbar_wait(acc_empty + 8 * buf, ((acc_ph >> buf) & 1u) ^ 1u, gave_up, GAVE_UP_MMA) && mbar_wait(full + 8 * s, ph, gave_up, GAVE_UP_MMA);
+                    ok = mbar_wait(full + 8 * s, ph, gave_up, GAVE_UP_MMA) && mbar_wait(acc_empty + 8 * buf, ((acc_ph >> buf) & 1u) ^ 1u, gave_up, GAVE_UP_MMA);
+                    ok = __all_sync(~0u, ok);
                     if (!ok) break;
                     tc_after();
-                    const u64 x = smem_desc(tiles + (u32)s * L::STAGE_BYTES), w = smem_desc(tiles + (u32)s * L::STAGE_BYTES + X_BYTES);
+                    const u64 at = (u64)(s * (L::STAGE_BYTES / 16));
 #pragma unroll
                     for (int k = 0; k < fp8::BLOCK / 32; ++k)              // K = 32 is 32 bytes along the swizzled row
-                        umma_f8(tmem + (u32)(buf * BN), x + 2ull * k, w + 2ull * k, L::IDESC, k > 0);
-                    umma_commit(empty + 8 * s);
-                    umma_commit(acc_full + 8 * buf);
+                        umma_f8<CG>(mine, tm + (u32)(buf * BN), dx + at + 2ull * k, dw + at + 2ull * k, L::IDESC, k > 0);
+                    umma_commit<CG>(mine, empty + 8 * s);
+                    umma_commit<CG>(mine, acc_full + 8 * buf);
                     acc_ph ^= 1u << buf;
                     buf ^= 1;
                     if (++s == L::STAGES) { s = 0; ph ^= 1u; }
                 }
             }
             // nothing of this CTA may still run on the tensor cores when tensor memory is given back
-            umma_commit(drain);
+            umma_commit_here<CG>(mine, drain);
             const u64 t0 = pop_global_ns();
             while (!mbar_try_wait(drain, 0u) && pop_global_ns() - t0 < WAIT_BUDGET_NS) {}
         }
@@ -256,7 +345,9 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
         u32 ph = 0;
         bool ok = true;
         for (int unit = first; unit < units && ok; unit += step) {
-            const int m0 = unit % G.m_tiles * BM, n0 = unit / G.m_tiles * BN;
+            int mt, nt;
+            place(G, unit, mt, nt);
+            const int m0 = mt * CG * BM + half_m, n0 = nt * BN;
             const float* ws[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) ws[h] = G.A.ws + (size_t)min((n0 + h * (BN / 2)) / fp8::BLOCK, (G.A.N - 1) / fp8::BLOCK) * G.A.KB;
@@ -292,7 +383,7 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
           cluster_sync();                        // and have been read
       }
       all_done();
-      if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::COLS) : "memory");
+      if (warp == 1) tmem_free<CG>(tmem, L::COLS);
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 " FP8_REGS_EPILOGUE ";");
         constexpr int HALF = BN / 2;
@@ -302,7 +393,8 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
         u32 acc_ph = 0, slot_ph = 0;
         bool ok = true;
         for (int unit = first; unit < units && ok; unit += step) {
-            const int mt = unit % G.m_tiles, nt = unit / G.m_tiles, m = mt * BM + row, n0 = nt * BN + half * HALF;
+            int mt, nt;
+            place(G, unit, mt, nt);
             float2 acc[HALF / 2];
 #pragma unroll
             for (int j = 0; j < HALF / 2; ++j) acc[j] = make_float2(0.f, 0.f);
@@ -322,7 +414,8 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
                 tc_before();
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive(acc_empty + 8 * buf);
+                    if (CG == 2) mbar_arrive_at(at_rank(acc_empty + 8 * buf, 0));
+                    else mbar_arrive(acc_empty + 8 * buf);
                     mbar_arrive(sc_empty + 8 * slot);
                 }
                 acc_ph ^= 1u << buf;
@@ -331,12 +424,14 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
             }
             if (!ok) break;
             if (S == 1) {
+                constexpr int N = 128 / (int)sizeof(T);
+                unsigned char* stage = raw_smem + (tiles - smem_u32(raw_smem)) + L::OUT + (warp - 4) * OUT_WARP;
 #pragma unroll
-                for (int j = 0; j < HALF; j += 8) {
-                    float v[8];
+                for (int j = 0; j < HALF; j += N) {
+                    float2 v[N / 2];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) { v[2 * i] = acc[j / 2 + i].x; v[2 * i + 1] = acc[j / 2 + i].y; }
-                    write8<T>(G, m, n0 + j, v);
+                    for (int i = 0; i < N / 2; ++i) v[i] = acc[j / 2 + i];
+                    write_rows<T>(G, stage, mt * CG * BM + half_m + quarter * 32, nt * BN + half * HALF + j, v);
                 }
             } else {                             // partial sums, by columns, where the stages were (all of them have been used)
                 float* part = reinterpret_cast<float*>(raw_smem + (tiles - smem_u32(raw_smem)));
@@ -350,13 +445,15 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
         __syncwarp();
         if (S > 1) {                             // one tile a cluster; rank r finishes columns [r, r + 1) BN / S, a multiple of 16 of them
             cluster_sync();
-            const int cols = BN / S / 2, c0 = rank * (BN / S) + half * cols, mt = first % G.m_tiles, nt = first / G.m_tiles;
+            const int cols = BN / S / 2, c0 = rank * (BN / S) + half * cols, m = row;
+            int mt, nt;
+            place(G, first, mt, nt);
             for (int c = c0; c < c0 + cols; c += 8) {
                 float v[8] = {};
                 for (int r = 0; r < S; ++r)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v[j] += remote(tiles + (u32)(((c + j) * BM + row) * 4), (u32)r);
-                write8<T>(G, mt * BM + row, nt * BN + c, v);
+                write8<T>(G, mt * BM + m, nt * BN + c, v);
             }
             cluster_sync();                      // the others' shared memory stays until all have read it
         }
@@ -391,46 +488,45 @@ int make_map(CUtensorMap* map, const void* codes, int rows, int K, int box_rows)
     return POP_OK;
 }
 
-template <typename T, int BN> int launch(const fp8::LinearArgs& A, int S, int sms, cudaStream_t st) {
-    typedef Tile<BN> L;
+template <typename T, int BN, int CG> int launch(const fp8::LinearArgs& A, int S, int sms, cudaStream_t st) {
+    typedef Tile<BN, CG> L;
     CUtensorMap mx, mw;
     int rc = make_map(&mx, A.x, A.M, A.K, BM);
-    if (rc == POP_OK) rc = make_map(&mw, A.w, A.N, A.K, BN);
+    if (rc == POP_OK) rc = make_map(&mw, A.w, A.N, A.K, L::W_ROWS);
     if (rc != POP_OK) return rc;
     static thread_local int ready = -1;
     int device = 0;
     POP_CUDA(cudaGetDevice(&device));
     if (ready != device) {
-        POP_CUDA(cudaFuncSetAttribute(fp8_gemm_kernel<T, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM));
+        POP_CUDA(cudaFuncSetAttribute(fp8_gemm_kernel<T, BN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM));
         ready = device;
     }
-    GemmArgs G = {A, (A.M + BM - 1) / BM, (A.N + BN - 1) / BN, 0};
+    GemmArgs G = {A, (A.M + CG * BM - 1) / (CG * BM), (A.N + BN - 1) / BN, 0};
     G.wide = ((uintptr_t)A.y & 15u) == 0 && (A.y_stride * (long long)sizeof(T)) % 16 == 0;
     if ((long long)G.m_tiles * G.n_tiles > 0x3fffffffll) return POP_ERR_UNSUPPORTED;
     const int units = G.m_tiles * G.n_tiles;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(S > 1 ? units * S : (units < sms ? units : sms));
+    cfg.gridDim = dim3(S > 1 ? units * S : CG * (units < sms / CG ? units : sms / CG));
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = L::SMEM;
     cfg.stream = st;
     cudaLaunchAttribute attr[2] = {kv::following()};
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = S;
+    attr[1].val.clusterDim.x = S * CG;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = S > 1 ? 2 : 1;
-    POP_CUDA(cudaLaunchKernelEx(&cfg, fp8_gemm_kernel<T, BN>, mx, mw, G, S));
+    cfg.numAttrs = S * CG > 1 ? 2 : 1;
+    POP_CUDA(cudaLaunchKernelEx(&cfg, fp8_gemm_kernel<T, BN, CG>, mx, mw, G, S));
     POP_LAUNCHED();
     return POP_OK;
 }
 
 template <typename T> int choose(const fp8::LinearArgs& A, int sms, cudaStream_t st) {
-    const long long m_tiles = (A.M + BM - 1) / BM;
-    auto tiles = [&](int bn) { return m_tiles * ((A.N + bn - 1) / bn); };
-    if (tiles(256) >= sms) return launch<T, 256>(A, 1, sms, st);
+    const long long m_tiles = (A.M + BM - 1) / BM, tiles = m_tiles * ((A.N + 127) / 128);
+    if (A.M > BM && tiles >= 2 * sms) return launch<T, 256, 2>(A, 1, sms, st);
     int S = 1;                                   // CTAs to a tile: as many as fill the machine, each with two blocks at least
-    while (S < 8 && tiles(128) * (2 * S) <= sms && A.KB >= 4 * S) S *= 2;
-    return launch<T, 128>(A, S, sms, st);
+    while (S < 8 && tiles * (2 * S) <= sms && A.KB >= 4 * S) S *= 2;
+    return launch<T, 128, 1>(A, S, sms, st);
 }
 
 }  // namespace
