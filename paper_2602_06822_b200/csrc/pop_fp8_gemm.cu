@@ -134,9 +134,8 @@ template <int CG> __device__ __forceinline__ void tmem_free(u32 tmem, u32 cols) 
     if constexpr (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
     else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
 }
-// 32 consecutive columns of this thread's tensor-memory lane.
-__device__ __forceinline__ void tmem_ld32(u32 addr, float (&v)[32]) {
-    u32 r[32];
+// 32 consecutive columns of this thread's tensor-memory lane; the registers are valid after tmem_wait().
+__device__ __forceinline__ void tmem_ld32(u32 addr, u32 (&r)[32]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
         "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
@@ -145,10 +144,15 @@ __device__ __forceinline__ void tmem_ld32(u32 addr, float (&v)[32]) {
           "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
           "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
           "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(addr) : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+        : "r"(addr));
+}
+// All loads so far have arrived.  (The registers are named so that nothing reads them before.)
+__device__ __forceinline__ void tmem_wait(u32 (&r)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+          "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+          "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+          "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
 }
 // K-major tile of 128-byte rows in the 128-byte swizzle: groups of 8 rows are 1024 bytes apart, descriptor version 1, layout type 2.
 __device__ __forceinline__ u64 smem_desc(u32 addr) { return (u64)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61); }
@@ -404,12 +408,16 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
                 if (!ok) break;
                 const float2 scale = make_float2(scales[slot][half][row], scales[slot][half][row]);
                 tc_after();
+                // a load is under way while the one before it is added
+                u32 v[2][32];
+                tmem_ld32(at + (u32)(buf * BN), v[0]);
 #pragma unroll
                 for (int p = 0; p < HALF / 32; ++p) {
-                    float v[32];
-                    tmem_ld32(at + (u32)(buf * BN + 32 * p), v);
+                    tmem_wait(v[p & 1]);
+                    if (p + 1 < HALF / 32) tmem_ld32(at + (u32)(buf * BN + 32 * (p + 1)), v[(p + 1) & 1]);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[16 * p + j] = __ffma2_rn(make_float2(v[2 * j], v[2 * j + 1]), scale, acc[16 * p + j]);
+                    for (int j = 0; j < 16; ++j)
+                        acc[16 * p + j] = __ffma2_rn(make_float2(__uint_as_float(v[p & 1][2 * j]), __uint_as_float(v[p & 1][2 * j + 1])), scale, acc[16 * p + j]);
                 }
                 tc_before();
                 __syncwarp();
