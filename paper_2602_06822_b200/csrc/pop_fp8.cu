@@ -21,19 +21,41 @@ template <int E> __device__ __forceinline__ void put_codes(unsigned char* to, co
     else *reinterpret_cast<uint2*>(to) = make_uint2(c[0], c[1]);
 }
 
-template <typename T> __global__ void __launch_bounds__(256) quantise_rows_kernel(const T* x, long long stride, int rows, int K, int KB, unsigned char* codes, float* scales) {
+// A CTA has 256 / LANES rows and V blocks of each: the rows' scales of a block lie side by side, and with V = 4 a thread has four loads on their
+// way.
+template <typename T, int V>
+__global__ void __launch_bounds__(256) quantise_rows_kernel(const T* x, long long stride, int rows, int K, int KB, unsigned char* codes, float* scales) {
     constexpr int E = Vec<T>::E, LANES = fp8::BLOCK / E;
     kv::follow();
-    const long long task = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;      // a block of a row
-    const int row = (int)(task / KB), kb = (int)(task - (long long)row * KB), at = kb * fp8::BLOCK + (threadIdx.x % LANES) * E;
-    const bool in = row < rows && at < K;
-    float v[E] = {};
-    if (in) Vec<T>::open(__ldcs(reinterpret_cast<const uint4*>(x + (long long)row * stride + at)), v);
-    u32 c[E / 4];
-    const float scale = fp8::quantise_row(v, c);
-    if (!in) return;
-    put_codes<E>(codes + (size_t)row * K + at, c);
-    if (threadIdx.x % LANES == 0) scales[(size_t)kb * rows + row] = scale;
+    const u32 groups = (u32)(KB + V - 1) / V;
+    const int row = (int)(blockIdx.x / groups) * (256 / LANES) + threadIdx.x / LANES, kb0 = (int)(blockIdx.x % groups) * V;
+    const int at = kb0 * fp8::BLOCK + (threadIdx.x % LANES) * E;
+    const T* from = x + (long long)row * stride + at;
+    uint4 raw[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        raw[v] = make_uint4(0u, 0u, 0u, 0u);
+        if (row < rows && at + v * fp8::BLOCK < K) raw[v] = __ldcs(reinterpret_cast<const uint4*>(from + v * fp8::BLOCK));
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        float f[E];
+        Vec<T>::open(raw[v], f);
+        u32 c[E / 4];
+        const float scale = fp8::quantise_row(f, c);
+        if (row >= rows || at + v * fp8::BLOCK >= K) continue;
+        put_codes<E>(codes + (size_t)row * K + at + v * fp8::BLOCK, c);
+        if (threadIdx.x % LANES == 0) scales[(size_t)(kb0 + v) * rows + row] = scale;
+    }
+}
+template <typename T> cudaError_t quantise_rows(const void* x, long long stride, int rows, int K, unsigned char* codes, float* scales, cudaStream_t st) {
+    constexpr int ROWS = 256 / (fp8::BLOCK / Vec<T>::E);
+    const int KB = fp8::blocks(K);
+    const long long tiles = ((long long)rows + ROWS - 1) / ROWS;
+    if (tiles * KB < 2048)                                   // few: every block's load at once, over as many SMs as there are
+        return kv::launch(quantise_rows_kernel<T, 1>, dim3((u32)(tiles * KB)), 256, st, (const T*)x, stride, rows, K, KB, codes, scales);
+    if (tiles * ((KB + 3) / 4) > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+    return kv::launch(quantise_rows_kernel<T, 4>, dim3((u32)(tiles * ((KB + 3) / 4))), 256, st, (const T*)x, stride, rows, K, KB, codes, scales);
 }
 
 // Weights: a CTA has a block of 128 x 128.
@@ -205,15 +227,13 @@ extern "C" int pop_fp8_quantize(const void* x, long long x_stride, int rows, int
     rc = check_x(x, x_stride, K, dtype);
     if (rc != POP_OK) return rc;
     if (!codes || !scales || ((uintptr_t)codes & 15u) != 0 || ((uintptr_t)scales & 3u) != 0) return POP_ERR_INVALID_ARG;
-    const int KB = fp8::blocks(K), lanes = fp8::BLOCK / (dtype == POP_F32 ? 4 : 8);
-    const long long ctas = block_rows == 1 ? ((long long)rows * KB + 256 / lanes - 1) / (256 / lanes) : (long long)fp8::blocks(rows) * KB;
-    if (ctas > 0x7fffffffll) return POP_ERR_UNSUPPORTED;
+    const int KB = fp8::blocks(K);
+    if ((long long)fp8::blocks(rows) * KB > 0x3fffffffll) return POP_ERR_UNSUPPORTED;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const dim3 grid((u32)ctas);
+    const dim3 grid((u32)(fp8::blocks(rows) * KB));
     unsigned char* to = (unsigned char*)codes;
     if (block_rows == 1) {
-        if (dtype == POP_BF16) POP_CUDA(kv::launch(quantise_rows_kernel<__nv_bfloat16>, grid, 256, st, (const __nv_bfloat16*)x, x_stride, rows, K, KB, to, scales));
-        else POP_CUDA(kv::launch(quantise_rows_kernel<float>, grid, 256, st, (const float*)x, x_stride, rows, K, KB, to, scales));
+        POP_CUDA((dtype == POP_BF16 ? quantise_rows<__nv_bfloat16>(x, x_stride, rows, K, to, scales, st) : quantise_rows<float>(x, x_stride, rows, K, to, scales, st)));
     } else if (dtype == POP_BF16) {
         quantise_blocks_kernel<<<grid, 256, 0, st>>>((const __nv_bfloat16*)x, x_stride, rows, K, KB, to, scales);
     } else {

@@ -28,10 +28,11 @@ struct Window {
         return i < 16 ? a : b;
     }
 };
-__device__ __forceinline__ Window look(const SlotArgs& S, int t0) {
+// (a token whose position is negative has no slot, either, where positions are given)
+__device__ __forceinline__ Window look(const SlotArgs& S, int t0, const int32_t* positions = nullptr) {
     const int lane = threadIdx.x & 31;
     auto get = [&](int t) -> long long {
-        const long long s = t >= 0 && t < S.T ? S.slots[t] : -1;
+        const long long s = t >= 0 && t < S.T && (!positions || positions[t] >= 0) ? S.slots[t] : -1;
         return s >= 0 && s < S.n_slots ? s : -1;
     };
     Window w;

@@ -174,6 +174,161 @@ template <typename T, int G> __global__ void __launch_bounds__(256) rope_append_
     }
 }
 
+// Many tokens: a CTA has a window of 16 tokens, whose angles it works out once for all heads.  A warp's task is eight tokens of HEADS query
+// heads, or the window's keys (or values) of one head, which go to the cache as whole tiles where they are some (see the kernels of pop_kv_append).
+// Four lanes have a token's head: 8 dimensions of each half of each group, so that a pair is one lane's where 64 or 128 dimensions are rotated, or
+// pairs are neighbours; other calls are left to the kernel above.
+constexpr int WARPS = 8, WINDOW = 16, HEADS = 2;
+constexpr int MANY = 128;                        // tokens of a call from which on windows are worth it
+
+// Where the angles of a pair stand in a token's row of the table: without bank conflicts for four lanes that each read eight pairs.
+template <bool INTERLEAVED> __device__ __forceinline__ int table_at(int pair) {
+    return INTERLEAVED ? pair : (pair & ~31) + (pair & 6) * 4 + (pair >> 3 & 3) * 2 + (pair & 1);
+}
+template <int G, bool INTERLEAVED> __device__ __forceinline__ void rotate_pieces(float (&x)[2 * G][8], const float2* cs, int pairs, int e) {
+#pragma unroll
+    for (int p = 0; p < (INTERLEAVED ? 2 * G : G); ++p) {
+        if (!INTERLEAVED && p >= pairs / 32) break;
+        const bool across = !INTERLEAVED && G == 2 && pairs == 64;          // the pair's other element is in the other group, else in the other half
+#pragma unroll
+        for (int j = 0; j < (INTERLEAVED ? 4 : 8); j += 2) {
+            const int pair = INTERLEAVED ? p * 16 + e * 4 + j : p * 32 + e * 8 + j;
+            if (INTERLEAVED && pair >= pairs) break;
+            const float4 c = *reinterpret_cast<const float4*>(cs + table_at<INTERLEAVED>(pair));
+            if (INTERLEAVED) {
+                rotate(x[p][2 * j], x[p][2 * j + 1], make_float2(c.x, c.y));
+                if (pair + 1 < pairs) rotate(x[p][2 * j + 2], x[p][2 * j + 3], make_float2(c.z, c.w));
+            } else if (across) {
+                rotate(x[p][j], x[p + 2 < 2 * G ? p + 2 : 0][j], make_float2(c.x, c.y));
+                rotate(x[p][j + 1], x[p + 2 < 2 * G ? p + 2 : 0][j + 1], make_float2(c.z, c.w));
+            } else {
+                rotate(x[0][j], x[1][j], make_float2(c.x, c.y));
+                rotate(x[0][j + 1], x[1][j + 1], make_float2(c.z, c.w));
+            }
+        }
+    }
+}
+
+template <typename T, int G, bool INTERLEAVED> __global__ void __launch_bounds__(WARPS * 32, 2) rope_append_kernel(const AppendArgs P) {
+    constexpr int D = 64 * G, WORDS = kv::tile_bytes(D) / 4, PIECES = 2 * G;
+    __shared__ __align__(16) float2 table[2 * WINDOW][D / 2 + 8];
+    __shared__ uint4 codes[WARPS][G * 32];
+    __shared__ u32 scales[WARPS][WINDOW * G];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pairs = P.A.pairs, t0 = blockIdx.x * WINDOW, Hk = P.S.H;
+    const kv::Window w = kv::look(P.S, t0, P.A.positions);
+    const int first = w.whole ? __ffs(w.whole) - 1 : 0;                      // (the same in all warps)
+    for (int i = threadIdx.x; i < (WINDOW + first) * pairs; i += WARPS * 32) {
+        const int t = i / pairs, pair = i - t * pairs, p = t0 + t < P.A.T ? P.A.positions[t0 + t] : -1;
+        table[t][table_at<INTERLEAVED>(pair)] = p >= 0 ? turn(P.A, p, pair) : make_float2(1.f, 0.f);
+    }
+    __syncthreads();
+    const int q_tasks = (P.Hq + HEADS - 1) / HEADS, tasks = 2 * Hk + 2 * q_tasks, e = lane & 3;
+    for (int task = blockIdx.y * WARPS + warp; task < tasks; task += gridDim.y * WARPS) {
+        if (task >= 2 * Hk) {
+            const int rest = task - 2 * Hk, half = rest >= q_tasks, h0 = (rest - half * q_tasks) * HEADS, row = half * 8 + lane / 4, t = t0 + row;
+            const bool there = t < P.A.T && P.A.positions[t] >= 0;
+            kv::Raw8<T> raw[HEADS][PIECES];
+#pragma unroll
+            for (int h = 0; h < HEADS; ++h)
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p) {
+                    raw[h][p] = kv::no_raw<T>();
+                    if (there && h0 + h < P.Hq) raw[h][p] = kv::load_raw((const T*)P.q + (long long)t * P.qs + (size_t)(h0 + h) * D + 32 * p + 8 * e);
+                }
+#pragma unroll
+            for (int h = 0; h < HEADS; ++h) {
+                float x[PIECES][8];
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p) kv::values_of(raw[h][p], x[p]);
+                rotate_pieces<G, INTERLEAVED>(x, table[row], pairs, e);
+                if (there && h0 + h < P.Hq) {
+#pragma unroll
+                    for (int p = 0; p < PIECES; ++p) kv::put8((T*)P.q_out + (long long)t * P.qos + (size_t)(h0 + h) * D + 32 * p + 8 * e, x[p]);
+                }
+            }
+            continue;
+        }
+        const int value = task >= Hk, h = task - value * Hk;
+        const T* from = (value ? (const T*)P.v : (const T*)P.k) + (size_t)h * D + 8 * e;
+        const long long stride = value ? P.vs : P.ks;
+        kv::Raw8<T> raw[2][PIECES];
+        auto fetch = [&](int begin) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int t = t0 + begin + 8 * i + lane / 4;
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p) {
+                    raw[i][p] = kv::no_raw<T>();
+                    if (t < P.A.T) raw[i][p] = kv::load_raw(from + (long long)t * stride + 32 * p);
+                }
+            }
+        };
+        // codes (a word for each of a lane's pieces) and parameters of token `row` of the window, which step i of the fetch has
+        auto quantised = [&](int i, int row, u32 (&word)[PIECES], u32 (&params)[G]) {
+            float x[PIECES][8];
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) kv::values_of(raw[i][p], x[p]);
+            if (!value) rotate_pieces<G, INTERLEAVED>(x, table[row], pairs, e);
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                kv::Raw8<float> r[2];
+                u32 two[2];
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const float* v = x[2 * g + p] + 4 * j;
+                        r[p].v[j] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+                    }
+                kv::quantise(r, two, params[g]);
+                word[2 * g] = two[0];
+                word[2 * g + 1] = two[1];
+            }
+        };
+        fetch(0);
+        u32 word[PIECES], params[G];
+        if (w.loose) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int n = 8 * i + lane / 4;
+                quantised(i, n, word, params);
+                const long long slot = w.slot(n);
+                if (w.loose >> n & 1u) {
+                    u32* to = P.S.pages + kv::tile_base(P.S, slot, h, WORDS);
+#pragma unroll
+                    for (int p = 0; p < PIECES; ++p) to[kv::word_at<G>((int)slot & 15, value, p / 2, e + 4 * (p & 1))] = word[p];
+                    if (e == 0) {
+#pragma unroll
+                        for (int g = 0; g < G; ++g) to[kv::param_at<G>((int)slot & 15, value, g)] = params[g];
+                    }
+                }
+            }
+        }
+        if (w.whole) {                               // (one run: the next one begins 16 tokens further)
+            if (first) fetch(first);
+            u32* to = reinterpret_cast<u32*>(codes[warp]);
+            __syncwarp();                            // the task before has read its codes
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int n = 8 * i + lane / 4;
+                quantised(i, first + n, word, params);
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p)
+                    to[p / 2 * kv::GROUP_WORDS + (value ? kv::value_word(n, e + 4 * (p & 1)) : kv::key_word(n, e + 4 * (p & 1)))] = word[p];
+                if (e == 0) {
+#pragma unroll
+                    for (int g = 0; g < G; ++g) scales[warp][n * G + g] = params[g];
+                }
+            }
+            __syncwarp();
+            u32* tile = P.S.pages + kv::tile_base(P.S, w.slot(first), h, WORDS);
+#pragma unroll
+            for (int g = 0; g < G; ++g) reinterpret_cast<uint4*>(tile + (value ? kv::value_words(G) : 0))[g * 32 + lane] = codes[warp][g * 32 + lane];
+            if (lane < WINDOW * G) tile[kv::param_at<G>(lane / G, value, lane % G)] = scales[warp][lane];
+        }
+    }
+}
+
 int check_rope(const pop_rope_t* r, int head_dim) {
     if (!r || !r->freq || r->rot_dim <= 0 || r->rot_dim % 2 != 0 || head_dim <= 0 || head_dim % 2 != 0 || r->rot_dim > head_dim) return POP_ERR_INVALID_ARG;
     if (((uintptr_t)r->freq & 7u) != 0 || !(r->magnitude == r->magnitude)) return POP_ERR_INVALID_ARG;
@@ -196,6 +351,16 @@ template <typename T> cudaError_t rope(RopeArgs R, bool vectors, cudaStream_t st
 }
 
 template <typename T, int G> cudaError_t append(const AppendArgs& P, cudaStream_t st) {
+    const int rot = 2 * P.A.pairs;
+    if (P.A.T >= MANY && (P.interleaved || rot == 64 || rot == 128)) {
+        const int windows = (P.A.T + WINDOW - 1) / WINDOW, tasks = 2 * P.S.H + 2 * ((P.Hq + HEADS - 1) / HEADS);
+        int parts = (1024 + windows - 1) / windows;          // some seven CTAs to an SM, as long as each warp has a task
+        parts = parts > (tasks + WARPS - 1) / WARPS ? (tasks + WARPS - 1) / WARPS : parts;
+        const dim3 grid(windows, parts);
+        if (P.interleaved) rope_append_kernel<T, G, true><<<grid, WARPS * 32, 0, st>>>(P);
+        else rope_append_kernel<T, G, false><<<grid, WARPS * 32, 0, st>>>(P);
+        return cudaGetLastError();
+    }
     const int items = (P.Hq + 2 * P.S.H) * 8 * G, parts = P.A.T >= 512 ? 1 : (items + 255) / 256;
     return kv::launch(rope_append_few_kernel<T, G>, dim3(P.A.T, parts < 65535 ? parts : 65535), 256, st, P);
 }
