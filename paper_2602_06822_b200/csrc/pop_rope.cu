@@ -179,7 +179,9 @@ template <typename T, int G> __global__ void __launch_bounds__(256) rope_append_
 // Four lanes have a token's head: 8 dimensions of each half of each group, so that a pair is one lane's where 64 or 128 dimensions are rotated, or
 // pairs are neighbours; other calls are left to the kernel above.
 constexpr int WARPS = 8, WINDOW = 16, HEADS = 2;
-constexpr int MANY = 128;                        // tokens of a call from which on windows are worth it
+// Elements of a call from which on windows are worth it (bf16, 48 heads of 128, 64 | 256 | 1024 tokens: 3.9 | 6.2 | 9.8 us in windows, 3.2 | 6.3 | 14.4 token by
+// token; 20 heads of 64, 512 | 1024 tokens: 4.5 | 4.9 and 3.9 | 5.6).
+constexpr long long MANY = 1 << 20;
 
 // Where the angles of a pair stand in a token's row of the table: without bank conflicts for four lanes that each read eight pairs.
 template <bool INTERLEAVED> __device__ __forceinline__ int table_at(int pair) {
@@ -352,7 +354,7 @@ template <typename T> cudaError_t rope(RopeArgs R, bool vectors, cudaStream_t st
 
 template <typename T, int G> cudaError_t append(const AppendArgs& P, cudaStream_t st) {
     const int rot = 2 * P.A.pairs;
-    if (P.A.T >= MANY && (P.interleaved || rot == 64 || rot == 128)) {
+    if ((long long)P.A.T * (P.Hq + 2 * P.S.H) * (64 * G) >= MANY && (P.interleaved || rot == 64 || rot == 128)) {
         const int windows = (P.A.T + WINDOW - 1) / WINDOW, tasks = 2 * P.S.H + 2 * ((P.Hq + HEADS - 1) / HEADS);
         int parts = (1024 + windows - 1) / windows;          // some seven CTAs to an SM, as long as each warp has a task
         parts = parts > (tasks + WARPS - 1) / WARPS ? (tasks + WARPS - 1) / WARPS : parts;
