@@ -713,114 +713,142 @@ class KVCache:
 # current device.
 # ---------------------------------------------------------------------------------------------------------------------
 
-def _inference_only(what, *tensors):
-    """These calls have no backward pass: a gradient must not end here unnoticed."""
+def _check_tensors(what: str, stream, dtype, tensors):
+    """What the tensors of a call (or None) have to be: on the current device, whose kernels follow their addresses, of one type (if ``dtype`` is given),
+    and without a gradient, which would end here unnoticed, as the calls have no backward pass."""
+    torch = _torch()
+    here = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and t.requires_grad and _torch().is_grad_enabled():
+        if t is None:
+            continue
+        if t.get_device() != here:
+            _on_current_device(None, t)
+        if dtype is not None and t.dtype is not dtype:
+            raise TypeError(f"{what}: dtype mismatch ({t.dtype}, {dtype})")
+        if t.requires_grad and torch.is_grad_enabled():
             raise ValueError(f"{what} has no backward pass: detach() what requires a gradient, or call under torch.no_grad()")
+    if stream is not None:
+        _on_current_device(stream)
 
 
 def _matrix(t, what: str, d: Optional[int] = None) -> int:
     """Row stride (in elements) of [rows, d] whose rows are contiguous."""
-    if t.dim() != 2 or t.shape[1] == 0 or (d is not None and t.shape[1] != d):
+    if t.dim() != 2 or t.size(1) == 0 or (d is not None and t.size(1) != d):
         raise ValueError(f"{what} must be [rows, {'d' if d is None else d}]")
-    if t.shape[0] and t.shape[1] > 1 and t.stride(1) != 1:
+    if t.is_contiguous():
+        return t.size(1)
+    if t.size(1) > 1 and t.stride(1) != 1:
         raise ValueError(f"{what}: the elements of a row must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.stride(0) if t.size(0) > 1 else t.size(1)
 
 
-def _same_type(dtype, *tensors):
-    for t in tensors:
-        if t is not None and t.dtype != dtype:
-            raise TypeError("dtype mismatch")
+def _like(t):
+    """An uninitialised dense tensor of t's shape and type.  (empty_like costs half of what empty does, but keeps the strides of a slice.)"""
+    torch = _torch()
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-class Fp8Rows(NamedTuple):
-    """Activations in 8 bits: a scale for every 128 elements of a row."""
-    codes: object         # float8_e4m3fn [rows, K]
-    scales: object        # float32 [ceil(K / 128), rows]
-
-
-class Fp8Weights(NamedTuple):
-    """A weight matrix in 8 bits: a scale for every 128 x 128 elements."""
-    codes: object         # float8_e4m3fn [N, K]
-    scales: object        # float32 [ceil(N / 128), ceil(K / 128)]
-
-
 def _fp8_blocks(n: int) -> int:
-    return -(-n // POP_FP8_BLOCK)
+    return (n + POP_FP8_BLOCK - 1) // POP_FP8_BLOCK
 
 
-def _check_fp8(codes, scales, shape, what: str):
-    torch = _torch()
-    if codes.dtype != torch.float8_e4m3fn or codes.dim() != 2 or not codes.is_contiguous():
-        raise ValueError(f"{what}: codes must be a contiguous float8_e4m3fn matrix")
-    if scales.dtype != torch.float32 or tuple(scales.shape) != shape or not scales.is_contiguous():
-        raise ValueError(f"{what}: scales must be a contiguous float32 tensor {list(shape)}")
+class _Fp8:
+    """Codes (float8_e4m3fn [rows, K]) and their scales (float32), both contiguous."""
+    __slots__ = ("codes", "scales")
+
+    def __init__(self, codes, scales):
+        torch = _torch()
+        if codes.dtype is not torch.float8_e4m3fn or codes.dim() != 2 or codes.shape[1] == 0 or not codes.is_contiguous():
+            raise ValueError("codes must be a contiguous float8_e4m3fn matrix")
+        shape = self._scales_of(*codes.shape)
+        if scales.dtype is not torch.float32 or tuple(scales.shape) != shape or not scales.is_contiguous():
+            raise ValueError(f"scales must be a contiguous float32 tensor {list(shape)}")
+        self.codes, self.scales = codes, scales
+
+    @classmethod
+    def _empty(cls, rows: int, K: int, device):
+        torch = _torch()
+        self = cls.__new__(cls)
+        self.codes = torch.empty((rows, K), dtype=torch.float8_e4m3fn, device=device)
+        self.scales = torch.empty(cls._scales_of(rows, K), dtype=torch.float32, device=device)
+        return self
 
 
-def _fp8_quantize(x, block_rows: int, shape, stream):
-    torch = _torch()
+class Fp8Rows(_Fp8):
+    """Activations in 8 bits: ``codes`` float8_e4m3fn [rows, K], ``scales`` float32 [ceil(K / 128), rows], one for every 128 elements of a row."""
+    __slots__ = ()
+
+    @staticmethod
+    def _scales_of(rows, K):
+        return (_fp8_blocks(K), rows)
+
+
+class Fp8Weights(_Fp8):
+    """A weight matrix in 8 bits: ``codes`` float8_e4m3fn [N, K], ``scales`` float32 [ceil(N / 128), ceil(K / 128)], one for every 128 x 128 elements."""
+    __slots__ = ()
+
+    @staticmethod
+    def _scales_of(rows, K):
+        return (_fp8_blocks(rows), _fp8_blocks(K))
+
+
+def _fp8_quantize(kind, x, block_rows: int, stream):
     stride = _matrix(x, "x")
-    _on_current_device(stream, x)
-    _inference_only("fp8_quantize", x)
-    rows, K = x.shape
-    codes = torch.empty(rows, K, dtype=torch.float8_e4m3fn, device=x.device)
-    scales = torch.empty(shape, dtype=torch.float32, device=x.device)
-    _check(lib().pop_fp8_quantize(x.data_ptr(), stride, rows, K, _dtype_code(x), block_rows, codes.data_ptr(), scales.data_ptr(), _stream_ptr(stream)),
-           "pop_fp8_quantize")
-    _used_on(stream, codes, scales)
-    return codes, scales
+    _check_tensors("fp8_quantize", stream, None, (x,))
+    out = kind._empty(x.shape[0], x.shape[1], x.device)
+    _check(lib().pop_fp8_quantize(x.data_ptr(), stride, x.shape[0], x.shape[1], _dtype_code(x), block_rows, out.codes.data_ptr(), out.scales.data_ptr(),
+                                  _stream_ptr(stream)), "pop_fp8_quantize")
+    if stream is not None:
+        _used_on(stream, out.codes, out.scales)
+    return out
 
 
 def fp8_quantize(x, stream=None) -> Fp8Rows:
     """pop_fp8_quantize of activations x [rows, K] (rows may be strided; K a multiple of 16)."""
-    return Fp8Rows(*_fp8_quantize(x, 1, (_fp8_blocks(x.shape[-1]), x.shape[0]), stream))
+    return _fp8_quantize(Fp8Rows, x, 1, stream)
 
 
 def fp8_weights(w, stream=None) -> Fp8Weights:
     """pop_fp8_quantize of a weight matrix w [N, K], once: the codes are a copy, w is not needed any more."""
-    return Fp8Weights(*_fp8_quantize(w, POP_FP8_BLOCK, (_fp8_blocks(w.shape[0]), _fp8_blocks(w.shape[-1])), stream))
+    return _fp8_quantize(Fp8Weights, w, POP_FP8_BLOCK, stream)
 
 
 def fp8_linear(x, w: Fp8Weights, out=None, dtype=None, stream=None):
     """pop_fp8_linear: x [M, K] (bf16 or fp32, quantised on the way, or Fp8Rows) times w^T -> [M, N] of ``dtype`` (x's own by default, bfloat16
     for Fp8Rows).  ``out``: rows may be strided."""
     torch = _torch()
-    wc, ws = w
-    _check_fp8(wc, ws, (_fp8_blocks(wc.shape[0]), _fp8_blocks(wc.shape[-1])), "w")
+    wc, ws = w.codes, w.scales
     N, K = wc.shape
     rows = isinstance(x, Fp8Rows)
     xc = x.codes if rows else x
-    if rows:
-        _check_fp8(xc, x.scales, (_fp8_blocks(K), xc.shape[0]), "x")
     stride = _matrix(xc, "x", K)
     M = xc.shape[0]
     made = out is None
     if made:
-        out = torch.empty(M, N, dtype=dtype if dtype is not None else torch.bfloat16 if rows else x.dtype, device=xc.device)
-    elif tuple(out.shape) != (M, N) or (dtype is not None and out.dtype != dtype):
-        raise ValueError(f"out must be [{M}, {N}] of the dtype asked for")
-    y_stride = _matrix(out, "out", N)
-    _on_current_device(stream, xc, wc, ws, out, x.scales if rows else None)
-    _inference_only("fp8_linear", xc, out)
+        out = torch.empty((M, N), dtype=dtype if dtype is not None else torch.bfloat16 if rows else x.dtype, device=wc.device)
+        y_stride = N
+    else:
+        if tuple(out.shape) != (M, N) or (dtype is not None and out.dtype is not dtype):
+            raise ValueError(f"out must be [{M}, {N}] of the dtype asked for")
+        y_stride = _matrix(out, "out", N)
+    _check_tensors("fp8_linear", stream, None, (xc, wc, ws, x.scales if rows else None, None if made else out))
     l, st = lib(), _stream_ptr(stream)
     if rows:
         _check(l.pop_fp8_linear(xc.data_ptr(), x.scales.data_ptr(), M, wc.data_ptr(), ws.data_ptr(), N, K, out.data_ptr(), y_stride, _dtype_code(out), st),
                "pop_fp8_linear")
-        if made:
+        if made and stream is not None:
             _used_on(stream, out)
         return out
-    need = C.c_size_t()
-    _check(l.pop_fp8_linear_workspace(M, K, C.byref(need)), "pop_fp8_linear_workspace")
-    workspace = torch.empty(need.value, dtype=torch.uint8, device=xc.device)
+    need = 4 * _fp8_blocks(K) * M + 16 + M * K              # pop_fp8_linear_workspace
+    workspace = torch.empty(need, dtype=torch.uint8, device=wc.device)
     _check(l.pop_fp8_linear_rows(x.data_ptr(), stride, _dtype_code(x), M, wc.data_ptr(), ws.data_ptr(), N, K, out.data_ptr(), y_stride, _dtype_code(out),
-                                 workspace.data_ptr(), need.value, st), "pop_fp8_linear_rows")
-    _used_on(stream, workspace, out if made else None)
+                                 workspace.data_ptr(), need, st), "pop_fp8_linear_rows")
+    if stream is not None:
+        _used_on(stream, workspace, out if made else None)
     return out
 
 
@@ -834,48 +862,62 @@ def block_norm(h, u=None, *, post_norm: bool = False, post_gain=None, gate=None,
     """pop_block_norm: (h', f) with h' = h_scale h + u_scale gate b, b = u or rms(u) post_gain, f = rms(h') gain.
     h, u [T, d] (rows may be strided); post_gain, gain [d]; gate [T, d], [1, d] or [d].  ``fp8``: f as Fp8Rows.  ``h_out`` receives h' (h itself, or
     another tensor; a new one by default).  Without u (and h_scale 1) h' is h, and nothing is written."""
-    torch = _torch()
     a = BlockNormArgs()
-    a.h_stride = _matrix(h, "h")
-    T, d = h.shape
+    a.h_stride = d = _matrix(h, "h")
+    shape = h.shape
+    if d != shape[1]:
+        d = shape[1]
+    a.h = h.data_ptr()
     if u is not None:
-        if u.shape != h.shape:
+        if u.shape != shape:
             raise ValueError("u must have h's shape")
         a.u_stride = _matrix(u, "u")
+        a.u = u.data_ptr()
     if gate is not None:
         if gate.dim() == 1:
             gate = gate.unsqueeze(0)
-        if gate.dim() != 2 or gate.shape[1] != d or gate.shape[0] not in (1, T):
+        if gate.dim() != 2 or gate.size(1) != d or gate.size(0) not in (1, shape[0]):
             raise ValueError("gate must be [T, d], [1, d] or [d]")
-        a.gate_stride = _matrix(gate, "gate") if gate.shape[0] == T and T > 1 else 0
-        if a.gate_stride == 0 and gate.stride(1) != 1 and d > 1:
-            raise ValueError("gate: the elements of a row must be contiguous")
-    for t in (post_gain, gain):
-        if t is not None and (tuple(t.shape) != (d,) or (d > 1 and t.stride(0) != 1)):
-            raise ValueError("gains must be contiguous tensors [d]")
-    _same_type(h.dtype, u, post_gain, gate, gain, h_out)
-    dt = _dtype_code(h)
-    made = h_out is None
-    if made:
-        h_out = h if u is None and h_scale == 1.0 else torch.empty(T, d, dtype=h.dtype, device=h.device)
-    elif h_out.shape != h.shape:
-        raise ValueError("h_out must have h's shape")
-    if h_out is not h or u is not None or h_scale != 1.0:
+        rows = _matrix(gate, "gate")
+        if gate.size(0) > 1:
+            a.gate_stride = rows
+        a.gate = gate.data_ptr()
+    if post_gain is not None:
+        a.post_gain = _gain(post_gain, d)
+    if gain is not None:
+        a.gain = _gain(gain, d)
+    if h_out is not None:
+        if h_out.shape != shape:
+            raise ValueError("h_out must have h's shape")
         a.h_out_stride = _matrix(h_out, "h_out")
+        made = False
+    elif u is None and h_scale == 1.0:
+        h_out, made = h, False
+    else:
+        h_out, made = _like(h), True
+        a.h_out_stride = d
+    if h_out is not h or u is not None or h_scale != 1.0:
         a.h_out = h_out.data_ptr()
     if fp8:
-        f = Fp8Rows(torch.empty(T, d, dtype=torch.float8_e4m3fn, device=h.device), torch.empty(_fp8_blocks(d), T, dtype=torch.float32, device=h.device))
+        f = Fp8Rows._empty(shape[0], d, h.device)
         a.f_codes, a.f_scales = f.codes.data_ptr(), f.scales.data_ptr()
     else:
-        f = torch.empty(T, d, dtype=h.dtype, device=h.device)
+        f = _like(h)
         a.f = f.data_ptr()
-    _on_current_device(stream, h, u, post_gain, gate, gain, h_out)
-    _inference_only("block_norm", h, u, post_gain, gate, gain, h_out)
-    a.h, a.u, a.post_gain, a.gate, a.gain = _ptr(h), _ptr(u), _ptr(post_gain), _ptr(gate), _ptr(gain)
-    a.h_scale, a.u_scale, a.eps, a.post_norm = h_scale, u_scale, eps, bool(post_norm)
-    _check(lib().pop_block_norm(C.byref(a), T, d, dt, _stream_ptr(stream)), "pop_block_norm")
-    _used_on(stream, *(f if fp8 else (f,)), h_out if made and h_out is not h else None)
+    _check_tensors("block_norm", stream, h.dtype, (h, u, post_gain, gate, gain, None if made else h_out))
+    a.h_scale, a.u_scale, a.eps = h_scale, u_scale, eps
+    if post_norm:
+        a.post_norm = 1
+    _check(lib().pop_block_norm(C.byref(a), shape[0], d, _dtype_code(h), _stream_ptr(stream)), "pop_block_norm")
+    if stream is not None:
+        _used_on(stream, *((f.codes, f.scales) if fp8 else (f,)), h_out if made else None)
     return h_out, f
+
+
+def _gain(t, d: int) -> int:
+    if t.dim() != 1 or t.size(0) != d or not t.is_contiguous():
+        raise ValueError("gains must be contiguous tensors [d]")
+    return t.data_ptr()
 
 
 class Rope:
@@ -905,6 +947,8 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none",
 def _rope_rows(t, dim: int, what: str):
     if t.dim() != 3 or t.shape[1] == 0:
         raise ValueError(f"{what} must be [tokens, heads, {dim}]")
+    if t.is_contiguous() and t.shape[2] == dim:
+        return t.shape[1] * dim
     return _rows(t, t.shape[1], dim, what)
 
 
@@ -920,21 +964,21 @@ def rope(rope: Rope, positions, q, k=None, inverse: bool = False, q_out=None, k_
         raise ValueError("q, k and positions must have one length")
     made = (q_out is None, k is not None and k_out is None)
     if made[0]:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = _like(q)
     if made[1]:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        k_out = _like(k)
     if q_out.shape != q.shape or (k is not None and k_out.shape != k.shape) or (k is None and k_out is not None):
         raise ValueError("outputs must have the shapes of q and k")
     qos = _rope_rows(q_out, dim, "q_out")
     ks = kos = 0
     if k is not None:
         ks, kos = _rope_rows(k, dim, "k"), _rope_rows(k_out, dim, "k_out")
-    _same_type(q.dtype, k, q_out, k_out)
-    _on_current_device(stream, rope.freq, positions, q, k, q_out, k_out)
-    _inference_only("rope", q, k, q_out, k_out)
+    _check_tensors("rope", stream, q.dtype, (q, k, q_out, k_out))
+    _check_tensors("rope", None, None, (rope.freq, positions))
     _check(lib().pop_rope(C.byref(rope.desc), int(inverse), positions.data_ptr(), T, dim, _dtype_code(q), q.data_ptr(), qs, q.shape[1], q_out.data_ptr(), qos,
                           _ptr(k), ks, 0 if k is None else k.shape[1], _ptr(k_out), kos, _stream_ptr(stream)), "pop_rope")
-    _used_on(stream, q_out if made[0] else None, k_out if made[1] else None)
+    if stream is not None:
+        _used_on(stream, q_out if made[0] else None, k_out if made[1] else None)
     return q_out if k is None else (q_out, k_out)
 
 
@@ -952,15 +996,14 @@ def kv_append_rope(pages, rope: Rope, positions, q, k, v, slots, q_out=None, str
         raise ValueError("q, k, v, positions and slots must have one length")
     made = q_out is None
     if made:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = _like(q)
     elif q_out.shape != q.shape:
         raise ValueError("q_out must have q's shape")
     qos = _rope_rows(q_out, D, "q_out")
-    _same_type(q.dtype, k, v, q_out)
-    _on_current_device(stream, pages, rope.freq, positions, q, k, v, slots, q_out)
-    _inference_only("kv_append_rope", q, k, v, q_out)
+    _check_tensors("kv_append_rope", stream, q.dtype, (q, k, v, q_out))
+    _check_tensors("kv_append_rope", None, None, (pages, rope.freq, positions, slots))
     _check(lib().pop_kv_append_rope(C.byref(desc), C.byref(rope.desc), positions.data_ptr(), q.data_ptr(), qs, q.shape[1], q_out.data_ptr(), qos,
                                     k.data_ptr(), ks, v.data_ptr(), vs, _dtype_code(q), slots.data_ptr(), T, _stream_ptr(stream)), "pop_kv_append_rope")
-    if made:
+    if made and stream is not None:
         _used_on(stream, q_out)
     return q_out

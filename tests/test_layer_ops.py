@@ -159,7 +159,8 @@ def test_quantise_equals_the_oracle(rows, K, dtype):
         x[3], x[4] = 0, 1e-39
     x = x[:, :K]
     for block_rows, fn in ((1, pop.fp8_quantize), (128, pop.fp8_weights)):
-        codes, scales = fn(x)
+        q = fn(x)
+        codes, scales = q.codes, q.scales
         want_c, want_s = lo.quantise(host(x), block_rows)
         np.testing.assert_array_equal(scales.cpu().numpy(), want_s)
         got = codes.view(torch.uint8).cpu().numpy()
@@ -475,7 +476,8 @@ def test_calls_on_another_stream():
     got = (pop.block_norm(y, y, stream=s), pop.fp8_linear(y, w, stream=s), pop.rope(r, pos, y.view(300, 8, 64), stream=s), pop.fp8_quantize(y, stream=s))
     s.synchronize()
     for a, b in zip(want, got):
-        for p, q in zip(a if isinstance(a, tuple) else (a,), b if isinstance(b, tuple) else (b,)):
+        parts = lambda v: v if isinstance(v, tuple) else (v.codes, v.scales) if isinstance(v, pop.Fp8Rows) else (v,)      # noqa: E731
+        for p, q in zip(parts(a), parts(b)):
             assert torch.equal(p.view(torch.uint8), q.view(torch.uint8))
 
 
