@@ -1,4 +1,4 @@
-// 8-bit floating point: the quantisers, the product for few tokens, argument checks and the choice of kernels.
+// 8-bit floating point: the quantisers, argument checks and the choice of the product's kernels.
 #include "pop_fp8.cuh"
 
 namespace {
@@ -103,190 +103,6 @@ template <typename T> __global__ void __launch_bounds__(256) quantise_blocks_ker
     }
 }
 
-// ------------------------------------------------------------------------------------------------- product, few tokens
-//
-// Bound by the weights' bytes, N K of them, each used for at most 16 tokens.  One CTA per SM, whose 16 warps share the blocks of 128 along K
-// and go through tiles of 8 rows of W together, their partial sums joined through shared memory after every tile.  mma.m16n8k32 takes the tokens as its
-// 16 rows and the rows of W as its 8 columns; in which order the 128 elements of a block go through its four steps does not matter as long
-// as both operands have the same, so a lane loads 16 bytes of a row of W at a time and uses them as they are.  The tokens' codes stand in
-// shared memory in that order, brought there (or worked out, where there are few elements of them) once a CTA.
-// A warp has four batches of two blocks on their way, 128 KB an SM in all.
-// A block's sum starts from zero and is scaled into the running sums in fp32.
-constexpr int STREAM_WARPS = 16, STREAM_ROWS = 8, STREAM_BATCHES = 4, STREAM_TOKENS = 16, STREAM_SMEM = 200 * 1024;
-constexpr long long STREAM_FUSED = 1 << 15;      // elements that the product's CTAs quantise for themselves
-
-__device__ __forceinline__ void mma_e4m3(float (&c)[4], u32 a0, u32 a1, u32 a2, u32 a3, u32 b0, u32 b1) {
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-// What the tokens come as: codes and scales, or values of type X to be quantised.
-struct StreamArgs {
-    fp8::LinearArgs A;
-    const void* rows;
-    long long stride;
-};
-// Shared memory: the tokens' codes, 16 bytes of every token by [block][half][token][t], their scales by [block][token], partial sums of two tiles.
-__host__ __device__ constexpr size_t stream_codes(int M, int KB) { return (size_t)M * KB * fp8::BLOCK; }
-__host__ __device__ constexpr size_t stream_scales(int M, int KB) { return ((size_t)M * KB * 4 + 15) / 16 * 16; }
-__host__ __device__ constexpr size_t stream_smem(int M, int KB) {
-    return stream_codes(M, KB) + stream_scales(M, KB) + 2 * STREAM_WARPS * (M > 8 ? 16 : 8) * STREAM_ROWS * 4;
-}
-
-template <typename X> __device__ __forceinline__ void bring_tokens(const StreamArgs& S, unsigned char* codes, float* scales) {
-    const int M = S.A.M, KB = S.A.KB, K = S.A.K;
-    if constexpr (sizeof(X) == 1) {
-        for (int i = threadIdx.x; i < M * KB * 8; i += STREAM_WARPS * 32) {
-            const int m = i / (KB * 8), c = i - m * (KB * 8);
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (c * 16 < K) v = *reinterpret_cast<const uint4*>(S.A.x + (size_t)m * K + c * 16);
-            reinterpret_cast<uint4*>(codes)[((c >> 2) * M + m) * 4 + (c & 3)] = v;
-        }
-        for (int i = threadIdx.x; i < M * KB; i += STREAM_WARPS * 32) scales[i] = S.A.xs[i];
-    } else {
-        constexpr int E = Vec<X>::E, LANES = fp8::BLOCK / E;
-        for (int i = threadIdx.x / LANES; i < M * KB; i += STREAM_WARPS * 32 / LANES) {      // (a warp's lanes leave together: M KB blocks, 2 or 1 a warp, the last alone)
-            const int m = i / KB, kb = i - m * KB, at = threadIdx.x % LANES * E, k = kb * fp8::BLOCK + at;
-            float v[E] = {};
-            if (k < K) Vec<X>::open(*reinterpret_cast<const uint4*>((const X*)S.rows + (long long)m * S.stride + k), v);
-            float top = 0.f;
-#pragma unroll
-            for (int e = 0; e < E; ++e) top = fmaxf(top, fp8::magnitude(v[e]));
-            const u32 together = LANES == 32 ? ~0u : 0xffffu << (threadIdx.x & 16);
-#pragma unroll
-            for (int o = LANES / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(together, top, o));
-            const float scale = fp8::scale_of(top), factor = fp8::factor_of(scale);
-            u32 c[E / 4];
-#pragma unroll
-            for (int j = 0; j < E / 4; ++j) c[j] = fp8::codes4(v + 4 * j, factor);
-            put_codes<E>(codes + ((size_t)(2 * kb + at / 64) * M + m) * 64 + at % 64, c);
-            if (at == 0) scales[kb * M + m] = scale;
-        }
-    }
-}
-
-template <typename X, typename Y, bool WIDE> __global__ void __launch_bounds__(STREAM_WARPS * 32, 1) fp8_stream_kernel(const StreamArgs S) {
-    extern __shared__ __align__(16) unsigned char stream_raw[];
-    const fp8::LinearArgs& A = S.A;
-    const int M = A.M, KB = A.KB, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    constexpr int TOKENS = WIDE ? 16 : 8;
-    unsigned char* codes = stream_raw;
-    float* scales = reinterpret_cast<float*>(stream_raw + stream_codes(M, KB));
-    float* sums = scales + stream_scales(M, KB) / 4;                         // [2][warps][TOKENS][rows]
-    const int tiles = (A.N + STREAM_ROWS - 1) / STREAM_ROWS, pairs = (KB + 2 * STREAM_WARPS - 1) / (2 * STREAM_WARPS);      // batches of a tile
-    const int mine = blockIdx.x < tiles ? (tiles - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0, total = mine * pairs;
-    kv::follow();
-
-    struct Batch { uint4 w[2][2]; float scale[2]; } batch[STREAM_BATCHES];
-    int next_tile = blockIdx.x, next_pair = 0, left = total;                 // what is asked for next
-    auto ask = [&](Batch& b) {
-        if (left <= 0) return;
-        --left;
-        const int row = next_tile * STREAM_ROWS + g;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int kb = (2 * next_pair + i) * STREAM_WARPS + warp;
-            const unsigned char* from = A.w + (size_t)row * A.K + kb * fp8::BLOCK + 16 * t;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                b.w[i][j] = make_uint4(0u, 0u, 0u, 0u);
-                if (row < A.N && kb * fp8::BLOCK + 64 * j + 16 * t < A.K) b.w[i][j] = __ldcs(reinterpret_cast<const uint4*>(from + 64 * j));
-            }
-            b.scale[i] = kb < KB ? __ldg(A.ws + (size_t)(next_tile * STREAM_ROWS / fp8::BLOCK) * KB + kb) : 0.f;
-        }
-        if (++next_pair == pairs) { next_pair = 0; next_tile += gridDim.x; }
-    };
-#pragma unroll
-    for (int u = 0; u < STREAM_BATCHES; ++u) ask(batch[u]);
-    bring_tokens<X>(S, codes, scales);
-    __syncthreads();
-
-    float acc[4] = {};
-    int tile = blockIdx.x, pair = 0, turn = 0;
-    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-    for (int b0 = 0; b0 < total; b0 += STREAM_BATCHES) {
-#pragma unroll
-        for (int u = 0; u < STREAM_BATCHES; ++u) {
-            if (b0 + u >= total) break;
-            Batch& b = batch[u];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int kb = (2 * pair + i) * STREAM_WARPS + warp;
-                if (kb >= KB) continue;
-                const uint4* x = reinterpret_cast<const uint4*>(codes) + (size_t)2 * kb * M * 4 + t;
-                uint4 lo[2], hi[2];
-                float s0 = 0.f, s1 = 0.f;
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    lo[j] = hi[j] = none;
-                    if (g < M) lo[j] = x[(j * M + g) * 4];
-                    if (WIDE && g + 8 < M) hi[j] = x[(j * M + g + 8) * 4];
-                }
-                if (g < M) s0 = scales[kb * M + g] * b.scale[i];
-                if (WIDE && g + 8 < M) s1 = scales[kb * M + g + 8] * b.scale[i];
-                float c[4] = {};
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    mma_e4m3(c, lo[j].x, hi[j].x, lo[j].y, hi[j].y, b.w[i][j].x, b.w[i][j].y);
-                    mma_e4m3(c, lo[j].z, hi[j].z, lo[j].w, hi[j].w, b.w[i][j].z, b.w[i][j].w);
-                }
-                acc[0] = fmaf(c[0], s0, acc[0]);
-                acc[1] = fmaf(c[1], s0, acc[1]);
-                if (WIDE) {
-                    acc[2] = fmaf(c[2], s1, acc[2]);
-                    acc[3] = fmaf(c[3], s1, acc[3]);
-                }
-            }
-            ask(b);
-            if (++pair < pairs) continue;
-            // the tile is done: rows 2 t, 2 t + 1 of tokens g and g + 8 from every warp
-            float* part = sums + turn * STREAM_WARPS * TOKENS * STREAM_ROWS;
-            reinterpret_cast<float2*>(part + (warp * TOKENS + g) * STREAM_ROWS)[t] = make_float2(acc[0], acc[1]);
-            if (WIDE) reinterpret_cast<float2*>(part + (warp * TOKENS + g + 8) * STREAM_ROWS)[t] = make_float2(acc[2], acc[3]);
-            __syncthreads();                                                 // (two buffers: the one before the last has been read)
-            const int m = threadIdx.x / STREAM_ROWS, n = tile * STREAM_ROWS + threadIdx.x % STREAM_ROWS;
-            if (m < M && n < A.N) {
-                float s = 0.f;
-#pragma unroll
-                for (int w = 0; w < STREAM_WARPS; ++w) s += part[(w * TOKENS + m) * STREAM_ROWS + threadIdx.x % STREAM_ROWS];
-                ((Y*)A.y)[(long long)m * A.y_stride + n] = Elem<Y>::from_f32(s);
-            }
-            acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
-            pair = 0;
-            tile += gridDim.x;
-            turn ^= 1;
-        }
-    }
-}
-
-template <typename X, typename Y, bool WIDE> int stream(const StreamArgs& S, int sms, cudaStream_t st) {
-    const size_t smem = stream_smem(S.A.M, S.A.KB);
-    static thread_local int ready = -1;
-    int device = 0;
-    POP_CUDA(cudaGetDevice(&device));
-    if (ready != device) {
-        POP_CUDA(cudaFuncSetAttribute(fp8_stream_kernel<X, Y, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, STREAM_SMEM));
-        ready = device;
-    }
-    const int tiles = (S.A.N + STREAM_ROWS - 1) / STREAM_ROWS;
-    cudaLaunchAttribute attr = kv::following();
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(tiles < sms ? tiles : sms);
-    cfg.blockDim = dim3(STREAM_WARPS * 32);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    POP_CUDA(cudaLaunchKernelEx(&cfg, fp8_stream_kernel<X, Y, WIDE>, S));
-    POP_LAUNCHED();
-    return POP_OK;
-}
-template <typename X> int stream(const StreamArgs& S, pop_dtype_t y_dtype, int sms, cudaStream_t st) {
-    if (S.A.M > 8) return y_dtype == POP_BF16 ? stream<X, __nv_bfloat16, true>(S, sms, st) : stream<X, float, true>(S, sms, st);
-    return y_dtype == POP_BF16 ? stream<X, __nv_bfloat16, false>(S, sms, st) : stream<X, float, false>(S, sms, st);
-}
-
 int sms_of(int* sms) {
     int device = 0;
     POP_CUDA(cudaGetDevice(&device));
@@ -348,11 +164,13 @@ extern "C" int pop_fp8_linear(const void* x_codes, const float* x_scales, int M,
     if ((uintptr_t)y & (y_dtype == POP_F32 ? 3u : 1u)) return POP_ERR_INVALID_ARG;
     const fp8::LinearArgs A = {(const unsigned char*)x_codes, (const unsigned char*)w_codes, x_scales, w_scales, M, N, K, fp8::blocks(K), y, y_stride};
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (M <= 64) {
+        rc = pop_launch_fp8_few(A, nullptr, 0, POP_BF16, y_dtype, st);
+        if (rc != POP_ERR_UNSUPPORTED) return rc;
+    }
     int sms = 0;
     rc = sms_of(&sms);
-    if (rc != POP_OK) return rc;
-    if (M <= STREAM_TOKENS && stream_smem(M, A.KB) <= STREAM_SMEM) return stream<unsigned char>({A, nullptr, 0}, y_dtype, sms, st);
-    return pop_launch_fp8_gemm(A, y_dtype, sms, st);
+    return rc != POP_OK ? rc : pop_launch_fp8_gemm(A, y_dtype, sms, st);
 }
 
 extern "C" int pop_fp8_linear_workspace(int M, int K, size_t* bytes) {
@@ -373,14 +191,13 @@ extern "C" int pop_fp8_linear_rows(const void* x, long long x_stride, pop_dtype_
     if (M == 0) return POP_OK;
     if (!w_codes || !w_scales || !y || y_stride < N || !workspace || workspace_bytes < need || ((uintptr_t)workspace & 15u) != 0) return POP_ERR_INVALID_ARG;
     if (((uintptr_t)w_codes & 15u) != 0 || ((uintptr_t)w_scales & 3u) != 0 || ((uintptr_t)y & (y_dtype == POP_F32 ? 3u : 1u))) return POP_ERR_INVALID_ARG;
+    rc = check_x(x, x_stride, K, x_dtype);
+    if (rc != POP_OK) return rc;
     const int KB = fp8::blocks(K);
-    if (M <= STREAM_TOKENS && (long long)M * K <= STREAM_FUSED && stream_smem(M, KB) <= STREAM_SMEM) {
-        rc = check_x(x, x_stride, K, x_dtype);
-        int sms = 0;
-        if (rc == POP_OK) rc = sms_of(&sms);
-        if (rc != POP_OK) return rc;
-        const StreamArgs S = {{nullptr, (const unsigned char*)w_codes, nullptr, w_scales, M, N, K, KB, y, y_stride}, x, x_stride};
-        return x_dtype == POP_BF16 ? stream<__nv_bfloat16>(S, y_dtype, sms, (cudaStream_t)cuda_stream) : stream<float>(S, y_dtype, sms, (cudaStream_t)cuda_stream);
+    if (M <= 16) {
+        const fp8::LinearArgs A = {nullptr, (const unsigned char*)w_codes, nullptr, w_scales, M, N, K, KB, y, y_stride};
+        rc = pop_launch_fp8_few(A, x, x_stride, x_dtype, y_dtype, (cudaStream_t)cuda_stream);
+        if (rc != POP_ERR_UNSUPPORTED) return rc;
     }
     float* scales = (float*)workspace;
     unsigned char* codes = (unsigned char*)workspace + (((size_t)KB * M * sizeof(float) + 15) & ~(size_t)15);

@@ -50,4 +50,7 @@ __host__ __device__ constexpr int blocks(int n) { return (n + BLOCK - 1) / BLOCK
 }  // namespace fp8
 
 // pop_fp8_gemm.cu: many tokens, on the tensor cores
+// up to 64 tokens as codes, or up to 16 as values (`rows`, not NULL) to be quantised on the way; POP_ERR_UNSUPPORTED, with nothing launched, where it does
+// not take the call (a K so long that the range of a CTA does not fit)
+int pop_launch_fp8_few(const fp8::LinearArgs& A, const void* rows, long long stride, pop_dtype_t x_dtype, pop_dtype_t y_dtype, cudaStream_t st);
 int pop_launch_fp8_gemm(const fp8::LinearArgs& A, pop_dtype_t y_dtype, int sms, cudaStream_t st);

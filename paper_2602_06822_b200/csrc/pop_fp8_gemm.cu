@@ -44,7 +44,7 @@ template <int BN, int CG> struct Tile {
     static constexpr u32 COLS = 2 * BN;          // two accumulators; a power of two, 32 at least
     // fp32 accumulator (bits 4-5 = 1), A and B e4m3 (bits 7-9, 10-12 = 0), both K-major, N / 8 at bit 17, M / 16 at bit 24
     static constexpr u32 IDESC = (1u << 4) | ((u32)(BN >> 3) << 17) | ((u32)(CG * BM >> 4) << 24);
-    static_assert(SMEM <= SMEM_LIMIT - 9 * 1024 && (CG == 2 || STAGES * STAGE_BYTES >= BM * BN * 4), "partial sums of a tile go where the stages were");
+    static_assert(SMEM <= SMEM_LIMIT - 9 * 1024 && (CG == 2 || STAGES * STAGE_BYTES >= BM * (BN + 4) * 4), "partial sums of a tile go where the stages were");
 };
 
 __device__ u32 fp8_status;                       // 0, or which role gave up a wait
@@ -96,6 +96,9 @@ template <int CG> __device__ __forceinline__ void tma_load(u32 mine, u32 dst, co
     else
         asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t@q cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
                      ::"r"(dst), "l"(reinterpret_cast<u64>(map)), "r"(x), "r"(y), "r"(bar), "r"(mine) : "memory");
+}
+__device__ __forceinline__ void prefetch_map(u32 mine, const CUtensorMap* map) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q prefetch.tensormap [%0];\n\t}" ::"l"(reinterpret_cast<u64>(map)), "r"(mine) : "memory");
 }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -166,9 +169,9 @@ __device__ __forceinline__ u32 at_rank(u32 addr, u32 rank) {             // the 
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
     return there;
 }
-__device__ __forceinline__ float remote(u32 addr, u32 rank) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at_rank(addr, rank)) : "memory");
+__device__ __forceinline__ float4 remote4(u32 addr, u32 rank) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at_rank(addr, rank)) : "memory");
     return v;
 }
 // An arrival at another CTA's barrier.  Nothing in memory is handed over with it (accumulators are, which tcgen05's own fences order), so it needs no
@@ -186,12 +189,19 @@ __device__ __forceinline__ void put8(__nv_bfloat16* y, const float (&v)[8]) {
     *reinterpret_cast<uint4*>(y) = *reinterpret_cast<const uint4*>(r);
 }
 
+__device__ __forceinline__ void put4(float* y, const float (&v)[4]) { *reinterpret_cast<float4*>(y) = make_float4(v[0], v[1], v[2], v[3]); }
+__device__ __forceinline__ void put4(__nv_bfloat16* y, const float (&v)[4]) {
+    const __nv_bfloat162 r[2] = {__floats2bfloat162_rn(v[0], v[1]), __floats2bfloat162_rn(v[2], v[3])};
+    *reinterpret_cast<uint2*>(y) = *reinterpret_cast<const uint2*>(r);
+}
+
 struct GemmArgs {
     fp8::LinearArgs A;
     int m_tiles, n_tiles, wide;                  // wide: rows of y may be written 16 bytes at a time
 };
 
 // Tiles in bands of BAND along the tokens, so that those worked on at one time share rows of x as much as rows of W.
+constexpr int PART_ROW = 128 + 4;                // floats of a row of partial sums (BN = 128), padded against bank conflicts
 constexpr int BAND = 8;
 __device__ __forceinline__ void place(const GemmArgs& G, int unit, int& mt, int& nt) {
     const int band = unit / (BAND * G.n_tiles), rest = unit - band * BAND * G.n_tiles, rows = min(BAND, G.m_tiles - band * BAND);
@@ -199,18 +209,6 @@ __device__ __forceinline__ void place(const GemmArgs& G, int unit, int& mt, int&
     mt = band * BAND + rest - nt * rows;
 }
 
-// Eight columns of token m's row, from column n on.
-template <typename T> __device__ __forceinline__ void write8(const GemmArgs& G, int m, int n, const float (&v)[8]) {
-    if (m >= G.A.M || n >= G.A.N) return;
-    T* y = (T*)G.A.y + (long long)m * G.A.y_stride + n;
-    if (G.wide && n + 8 <= G.A.N) {
-        put8(y, v);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (n + j < G.A.N) y[j] = Elem<T>::from_f32(v[j]);
-    }
-}
 // A warp's 32 rows (from m0 on) of 128 bytes each (from column n on), which its lanes have by rows, go to memory by lines: a row's 128 bytes are
 // written by eight lanes.  (Written straight from the registers, 16 bytes of 32 rows at a time, a tile took 10000 cycles.)
 template <typename T> __device__ __forceinline__ void write_rows(const GemmArgs& G, unsigned char* stage, int m0, int n, const float2 (&v)[64 / (int)sizeof(T)]) {
@@ -268,6 +266,10 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
     else __syncthreads();
     tc_after();
     const u32 tmem = tmem_slot;
+    if (warp == 0) {                             // while the kernel before this one winds down
+        prefetch_map(lane == 0, &map_x);
+        prefetch_map(lane == 0, &map_w);
+    }
     kv::follow();
 
     // This CTA's tiles: one, if a cluster of S shares it by blocks; of a pair, its half of them (tokens and rows of W).  The first CTA of a pair has the
@@ -441,32 +443,327 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
                     for (int i = 0; i < N / 2; ++i) v[i] = acc[j / 2 + i];
                     write_rows<T>(G, stage, mt * CG * BM + half_m + quarter * 32, nt * BN + half * HALF + j, v);
                 }
-            } else {                             // partial sums, by columns, where the stages were (all of them have been used)
-                float* part = reinterpret_cast<float*>(raw_smem + (tiles - smem_u32(raw_smem)));
+            } else {                             // partial sums, by rows, where the stages were (all of them have been used)
+                float* part = reinterpret_cast<float*>(raw_smem + (tiles - smem_u32(raw_smem))) + row * PART_ROW + half * HALF;
 #pragma unroll
-                for (int j = 0; j < HALF / 2; ++j) {
-                    part[(half * HALF + 2 * j) * BM + row] = acc[j].x;
-                    part[(half * HALF + 2 * j + 1) * BM + row] = acc[j].y;
-                }
+                for (int j = 0; j < HALF; j += 4) *reinterpret_cast<float4*>(part + j) = make_float4(acc[j / 2].x, acc[j / 2].y, acc[j / 2 + 1].x, acc[j / 2 + 1].y);
             }
         }
         __syncwarp();
-        if (S > 1) {                             // one tile a cluster; rank r finishes columns [r, r + 1) BN / S, a multiple of 16 of them
+        if (S > 1) {                             // one tile a cluster; rank r finishes rows r, r + S, ...: a warp has one of them at a time, a lane four columns
             cluster_sync();
-            const int cols = BN / S / 2, c0 = rank * (BN / S) + half * cols, m = row;
             int mt, nt;
             place(G, first, mt, nt);
-            for (int c = c0; c < c0 + cols; c += 8) {
-                float v[8] = {};
-                for (int r = 0; r < S; ++r)
+            const int n = nt * BN + lane * 4, most = min(BM, G.A.M - mt * BM);
+            for (int r = rank + (warp - 4) * S; r < most; r += EPI_WARPS * S) {
+                float4 v[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] += remote(tiles + (u32)(((c + j) * BM + row) * 4), (u32)r);
-                write8<T>(G, mt * BM + m, nt * BN + c, v);
+                for (int k = 0; k < 8; ++k)
+                    if (k < S) v[k] = remote4(tiles + (u32)((r * PART_ROW + lane * 4) * 4), (u32)k);
+                float sum[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+                for (int k = 1; k < 8; ++k)
+                    if (k < S) { sum[0] += v[k].x; sum[1] += v[k].y; sum[2] += v[k].z; sum[3] += v[k].w; }
+                T* y = (T*)G.A.y + (long long)(mt * BM + r) * G.A.y_stride + n;
+                if (G.wide && n + 4 <= G.A.N) {
+                    put4(y, sum);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (n + j < G.A.N) y[j] = Elem<T>::from_f32(sum[j]);
+                }
             }
             cluster_sync();                      // the others' shared memory stays until all have read it
         }
         all_done();
     }
+}
+
+// ------------------------------------------------------------------------------------------------------------ few tokens
+//
+// Bound by the weights' bytes, N K of them.  What counts is that every SM has as many of them on their way as it can hold, and equal shares.  So the
+// operands change sides: 128 rows of W are the MMA's rows, the tokens (up to TN, padded) its columns; a CTA streams the 16 KB tiles of its rows' blocks through
+// a ring of stages, two or three CTAs to an SM, and a tile of rows is shared by a cluster of S CTAs, each with a range of the blocks, as many as
+// can all run at one time (few_plan).  Partial sums are joined through distributed shared memory in the order of the ranks.
+// Up to 16 tokens stand in shared memory with all the blocks of the CTA's range (quantised there, if they come as values), more come with the
+// weights' tiles.  The scales of the range, x's times W's, stand there in any case.
+// (mma.sync with loads to registers took 17 us where this takes 10.6, one token, 12288 x 4096.)
+// Warps: 0 producer, 1 MMAs and tensor memory, 2 to 5 epilogue (a thread has a row of W and the sums of all tokens with it).
+constexpr int FEW_THREADS = 192, FEW_ACCS = 4, W_BYTES = 128 * fp8::BLOCK, FEW_MAX_STAGES = 8;
+constexpr int FEW_SMEM[2] = {112 * 1024, 74 * 1024};       // of a CTA, two or three to an SM
+
+struct FewArgs {
+    fp8::LinearArgs A;
+    const void* rows;                            // the tokens as values, if they are to be quantised here
+    long long stride;
+    int S, stages, blocks;                       // CTAs to a tile, stages of the ring, most blocks of a CTA
+};
+// Shared memory of a CTA: ring, tokens' codes of all blocks (TN = 16), scales [block][TN], then 1 KB to align all that.  The partial sums
+// go where the ring was.
+template <int TN> struct Few {
+    static constexpr int X_TILE = TN * fp8::BLOCK;
+    static constexpr bool RESIDENT = TN == 16;
+    static constexpr int STAGE = W_BYTES + (RESIDENT ? 0 : X_TILE);
+    static constexpr u32 COLS = FEW_ACCS * TN;
+    static constexpr int PER_SM = TN < 64 ? 3 : 2;       // CTAs, at most
+    static constexpr u32 IDESC = (1u << 4) | ((u32)(TN >> 3) << 17) | ((u32)(128 >> 4) << 24);
+    __host__ __device__ static int fixed(int blocks) { return (RESIDENT ? blocks * X_TILE : 0) + blocks * TN * 4 + 1024; }
+    __host__ __device__ static int smem(int stages, int blocks) { return stages * STAGE + fixed(blocks); }
+};
+// byte c of row r of a tile of 128-byte rows in the 128-byte swizzle
+__device__ __forceinline__ int swizzled(int r, int c) { return r * 128 + ((((c >> 4) ^ r) & 7) << 4) + (c & 15); }
+
+template <typename X> struct Values;
+template <> struct Values<float> { static constexpr int E = 4; };
+template <> struct Values<__nv_bfloat16> { static constexpr int E = 8; };
+
+// The tokens' codes of blocks kb0 .. kb1 - 1 and the scales of the sums: by all threads of the CTA, a few loads at a time.
+template <typename X, int TN> __device__ __forceinline__ void few_tokens(const FewArgs& F, unsigned char* codes, float* scales, int nb, int kb0, int kb1) {
+    const int M = F.A.M, n = kb1 - kb0, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const float* ws = F.A.ws + (size_t)nb * F.A.KB + kb0;
+    if (Few<TN>::RESIDENT) {                     // the tokens that pad
+        const int pad = TN - M;
+        for (int i = threadIdx.x; i < n * pad * 8; i += FEW_THREADS) {
+            const int b = i / (pad * 8), r = i - b * (pad * 8);
+            *reinterpret_cast<uint4*>(codes + b * Few<TN>::X_TILE + swizzled(M + r / 8, r % 8 * 16)) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        for (int i = threadIdx.x; i < n * pad; i += FEW_THREADS) scales[i / pad * TN + M + i % pad] = 0.f;
+    }
+    if constexpr (sizeof(X) == 1) {
+        constexpr int AT_ONCE = 4;
+        for (int i0 = threadIdx.x; i0 < n * TN; i0 += FEW_THREADS * AT_ONCE) {
+            float x[AT_ONCE], w[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int i = i0 + u * FEW_THREADS, b = i / TN, m = i % TN;
+                const bool in = i < n * TN && m < M;
+                x[u] = in ? __ldg(F.A.xs + (size_t)(kb0 + b) * M + m) : 0.f;
+                w[u] = in ? __ldg(ws + b) : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u)
+                if (i0 + u * FEW_THREADS < n * TN) scales[i0 + u * FEW_THREADS] = x[u] * w[u];
+        }
+        if (Few<TN>::RESIDENT)
+            for (int i0 = threadIdx.x; i0 < n * M * 8; i0 += FEW_THREADS * AT_ONCE) {
+                uint4 v[AT_ONCE];
+#pragma unroll
+                for (int u = 0; u < AT_ONCE; ++u) {
+                    const int i = i0 + u * FEW_THREADS, m = i / (n * 8), c = i - m * (n * 8), k = kb0 * fp8::BLOCK + c * 16;
+                    v[u] = make_uint4(0u, 0u, 0u, 0u);
+                    if (i < n * M * 8 && k < F.A.K) v[u] = __ldg(reinterpret_cast<const uint4*>(F.A.x + (size_t)m * F.A.K + k));
+                }
+#pragma unroll
+                for (int u = 0; u < AT_ONCE; ++u) {
+                    const int i = i0 + u * FEW_THREADS, m = i / (n * 8), c = i - m * (n * 8);
+                    if (i < n * M * 8) *reinterpret_cast<uint4*>(codes + (c >> 3) * Few<TN>::X_TILE + swizzled(m, (c & 7) * 16)) = v[u];
+                }
+            }
+    } else {
+        constexpr int E = Values<X>::E, LANES = fp8::BLOCK / E, PER_WARP = 32 / LANES, STEP = FEW_THREADS / 32 * PER_WARP, AT_ONCE = 4;      // blocks that a warp, the CTA has at a time
+        for (int i0 = warp * PER_WARP; i0 < n * M; i0 += STEP * AT_ONCE) {
+            uint4 raw[AT_ONCE];
+            float w[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int i = i0 + u * STEP + lane / LANES, m = i / n, b = i - m * n, k = (kb0 + b) * fp8::BLOCK + lane % LANES * E;
+                const bool in = i < n * M;
+                raw[u] = make_uint4(0u, 0u, 0u, 0u);
+                if (in && k < F.A.K) raw[u] = __ldg(reinterpret_cast<const uint4*>((const X*)F.rows + (long long)m * F.stride + k));
+                w[u] = in ? __ldg(ws + b) : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                if (i0 + u * STEP >= n * M) break;
+                const int i = i0 + u * STEP + lane / LANES, m = i / n, b = i - m * n, at = lane % LANES * E;
+                float v[E];
+                u32 c[E / 4];
+                Elem<X>::unpack(raw[u], v);
+                const float scale = fp8::quantise_row(v, c);
+                if (i >= n * M) continue;
+                unsigned char* to = codes + b * Few<TN>::X_TILE + swizzled(m, at);
+                if constexpr (E == 8) *reinterpret_cast<uint2*>(to) = make_uint2(c[0], c[1]);
+                else *reinterpret_cast<u32*>(to) = c[0];
+                if (at == 0) scales[b * TN + m] = scale * w[u];
+            }
+        }
+    }
+}
+
+template <int N> __device__ __forceinline__ void tmem_ld(u32 addr, u32 (&r)[N]);
+template <> __device__ __forceinline__ void tmem_ld<32>(u32 addr, u32 (&r)[32]) { tmem_ld32(addr, r); }
+template <> __device__ __forceinline__ void tmem_ld<16>(u32 addr, u32 (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_wait(u32 (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+          "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+}
+
+template <typename X, typename Y, int TN>
+__global__ void __launch_bounds__(FEW_THREADS, Few<TN>::PER_SM) fp8_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const FewArgs F) {
+    typedef Few<TN> L;
+    extern __shared__ unsigned char raw_smem[];
+    __shared__ u32 tmem_slot;
+    __shared__ int gave_up_flag;
+    __shared__ u64 bars[2 * FEW_MAX_STAGES + 2 * FEW_ACCS + 1];
+    volatile int* gave_up = &gave_up_flag;
+    const u32 ring = (smem_u32(raw_smem) + 1023u) & ~1023u;
+    unsigned char* ring_at = raw_smem + (ring - smem_u32(raw_smem));
+    unsigned char* codes = ring_at + F.stages * L::STAGE;
+    float* scales = reinterpret_cast<float*>(codes + (L::RESIDENT ? F.blocks * L::X_TILE : 0));
+    const u32 full = smem_u32(bars), empty = full + 8 * FEW_MAX_STAGES, acc_full = empty + 8 * FEW_MAX_STAGES, acc_empty = acc_full + 8 * FEW_ACCS,
+              drain = acc_empty + 8 * FEW_ACCS;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, S = F.S, rank = blockIdx.x % S, tile = blockIdx.x / S;
+    const int kb0 = (int)((long long)F.A.KB * rank / S), kb1 = (int)((long long)F.A.KB * (rank + 1) / S), n = kb1 - kb0;
+    if (threadIdx.x == 0) {
+        gave_up_flag = 0;
+        for (int s = 0; s < F.stages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
+        for (int b = 0; b < FEW_ACCS; ++b) { mbar_init(acc_full + 8 * b, 1); mbar_init(acc_empty + 8 * b, 4); }
+        mbar_init(drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    const u32 mine = elect_lane();
+    auto load = [&](int i, int s) {                                          // block i of the range
+        mbar_expect_tx(mine, full + 8 * s, L::STAGE);
+        tma_load<1>(mine, ring + (u32)(s * L::STAGE), &map_w, (kb0 + i) * fp8::BLOCK, tile * 128, full + 8 * s);
+        if (!L::RESIDENT) tma_load<1>(mine, ring + (u32)(s * L::STAGE) + W_BYTES, &map_x, (kb0 + i) * fp8::BLOCK, 0, full + 8 * s);
+    };
+    if (warp == 0) prefetch_map(mine, &map_w);                               // while the kernel before this one winds down
+    if (warp == 1) tmem_alloc<1>(smem_u32(&tmem_slot), L::COLS);
+    kv::follow();
+    if (warp == 0)
+        for (int i = 0; i < min(F.stages, n); ++i) load(i, i);
+    few_tokens<X, TN>(F, codes, scales, tile, kb0, kb1);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");             // the tensor cores read what was written here
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const u32 tmem = tmem_slot;
+
+    if (warp == 0) {
+        int s = 0, issued = min(F.stages, n);
+        u32 ph = 0;
+        bool ok = true;
+        for (int i = issued; i < n; ++i) {
+            ok = __all_sync(~0u, mbar_wait(empty + 8 * s, ph, gave_up, GAVE_UP_PRODUCER));
+            if (!ok) break;
+            load(i, s);
+            ++issued;
+            if (++s == F.stages) { s = 0; ph ^= 1u; }
+        }
+        if (!ok)                                 // copies in flight still land in this CTA's shared memory: wait for them (bounded)
+            for (int i = max(0, issued - F.stages); i < issued; ++i) {
+                const u64 t0 = pop_global_ns();
+                while (!mbar_try_wait(full + 8 * (i % F.stages), (u32)(i / F.stages) & 1u) && pop_global_ns() - t0 < WAIT_BUDGET_NS) {}
+            }
+    } else if (warp == 1) {
+        const u32 tm = __shfl_sync(~0u, tmem, 0);
+        const u64 dw = smem_desc(ring), dx = smem_desc(L::RESIDENT ? smem_u32(codes) : ring + W_BYTES);
+        int s = 0, buf = 0;
+        u32 ph = 0, acc_ph = 0;
+        for (int i = 0; i < n; ++i) {
+            bool ok = mbar_wait(full + 8 * s, ph, gave_up, GAVE_UP_MMA) && mbar_wait(acc_empty + 8 * buf, ((acc_ph >> buf) & 1u) ^ 1u, gave_up, GAVE_UP_MMA);
+            ok = __all_sync(~0u, ok);
+            if (!ok) break;
+            tc_after();
+            const u64 w = dw + (u64)(s * (L::STAGE / 16)), x = dx + (u64)(L::RESIDENT ? i * (L::X_TILE / 16) : s * (L::STAGE / 16));
+#pragma unroll
+            for (int k = 0; k < fp8::BLOCK / 32; ++k) umma_f8<1>(mine, tm + (u32)(buf * TN), w + 2ull * k, x + 2ull * k, L::IDESC, k > 0);
+            umma_commit<1>(mine, empty + 8 * s);
+            umma_commit<1>(mine, acc_full + 8 * buf);
+            acc_ph ^= 1u << buf;
+            if (++buf == FEW_ACCS) buf = 0;
+            if (++s == F.stages) { s = 0; ph ^= 1u; }
+        }
+        // nothing of this CTA may still run on the tensor cores when tensor memory is given back
+        umma_commit_here<1>(mine, drain);
+        const u64 t0 = pop_global_ns();
+        while (!mbar_try_wait(drain, 0u) && pop_global_ns() - t0 < WAIT_BUDGET_NS) {}
+    }
+    constexpr int CHUNK = TN < 32 ? TN : 32;
+    float acc[TN];
+    const int quarter = warp & 3, row = quarter * 32 + lane;
+    if (warp >= 2) {
+        const u32 at = tmem + ((u32)(quarter * 32) << 16);
+        int buf = 0;
+        u32 acc_ph = 0;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[j] = 0.f;
+        for (int i = 0; i < n; ++i) {
+            if (!__all_sync(~0u, mbar_wait(acc_full + 8 * buf, (acc_ph >> buf) & 1u, gave_up, GAVE_UP_EPILOGUE))) break;
+            tc_after();
+            const float* scale = scales + i * TN;
+#pragma unroll
+            for (int p = 0; p < TN / CHUNK; ++p) {
+                u32 v[CHUNK];
+                tmem_ld<CHUNK>(at + (u32)(buf * TN + p * CHUNK), v);
+                tmem_wait(v);
+#pragma unroll
+                for (int j = 0; j < CHUNK; j += 4) {
+                    const float4 sc = *reinterpret_cast<const float4*>(scale + p * CHUNK + j);
+                    float* a = acc + p * CHUNK + j;
+                    a[0] = fmaf(__uint_as_float(v[j]), sc.x, a[0]);
+                    a[1] = fmaf(__uint_as_float(v[j + 1]), sc.y, a[1]);
+                    a[2] = fmaf(__uint_as_float(v[j + 2]), sc.z, a[2]);
+                    a[3] = fmaf(__uint_as_float(v[j + 3]), sc.w, a[3]);
+                }
+            }
+            tc_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
+            acc_ph ^= 1u << buf;
+            if (++buf == FEW_ACCS) buf = 0;
+        }
+    }
+    const int M = F.A.M, out_n = tile * 128 + row;
+    __syncwarp();
+    if (S == 1) {
+        if (warp >= 2 && out_n < F.A.N) {
+#pragma unroll
+            for (int m = 0; m < TN; ++m)
+                if (m < M) ((Y*)F.A.y)[(long long)m * F.A.y_stride + out_n] = Elem<Y>::from_f32(acc[m]);
+        }
+    } else {
+        float* part = reinterpret_cast<float*>(ring_at);                     // [token][row]; the ring has been used up
+        if (warp >= 2) {
+#pragma unroll
+            for (int m = 0; m < TN; ++m)
+                if (m < M) part[m * 128 + row] = acc[m];
+        }
+        __syncwarp();
+        cluster_sync();
+        // rank r finishes tokens r, r + S, ...: a warp one of them, a lane four rows of W
+        if (warp >= 2) {
+            const int n0 = tile * 128 + lane * 4;
+            for (int m = rank + (warp - 2) * S; m < M; m += 4 * S) {
+                float4 v[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r < S) v[r] = remote4(ring + (u32)((m * 128 + lane * 4) * 4), (u32)r);
+                float sum[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+                for (int r = 1; r < 8; ++r)
+                    if (r < S) { sum[0] += v[r].x; sum[1] += v[r].y; sum[2] += v[r].z; sum[3] += v[r].w; }
+                Y* y = (Y*)F.A.y + (long long)m * F.A.y_stride + n0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (n0 + j < F.A.N) y[j] = Elem<Y>::from_f32(sum[j]);
+            }
+        }
+        __syncwarp();
+        cluster_sync();                          // the others' shared memory stays until all have read it
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (warp == 1) tmem_free<1>(tmem, L::COLS);
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -529,6 +826,88 @@ template <typename T, int BN, int CG> int launch(const fp8::LinearArgs& A, int S
     return POP_OK;
 }
 
+// Clusters of S that run at one time with two (p = 0) or three CTAs to an SM.  Asked for once per device: the SMs of a processor cluster that are left over
+// make it fewer than the SMs' number says (S = 4: 71 and 104, not 74 and 111).  The question is put for a kernel of the same size without tensor memory; for one with
+// it the answer is that of one CTA to an SM, which is not what happens.
+__global__ void __launch_bounds__(FEW_THREADS) few_size_kernel() {}
+int few_clusters(int S, int p, int* clusters) {
+    static int known[64][9][2];
+    int device = 0;
+    POP_CUDA(cudaGetDevice(&device));
+    int n = device < 64 ? known[device][S][p] : 0;
+    if (!n) {
+        POP_CUDA(cudaFuncSetAttribute(few_size_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM[0] + 256));
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(S * 512);
+        cfg.blockDim = dim3(FEW_THREADS);
+        cfg.dynamicSmemBytes = FEW_SMEM[p] + 256;                            // (and the barriers)
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = S;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        POP_CUDA(cudaOccupancyMaxActiveClusters(&n, few_size_kernel, &cfg));
+        if (device < 64) known[device][S][p] = n;
+    }
+    *clusters = n;
+    return POP_OK;
+}
+// How many CTAs share a tile of 128 rows of W: as many as can all run at one time, which splits the work finest; with fewer to an SM, and more stages each, if
+// there is a choice.  (One token, 12288 x 4096, 96 tiles, S = 2 | 3 | 4 with three to an SM: 14.3 | 11.7 | 10.7 us; 8, which takes two rounds: 15.8; 3 with two
+// to an SM, 93 clusters of the 96 at a time: 15.6.  1024 x 4096, S = 2 | 4 | 8 with two: 7.6 | 5.2 | 4.6.)  Tiles for more than one round are shared by as
+// few as have room for two stages.
+template <int TN> int few_plan(const fp8::LinearArgs& A, FewArgs* F) {
+    const int tiles = (A.N + 127) / 128;
+    auto take = [&](int S, int p) {
+        F->S = S;
+        F->blocks = (A.KB + S - 1) / S;
+        const int left = FEW_SMEM[p] - Few<TN>::fixed(F->blocks);
+        F->stages = left < 0 ? 0 : left / Few<TN>::STAGE;
+        if (F->stages > FEW_MAX_STAGES) F->stages = FEW_MAX_STAGES;
+        return F->stages >= 2;
+    };
+    const int most = A.KB < 8 ? A.KB : 8;
+    for (int S = most; S >= 1; --S)
+        for (int p = 0; p + 2 <= Few<TN>::PER_SM; ++p) {
+            int clusters = 0;
+            const int rc = few_clusters(S, p, &clusters);
+            if (rc != POP_OK) return rc;
+            if (tiles <= clusters && take(S, p)) return POP_OK;
+        }
+    for (int p = Few<TN>::PER_SM - 2; p >= 0; --p)
+        for (int S = 1; S <= most; ++S)
+            if (take(S, p)) return POP_OK;
+    return POP_ERR_UNSUPPORTED;
+}
+template <typename X, typename Y, int TN> int launch_few(const FewArgs& F, cudaStream_t st) {
+    CUtensorMap mx = {}, mw;
+    int rc = make_map(&mw, F.A.w, F.A.N, F.A.K, 128);
+    if (rc == POP_OK && !Few<TN>::RESIDENT) rc = make_map(&mx, F.A.x, F.A.M, F.A.K, TN);
+    if (rc != POP_OK) return rc;
+    static thread_local int ready = -1;
+    int device = 0;
+    POP_CUDA(cudaGetDevice(&device));
+    if (ready != device) {
+        POP_CUDA(cudaFuncSetAttribute(fp8_few_kernel<X, Y, TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM[0]));
+        ready = device;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((F.A.N + 127) / 128 * F.S);
+    cfg.blockDim = dim3(FEW_THREADS);
+    cfg.dynamicSmemBytes = Few<TN>::smem(F.stages, F.blocks);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2] = {kv::following()};
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = F.S;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = F.S > 1 ? 2 : 1;
+    POP_CUDA(cudaLaunchKernelEx(&cfg, fp8_few_kernel<X, Y, TN>, mx, mw, F));
+    POP_LAUNCHED();
+    return POP_OK;
+}
+
 template <typename T> int choose(const fp8::LinearArgs& A, int sms, cudaStream_t st) {
     const long long m_tiles = (A.M + BM - 1) / BM, tiles = m_tiles * ((A.N + 127) / 128);
     if (A.M > BM && tiles >= 2 * sms) return launch<T, 256, 2>(A, 1, sms, st);
@@ -538,6 +917,23 @@ template <typename T> int choose(const fp8::LinearArgs& A, int sms, cudaStream_t
 }
 
 }  // namespace
+
+int pop_launch_fp8_few(const fp8::LinearArgs& A, const void* rows, long long stride, pop_dtype_t x_dtype, pop_dtype_t y_dtype, cudaStream_t st) {
+    FewArgs F = {A, rows, stride, 1, 0, 0};
+    const bool bf16 = y_dtype == POP_BF16;
+    if (A.M <= 16) {
+        const int rc = few_plan<16>(A, &F);
+        if (rc != POP_OK) return rc;
+        if (!rows) return bf16 ? launch_few<unsigned char, __nv_bfloat16, 16>(F, st) : launch_few<unsigned char, float, 16>(F, st);
+        if (x_dtype == POP_BF16) return bf16 ? launch_few<__nv_bfloat16, __nv_bfloat16, 16>(F, st) : launch_few<__nv_bfloat16, float, 16>(F, st);
+        return bf16 ? launch_few<float, __nv_bfloat16, 16>(F, st) : launch_few<float, float, 16>(F, st);
+    }
+    if (rows || A.M > 64) return POP_ERR_UNSUPPORTED;
+    const int rc = A.M <= 32 ? few_plan<32>(A, &F) : few_plan<64>(A, &F);
+    if (rc != POP_OK) return rc;
+    if (A.M <= 32) return bf16 ? launch_few<unsigned char, __nv_bfloat16, 32>(F, st) : launch_few<unsigned char, float, 32>(F, st);
+    return bf16 ? launch_few<unsigned char, __nv_bfloat16, 64>(F, st) : launch_few<unsigned char, float, 64>(F, st);
+}
 
 int pop_launch_fp8_gemm(const fp8::LinearArgs& A, pop_dtype_t y_dtype, int sms, cudaStream_t st) {
     return y_dtype == POP_BF16 ? choose<__nv_bfloat16>(A, sms, st) : choose<float>(A, sms, st);
