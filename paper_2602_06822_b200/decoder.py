@@ -8,7 +8,9 @@ and the residual stream are plain torch ops in bf16; every FFN goes through the 
 for the dense baseline of the latency table, through torch linear layers.
 
 With ``kv_cache="int4"`` keys and values go to the library's paged 4-bit cache instead and attention reads them there
-(`pop_kv_plan` once a step, `pop_kv_append` and `pop_kv_attention` in every layer).
+(`pop_kv_plan` once a step, `pop_kv_append` and `pop_kv_attention` in every layer).  With ``block="fused"`` the rest of the attention
+block is the library's, too: norms with the residual additions (`pop_block_norm`), the projections in 8 bits (`pop_fp8_linear`) and rotary positions on the way into
+the cache (`pop_kv_append_rope`).
 
 Weights are synthetic (seeded, ~ N(0, 0.02^2)); token ids are a seeded sequence that is fed
 teacher-forced, so that no sampling and no LM head are needed.
@@ -44,12 +46,17 @@ def ratios_for(r: float, gamma: float = 0.1):
 
 class Decoder:
     """ffn = "pop" (every FFN through the library, ratios given) or "dense" (torch linear layers); kv_cache = "bf16" (torch) or
-    "int4" (the library's paged 4-bit cache, for up to kv_tokens tokens, in whole pages; more are refused)."""
+    "int4" (the library's paged 4-bit cache, for up to kv_tokens tokens, in whole pages; more are refused); block = "torch" (norms, projections in
+    bf16 and rotary positions by torch) or "fused" (by the library, projections in 8 bits; with the 4-bit cache)."""
 
     def __init__(self, cfg: DecoderConfig, device="cuda:0", ffn: str = "pop", ratios=None, k: Optional[int] = None, kv_cache: str = "bf16",
-                 kv_tokens: int = 2048):
+                 kv_tokens: int = 2048, block: str = "torch"):
         if kv_cache not in ("bf16", "int4"):
             raise ValueError("kv_cache must be \"bf16\" or \"int4\"")
+        if block not in ("torch", "fused"):
+            raise ValueError("block must be \"torch\" or \"fused\"")
+        if block == "fused" and kv_cache != "int4":
+            raise ValueError("block=\"fused\" goes with kv_cache=\"int4\"")
         self.cfg, self.dev, self.ffn = cfg, torch.device(device), ffn
         g = torch.Generator(device=self.dev)
         g.manual_seed(cfg.seed)
@@ -71,6 +78,10 @@ class Decoder:
         self.parts: List[Optional[pop.Partition]] = [None] * cfg.n_layers
         self.kv: List[Optional[tuple]] = [None] * cfg.n_layers
         self.cache4 = pop.KVCache(cfg.n_layers, 1, kv_tokens, cfg.n_heads, self.hd, device=self.dev) if kv_cache == "int4" else None
+        self.fused = None
+        if block == "fused":                       # per layer the [q | k | v] projection and the output projection in 8 bits
+            self.fused = [(pop.fp8_weights(torch.cat([l["Wq"], l["Wk"], l["Wv"]])), pop.fp8_weights(l["Wo"])) for l in self.layers]
+            self.rope_table = pop.Rope(self.hd, cfg.rope_base, device=self.dev)
         self.one = torch.ones(1, device=self.dev, dtype=torch.int32)
         self.pos = 0
         self.trace = None          # when a dict: (layer, step) -> recorded FFN inputs / outputs, for layer-local parity
@@ -110,6 +121,34 @@ class Decoder:
         o = F.scaled_dot_product_attention(q.transpose(0, 1), K.transpose(0, 1), V.transpose(0, 1), is_causal=(T > 1))
         return F.linear(o.transpose(0, 1).reshape(T, cfg.d), L["Wo"])
 
+    def fused_attention(self, li, h, u, pos):
+        """The attention block of one layer by the library: h [T, d] the residual stream, which gets the block before's output u (or None) added
+        in place; returns the block's own output, which is still to be added."""
+        T, cfg = h.shape[0], self.cfg
+        wqkv, wo = self.fused[li]
+        h, f = pop.block_norm(h, u, eps=cfg.rms_eps, fp8=True, h_out=h)
+        qkv = pop.fp8_linear(f, wqkv).view(T, 3 * cfg.n_heads, self.hd)
+        k, v = qkv[:, cfg.n_heads:2 * cfg.n_heads], qkv[:, 2 * cfg.n_heads:]
+        q = self.cache4.append_rope(li, self.rope_table, qkv[:, :cfg.n_heads], k, v)
+        o = self.cache4.attend(li, q)
+        a = pop.fp8_linear(o.view(T, cfg.d), wo)
+        if self.trace is not None:
+            self.trace[("attention", li, pos)] = (h.clone(), qkv, q, o, a)
+        return a
+
+    def fused_layers(self, h, ffn, pos=None, attention=True, mlp=True):
+        """All layers with block = "fused": every block's output is added to the stream by the norm that follows it.  ffn(li, f) is the FFN of f."""
+        u = None
+        for li in range(self.cfg.n_layers):
+            if attention:
+                with self._timed("attention"):
+                    u = self.fused_attention(li, h, u, pos)
+            if mlp:
+                h, f = pop.block_norm(h, u, eps=self.cfg.rms_eps, h_out=h)
+                with self._timed("mlp"):
+                    u = ffn(li, f)
+        return h if u is None else h.add_(u)
+
     def _timed(self, name):
         class _T:
             def __init__(s2, outer):
@@ -132,6 +171,31 @@ class Decoder:
         if self.cache4 is not None and tokens > self.cache4.max_tokens:
             raise ValueError(f"{tokens} tokens are more than the 4-bit cache has room for ({self.cache4.max_tokens}, from kv_tokens)")
 
+    def _prefill_ffn(self, li, f):
+        if self.ffn == "pop":
+            if self.parts[li] is not None:
+                self.parts[li].destroy()
+            kk = self.k if self.k is not None else pop.region_sizes(self.cfg.N, self.ratios)[3]
+            self.parts[li], y = self.weights[li].prefill_partition_with_output(f, self.ratios, kk)
+        else:
+            y = self.dense_ffn(li, f)
+        if self.trace is not None:
+            self.trace[("prefill", li)] = (f.clone(), y.clone())
+        return y
+
+    def _decode_ffn(self, li, f, step):
+        if self.ffn != "pop":
+            return self.dense_ffn(li, f)
+        p = self.parts[li]
+        kk = self.k if self.k is not None else p.n_cand // 2
+        if not (self.trace is not None and self.trace.get("want", lambda l, s: True)(li, step)):
+            return pop.decode_step(p, f, kk)
+        mask = torch.empty(p.n_cand, dtype=torch.uint8, device=self.dev)
+        sel = torch.empty(kk, dtype=torch.int32, device=self.dev)
+        y = pop.decode_step(p, f, kk, mask_out=mask, sel_out=sel)
+        self.trace[(li, step)] = (f.clone(), y.clone(), mask, sel)
+        return y
+
     # ------------------------------------------------------------------ the two stages
     def prefill(self, ids: torch.Tensor):
         """ids [T] prompt token ids -> hidden states [T, d] after the last layer.  Builds every layer's partition."""
@@ -140,21 +204,16 @@ class Decoder:
         if self.cache4 is not None:
             self.cache4.plan(torch.tensor([ids.shape[0]], device=self.dev, dtype=torch.int32), ids.shape[0])
         h = self.embed[ids]
-        for li in range(self.cfg.n_layers):
-            with self._timed("attention"):
-                h = h + self.attention(li, self.rmsnorm(h), 0)
-            f = self.rmsnorm(h)
-            with self._timed("mlp"):
-                if self.ffn == "pop":
-                    if self.parts[li] is not None:
-                        self.parts[li].destroy()
-                    kk = self.k if self.k is not None else pop.region_sizes(self.cfg.N, self.ratios)[3]
-                    self.parts[li], y = self.weights[li].prefill_partition_with_output(f, self.ratios, kk)
-                else:
-                    y = self.dense_ffn(li, f)
-            if self.trace is not None:
-                self.trace[("prefill", li)] = (f.clone(), y.clone())
-            h = h + y
+        if self.fused is not None:
+            h = self.fused_layers(h, self._prefill_ffn, 0)
+        else:
+            for li in range(self.cfg.n_layers):
+                with self._timed("attention"):
+                    h = h + self.attention(li, self.rmsnorm(h), 0)
+                f = self.rmsnorm(h)
+                with self._timed("mlp"):
+                    y = self._prefill_ffn(li, f)
+                h = h + y
         self.pos = ids.shape[0]
         return h
 
@@ -164,25 +223,16 @@ class Decoder:
         if self.cache4 is not None:
             self.cache4.plan(self.one, 1)
         h = self.embed[tok]
-        for li in range(self.cfg.n_layers):
-            with self._timed("attention"):
-                h = h + self.attention(li, self.rmsnorm(h), self.pos)
-            f = self.rmsnorm(h)
-            with self._timed("mlp"):
-                if self.ffn == "pop":
-                    p = self.parts[li]
-                    kk = self.k if self.k is not None else p.n_cand // 2
-                    want = self.trace is not None and self.trace.get("want", lambda l, s: True)(li, step)
-                    if want:
-                        mask = torch.empty(p.n_cand, dtype=torch.uint8, device=self.dev)
-                        sel = torch.empty(kk, dtype=torch.int32, device=self.dev)
-                        y = pop.decode_step(p, f, kk, mask_out=mask, sel_out=sel)
-                        self.trace[(li, step)] = (f.clone(), y.clone(), mask, sel)
-                    else:
-                        y = pop.decode_step(p, f, kk)
-                else:
-                    y = self.dense_ffn(li, f)
-            h = h + y
+        if self.fused is not None:
+            h = self.fused_layers(h, lambda li, f: self._decode_ffn(li, f, step), self.pos)
+        else:
+            for li in range(self.cfg.n_layers):
+                with self._timed("attention"):
+                    h = h + self.attention(li, self.rmsnorm(h), self.pos)
+                f = self.rmsnorm(h)
+                with self._timed("mlp"):
+                    y = self._decode_ffn(li, f, step)
+                h = h + y
         self.pos += 1
         return h
 
@@ -212,6 +262,16 @@ class Decoder:
         if attention and self.cache4 is not None:
             self.cache4.plan(self.one, 1)
         h = self.embed.index_select(0, self.ids_dev.index_select(0, self.pos_t))
+        if self.fused is not None:
+            def ffn(li, f):
+                if self.ffn != "pop":
+                    return self.dense_ffn(li, f)
+                p = self.parts[li]
+                return pop.decode_step(p, f, self.k if self.k is not None else p.n_cand // 2, y=self.y_static, stream=torch.cuda.current_stream())
+
+            h = self.fused_layers(h, ffn, None, attention, mlp)
+            self.pos_t += 1
+            return h
         ang = self.pos_t.float()[:, None] * self.inv_freq[None, :]
         cos, sin = torch.cos(ang)[:, None, :], torch.sin(ang)[:, None, :]
         mask = (self.arange <= self.pos_t)[None, None, :]
@@ -298,7 +358,7 @@ def _replay_ms(graph, n, m, pos0):
 
 
 def latency_table(cfg: Optional[DecoderConfig] = None, n_in: int = 128, n_out: int = 128, device="cuda:0", reps: int = 3,
-                  kv_cache: str = "bf16"):
+                  kv_cache: str = "bf16", block: str = "torch"):
     """Attention / MLP / end-to-end latency of `n_in` prompt tokens + `n_out` generated tokens, dense and with POP
     at the paper's two MLP channel ratios for Llama-2-7B (29.9 % and 59.8 %: App. A.1), gamma 0.1: the shape of the
     paper's Table 4 (which was measured on an RTX A6000 with trained weights, module times by CUDA events).
@@ -310,7 +370,8 @@ def latency_table(cfg: Optional[DecoderConfig] = None, n_in: int = 128, n_out: i
     rows = []
     for label, ffn, r in (("dense", "dense", None), ("POP, MLP ratio 29.9 %", "pop", 0.299), ("POP, MLP ratio 59.8 %", "pop", 0.598)):
         # every replay of a captured step appends a token: room for all of them in the 4-bit cache
-        m = Decoder(cfg, device, ffn=ffn, ratios=ratios_for(r) if r is not None else None, kv_cache=kv_cache, kv_tokens=n_in + n_out + 8)
+        m = Decoder(cfg, device, ffn=ffn, ratios=ratios_for(r) if r is not None else None, kv_cache=kv_cache, kv_tokens=n_in + n_out + 8,
+                    block=block)
         ids = seeded_ids(cfg, n_in + n_out + 1, 17, m.dev)
         prefill_ms = []
         for rep in range(2):
@@ -340,6 +401,8 @@ def latency_table(cfg: Optional[DecoderConfig] = None, n_in: int = 128, n_out: i
         t = {name: min(_replay_ms(gph, n_out, m, n_in) for _ in range(reps)) for name, gph in graphs.items()}
         if m.cache4 is not None:
             m.cache4.check()
+        if m.fused is not None:
+            pop.fp8_check()
         if ffn == "pop":
             for p in m.parts:
                 p.check()
@@ -370,7 +433,8 @@ if __name__ == "__main__":
     ap.add_argument("--n-in", type=int, default=128)
     ap.add_argument("--n-out", type=int, default=128)
     ap.add_argument("--kv-cache", choices=("bf16", "int4"), default="bf16")
+    ap.add_argument("--block", choices=("torch", "fused"), default="torch")
     a = ap.parse_args()
     ge.build()
-    for rw in latency_table(DecoderConfig(n_layers=a.layers), a.n_in, a.n_out, kv_cache=a.kv_cache):
+    for rw in latency_table(DecoderConfig(n_layers=a.layers), a.n_in, a.n_out, kv_cache=a.kv_cache, block=a.block):
         print(json.dumps(rw))

@@ -568,3 +568,82 @@ def test_binding_refusals():
             fn()
     with torch.no_grad():
         pop.block_norm(grad)
+
+
+# ------------------------------------------------------------------------------------------------------------- the decoder
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ffn", ["pop", "dense"])
+def test_fused_decoder_layer_by_layer(ffn):
+    """The decoder with block = "fused": in every layer and step, what each call of the attention block gave, from what it actually had.  Rotations are equal
+    to the oracle's; attention is over what the cache holds of the rotated keys, as in test_kv_decoder.py (2.5e-3 in the 2-norm, a single row 4e-3);
+    the products are compared with 64 bits over the codes of their actual rows, within what test_linear_sizes allows; the stream with its sum."""
+    from paper_2602_06822_b200 import decoder as dec
+    cfg = dec.DecoderConfig(n_layers=2, d=2048, n_heads=16, N=2816, vocab=512, seed=5)
+    n_in, n_out = 130, 4
+    m = dec.Decoder(cfg, ffn=ffn, ratios=dec.ratios_for(0.2) if ffn == "pop" else None, kv_cache="int4", kv_tokens=160, block="fused")
+    ids = dec.seeded_ids(cfg, n_in + n_out, 9, m.dev)
+    m.trace = {}
+    m.prefill(ids[:n_in])
+    for s in range(n_out):
+        m.decode(ids[n_in + s: n_in + s + 1], s)
+    torch.cuda.synchronize()
+    H, D = cfg.n_heads, m.hd
+    freq = pop.rope_frequencies(D, cfg.rope_base)[0]
+    for li in range(cfg.n_layers):
+        at, held = 0, []
+        for p in [0] + list(range(n_in, n_in + n_out)):
+            h, qkv, q, o, a = m.trace[("attention", li, p)]
+            n = h.shape[0]
+            _, f = pop.block_norm(h, eps=cfg.rms_eps, fp8=True)              # (the stream as it stood, rounded: the call itself had 32 bits of it)
+            for x, w, y in ((f, m.fused[li][0], qkv.reshape(n, -1)), (pop.fp8_quantize(o.reshape(n, -1)), m.fused[li][1], a)):
+                xv, wv = (lo.values(t.codes.view(torch.uint8).cpu().numpy(), t.scales.cpu().numpy(), r) for t, r in ((x, 1), (w, 128)))
+                want = xv @ wv.T
+                size = np.abs(xv) @ np.abs(wv).T
+                bound = (4 * (2.0 ** -21 + 2.0 ** -23) + (cfg.d // 128 + 12) * U) * size
+                if x is f:       # bf16 stream: f off by 2^-8 of each element and rounded to e4m3 from there: a code may be the next one, 2^-3 of it, independent: in the 2-norm
+                    assert np.linalg.norm(host(y) - want) <= 0.02 * np.linalg.norm(want)
+                else:
+                    within(y, want, bound + HALF[BF16] * (np.abs(want) + bound), "product")
+            cos, sin = lo.cos_sin(freq, 1.0, np.arange(at, at + n))
+            check_equal(q, lo.rotate(host(qkv[:, :H]), cos, sin, False), BF16)
+            held.append(np.stack([lo.rotate(host(qkv[:, H:2 * H]), cos, sin, False), host(qkv[:, 2 * H:]).astype(np.float32)]))
+            k, v = (ko.stored(np.concatenate([t[i] for t in held])) for i in (0, 1))
+            want, _ = ko.attention(host(q), k, v, at, D ** -0.5, True, 0)
+            assert np.linalg.norm(host(o) - want) <= (2.5e-3 if n > 1 else 4e-3) * np.linalg.norm(want)
+            at += n
+    pop.fp8_check()
+    m.close()
+
+
+@pytest.mark.gpu
+def test_fused_decoder_captured_steps_equal_eager_ones():
+    from paper_2602_06822_b200 import decoder as dec
+    cfg = dec.DecoderConfig(n_layers=2, d=2048, n_heads=16, N=2816, vocab=512, seed=6)
+    n_in, n_out = 70, 5
+    m = dec.Decoder(cfg, ffn="dense", kv_cache="int4", kv_tokens=96, block="fused")
+    ids = dec.seeded_ids(cfg, n_in + n_out, 3, m.dev)
+    m.prefill(ids[:n_in])
+    m.begin_static(ids, n_in + n_out)
+    eager = [m.step_static().clone() for _ in range(n_out)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    m.rewind(n_in)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        h = m.step_static()
+    m.rewind(n_in)
+    for s in range(n_out):
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(h, eager[s]), f"step {s}"
+    m.close()
+
+
+@pytest.mark.gpu
+def test_fused_decoder_refusals():
+    from paper_2602_06822_b200 import decoder as dec
+    cfg = dec.DecoderConfig(n_layers=1, d=128, n_heads=2, N=256, vocab=16)
+    for kw in (dict(block="fast"), dict(block="fused"), dict(block="fused", kv_cache="bf16")):
+        with pytest.raises(ValueError):
+            dec.Decoder(cfg, ffn="dense", **kw)
