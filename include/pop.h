@@ -449,7 +449,8 @@ int pop_block_norm(const pop_block_norm_t* args, int n_tokens, int d, pop_dtype_
  *   y rows [N] of `dtype`, y_stride elements apart.  The sum inside a block runs on the tensor cores (32-bit accumulators), the sum over
  *   blocks in fp32.  Any M >= 0 and N >= 1; K a multiple of 16; codes 16-byte aligned.
  * pop_fp8_linear_rows: the same for x [M][K] of x_dtype, quantised on the way (block_rows 1).  workspace: device memory of
- *   pop_fp8_linear_workspace() bytes, 16-byte aligned, need not be initialised, for one call at a time.
+ *   pop_fp8_linear_workspace() bytes, 16-byte aligned, need not be initialised, for one call at a time (none, and it may be NULL, where few tokens are quantised
+ *   within the product: 0 bytes).
  * Equal calls give equal results, bit for bit, and so does a token among others (whatever M, up to the order of the fp32 sums, which
  * goes by M, N and K).
  * pop_fp8_check synchronises the stream and reports whether a bounded device-side wait of one of these calls ran out on the current device

@@ -177,7 +177,7 @@ extern "C" int pop_fp8_linear_workspace(int M, int K, size_t* bytes) {
     if (!bytes) return POP_ERR_INVALID_ARG;
     const int rc = check_shape(M, K);
     if (rc != POP_OK) return rc;
-    *bytes = (size_t)fp8::blocks(K) * M * sizeof(float) + 16 + (size_t)M * K;      // scales, then codes at the next 16 bytes
+    *bytes = fp8::rows_in_product(M, K) ? 0 : (size_t)fp8::blocks(K) * M * sizeof(float) + 16 + (size_t)M * K;      // scales, then codes at the next 16 bytes
     return POP_OK;
 }
 
@@ -189,16 +189,16 @@ extern "C" int pop_fp8_linear_rows(const void* x, long long x_stride, pop_dtype_
     if (N <= 0) return POP_ERR_INVALID_ARG;
     if (y_dtype != POP_F32 && y_dtype != POP_BF16) return POP_ERR_UNSUPPORTED;
     if (M == 0) return POP_OK;
-    if (!w_codes || !w_scales || !y || y_stride < N || !workspace || workspace_bytes < need || ((uintptr_t)workspace & 15u) != 0) return POP_ERR_INVALID_ARG;
+    if (!w_codes || !w_scales || !y || y_stride < N) return POP_ERR_INVALID_ARG;
     if (((uintptr_t)w_codes & 15u) != 0 || ((uintptr_t)w_scales & 3u) != 0 || ((uintptr_t)y & (y_dtype == POP_F32 ? 3u : 1u))) return POP_ERR_INVALID_ARG;
     rc = check_x(x, x_stride, K, x_dtype);
     if (rc != POP_OK) return rc;
     const int KB = fp8::blocks(K);
-    if (M <= 16) {
+    if (fp8::rows_in_product(M, K)) {
         const fp8::LinearArgs A = {nullptr, (const unsigned char*)w_codes, nullptr, w_scales, M, N, K, KB, y, y_stride};
-        rc = pop_launch_fp8_few(A, x, x_stride, x_dtype, y_dtype, (cudaStream_t)cuda_stream);
-        if (rc != POP_ERR_UNSUPPORTED) return rc;
+        return pop_launch_fp8_few(A, x, x_stride, x_dtype, y_dtype, (cudaStream_t)cuda_stream);
     }
+    if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15u) != 0) return POP_ERR_INVALID_ARG;
     float* scales = (float*)workspace;
     unsigned char* codes = (unsigned char*)workspace + (((size_t)KB * M * sizeof(float) + 15) & ~(size_t)15);
     rc = pop_fp8_quantize(x, x_stride, M, K, x_dtype, 1, codes, scales, cuda_stream);

@@ -46,11 +46,14 @@ struct LinearArgs {
 };
 
 __host__ __device__ constexpr int blocks(int n) { return (n + BLOCK - 1) / BLOCK; }
+// Tokens that the product for few tokens quantises itself, so that no workspace is needed.  (The bound on K leaves an eighth of the blocks, with the
+// tokens' codes and scales of each, room beside two stages of the ring.)
+__host__ __device__ constexpr bool rows_in_product(int M, int K) { return M <= 16 && blocks(K) <= 8 * 36; }
 
 }  // namespace fp8
 
 // pop_fp8_gemm.cu: many tokens, on the tensor cores
-// up to 64 tokens as codes, or up to 16 as values (`rows`, not NULL) to be quantised on the way; POP_ERR_UNSUPPORTED, with nothing launched, where it does
-// not take the call (a K so long that the range of a CTA does not fit)
+// up to 64 tokens as codes, or as values (`rows`, not NULL) to be quantised on the way where rows_in_product() says so; POP_ERR_UNSUPPORTED, with nothing
+// launched, where it does not take the call (a K so long that the range of a CTA does not fit)
 int pop_launch_fp8_few(const fp8::LinearArgs& A, const void* rows, long long stride, pop_dtype_t x_dtype, pop_dtype_t y_dtype, cudaStream_t st);
 int pop_launch_fp8_gemm(const fp8::LinearArgs& A, pop_dtype_t y_dtype, int sms, cudaStream_t st);

@@ -830,10 +830,8 @@ template <typename T, int BN, int CG> int launch(const fp8::LinearArgs& A, int S
 // make it fewer than the SMs' number says (S = 4: 71 and 104, not 74 and 111).  The question is put for a kernel of the same size without tensor memory; for one with
 // it the answer is that of one CTA to an SM, which is not what happens.
 __global__ void __launch_bounds__(FEW_THREADS) few_size_kernel() {}
-int few_clusters(int S, int p, int* clusters) {
+int few_clusters(int device, int S, int p, int* clusters) {
     static int known[64][9][2];
-    int device = 0;
-    POP_CUDA(cudaGetDevice(&device));
     int n = device < 64 ? known[device][S][p] : 0;
     if (!n) {
         POP_CUDA(cudaFuncSetAttribute(few_size_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM[0] + 256));
@@ -858,6 +856,8 @@ int few_clusters(int S, int p, int* clusters) {
 // to an SM, 93 clusters of the 96 at a time: 15.6.  1024 x 4096, S = 2 | 4 | 8 with two: 7.6 | 5.2 | 4.6.)  Tiles for more than one round are shared by as
 // few as have room for two stages.
 template <int TN> int few_plan(const fp8::LinearArgs& A, FewArgs* F) {
+    int device = 0;
+    POP_CUDA(cudaGetDevice(&device));
     const int tiles = (A.N + 127) / 128;
     auto take = [&](int S, int p) {
         F->S = S;
@@ -871,7 +871,7 @@ template <int TN> int few_plan(const fp8::LinearArgs& A, FewArgs* F) {
     for (int S = most; S >= 1; --S)
         for (int p = 0; p + 2 <= Few<TN>::PER_SM; ++p) {
             int clusters = 0;
-            const int rc = few_clusters(S, p, &clusters);
+            const int rc = few_clusters(device, S, p, &clusters);
             if (rc != POP_OK) return rc;
             if (tiles <= clusters && take(S, p)) return POP_OK;
         }

@@ -733,19 +733,20 @@ def _check_tensors(what: str, stream, dtype, tensors):
 
 def _matrix(t, what: str, d: Optional[int] = None) -> int:
     """Row stride (in elements) of [rows, d] whose rows are contiguous."""
-    if t.dim() != 2 or t.size(1) == 0 or (d is not None and t.size(1) != d):
+    shape = t.shape
+    if len(shape) != 2 or shape[1] == 0 or (d is not None and shape[1] != d):
         raise ValueError(f"{what} must be [rows, {'d' if d is None else d}]")
     if t.is_contiguous():
-        return t.size(1)
-    if t.size(1) > 1 and t.stride(1) != 1:
+        return shape[1]
+    row, one = t.stride()
+    if shape[1] > 1 and one != 1:
         raise ValueError(f"{what}: the elements of a row must be contiguous")
-    return t.stride(0) if t.size(0) > 1 else t.size(1)
+    return row if shape[0] > 1 else shape[1]
 
 
 def _like(t):
     """An uninitialised dense tensor of t's shape and type.  (empty_like costs half of what empty does, but keeps the strides of a slice.)"""
-    torch = _torch()
-    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    return _torch().empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
 
 
 def _ptr(t):
@@ -770,11 +771,11 @@ class _Fp8:
         self.codes, self.scales = codes, scales
 
     @classmethod
-    def _empty(cls, rows: int, K: int, device):
+    def _empty(cls, x):
         torch = _torch()
         self = cls.__new__(cls)
-        self.codes = torch.empty((rows, K), dtype=torch.float8_e4m3fn, device=device)
-        self.scales = torch.empty(cls._scales_of(rows, K), dtype=torch.float32, device=device)
+        self.codes = x.new_empty(x.shape, dtype=torch.float8_e4m3fn)
+        self.scales = x.new_empty(cls._scales_of(*x.shape), dtype=torch.float32)
         return self
 
 
@@ -799,7 +800,7 @@ class Fp8Weights(_Fp8):
 def _fp8_quantize(kind, x, block_rows: int, stream):
     stride = _matrix(x, "x")
     _check_tensors("fp8_quantize", stream, None, (x,))
-    out = kind._empty(x.shape[0], x.shape[1], x.device)
+    out = kind._empty(x)
     _check(lib().pop_fp8_quantize(x.data_ptr(), stride, x.shape[0], x.shape[1], _dtype_code(x), block_rows, out.codes.data_ptr(), out.scales.data_ptr(),
                                   _stream_ptr(stream)), "pop_fp8_quantize")
     if stream is not None:
@@ -829,7 +830,10 @@ def fp8_linear(x, w: Fp8Weights, out=None, dtype=None, stream=None):
     M = xc.shape[0]
     made = out is None
     if made:
-        out = torch.empty((M, N), dtype=dtype if dtype is not None else torch.bfloat16 if rows else x.dtype, device=wc.device)
+        if rows or (dtype is not None and dtype is not x.dtype):
+            out = wc.new_empty((M, N), dtype=torch.bfloat16 if dtype is None else dtype)
+        else:
+            out = x.new_empty((M, N))
         y_stride = N
     else:
         if tuple(out.shape) != (M, N) or (dtype is not None and out.dtype is not dtype):
@@ -843,13 +847,20 @@ def fp8_linear(x, w: Fp8Weights, out=None, dtype=None, stream=None):
         if made and stream is not None:
             _used_on(stream, out)
         return out
-    need = 4 * _fp8_blocks(K) * M + 16 + M * K              # pop_fp8_linear_workspace
-    workspace = torch.empty(need, dtype=torch.uint8, device=wc.device)
+    need = _fp8_needs.get((M, K))
+    if need is None:
+        size = C.c_size_t()
+        _check(l.pop_fp8_linear_workspace(M, K, C.byref(size)), "pop_fp8_linear_workspace")
+        need = _fp8_needs[(M, K)] = size.value
+    workspace = wc.new_empty(need, dtype=torch.uint8) if need else None
     _check(l.pop_fp8_linear_rows(x.data_ptr(), stride, _dtype_code(x), M, wc.data_ptr(), ws.data_ptr(), N, K, out.data_ptr(), y_stride, _dtype_code(out),
-                                 workspace.data_ptr(), need, st), "pop_fp8_linear_rows")
+                                 _ptr(workspace), need, st), "pop_fp8_linear_rows")
     if stream is not None:
         _used_on(stream, workspace, out if made else None)
     return out
+
+
+_fp8_needs = {}             # bytes of workspace by (tokens, K): a few integers for every shape that a program uses
 
 
 def fp8_check(stream=None):
@@ -899,7 +910,7 @@ def block_norm(h, u=None, *, post_norm: bool = False, post_gain=None, gate=None,
     if h_out is not h or u is not None or h_scale != 1.0:
         a.h_out = h_out.data_ptr()
     if fp8:
-        f = Fp8Rows._empty(shape[0], d, h.device)
+        f = Fp8Rows._empty(h)
         a.f_codes, a.f_scales = f.codes.data_ptr(), f.scales.data_ptr()
     else:
         f = _like(h)
@@ -944,35 +955,39 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none",
     return freq, magnitude.value
 
 
-def _rope_rows(t, dim: int, what: str):
-    if t.dim() != 3 or t.shape[1] == 0:
-        raise ValueError(f"{what} must be [tokens, heads, {dim}]")
-    if t.is_contiguous() and t.shape[2] == dim:
-        return t.shape[1] * dim
-    return _rows(t, t.shape[1], dim, what)
+def _token_heads(t, T: int, dim: int, what: str, heads: Optional[int] = None) -> int:
+    """Token stride (in elements) of [T, heads, dim] whose heads lie one after another."""
+    shape = t.shape                                 # (one look: every question to a tensor costs a tenth of a microsecond)
+    if len(shape) != 3 or shape[0] != T or shape[2] != dim or shape[1] == 0 or (heads is not None and shape[1] != heads):
+        raise ValueError(f"{what} must be [{T}, {'heads' if heads is None else heads}, {dim}]")
+    heads = shape[1]
+    if t.is_contiguous():
+        return heads * dim
+    token, head, one = t.stride()
+    if T and ((dim > 1 and one != 1) or (heads > 1 and head != dim)):
+        raise ValueError(f"{what}: the heads of a token must be contiguous")
+    return token if T > 1 else heads * dim
 
 
 def rope(rope: Rope, positions, q, k=None, inverse: bool = False, q_out=None, k_out=None, stream=None):
     """pop_rope: q (and k) [T, heads, head_dim] turned to their positions (int32 [T]; rows of negative ones are left out): new tensors, or ``q_out`` /
     ``k_out``, which may be q and k themselves.  Returns q_out, or (q_out, k_out)."""
     torch = _torch()
-    dim = q.shape[-1]
-    qs = _rope_rows(q, dim, "q")
-    T = q.shape[0]
     _ints(positions, torch.int32, "positions")
-    if positions.shape[0] != T or (k is not None and k.shape[0] != T):
-        raise ValueError("q, k and positions must have one length")
+    T, dim = positions.size(0), q.size(-1)
+    qs = _token_heads(q, T, dim, "q")
     made = (q_out is None, k is not None and k_out is None)
     if made[0]:
         q_out = _like(q)
     if made[1]:
         k_out = _like(k)
-    if q_out.shape != q.shape or (k is not None and k_out.shape != k.shape) or (k is None and k_out is not None):
-        raise ValueError("outputs must have the shapes of q and k")
-    qos = _rope_rows(q_out, dim, "q_out")
+    if k is None and k_out is not None:
+        raise ValueError("k_out goes with k")
+    qos = q.size(1) * dim if made[0] else _token_heads(q_out, T, dim, "q_out", q.size(1))
     ks = kos = 0
     if k is not None:
-        ks, kos = _rope_rows(k, dim, "k"), _rope_rows(k_out, dim, "k_out")
+        ks = _token_heads(k, T, dim, "k")
+        kos = k.size(1) * dim if made[1] else _token_heads(k_out, T, dim, "k_out", k.size(1))
     _check_tensors("rope", stream, q.dtype, (q, k, q_out, k_out))
     _check_tensors("rope", None, None, (rope.freq, positions))
     _check(lib().pop_rope(C.byref(rope.desc), int(inverse), positions.data_ptr(), T, dim, _dtype_code(q), q.data_ptr(), qs, q.shape[1], q_out.data_ptr(), qos,
@@ -988,18 +1003,16 @@ def kv_append_rope(pages, rope: Rope, positions, q, k, v, slots, q_out=None, str
     torch = _torch()
     desc = _kv_desc(pages)
     H, D = desc.n_kv_heads, desc.head_dim
-    qs, ks, vs = _rope_rows(q, D, "q"), _rows(k, H, D, "k"), _rows(v, H, D, "v")
-    T = q.shape[0]
     _ints(slots, torch.int64, "slots")
     _ints(positions, torch.int32, "positions")
-    if k.shape[0] != T or v.shape[0] != T or slots.shape[0] != T or positions.shape[0] != T:
+    T = slots.size(0)
+    if positions.size(0) != T:
         raise ValueError("q, k, v, positions and slots must have one length")
+    qs, ks, vs = _token_heads(q, T, D, "q"), _token_heads(k, T, D, "k", H), _token_heads(v, T, D, "v", H)
     made = q_out is None
     if made:
         q_out = _like(q)
-    elif q_out.shape != q.shape:
-        raise ValueError("q_out must have q's shape")
-    qos = _rope_rows(q_out, D, "q_out")
+    qos = q.size(1) * D if made else _token_heads(q_out, T, D, "q_out", q.size(1))
     _check_tensors("kv_append_rope", stream, q.dtype, (q, k, v, q_out))
     _check_tensors("kv_append_rope", None, None, (pages, rope.freq, positions, slots))
     _check(lib().pop_kv_append_rope(C.byref(desc), C.byref(rope.desc), positions.data_ptr(), q.data_ptr(), qs, q.shape[1], q_out.data_ptr(), qos,

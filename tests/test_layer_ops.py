@@ -518,8 +518,8 @@ def test_fp8_refusals():
         assert lin(**kw) == status, kw
     need = C.c_size_t()
     assert l.pop_fp8_linear_workspace(3, 64, None) == BAD and l.pop_fp8_linear_workspace(3, 63, C.byref(need)) == NO
-    assert l.pop_fp8_linear_workspace(3, 64, C.byref(need)) == 0 and need.value >= 3 * 64 + 12
-    rows = lambda ws=A, n=1 << 20, x=A: l.pop_fp8_linear_rows(x, 64, 1, 4, A, A, 64, 64, A, 64, 1, ws, n, None)                                                      # noqa: E731
+    assert l.pop_fp8_linear_workspace(300, 64, C.byref(need)) == 0 and need.value >= 300 * 64 + 1200
+    rows = lambda ws=A, n=1 << 20, x=A: l.pop_fp8_linear_rows(x, 64, 1, 400, A, A, 64, 64, A, 64, 1, ws, n, None)                                                      # noqa: E731
     assert rows(ws=None) == BAD and rows(n=8) == BAD and rows(ws=A + 8) == BAD and rows(x=None) == BAD
 
 
