@@ -24,12 +24,31 @@ struct Angles {
     int inverse;
 };
 
-// (cos, sin) of pair i at position p
-__device__ __forceinline__ float2 turn(const Angles& A, int p, int i) {
-    const u64 part = (u64)p * A.freq[i];                                     // of a turn, in 2^-64
-    double s, c;
-    sincospi((double)(long long)part * 0x1p-63, &s, &c);
-    return make_float2((float)(c * A.magnitude), (float)((A.inverse ? -s : s) * A.magnitude));
+// (cos, sin) of pair i at position p.  The nearest quarter turn is taken off the fraction in integers; what is left, at most an eighth of a turn either way,
+// goes through the Taylor series of sine and cosine up to x^15 and x^16 (the next terms are below 2^-54), and the quarter turns exchange and negate the two.
+// (CUDA's sincospi takes any double, in about twice as many instructions.)
+__device__ __forceinline__ float2 turn(const Angles& A, int p, u64 freq) {
+    const u64 part = (u64)p * freq;                                          // of a turn, in 2^-64
+    const u32 quarter = (u32)((part + (1ull << 61)) >> 62);                  // nearest
+    const double x = (double)(long long)(part - ((u64)quarter << 62)) * (6.283185307179586476925286766559 * 0x1p-64), y = x * x;
+    double s = -1.0 / 1307674368000.0, c = 1.0 / 20922789888000.0;
+    s = fma(s, y, 1.0 / 6227020800.0);
+    c = fma(c, y, -1.0 / 87178291200.0);
+    s = fma(s, y, -1.0 / 39916800.0);
+    c = fma(c, y, 1.0 / 479001600.0);
+    s = fma(s, y, 1.0 / 362880.0);
+    c = fma(c, y, -1.0 / 3628800.0);
+    s = fma(s, y, -1.0 / 5040.0);
+    c = fma(c, y, 1.0 / 40320.0);
+    s = fma(s, y, 1.0 / 120.0);
+    c = fma(c, y, -1.0 / 720.0);
+    s = fma(s, y, -1.0 / 6.0);
+    c = fma(c, y, 1.0 / 24.0);
+    c = fma(c, y, -0.5);
+    s = fma(s * y, x, x);
+    c = fma(c, y, 1.0);
+    const float a = (float)((quarter & 1u ? s : c) * A.magnitude), b = (float)((quarter & 1u ? c : s) * A.magnitude);
+    return make_float2(quarter + 1u & 2u ? -a : a, (quarter >> 1 & 1u) != (u32)A.inverse ? -b : b);
 }
 __device__ __forceinline__ void rotate(float& a, float& b, float2 cs) {
     const float x = __fsub_rn(__fmul_rn(a, cs.x), __fmul_rn(b, cs.y)), y = __fadd_rn(__fmul_rn(b, cs.x), __fmul_rn(a, cs.y));
@@ -84,7 +103,7 @@ template <typename T, int E> __global__ void __launch_bounds__(256) rope_kernel(
     if (X.heads == 0) return;
     for (int i = threadIdx.x; i < n * pairs; i += 256) {
         const int p = R.A.positions[t0 + i / pairs];
-        if (p >= 0) table[i] = turn(R.A, p, i % pairs);
+        if (p >= 0) table[i] = turn(R.A, p, R.A.freq[i % pairs]);
     }
     __syncthreads();
     const int turned = pairs / E, per_head = turned + X.copy, per_token = X.heads * per_head;
@@ -134,7 +153,7 @@ template <typename T, int G> __global__ void __launch_bounds__(256) rope_append_
     kv::follow();
     const int t = blockIdx.x, pairs = P.A.pairs, p = P.A.positions[t];
     if (p < 0) return;
-    for (int i = threadIdx.x; i < pairs; i += 256) table[i] = turn(P.A, p, i);
+    for (int i = threadIdx.x; i < pairs; i += 256) table[i] = turn(P.A, p, P.A.freq[i]);
     __syncthreads();
     const int Hk = P.S.H, per_token = (P.Hq + 2 * Hk) * PIECES;
     const long long slot = P.S.slots[t];
@@ -211,7 +230,7 @@ template <int G, bool INTERLEAVED> __device__ __forceinline__ void rotate_pieces
     }
 }
 
-template <typename T, int G, bool INTERLEAVED> __global__ void __launch_bounds__(WARPS * 32, 2) rope_append_kernel(const AppendArgs P) {
+template <typename T, int G, bool INTERLEAVED> __global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 2 ? 3 : 2) rope_append_kernel(const AppendArgs P) {
     constexpr int D = 64 * G, WORDS = kv::tile_bytes(D) / 4, PIECES = 2 * G;
     __shared__ __align__(16) float2 table[2 * WINDOW][D / 2 + 8];
     __shared__ uint4 codes[WARPS][G * 32];
@@ -219,9 +238,23 @@ template <typename T, int G, bool INTERLEAVED> __global__ void __launch_bounds__
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pairs = P.A.pairs, t0 = blockIdx.x * WINDOW, Hk = P.S.H;
     const kv::Window w = kv::look(P.S, t0, P.A.positions);
     const int first = w.whole ? __ffs(w.whole) - 1 : 0;                      // (the same in all warps)
-    for (int i = threadIdx.x; i < (WINDOW + first) * pairs; i += WARPS * 32) {
-        const int t = i / pairs, pair = i - t * pairs, p = t0 + t < P.A.T ? P.A.positions[t0 + t] : -1;
-        table[t][table_at<INTERLEAVED>(pair)] = p >= 0 ? turn(P.A, p, pair) : make_float2(1.f, 0.f);
+    constexpr int AT_ONCE = 4;                   // angles of a thread that are worked out side by side
+    for (int i0 = threadIdx.x; i0 < (WINDOW + first) * pairs; i0 += WARPS * 32 * AT_ONCE) {
+        int p[AT_ONCE];
+        u64 freq[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int i = i0 + u * WARPS * 32, t = i / pairs;
+            const bool in = i < (WINDOW + first) * pairs;
+            p[u] = in && t0 + t < P.A.T ? P.A.positions[t0 + t] : -1;
+            freq[u] = in ? P.A.freq[i - t * pairs] : 0ull;
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int i = i0 + u * WARPS * 32, t = i / pairs;
+            const float2 cs = turn(P.A, p[u], freq[u]);
+            if (i < (WINDOW + first) * pairs) table[t][table_at<INTERLEAVED>(i - t * pairs)] = cs;          // (of no use where p is negative)
+        }
     }
     __syncthreads();
     const int q_tasks = (P.Hq + HEADS - 1) / HEADS, tasks = 2 * Hk + 2 * q_tasks, e = lane & 3;
