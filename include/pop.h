@@ -422,7 +422,8 @@ int pop_kv_attention(const pop_kv_cache_t* cache, const void* q, long long q_str
  *   f [n_tokens][d] contiguous of `dtype`, or NULL.  f_codes [n_tokens][d] with f_scales [ceil(d / 128)][n_tokens]: the same f as
  *   pop_fp8_quantize would give it for f in 32 bits, or NULL (both, one, or neither of f and f_codes may be asked for; d a multiple of 16, all
  *   pointers and rows 16-byte aligned for the codes).
- * Any d up to POP_NORM_MAX_D.  Arithmetic and sums are 32-bit, f comes from h' before h' is rounded to `dtype`.
+ * Any d up to POP_NORM_MAX_D.  Arithmetic and sums are 32-bit, f comes from h' before h' is rounded to `dtype`.  So rms(x) is 0 for a row whose squares' sum
+ * leaves 32 bits (elements beyond some 1e18), and an element that is not finite makes itself NaN and its row's others 0 or NaN.
  */
 #define POP_NORM_MAX_D  32768
 typedef struct {
@@ -481,10 +482,11 @@ int pop_fp8_check(void* cuda_stream);
  *   beta_fast, beta_slow: 0 = 32 and 1 (YARN), 4 and 1 (BANDS).  *magnitude receives that factor, 1 for the others.
  * pop_rope: q [n_tokens][q_heads][head_dim] -> q_out, and k with k_heads alike (k NULL: q alone).  Rows may be strided, heads of a token are contiguous;
  *   the outputs may be the inputs (then with the same strides).  freq: device array of rot_dim / 2.  inverse: turned by -p * w (the transposed map).
- *   A token whose position is negative is left out: its rows are not written.  head_dim and rot_dim even, rot_dim <= head_dim <= POP_ROPE_MAX_DIM.
+ *   A token whose position is negative is left out: its rows are not written.  head_dim and rot_dim even, rot_dim <= head_dim <= POP_ROPE_MAX_DIM, at most 2^24
+ *   elements to a token.
  *   cos and sin are computed in 64 bits and rounded to fp32; every product and sum of the rotation is an fp32 operation.
  * pop_kv_append_rope: q -> q_out as above, and k, rotated in fp32, and v into their slots of the 4-bit cache as pop_kv_append does it (a token whose
- *   slot is outside the cache or whose position is negative is not stored).  Heads, alignment and strides as in pop_kv_append.
+ *   slot is outside the cache or whose position is negative is not stored).  Heads, alignment and strides as in pop_kv_append; q_out must not overlap q.
  */
 #define POP_ROPE_MAX_DIM  512
 typedef enum { POP_ROPE_NONE = 0, POP_ROPE_LINEAR = 1, POP_ROPE_NTK = 2, POP_ROPE_YARN = 3, POP_ROPE_BANDS = 4 } pop_rope_scaling_t;

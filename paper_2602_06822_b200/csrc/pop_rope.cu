@@ -380,6 +380,7 @@ template <typename T> cudaError_t rope(RopeArgs R, bool vectors, cudaStream_t st
     }
     R.tokens = TABLE / R.A.pairs;
     if (R.tokens > 1 && (R.A.T + R.tokens - 1) / R.tokens < 1024) R.tokens = 1;      // few tokens: a CTA for each
+    while (R.tokens > 1 && items * R.tokens > 1 << 20) R.tokens /= 2;                 // (items of a CTA stay far below 2^31)
     const long long parts = (items * R.tokens + 1023) / 1024;                         // some four items a thread
     const dim3 grid((R.A.T + R.tokens - 1) / R.tokens, 2 * (u32)(parts < 1 ? 1 : parts > 16 ? 16 : parts));
     return vectors ? kv::launch(rope_kernel<T, 16 / (int)sizeof(T)>, grid, 256, st, R) : kv::launch(rope_kernel<T, 1>, grid, 256, st, R);

@@ -713,7 +713,17 @@ class KVCache:
 # current device.
 # ---------------------------------------------------------------------------------------------------------------------
 
-def _check_tensors(what: str, stream, dtype, tensors):
+def _on_stream(stream, call, *args, **kw):
+    """A call on another stream is made with that one current: what it allocates then belongs to it, and cannot be memory that work of this one still uses."""
+    torch = _torch()
+    _on_current_device(stream)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+    with torch.cuda.stream(stream):
+        return call(*args, **kw)
+
+
+def _check_tensors(what: str, dtype, tensors):
     """What the tensors of a call (or None) have to be: on the current device, whose kernels follow their addresses, of one type (if ``dtype`` is given),
     and without a gradient, which would end here unnoticed, as the calls have no backward pass."""
     torch = _torch()
@@ -727,8 +737,6 @@ def _check_tensors(what: str, stream, dtype, tensors):
             raise TypeError(f"{what}: dtype mismatch ({t.dtype}, {dtype})")
         if t.requires_grad and torch.is_grad_enabled():
             raise ValueError(f"{what} has no backward pass: detach() what requires a gradient, or call under torch.no_grad()")
-    if stream is not None:
-        _on_current_device(stream)
 
 
 def _matrix(t, what: str, d: Optional[int] = None) -> int:
@@ -797,14 +805,14 @@ class Fp8Weights(_Fp8):
         return (_fp8_blocks(rows), _fp8_blocks(K))
 
 
-def _fp8_quantize(kind, x, block_rows: int, stream):
+def _fp8_quantize(kind, x, block_rows: int, stream=None):
+    if stream is not None:
+        return _on_stream(stream, _fp8_quantize, kind, x, block_rows)
     stride = _matrix(x, "x")
-    _check_tensors("fp8_quantize", stream, None, (x,))
+    _check_tensors("fp8_quantize", None, (x,))
     out = kind._empty(x)
     _check(lib().pop_fp8_quantize(x.data_ptr(), stride, x.shape[0], x.shape[1], _dtype_code(x), block_rows, out.codes.data_ptr(), out.scales.data_ptr(),
-                                  _stream_ptr(stream)), "pop_fp8_quantize")
-    if stream is not None:
-        _used_on(stream, out.codes, out.scales)
+                                  _stream_ptr()), "pop_fp8_quantize")
     return out
 
 
@@ -821,6 +829,8 @@ def fp8_weights(w, stream=None) -> Fp8Weights:
 def fp8_linear(x, w: Fp8Weights, out=None, dtype=None, stream=None):
     """pop_fp8_linear: x [M, K] (bf16 or fp32, quantised on the way, or Fp8Rows) times w^T -> [M, N] of ``dtype`` (x's own by default, bfloat16
     for Fp8Rows).  ``out``: rows may be strided."""
+    if stream is not None:
+        return _on_stream(stream, fp8_linear, x, w, out, dtype)
     torch = _torch()
     wc, ws = w.codes, w.scales
     N, K = wc.shape
@@ -839,13 +849,11 @@ def fp8_linear(x, w: Fp8Weights, out=None, dtype=None, stream=None):
         if tuple(out.shape) != (M, N) or (dtype is not None and out.dtype is not dtype):
             raise ValueError(f"out must be [{M}, {N}] of the dtype asked for")
         y_stride = _matrix(out, "out", N)
-    _check_tensors("fp8_linear", stream, None, (xc, wc, ws, x.scales if rows else None, None if made else out))
-    l, st = lib(), _stream_ptr(stream)
+    _check_tensors("fp8_linear", None, (xc, wc, ws, x.scales if rows else None, None if made else out))
+    l, st = lib(), _stream_ptr()
     if rows:
         _check(l.pop_fp8_linear(xc.data_ptr(), x.scales.data_ptr(), M, wc.data_ptr(), ws.data_ptr(), N, K, out.data_ptr(), y_stride, _dtype_code(out), st),
                "pop_fp8_linear")
-        if made and stream is not None:
-            _used_on(stream, out)
         return out
     need = _fp8_needs.get((M, K))
     if need is None:
@@ -855,8 +863,6 @@ def fp8_linear(x, w: Fp8Weights, out=None, dtype=None, stream=None):
     workspace = wc.new_empty(need, dtype=torch.uint8) if need else None
     _check(l.pop_fp8_linear_rows(x.data_ptr(), stride, _dtype_code(x), M, wc.data_ptr(), ws.data_ptr(), N, K, out.data_ptr(), y_stride, _dtype_code(out),
                                  _ptr(workspace), need, st), "pop_fp8_linear_rows")
-    if stream is not None:
-        _used_on(stream, workspace, out if made else None)
     return out
 
 
@@ -873,6 +879,9 @@ def block_norm(h, u=None, *, post_norm: bool = False, post_gain=None, gate=None,
     """pop_block_norm: (h', f) with h' = h_scale h + u_scale gate b, b = u or rms(u) post_gain, f = rms(h') gain.
     h, u [T, d] (rows may be strided); post_gain, gain [d]; gate [T, d], [1, d] or [d].  ``fp8``: f as Fp8Rows.  ``h_out`` receives h' (h itself, or
     another tensor; a new one by default).  Without u (and h_scale 1) h' is h, and nothing is written."""
+    if stream is not None:
+        return _on_stream(stream, block_norm, h, u, post_norm=post_norm, post_gain=post_gain, gate=gate, h_scale=h_scale, u_scale=u_scale, gain=gain, eps=eps,
+                          fp8=fp8, h_out=h_out)
     a = BlockNormArgs()
     a.h_stride = d = _matrix(h, "h")
     shape = h.shape
@@ -915,13 +924,11 @@ def block_norm(h, u=None, *, post_norm: bool = False, post_gain=None, gate=None,
     else:
         f = _like(h)
         a.f = f.data_ptr()
-    _check_tensors("block_norm", stream, h.dtype, (h, u, post_gain, gate, gain, None if made else h_out))
+    _check_tensors("block_norm", h.dtype, (h, u, post_gain, gate, gain, None if made else h_out))
     a.h_scale, a.u_scale, a.eps = h_scale, u_scale, eps
     if post_norm:
         a.post_norm = 1
-    _check(lib().pop_block_norm(C.byref(a), shape[0], d, _dtype_code(h), _stream_ptr(stream)), "pop_block_norm")
-    if stream is not None:
-        _used_on(stream, *((f.codes, f.scales) if fp8 else (f,)), h_out if made else None)
+    _check(lib().pop_block_norm(C.byref(a), shape[0], d, _dtype_code(h), _stream_ptr()), "pop_block_norm")
     return h_out, f
 
 
@@ -972,6 +979,9 @@ def _token_heads(t, T: int, dim: int, what: str, heads: Optional[int] = None) ->
 def rope(rope: Rope, positions, q, k=None, inverse: bool = False, q_out=None, k_out=None, stream=None):
     """pop_rope: q (and k) [T, heads, head_dim] turned to their positions (int32 [T]; rows of negative ones are left out): new tensors, or ``q_out`` /
     ``k_out``, which may be q and k themselves.  Returns q_out, or (q_out, k_out)."""
+    if stream is not None:
+        # (the function's own name is that of its first parameter)
+        return _on_stream(stream, globals()["rope"], rope, positions, q, k, inverse, q_out, k_out)
     torch = _torch()
     _ints(positions, torch.int32, "positions")
     T, dim = positions.size(0), q.size(-1)
@@ -988,18 +998,18 @@ def rope(rope: Rope, positions, q, k=None, inverse: bool = False, q_out=None, k_
     if k is not None:
         ks = _token_heads(k, T, dim, "k")
         kos = k.size(1) * dim if made[1] else _token_heads(k_out, T, dim, "k_out", k.size(1))
-    _check_tensors("rope", stream, q.dtype, (q, k, q_out, k_out))
-    _check_tensors("rope", None, None, (rope.freq, positions))
+    _check_tensors("rope", q.dtype, (q, k, q_out, k_out))
+    _check_tensors("rope", None, (rope.freq, positions))
     _check(lib().pop_rope(C.byref(rope.desc), int(inverse), positions.data_ptr(), T, dim, _dtype_code(q), q.data_ptr(), qs, q.shape[1], q_out.data_ptr(), qos,
-                          _ptr(k), ks, 0 if k is None else k.shape[1], _ptr(k_out), kos, _stream_ptr(stream)), "pop_rope")
-    if stream is not None:
-        _used_on(stream, q_out if made[0] else None, k_out if made[1] else None)
+                          _ptr(k), ks, 0 if k is None else k.shape[1], _ptr(k_out), kos, _stream_ptr()), "pop_rope")
     return q_out if k is None else (q_out, k_out)
 
 
 def kv_append_rope(pages, rope: Rope, positions, q, k, v, slots, q_out=None, stream=None):
     """pop_kv_append_rope: q [T, heads, head_dim] and k [T, n_kv_heads, head_dim] turned to their positions; k and v quantised into the slots (int64 [T])
     of the 4-bit cache, the turned q returned.  Token rows may be strided."""
+    if stream is not None:
+        return _on_stream(stream, kv_append_rope, pages, rope, positions, q, k, v, slots, q_out)
     torch = _torch()
     desc = _kv_desc(pages)
     H, D = desc.n_kv_heads, desc.head_dim
@@ -1013,10 +1023,8 @@ def kv_append_rope(pages, rope: Rope, positions, q, k, v, slots, q_out=None, str
     if made:
         q_out = _like(q)
     qos = q.size(1) * D if made else _token_heads(q_out, T, D, "q_out", q.size(1))
-    _check_tensors("kv_append_rope", stream, q.dtype, (q, k, v, q_out))
-    _check_tensors("kv_append_rope", None, None, (pages, rope.freq, positions, slots))
+    _check_tensors("kv_append_rope", q.dtype, (q, k, v, q_out))
+    _check_tensors("kv_append_rope", None, (pages, rope.freq, positions, slots))
     _check(lib().pop_kv_append_rope(C.byref(desc), C.byref(rope.desc), positions.data_ptr(), q.data_ptr(), qs, q.shape[1], q_out.data_ptr(), qos,
-                                    k.data_ptr(), ks, v.data_ptr(), vs, _dtype_code(q), slots.data_ptr(), T, _stream_ptr(stream)), "pop_kv_append_rope")
-    if made and stream is not None:
-        _used_on(stream, q_out)
+                                    k.data_ptr(), ks, v.data_ptr(), vs, _dtype_code(q), slots.data_ptr(), T, _stream_ptr()), "pop_kv_append_rope")
     return q_out

@@ -14,6 +14,8 @@ Tolerances, derived before the first run (u = 2^-24, half a step of fp32; H = ha
          one rounding in bf16.  A cosine in 64 bits may round to the other fp32 neighbour only within 2^-29 of a step of the border: not in these inputs.
 """
 import ctypes as C
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -201,6 +203,7 @@ def check_linear(M, N, K, x_dtype, rng, x=None, **kw):
 @pytest.mark.parametrize("M,N,K", [
     (1, 1, 16), (1, 4096, 4096), (2, 17, 128), (8, 129, 1360), (9, 300, 256), (16, 1000, 4112), (17, 64, 144), (17, 1000, 4096), (31, 129, 11008),
     (64, 4096, 512), (100, 250, 2000), (127, 128, 128), (128, 256, 1024), (129, 257, 1040), (333, 1000, 1360), (1000, 4100, 528), (600, 12000, 272),
+    (100, 64, 16), (300, 300, 16), (38000, 100, 144), (33, 40000, 128), (2, 60000, 256), (16, 64, 37904), (5, 64, 36864),
 ])
 def test_linear_sizes(M, N, K, dtype):
     check_linear(M, N, K, dtype, np.random.default_rng(M * 31 + N * 7 + K))
@@ -307,6 +310,18 @@ def test_rope_equals_the_oracle(T, H, Hk, D, rot, interleaved, dtype):
     rows = torch.cat([q, k], 1)
     pop.rope(r, p, rows[:, :H], rows[:, H:], inverse=True, q_out=rows[:, :H], k_out=rows[:, H:])
     assert torch.equal(rows, torch.cat([gq, gk], 1))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,H,D,rot", [(5, 70000, 64, 2), (1, 1, 512, 2), (3000, 9, 130, 2)])
+def test_rope_of_very_many_heads_and_very_few_pairs(T, H, D, rot):
+    x = (torch.arange(T * H * D, device=DEV) % 251).view(T, H, D).bfloat16()
+    r, pos = pop.Rope(rot, device=DEV), to_dev(np.arange(T))
+    got = pop.rope(r, pos, x)
+    cos, sin = lo.cos_sin(pop.rope_frequencies(rot)[0], 1.0, np.arange(T))
+    at = [0, H // 2, H - 1]
+    check_equal(got[:, at], lo.rotate(host(x[:, at]), cos, sin, False), BF16)
+    assert torch.equal(got[..., rot:], x[..., rot:])
 
 
 @pytest.mark.gpu
@@ -458,6 +473,40 @@ def test_layer_captured_and_replayed(tokens):
         torch.cuda.synchronize()
         for o in outs:
             assert torch.equal(o[0], want[i][0]) and torch.equal(o[1], want[i][1])
+
+
+@pytest.mark.gpu
+def test_captured_as_the_first_calls_of_a_process():
+    """Nothing of the library has run before the capture: what the calls set up for themselves, they may set up there."""
+    code = """
+import torch, __graft_entry__ as ge
+from paper_2602_06822_b200 import pop
+ge.build()
+x = torch.arange(300 * 512, device="cuda:0").reshape(300, 512).remainder(37).bfloat16()
+codes, scales = torch.full((512, 512), 56, dtype=torch.uint8, device="cuda:0").view(torch.float8_e4m3fn), torch.ones(4, 4, device="cuda:0")
+r, pos, slots = pop.Rope(64, device="cuda:0"), torch.arange(300, dtype=torch.int32, device="cuda:0"), torch.arange(300, device="cuda:0")
+pages = pop.kv_pages(6, 64, 8, 64, "cuda:0")
+w = pop.Fp8Weights(codes, scales)
+def step():
+    h, f = pop.block_norm(x, x, fp8=True)
+    y = [pop.fp8_linear(f, w), pop.fp8_linear(h, w), pop.fp8_linear(h[:3], w), pop.fp8_linear(pop.fp8_quantize(h[:40]), w)]
+    q = pop.kv_append_rope(pages, r, pos, *(y[0].view(300, 8, 64),) * 3, slots)
+    return [h, f.codes.float(), *y, q, pop.rope(r, pos, q)]
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    a = step()
+g.replay()
+torch.cuda.synchronize()
+for p, q in zip(a, step()):
+    assert torch.equal(p, q)
+pop.fp8_check()
+print("fine")
+"""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0 and "fine" in out.stdout, out.stderr[-2000:]
 
 
 @pytest.mark.gpu
