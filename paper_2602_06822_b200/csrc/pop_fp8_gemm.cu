@@ -97,6 +97,10 @@ template <int CG> __device__ __forceinline__ void tma_load(u32 mine, u32 dst, co
         asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t@q cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
                      ::"r"(dst), "l"(reinterpret_cast<u64>(map)), "r"(x), "r"(y), "r"(bar), "r"(mine) : "memory");
 }
+__device__ __forceinline__ void tma_prefetch(u32 mine, const CUtensorMap* map, int x, int y) {              // to L2
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %3, 0;\n\t@q cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];\n\t}"
+                 ::"l"(reinterpret_cast<u64>(map)), "r"(x), "r"(y), "r"(mine) : "memory");
+}
 __device__ __forceinline__ void prefetch_map(u32 mine, const CUtensorMap* map) {
     asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q prefetch.tensormap [%0];\n\t}" ::"l"(reinterpret_cast<u64>(map)), "r"(mine) : "memory");
 }
@@ -635,7 +639,12 @@ __global__ void __launch_bounds__(FEW_THREADS, Few<TN>::PER_SM) fp8_few_kernel(c
         tma_load<1>(mine, ring + (u32)(s * L::STAGE), &map_w, (kb0 + i) * fp8::BLOCK, tile * 128, full + 8 * s);
         if (!L::RESIDENT) tma_load<1>(mine, ring + (u32)(s * L::STAGE) + W_BYTES, &map_x, (kb0 + i) * fp8::BLOCK, 0, full + 8 * s);
     };
-    if (warp == 0) prefetch_map(mine, &map_w);                               // while the kernel before this one winds down
+    // While the kernel before this one winds down, the tiles that are loaded first are asked for as far as L2 (which is coherent: nothing is read of them
+    // here): 13 tokens through 12288 x 4096 12.1 -> 11.7 us, the fused decoder's step 1.5 % shorter.  All of the range's tiles at once: 12.6.
+    if (warp == 0) {
+        prefetch_map(mine, &map_w);
+        for (int i = 0; i < min(F.stages, n); ++i) tma_prefetch(mine, &map_w, (kb0 + i) * fp8::BLOCK, tile * 128);
+    }
     if (warp == 1) tmem_alloc<1>(smem_u32(&tmem_slot), L::COLS);
     kv::follow();
     if (warp == 0)

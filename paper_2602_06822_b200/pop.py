@@ -178,6 +178,7 @@ def set_config(**fields) -> Config:
 
 def release_cached_memory():
     _kv_workspaces.clear()              # (their memory goes back to torch, in the order of the streams that they were made on)
+    _fp8_workspaces.clear()
     _check(lib().pop_release_cached_memory(), "pop_release_cached_memory")
 
 
@@ -860,13 +861,23 @@ def fp8_linear(x, w: Fp8Weights, out=None, dtype=None, stream=None):
         size = C.c_size_t()
         _check(l.pop_fp8_linear_workspace(M, K, C.byref(size)), "pop_fp8_linear_workspace")
         need = _fp8_needs[(M, K)] = size.value
-    workspace = wc.new_empty(need, dtype=torch.uint8) if need else None
+    workspace = None
+    if need:
+        key = (wc.get_device(), st)
+        workspace = _fp8_workspaces.get(key)
+        if workspace is None or workspace.numel() < need or torch._C._cuda_isCurrentStreamCapturing():
+            workspace = wc.new_empty(need, dtype=torch.uint8)
+            if need <= POP_FP8_KEPT and not torch._C._cuda_isCurrentStreamCapturing():
+                _fp8_workspaces[key] = workspace
     _check(l.pop_fp8_linear_rows(x.data_ptr(), stride, _dtype_code(x), M, wc.data_ptr(), ws.data_ptr(), N, K, out.data_ptr(), y_stride, _dtype_code(out),
                                  _ptr(workspace), need, st), "pop_fp8_linear_rows")
     return out
 
 
 _fp8_needs = {}             # bytes of workspace by (tokens, K): a few integers for every shape that a program uses
+# The workspace of small calls, kept for each (device, stream), whose calls run one after another; a captured call has its own from the graph's memory.
+_fp8_workspaces = {}
+POP_FP8_KEPT = 8 << 20
 
 
 def fp8_check(stream=None):

@@ -510,6 +510,38 @@ print("fine")
 
 
 @pytest.mark.gpu
+def test_products_of_two_streams_side_by_side():
+    """Calls that need a workspace, on two streams at once and of alternating sizes: each has its own, and a captured one a third."""
+    rng = np.random.default_rng(12)
+    w = pop.fp8_weights(rnd(rng, (1000, 2048), BF16, 0.05))
+    xs = [rnd(rng, (m, 2048), BF16) for m in (100, 700, 300, 100)]
+    want = [pop.fp8_linear(x, w) for x in xs]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] += [pop.fp8_linear(x, w) for x in (xs if i else xs[::-1])]
+    torch.cuda.synchronize()
+    for i, outs in enumerate(got):
+        for j, y in enumerate(outs):
+            assert torch.equal(y, want[j % 4 if i else 3 - j % 4])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        y = pop.fp8_linear(xs[0], w)
+    for _ in range(3):
+        g.replay()
+        z = pop.fp8_linear(xs[3], w)
+        with torch.cuda.stream(streams[0]):
+            pop.fp8_linear(xs[2], w)
+    torch.cuda.synchronize()
+    assert torch.equal(y, want[0]) and torch.equal(z, want[3])
+    pop.release_cached_memory()
+    assert not pop._fp8_workspaces and torch.equal(pop.fp8_linear(xs[1], w), want[1])
+
+
+@pytest.mark.gpu
 def test_calls_on_another_stream():
     rng = np.random.default_rng(8)
     x, big = rnd(rng, (300, 512), BF16), rnd(rng, (4096, 4096), F32)
