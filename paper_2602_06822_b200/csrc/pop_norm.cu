@@ -5,7 +5,8 @@
 // Bound by memory: h and u are read, h' and f written, once each.  So a row is kept in registers from its first load to its
 // last store: one CTA a row, a thread has up to V vectors of 16 bytes of it, and the row's one or two sums go through
 // shared memory.  All that is read is asked for at once, so that the first sum's barrier costs no second trip to memory.  16384 rows of 4096 in bf16, with post-norm and
-// a gate for every token (671 MB): 100 us, 6.7 TB/s.  Rows that are not aligned to 16 bytes go element by element (16384 of 1001: 48 us, 2.7 TB/s).
+// a gate for every token (671 MB): 100 us, 6.7 TB/s.  Rows that are not aligned to 16 bytes go by pairs or element by element (16384 of 1002 | 1001:
+// 38 | 48 us).
 #include "pop_fp8.cuh"
 
 namespace {
@@ -29,7 +30,7 @@ __device__ __forceinline__ float cta_sum(float x, float* part) {
     return warp_sum(lane < warps ? part[lane] : 0.f);
 }
 
-// E consecutive elements: a vector of 16 bytes, or (E = 1) one element.
+// E consecutive elements: a vector of 16 bytes, a pair, or (E = 1) one element.
 template <typename T, int E> struct Piece;
 template <> struct Piece<float, 4> {
     typedef float4 raw;
@@ -45,6 +46,16 @@ template <> struct Piece<__nv_bfloat16, 8> {
         for (int i = 0; i < 4; ++i) r[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
         return *reinterpret_cast<const uint4*>(r);
     }
+};
+template <> struct Piece<float, 2> {
+    typedef float2 raw;
+    __device__ static void open(const raw& r, float (&x)[2]) { x[0] = r.x; x[1] = r.y; }
+    __device__ static raw close(const float (&x)[2]) { return make_float2(x[0], x[1]); }
+};
+template <> struct Piece<__nv_bfloat16, 2> {
+    typedef __nv_bfloat162 raw;
+    __device__ static void open(const raw& r, float (&x)[2]) { x[0] = __low2float(r); x[1] = __high2float(r); }
+    __device__ static raw close(const float (&x)[2]) { return __floats2bfloat162_rn(x[0], x[1]); }
 };
 template <typename T> struct Piece<T, 1> {
     typedef T raw;
@@ -193,14 +204,14 @@ extern "C" int pop_block_norm(const pop_block_norm_t* a, int n_tokens, int d, po
                           (uintptr_t)a->f;
     if (any & (es - 1)) return POP_ERR_INVALID_ARG;
     const long long strides = (long long)d | a->h_stride | (a->u ? a->u_stride : 0) | (a->h_out ? a->h_out_stride : 0) | (a->gate ? a->gate_stride : 0);
-    const bool vectors = (any & 15u) == 0 && (strides * (long long)es) % 16 == 0;
+    const bool vectors = (any & 15u) == 0 && (strides * (long long)es) % 16 == 0, pairs = (any & (2 * es - 1)) == 0 && strides % 2 == 0;
     if (a->f_codes && (!vectors || d % 16 != 0 || ((uintptr_t)a->f_codes & 15u) != 0 || ((uintptr_t)a->f_scales & 3u) != 0)) return POP_ERR_UNSUPPORTED;
     const NormArgs N = {*a, n_tokens, d};
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (dtype == POP_BF16)
-        POP_CUDA((vectors ? launch_norm<__nv_bfloat16, 8>(N, st) : launch_norm<__nv_bfloat16, 1>(N, st)));
+        POP_CUDA((vectors ? launch_norm<__nv_bfloat16, 8>(N, st) : pairs ? launch_norm<__nv_bfloat16, 2>(N, st) : launch_norm<__nv_bfloat16, 1>(N, st)));
     else
-        POP_CUDA((vectors ? launch_norm<float, 4>(N, st) : launch_norm<float, 1>(N, st)));
+        POP_CUDA((vectors ? launch_norm<float, 4>(N, st) : pairs ? launch_norm<float, 2>(N, st) : launch_norm<float, 1>(N, st)));
     POP_LAUNCHED();
     return POP_OK;
 }

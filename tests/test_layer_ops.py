@@ -85,7 +85,7 @@ def check_norm(h, u, dtype, post=False, post_gain=None, gate=None, h_scale=1.0, 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("T,d", [(1, 1), (1, 4096), (3, 7), (5, 128), (33, 1001), (2, 8192), (2, 8200), (3, 12289), (1, 32768), (700, 64)])
+@pytest.mark.parametrize("T,d", [(1, 1), (1, 4096), (3, 7), (5, 128), (33, 1001), (2, 8192), (2, 8200), (3, 12289), (1, 32768), (700, 64), (3, 1002), (2, 30002), (900, 514)])
 def test_norm_sizes(T, d, dtype):
     rng = np.random.default_rng(T * 100003 + d)
     h, u, g1, g2 = (rnd(rng, s, dtype) for s in ((T, d), (T, d), (d,), (d,)))
@@ -97,7 +97,7 @@ def test_norm_sizes(T, d, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("d", [256, 1001])
+@pytest.mark.parametrize("d", [256, 1001, 1002])
 def test_norm_options_and_strides(d, dtype):
     rng = np.random.default_rng(d)
     T = 9
