@@ -203,7 +203,7 @@ __device__ __forceinline__ void put4(__nv_bfloat16* y, const float (&v)[4]) {
 
 struct GemmArgs {
     fp8::LinearArgs A;
-    int m_tiles, n_tiles, wide;                  // wide: rows of y may be written 16 bytes at a time
+    int m_tiles, n_tiles, wide;                  // wide: bytes of a row of y that may be written at a time, 16, 8, 4 or an element's
 };
 
 // Tiles in bands of BAND along the tokens, so that those worked on at one time share rows of x as much as rows of W.
@@ -215,6 +215,18 @@ __device__ __forceinline__ void place(const GemmArgs& G, int unit, int& mt, int&
     mt = band * BAND + rest - nt * rows;
 }
 
+// 128 bytes of each of a warp's staged rows, a W at a time: 128 / sizeof(W) lanes have a row.  W is the widest that y's base and stride allow (11308 rows of 12262
+// in bf16, K = 240, which begin every 4 bytes: 115 us by words, some 240 by elements; rows of 12264, which go by 16 bytes, 74).
+template <typename W, typename T> __device__ __forceinline__ void copy_rows(T* y, long long stride, const unsigned char* stage, int rows) {
+    constexpr int LANES = 128 / (int)sizeof(W);
+    const int lane = threadIdx.x & 31, at = lane % LANES * (int)sizeof(W);
+#pragma unroll 4
+    for (int r0 = 0; r0 < 32; r0 += 32 / LANES) {
+        const int r = r0 + lane / LANES;
+        const W x = *reinterpret_cast<const W*>(stage + r * OUT_ROW + at);
+        if (r < rows) *reinterpret_cast<W*>(reinterpret_cast<unsigned char*>(y + (long long)r * stride) + at) = x;
+    }
+}
 // A warp's 32 rows (from m0 on) of 128 bytes each (from column n on), which its lanes have by rows, go to memory by lines: a row's 128 bytes are
 // written by eight lanes.  (Written straight from the registers, 16 bytes of 32 rows at a time, a tile took 10000 cycles.)
 template <typename T> __device__ __forceinline__ void write_rows(const GemmArgs& G, unsigned char* stage, int m0, int n, const float2 (&v)[64 / (int)sizeof(T)]) {
@@ -228,18 +240,16 @@ template <typename T> __device__ __forceinline__ void write_rows(const GemmArgs&
         put8(reinterpret_cast<T*>(stage + lane * OUT_ROW) + j, x);
     }
     __syncwarp();
-    if (G.wide && n + N <= G.A.N) {
+    const int rows = min(32, G.A.M - m0);
+    T* y = (T*)G.A.y + (long long)m0 * G.A.y_stride + n;
+    if (G.wide == 16 && n + N <= G.A.N) copy_rows<uint4, T>(y, G.A.y_stride, stage, rows);
+    else if (G.wide >= 8 && n + N <= G.A.N) copy_rows<uint2, T>(y, G.A.y_stride, stage, rows);
+    else if (G.wide >= 4 && n + N <= G.A.N) copy_rows<u32, T>(y, G.A.y_stride, stage, rows);
+    else
+        for (int r = 0; r < rows; ++r)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = 4 * i + (lane >> 3);
-            const uint4 x = *reinterpret_cast<const uint4*>(stage + r * OUT_ROW + (lane & 7) * 16);
-            if (m0 + r < G.A.M) *reinterpret_cast<uint4*>((unsigned char*)((T*)G.A.y + (long long)(m0 + r) * G.A.y_stride + n) + (lane & 7) * 16) = x;
-        }
-    } else {
-        for (int r = 0; r < 32 && m0 + r < G.A.M; ++r)
-            for (int j = lane; j < N && n + j < G.A.N; j += 32)
-                ((T*)G.A.y + (long long)(m0 + r) * G.A.y_stride + n)[j] = reinterpret_cast<const T*>(stage + r * OUT_ROW)[j];
-    }
+            for (int j = lane; j < N; j += 32)
+                if (n + j < G.A.N) y[(long long)r * G.A.y_stride + j] = reinterpret_cast<const T*>(stage + r * OUT_ROW)[j];
     __syncwarp();
 }
 
@@ -471,7 +481,7 @@ __global__ void __launch_bounds__(THREADS, 1) fp8_gemm_kernel(const __grid_const
                 for (int k = 1; k < 8; ++k)
                     if (k < S) { sum[0] += v[k].x; sum[1] += v[k].y; sum[2] += v[k].z; sum[3] += v[k].w; }
                 T* y = (T*)G.A.y + (long long)(mt * BM + r) * G.A.y_stride + n;
-                if (G.wide && n + 4 <= G.A.N) {
+                if (G.wide >= 4 * (int)sizeof(T) && n + 4 <= G.A.N) {
                     put4(y, sum);
                 } else {
 #pragma unroll
@@ -818,7 +828,8 @@ template <typename T, int BN, int CG> int launch(const fp8::LinearArgs& A, int S
         ready = device;
     }
     GemmArgs G = {A, (A.M + CG * BM - 1) / (CG * BM), (A.N + BN - 1) / BN, 0};
-    G.wide = ((uintptr_t)A.y & 15u) == 0 && (A.y_stride * (long long)sizeof(T)) % 16 == 0;
+    const u64 together = (u64)(uintptr_t)A.y | (u64)(A.y_stride * (long long)sizeof(T));
+    G.wide = together % 16 == 0 ? 16 : together % 8 == 0 ? 8 : together % 4 == 0 ? 4 : (int)sizeof(T);
     if ((long long)G.m_tiles * G.n_tiles > 0x3fffffffll) return POP_ERR_UNSUPPORTED;
     const int units = G.m_tiles * G.n_tiles;
     cudaLaunchConfig_t cfg = {};
