@@ -58,79 +58,141 @@ __device__ __forceinline__ void rotate(float& a, float& b, float2 cs) {
 
 // ------------------------------------------------------------------------------------------------------------- alone
 //
-// An item is E pairs of a head: two vectors of E elements, which hold the pairs' first and second elements (halves of the rotated part) or,
-// interleaved, E / 2 whole pairs each; or one vector of the part that is not rotated, where it has to be copied.
-// E = 1 serves any size, stride and alignment.
+// An item is E pairs of a head whose halves are turned: two vectors of E elements, which hold the pairs' first and second elements; or one vector that
+// is not turned, where it has to be copied.  Where neighbours are pairs it is two vectors, as far as the head is turned or has to be copied (two elements for E = 1).
+// E is the largest that sizes, strides and alignment allow: 16, 8, 4 bytes or one element.  Heads of 80, 14534 x 12 of them in bf16, a quarter turned: by neighbours
+// (16 bytes) 18.0 us, by halves (10 pairs: 4 bytes) 42.7, by elements 83.5.  All of 16384 x 40 heads of 128 is bound by memory: 59.8 us, 5.6 TB/s (neighbours 66.1).
 struct Rows {
     const void* in;
     void* out;
     long long in_stride, out_stride;
-    int heads, copy;                             // copy: vectors of a head that are not rotated and go to another place
+    int heads, items, elements;                  // items of a head, and the elements that they are of
 };
 struct RopeArgs {
     Angles A;
     int D, tokens, interleaved;                  // tokens of a CTA
-    Rows x[2];                                   // q, k
+    Rows q, k;
 };
 
-template <typename T, int E> struct Vec { uint4 v; };
-template <typename T> struct Vec<T, 1> { T v; };
+// (as words, so that they are loaded and stored as a whole)
+template <int BYTES> struct Word;
+template <> struct Word<16> { typedef uint4 type; };
+template <> struct Word<8> { typedef uint2 type; };
+template <> struct Word<4> { typedef u32 type; };
+template <> struct Word<2> { typedef unsigned short type; };
+template <typename T, int E> struct Vec { typename Word<sizeof(T) * E>::type w; };
 template <typename T, int E> __device__ __forceinline__ void open(const Vec<T, E>& r, float (&x)[E]) {
-    if constexpr (E == 1) x[0] = Elem<T>::to_f32(r.v);
-    else Elem<T>::unpack(r.v, x);
-}
-__device__ __forceinline__ Vec<float, 4> close(const float (&x)[4]) {
-    return {make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]))};
-}
-__device__ __forceinline__ Vec<__nv_bfloat16, 8> close(const float (&x)[8]) {
-    __nv_bfloat162 r[4];
+    if constexpr (sizeof(T) * E == 2) {
+        x[0] = __uint_as_float((u32)r.w << 16);
+    } else {
+        constexpr int WORDS = sizeof(T) * E / 4;
+        __align__(16) u32 w[WORDS];
+        *reinterpret_cast<typename Word<sizeof(T) * E>::type*>(w) = r.w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-    return {*reinterpret_cast<const uint4*>(r)};
+        for (int i = 0; i < WORDS; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                x[i] = __uint_as_float(w[i]);
+            } else {
+                x[2 * i] = __uint_as_float(w[i] << 16);
+                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            }
+        }
+    }
 }
-template <typename T> __device__ __forceinline__ Vec<T, 1> close1(const float (&x)[1]) { return {Elem<T>::from_f32(x[0])}; }
 template <typename T, int E> __device__ __forceinline__ Vec<T, E> closed(const float (&x)[E]) {
-    if constexpr (E == 1) return close1<T>(x);
-    else return close(x);
+    Vec<T, E> r;
+    if constexpr (sizeof(T) * E == 2) {
+        r.w = __bfloat16_as_ushort(__float2bfloat16_rn(x[0]));
+    } else {
+        constexpr int WORDS = sizeof(T) * E / 4;
+        __align__(16) u32 w[WORDS];
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                w[i] = __float_as_uint(x[i]);
+            } else {
+                const __nv_bfloat162 two = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+                w[i] = *reinterpret_cast<const u32*>(&two);
+            }
+        }
+        r.w = *reinterpret_cast<const typename Word<sizeof(T) * E>::type*>(w);
+    }
+    return r;
 }
 
 template <typename T, int E> __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs R) {
     typedef Vec<T, E> V;
     __shared__ float2 table[TABLE];
     kv::follow();
-    const Rows X = blockIdx.y % 2u ? R.x[1] : R.x[0];
-    const int t0 = blockIdx.x * R.tokens, n = min(R.tokens, R.A.T - t0), pairs = R.A.pairs, parts = gridDim.y / 2u, part = blockIdx.y / 2u;
-    if (X.heads == 0) return;
+    const u32 both = R.k.heads ? 2u : 1u, part = blockIdx.y / both, parts = gridDim.y / both;
+    const Rows X = blockIdx.y % both ? R.k : R.q;
+    const int t0 = blockIdx.x * R.tokens, n = min(R.tokens, R.A.T - t0), pairs = R.A.pairs;
     for (int i = threadIdx.x; i < n * pairs; i += 256) {
         const int p = R.A.positions[t0 + i / pairs];
         if (p >= 0) table[i] = turn(R.A, p, R.A.freq[i % pairs]);
     }
     __syncthreads();
-    const int turned = pairs / E, per_head = turned + X.copy, per_token = X.heads * per_head;
+    const int per_token = X.heads * X.items;
     for (int i = part * 256 + threadIdx.x; i < n * per_token; i += 256 * parts) {
-        const int token = i / per_token, rest = i - token * per_token, head = rest / per_head, c = rest - head * per_head;
+        const int token = i / per_token, rest = i - token * per_token, head = rest / X.items, c = rest - head * X.items;
         if (R.A.positions[t0 + token] < 0) continue;
         const T* from = (const T*)X.in + (long long)(t0 + token) * X.in_stride + (long long)head * R.D;
         T* to = (T*)X.out + (long long)(t0 + token) * X.out_stride + (long long)head * R.D;
+        const float2* cs = table + token * pairs;
+        if (R.interleaved) {
+            if constexpr (E == 1) {
+                float a = Elem<T>::to_f32(from[2 * c]), b = Elem<T>::to_f32(from[2 * c + 1]);
+                if (c < pairs) rotate(a, b, cs[c]);
+                to[2 * c] = Elem<T>::from_f32(a);
+                to[2 * c + 1] = Elem<T>::from_f32(b);
+            } else {
+                V v[2];
+                if ((c + 1) * E <= pairs) {                                         // wholly turned
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) v[h] = *reinterpret_cast<const V*>(from + (2 * c + h) * E);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float x[E];
+                        open(v[h], x);
+#pragma unroll
+                        for (int e = 0; e < E; e += 2) rotate(x[e], x[e + 1], cs[c * E + (h * E + e) / 2]);
+                        *reinterpret_cast<V*>(to + (2 * c + h) * E) = closed<T, E>(x);
+                    }
+                    continue;
+                }
+                const bool two = (2 * c + 2) * E <= X.elements;
+                v[0] = *reinterpret_cast<const V*>(from + 2 * c * E);
+                if (two) v[1] = *reinterpret_cast<const V*>(from + (2 * c + 1) * E);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (h && !two) break;
+                    const int at = (2 * c + h) * E;
+                    if (at < 2 * pairs) {
+                        float x[E];
+                        open(v[h], x);
+#pragma unroll
+                        for (int e = 0; e < E; e += 2)
+                            if (at + e < 2 * pairs) rotate(x[e], x[e + 1], cs[(at + e) / 2]);
+                        v[h] = closed<T, E>(x);
+                    }
+                    *reinterpret_cast<V*>(to + at) = v[h];
+                }
+            }
+            continue;
+        }
+        const int turned = pairs / E;
         if (c >= turned) {
             const int at = 2 * pairs + (c - turned) * E;
             *reinterpret_cast<V*>(to + at) = *reinterpret_cast<const V*>(from + at);
             continue;
         }
-        const int a0 = R.interleaved ? 2 * c * E : c * E, b0 = R.interleaved ? a0 + E : pairs + c * E;
         float a[E], b[E];
-        open(*reinterpret_cast<const V*>(from + a0), a);
-        open(*reinterpret_cast<const V*>(from + b0), b);
-        const float2* cs = table + token * pairs + c * E;
-        if (E > 1 && R.interleaved) {
+        open(*reinterpret_cast<const V*>(from + c * E), a);
+        open(*reinterpret_cast<const V*>(from + pairs + c * E), b);
 #pragma unroll
-            for (int e = 0; e + 1 < E; e += 2) { rotate(a[e], a[e + 1], cs[e / 2]); rotate(b[e], b[e + 1], cs[E / 2 + e / 2]); }
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) rotate(a[e], b[e], cs[e]);
-        }
-        *reinterpret_cast<V*>(to + a0) = closed<T, E>(a);
-        *reinterpret_cast<V*>(to + b0) = closed<T, E>(b);
+        for (int e = 0; e < E; ++e) rotate(a[e], b[e], cs[c * E + e]);
+        *reinterpret_cast<V*>(to + c * E) = closed<T, E>(a);
+        *reinterpret_cast<V*>(to + pairs + c * E) = closed<T, E>(b);
     }
 }
 
@@ -371,20 +433,28 @@ int check_rope(const pop_rope_t* r, int head_dim) {
     return head_dim <= POP_ROPE_MAX_DIM ? POP_OK : POP_ERR_UNSUPPORTED;
 }
 
-template <typename T> cudaError_t rope(RopeArgs R, bool vectors, cudaStream_t st) {
-    const int E = vectors ? 16 / (int)sizeof(T) : 1;
-    long long items = 0;
-    for (int i = 0; i < 2; ++i) {
-        R.x[i].copy = R.x[i].in == R.x[i].out ? 0 : (R.D - 2 * R.A.pairs) / E;
-        const long long n = (long long)R.x[i].heads * (R.A.pairs / E + R.x[i].copy);
-        items = n > items ? n : items;
-    }
+// E: elements of a vector
+template <typename T> cudaError_t rope(RopeArgs R, int E, cudaStream_t st) {
+    auto items_of = [&](Rows& x) {
+        const int rot = 2 * R.A.pairs;
+        x.elements = x.in != x.out ? R.D : R.interleaved ? (rot + E - 1) / E * E : rot;
+        x.items = R.interleaved ? (E == 1 ? x.elements / 2 : (x.elements / E + 1) / 2) : R.A.pairs / E + (x.elements - rot) / E;
+    };
+    items_of(R.q);
+    items_of(R.k);
+    const long long of_q = (long long)R.q.heads * R.q.items, of_k = (long long)R.k.heads * R.k.items, items = of_q > of_k ? of_q : of_k;
+    // tokens that share a CTA's table of angles: as many as it holds, while there are CTAs for all SMs to have several (7157 tokens of three heads: 24 us with
+    // one token to a CTA, 6.6 us so); then CTAs of some four items a thread
     R.tokens = TABLE / R.A.pairs;
-    if (R.tokens > 1 && (R.A.T + R.tokens - 1) / R.tokens < 1024) R.tokens = 1;      // few tokens: a CTA for each
-    while (R.tokens > 1 && items * R.tokens > 1 << 20) R.tokens /= 2;                 // (items of a CTA stay far below 2^31)
-    const long long parts = (items * R.tokens + 1023) / 1024;                         // some four items a thread
-    const dim3 grid((R.A.T + R.tokens - 1) / R.tokens, 2 * (u32)(parts < 1 ? 1 : parts > 16 ? 16 : parts));
-    return vectors ? kv::launch(rope_kernel<T, 16 / (int)sizeof(T)>, grid, 256, st, R) : kv::launch(rope_kernel<T, 1>, grid, 256, st, R);
+    if (R.tokens > R.A.T / 1024) R.tokens = R.A.T / 1024;
+    while (R.tokens > 1 && items * R.tokens > 1 << 20) R.tokens /= 2;        // (items of a CTA stay far below 2^31)
+    if (R.tokens < 1) R.tokens = 1;
+    long long parts = (items * R.tokens + 1023) / 1024;
+    const dim3 grid((R.A.T + R.tokens - 1) / R.tokens, (R.k.heads ? 2 : 1) * (u32)(parts < 1 ? 1 : parts > 64 ? 64 : parts));
+    if (E * sizeof(T) == 16) return kv::launch(rope_kernel<T, 16 / (int)sizeof(T)>, grid, 256, st, R);
+    if (E * sizeof(T) == 8) return kv::launch(rope_kernel<T, 8 / (int)sizeof(T)>, grid, 256, st, R);
+    if (E == 2) return kv::launch(rope_kernel<T, 2>, grid, 256, st, R);
+    return kv::launch(rope_kernel<T, 1>, grid, 256, st, R);
 }
 
 template <typename T, int G> cudaError_t append(const AppendArgs& P, cudaStream_t st) {
@@ -448,15 +518,18 @@ extern "C" int pop_rope(const pop_rope_t* rope_, int inverse, const int32_t* pos
     long long sizes = head_dim | q_stride | q_out_stride;
     if (k) { at |= (uintptr_t)k | (uintptr_t)k_out; sizes |= k_stride | k_out_stride; }
     if (at & (es - 1)) return POP_ERR_INVALID_ARG;
-    const bool vectors = (at & 15u) == 0 && sizes % E == 0 && rope_->rot_dim % (2 * E) == 0;
+    const bool inter = rope_->interleaved != 0;
+    auto fits = [&](int n) { return (at & (uintptr_t)(n * es - 1)) == 0 && sizes % n == 0 && (inter || rope_->rot_dim % (2 * n) == 0); };
+    int n = E;
+    while (n > 1 && !fits(n)) n /= 2;
     RopeArgs R = {};
     R.A = {(const u64*)rope_->freq, positions, n_tokens, rope_->rot_dim / 2, rope_->magnitude, inverse != 0};
     R.D = head_dim;
-    R.interleaved = rope_->interleaved != 0;
-    R.x[0] = {q, q_out, q_stride, q_out_stride, q_heads, 0};
-    if (k) R.x[1] = {k, k_out, k_stride, k_out_stride, k_heads, 0};
+    R.interleaved = inter;
+    R.q = {q, q_out, q_stride, q_out_stride, q_heads, 0, 0};
+    if (k) R.k = {k, k_out, k_stride, k_out_stride, k_heads, 0, 0};
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    POP_CUDA((dtype == POP_BF16 ? rope<__nv_bfloat16>(R, vectors, st) : rope<float>(R, vectors, st)));
+    POP_CUDA((dtype == POP_BF16 ? rope<__nv_bfloat16>(R, n, st) : rope<float>(R, n, st)));
     POP_LAUNCHED();
     return POP_OK;
 }

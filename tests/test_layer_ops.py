@@ -221,9 +221,11 @@ def test_linear_types_strides_and_repeats(M):
         assert torch.all(wide[:, :4] == 7) and torch.all(wide[:, 4 + N:] == 7)
         z = check_linear(M, N, K, BF16, np.random.default_rng(5), x=x, dtype=dtype)
         assert torch.equal(y, z)
-    odd = torch.full((M, 517), 7.0, dtype=BF16, device=DEV)                  # rows that are no multiple of 16 bytes
-    check_linear(M, 516, K, BF16, np.random.default_rng(5), x=x, out=odd[:, 1:])
-    assert torch.all(odd[:, 0] == 7)
+    for pitch, at in ((517, 1), (520, 4), (518, 2), (518, 1)):               # rows that are no multiple of 16 bytes, or begin anywhere
+        for dtype in (BF16, F32):
+            odd = torch.full((M, pitch), 7.0, dtype=dtype, device=DEV)
+            check_linear(M, 516, K, BF16, np.random.default_rng(5), x=x, out=odd[:, at:at + 516])
+            assert torch.all(odd[:, :at] == 7) and torch.all(odd[:, at + 516:] == 7)
 
 
 @pytest.mark.gpu
@@ -294,7 +296,8 @@ def check_equal(got, want32, dtype):
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("T,H,Hk,D,rot", [(1, 32, 32, 128, 128), (13, 8, 2, 64, 64), (5, 3, 1, 80, 20), (300, 6, 2, 96, 24), (2, 1, 1, 2, 2), (7, 5, 3, 130, 66),
-                                          (3, 2, 1, 512, 512), (1500, 4, 1, 128, 64)])
+                                          (3, 2, 1, 512, 512), (1500, 4, 1, 128, 64),
+                                          (5000, 3, 1, 80, 20), (300, 2, 2, 96, 48), (2500, 2, 1, 128, 32), (9, 2, 2, 72, 36)])
 def test_rope_equals_the_oracle(T, H, Hk, D, rot, interleaved, dtype):
     rng = np.random.default_rng(T + D + rot)
     q, k, _, pos = rope_case(rng, T, H, Hk, D, dtype, far=100000 if T < 20 else 0)
