@@ -258,42 +258,62 @@ template <typename T, int G> __global__ void __launch_bounds__(256) rope_append_
 // Many tokens: a CTA has a window of 16 tokens, whose angles it works out once for all heads.  A warp's task is eight tokens of HEADS query
 // heads, or the window's keys (or values) of one head, which go to the cache as whole tiles where they are some (see the kernels of pop_kv_append).
 // Four lanes have a token's head: 8 dimensions of each half of each group, so that a pair is one lane's where 64 or 128 dimensions are rotated, or
-// pairs are neighbours; other calls are left to the kernel above.
-// 16384 tokens of 32 + 8 + 8 heads of 128 in bf16 (373 MB): 73 us, 5.1 TB/s; the queries' part alone 52.
+// pairs are neighbours; where 16 or 32 are, two lanes exchange theirs.  Other calls are left to the kernel above.
+// 16384 tokens of 32 + 8 + 8 heads of 128 in bf16 (373 MB): 73 us, 5.1 TB/s; the queries' part alone 52.  With 32 of the 128 rotated: by halves 70 us
+// (token by token 163), by neighbours 72.
 constexpr int WARPS = 8, WINDOW = 16, HEADS = 2;
 // Elements of a call from which on windows are worth it (bf16, 48 heads of 128, 64 | 256 | 1024 tokens: 3.9 | 6.2 | 9.8 us in windows, 3.2 | 6.3 | 14.4 token by
 // token; 20 heads of 64, 512 | 1024 tokens: 4.5 | 4.9 and 3.9 | 5.6).
 constexpr long long MANY = 1 << 20;
 
+// How pairs lie: 32 or 64 of them by halves, 8 or 16 so, or any number of neighbours.  (A kernel each: in one, the form for few cost the others 2%.)
+enum { HALVES, FEW_HALVES, NEIGHBOURS };
 // Where the angles of a pair stand in a token's row of the table: without bank conflicts for four lanes that each read eight pairs.
-template <bool INTERLEAVED> __device__ __forceinline__ int table_at(int pair) {
-    return INTERLEAVED ? pair : (pair & ~31) + (pair & 6) * 4 + (pair >> 3 & 3) * 2 + (pair & 1);
+template <int FORM> __device__ __forceinline__ int table_at(int pair) {
+    return FORM == NEIGHBOURS ? pair : (pair & ~31) + (pair & 6) * 4 + (pair >> 3 & 3) * 2 + (pair & 1);
 }
-template <int G, bool INTERLEAVED> __device__ __forceinline__ void rotate_pieces(float (&x)[2 * G][8], const float2* cs, int pairs, int e) {
+template <int G, int FORM> __device__ __forceinline__ void rotate_pieces(float (&x)[2 * G][8], const float2* cs, int pairs, int e) {
+    constexpr bool INTERLEAVED = FORM == NEIGHBOURS;
+    if constexpr (FORM == FEW_HALVES) {              // a pair's other element is in the first piece of the lane that is pairs / 8 away
+        const int away = pairs / 8;
+        const bool turned = e < 2 * away, second = (e & away) != 0;
 #pragma unroll
-    for (int p = 0; p < (INTERLEAVED ? 2 * G : G); ++p) {
-        if (!INTERLEAVED && p >= pairs / 32) break;
-        const bool across = !INTERLEAVED && G == 2 && pairs == 64;          // the pair's other element is in the other group, else in the other half
+        for (int j = 0; j < 8; j += 2) {
+            const float4 c = *reinterpret_cast<const float4*>(cs + table_at<FORM>((e & (away - 1)) * 8 + j));
 #pragma unroll
-        for (int j = 0; j < (INTERLEAVED ? 4 : 8); j += 2) {
-            const int pair = INTERLEAVED ? p * 16 + e * 4 + j : p * 32 + e * 8 + j;
-            if (INTERLEAVED && pair >= pairs) break;
-            const float4 c = *reinterpret_cast<const float4*>(cs + table_at<INTERLEAVED>(pair));
-            if (INTERLEAVED) {
-                rotate(x[p][2 * j], x[p][2 * j + 1], make_float2(c.x, c.y));
-                if (pair + 1 < pairs) rotate(x[p][2 * j + 2], x[p][2 * j + 3], make_float2(c.z, c.w));
-            } else if (across) {
-                rotate(x[p][j], x[p + 2 < 2 * G ? p + 2 : 0][j], make_float2(c.x, c.y));
-                rotate(x[p][j + 1], x[p + 2 < 2 * G ? p + 2 : 0][j + 1], make_float2(c.z, c.w));
-            } else {
-                rotate(x[0][j], x[1][j], make_float2(c.x, c.y));
-                rotate(x[0][j + 1], x[1][j + 1], make_float2(c.z, c.w));
+            for (int i = 0; i < 2; ++i) {
+                const float o = __shfl_xor_sync(~0u, x[0][j + i], away);
+                float a = second ? o : x[0][j + i], b = second ? x[0][j + i] : o;
+                rotate(a, b, i ? make_float2(c.z, c.w) : make_float2(c.x, c.y));
+                if (turned) x[0][j + i] = second ? b : a;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int p = 0; p < (INTERLEAVED ? 2 * G : G); ++p) {
+            if (!INTERLEAVED && p >= pairs / 32) break;
+            const bool across = !INTERLEAVED && G == 2 && pairs == 64;          // the pair's other element is in the other group, else in the other half
+#pragma unroll
+            for (int j = 0; j < (INTERLEAVED ? 4 : 8); j += 2) {
+                const int pair = INTERLEAVED ? p * 16 + e * 4 + j : p * 32 + e * 8 + j;
+                if (INTERLEAVED && pair >= pairs) break;
+                const float4 c = *reinterpret_cast<const float4*>(cs + table_at<FORM>(pair));
+                if (INTERLEAVED) {
+                    rotate(x[p][2 * j], x[p][2 * j + 1], make_float2(c.x, c.y));
+                    if (pair + 1 < pairs) rotate(x[p][2 * j + 2], x[p][2 * j + 3], make_float2(c.z, c.w));
+                } else if (across) {
+                    rotate(x[p][j], x[p + 2 < 2 * G ? p + 2 : 0][j], make_float2(c.x, c.y));
+                    rotate(x[p][j + 1], x[p + 2 < 2 * G ? p + 2 : 0][j + 1], make_float2(c.z, c.w));
+                } else {
+                    rotate(x[0][j], x[1][j], make_float2(c.x, c.y));
+                    rotate(x[0][j + 1], x[1][j + 1], make_float2(c.z, c.w));
+                }
             }
         }
     }
 }
 
-template <typename T, int G, bool INTERLEAVED> __global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 2 ? 3 : 2) rope_append_kernel(const AppendArgs P) {
+template <typename T, int G, int FORM> __global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 2 ? 3 : 2) rope_append_kernel(const AppendArgs P) {
     constexpr int D = 64 * G, WORDS = kv::tile_bytes(D) / 4, PIECES = 2 * G;
     __shared__ __align__(16) float2 table[2 * WINDOW][D / 2 + 8];
     __shared__ uint4 codes[WARPS][G * 32];
@@ -316,7 +336,7 @@ template <typename T, int G, bool INTERLEAVED> __global__ void __launch_bounds__
         for (int u = 0; u < AT_ONCE; ++u) {
             const int i = i0 + u * WARPS * 32, t = i / pairs;
             const float2 cs = turn(P.A, p[u], freq[u]);
-            if (i < (WINDOW + first) * pairs) table[t][table_at<INTERLEAVED>(i - t * pairs)] = cs;          // (of no use where p is negative)
+            if (i < (WINDOW + first) * pairs) table[t][table_at<FORM>(i - t * pairs)] = cs;          // (of no use where p is negative)
         }
     }
     __syncthreads();
@@ -338,7 +358,7 @@ template <typename T, int G, bool INTERLEAVED> __global__ void __launch_bounds__
                 float x[PIECES][8];
 #pragma unroll
                 for (int p = 0; p < PIECES; ++p) kv::values_of(raw[h][p], x[p]);
-                rotate_pieces<G, INTERLEAVED>(x, table[row], pairs, e);
+                rotate_pieces<G, FORM>(x, table[row], pairs, e);
                 if (there && h0 + h < P.Hq) {
 #pragma unroll
                     for (int p = 0; p < PIECES; ++p) kv::put8((T*)P.q_out + (long long)t * P.qos + (size_t)(h0 + h) * D + 32 * p + 8 * e, x[p]);
@@ -366,7 +386,7 @@ template <typename T, int G, bool INTERLEAVED> __global__ void __launch_bounds__
             float x[PIECES][8];
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) kv::values_of(raw[i][p], x[p]);
-            if (!value) rotate_pieces<G, INTERLEAVED>(x, table[row], pairs, e);
+            if (!value) rotate_pieces<G, FORM>(x, table[row], pairs, e);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 kv::Raw8<float> r[2];
@@ -459,13 +479,14 @@ template <typename T> cudaError_t rope(RopeArgs R, int E, cudaStream_t st) {
 
 template <typename T, int G> cudaError_t append(const AppendArgs& P, cudaStream_t st) {
     const int rot = 2 * P.A.pairs;
-    if ((long long)P.A.T * (P.Hq + 2 * P.S.H) * (64 * G) >= MANY && (P.interleaved || rot == 64 || rot == 128)) {
+    if ((long long)P.A.T * (P.Hq + 2 * P.S.H) * (64 * G) >= MANY && (P.interleaved || rot == 16 || rot == 32 || rot == 64 || rot == 128)) {
         const int windows = (P.A.T + WINDOW - 1) / WINDOW, tasks = 2 * P.S.H + 2 * ((P.Hq + HEADS - 1) / HEADS);
         int parts = (1024 + windows - 1) / windows;          // some seven CTAs to an SM, as long as each warp has a task
         parts = parts > (tasks + WARPS - 1) / WARPS ? (tasks + WARPS - 1) / WARPS : parts;
         const dim3 grid(windows, parts);
-        if (P.interleaved) rope_append_kernel<T, G, true><<<grid, WARPS * 32, 0, st>>>(P);
-        else rope_append_kernel<T, G, false><<<grid, WARPS * 32, 0, st>>>(P);
+        if (P.interleaved) rope_append_kernel<T, G, NEIGHBOURS><<<grid, WARPS * 32, 0, st>>>(P);
+        else if (rot < 64) rope_append_kernel<T, G, FEW_HALVES><<<grid, WARPS * 32, 0, st>>>(P);
+        else rope_append_kernel<T, G, HALVES><<<grid, WARPS * 32, 0, st>>>(P);
         return cudaGetLastError();
     }
     const int items = (P.Hq + 2 * P.S.H) * 8 * G, parts = P.A.T >= 512 ? 1 : (items + 255) / 256;

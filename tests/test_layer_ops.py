@@ -355,7 +355,8 @@ def cached(pages, slots, dtype=F32):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("D,rot,interleaved", [(64, 64, False), (128, 128, False), (128, 64, False), (128, 128, True), (64, 16, True), (64, 20, False), (128, 48, False)])
+@pytest.mark.parametrize("D,rot,interleaved", [(64, 64, False), (128, 128, False), (128, 64, False), (128, 128, True), (64, 16, True), (64, 20, False), (128, 48, False),
+                                               (128, 32, False), (128, 16, False), (64, 32, False), (64, 16, False)])
 @pytest.mark.parametrize("T,H,Hk,page", [(1, 4, 4, 16), (13, 8, 2, 64), (700, 6, 3, 32), (3000, 4, 2, 64)])
 def test_append_rope_is_rope_then_append(T, H, Hk, page, D, rot, interleaved, dtype):
     """q as pop_rope gives it, and the pages, byte for byte, as pop_kv_append leaves them for keys that pop_rope turned in fp32."""
