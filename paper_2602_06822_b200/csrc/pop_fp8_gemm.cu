@@ -852,27 +852,40 @@ template <typename T, int BN, int CG> int launch(const fp8::LinearArgs& A, int S
 // make it fewer than the SMs' number says (S = 4: 71 and 104, not 74 and 111).  The question is put for a kernel of the same size without tensor memory; for one with
 // it the answer is that of one CTA to an SM, which is not what happens.
 __global__ void __launch_bounds__(FEW_THREADS) few_size_kernel() {}
-int few_clusters(int device, int S, int p, int* clusters) {
-    static int known[64][9][2];
-    int n = device < 64 ? known[device][S][p] : 0;
-    if (!n) {
-        POP_CUDA(cudaFuncSetAttribute(few_size_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM[0] + 256));
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(S * 512);
-        cfg.blockDim = dim3(FEW_THREADS);
-        cfg.dynamicSmemBytes = FEW_SMEM[p] + 256;                            // (and the barriers)
-        cudaLaunchAttribute attr;
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim.x = S;
-        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-        cfg.attrs = &attr;
-        cfg.numAttrs = 1;
-        POP_CUDA(cudaOccupancyMaxActiveClusters(&n, few_size_kernel, &cfg));
-        if (device < 64) known[device][S][p] = n;
-    }
-    *clusters = n;
+__global__ void __launch_bounds__(THREADS) gemm_size_kernel() {}
+int clusters_at_once(void (*kernel)(), int threads, int smem, int S, int* clusters) {
+    POP_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(S * 512);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = S;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    POP_CUDA(cudaOccupancyMaxActiveClusters(clusters, kernel, &cfg));
     return POP_OK;
 }
+int few_clusters(int device, int S, int p, int* clusters) {
+    static int known[64][9][2];
+    *clusters = device < 64 ? known[device][S][p] : 0;
+    if (*clusters) return POP_OK;
+    const int rc = clusters_at_once(few_size_kernel, FEW_THREADS, FEW_SMEM[p] + 256, S, clusters);           // (and the barriers)
+    if (rc == POP_OK && device < 64) known[device][S][p] = *clusters;
+    return rc;
+}
+// The same for tiles of 128 x 128, one CTA to an SM.
+int gemm_clusters(int device, int S, int* clusters) {
+    static int known[64][9];
+    *clusters = device < 64 ? known[device][S] : 0;
+    if (*clusters) return POP_OK;
+    const int rc = clusters_at_once(gemm_size_kernel, THREADS, Tile<128, 1>::SMEM, S, clusters);
+    if (rc == POP_OK && device < 64) known[device][S] = *clusters;
+    return rc;
+}
+
 // How many CTAs share a tile of 128 rows of W: as many as can all run at one time, which splits the work finest; with fewer to an SM, and more stages each, if
 // there is a choice.  (One token, 12288 x 4096, 96 tiles, S = 2 | 3 | 4 with three to an SM: 14.3 | 11.7 | 10.7 us; 8, which takes two rounds: 15.8; 3 with two
 // to an SM, 93 clusters of the 96 at a time: 15.6.  1024 x 4096, S = 2 | 4 | 8 with two: 7.6 | 5.2 | 4.6.)  Tiles for more than one round are shared by as
@@ -930,11 +943,27 @@ template <typename X, typename Y, int TN> int launch_few(const FewArgs& F, cudaS
     return POP_OK;
 }
 
+// Pairs, tiles alone or tiles that S CTAs share: what is the quickest by these estimates (us, fitted to 28 sizes of 76 to 14846 tokens; a CTA's start and its first
+// stages, then for each tile its epilogue and its blocks of 128; a join costs 3 us, so that less than some 14 blocks are not worth one).  Rows of codes that do not
+// begin on sectors of 32 bytes come slower.  Codes given, measured on both sides of the choice: 1024 x 4096 x 4096 pairs 18.0, alone 23.2; 512 x 4096 x 4096 alone 13.4,
+// pairs 17.1; 1024 x 1024 x 1024 alone 6.0, pairs 7.2, S = 2 7.7; 1055 x 163 x 9856 S = 6 10.2, alone 24.5, S = 8, of which not all run at one time, 17.8.
 template <typename T> int choose(const fp8::LinearArgs& A, int sms, cudaStream_t st) {
-    const long long m_tiles = (A.M + BM - 1) / BM, tiles = m_tiles * ((A.N + 127) / 128);
-    if (A.M > BM && tiles >= 2 * sms) return launch<T, 256, 2>(A, 1, sms, st);
-    int S = 1;                                   // CTAs to a tile: as many as fill the machine, each with two blocks at least
-    while (S < 8 && tiles * (2 * S) <= sms && A.KB >= 4 * S) S *= 2;
+    auto tiles_of = [&](int rows, int columns) { return (long long)((A.M + rows - 1) / rows) * ((A.N + columns - 1) / columns); };
+    const long long tiles = tiles_of(BM, 128), pairs = tiles_of(2 * BM, 256);
+    const float block = A.K % 32 ? 0.42f : 0.30f;
+    const float paired = 1.4f + (float)((pairs + sms / 2 - 1) / (sms / 2)) * (2.4f + 0.43f * A.KB);
+    float best = 2.1f + (float)((tiles + sms - 1) / sms) * (1.4f + block * A.KB);
+    int S = 1, device = 0;
+    POP_CUDA(cudaGetDevice(&device));
+    for (int s = 2; s <= 8 && tiles * s <= sms && A.KB >= 2 * s; ++s) {
+        const float t = 6.5f + block * ((A.KB + s - 1) / s);
+        if (t >= best) continue;
+        int at_once = 0;
+        const int rc = gemm_clusters(device, s, &at_once);
+        if (rc != POP_OK) return rc;
+        if (tiles <= at_once) { best = t; S = s; }
+    }
+    if (paired < best) return launch<T, 256, 2>(A, 1, sms, st);
     return launch<T, 128, 1>(A, S, sms, st);
 }
 
