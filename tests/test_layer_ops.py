@@ -204,6 +204,7 @@ def check_linear(M, N, K, x_dtype, rng, x=None, **kw):
     (1, 1, 16), (1, 4096, 4096), (2, 17, 128), (8, 129, 1360), (9, 300, 256), (16, 1000, 4112), (17, 64, 144), (17, 1000, 4096), (31, 129, 11008),
     (64, 4096, 512), (100, 250, 2000), (127, 128, 128), (128, 256, 1024), (129, 257, 1040), (333, 1000, 1360), (1000, 4100, 528), (600, 12000, 272),
     (100, 64, 16), (300, 300, 16), (38000, 100, 144), (33, 40000, 128), (2, 60000, 256), (16, 64, 37904), (5, 64, 36864),
+    (640, 1024, 4096), (1055, 163, 2560), (1055, 163, 9856), (130, 500, 3584), (130, 300, 2992), (300, 7000, 384),      # 3, 5, 6, 7, 8 CTAs to a tile; pairs, few tiles
 ])
 def test_linear_sizes(M, N, K, dtype):
     check_linear(M, N, K, dtype, np.random.default_rng(M * 31 + N * 7 + K))
